@@ -40,7 +40,8 @@ extern "C" {
 #define CPRUNE_ERR_NOT_TUNED (-5)   /* reserved */
 
 typedef enum { CPRUNE_F32 = 0, CPRUNE_F16 = 1, CPRUNE_BF16 = 2 } cprune_dtype;
-typedef enum { CPRUNE_ACT_NONE = 0, CPRUNE_ACT_RELU = 1, CPRUNE_ACT_RELU6 = 2 } cprune_act;
+/* CPRUNE_ACT_SILU, z / (1 + exp(-z)): the group norm and the 4-bit products; the convolutions refuse it */
+typedef enum { CPRUNE_ACT_NONE = 0, CPRUNE_ACT_RELU = 1, CPRUNE_ACT_RELU6 = 2, CPRUNE_ACT_SILU = 3 } cprune_act;
 
 const char* cprune_status_string(int status); /* host string, never NULL */
 int cprune_last_hip_error(void);              /* hipError_t of the last CPRUNE_ERR_DEVICE */
@@ -491,6 +492,74 @@ int cprune_search_log_size(const cprune_search* s);
 int cprune_search_log_entry(const cprune_search* s, int index, int64_t* task_out, double* l_m_out,
                             double* l_t_out, double* a_s_out, int* verdict_out);
 int cprune_search_destroy(cprune_search* s);
+
+/* ------------------------------------------------------------------------
+ * Group norm with an activation, channels last, and its gradient: the normalisation of a
+ * network that is tuned between pruning steps on batches too small for batch statistics.
+ *
+ * x [n][pixels][c], pixel i of an image x_stride elements behind pixel i - 1 (x_stride >= c, images n * pixels apart:
+ * a dense tensor has x_stride = c, the first channels of a wider map have that map's c).  Over the pixels and the
+ * c / groups channels of each (image, group):
+ *   mean = sum x / m, var = sum (x - mean)^2 / m, rstd = 1 / sqrt(var + eps), m = pixels * c / groups
+ *   y = act((x - mean) * rstd * weight_c + bias_c)
+ * Statistics and sums are held in 32 bits or more whatever the type; y is rounded once.  An infinity or NaN in x spreads
+ * over its own (image, group); ReLU and ReLU6 pass a NaN on.
+ *
+ * Backward, with z the activation's argument and dz = dy * act'(z) (0 at both ends of a clamp):
+ *   dbias_c = sum dz, dweight_c = sum dz * xhat   over images and pixels
+ *   dx = rstd * (weight_c dz - mean(weight dz) - xhat * mean(weight dz xhat)),   means over the (image, group)
+ *
+ * weight, bias   fp32 [c]; NULL = ones / zeros
+ * y, dx          dense [n][pixels][c], the type of x; they overlap no input
+ * mean, rstd     fp32 [n][groups]; mean_out / rstd_out may be NULL
+ * dy             as x, with dy_stride
+ * dweight, dbias fp32 [c], each may be NULL.  Summed in a fixed order: repeated calls give identical bits.
+ * n, pixels >= 1; groups divides c; eps > 0 and finite.  n * groups of 2^24 and more: CPRUNE_ERR_UNSUPPORTED. */
+typedef struct {
+  int32_t n, pixels, c, groups;
+  int32_t dtype; /* cprune_dtype of x, y, dy, dx */
+  int32_t act;   /* cprune_act */
+  int32_t x_stride, dy_stride; /* dy_stride: backward only */
+  float eps;     /* forward only */
+} cprune_norm_desc;
+size_t cprune_group_norm_workspace_bytes(const cprune_norm_desc* d, int backward);
+int cprune_group_norm_act(const cprune_norm_desc* d, const void* x, const float* weight, const float* bias, void* y,
+                          float* mean_out, float* rstd_out, void* ws, size_t ws_bytes, void* stream);
+int cprune_group_norm_act_backward(const cprune_norm_desc* d, const void* dy, const void* x, const float* mean,
+                                   const float* rstd, const float* weight, const float* bias, void* dx, float* dweight,
+                                   float* dbias, void* ws, size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
+ * Microscaled 4-bit numbers and products on them: a 1x1 convolution on channels-last pixels or a fully connected layer
+ * whose weights are stored, and multiplied, in 4 bits (the matrix instructions take them as they are).
+ *
+ * A row of k numbers is ceil(k / 32) blocks of 32, the last one filled up with zeros.  A block is one scale byte s, standing for
+ * 2^(s - 127), and 16 bytes of codes: element 2 i in the low half of byte i, element 2 i + 1 in the high half, each a
+ * sign (8) and an index (0..7) into 0, 0.5, 1, 1.5, 2, 3, 4, 6.
+ *   s = max(0, floor(log2(largest magnitude)) + 125), 0 for a block of zeros
+ *   code = x / 2^(s - 127) rounded to the nearest, ties to the even index, magnitudes past 6 to 6
+ * A block that holds an infinity or NaN gets s = 255 and codes 0: all its numbers stand for NaN.
+ *
+ * codes   uint8 [rows][ceil(k / 32) * 16], 16-byte aligned
+ * scales  uint8 [rows][ceil(k / 32)]
+ * x       [rows][k] of dtype, rows x_stride elements apart (x_stride >= k)
+ * y       dense [rows][k] of dtype (dequantize), [rows][c_out] (products)
+ *
+ * Products: y[r][o] = act(sum over k of x_r * w_o + bias_o), summed in fp32, rounded once.  cprune_mx4_matmul takes x as codes;
+ * cprune_mx4_linear takes numbers, makes their codes within the call (the same as cprune_mx4_quantize would) and multiplies those.
+ * bias    fp32 [c_out] or NULL
+ * ws      cprune_mx4_linear_workspace_bytes(...) of scratch, 16-byte aligned; cprune_mx4_matmul needs none */
+int cprune_mx4_quantize(const void* x, int rows, int k, int x_stride, cprune_dtype dtype, void* codes, void* scales,
+                        void* stream);
+int cprune_mx4_dequantize(const void* codes, const void* scales, int rows, int k, cprune_dtype dtype, void* y,
+                          void* stream);
+int cprune_mx4_matmul(const void* x_codes, const void* x_scales, int rows, int k, const void* w_codes,
+                      const void* w_scales, int c_out, const float* bias, cprune_act act, cprune_dtype dtype, void* y,
+                      void* stream);
+size_t cprune_mx4_linear_workspace_bytes(int rows, int k, int c_out, cprune_dtype dtype);
+int cprune_mx4_linear(const void* x, int rows, int k, int x_stride, const void* w_codes, const void* w_scales, int c_out,
+                      const float* bias, cprune_act act, cprune_dtype dtype, void* y, void* ws, size_t ws_bytes,
+                      void* stream);
 
 /* ---- measured ceilings (for reporting kernel throughput against what the device
  * delivers, next to its datasheet peaks; the paper reports end-to-end rates only) ----

@@ -7,6 +7,7 @@ fallback: a missing library raises.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 from typing import Optional, Tuple
 
@@ -15,7 +16,7 @@ import torch
 from . import build as _build
 
 F32, F16, BF16 = 0, 1, 2
-ACT_NONE, ACT_RELU, ACT_RELU6 = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_RELU6, ACT_SILU = 0, 1, 2, 3     # (SILU: group norm and 4-bit products)
 LAYER_CONV, LAYER_MAXPOOL, LAYER_GAVGPOOL, LAYER_FC = 0, 1, 2, 3
 
 OK = 0
@@ -45,6 +46,10 @@ class PruneLayer(C.Structure):
                                           "kept_out")]
 
 
+class NormDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n", "pixels", "c", "groups", "dtype", "act", "x_stride", "dy_stride")] + [("eps", C.c_float)]
+
+
 EXPORTS = [
     "cprune_status_string", "cprune_last_hip_error",
     "cprune_rank_filters_workspace_bytes", "cprune_rank_filters", "cprune_rank_filter_group",
@@ -71,6 +76,9 @@ EXPORTS = [
     "cprune_search_create", "cprune_search_start", "cprune_search_next_task",
     "cprune_search_report_exhausted", "cprune_search_report_latency", "cprune_search_report_accuracy",
     "cprune_search_log_size", "cprune_search_log_entry", "cprune_search_destroy",
+    "cprune_group_norm_workspace_bytes", "cprune_group_norm_act", "cprune_group_norm_act_backward",
+    "cprune_mx4_quantize", "cprune_mx4_dequantize", "cprune_mx4_matmul",
+    "cprune_mx4_linear_workspace_bytes", "cprune_mx4_linear",
 ]
 
 _lib = None
@@ -103,6 +111,16 @@ def lib():
         L.cprune_cached_tile.argtypes = [C.POINTER(ConvDesc), C.POINTER(C.c_int), C.POINTER(C.c_int)]
         L.cprune_conv_workspace_bytes.argtypes = [C.POINTER(ConvDesc), C.c_int]
         L.cprune_conv2d_bn_relu.argtypes = [C.POINTER(ConvDesc)] + [C.c_void_p] * 5 + [C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.cprune_group_norm_workspace_bytes.restype = L.cprune_mx4_linear_workspace_bytes.restype = C.c_size_t
+        L.cprune_group_norm_workspace_bytes.argtypes = [C.POINTER(NormDesc), C.c_int]
+        L.cprune_group_norm_act.argtypes = [C.POINTER(NormDesc)] + [C.c_void_p] * 7 + [C.c_size_t, C.c_void_p]
+        L.cprune_group_norm_act_backward.argtypes = [C.POINTER(NormDesc)] + [C.c_void_p] * 10 + [C.c_size_t, C.c_void_p]
+        L.cprune_mx4_quantize.argtypes = [C.c_void_p] + [C.c_int] * 4 + [C.c_void_p] * 3
+        L.cprune_mx4_dequantize.argtypes = [C.c_void_p] * 2 + [C.c_int] * 3 + [C.c_void_p] * 2
+        L.cprune_mx4_matmul.argtypes = [C.c_void_p] * 2 + [C.c_int] * 2 + [C.c_void_p] * 2 + [C.c_int, C.c_void_p, C.c_int, C.c_int] + [C.c_void_p] * 2
+        L.cprune_mx4_linear_workspace_bytes.argtypes = [C.c_int] * 4
+        L.cprune_mx4_linear.argtypes = [C.c_void_p] + [C.c_int] * 3 + [C.c_void_p] * 2 + [C.c_int, C.c_void_p, C.c_int, C.c_int] + \
+            [C.c_void_p] * 2 + [C.c_size_t, C.c_void_p]
         _lib = L
     return _lib
 
@@ -451,6 +469,171 @@ def cprune_fc(x, w, bias=None, act=ACT_NONE, stream=None):
                          C.c_int(act), C.c_int(dt), _ptr(y), _ptr(ws), C.c_size_t(_size(ws)),
                          _stream(stream))
     _check(st, "cprune_fc")
+    return y
+
+
+# ---- group norm, channels last ---------------------------------------------------
+
+def _expect(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _rows_of(x: torch.Tensor, image_dims: int):
+    """(product of the first `image_dims` sizes, product of those between, channels, elements between pixels) of a channels-last tensor whose
+    pixels lie evenly: dense, or the first channels of a wider dense tensor."""
+    shape = x.shape
+    c = shape[-1]
+    lead = math.prod(shape[:image_dims])
+    pixels = math.prod(shape[image_dims:-1])
+    if x.is_contiguous():
+        return lead, pixels, c, c
+    _expect(c == 1 or x.stride(-1) == 1, "channels must lie next to each other")
+    pitch, span = None, 1
+    for size, stride in zip(reversed(shape[:-1]), reversed(x.stride()[:-1])):
+        if size != 1:
+            if pitch is None:
+                pitch, rest = divmod(stride, span)
+                _expect(rest == 0, "pixels must lie evenly")
+            _expect(stride == pitch * span, "pixels must lie evenly")
+        span *= size
+    pitch = c if pitch is None else pitch
+    _expect(pitch >= c, "pixels must not overlap")
+    return lead, pixels, c, pitch
+
+
+def _on_gpu(x: torch.Tensor, dtype=None, shape=None) -> int:
+    """Address of a dense device tensor of a type and shape."""
+    _expect(x.is_cuda and x.is_contiguous(), "device-resident contiguous tensors only")
+    _expect(dtype is None or x.dtype == dtype, f"expected {dtype}, got {x.dtype}")
+    _expect(shape is None or tuple(x.shape) == shape, f"expected shape {shape}, got {tuple(x.shape)}")
+    return x.data_ptr()
+
+
+def _vector(x: Optional[torch.Tensor], c: int):
+    return None if x is None else _on_gpu(x, torch.float32, (c,))
+
+
+def _used_on(stream, *tensors) -> None:
+    """Memory taken from torch's current stream is not handed out again before work on `stream` is done with it."""
+    if stream is not None:
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
+
+
+def _norm_desc(x: torch.Tensor, groups: int, act: int, eps: float):
+    _expect(x.is_cuda and x.dim() >= 2, "a channels-last device tensor [n, ..., c]")
+    _expect(x.dtype in DTYPE_OF_TORCH, f"no {x.dtype}")
+    n, pixels, c, pitch = _rows_of(x, 1)
+    return NormDesc(n, pixels, c, groups, DTYPE_OF_TORCH[x.dtype], act, pitch, c, eps)
+
+
+def cprune_group_norm_act(x: torch.Tensor, groups: int, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
+                          eps: float = 1e-5, act: int = ACT_NONE, want_stats: bool = False, stream=None):
+    """x [n, ..., c], channels last (dense, or the first channels of a wider map); weight, bias fp32 [c].
+    -> y dense, or (y, mean [n, groups], rstd [n, groups]) for the backward call."""
+    L = _lib or lib()
+    d = _norm_desc(x, groups, act, eps)
+    y = x.new_empty(x.shape)
+    mean = rstd = None
+    if want_stats:
+        mean, rstd = x.new_empty((2, d.n, max(groups, 0)), dtype=torch.float32).unbind()
+    ws = _ws(L.cprune_group_norm_workspace_bytes(d, 0), x.device)
+    st = L.cprune_group_norm_act(d, x.data_ptr(), _vector(weight, d.c), _vector(bias, d.c), y.data_ptr(), _addr(mean), _addr(rstd),
+                                 _addr(ws), _size(ws), _raw_stream(stream))
+    _check(st, "cprune_group_norm_act")
+    _used_on(stream, y, mean, rstd, ws)
+    return (y, mean, rstd) if want_stats else y
+
+
+def cprune_group_norm_act_backward(dy: torch.Tensor, x: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor, groups: int,
+                                   weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, act: int = ACT_NONE,
+                                   want_vectors: bool = True, stream=None):
+    """The gradient of cprune_group_norm_act at x: -> (dx dense, dweight fp32 [c], dbias fp32 [c]); the latter None without want_vectors."""
+    L = _lib or lib()
+    d = _norm_desc(x, groups, act, 0.0)
+    _expect(dy.is_cuda and dy.shape == x.shape and dy.dtype == x.dtype, "dy must be like x")
+    d.dy_stride = _rows_of(dy, 1)[3]
+    stats = (d.n, groups)
+    dx = x.new_empty(x.shape)
+    dweight = dbias = None
+    if want_vectors:
+        dweight, dbias = x.new_empty((2, d.c), dtype=torch.float32).unbind()
+    ws = _ws(L.cprune_group_norm_workspace_bytes(d, 1), x.device)
+    st = L.cprune_group_norm_act_backward(d, dy.data_ptr(), x.data_ptr(), _on_gpu(mean, torch.float32, stats),
+                                          _on_gpu(rstd, torch.float32, stats), _vector(weight, d.c), _vector(bias, d.c), dx.data_ptr(),
+                                          _addr(dweight), _addr(dbias), _addr(ws), _size(ws), _raw_stream(stream))
+    _check(st, "cprune_group_norm_act_backward")
+    _used_on(stream, dx, dweight, dbias, ws)
+    return dx, dweight, dbias
+
+
+# ---- microscaled 4-bit numbers ---------------------------------------------------
+
+def _mx4_rows(x: torch.Tensor):
+    _expect(x.is_cuda and x.dim() >= 1, "a device tensor [..., k]")
+    _expect(x.dtype in DTYPE_OF_TORCH, f"no {x.dtype}")
+    _, rows, k, pitch = _rows_of(x, 0)
+    return rows, k, pitch, DTYPE_OF_TORCH[x.dtype]
+
+
+def _mx4_pair(codes: torch.Tensor, scales: torch.Tensor, k: Optional[int]):
+    """Addresses of codes and scales, and their rows and blocks."""
+    _expect(codes.dim() == 2 and scales.dim() == 2, "codes [rows, blocks * 16], scales [rows, blocks]")
+    rows, blocks = scales.shape
+    if k is not None:
+        _expect(blocks == (k + 31) // 32, f"{blocks} blocks do not hold {k} numbers a row")
+    return _on_gpu(codes, torch.uint8, (rows, 16 * blocks)), _on_gpu(scales, torch.uint8), rows, blocks
+
+
+def cprune_mx4_quantize(x: torch.Tensor, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """x [..., k] -> (codes uint8 [rows, ceil(k / 32) * 16], scales uint8 [rows, ceil(k / 32)])."""
+    rows, k, pitch, dtype = _mx4_rows(x)
+    blocks = (k + 31) // 32
+    codes = x.new_empty((rows, 16 * blocks), dtype=torch.uint8)
+    scales = x.new_empty((rows, blocks), dtype=torch.uint8)
+    st = (_lib or lib()).cprune_mx4_quantize(x.data_ptr(), rows, k, pitch, dtype, codes.data_ptr(), scales.data_ptr(), _raw_stream(stream))
+    _check(st, "cprune_mx4_quantize")
+    _used_on(stream, codes, scales)
+    return codes, scales
+
+
+def cprune_mx4_dequantize(codes: torch.Tensor, scales: torch.Tensor, k: int, dtype: int = F32, stream=None) -> torch.Tensor:
+    """-> [rows, k], the numbers that the codes stand for."""
+    ca, sa, rows, _ = _mx4_pair(codes, scales, k)
+    y = codes.new_empty((rows, k), dtype=TORCH_DTYPE[dtype])
+    st = (_lib or lib()).cprune_mx4_dequantize(ca, sa, rows, k, dtype, y.data_ptr(), _raw_stream(stream))
+    _check(st, "cprune_mx4_dequantize")
+    _used_on(stream, y)
+    return y
+
+
+def cprune_mx4_matmul(x_codes: torch.Tensor, x_scales: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tensor, dtype: int,
+                      bias: Optional[torch.Tensor] = None, act: int = ACT_NONE, stream=None) -> torch.Tensor:
+    """Both operands as codes (rows filled up with zeros past k): -> y [rows, c_out] of dtype."""
+    xa, xs, rows, blocks = _mx4_pair(x_codes, x_scales, None)
+    wa, wsc, c_out, _ = _mx4_pair(w_codes, w_scales, 32 * blocks)
+    y = x_codes.new_empty((rows, c_out), dtype=TORCH_DTYPE[dtype])
+    st = (_lib or lib()).cprune_mx4_matmul(xa, xs, rows, 32 * blocks, wa, wsc, c_out, _vector(bias, c_out), act, dtype, y.data_ptr(),
+                                           _raw_stream(stream))
+    _check(st, "cprune_mx4_matmul")
+    _used_on(stream, y)
+    return y
+
+
+def cprune_mx4_linear(x: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tensor, bias: Optional[torch.Tensor] = None,
+                      act: int = ACT_NONE, stream=None) -> torch.Tensor:
+    """x [..., k] in numbers, w as codes: -> y [..., c_out], the type of x."""
+    L = _lib or lib()
+    rows, k, pitch, dtype = _mx4_rows(x)
+    wa, wsc, c_out, _ = _mx4_pair(w_codes, w_scales, k)
+    y = x.new_empty(x.shape[:-1] + (c_out,))
+    ws = _ws(L.cprune_mx4_linear_workspace_bytes(rows, k, c_out, dtype), x.device)
+    st = L.cprune_mx4_linear(x.data_ptr(), rows, k, pitch, wa, wsc, c_out, _vector(bias, c_out), act, dtype, y.data_ptr(), _addr(ws),
+                             _size(ws), _raw_stream(stream))
+    _check(st, "cprune_mx4_linear")
+    _used_on(stream, y, ws)
     return y
 
 
