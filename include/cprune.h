@@ -548,14 +548,15 @@ int cprune_group_norm_act_backward(const cprune_norm_desc* d, const void* dy, co
  * Products: y[r][o] = act(sum over k of x_r * w_o + bias_o), summed in fp32, rounded once.  cprune_mx4_matmul takes x as codes;
  * cprune_mx4_linear takes numbers, makes their codes within the call (the same as cprune_mx4_quantize would) and multiplies those.
  * bias    fp32 [c_out] or NULL
- * ws      cprune_mx4_linear_workspace_bytes(...) of scratch, 16-byte aligned; cprune_mx4_matmul needs none */
+ * ws      cprune_mx4_{matmul,linear}_workspace_bytes(...) of scratch, 16-byte aligned; NULL where that is 0 */
 int cprune_mx4_quantize(const void* x, int rows, int k, int x_stride, cprune_dtype dtype, void* codes, void* scales,
                         void* stream);
 int cprune_mx4_dequantize(const void* codes, const void* scales, int rows, int k, cprune_dtype dtype, void* y,
                           void* stream);
+size_t cprune_mx4_matmul_workspace_bytes(int rows, int k, int c_out);
 int cprune_mx4_matmul(const void* x_codes, const void* x_scales, int rows, int k, const void* w_codes,
                       const void* w_scales, int c_out, const float* bias, cprune_act act, cprune_dtype dtype, void* y,
-                      void* stream);
+                      void* ws, size_t ws_bytes, void* stream);
 size_t cprune_mx4_linear_workspace_bytes(int rows, int k, int c_out, cprune_dtype dtype);
 int cprune_mx4_linear(const void* x, int rows, int k, int x_stride, const void* w_codes, const void* w_scales, int c_out,
                       const float* bias, cprune_act act, cprune_dtype dtype, void* y, void* ws, size_t ws_bytes,

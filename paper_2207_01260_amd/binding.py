@@ -77,7 +77,7 @@ EXPORTS = [
     "cprune_search_report_exhausted", "cprune_search_report_latency", "cprune_search_report_accuracy",
     "cprune_search_log_size", "cprune_search_log_entry", "cprune_search_destroy",
     "cprune_group_norm_workspace_bytes", "cprune_group_norm_act", "cprune_group_norm_act_backward",
-    "cprune_mx4_quantize", "cprune_mx4_dequantize", "cprune_mx4_matmul",
+    "cprune_mx4_quantize", "cprune_mx4_dequantize", "cprune_mx4_matmul_workspace_bytes", "cprune_mx4_matmul",
     "cprune_mx4_linear_workspace_bytes", "cprune_mx4_linear",
 ]
 
@@ -111,13 +111,16 @@ def lib():
         L.cprune_cached_tile.argtypes = [C.POINTER(ConvDesc), C.POINTER(C.c_int), C.POINTER(C.c_int)]
         L.cprune_conv_workspace_bytes.argtypes = [C.POINTER(ConvDesc), C.c_int]
         L.cprune_conv2d_bn_relu.argtypes = [C.POINTER(ConvDesc)] + [C.c_void_p] * 5 + [C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]
-        L.cprune_group_norm_workspace_bytes.restype = L.cprune_mx4_linear_workspace_bytes.restype = C.c_size_t
+        for name in ("cprune_group_norm_workspace_bytes", "cprune_mx4_matmul_workspace_bytes", "cprune_mx4_linear_workspace_bytes"):
+            getattr(L, name).restype = C.c_size_t
         L.cprune_group_norm_workspace_bytes.argtypes = [C.POINTER(NormDesc), C.c_int]
         L.cprune_group_norm_act.argtypes = [C.POINTER(NormDesc)] + [C.c_void_p] * 7 + [C.c_size_t, C.c_void_p]
         L.cprune_group_norm_act_backward.argtypes = [C.POINTER(NormDesc)] + [C.c_void_p] * 10 + [C.c_size_t, C.c_void_p]
         L.cprune_mx4_quantize.argtypes = [C.c_void_p] + [C.c_int] * 4 + [C.c_void_p] * 3
         L.cprune_mx4_dequantize.argtypes = [C.c_void_p] * 2 + [C.c_int] * 3 + [C.c_void_p] * 2
-        L.cprune_mx4_matmul.argtypes = [C.c_void_p] * 2 + [C.c_int] * 2 + [C.c_void_p] * 2 + [C.c_int, C.c_void_p, C.c_int, C.c_int] + [C.c_void_p] * 2
+        L.cprune_mx4_matmul.argtypes = [C.c_void_p] * 2 + [C.c_int] * 2 + [C.c_void_p] * 2 + [C.c_int, C.c_void_p, C.c_int, C.c_int] + \
+            [C.c_void_p] * 2 + [C.c_size_t, C.c_void_p]
+        L.cprune_mx4_matmul_workspace_bytes.argtypes = [C.c_int] * 3
         L.cprune_mx4_linear_workspace_bytes.argtypes = [C.c_int] * 4
         L.cprune_mx4_linear.argtypes = [C.c_void_p] + [C.c_int] * 3 + [C.c_void_p] * 2 + [C.c_int, C.c_void_p, C.c_int, C.c_int] + \
             [C.c_void_p] * 2 + [C.c_size_t, C.c_void_p]
@@ -612,13 +615,15 @@ def cprune_mx4_dequantize(codes: torch.Tensor, scales: torch.Tensor, k: int, dty
 def cprune_mx4_matmul(x_codes: torch.Tensor, x_scales: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tensor, dtype: int,
                       bias: Optional[torch.Tensor] = None, act: int = ACT_NONE, stream=None) -> torch.Tensor:
     """Both operands as codes (rows filled up with zeros past k): -> y [rows, c_out] of dtype."""
+    L = _lib or lib()
     xa, xs, rows, blocks = _mx4_pair(x_codes, x_scales, None)
     wa, wsc, c_out, _ = _mx4_pair(w_codes, w_scales, 32 * blocks)
     y = x_codes.new_empty((rows, c_out), dtype=TORCH_DTYPE[dtype])
-    st = (_lib or lib()).cprune_mx4_matmul(xa, xs, rows, 32 * blocks, wa, wsc, c_out, _vector(bias, c_out), act, dtype, y.data_ptr(),
-                                           _raw_stream(stream))
+    ws = _ws(L.cprune_mx4_matmul_workspace_bytes(rows, 32 * blocks, c_out), y.device)
+    st = L.cprune_mx4_matmul(xa, xs, rows, 32 * blocks, wa, wsc, c_out, _vector(bias, c_out), act, dtype, y.data_ptr(), _addr(ws), _size(ws),
+                             _raw_stream(stream))
     _check(st, "cprune_mx4_matmul")
-    _used_on(stream, y)
+    _used_on(stream, y, ws)
     return y
 
 

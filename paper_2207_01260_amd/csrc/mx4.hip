@@ -24,15 +24,9 @@ __device__ __forceinline__ float scale_value(int s) {      // 2^(s - 127), NaN f
   return __uint_as_float(s == 255 ? 0x7fc00000u : s == 0 ? 0x00400000u : (unsigned)s << 23);
 }
 
-template <typename T>
-__global__ __launch_bounds__(kQuad) void mx4_quantize_kernel(const T* __restrict__ x, int rows, int k, long x_stride, int blocks,
-                                                             unsigned* __restrict__ codes, unsigned char* __restrict__ scales) {
+// Codes and scale of eight numbers at p, of which `valid` are there; the four lanes of a quad hold a block.
+template <typename T> __device__ __forceinline__ unsigned quantize8(const T* p, int valid, int& s) {
   constexpr int V = 16 / (int)sizeof(T);
-  const unsigned i = blockIdx.x * (unsigned)kQuad + threadIdx.x, per = 4u * blocks;
-  if (i >= (unsigned)rows * per) return;      // (whole quads)
-  const unsigned row = i / per, at = (i - row * per) * 8;
-  const T* p = x + row * x_stride + at;
-  const int valid = k - (int)at;
   float v[8];
 #pragma unroll
   for (int h = 0; h < 8; h += V) {
@@ -48,15 +42,76 @@ __global__ __launch_bounds__(kQuad) void mx4_quantize_kernel(const T* __restrict
   unsigned top = 0;
 #pragma unroll
   for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
-  const int s = scale_byte(quad_max(top));
+  s = scale_byte(quad_max(top));
   const float f = scale_value(s);
   unsigned c = 0;
   c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[0], v[1], f, 0);
   c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2], v[3], f, 1);
   c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4], v[5], f, 2);
   c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6], v[7], f, 3);
-  codes[i] = s == 255 ? 0u : c;
+  return s == 255 ? 0u : c;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kQuad) void mx4_quantize_kernel(const T* __restrict__ x, int rows, int k, long x_stride, int blocks,
+                                                             unsigned* __restrict__ codes, unsigned char* __restrict__ scales) {
+  const unsigned i = blockIdx.x * (unsigned)kQuad + threadIdx.x, per = 4u * blocks;
+  if (i >= (unsigned)rows * per) return;      // (whole quads)
+  const unsigned row = i / per, at = (i - row * per) * 8;
+  int s;
+  codes[i] = quantize8(x + row * x_stride + at, k - (int)at, s);
   if ((threadIdx.x & 3) == 0) scales[i >> 2] = (unsigned char)s;
+}
+
+// What the tile kernel reads.  Work-groups up to `row_groups`: 16 rows x 512 terms of the rows in operand order, from numbers or (T = void) from codes; a wavefront takes
+// every fourth block of a row, a quad of lanes one block.  The others: 256 words of the weights' scales.
+struct Mx4Arrange {
+  const void* x;                     // numbers, or codes
+  const unsigned char *xs, *ws;      // scales of codes, of the weights
+  long x_stride;
+  int rows, k, c_out, blocks, mi;    // mi: blocks of c_out of a wavefront of the tile kernel
+  int row_groups;
+  unsigned *codes, *x_scales, *w_scales;
+};
+
+template <typename T> __global__ __launch_bounds__(256) void mx4_arrange_kernel(const Mx4Arrange p) {
+  const int fours = (p.blocks + 15) / 16;
+  if ((int)blockIdx.x < p.row_groups) {
+    const int b = blockIdx.x / (unsigned)fours, four = (int)blockIdx.x - b * fours;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, lrow = lane >> 2, quarter = lane & 3;
+    const int row = b * 16 + lrow;
+    unsigned scales = 0;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int step = four * 4 + t, blk = step * 4 + wave;
+      unsigned c = 0;
+      int s = 0;
+      if constexpr (std::is_same<T, void>::value) {
+        if (row < p.rows && blk < p.blocks) {
+          const long at = (long)row * p.blocks + blk;
+          c = static_cast<const unsigned*>(p.x)[at * 4 + quarter];
+          s = p.xs[at];
+        }
+      } else {
+        const int at = blk * 32 + quarter * 8;
+        c = quantize8(static_cast<const T*>(p.x) + min(row, p.rows - 1) * p.x_stride + at, row < p.rows ? p.k - at : 0, s);
+      }
+      p.codes[((long)b * 4 * fours + step) * 256 + (wave * 16 + lrow) * 4 + quarter] = c;
+      scales |= (unsigned)s << (8 * t);
+    }
+    if (quarter == 0) p.x_scales[((long)(b >> 2) * fours + four) * 256 + (b & 3) * 64 + wave * 16 + lrow] = scales;
+    return;
+  }
+  const int chunk = (int)blockIdx.x - p.row_groups, g = chunk / fours, four = chunk - g * fours;
+  const int b = g * 4 + ((int)threadIdx.x >> 6), lane = threadIdx.x & 63, lrow = lane & 15, lblk = lane >> 4;
+  const int o = b / p.mi * 16 * p.mi + (p.mi == 8 ? mx4::spread_row<8>(b % 8, lrow) : mx4::spread_row<4>(b % 4, lrow));
+  unsigned w = 0;
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    const int blk = (four * 4 + t) * 4 + lblk;
+    if (o < p.c_out && blk < p.blocks) w |= (unsigned)p.ws[(long)o * p.blocks + blk] << (8 * t);
+  }
+  p.w_scales[(long)chunk * 256 + threadIdx.x] = w;
 }
 
 template <typename T>
@@ -119,16 +174,74 @@ void launch_quantize(const void* x, int rows, int k, int x_stride, int dtype, vo
   });
 }
 
-void launch_product(Mx4Args p, int act, int dtype, hipStream_t s) {
+// Scratch of a product: the tile kernel's operands, or the rows' codes.
+struct ProductPlan {
+  int mi;                            // blocks a wavefront of the tile kernel has on a side, 0: the wave kernel
+  size_t codes, x_scales, w_scales;  // bytes
+  size_t total() const { return codes + x_scales + w_scales; }
+};
+
+ProductPlan plan_product(int rows, int k, int c_out, bool numbers) {
+  const long blocks = blocks_of(k), fours = (blocks + 15) / 16;
+  ProductPlan q = {};
+  if (rows >= 512 && (double)(rows + 63) * fours * 512 < 2147483648.0) q.mi = (double)rows * c_out >= 256.0 * 256 * 128 ? 8 : 4;
+  if (q.mi) {
+    q.codes = (size_t)((rows + 15L) / 16 * fours * 4096);
+    q.x_scales = (size_t)((rows + 63L) / 64 * fours * 1024);
+    q.w_scales = (size_t)((c_out + 32L * q.mi - 1) / (32L * q.mi) * (q.mi / 2) * fours * 1024);
+  } else if (numbers) {
+    q.codes = (size_t)((long)rows * blocks * 16);
+    q.x_scales = (size_t)((long)rows * blocks + 15) & ~(size_t)15;
+  }
+  return q;
+}
+
+// x: numbers of x_dtype, or (x_scales given) codes
+void launch_product(Mx4Args p, const void* x, const void* x_scales, int k, long x_stride, int act, int dtype, void* ws, const ProductPlan& q, hipStream_t s) {
   const float inf = std::numeric_limits<float>::infinity();
   p.lo = act == CPRUNE_ACT_NONE ? -inf : 0.0f;
   p.hi = act == CPRUNE_ACT_RELU6 ? 6.0f : inf;
-  p.tiles = (p.c_out + 31) / 32;
-  const dim3 grid((unsigned)((long)p.tiles * ((p.rows + 31) / 32)));
+  const bool silu = act == CPRUNE_ACT_SILU;
+  auto tiles = [&](int outs, int rows) {
+    p.tiles = (p.c_out + outs - 1) / outs;
+    p.row_tiles = (p.rows + rows - 1) / rows;
+    return dim3((unsigned)((long)p.tiles * p.row_tiles));
+  };
+  char* const scratch = static_cast<char*>(ws);
+  if (q.mi) {
+    const int fours = (p.blocks + 15) / 16;
+    Mx4Arrange r = {};
+    r.x = x, r.xs = static_cast<const unsigned char*>(x_scales), r.ws = p.as, r.x_stride = x_stride;
+    r.rows = p.rows, r.k = k, r.c_out = p.c_out, r.blocks = p.blocks, r.mi = q.mi;
+    r.row_groups = (p.rows + 15) / 16 * fours;
+    r.codes = reinterpret_cast<unsigned*>(scratch);
+    r.x_scales = reinterpret_cast<unsigned*>(scratch + q.codes);
+    r.w_scales = reinterpret_cast<unsigned*>(scratch + q.codes + q.x_scales);
+    const unsigned groups = (unsigned)(r.row_groups + q.w_scales / 1024);
+    if (x_scales) mx4_arrange_kernel<void><<<groups, 256, 0, s>>>(r);
+    else with_type(dtype, [&](auto t) { mx4_arrange_kernel<decltype(t)><<<groups, 256, 0, s>>>(r); });
+    p.bo = reinterpret_cast<const unsigned char*>(r.codes), p.bso = r.x_scales, p.aso = r.w_scales;
+  } else if (!x_scales) {
+    launch_quantize(x, p.rows, k, (int)x_stride, dtype, scratch, scratch + q.codes, s);
+    p.b = reinterpret_cast<const unsigned char*>(scratch), p.bs = p.b + q.codes;
+  } else {
+    p.b = static_cast<const unsigned char*>(x), p.bs = static_cast<const unsigned char*>(x_scales);
+  }
   with_type(dtype, [&](auto t) {
     using T = decltype(t);
-    if (act == CPRUNE_ACT_SILU) mx4_wave_kernel<T, true, 2, 2, 4><<<grid, 256, 0, s>>>(p);
-    else mx4_wave_kernel<T, false, 2, 2, 4><<<grid, 256, 0, s>>>(p);
+    if (q.mi == 8) {
+      const dim3 grid = tiles(256, 256);
+      if (silu) mx4_tile_kernel<T, true, 8, 8><<<grid, 256, 0, s>>>(p);
+      else mx4_tile_kernel<T, false, 8, 8><<<grid, 256, 0, s>>>(p);
+    } else if (q.mi == 4) {
+      const dim3 grid = tiles(128, 128);
+      if (silu) mx4_tile_kernel<T, true, 4, 4><<<grid, 256, 0, s>>>(p);
+      else mx4_tile_kernel<T, false, 4, 4><<<grid, 256, 0, s>>>(p);
+    } else {
+      const dim3 grid = tiles(32, 32);
+      if (silu) mx4_wave_kernel<T, true, 2, 2, 4><<<grid, 256, 0, s>>>(p);
+      else mx4_wave_kernel<T, false, 2, 2, 4><<<grid, 256, 0, s>>>(p);
+    }
   });
 }
 
@@ -166,24 +279,31 @@ extern "C" int cprune_mx4_dequantize(const void* codes, const void* scales, int 
   return CPRUNE_OK;
 }
 
+extern "C" size_t cprune_mx4_matmul_workspace_bytes(int rows, int k, int c_out) {
+  if (check_product(rows, k, c_out, CPRUNE_ACT_NONE, CPRUNE_F32) != CPRUNE_OK) return 0;
+  return plan_product(rows, k, c_out, false).total();
+}
+
 extern "C" int cprune_mx4_matmul(const void* x_codes, const void* x_scales, int rows, int k, const void* w_codes, const void* w_scales,
-                                 int c_out, const float* bias, cprune_act act, cprune_dtype dtype, void* y, void* stream) {
+                                 int c_out, const float* bias, cprune_act act, cprune_dtype dtype, void* y, void* ws, size_t ws_bytes,
+                                 void* stream) {
   const int rc = check_product(rows, k, c_out, act, dtype);
   if (rc != CPRUNE_OK) return rc;
   if (!x_codes || !x_scales || !w_codes || !w_scales || !y || !aligned16(x_codes) || !aligned16(w_codes)) return CPRUNE_ERR_INVALID_ARG;
+  const ProductPlan q = plan_product(rows, k, c_out, false);
+  if (q.total() && (!ws || ws_bytes < q.total())) return CPRUNE_ERR_WORKSPACE;
+  if (!aligned16(ws)) return CPRUNE_ERR_INVALID_ARG;
   Mx4Args p = {};
   p.a = static_cast<const unsigned char*>(w_codes), p.as = static_cast<const unsigned char*>(w_scales);
-  p.b = static_cast<const unsigned char*>(x_codes), p.bs = static_cast<const unsigned char*>(x_scales);
   p.bias = bias, p.y = y, p.rows = rows, p.c_out = c_out, p.blocks = blocks_of(k);
-  launch_product(p, act, dtype, static_cast<hipStream_t>(stream));
+  launch_product(p, x_codes, x_scales, k, 0, act, dtype, ws, q, static_cast<hipStream_t>(stream));
   CPRUNE_LAUNCH_CHECK();
   return CPRUNE_OK;
 }
 
 extern "C" size_t cprune_mx4_linear_workspace_bytes(int rows, int k, int c_out, cprune_dtype dtype) {
   if (check_product(rows, k, c_out, CPRUNE_ACT_NONE, dtype) != CPRUNE_OK) return 0;
-  const size_t blocks = (size_t)rows * blocks_of(k);
-  return blocks * 16 + ((blocks + 15) & ~(size_t)15);
+  return plan_product(rows, k, c_out, true).total();
 }
 
 extern "C" int cprune_mx4_linear(const void* x, int rows, int k, int x_stride, const void* w_codes, const void* w_scales, int c_out,
@@ -192,17 +312,13 @@ extern "C" int cprune_mx4_linear(const void* x, int rows, int k, int x_stride, c
   if (rc == CPRUNE_OK) rc = check_numbers(rows, k, x_stride, dtype);
   if (rc != CPRUNE_OK) return rc;
   if (!x || !w_codes || !w_scales || !y || !aligned16(w_codes)) return CPRUNE_ERR_INVALID_ARG;
-  if (!ws || ws_bytes < cprune_mx4_linear_workspace_bytes(rows, k, c_out, dtype)) return CPRUNE_ERR_WORKSPACE;
+  const ProductPlan q = plan_product(rows, k, c_out, true);
+  if (q.total() && (!ws || ws_bytes < q.total())) return CPRUNE_ERR_WORKSPACE;
   if (!aligned16(ws)) return CPRUNE_ERR_INVALID_ARG;
-  hipStream_t s = static_cast<hipStream_t>(stream);
-  unsigned char* codes = static_cast<unsigned char*>(ws);
-  unsigned char* scales = codes + (size_t)rows * blocks_of(k) * 16;
   Mx4Args p = {};
   p.a = static_cast<const unsigned char*>(w_codes), p.as = static_cast<const unsigned char*>(w_scales);
-  p.b = codes, p.bs = scales;
   p.bias = bias, p.y = y, p.rows = rows, p.c_out = c_out, p.blocks = blocks_of(k);
-  launch_quantize(x, rows, k, x_stride, dtype, codes, scales, s);
-  launch_product(p, act, dtype, s);
+  launch_product(p, x, nullptr, k, x_stride, act, dtype, ws, q, static_cast<hipStream_t>(stream));
   CPRUNE_LAUNCH_CHECK();
   return CPRUNE_OK;
 }

@@ -13,7 +13,10 @@ struct Mx4Args {
   void* y;                       // [rows][c_out]
   int rows, c_out, blocks;
   float lo, hi;
-  int tiles;                     // tiles of c_out; work-groups are (rows, c_out), c_out first
+  int tiles, row_tiles;          // tiles of c_out, of rows
+  // tile kernel: the rows' codes in operand order and both sides' scales, from mx4_arrange_kernel
+  const unsigned char* bo;       // [16-row block][step of four blocks, a multiple of four][lane][16 bytes], zeros past the last row and block
+  const unsigned *aso, *bso;     // [four 16-row blocks][four steps][16-row block][lane], byte t the scale of step t
 };
 
 namespace mx4 {
@@ -21,10 +24,24 @@ namespace mx4 {
 typedef int int8v __attribute__((ext_vector_type(8)));
 constexpr unsigned kOne = 127;   // the scale's byte that stands for 1
 
-// The matrix instruction's operand: lane l holds row l % 16 and the 32 elements of block l / 16, in four registers.
-__device__ __forceinline__ float4_t mma(uint4 a, int as, uint4 b, int bs, float4_t acc) {
+// The matrix instruction's operand: lane l holds row l % 16 and the 32 elements of block l / 16, in four registers; byte BYTE of `as` and `bs` is the
+// block's scale.
+template <int BYTE = 0> __device__ __forceinline__ float4_t mma(uint4 a, int as, uint4 b, int bs, float4_t acc) {
   const int8v av = {(int)a.x, (int)a.y, (int)a.z, (int)a.w, 0, 0, 0, 0}, bv = {(int)b.x, (int)b.y, (int)b.z, (int)b.w, 0, 0, 0, 0};
-  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(av, bv, acc, 4, 4, 0, as, 0, bs);
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(av, bv, acc, 4, 4, BYTE, as, BYTE, bs);
+}
+
+// The same for 32 x 32 results and 64 terms: lane l holds row l % 32 and block l / 32; result v of lane l is row 8 (v / 4) + 4 (l / 32) + v % 4, column l % 32.
+typedef float float16v __attribute__((ext_vector_type(16)));
+template <int BYTE> __device__ __forceinline__ float16v mma32(uint4 a, int as, uint4 b, int bs, float16v acc) {
+  const int8v av = {(int)a.x, (int)a.y, (int)a.z, (int)a.w, 0, 0, 0, 0}, bv = {(int)b.x, (int)b.y, (int)b.z, (int)b.w, 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(av, bv, acc, 4, 4, BYTE, as, BYTE, bs);
+}
+
+template <bool SILU> __device__ __forceinline__ float finish(float z, float lo, float hi) {
+  if constexpr (SILU) return z * __builtin_amdgcn_rcpf(1.0f + __expf(-z));
+  z = z < lo ? lo : z;      // (comparisons and not minimum / maximum: a NaN stays one)
+  return z > hi ? hi : z;
 }
 
 __device__ __forceinline__ uint4 load16(__amdgpu_buffer_rsrc_t r, unsigned off) {
@@ -99,19 +116,210 @@ __global__ __launch_bounds__(64 * WAVES) void mx4_wave_kernel(const Mx4Args p) {
       float z[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        z[e] = v[e] + bias[e];
-        if constexpr (SILU) {
-          z[e] = z[e] * __builtin_amdgcn_rcpf(1.0f + __expf(-z[e]));
-        } else {
-          z[e] = z[e] < p.lo ? p.lo : z[e];     // (comparisons: a NaN stays one)
-          z[e] = z[e] > p.hi ? p.hi : z[e];
-        }
+        z[e] = finish<SILU>(v[e] + bias[e], p.lo, p.hi);
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         if (o + e < p.c_out) y[e] = Elem<T>::from_f32(z[e]);
     }
   }
+}
+
+// ---- many rows: tiles through LDS -----------------------------------------------------------------
+// Four wavefronts (2 x 2) of MI x NI blocks each: 32 MI outputs of c_out by 32 NI rows a work-group, K in steps of 128 terms.  A stage is the tile's codes
+// of one step in operand order, [16-row block][lane][16 bytes], written to LDS by the loads themselves (a lane's address picks what its place gets).
+// While step s is multiplied, the operands of s + 1 go to registers and the codes of s + 4 into the stage that s has left.
+// The matrix instruction takes 32 rows of each side; those of a wavefront's c_out are dealt so that a lane's results are 8 MI neighbours of one row of y.
+namespace mx4 {
+
+typedef __attribute__((address_space(3))) void lds_void;
+typedef const __attribute__((address_space(1))) void global_void;
+
+// row of c_out, counted from the 16 MI outputs it belongs to, that is row m of 16-row block i: of the instruction's rows 8 q + 4 g + e, g picks the half
+template <int MI> __device__ __forceinline__ int spread_row(int i, int m) {
+  const int r = (i & 1) * 16 + m;
+  return 8 * MI * ((r >> 2) & 1) + 16 * (i >> 1) + 4 * (r >> 3) + (r & 3);
+}
+
+// Waits until all but the last `newer` loads and all LDS accesses of this wavefront are done, then for the others.
+template <int NEWER> __device__ __forceinline__ void wait_and_meet() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);      // (nor do products drift past it: their operands would be held for another step)
+  __builtin_amdgcn_s_waitcnt((NEWER & 15) | (7 << 4) | ((NEWER >> 4) << 14));
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" ::: "memory");
+}
+
+// The tile of a work-group: neighbouring work-groups run on different XCDs, each with an L2 of its own, so each XCD gets a run of tiles, and a run walks
+// eight tiles of rows before the next tile of c_out.
+__device__ __forceinline__ void tile_of(const Mx4Args& p, int& tr, int& tc) {
+  const unsigned total = gridDim.x, xcd = blockIdx.x & 7, per = total >> 3, rest = total & 7;
+  const unsigned t = xcd * per + min(xcd, rest) + (blockIdx.x >> 3);
+  const unsigned group = t / (8u * p.tiles), local = t - group * 8u * p.tiles;
+  const unsigned wide = min(8u, (unsigned)p.row_tiles - group * 8u);
+  tc = (int)(local / wide);
+  tr = (int)(group * 8u + (local - (unsigned)tc * wide));
+}
+
+}  // namespace mx4
+
+template <typename T, bool SILU, int MI, int NI>
+__global__ __launch_bounds__(256) void mx4_tile_kernel(const Mx4Args p) {
+  using namespace mx4;
+  static_assert(MI == NI && MI % 4 == 0, "a wavefront loads blocks of one side, scales come for four blocks");
+  constexpr int AB = 2 * MI, BB = 2 * NI;           // 16-row blocks of the tile
+  constexpr int LOADS = (AB + BB) / 4;              // of which a wavefront loads these a step
+  constexpr int CHUNKS = LOADS / 4;                 // and for four of them at a time the scales of four steps
+  __shared__ uint4 st0[(AB + BB) * 64], st1[(AB + BB) * 64], st2[(AB + BB) * 64], st3[(AB + BB) * 64];
+  __shared__ unsigned sc[(AB + BB) * 64];      // [16-row block][lane]: the scales of four steps
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), lrow = lane & 15, lblk = lane >> 4;
+  const int wm = wave & 1, wn = wave >> 1;
+  int tr, tc;
+  tile_of(p, tr, tc);
+  const int o0 = tc * 16 * AB, r0 = tr * 16 * BB;
+  const int steps = (p.blocks + 3) / 4, fours = (steps + 3) / 4;
+
+  // Wavefronts 0 and 1 load the weights, 2 and 3 the rows.  What lies past the last output, row or step reads the last one again: results of such rows
+  // are not stored, and terms past the last block are zeros on the rows' side.
+  const unsigned char* const from = wave < 2 ? p.a : p.bo;
+  const unsigned pitch = wave < 2 ? 64u : 1024u;      // from step to step
+  unsigned off[LOADS], less = 0;
+  if (wave < 2) {
+#pragma unroll
+    for (int q = 0; q < LOADS; ++q) {
+      const int b = wave * LOADS + q;
+      off[q] = ((unsigned)min(o0 + b / MI * 16 * MI + spread_row<MI>(b % MI, lrow), p.c_out - 1) * p.blocks + lblk) * 16u;
+    }
+    less = 16u * max(0, (steps - 1) * 4 + lblk - (p.blocks - 1));
+  } else {
+#pragma unroll
+    for (int q = 0; q < LOADS; ++q)
+      off[q] = (unsigned)min((r0 >> 4) + (wave - 2) * LOADS + q, (p.rows - 1) >> 4) * fours * 4096u + lane * 16u;
+  }
+  const int last = wave < 2 ? steps - 1 : 4 * fours - 1;
+  auto fetch = [&](uint4* stage, int s) __attribute__((always_inline)) {
+    const unsigned char* const at = from + (size_t)min(s, last) * pitch;
+    const unsigned back = s >= last ? less : 0u;
+#pragma unroll
+    for (int q = 0; q < LOADS; ++q)
+      __builtin_amdgcn_global_load_lds((global_void*)(at + (off[q] - back)), (lds_void*)(stage + (wave * LOADS + q) * 64), 16, 0, 0);
+  };
+  const unsigned* const scales_from = wave < 2 ? p.aso : p.bso;
+  unsigned scales_off[CHUNKS];
+#pragma unroll
+  for (int q = 0; q < CHUNKS; ++q)
+    scales_off[q] = (unsigned)(wave < 2 ? (o0 >> 6) + wave * CHUNKS + q : min((r0 >> 6) + (wave - 2) * CHUNKS + q, (p.rows - 1) >> 6)) * fours * 256u + lane * 4u;
+  auto fetch_scales = [&](int four) __attribute__((always_inline)) {
+    const unsigned* const at = scales_from + (size_t)min(four, fours - 1) * 256;
+#pragma unroll
+    for (int q = 0; q < CHUNKS; ++q)
+      __builtin_amdgcn_global_load_lds((global_void*)(at + scales_off[q]), (lds_void*)(sc + (wave * CHUNKS + q) * 256), 16, 0, 0);
+  };
+
+  constexpr int M = MI / 2, N = NI / 2;      // 32 x 32 results of a wavefront
+  float16v acc[M][N];
+#pragma unroll
+  for (int i = 0; i < M; ++i)
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+  // operands and scales of a step's two halves
+  uint4 fa[2][2][M], fb[2][2][N];
+  int sa[2][M], sb[2][N];
+  const int at0 = ((lane >> 4) & 1) * 64 + (lane >> 5) * 16 + lrow;      // a lane's place in two 16-row blocks, of the first half
+  auto operands = [&](const uint4* stage, uint4 (&a)[2][M], uint4 (&b)[2][N]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int i = 0; i < M; ++i) a[h][i] = stage[(wm * MI + 2 * i) * 64 + h * 32 + at0];
+#pragma unroll
+      for (int j = 0; j < N; ++j) b[h][j] = stage[(AB + wn * NI + 2 * j) * 64 + h * 32 + at0];
+    }
+  };
+  auto scales = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int i = 0; i < M; ++i) sa[h][i] = (int)sc[(wm * MI + 2 * i) * 64 + h * 32 + at0];
+#pragma unroll
+      for (int j = 0; j < N; ++j) sb[h][j] = (int)sc[(AB + wn * NI + 2 * j) * 64 + h * 32 + at0];
+    }
+  };
+
+  fetch_scales(0);
+  fetch(st0, 0);
+  fetch(st1, 1);
+  fetch(st2, 2);
+  fetch(st3, 3);
+  wait_and_meet<3 * LOADS>();
+  operands(st0, fa[0], fb[0]);
+  scales();
+  // Step s = 4 n + B: its operands are in fa[B & 1], fb[B & 1].
+  auto step = [&](auto byte, int s, uint4* own, uint4* next) __attribute__((always_inline)) {
+    constexpr int B = decltype(byte)::value;
+    wait_and_meet<2 * LOADS>();      // the codes of s + 1 are there (s + 2 and s + 3 may be under way), and nobody reads `own` any more
+    if (B == 0) fetch_scales(s / 4 + 1);      // (ahead of the codes of s + 4: there when those are)
+    fetch(own, s + 4);
+    operands(next, fa[(B + 1) & 1], fb[(B + 1) & 1]);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int i = 0; i < M; ++i) acc[i][j] = mma32<B>(fa[B & 1][h][i], sa[h][i], fb[B & 1][h][j], sb[h][j], acc[i][j]);
+    // an LDS read, a load and two products in turn
+#pragma unroll
+    for (int q = 0; q < 2 * (M + N); ++q) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      if (q < LOADS) __builtin_amdgcn_sched_group_barrier(0x20, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x8, 2 * M * N / (2 * (M + N)), 0);
+    }
+    if (B == 3) scales();
+    asm volatile("" ::: "memory");      // (the reads above belong to this turn of the loop)
+  };
+  // (One way out of the loop where the sums fill half the registers: with an exit behind each step they are copied at every turn.  The steps that
+  // fill up the last four multiply the zeros of the rows' side.)
+  for (int s = 0;; s += 4) {
+    step(std::integral_constant<int, 0>(), s, st0, st1);
+    if (MI < 8 && s + 1 >= steps) break;
+    step(std::integral_constant<int, 1>(), s + 1, st1, st2);
+    if (MI < 8 && s + 2 >= steps) break;
+    step(std::integral_constant<int, 2>(), s + 2, st2, st3);
+    if (MI < 8 && s + 3 >= steps) break;
+    step(std::integral_constant<int, 3>(), s + 3, st3, st0);
+    if (s + 4 >= steps) break;
+  }
+
+  // 8 MI neighbouring outputs of a row
+  const int o = o0 + wm * 16 * MI + 8 * MI * (lane >> 5);
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    const int r = r0 + (wn * N + j) * 32 + (lane & 31);
+    if (r >= p.rows) continue;
+    T* y = static_cast<T*>(p.y) + (long)r * p.c_out + o;
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int at = 16 * i + 4 * q;
+        const float4_t bias = load_bias4(p.bias, p.c_out, o + at);
+        typedef T out4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+        out4 z;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) z[e] = Elem<T>::from_f32(finish<SILU>(acc[i][j][4 * q + e] + bias[e], p.lo, p.hi));
+        if (o + at + 4 <= p.c_out) {
+          *reinterpret_cast<out4*>(y + at) = z;
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (o + at + e < p.c_out) y[at + e] = z[e];
+        }
+      }
+    }
+  }
+  __builtin_amdgcn_s_waitcnt(7 << 4);      // (no load into LDS outlives its work-group)
 }
 
 }  // namespace cprune

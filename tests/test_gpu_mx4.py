@@ -209,7 +209,7 @@ def test_leading_sizes_and_outputs_that_hold_nothing_else():
         for off in (0, 1, 3):
             out = torch.full((rows * c_out + 128,), 9.0, dtype=torch.float16, device="cuda")
             st = B.lib().cprune_mx4_matmul(xc.data_ptr(), xs.data_ptr(), rows, 64, wc.data_ptr(), ws.data_ptr(), c_out, None, 0, B.F16,
-                                           out.data_ptr() + 2 * (64 + off), torch.cuda.current_stream().cuda_stream)
+                                           out.data_ptr() + 2 * (64 + off), None, 0, torch.cuda.current_stream().cuda_stream)
             assert st == B.OK
             assert torch.equal(out[64 + off:64 + off + rows * c_out].reshape(rows, c_out), y.reshape(24, 40)[:rows, :c_out])
             assert (out[:64 + off] == 9).all() and (out[64 + off + rows * c_out:] == 9).all()
