@@ -514,7 +514,7 @@ int cprune_search_destroy(cprune_search* s);
  * mean, rstd     fp32 [n][groups]; mean_out / rstd_out may be NULL
  * dy             as x, with dy_stride
  * dweight, dbias fp32 [c], each may be NULL.  Summed in a fixed order: repeated calls give identical bits.
- * n, pixels >= 1; groups divides c; eps > 0 and finite.  n * groups of 2^24 and more: CPRUNE_ERR_UNSUPPORTED. */
+ * n, pixels >= 1; groups divides c; eps > 0 and finite.  More (image, group) pairs than a launch has work-groups (2^22): CPRUNE_ERR_UNSUPPORTED. */
 typedef struct {
   int32_t n, pixels, c, groups;
   int32_t dtype; /* cprune_dtype of x, y, dy, dx */

@@ -15,86 +15,77 @@ __device__ __forceinline__ int chunk_count(const NormGeom& g, int chunk, int rr)
   return sr1 - sr0 - (sr1 == g.SR && rr >= g.tail ? 1 : 0);
 }
 
-__device__ __forceinline__ double2 group_sum(double2 v) {
-  __shared__ double2 part[norm::kThreads / 64];
+// Sum over the entries (chunk, pixel of the superrow, channel of the group) of an (image, group), one work-group, in 64 bits and a fixed order: f(chunk,
+// pixel, channel, entry).  Four entries are under way at a time; a thread counts its place on instead of dividing.
+template <typename F> __device__ __forceinline__ double2 entries_sum(const NormArgs& a, const float2* part, F&& f) {
+  __shared__ double2 sums[1024 / 64];
+  const int t = (int)threadIdx.x, n = (int)blockDim.x, row = a.g.R * a.c, per = a.g.R * a.cg;
+  int chunk = t / per, rr = (t - chunk * per) / a.cg, ch = t - chunk * per - rr * a.cg;
+  const int d_chunk = n / per, d_rr = (n - d_chunk * per) / a.cg, d_ch = n - d_chunk * per - d_rr * a.cg;
+  double2 s = {0.0, 0.0};
+  while (chunk < a.g.chunks) {
+    float2 e[4];
+    int at[4][3];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      at[u][0] = chunk, at[u][1] = rr, at[u][2] = ch;
+      e[u] = chunk < a.g.chunks ? part[(long)chunk * row + rr * a.c + ch] : make_float2(0.0f, 0.0f);
+      ch += d_ch, rr += d_rr, chunk += d_chunk;
+      if (ch >= a.cg) ch -= a.cg, ++rr;
+      if (rr >= a.g.R) rr -= a.g.R, ++chunk;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (at[u][0] < a.g.chunks) {
+        const double2 v = f(at[u][0], at[u][1], at[u][2], e[u]);
+        s.x += v.x, s.y += v.y;
+      }
+  }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) {
-    v.x += __shfl_down(v.x, o, 64);
-    v.y += __shfl_down(v.y, o, 64);
+    s.x += __shfl_down(s.x, o, 64);
+    s.y += __shfl_down(s.y, o, 64);
   }
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+  if ((t & 63) == 0) sums[t >> 6] = s;
   __syncthreads();
-  v = part[0];
-  for (int i = 1; i < norm::kThreads / 64; ++i) v.x += part[i].x, v.y += part[i].y;
-  return v;
+  s = sums[0];
+  for (int i = 1; i < n / 64; ++i) s.x += sums[i].x, s.y += sums[i].y;
+  return s;
 }
 
-// The chunks' statistics as those of an (image, group), one work-group each: sums over (count, mean, squares) about the first mean, in 64 bits.
-__global__ __launch_bounds__(norm::kThreads) void norm_join_stats_kernel(const NormArgs a, float eps, float* __restrict__ mean_out,
-                                                                         float* __restrict__ rstd_out) {
-  const int image = blockIdx.x / a.groups, group = blockIdx.x - image * a.groups;
+// The chunks' statistics as those of an (image, group): sums over (count, mean, squares) about the first mean.
+__global__ __launch_bounds__(1024) void norm_join_stats_kernel(const NormArgs a, float* __restrict__ mean_out, float* __restrict__ rstd_out) {
+  const int image = blockIdx.x / (unsigned)a.groups, group = blockIdx.x - image * a.groups;
   const float2* part = a.part + (long)image * a.g.chunks * a.g.R * a.c + group * a.cg;
   const double first = part[0].x;
-  const int per = a.g.R * a.cg, count = per * a.g.chunks;
-  double2 s = {0.0, 0.0};
-  for (int i = threadIdx.x; i < count; i += norm::kThreads) {
-    const int chunk = i / per, e = i - chunk * per, rr = e / a.cg, ch = e - rr * a.cg;
-    const int n = chunk_count(a.g, chunk, rr);
-    if (n == 0) continue;
-    const float2 p = part[(long)chunk * a.g.R * a.c + rr * a.c + ch];
-    const double d = (double)p.x - first;
-    s.x += n * d;
-    s.y += (double)p.y + n * d * d;
-  }
-  s = group_sum(s);
+  const double2 s = entries_sum(a, part, [&](int chunk, int rr, int, float2 e) __attribute__((always_inline)) {
+    const double n = chunk_count(a.g, chunk, rr), d = (double)e.x - first;
+    return n > 0.0 ? make_double2(n * d, (double)e.y + n * d * d) : make_double2(0.0, 0.0);
+  });
   if (threadIdx.x == 0) {
-    const double m = (double)a.pixels * a.cg, shift = s.x / m;
-    double var = s.y / m - shift * shift;
-    var = var < 0.0 ? 0.0 : var;
-    mean_out[blockIdx.x] = (float)(first + shift);
-    rstd_out[blockIdx.x] = (float)(1.0 / sqrt(var + (double)eps));
+    const float2 m = norm::statistics(s, first, a);
+    mean_out[blockIdx.x] = m.x;
+    rstd_out[blockIdx.x] = m.y;
   }
 }
 
-// Work-groups up to n * groups: the two means of an (image, group).  The others: 32 channels of dweight and dbias each, eight threads a channel.
-__global__ __launch_bounds__(norm::kThreads) void norm_join_grads_kernel(const NormArgs a, int n, float2* __restrict__ terms,
-                                                                         float* __restrict__ dweight, float* __restrict__ dbias) {
-  const long row = (long)a.g.R * a.c;      // partial sums of a chunk
-  if ((int)blockIdx.x < n * a.groups) {
-    const int image = blockIdx.x / a.groups, group = blockIdx.x - image * a.groups;
-    const float2* part = a.part + (long)image * a.g.chunks * row + group * a.cg;
-    const int per = a.g.R * a.cg, count = per * a.g.chunks;
-    double2 s = {0.0, 0.0};
-    for (int i = threadIdx.x; i < count; i += norm::kThreads) {
-      const int chunk = i / per, e = i - chunk * per, rr = e / a.cg, ch = e - rr * a.cg;
-      const float2 p = part[chunk * row + rr * a.c + ch];
-      const double w = a.weight ? a.weight[group * a.cg + ch] : 1.0f;
-      s.x += w * p.x;
-      s.y += w * p.y;
-    }
-    s = group_sum(s);
-    const double m = (double)a.pixels * a.cg;
-    if (threadIdx.x == 0) terms[blockIdx.x] = make_float2((float)(s.x / m), (float)(s.y / m));
-    return;
-  }
-  const int ch = ((int)blockIdx.x - n * a.groups) * 32 + (threadIdx.x & 31), lane = threadIdx.x >> 5;
-  __shared__ double2 sums[8][32];
-  double2 s = {0.0, 0.0};
-  if (ch < a.c) {
-    const long count = (long)n * a.g.chunks * a.g.R;
-    for (long i = lane; i < count; i += 8) {
-      const float2 p = a.part[i * a.c + ch];
-      s.x += p.x;
-      s.y += p.y;
-    }
-  }
-  sums[lane][threadIdx.x & 31] = s;
-  __syncthreads();
-  if (lane == 0 && ch < a.c) {
-    for (int i = 1; i < 8; ++i) s.x += sums[i][threadIdx.x].x, s.y += sums[i][threadIdx.x].y;
-    if (dbias) dbias[ch] = (float)s.x;
-    if (dweight) dweight[ch] = (float)s.y;
-  }
+// The two means of an (image, group).
+__global__ __launch_bounds__(1024) void norm_join_grads_kernel(const NormArgs a, float2* __restrict__ terms) {
+  const int image = blockIdx.x / (unsigned)a.groups, group = blockIdx.x - image * a.groups;
+  const float2* part = a.part + (long)image * a.g.chunks * a.g.R * a.c + group * a.cg;
+  const double2 s = entries_sum(a, part, [&](int, int, int ch, float2 e) __attribute__((always_inline)) {
+    const double w = a.weight ? a.weight[group * a.cg + ch] : 1.0f;
+    return make_double2(w * e.x, w * e.y);
+  });
+  if (threadIdx.x == 0) terms[blockIdx.x] = make_float2((float)(s.x * a.inv_count), (float)(s.y * a.inv_count));
+}
+
+// threads of those: four entries each, 64 to 1024
+int join_threads(const NormArgs& a) {
+  const long entries = (long)a.g.chunks * a.g.R * a.cg;
+  int t = 64;
+  while (t < 1024 && 4L * t < entries) t *= 2;
+  return t;
 }
 
 int vector_of(int c, int dtype, bool dense) {
@@ -104,20 +95,59 @@ int vector_of(int c, int dtype, bool dense) {
   return v;
 }
 
+constexpr int kWholeVectors = 16, kWholeGradVectors = 8;      // a thread holds at most, of x or of x and dy each
+constexpr int kWholeColumns = 4096;                           // elements of a slab's superrow (LDS)
+
+// Work-groups of the whole form for a slab of `tp` vectors a superrow: as few threads as hold four vectors each, or up to the most.  false: too much.
+bool fit_whole(NormGeom& g, int tp, int most_threads, int most_vectors) {
+  if (tp > most_threads || (long)tp * g.V > kWholeColumns) return false;
+  for (int t = 256; t <= most_threads; t *= 2) {
+    if (t < tp) continue;
+    const int rpi = std::min(t / tp, g.SR), nv = (g.SR + rpi - 1) / rpi;
+    if (nv <= 4 || (t == most_threads && nv <= most_vectors)) {
+      g.tp = tp, g.rpi = rpi, g.nv = nv, g.slabs = g.P / tp;
+      g.threads = (tp * rpi + 63) / 64 * 64;
+      g.few = g.SR / rpi, g.more = g.SR % rpi, g.last_r = (g.SR - 1) % rpi;
+      g.by_tp = norm_div(tp, 1024);
+      return true;
+    }
+  }
+  return false;
+}
+
+// The whole form where a slab's pixels fit a work-group's registers: of the slabs of whole groups, the widest up to a cache line that still gives every
+// compute unit one, otherwise the narrowest.
+bool choose_whole(const cprune_norm_desc& d, bool backward, NormGeom& g) {
+  const int v = d.dtype == CPRUNE_F32 ? 4 : 8, cg = d.c / d.groups;
+  if (g.V != v) return false;
+  const bool merge = cg % v == 0;
+  const int most_threads = backward || merge || v == 4 ? 1024 : 512;      // (LDS: a pair a thread, or one for each of its elements)
+  const int most_vectors = backward ? kWholeGradVectors : kWholeVectors;
+  const int least = g.R > 1 ? g.P : std::lcm(v, cg) / v;                  // vectors
+  const int times = g.P / least;
+  for (int k = times; k > 1; --k)
+    if (times % k == 0 && (long)least * k * 16 <= 128 && (long)d.n * (times / k) >= 256 && fit_whole(g, least * k, most_threads, most_vectors)) return true;
+  return fit_whole(g, least, most_threads, most_vectors);
+}
+
 NormGeom geometry(const cprune_norm_desc& d, bool backward) {
-  NormGeom g;
+  NormGeom g = {};
   const bool dense = d.x_stride == d.c && (!backward || d.dy_stride == d.c);
   g.V = vector_of(d.c, d.dtype, dense);
   g.R = g.V / std::gcd(g.V, d.c);
   g.P = (int)((long)g.R * d.c / g.V);
+  g.SR = (d.pixels + g.R - 1) / g.R;
+  g.tail = d.pixels - (g.SR - 1) * g.R;
+  g.tiles = g.chunks = 1;
+  if (choose_whole(d, backward, g)) return g;
+  g.slabs = g.nv = 0;
   g.tiles = (g.P + norm::kThreads - 1) / norm::kThreads;
   g.tp = (g.P + g.tiles - 1) / g.tiles;
   g.rpi = norm::kThreads / g.tp;
   g.threads = norm::kThreads;
-  g.SR = (d.pixels + g.R - 1) / g.R;
-  g.tail = d.pixels - (g.SR - 1) * g.R;
-  // about eight work-groups a compute unit, and at least four vectors a thread
-  const long want = (2048 + (long)d.n * g.tiles - 1) / ((long)d.n * g.tiles);
+  g.by_tp = norm_div(g.tp, 1024);
+  // about six work-groups a compute unit, what the statistics' LDS lets run together, and at least four vectors a thread
+  const long want = std::max(1L, 1536 / ((long)d.n * g.tiles));
   const long most = (g.SR + 4L * g.rpi - 1) / (4L * g.rpi);
   const long chunks = std::max(1L, std::min(want, most));
   g.spc = (int)((g.SR + chunks - 1) / chunks);
@@ -140,14 +170,20 @@ int check(const cprune_norm_desc* d, bool backward) {
 
 // (a launch holds fewer than 2^32 threads)
 bool too_many_groups(const cprune_norm_desc& d, const NormGeom& g) {
-  return std::max((double)d.n * g.chunks * g.tiles, (double)d.n * d.groups + (d.c + 31) / 32) * norm::kThreads >= 4294967296.0;
+  const double launch = g.nv ? (double)d.n * g.slabs * g.threads
+                             : std::max((double)d.n * g.chunks * g.tiles + (d.c + 7) / 8, (double)d.n * d.groups * 4) * norm::kThreads;
+  return launch >= 4294967296.0;
 }
 
 size_t round16(size_t b) { return (b + 15) & ~(size_t)15; }
-size_t part_bytes(const cprune_norm_desc& d, const NormGeom& g) {
+// scratch: partial sums, then statistics or means of (image, group)
+size_t part_bytes(const cprune_norm_desc& d, const NormGeom& g, bool backward) {
+  if (g.nv) return backward && d.n > 1 ? round16((size_t)d.n * d.c * sizeof(float2)) : 0;
   return round16((size_t)d.n * g.chunks * g.R * d.c * sizeof(float2));
 }
-size_t stats_bytes(const cprune_norm_desc& d) { return round16((size_t)d.n * d.groups * sizeof(float2)); }
+size_t scratch_bytes(const cprune_norm_desc& d, const NormGeom& g, bool backward) {
+  return part_bytes(d, g, backward) + (g.nv ? 0 : round16((size_t)d.n * d.groups * sizeof(float2)));
+}
 
 NormArgs args_of(const cprune_norm_desc& d, const NormGeom& g) {
   NormArgs a = {};
@@ -157,6 +193,10 @@ NormArgs args_of(const cprune_norm_desc& d, const NormGeom& g) {
   const float inf = std::numeric_limits<float>::infinity();
   a.lo = d.act == CPRUNE_ACT_NONE ? -inf : 0.0f;
   a.hi = d.act == CPRUNE_ACT_RELU6 ? 6.0f : inf;
+  a.silu = d.act == CPRUNE_ACT_SILU;
+  a.n = d.n, a.eps = d.eps;
+  a.by_cg = norm_div(a.cg, a.c);
+  a.inv_count = 1.0 / ((double)d.pixels * a.cg);
   a.g = g;
   return a;
 }
@@ -177,6 +217,50 @@ template <typename F> void with_form(int dtype, int v, bool silu, F&& f) {
   else v == 8 ? act(__bf16(), std::integral_constant<int, 8>()) : vec(__bf16());
 }
 
+// calls f(vectors a thread holds), rounded up to a built form
+template <typename F> void with_vectors(int nv, F&& f) {
+  if (nv <= 1) f(std::integral_constant<int, 1>());
+  else if (nv <= 2) f(std::integral_constant<int, 2>());
+  else if (nv <= 4) f(std::integral_constant<int, 4>());
+  else if (nv <= 8) f(std::integral_constant<int, 8>());
+  else f(std::integral_constant<int, 16>());
+}
+template <typename F> void with_type(int dtype, F&& f) {
+  if (dtype == CPRUNE_F32) f(float());
+  else if (dtype == CPRUNE_F16) f(_Float16());
+  else f(__bf16());
+}
+
+void launch_whole(const NormArgs& a, int dtype, hipStream_t s) {
+  const NormGeom& g = a.g;
+  const bool merge = a.cg % g.V == 0;
+  const int cols = g.tp * g.V, groups = cols / (g.R * a.cg);
+  const size_t lds = ((size_t)(merge ? g.tp : cols) * g.rpi + groups) * sizeof(float2);
+  const unsigned grid = (unsigned)(a.n * g.slabs);
+  with_type(dtype, [&](auto t) {
+    with_vectors(g.nv, [&](auto nv) {
+      using T = decltype(t);
+      if (merge) norm_whole_kernel<T, decltype(nv)::value, true><<<grid, g.threads, lds, s>>>(a);
+      else norm_whole_kernel<T, decltype(nv)::value, false><<<grid, g.threads, lds, s>>>(a);
+    });
+  });
+}
+
+void launch_whole_grad(const NormArgs& a, int dtype, bool silu, hipStream_t s) {
+  const NormGeom& g = a.g;
+  const int cols = g.tp * g.V, groups = cols / (g.R * a.cg);
+  const size_t lds = std::max((size_t)g.V * g.threads / 2, (size_t)cols + groups) * sizeof(float2);
+  const unsigned grid = (unsigned)(a.n * g.slabs);
+  with_type(dtype, [&](auto t) {
+    with_vectors(g.nv, [&](auto nv) {
+      using T = decltype(t);
+      constexpr int NV = decltype(nv)::value < kWholeGradVectors ? decltype(nv)::value : kWholeGradVectors;
+      if (silu) norm_whole_grad_kernel<T, NV, true><<<grid, g.threads, lds, s>>>(a);
+      else norm_whole_grad_kernel<T, NV, false><<<grid, g.threads, lds, s>>>(a);
+    });
+  });
+}
+
 }  // namespace
 }  // namespace cprune
 
@@ -184,7 +268,7 @@ using namespace cprune;
 
 extern "C" size_t cprune_group_norm_workspace_bytes(const cprune_norm_desc* d, int backward) {
   if (check(d, backward != 0) != CPRUNE_OK) return 0;
-  return part_bytes(*d, geometry(*d, backward != 0)) + stats_bytes(*d);
+  return scratch_bytes(*d, geometry(*d, backward != 0), backward != 0);
 }
 
 extern "C" int cprune_group_norm_act(const cprune_norm_desc* d, const void* x, const float* weight, const float* bias, void* y,
@@ -194,21 +278,28 @@ extern "C" int cprune_group_norm_act(const cprune_norm_desc* d, const void* x, c
   if (!x || !y) return CPRUNE_ERR_INVALID_ARG;
   const NormGeom g = geometry(*d, false);
   if (too_many_groups(*d, g)) return CPRUNE_ERR_UNSUPPORTED;
-  if (!ws || ws_bytes < part_bytes(*d, g) + stats_bytes(*d)) return CPRUNE_ERR_WORKSPACE;
+  const size_t need = scratch_bytes(*d, g, false);
+  if (need && (!ws || ws_bytes < need)) return CPRUNE_ERR_WORKSPACE;
   hipStream_t s = static_cast<hipStream_t>(stream);
   NormArgs a = args_of(*d, g);
   a.x = x, a.y = y, a.weight = weight, a.bias = bias;
+  if (g.nv) {
+    a.mean_out = mean_out, a.rstd_out = rstd_out;
+    launch_whole(a, d->dtype, s);
+    CPRUNE_LAUNCH_CHECK();
+    return CPRUNE_OK;
+  }
   a.part = static_cast<float2*>(ws);
-  float* stats = reinterpret_cast<float*>(static_cast<char*>(ws) + part_bytes(*d, g));
+  float* stats = reinterpret_cast<float*>(static_cast<char*>(ws) + part_bytes(*d, g, false));
   float* mean = mean_out ? mean_out : stats;
   float* rstd = rstd_out ? rstd_out : stats + (size_t)d->n * d->groups;
   a.mean = mean, a.rstd = rstd;
-  const dim3 grid((unsigned)(d->n * g.chunks * g.tiles)), block(g.threads);
+  const unsigned grid = (unsigned)(d->n * g.chunks * g.tiles);
   with_form(d->dtype, g.V, d->act == CPRUNE_ACT_SILU, [&](auto t, auto v, auto silu) {
     using T = decltype(t);
-    norm_stats_kernel<T, decltype(v)::value><<<grid, block, 0, s>>>(a);
-    norm_join_stats_kernel<<<d->n * d->groups, norm::kThreads, 0, s>>>(a, d->eps, mean, rstd);
-    norm_apply_kernel<T, decltype(v)::value, decltype(silu)::value><<<grid, block, 0, s>>>(a);
+    norm_stats_kernel<T, decltype(v)::value><<<grid, norm::kThreads, 0, s>>>(a);
+    norm_join_stats_kernel<<<d->n * d->groups, join_threads(a), 0, s>>>(a, mean, rstd);
+    norm_apply_kernel<T, decltype(v)::value, decltype(silu)::value><<<grid, norm::kThreads, 0, s>>>(a);
   });
   CPRUNE_LAUNCH_CHECK();
   return CPRUNE_OK;
@@ -222,20 +313,28 @@ extern "C" int cprune_group_norm_act_backward(const cprune_norm_desc* d, const v
   if (!dy || !x || !mean || !rstd || !dx) return CPRUNE_ERR_INVALID_ARG;
   const NormGeom g = geometry(*d, true);
   if (too_many_groups(*d, g)) return CPRUNE_ERR_UNSUPPORTED;
-  if (!ws || ws_bytes < part_bytes(*d, g) + stats_bytes(*d)) return CPRUNE_ERR_WORKSPACE;
+  const size_t need = scratch_bytes(*d, g, true);
+  if (need && (!ws || ws_bytes < need)) return CPRUNE_ERR_WORKSPACE;
   hipStream_t s = static_cast<hipStream_t>(stream);
   NormArgs a = args_of(*d, g);
   a.x = x, a.dy = dy, a.y = dx, a.weight = weight, a.bias = bias, a.mean = mean, a.rstd = rstd;
+  a.dweight = dweight, a.dbias = dbias;
   a.part = static_cast<float2*>(ws);
-  float2* terms = reinterpret_cast<float2*>(static_cast<char*>(ws) + part_bytes(*d, g));
+  const unsigned vector_groups = dweight || dbias ? (unsigned)(d->c + 7) / 8 : 0u;
+  if (g.nv) {
+    launch_whole_grad(a, d->dtype, d->act == CPRUNE_ACT_SILU, s);
+    if (vector_groups && d->n > 1) norm_vectors_kernel<<<vector_groups, norm::kThreads, 0, s>>>(a);
+    CPRUNE_LAUNCH_CHECK();
+    return CPRUNE_OK;
+  }
+  float2* terms = reinterpret_cast<float2*>(static_cast<char*>(ws) + part_bytes(*d, g, true));
   a.terms = terms;
-  const dim3 grid((unsigned)(d->n * g.chunks * g.tiles)), block(g.threads);
-  const int sums = dweight || dbias ? (d->c + 31) / 32 : 0;
+  const unsigned grid = (unsigned)(d->n * g.chunks * g.tiles);
   with_form(d->dtype, g.V, d->act == CPRUNE_ACT_SILU, [&](auto t, auto v, auto silu) {
     using T = decltype(t);
-    norm_grad_sums_kernel<T, decltype(v)::value, decltype(silu)::value><<<grid, block, 0, s>>>(a);
-    norm_join_grads_kernel<<<d->n * d->groups + sums, norm::kThreads, 0, s>>>(a, d->n, terms, dweight, dbias);
-    norm_grad_apply_kernel<T, decltype(v)::value, decltype(silu)::value><<<grid, block, 0, s>>>(a);
+    norm_grad_sums_kernel<T, decltype(v)::value, decltype(silu)::value><<<grid, norm::kThreads, 0, s>>>(a);
+    norm_join_grads_kernel<<<d->n * d->groups, join_threads(a), 0, s>>>(a, terms);
+    norm_grad_apply_kernel<T, decltype(v)::value, decltype(silu)::value><<<grid + vector_groups, norm::kThreads, 0, s>>>(a, vector_groups);
   });
   CPRUNE_LAUNCH_CHECK();
   return CPRUNE_OK;

@@ -4,8 +4,12 @@
 // kernel, so that what belongs to a channel (weight, bias, statistics, sums) stays in registers.  Where V does not divide c and pixels lie
 // without gaps, a "superrow" of R = V / gcd(V, c) pixels is P = R c / V whole vectors; its element q is channel q mod c, and it
 // comes back every superrow.  83 channels of fp32: R = 4, P = 83.  Maps with gaps between pixels: R = 1 and the largest V that divides c.
-// A work-group is `rpi` superrows of `tp` vectors; it walks over a run ("chunk") of superrows of one image.  The last superrow of an image may hold fewer
-// than R pixels: its elements are checked one by one.  No alignment is assumed (loads of 16 bytes may begin at any element).
+// A work-group is `rpi` superrows of `tp` vectors.  The last superrow of an image may hold fewer than R pixels: its elements are checked one by one.  No
+// alignment is assumed (loads of 16 bytes may begin at any element).
+//
+// Two forms, one launch or three (two launches or three for the gradient), chosen by what an image's channels take:
+//  - whole: a work-group holds all pixels of some whole groups' channels in registers, so x is read once;
+//  - split: work-groups walk over runs ("chunks") of superrows of an image; sums of chunks are joined by a launch between, and x is read twice.
 #pragma once
 #include <type_traits>
 
@@ -13,12 +17,21 @@
 
 namespace cprune {
 
+// Division of numbers below `limit` by d: the high half of a product where that is exact (n d < 2^32), the instruction sequence otherwise.
+struct NormDiv {
+  unsigned d, magic;
+};
+inline NormDiv norm_div(long d, long limit) { return {(unsigned)d, d > 1 && limit * d < (1l << 32) ? (unsigned)(((1l << 32) + d - 1) / d) : 0u}; }
+
 struct NormGeom {
   int V, R, P;         // as above
   int tp, tiles, rpi;  // vectors of a superrow a work-group takes, work-groups side by side, superrows at a time
   int threads;
   int SR, spc, chunks;  // superrows of an image, of a chunk; chunks of an image
   int tail;             // pixels of the last superrow
+  NormDiv by_tp;        // of a thread's number
+  int few, more, last_r;   // whole form: superrows of a thread, one more for r < more; the r that has the last one
+  int slabs, nv;        // whole form: work-groups an image (of tp vectors a superrow each), vectors a thread holds
 };
 
 struct NormArgs {
@@ -26,11 +39,18 @@ struct NormArgs {
   const float *weight, *bias;
   const float *mean, *rstd;   // [n][g]
   const float2* terms;        // backward: (mean(w dz), mean(w dz xhat)) [n][g]
+  float *mean_out, *rstd_out; // whole form, or null
+  float eps;
+  float *dweight, *dbias;     // backward, or null
+  int n;
   void* y;                    // forward: y, backward: dx
   float2* part;               // [n][chunk][R * c]: forward (mean, squares about it), backward (sum dz, sum dz xhat)
   int pixels, c, cg, groups;
+  NormDiv by_cg;              // of a channel
+  double inv_count;           // 1 / (numbers of an (image, group))
   long x_image, x_pitch, dy_image, dy_pitch;   // elements from image to image, from superrow to superrow
   float lo, hi;               // clamp of the activation
+  int silu;                   // or this
   NormGeom g;
 };
 
@@ -101,63 +121,223 @@ __device__ __forceinline__ float argument(float xhat, float w, float b) {
   return p + b;
 }
 
-// What a thread works on.
+__device__ __forceinline__ int quotient(int n, const NormDiv& d) { return d.magic ? (int)__umulhi((unsigned)n, d.magic) : d.d == 1 ? n : (int)((unsigned)n / d.d); }
+
+// What a thread works on: vector p of the superrows sr0 + r, sr0 + r + rpi, ... below sr1.
 struct Place {
-  int image, chunk, r, p, sr0, sr1;
+  int image, part, r, p, sr0, sr1;      // part: chunk or slab
   bool active;
 };
-__device__ __forceinline__ Place place(const NormGeom& g) {
+__device__ __forceinline__ Place place(const NormGeom& g, unsigned block) {
   Place k;
-  unsigned b = blockIdx.x;
-  const int tile = (int)(b % (unsigned)g.tiles);
-  b /= (unsigned)g.tiles;
-  k.chunk = (int)(b % (unsigned)g.chunks);
-  k.image = (int)(b / (unsigned)g.chunks);
-  k.r = (int)threadIdx.x / g.tp;
+  const int tile = (int)(block % (unsigned)g.tiles);
+  block /= (unsigned)g.tiles;
+  k.part = (int)(block % (unsigned)g.chunks);
+  k.image = (int)(block / (unsigned)g.chunks);
+  k.r = quotient((int)threadIdx.x, g.by_tp);
   k.p = tile * g.tp + ((int)threadIdx.x - k.r * g.tp);
   k.active = k.r < g.rpi && k.p < g.P;
-  k.sr0 = k.chunk * g.spc;
+  k.sr0 = k.part * g.spc;
   k.sr1 = min(g.SR, k.sr0 + g.spc);
+  return k;
+}
+// Whole form.  Work-groups next to each other run on different XCDs; each XCD gets a run of (image, slab), so that slabs of an image, which share
+// cache lines where a slab is narrower than one, share an L2.
+__device__ __forceinline__ Place place_whole(const NormGeom& g) {
+  Place k;
+  const unsigned total = gridDim.x, xcd = blockIdx.x & 7, per = total >> 3, rest = total & 7;
+  const unsigned t = xcd * per + min(xcd, rest) + (blockIdx.x >> 3);
+  k.image = (int)(t / (unsigned)g.slabs);
+  k.part = (int)t - k.image * g.slabs;
+  k.r = quotient((int)threadIdx.x, g.by_tp);
+  const int q = (int)threadIdx.x - k.r * g.tp;
+  k.p = k.part * g.tp + q;
+  k.active = k.r < g.rpi;
+  k.sr0 = 0;
+  k.sr1 = g.SR;
   return k;
 }
 // elements of the vector at position p that superrow sr has
 __device__ __forceinline__ int valid_of(const NormGeom& g, int c, int sr, int p) {
   return sr == g.SR - 1 ? g.tail * c - p * g.V : g.V;
 }
+// superrows below which every element is there
+__device__ __forceinline__ int full_rows(const NormGeom& g) { return g.tail == g.R ? g.SR : g.SR - 1; }
 
 constexpr int kThreads = 256;
+// vectors under way at a time in the split form's loops
+template <int V> constexpr int kBatch = 8;
+
+// Sum of a pair over the superrows of a work-group, in threads of r = 0; buffer: V * threads / 2 pairs.  The upper half hands over to the lower one,
+// halving: a fixed order.
+template <int V> __device__ __forceinline__ void add_rows(float (&a)[V], float (&b)[V], int r, int tp, int rpi, bool active, float2* buffer) {
+  int half = 1;
+  while (2 * half < rpi) half *= 2;
+  const int stride = tp * max(rpi - half, half >> 1), t = (int)threadIdx.x;      // (threads that hand over, at most half of them)
+  if (rpi == 1) return;
+  for (int live = rpi; half > 0; live = half, half >>= 1) {
+    const bool gives = active && r >= half && r < live, takes = active && r < half && r + half < live;
+    if (gives) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) buffer[j * stride + t - half * tp] = make_float2(a[j], b[j]);
+    }
+    __syncthreads();
+    if (takes) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const float2 o = buffer[j * stride + t];
+        a[j] += o.x, b[j] += o.y;
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// channels and groups of a vector's elements, which begin at element q of a superrow: one division, then counted on
+template <int V> struct Where {
+  int ch[V], group[V];
+};
+template <int V> __device__ __forceinline__ Where<V> where(const NormArgs& a, int q) {
+  Where<V> k;
+  int ch = a.g.R == 1 ? q : q % a.c, group = quotient(ch, a.by_cg), left = a.cg - (ch - group * a.cg);      // (left: channels of the group from here on)
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    k.ch[j] = ch, k.group[j] = group;
+    ++ch;
+    if (--left == 0) {
+      left = a.cg, ++group;
+      if (ch == a.c) ch = 0, group = 0;
+    }
+  }
+  return k;
+}
+
+// weight, bias and statistics of a vector's elements
+template <int V> struct Terms {
+  float mean[V], rstd[V], w[V], b[V];
+};
+template <int V> __device__ __forceinline__ void channel_terms(const NormArgs& a, const Where<V>& at, Terms<V>& k) {
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    k.w[j] = a.weight ? a.weight[at.ch[j]] : 1.0f;
+    k.b[j] = a.bias ? a.bias[at.ch[j]] : 0.0f;
+  }
+}
+template <int V> __device__ __forceinline__ void all_terms(const NormArgs& a, int image, const Where<V>& at, Terms<V>& k) {
+  channel_terms<V>(a, at, k);
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    k.mean[j] = a.mean[image * a.groups + at.group[j]];
+    k.rstd[j] = a.rstd[image * a.groups + at.group[j]];
+  }
+}
+
+// mean and rstd from sums of (count, squares) about `first`
+__device__ __forceinline__ float2 statistics(double2 s, double first, const NormArgs& a) {
+  const double shift = s.x * a.inv_count, var = s.y * a.inv_count - shift * shift;
+  return make_float2((float)(first + shift), 1.0f / sqrtf((var < 0.0 ? 0.0f : (float)var) + a.eps));
+}
+
+// a vector of outputs; k.w holds weight * rstd
+template <typename T, int V, bool SILU, typename Raw> __device__ __forceinline__ void normalise(const NormArgs& a, const Raw& raw, const Terms<V>& k, char* out, int valid) {
+  float v[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) v[j] = activate<SILU>(fmaf(widen<T>(raw[j]) - k.mean[j], k.w[j], k.b[j]), a.lo, a.hi);
+  store<T, V>(out, v, valid);
+}
+template <typename T, int V, bool SILU, typename Raw> __device__ __forceinline__ void gradient(const NormArgs& a, const Raw& x, const Raw& dy, const Terms<V>& k, const float2 (&t)[V], char* out, int valid) {
+  float v[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const float xhat = centred(widen<T>(x[j]), k.mean[j], k.rstd[j]);
+    const float dz = widen<T>(dy[j]) * slope<SILU>(argument(xhat, k.w[j], k.b[j]), a.lo, a.hi);
+    v[j] = k.rstd[j] * (fmaf(k.w[j], dz, -t[j].x) - xhat * t[j].y);
+  }
+  store<T, V>(out, v, valid);
+}
+template <typename T, int V, bool SILU, typename Raw> __device__ __forceinline__ void gradient_sums(const NormArgs& a, const Raw& x, const Raw& dy, const Terms<V>& k, float (&sb)[V], float (&sw)[V], int valid) {
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const float xhat = centred(widen<T>(x[j]), k.mean[j], k.rstd[j]);
+    const float dz = widen<T>(dy[j]) * slope<SILU>(argument(xhat, k.w[j], k.b[j]), a.lo, a.hi);
+    if (j < valid) {      // (elements past the image: zeros may still have a slope)
+      sb[j] += dz;
+      sw[j] = fmaf(dz, xhat, sw[j]);
+    }
+  }
+}
 
 }  // namespace norm
 
-// Statistics of a chunk: each thread's running mean and squares about it (an update by 1 / count per number: no difference of large sums, whatever
+// ---- split form ----------------------------------------------------------------------------------
+
+// Statistics of a chunk: each thread's running mean and squares about it, four numbers at a time about their own mean (no difference of large sums, whatever
 // the numbers' mean), then joined over the work-group's superrows pair by pair.
 template <typename T, int V>
 __global__ __launch_bounds__(norm::kThreads) void norm_stats_kernel(const NormArgs a) {
   using namespace norm;
+  constexpr int U = kBatch<V>;
   __shared__ float s_mean[V][kThreads], s_sq[V][kThreads], s_n[V][kThreads];
-  const Place k = place(a.g);
+  const Place k = place(a.g, blockIdx.x);
   float mean[V], sq[V], cnt[V];
 #pragma unroll
-  for (int j = 0; j < V; ++j) mean[j] = sq[j] = cnt[j] = 0.0f;
+  for (int j = 0; j < V; ++j) mean[j] = sq[j] = 0.0f;
+  float n = 0.0f;
+  int missing = V;      // elements from this one on lack the last vector
   if (k.active) {
     const char* base = static_cast<const char*>(a.x) + (k.image * a.x_image + (long)k.p * V) * (long)sizeof(T);
-    int i = 0;
-    for (int sr = k.sr0 + k.r; sr < k.sr1; sr += a.g.rpi, ++i) {
-      const int valid = valid_of(a.g, a.c, sr, k.p);
-      if (valid <= 0) break;
-      const auto raw = load<T, V>(base + sr * a.x_pitch * (long)sizeof(T), valid);
-      const float rc = __builtin_amdgcn_rcpf((float)(i + 1));
+    const long pitch = a.x_pitch * (long)sizeof(T);
+    const int step = a.g.rpi, full = min(k.sr1, full_rows(a.g));
+    auto one = [&](const auto& raw, int valid) __attribute__((always_inline)) {
+      n += 1.0f;
+      const float rc = __builtin_amdgcn_rcpf(n);
 #pragma unroll
       for (int j = 0; j < V; ++j) {
         if (j < valid) {
           const float v = widen<T>(raw[j]), d = v - mean[j];
           mean[j] = fmaf(d, rc, mean[j]);
           sq[j] = fmaf(d, v - mean[j], sq[j]);
-          cnt[j] += 1.0f;
         }
       }
+    };
+    typename RawOf<typename Bits<T>::type, V>::type raw[U];
+    int sr = k.sr0 + k.r;
+    for (; sr + (U - 1) * step < full; sr += U * step) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) raw[u] = load<T, V>(base + (sr + u * step) * pitch, V);
+      const float f = (float)U * __builtin_amdgcn_rcpf(n + (float)U), nf = n * f;
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        float m = 0.0f, q = 0.0f;
+#pragma unroll
+        for (int u = 0; u < U; ++u) m += widen<T>(raw[u][j]);
+        m *= 1.0f / U;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const float d = widen<T>(raw[u][j]) - m;
+          q = fmaf(d, d, q);
+        }
+        const float d = m - mean[j];
+        mean[j] = fmaf(d, f, mean[j]);
+        sq[j] += fmaf(d * d, nf, q);
+      }
+      n += (float)U;
+    }
+    // what is left: the loads together all the same
+#pragma unroll
+    for (int u = 0; u < U - 1; ++u)
+      if (sr + u * step < full) raw[u] = load<T, V>(base + (sr + u * step) * pitch, V);
+#pragma unroll
+    for (int u = 0; u < U - 1; ++u)
+      if (sr + u * step < full) one(raw[u], V);
+    const int end = a.g.SR - 1, valid = valid_of(a.g, a.c, end, k.p);
+    if (full < k.sr1 && (unsigned)(end - k.sr0) % (unsigned)step == (unsigned)k.r && valid > 0) {
+      one(load<T, V>(base + end * pitch, valid), valid);
+      missing = valid;
     }
   }
+#pragma unroll
+  for (int j = 0; j < V; ++j) cnt[j] = j < missing ? n : n - 1.0f;
   const int t = threadIdx.x;
   int half = 1;
   while (2 * half < a.g.rpi) half *= 2;
@@ -169,19 +349,19 @@ __global__ __launch_bounds__(norm::kThreads) void norm_stats_kernel(const NormAr
       const int o = t + half * a.g.tp;
 #pragma unroll
       for (int j = 0; j < V; ++j) {
-        const float nb = s_n[j][o], n = cnt[j] + nb;
+        const float nb = s_n[j][o], sum = cnt[j] + nb;
         if (nb > 0.0f) {
-          const float d = s_mean[j][o] - mean[j], f = nb / n;
+          const float d = s_mean[j][o] - mean[j], f = nb / sum;
           mean[j] = fmaf(d, f, mean[j]);
           sq[j] += s_sq[j][o] + d * d * cnt[j] * f;
-          cnt[j] = n;
+          cnt[j] = sum;
         }
         s_mean[j][t] = mean[j], s_sq[j][t] = sq[j], s_n[j][t] = cnt[j];
       }
     }
   }
   if (k.active && k.r == 0) {
-    float2* out = a.part + ((long)k.image * a.g.chunks + k.chunk) * a.g.P * V + (long)k.p * V;
+    float2* out = a.part + ((long)k.image * a.g.chunks + k.part) * a.g.P * V + (long)k.p * V;
 #pragma unroll
     for (int j = 0; j < V; ++j) out[j] = make_float2(mean[j], sq[j]);
   }
@@ -190,26 +370,34 @@ __global__ __launch_bounds__(norm::kThreads) void norm_stats_kernel(const NormAr
 template <typename T, int V, bool SILU>
 __global__ __launch_bounds__(norm::kThreads) void norm_apply_kernel(const NormArgs a) {
   using namespace norm;
-  const Place k = place(a.g);
+  constexpr int U = kBatch<V>;
+  const Place k = place(a.g, blockIdx.x);
   if (!k.active) return;
-  float mean[V], w[V], b[V];
+  Terms<V> c;
+  all_terms<V>(a, k.image, where<V>(a, k.p * V), c);
 #pragma unroll
-  for (int j = 0; j < V; ++j) {
-    const int ch = (k.p * V + j) % a.c, s = k.image * a.groups + ch / a.cg;
-    mean[j] = a.mean[s];
-    w[j] = a.rstd[s] * (a.weight ? a.weight[ch] : 1.0f);
-    b[j] = a.bias ? a.bias[ch] : 0.0f;
-  }
+  for (int j = 0; j < V; ++j) c.w[j] *= c.rstd[j];
   const char* base = static_cast<const char*>(a.x) + (k.image * a.x_image + (long)k.p * V) * (long)sizeof(T);
   char* out = static_cast<char*>(a.y) + ((long)k.image * a.pixels * a.c + (long)k.p * V) * (long)sizeof(T);
-  for (int sr = k.sr0 + k.r; sr < k.sr1; sr += a.g.rpi) {
-    const int valid = valid_of(a.g, a.c, sr, k.p);
-    if (valid <= 0) break;
-    const auto raw = load<T, V>(base + sr * a.x_pitch * (long)sizeof(T), valid);
-    float v[V];
+  const long pitch = a.x_pitch * (long)sizeof(T), out_pitch = (long)a.g.P * V * (long)sizeof(T);
+  const int step = a.g.rpi, full = min(k.sr1, full_rows(a.g));
+  int sr = k.sr0 + k.r;
+  typename RawOf<typename Bits<T>::type, V>::type raw[U];
+  for (; sr + (U - 1) * step < full; sr += U * step) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) v[j] = activate<SILU>(fmaf(widen<T>(raw[j]) - mean[j], w[j], b[j]), a.lo, a.hi);
-    store<T, V>(out + (long)sr * a.g.P * V * (long)sizeof(T), v, valid);
+    for (int u = 0; u < U; ++u) raw[u] = load<T, V>(base + (sr + u * step) * pitch, V);
+#pragma unroll
+    for (int u = 0; u < U; ++u) normalise<T, V, SILU>(a, raw[u], c, out + (sr + u * step) * out_pitch, V);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int at = sr + u * step, valid = at < k.sr1 ? valid_of(a.g, a.c, at, k.p) : 0;
+    if (valid > 0) raw[u] = load<T, V>(base + at * pitch, valid);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int at = sr + u * step, valid = at < k.sr1 ? valid_of(a.g, a.c, at, k.p) : 0;
+    if (valid > 0) normalise<T, V, SILU>(a, raw[u], c, out + at * out_pitch, valid);
   }
 }
 
@@ -217,94 +405,351 @@ __global__ __launch_bounds__(norm::kThreads) void norm_apply_kernel(const NormAr
 template <typename T, int V, bool SILU>
 __global__ __launch_bounds__(norm::kThreads) void norm_grad_sums_kernel(const NormArgs a) {
   using namespace norm;
-  __shared__ float s_b[V][kThreads], s_w[V][kThreads];
-  const Place k = place(a.g);
+  constexpr int U = kBatch<V> / 2;
+  __shared__ float2 buffer[V * kThreads / 2];
+  const Place k = place(a.g, blockIdx.x);
   float sb[V], sw[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) sb[j] = sw[j] = 0.0f;
   if (k.active) {
-    float mean[V], rstd[V], w[V], b[V];
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const int ch = (k.p * V + j) % a.c, s = k.image * a.groups + ch / a.cg;
-      mean[j] = a.mean[s];
-      rstd[j] = a.rstd[s];
-      w[j] = a.weight ? a.weight[ch] : 1.0f;
-      b[j] = a.bias ? a.bias[ch] : 0.0f;
-    }
+    Terms<V> c;
+    all_terms<V>(a, k.image, where<V>(a, k.p * V), c);
     const char* xb = static_cast<const char*>(a.x) + (k.image * a.x_image + (long)k.p * V) * (long)sizeof(T);
     const char* db = static_cast<const char*>(a.dy) + (k.image * a.dy_image + (long)k.p * V) * (long)sizeof(T);
-    for (int sr = k.sr0 + k.r; sr < k.sr1; sr += a.g.rpi) {
-      const int valid = valid_of(a.g, a.c, sr, k.p);
-      if (valid <= 0) break;
-      const auto xr = load<T, V>(xb + sr * a.x_pitch * (long)sizeof(T), valid);
-      const auto dr = load<T, V>(db + sr * a.dy_pitch * (long)sizeof(T), valid);
+    const long pitch = a.x_pitch * (long)sizeof(T), dy_pitch = a.dy_pitch * (long)sizeof(T);
+    const int step = a.g.rpi, full = min(k.sr1, full_rows(a.g));
+    int sr = k.sr0 + k.r;
+    typename RawOf<typename Bits<T>::type, V>::type x[U], dy[U];
+    for (; sr + (U - 1) * step < full; sr += U * step) {
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        if (j < valid) {
-          const float xhat = centred(widen<T>(xr[j]), mean[j], rstd[j]);
-          const float dz = widen<T>(dr[j]) * slope<SILU>(argument(xhat, w[j], b[j]), a.lo, a.hi);
-          sb[j] += dz;
-          sw[j] = fmaf(dz, xhat, sw[j]);
-        }
-      }
+      for (int u = 0; u < U; ++u) x[u] = load<T, V>(xb + (sr + u * step) * pitch, V), dy[u] = load<T, V>(db + (sr + u * step) * dy_pitch, V);
+#pragma unroll
+      for (int u = 0; u < U; ++u) gradient_sums<T, V, SILU>(a, x[u], dy[u], c, sb, sw, V);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int at = sr + u * step, valid = at < k.sr1 ? valid_of(a.g, a.c, at, k.p) : 0;
+      if (valid > 0) x[u] = load<T, V>(xb + at * pitch, valid), dy[u] = load<T, V>(db + at * dy_pitch, valid);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int at = sr + u * step, valid = at < k.sr1 ? valid_of(a.g, a.c, at, k.p) : 0;
+      if (valid > 0) gradient_sums<T, V, SILU>(a, x[u], dy[u], c, sb, sw, valid);
     }
   }
-  const int t = threadIdx.x;
-  int half = 1;
-  while (2 * half < a.g.rpi) half *= 2;
-#pragma unroll
-  for (int j = 0; j < V; ++j) s_b[j][t] = sb[j], s_w[j][t] = sw[j];
-  for (; half > 0; half >>= 1) {
-    __syncthreads();
-    if (k.active && k.r < half && k.r + half < a.g.rpi) {
-      const int o = t + half * a.g.tp;
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        s_b[j][t] = sb[j] += s_b[j][o];
-        s_w[j][t] = sw[j] += s_w[j][o];
-      }
-    }
-  }
+  add_rows<V>(sb, sw, k.r, a.g.tp, a.g.rpi, k.active, buffer);
   if (k.active && k.r == 0) {
-    float2* out = a.part + ((long)k.image * a.g.chunks + k.chunk) * a.g.P * V + (long)k.p * V;
+    float2* out = a.part + ((long)k.image * a.g.chunks + k.part) * a.g.P * V + (long)k.p * V;
 #pragma unroll
     for (int j = 0; j < V; ++j) out[j] = make_float2(sb[j], sw[j]);
   }
 }
 
+// dweight and dbias of eight channels from all images' partial sums, `per` rows of c of them an image; 32 threads a channel, 64 bits, a fixed order.
+__device__ inline void norm_vector_sums(const NormArgs& a, unsigned block, long count) {
+  __shared__ double2 sums[32][8];
+  const int ch = (int)block * 8 + ((int)threadIdx.x & 7), lane = (int)threadIdx.x >> 3;
+  double2 s = {0.0, 0.0};
+  if (ch < a.c) {
+    long i = lane;
+    for (; i + 7 * 32 < count; i += 8 * 32) {
+      float2 p[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) p[u] = a.part[(i + u * 32) * a.c + ch];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) s.x += p[u].x, s.y += p[u].y;
+    }
+    for (; i < count; i += 32) {
+      const float2 p = a.part[i * a.c + ch];
+      s.x += p.x, s.y += p.y;
+    }
+  }
+  sums[lane][threadIdx.x & 7] = s;
+  __syncthreads();
+  if (lane == 0 && ch < a.c) {
+    for (int i = 1; i < 32; ++i) s.x += sums[i][threadIdx.x].x, s.y += sums[i][threadIdx.x].y;
+    if (a.dbias) a.dbias[ch] = (float)s.x;
+    if (a.dweight) a.dweight[ch] = (float)s.y;
+  }
+}
+
+__global__ __launch_bounds__(norm::kThreads) inline void norm_vectors_kernel(const NormArgs a) { norm_vector_sums(a, blockIdx.x, a.n); }
+
+// The first `vector_groups` work-groups sum dweight and dbias (few numbers, long chains: beside the others they cost nothing), the others dx.
 template <typename T, int V, bool SILU>
-__global__ __launch_bounds__(norm::kThreads) void norm_grad_apply_kernel(const NormArgs a) {
+__global__ __launch_bounds__(norm::kThreads) void norm_grad_apply_kernel(const NormArgs a, unsigned vector_groups) {
   using namespace norm;
-  const Place k = place(a.g);
+  constexpr int U = kBatch<V> / 2;
+  if (blockIdx.x < vector_groups) {
+    norm_vector_sums(a, blockIdx.x, (long)a.n * a.g.chunks * a.g.R);
+    return;
+  }
+  const Place k = place(a.g, blockIdx.x - vector_groups);
   if (!k.active) return;
-  float mean[V], rstd[V], w[V], b[V];
+  Terms<V> c;
+  const Where<V> here = where<V>(a, k.p * V);
+  all_terms<V>(a, k.image, here, c);
   float2 t[V];
 #pragma unroll
-  for (int j = 0; j < V; ++j) {
-    const int ch = (k.p * V + j) % a.c, s = k.image * a.groups + ch / a.cg;
-    mean[j] = a.mean[s];
-    rstd[j] = a.rstd[s];
-    w[j] = a.weight ? a.weight[ch] : 1.0f;
-    b[j] = a.bias ? a.bias[ch] : 0.0f;
-    t[j] = a.terms[s];
-  }
+  for (int j = 0; j < V; ++j) t[j] = a.terms[k.image * a.groups + here.group[j]];
   const char* xb = static_cast<const char*>(a.x) + (k.image * a.x_image + (long)k.p * V) * (long)sizeof(T);
   const char* db = static_cast<const char*>(a.dy) + (k.image * a.dy_image + (long)k.p * V) * (long)sizeof(T);
   char* out = static_cast<char*>(a.y) + ((long)k.image * a.pixels * a.c + (long)k.p * V) * (long)sizeof(T);
-  for (int sr = k.sr0 + k.r; sr < k.sr1; sr += a.g.rpi) {
-    const int valid = valid_of(a.g, a.c, sr, k.p);
-    if (valid <= 0) break;
-    const auto xr = load<T, V>(xb + sr * a.x_pitch * (long)sizeof(T), valid);
-    const auto dr = load<T, V>(db + sr * a.dy_pitch * (long)sizeof(T), valid);
-    float v[V];
+  const long pitch = a.x_pitch * (long)sizeof(T), dy_pitch = a.dy_pitch * (long)sizeof(T), out_pitch = (long)a.g.P * V * (long)sizeof(T);
+  const int step = a.g.rpi, full = min(k.sr1, full_rows(a.g));
+  int sr = k.sr0 + k.r;
+  typename RawOf<typename Bits<T>::type, V>::type x[U], dy[U];
+  for (; sr + (U - 1) * step < full; sr += U * step) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const float xhat = centred(widen<T>(xr[j]), mean[j], rstd[j]);
-      const float dz = widen<T>(dr[j]) * slope<SILU>(argument(xhat, w[j], b[j]), a.lo, a.hi);
-      v[j] = rstd[j] * (fmaf(w[j], dz, -t[j].x) - xhat * t[j].y);
+    for (int u = 0; u < U; ++u) x[u] = load<T, V>(xb + (sr + u * step) * pitch, V), dy[u] = load<T, V>(db + (sr + u * step) * dy_pitch, V);
+#pragma unroll
+    for (int u = 0; u < U; ++u) gradient<T, V, SILU>(a, x[u], dy[u], c, t, out + (sr + u * step) * out_pitch, V);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int at = sr + u * step, valid = at < k.sr1 ? valid_of(a.g, a.c, at, k.p) : 0;
+    if (valid > 0) x[u] = load<T, V>(xb + at * pitch, valid), dy[u] = load<T, V>(db + at * dy_pitch, valid);
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int at = sr + u * step, valid = at < k.sr1 ? valid_of(a.g, a.c, at, k.p) : 0;
+    if (valid > 0) gradient<T, V, SILU>(a, x[u], dy[u], c, t, out + at * out_pitch, valid);
+  }
+}
+
+// ---- whole form ----------------------------------------------------------------------------------
+// V numbers are 16 bytes; a thread holds NV vectors.
+
+namespace norm {
+
+// Sum over a group of pairs f(i) of its `outer` x `inner` entries, in 64 bits, by `lanes` neighbouring lanes (a power of two up to 64); all of them get it.
+template <typename F> __device__ __forceinline__ double2 lanes_sum(int lane, int lanes, int outer, int inner, F&& f) {
+  double2 s = {0.0, 0.0};
+  const int skip = lanes / inner, step = lanes - skip * inner;
+  int o = lane / inner, in = lane - o * inner;
+  while (o < outer) {
+    const double2 v = f(o, in);
+    s.x += v.x, s.y += v.y;
+    o += skip, in += step;
+    if (in >= inner) in -= inner, ++o;
+  }
+  for (int m = lanes >> 1; m > 0; m >>= 1) {
+    s.x += __shfl_xor(s.x, m, 64);
+    s.y += __shfl_xor(s.y, m, 64);
+  }
+  return s;
+}
+
+// lanes of a group so that `groups` of them fill the work-group
+__device__ __forceinline__ int lanes_of(int groups) {
+  int lanes = 64;
+  while (lanes > 1 && lanes * groups > (int)blockDim.x) lanes >>= 1;
+  return lanes;
+}
+
+}  // namespace norm
+
+// MERGE: V divides a group's channels, so a thread's numbers are of one group.
+template <typename T, int NV, bool MERGE>
+__global__ __launch_bounds__(1024) void norm_whole_kernel(const NormArgs a) {
+  using namespace norm;
+  constexpr int V = 16 / (int)sizeof(T);
+  extern __shared__ char lds[];
+  const Place k = place_whole(a.g);
+  const int cols = a.g.tp * V, groups = a.groups / a.g.slabs;      // of the slab
+  float2* const part = reinterpret_cast<float2*>(lds);              // [r][vector or element]: (mean, squares)
+  float2* const stat = part + (MERGE ? a.g.tp : cols) * a.g.rpi;    // [group]: (mean, rstd)
+  const char* base = static_cast<const char*>(a.x) + (k.image * a.x_image + (long)k.p * V) * (long)sizeof(T);
+  const long pitch = a.x_pitch * (long)sizeof(T);
+  typename RawOf<typename Bits<T>::type, V>::type raw[NV];
+  Terms<V> c;
+  Where<V> here;
+  if (k.active) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int sr = k.r + i * a.g.rpi;
+      const int valid = sr < a.g.SR ? valid_of(a.g, a.c, sr, k.p) : 0;
+      if (valid > 0) raw[i] = load<T, V>(base + sr * pitch, valid);
     }
-    store<T, V>(out + (long)sr * a.g.P * V * (long)sizeof(T), v, valid);
+    here = where<V>(a, k.p * V);
+    channel_terms<V>(a, here, c);
+    // superrows of this thread; the last one of the image may lack elements
+    const int rows = a.g.few + (k.r < a.g.more ? 1 : 0);
+    const int last = k.r == a.g.last_r ? valid_of(a.g, a.c, a.g.SR - 1, k.p) : V;      // elements of its last vector
+    if constexpr (MERGE) {
+      float m = 0.0f, q = 0.0f;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (i < rows)
+#pragma unroll
+          for (int j = 0; j < V; ++j) m += widen<T>(raw[i][j]);
+      m *= __builtin_amdgcn_rcpf((float)max(rows * V, 1));
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (i < rows)
+#pragma unroll
+          for (int j = 0; j < V; ++j) {
+            const float d = widen<T>(raw[i][j]) - m;
+            q = fmaf(d, d, q);
+          }
+      part[threadIdx.x] = make_float2(m, q);
+    } else {
+      const float all = __builtin_amdgcn_rcpf((float)max(rows, 1)), less = __builtin_amdgcn_rcpf((float)max(rows - 1, 1));
+#pragma unroll
+      for (int j = 0; j < V; ++j) {
+        const int have = j < last ? rows : rows - 1;
+        float m = 0.0f, q = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+          if (i < have) m += widen<T>(raw[i][j]);
+        m *= j < last ? all : less;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+          if (i < have) {
+            const float d = widen<T>(raw[i][j]) - m;
+            q = fmaf(d, d, q);
+          }
+        part[k.r * cols + ((int)threadIdx.x - k.r * a.g.tp) * V + j] = make_float2(m, q);
+      }
+    }
+  }
+  __syncthreads();
+  {
+    const int lanes = lanes_of(groups), lane = (int)threadIdx.x & (lanes - 1), per = (int)blockDim.x / lanes;
+    const int more = a.g.more, few = a.g.few, last_r = a.g.last_r;
+    for (int g = (int)threadIdx.x / lanes; g < groups; g += per) {
+      double2 s;
+      double first;
+      if constexpr (MERGE) {
+        const int vg = a.cg / V;
+        first = part[g * vg].x;
+        s = lanes_sum(lane, lanes, a.g.rpi, vg, [&](int r, int v) __attribute__((always_inline)) {
+          const float2 e = part[r * a.g.tp + g * vg + v];
+          const double n = (few + (r < more ? 1 : 0)) * V, d = (double)e.x - first;
+          return n > 0.0 ? make_double2(n * d, (double)e.y + n * d * d) : make_double2(0.0, 0.0);
+        });
+      } else {
+        first = part[g * a.cg].x;
+        s = lanes_sum(lane, lanes, a.g.rpi * a.g.R, a.cg, [&](int o, int ch) __attribute__((always_inline)) {
+          const int r = a.g.R == 1 ? o : o / a.g.R, rr = o - r * a.g.R;
+          const float2 e = part[r * cols + rr * a.c + g * a.cg + ch];
+          const double n = few + (r < more ? 1 : 0) - (r == last_r && rr >= a.g.tail ? 1 : 0), d = (double)e.x - first;
+          return n > 0.0 ? make_double2(n * d, (double)e.y + n * d * d) : make_double2(0.0, 0.0);
+        });
+      }
+      if (lane == 0) {
+        const float2 m = statistics(s, first, a);
+        const float mean = m.x, rstd = m.y;
+        stat[g] = make_float2(mean, rstd);
+        const int at = k.image * a.groups + k.part * groups + g;
+        if (a.mean_out) a.mean_out[at] = mean;
+        if (a.rstd_out) a.rstd_out[at] = rstd;
+      }
+    }
+  }
+  __syncthreads();
+  if (!k.active) return;
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    const float2 s = stat[here.group[MERGE ? 0 : j] - k.part * groups];
+    c.mean[j] = s.x;
+    c.w[j] *= s.y;
+  }
+  char* out = static_cast<char*>(a.y) + ((long)k.image * a.pixels * a.c + (long)k.p * V) * (long)sizeof(T);
+  const long out_pitch = (long)a.g.P * V * (long)sizeof(T);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int sr = k.r + i * a.g.rpi;
+    const int valid = sr < a.g.SR ? valid_of(a.g, a.c, sr, k.p) : 0;
+    if (valid > 0) {
+      if (a.silu) normalise<T, V, true>(a, raw[i], c, out + sr * out_pitch, valid);
+      else normalise<T, V, false>(a, raw[i], c, out + sr * out_pitch, valid);
+    }
+  }
+}
+
+// The gradient; dweight and dbias go to `part` [n][c] as an image's sums (or straight to their place where there is one image).
+template <typename T, int NV, bool SILU>
+__global__ __launch_bounds__(1024) void norm_whole_grad_kernel(const NormArgs a) {
+  using namespace norm;
+  constexpr int V = 16 / (int)sizeof(T);
+  extern __shared__ char lds[];
+  const Place k = place_whole(a.g);
+  const int cols = a.g.tp * V, groups = a.groups / a.g.slabs, channels = groups * a.cg;      // of the slab
+  float2* const buffer = reinterpret_cast<float2*>(lds);
+  float2* const col = buffer;                                // [element of the superrow]: sums (the buffer is free by then)
+  float2* const term = buffer + cols;                        // [group]
+  const char* xb = static_cast<const char*>(a.x) + (k.image * a.x_image + (long)k.p * V) * (long)sizeof(T);
+  const char* db = static_cast<const char*>(a.dy) + (k.image * a.dy_image + (long)k.p * V) * (long)sizeof(T);
+  const long pitch = a.x_pitch * (long)sizeof(T), dy_pitch = a.dy_pitch * (long)sizeof(T);
+  typename RawOf<typename Bits<T>::type, V>::type x[NV], dy[NV];
+  Terms<V> c;
+  Where<V> here;
+  float sb[V], sw[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) sb[j] = sw[j] = 0.0f;
+  if (k.active) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int sr = k.r + i * a.g.rpi;
+      const int valid = sr < a.g.SR ? valid_of(a.g, a.c, sr, k.p) : 0;
+      if (valid > 0) {
+        x[i] = load<T, V>(xb + sr * pitch, valid);
+        dy[i] = load<T, V>(db + sr * dy_pitch, valid);
+      }
+    }
+    here = where<V>(a, k.p * V);
+    all_terms<V>(a, k.image, here, c);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int sr = k.r + i * a.g.rpi;
+      const int valid = sr < a.g.SR ? valid_of(a.g, a.c, sr, k.p) : 0;
+      if (valid > 0) gradient_sums<T, V, SILU>(a, x[i], dy[i], c, sb, sw, valid);
+    }
+  }
+  add_rows<V>(sb, sw, k.r, a.g.tp, a.g.rpi, k.active, buffer);
+  const int q0 = ((int)threadIdx.x) * V;
+  if (k.active && k.r == 0) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) col[q0 + j] = make_float2(sb[j], sw[j]);
+  }
+  __syncthreads();
+  const int ch0 = k.part * channels;
+  if (a.dweight || a.dbias) {
+    for (int ch = threadIdx.x; ch < channels; ch += blockDim.x) {
+      float2 s = col[ch];
+      for (int rr = 1; rr < a.g.R; ++rr) s.x += col[rr * a.c + ch].x, s.y += col[rr * a.c + ch].y;
+      if (a.n > 1) {
+        a.part[(long)k.image * a.c + ch0 + ch] = s;
+      } else {
+        if (a.dbias) a.dbias[ch0 + ch] = s.x;
+        if (a.dweight) a.dweight[ch0 + ch] = s.y;
+      }
+    }
+  }
+  {
+    const int lanes = lanes_of(groups), lane = (int)threadIdx.x & (lanes - 1), per = (int)blockDim.x / lanes;
+    for (int g = (int)threadIdx.x / lanes; g < groups; g += per) {
+      const double2 s = lanes_sum(lane, lanes, a.g.R, a.cg, [&](int rr, int ch) __attribute__((always_inline)) {
+        const float2 e = col[rr * a.c + g * a.cg + ch];
+        const double w = a.weight ? a.weight[ch0 + g * a.cg + ch] : 1.0f;
+        return make_double2(w * e.x, w * e.y);
+      });
+      if (lane == 0) term[g] = make_float2((float)(s.x * a.inv_count), (float)(s.y * a.inv_count));
+    }
+  }
+  __syncthreads();
+  if (!k.active) return;
+  float2 t[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) t[j] = term[here.group[j] - k.part * groups];
+  char* out = static_cast<char*>(a.y) + ((long)k.image * a.pixels * a.c + (long)k.p * V) * (long)sizeof(T);
+  const long out_pitch = (long)a.g.P * V * (long)sizeof(T);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int sr = k.r + i * a.g.rpi;
+    const int valid = sr < a.g.SR ? valid_of(a.g, a.c, sr, k.p) : 0;
+    if (valid > 0) gradient<T, V, SILU>(a, x[i], dy[i], c, t, out + sr * out_pitch, valid);
   }
 }
 

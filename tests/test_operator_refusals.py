@@ -34,7 +34,7 @@ def test_norm_gradient_refuses(kw):
 
 
 def test_norm_refuses_missing_pointers_and_scratch():
-    L, d = B.lib(), _norm()
+    L, d = B.lib(), _norm(n=2, pixels=1 << 16, c=12)      # (a map that needs scratch)
     need, back = L.cprune_group_norm_workspace_bytes(d, 0), L.cprune_group_norm_workspace_bytes(d, 1)
     assert need > 0 and back > 0
     f = lambda x=FAKE, y=FAKE, ws=FAKE, size=need: L.cprune_group_norm_act(d, x, None, None, y, None, None, ws, size, None)
