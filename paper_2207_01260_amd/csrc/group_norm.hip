@@ -53,17 +53,15 @@ template <typename F> __device__ __forceinline__ double2 entries_sum(const NormA
   return s;
 }
 
-// The chunks' statistics as those of an (image, group): sums over (count, mean, squares) about the first mean.
+// The chunks' statistics as those of an (image, group).
 __global__ __launch_bounds__(1024) void norm_join_stats_kernel(const NormArgs a, float* __restrict__ mean_out, float* __restrict__ rstd_out) {
   const int image = blockIdx.x / (unsigned)a.groups, group = blockIdx.x - image * a.groups;
   const float2* part = a.part + (long)image * a.g.chunks * a.g.R * a.c + group * a.cg;
-  const double first = part[0].x;
   const double2 s = entries_sum(a, part, [&](int chunk, int rr, int, float2 e) __attribute__((always_inline)) {
-    const double n = chunk_count(a.g, chunk, rr), d = (double)e.x - first;
-    return n > 0.0 ? make_double2(n * d, (double)e.y + n * d * d) : make_double2(0.0, 0.0);
+    return norm::raw_sums((double)chunk_count(a.g, chunk, rr), e);
   });
   if (threadIdx.x == 0) {
-    const float2 m = norm::statistics(s, first, a);
+    const float2 m = norm::statistics(s, a);
     mean_out[blockIdx.x] = m.x;
     rstd_out[blockIdx.x] = m.y;
   }
@@ -95,11 +93,17 @@ int vector_of(int c, int dtype, bool dense) {
   return v;
 }
 
-constexpr int kWholeVectors = 16, kWholeGradVectors = 8;      // a thread holds at most, of x or of x and dy each
-constexpr int kWholeColumns = 4096;                           // elements of a slab's superrow (LDS)
+constexpr int kWholeColumns = 4096;      // elements of a slab's superrow (LDS)
+
+// Lanes that sum one of `groups` groups so that they fill the threads: a power of two up to a wavefront.
+int lanes_of(int groups, int threads) {
+  int lanes = 64;
+  while (lanes > 1 && lanes * groups > threads) lanes /= 2;
+  return lanes;
+}
 
 // Work-groups of the whole form for a slab of `tp` vectors a superrow: as few threads as hold four vectors each, or up to the most.  false: too much.
-bool fit_whole(NormGeom& g, int tp, int most_threads, int most_vectors) {
+bool fit_whole(NormGeom& g, int tp, int cg, int most_threads, int most_vectors) {
   if (tp > most_threads || (long)tp * g.V > kWholeColumns) return false;
   for (int t = 256; t <= most_threads; t *= 2) {
     if (t < tp) continue;
@@ -109,6 +113,8 @@ bool fit_whole(NormGeom& g, int tp, int most_threads, int most_vectors) {
       g.threads = (tp * rpi + 63) / 64 * 64;
       g.few = g.SR / rpi, g.more = g.SR % rpi, g.last_r = (g.SR - 1) % rpi;
       g.by_tp = norm_div(tp, 1024);
+      g.groups = tp * g.V / (g.R * cg);
+      g.lanes = lanes_of(g.groups, g.threads);
       return true;
     }
   }
@@ -122,12 +128,12 @@ bool choose_whole(const cprune_norm_desc& d, bool backward, NormGeom& g) {
   if (g.V != v) return false;
   const bool merge = cg % v == 0;
   const int most_threads = backward || merge || v == 4 ? 1024 : 512;      // (LDS: a pair a thread, or one for each of its elements)
-  const int most_vectors = backward ? kWholeGradVectors : kWholeVectors;
+  const int most_vectors = backward ? kNormWholeGradVectors : kNormWholeVectors;
   const int least = g.R > 1 ? g.P : std::lcm(v, cg) / v;                  // vectors
   const int times = g.P / least;
   for (int k = times; k > 1; --k)
-    if (times % k == 0 && (long)least * k * 16 <= 128 && (long)d.n * (times / k) >= 256 && fit_whole(g, least * k, most_threads, most_vectors)) return true;
-  return fit_whole(g, least, most_threads, most_vectors);
+    if (times % k == 0 && (long)least * k * 16 <= 128 && (long)d.n * (times / k) >= 256 && fit_whole(g, least * k, cg, most_threads, most_vectors)) return true;
+  return fit_whole(g, least, cg, most_threads, most_vectors);
 }
 
 NormGeom geometry(const cprune_norm_desc& d, bool backward) {
@@ -145,11 +151,16 @@ NormGeom geometry(const cprune_norm_desc& d, bool backward) {
   g.tp = (g.P + g.tiles - 1) / g.tiles;
   g.rpi = norm::kThreads / g.tp;
   g.threads = norm::kThreads;
+  g.groups = d.groups, g.lanes = lanes_of(d.groups, norm::kThreads);
   g.by_tp = norm_div(g.tp, 1024);
-  // about six work-groups a compute unit, what the statistics' LDS lets run together, and at least four vectors a thread
-  const long want = std::max(1L, 1536 / ((long)d.n * g.tiles));
+  // two work-groups a compute unit, which run at once (registers): what a work-group does but once, its sums' way through LDS before all, is much of a
+  // launch on maps of some MB (32 x 56 x 56 x 64 bf16 with 512 work-groups 18.7 us, 1024 21.7, 256 18.5; 64 x 112 x 112 x 96 fp16 105, 108, 110).  At least
+  // four vectors a thread.
+  const long want = std::max(1L, 512 / ((long)d.n * g.tiles));
   const long most = (g.SR + 4L * g.rpi - 1) / (4L * g.rpi);
-  const long chunks = std::max(1L, std::min(want, most));
+  // (and few enough that a work-group joins an image's sums with eight entries a thread)
+  const long few = std::max(4L, 8L * norm::kThreads / d.groups);
+  const long chunks = std::max(1L, std::min({want, most, few}));
   g.spc = (int)((g.SR + chunks - 1) / chunks);
   g.spc = (g.spc + g.rpi - 1) / g.rpi * g.rpi;
   g.chunks = (g.SR + g.spc - 1) / g.spc;
@@ -176,13 +187,22 @@ bool too_many_groups(const cprune_norm_desc& d, const NormGeom& g) {
 }
 
 size_t round16(size_t b) { return (b + 15) & ~(size_t)15; }
-// scratch: partial sums, then statistics or means of (image, group)
-size_t part_bytes(const cprune_norm_desc& d, const NormGeom& g, bool backward) {
-  if (g.nv) return backward && d.n > 1 ? round16((size_t)d.n * d.c * sizeof(float2)) : 0;
-  return round16((size_t)d.n * g.chunks * g.R * d.c * sizeof(float2));
-}
-size_t scratch_bytes(const cprune_norm_desc& d, const NormGeom& g, bool backward) {
-  return part_bytes(d, g, backward) + (g.nv ? 0 : round16((size_t)d.n * d.groups * sizeof(float2)));
+// Scratch, as far as a form needs each: sums of elements, sums of groups, statistics or means of (image, group).
+struct NormScratch {
+  size_t part, gpart, stats;
+  size_t total() const { return part + gpart + stats; }
+};
+NormScratch scratch_of(const cprune_norm_desc& d, const NormGeom& g, bool backward) {
+  const size_t pair = sizeof(float2);
+  NormScratch q = {};
+  if (g.nv) {
+    if (backward && d.n > 1) q.part = round16((size_t)d.n * d.c * pair);
+    return q;
+  }
+  if (backward || g.tiles > 1) q.part = round16((size_t)d.n * g.chunks * g.R * d.c * pair);
+  if (g.tiles == 1) q.gpart = round16((size_t)d.n * g.chunks * d.groups * pair);
+  else q.stats = round16((size_t)d.n * d.groups * pair);
+  return q;
 }
 
 NormArgs args_of(const cprune_norm_desc& d, const NormGeom& g) {
@@ -193,7 +213,6 @@ NormArgs args_of(const cprune_norm_desc& d, const NormGeom& g) {
   const float inf = std::numeric_limits<float>::infinity();
   a.lo = d.act == CPRUNE_ACT_NONE ? -inf : 0.0f;
   a.hi = d.act == CPRUNE_ACT_RELU6 ? 6.0f : inf;
-  a.silu = d.act == CPRUNE_ACT_SILU;
   a.n = d.n, a.eps = d.eps;
   a.by_cg = norm_div(a.cg, a.c);
   a.inv_count = 1.0 / ((double)d.pixels * a.cg);
@@ -201,64 +220,30 @@ NormArgs args_of(const cprune_norm_desc& d, const NormGeom& g) {
   return a;
 }
 
-// calls f(type, vector length, activation) with what the call needs
-template <typename F> void with_form(int dtype, int v, bool silu, F&& f) {
-  auto act = [&](auto t, auto vec) {
-    if (silu) f(t, vec, std::true_type());
-    else f(t, vec, std::false_type());
-  };
-  auto vec = [&](auto t) {
-    if (v == 4) act(t, std::integral_constant<int, 4>());
-    else if (v == 2) act(t, std::integral_constant<int, 2>());
-    else act(t, std::integral_constant<int, 1>());
-  };
-  if (dtype == CPRUNE_F32) vec(float());
-  else if (dtype == CPRUNE_F16) v == 8 ? act(_Float16(), std::integral_constant<int, 8>()) : vec(_Float16());
-  else v == 8 ? act(__bf16(), std::integral_constant<int, 8>()) : vec(__bf16());
+void launch(int dtype, NormPass pass, const NormArgs& a, const NormLaunch& l, hipStream_t s) {
+  if (dtype == CPRUNE_F32) launch_norm_f32(pass, a, l, s);
+  else if (dtype == CPRUNE_F16) launch_norm_f16(pass, a, l, s);
+  else launch_norm_bf16(pass, a, l, s);
 }
 
-// calls f(vectors a thread holds), rounded up to a built form
-template <typename F> void with_vectors(int nv, F&& f) {
-  if (nv <= 1) f(std::integral_constant<int, 1>());
-  else if (nv <= 2) f(std::integral_constant<int, 2>());
-  else if (nv <= 4) f(std::integral_constant<int, 4>());
-  else if (nv <= 8) f(std::integral_constant<int, 8>());
-  else f(std::integral_constant<int, 16>());
-}
-template <typename F> void with_type(int dtype, F&& f) {
-  if (dtype == CPRUNE_F32) f(float());
-  else if (dtype == CPRUNE_F16) f(_Float16());
-  else f(__bf16());
-}
-
-void launch_whole(const NormArgs& a, int dtype, hipStream_t s) {
+NormLaunch launch_of(const cprune_norm_desc& d, const NormArgs& a, bool backward) {
   const NormGeom& g = a.g;
-  const bool merge = a.cg % g.V == 0;
-  const int cols = g.tp * g.V, groups = cols / (g.R * a.cg);
-  const size_t lds = ((size_t)(merge ? g.tp : cols) * g.rpi + groups) * sizeof(float2);
-  const unsigned grid = (unsigned)(a.n * g.slabs);
-  with_type(dtype, [&](auto t) {
-    with_vectors(g.nv, [&](auto nv) {
-      using T = decltype(t);
-      if (merge) norm_whole_kernel<T, decltype(nv)::value, true><<<grid, g.threads, lds, s>>>(a);
-      else norm_whole_kernel<T, decltype(nv)::value, false><<<grid, g.threads, lds, s>>>(a);
-    });
-  });
-}
-
-void launch_whole_grad(const NormArgs& a, int dtype, bool silu, hipStream_t s) {
-  const NormGeom& g = a.g;
-  const int cols = g.tp * g.V, groups = cols / (g.R * a.cg);
-  const size_t lds = std::max((size_t)g.V * g.threads / 2, (size_t)cols + groups) * sizeof(float2);
-  const unsigned grid = (unsigned)(a.n * g.slabs);
-  with_type(dtype, [&](auto t) {
-    with_vectors(g.nv, [&](auto nv) {
-      using T = decltype(t);
-      constexpr int NV = decltype(nv)::value < kWholeGradVectors ? decltype(nv)::value : kWholeGradVectors;
-      if (silu) norm_whole_grad_kernel<T, NV, true><<<grid, g.threads, lds, s>>>(a);
-      else norm_whole_grad_kernel<T, NV, false><<<grid, g.threads, lds, s>>>(a);
-    });
-  });
+  NormLaunch l = {};
+  l.silu = d.act == CPRUNE_ACT_SILU;
+  // A map that does not stay in the last-level cache (256 MB, shared with what else is in use) is stored past it: kept there, it leaves while the next
+  // launch reads (64 x 112 x 112 x 96 fp16 107 -> 93 us, the gradient of 64 x 56 x 56 x 144 59 -> 56; 58 MB forward no difference).
+  l.stream = (backward ? 3.0 : 2.0) * d.n * d.pixels * d.c * dtype_size(d.dtype) > 134217728.0;
+  if (backward && (a.dweight || a.dbias)) l.vector_groups = (unsigned)(d.c + 7) / 8;
+  if (g.nv) {
+    l.grid = (unsigned)(d.n * g.slabs);
+    const int cols = g.tp * g.V;
+    const size_t pairs = backward ? std::max(g.V * g.threads / 2, cols + g.groups) : (a.cg % g.V == 0 ? g.tp : cols) * g.rpi + g.groups;
+    l.lds = (unsigned)(pairs * sizeof(float2));
+  } else {
+    if (g.tiles == 1) l.lds = (unsigned)(d.groups * sizeof(float2));
+    l.grid = (unsigned)(d.n * g.chunks * g.tiles);
+  }
+  return l;
 }
 
 }  // namespace
@@ -268,7 +253,7 @@ using namespace cprune;
 
 extern "C" size_t cprune_group_norm_workspace_bytes(const cprune_norm_desc* d, int backward) {
   if (check(d, backward != 0) != CPRUNE_OK) return 0;
-  return scratch_bytes(*d, geometry(*d, backward != 0), backward != 0);
+  return scratch_of(*d, geometry(*d, backward != 0), backward != 0).total();
 }
 
 extern "C" int cprune_group_norm_act(const cprune_norm_desc* d, const void* x, const float* weight, const float* bias, void* y,
@@ -278,29 +263,30 @@ extern "C" int cprune_group_norm_act(const cprune_norm_desc* d, const void* x, c
   if (!x || !y) return CPRUNE_ERR_INVALID_ARG;
   const NormGeom g = geometry(*d, false);
   if (too_many_groups(*d, g)) return CPRUNE_ERR_UNSUPPORTED;
-  const size_t need = scratch_bytes(*d, g, false);
-  if (need && (!ws || ws_bytes < need)) return CPRUNE_ERR_WORKSPACE;
+  const NormScratch q = scratch_of(*d, g, false);
+  if (q.total() && (!ws || ws_bytes < q.total())) return CPRUNE_ERR_WORKSPACE;
   hipStream_t s = static_cast<hipStream_t>(stream);
   NormArgs a = args_of(*d, g);
   a.x = x, a.y = y, a.weight = weight, a.bias = bias;
+  a.mean_out = mean_out, a.rstd_out = rstd_out;
+  const NormLaunch l = launch_of(*d, a, false);
+  char* const scratch = static_cast<char*>(ws);
   if (g.nv) {
-    a.mean_out = mean_out, a.rstd_out = rstd_out;
-    launch_whole(a, d->dtype, s);
-    CPRUNE_LAUNCH_CHECK();
-    return CPRUNE_OK;
-  }
-  a.part = static_cast<float2*>(ws);
-  float* stats = reinterpret_cast<float*>(static_cast<char*>(ws) + part_bytes(*d, g, false));
-  float* mean = mean_out ? mean_out : stats;
-  float* rstd = rstd_out ? rstd_out : stats + (size_t)d->n * d->groups;
-  a.mean = mean, a.rstd = rstd;
-  const unsigned grid = (unsigned)(d->n * g.chunks * g.tiles);
-  with_form(d->dtype, g.V, d->act == CPRUNE_ACT_SILU, [&](auto t, auto v, auto silu) {
-    using T = decltype(t);
-    norm_stats_kernel<T, decltype(v)::value><<<grid, norm::kThreads, 0, s>>>(a);
+    launch(d->dtype, kNormWhole, a, l, s);
+  } else if (q.gpart) {
+    a.gpart = reinterpret_cast<float2*>(scratch);
+    launch(d->dtype, kNormStats, a, l, s);
+    launch(d->dtype, kNormApply, a, l, s);
+  } else {
+    a.part = reinterpret_cast<float2*>(scratch);
+    float* stats = reinterpret_cast<float*>(scratch + q.part);
+    float* mean = mean_out ? mean_out : stats;
+    float* rstd = rstd_out ? rstd_out : stats + (size_t)d->n * d->groups;
+    a.mean = mean, a.rstd = rstd;
+    launch(d->dtype, kNormStats, a, l, s);
     norm_join_stats_kernel<<<d->n * d->groups, join_threads(a), 0, s>>>(a, mean, rstd);
-    norm_apply_kernel<T, decltype(v)::value, decltype(silu)::value><<<grid, norm::kThreads, 0, s>>>(a);
-  });
+    launch(d->dtype, kNormApply, a, l, s);
+  }
   CPRUNE_LAUNCH_CHECK();
   return CPRUNE_OK;
 }
@@ -313,29 +299,26 @@ extern "C" int cprune_group_norm_act_backward(const cprune_norm_desc* d, const v
   if (!dy || !x || !mean || !rstd || !dx) return CPRUNE_ERR_INVALID_ARG;
   const NormGeom g = geometry(*d, true);
   if (too_many_groups(*d, g)) return CPRUNE_ERR_UNSUPPORTED;
-  const size_t need = scratch_bytes(*d, g, true);
-  if (need && (!ws || ws_bytes < need)) return CPRUNE_ERR_WORKSPACE;
+  const NormScratch q = scratch_of(*d, g, true);
+  if (q.total() && (!ws || ws_bytes < q.total())) return CPRUNE_ERR_WORKSPACE;
   hipStream_t s = static_cast<hipStream_t>(stream);
   NormArgs a = args_of(*d, g);
   a.x = x, a.dy = dy, a.y = dx, a.weight = weight, a.bias = bias, a.mean = mean, a.rstd = rstd;
   a.dweight = dweight, a.dbias = dbias;
   a.part = static_cast<float2*>(ws);
-  const unsigned vector_groups = dweight || dbias ? (unsigned)(d->c + 7) / 8 : 0u;
+  const NormLaunch l = launch_of(*d, a, true);
   if (g.nv) {
-    launch_whole_grad(a, d->dtype, d->act == CPRUNE_ACT_SILU, s);
-    if (vector_groups && d->n > 1) norm_vectors_kernel<<<vector_groups, norm::kThreads, 0, s>>>(a);
-    CPRUNE_LAUNCH_CHECK();
-    return CPRUNE_OK;
+    launch(d->dtype, kNormWholeGrad, a, l, s);
+    if (l.vector_groups && d->n > 1) norm_vectors_kernel<<<l.vector_groups, norm::kThreads, 0, s>>>(a);
+  } else {
+    char* const behind = static_cast<char*>(ws) + q.part;
+    float2* const terms = reinterpret_cast<float2*>(behind + q.gpart);
+    if (q.gpart) a.gpart = reinterpret_cast<float2*>(behind);
+    a.terms = terms;
+    launch(d->dtype, kNormGradSums, a, l, s);
+    if (!q.gpart) norm_join_grads_kernel<<<d->n * d->groups, join_threads(a), 0, s>>>(a, terms);
+    launch(d->dtype, kNormGradApply, a, l, s);
   }
-  float2* terms = reinterpret_cast<float2*>(static_cast<char*>(ws) + part_bytes(*d, g, true));
-  a.terms = terms;
-  const unsigned grid = (unsigned)(d->n * g.chunks * g.tiles);
-  with_form(d->dtype, g.V, d->act == CPRUNE_ACT_SILU, [&](auto t, auto v, auto silu) {
-    using T = decltype(t);
-    norm_grad_sums_kernel<T, decltype(v)::value, decltype(silu)::value><<<grid, norm::kThreads, 0, s>>>(a);
-    norm_join_grads_kernel<<<d->n * d->groups, join_threads(a), 0, s>>>(a, terms);
-    norm_grad_apply_kernel<T, decltype(v)::value, decltype(silu)::value><<<grid + vector_groups, norm::kThreads, 0, s>>>(a, vector_groups);
-  });
   CPRUNE_LAUNCH_CHECK();
   return CPRUNE_OK;
 }

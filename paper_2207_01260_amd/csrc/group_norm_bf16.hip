@@ -1,0 +1,8 @@
+// bf16 kernels of the channels-last group norm.
+#include "group_norm_kernel.hpp"
+
+namespace cprune {
+
+void launch_norm_bf16(NormPass pass, const NormArgs& a, const NormLaunch& l, hipStream_t s) { launch_norm<__bf16>(pass, a, l, s); }
+
+}  // namespace cprune

@@ -7,9 +7,10 @@
 // A work-group is `rpi` superrows of `tp` vectors.  The last superrow of an image may hold fewer than R pixels: its elements are checked one by one.  No
 // alignment is assumed (loads of 16 bytes may begin at any element).
 //
-// Two forms, one launch or three (two launches or three for the gradient), chosen by what an image's channels take:
-//  - whole: a work-group holds all pixels of some whole groups' channels in registers, so x is read once;
-//  - split: work-groups walk over runs ("chunks") of superrows of an image; sums of chunks are joined by a launch between, and x is read twice.
+// Two forms, chosen by what an image's channels take:
+//  - whole: a work-group holds all pixels of some whole groups' channels in registers, so x is read once, in one launch (two for the gradient);
+//  - split: work-groups walk over runs ("chunks") of superrows of an image, leaving sums for each group; a second launch joins an image's sums where
+//    it needs them and reads x again.  Where a superrow is wider than a work-group, sums are left for each of its elements and a launch between joins them.
 #pragma once
 #include <type_traits>
 
@@ -32,25 +33,28 @@ struct NormGeom {
   NormDiv by_tp;        // of a thread's number
   int few, more, last_r;   // whole form: superrows of a thread, one more for r < more; the r that has the last one
   int slabs, nv;        // whole form: work-groups an image (of tp vectors a superrow each), vectors a thread holds
+  int groups, lanes;    // groups of a slab; lanes that sum one, a power of two
 };
+
+constexpr int kNormWholeVectors = 16, kNormWholeGradVectors = 8;      // a thread of the whole form holds at most, of x or of x and dy each
 
 struct NormArgs {
   const void *x, *dy;
   const float *weight, *bias;
-  const float *mean, *rstd;   // [n][g]
+  const float *mean, *rstd;   // [n][g]; forward: where gpart is null
   const float2* terms;        // backward: (mean(w dz), mean(w dz xhat)) [n][g]
   float *mean_out, *rstd_out; // whole form, or null
   float eps;
   float *dweight, *dbias;     // backward, or null
   int n;
   void* y;                    // forward: y, backward: dx
-  float2* part;               // [n][chunk][R * c]: forward (mean, squares about it), backward (sum dz, sum dz xhat)
+  float2* part;               // split form [n][chunk][R * c]: forward (mean, squares about it), backward (sum dz, sum dz xhat)
+  float2* gpart;              // the same of each group [n][chunk][group], backward weighted; null: superrows wider than a work-group
   int pixels, c, cg, groups;
   NormDiv by_cg;              // of a channel
   double inv_count;           // 1 / (numbers of an (image, group))
   long x_image, x_pitch, dy_image, dy_pitch;   // elements from image to image, from superrow to superrow
   float lo, hi;               // clamp of the activation
-  int silu;                   // or this
   NormGeom g;
 };
 
@@ -80,14 +84,16 @@ template <typename T, int V> __device__ __forceinline__ typename RawOf<typename 
   for (int j = 0; j < V; ++j) r[j] = j < valid ? static_cast<const B*>(p)[j] : B(0);
   return r;
 }
-template <typename T, int V> __device__ __forceinline__ void store(void* p, const float (&v)[V], int valid) {
+// STREAM: past the caches, for a map that would only push itself out of them
+template <typename T, int V, bool STREAM = false> __device__ __forceinline__ void store(void* p, const float (&v)[V], int valid) {
   typedef typename Bits<T>::type B;
   typedef typename RawOf<B, V>::type Raw;
   Raw r;
 #pragma unroll
   for (int j = 0; j < V; ++j) r[j] = narrow<T>(v[j]);
   if (V == 1 || valid >= V) {
-    *static_cast<Raw*>(p) = r;
+    if constexpr (STREAM) __builtin_nontemporal_store(r, static_cast<Raw*>(p));
+    else *static_cast<Raw*>(p) = r;
   } else {
 #pragma unroll
     for (int j = 0; j < V; ++j)
@@ -95,8 +101,9 @@ template <typename T, int V> __device__ __forceinline__ void store(void* p, cons
   }
 }
 
-// z / (1 + e^-z): the exponential's overflow at very negative z gives z * 0
-__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
+// 1 / (1 + e^-z) on the bare instruction for 2^x (the exponential of the library mends results below 2^-126, which 1 + e^-z does not see); its
+// overflow at very negative z gives z * 0
+__device__ __forceinline__ float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504f)); }
 template <bool SILU> __device__ __forceinline__ float activate(float z, float lo, float hi) {
   if constexpr (SILU) return z * sigmoid(z);
   z = z < lo ? lo : z;      // (comparisons and not minimum / maximum: a NaN stays one)
@@ -157,6 +164,10 @@ __device__ __forceinline__ Place place_whole(const NormGeom& g) {
   k.sr1 = g.SR;
   return k;
 }
+// pixels of a chunk
+__device__ __forceinline__ int chunk_pixels(const NormArgs& a, int chunk) {
+  return min(a.pixels, (chunk + 1) * a.g.spc * a.g.R) - chunk * a.g.spc * a.g.R;
+}
 // elements of the vector at position p that superrow sr has
 __device__ __forceinline__ int valid_of(const NormGeom& g, int c, int sr, int p) {
   return sr == g.SR - 1 ? g.tail * c - p * g.V : g.V;
@@ -165,8 +176,21 @@ __device__ __forceinline__ int valid_of(const NormGeom& g, int c, int sr, int p)
 __device__ __forceinline__ int full_rows(const NormGeom& g) { return g.tail == g.R ? g.SR : g.SR - 1; }
 
 constexpr int kThreads = 256;
-// vectors under way at a time in the split form's loops
-template <int V> constexpr int kBatch = 8;
+// The split form's loops: `whole` batches of vectors and one of what is left, the loads of a batch ahead of the work on the one before.
+// The caller has fetched the first one into `a`.
+template <typename Batch, typename Fetch, typename Work, typename Rest> __device__ __forceinline__ void walk(Batch& a, int whole, Fetch&& fetch, Work&& work, Rest&& rest) {
+  Batch b;
+  for (int i = 0;; i += 2) {
+    if (i == whole) return rest(a);
+    fetch(b, i + 1);
+    work(a);
+    if (i + 1 == whole) return rest(b);
+    fetch(a, i + 2);
+    work(b);
+  }
+}
+// vectors of a batch, of x alone and of x and dy
+constexpr int kBatch = 4, kGradBatch = 2;
 
 // Sum of a pair over the superrows of a work-group, in threads of r = 0; buffer: V * threads / 2 pairs.  The upper half hands over to the lower one,
 // halving: a fixed order.
@@ -232,20 +256,22 @@ template <int V> __device__ __forceinline__ void all_terms(const NormArgs& a, in
   }
 }
 
-// mean and rstd from sums of (count, squares) about `first`
-__device__ __forceinline__ float2 statistics(double2 s, double first, const NormArgs& a) {
-  const double shift = s.x * a.inv_count, var = s.y * a.inv_count - shift * shift;
-  return make_float2((float)(first + shift), 1.0f / sqrtf((var < 0.0 ? 0.0f : (float)var) + a.eps));
+// mean and rstd from the sums of the numbers and of their squares (in 64 bits: the difference below loses what (mean / spread)^2 takes of 53 bits)
+__device__ __forceinline__ float2 statistics(double2 s, const NormArgs& a) {
+  const double mean = s.x * a.inv_count, var = s.y * a.inv_count - mean * mean;
+  return make_float2((float)mean, 1.0f / sqrtf((var < 0.0 ? 0.0f : (float)var) + a.eps));
 }
 
 // a vector of outputs; k.w holds weight * rstd
-template <typename T, int V, bool SILU, typename Raw> __device__ __forceinline__ void normalise(const NormArgs& a, const Raw& raw, const Terms<V>& k, char* out, int valid) {
+template <typename T, int V, bool SILU, bool STREAM, typename Raw>
+__device__ __forceinline__ void normalise(const NormArgs& a, const Raw& raw, const Terms<V>& k, char* out, int valid) {
   float v[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) v[j] = activate<SILU>(fmaf(widen<T>(raw[j]) - k.mean[j], k.w[j], k.b[j]), a.lo, a.hi);
-  store<T, V>(out, v, valid);
+  store<T, V, STREAM>(out, v, valid);
 }
-template <typename T, int V, bool SILU, typename Raw> __device__ __forceinline__ void gradient(const NormArgs& a, const Raw& x, const Raw& dy, const Terms<V>& k, const float2 (&t)[V], char* out, int valid) {
+template <typename T, int V, bool SILU, bool STREAM, typename Raw>
+__device__ __forceinline__ void gradient(const NormArgs& a, const Raw& x, const Raw& dy, const Terms<V>& k, const float2 (&t)[V], char* out, int valid) {
   float v[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) {
@@ -253,9 +279,10 @@ template <typename T, int V, bool SILU, typename Raw> __device__ __forceinline__
     const float dz = widen<T>(dy[j]) * slope<SILU>(argument(xhat, k.w[j], k.b[j]), a.lo, a.hi);
     v[j] = k.rstd[j] * (fmaf(k.w[j], dz, -t[j].x) - xhat * t[j].y);
   }
-  store<T, V>(out, v, valid);
+  store<T, V, STREAM>(out, v, valid);
 }
-template <typename T, int V, bool SILU, typename Raw> __device__ __forceinline__ void gradient_sums(const NormArgs& a, const Raw& x, const Raw& dy, const Terms<V>& k, float (&sb)[V], float (&sw)[V], int valid) {
+template <typename T, int V, bool SILU, typename Raw>
+__device__ __forceinline__ void gradient_sums(const NormArgs& a, const Raw& x, const Raw& dy, const Terms<V>& k, float (&sb)[V], float (&sw)[V], int valid) {
 #pragma unroll
   for (int j = 0; j < V; ++j) {
     const float xhat = centred(widen<T>(x[j]), k.mean[j], k.rstd[j]);
@@ -267,6 +294,64 @@ template <typename T, int V, bool SILU, typename Raw> __device__ __forceinline__
   }
 }
 
+// The sum over neighbouring lanes, a power of two of them up to 64, in every one of them.
+template <int CTRL> __device__ __forceinline__ double from_lane(double v) {
+  const long long b = __double_as_longlong(v);
+  const unsigned lo = (unsigned)__builtin_amdgcn_mov_dpp((int)b, CTRL, 0xF, 0xF, true), hi = (unsigned)__builtin_amdgcn_mov_dpp((int)(b >> 32), CTRL, 0xF, 0xF, true);
+  return __longlong_as_double((long long)hi << 32 | lo);
+}
+__device__ __forceinline__ double2 sum_lanes(double2 s, int lanes) {
+  if (lanes > 1) s.x += from_lane<0xB1>(s.x), s.y += from_lane<0xB1>(s.y);          // the other of a pair
+  if (lanes > 2) s.x += from_lane<0x4E>(s.x), s.y += from_lane<0x4E>(s.y);          // the other pair of a quad
+  if (lanes > 4) s.x += from_lane<0x141>(s.x), s.y += from_lane<0x141>(s.y);        // mirrored in eight
+  if (lanes > 8) s.x += from_lane<0x140>(s.x), s.y += from_lane<0x140>(s.y);        // mirrored in sixteen
+  if (lanes > 16) s.x += __shfl_xor(s.x, 16, 64), s.y += __shfl_xor(s.y, 16, 64);
+  if (lanes > 32) s.x += __shfl_xor(s.x, 32, 64), s.y += __shfl_xor(s.y, 32, 64);
+  return s;
+}
+
+// Sum over a group's `outer` x `inner` entries of pairs add(outer, inner, get(outer, inner)), in 64 bits and a fixed order, by `lanes` neighbouring lanes; all
+// of them get it.  Four entries are under way at a time; a lane counts its place on instead of dividing.
+template <typename Get, typename Add> __device__ __forceinline__ double2 lanes_sum(int lane, int lanes, int outer, int inner, Get&& get, Add&& add) {
+  double2 s = {0.0, 0.0};
+  const int skip = lanes / inner, step = lanes - skip * inner;
+  int o = lane / inner, in = lane - o * inner;
+  while (o < outer) {
+    float2 e[4];
+    int at[4][2];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      at[u][0] = o, at[u][1] = in;
+      if (o < outer) e[u] = get(o, in);
+      o += skip, in += step;
+      if (in >= inner) in -= inner, ++o;
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (at[u][0] < outer) {
+        const double2 v = add(at[u][0], at[u][1], e[u]);
+        s.x += v.x, s.y += v.y;
+      }
+  }
+  return sum_lanes(s, lanes);
+}
+
+// sums of n numbers and of their squares from their (mean, squares about it)
+__device__ __forceinline__ double2 raw_sums(double n, float2 e) {
+  const double nm = n * e.x;
+  return n > 0.0 ? make_double2(nm, (double)e.y + nm * e.x) : make_double2(0.0, 0.0);
+}
+
+// Weighted sums of dz and dz xhat over the columns of group g, whose first channel is ch0.
+__device__ __forceinline__ double2 group_terms(const NormArgs& a, const float2* col, int lane, int lanes, int g, int ch0) {
+  return lanes_sum(
+      lane, lanes, a.g.R, a.cg, [&](int rr, int ch) __attribute__((always_inline)) { return col[rr * a.c + g * a.cg + ch]; },
+      [&](int, int ch, float2 e) __attribute__((always_inline)) {
+        const double w = a.weight ? a.weight[ch0 + ch] : 1.0f;
+        return make_double2(w * e.x, w * e.y);
+      });
+}
+
 }  // namespace norm
 
 // ---- split form ----------------------------------------------------------------------------------
@@ -274,9 +359,9 @@ template <typename T, int V, bool SILU, typename Raw> __device__ __forceinline__
 // Statistics of a chunk: each thread's running mean and squares about it, four numbers at a time about their own mean (no difference of large sums, whatever
 // the numbers' mean), then joined over the work-group's superrows pair by pair.
 template <typename T, int V>
-__global__ __launch_bounds__(norm::kThreads) void norm_stats_kernel(const NormArgs a) {
+__global__ __launch_bounds__(norm::kThreads, 4) void norm_stats_kernel(const NormArgs a) {
   using namespace norm;
-  constexpr int U = kBatch<V>;
+  constexpr int U = kBatch;
   __shared__ float s_mean[V][kThreads], s_sq[V][kThreads], s_n[V][kThreads];
   const Place k = place(a.g, blockIdx.x);
   float mean[V], sq[V], cnt[V];
@@ -300,36 +385,49 @@ __global__ __launch_bounds__(norm::kThreads) void norm_stats_kernel(const NormAr
         }
       }
     };
-    typename RawOf<typename Bits<T>::type, V>::type raw[U];
-    int sr = k.sr0 + k.r;
-    for (; sr + (U - 1) * step < full; sr += U * step) {
+    struct Batch {
+      typename RawOf<typename Bits<T>::type, V>::type raw[U];
+    };
+    const int sr = k.sr0 + k.r, whole = max(full - k.sr0, 0) / (U * step);
+    auto fetch = [&](Batch& q, int i) __attribute__((always_inline)) {
+      const int at = sr + i * U * step;
+      if (i < whole) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) raw[u] = load<T, V>(base + (sr + u * step) * pitch, V);
-      const float f = (float)U * __builtin_amdgcn_rcpf(n + (float)U), nf = n * f;
+        for (int u = 0; u < U; ++u) q.raw[u] = load<T, V>(base + (at + u * step) * pitch, V);
+      } else {
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        float m = 0.0f, q = 0.0f;
-#pragma unroll
-        for (int u = 0; u < U; ++u) m += widen<T>(raw[u][j]);
-        m *= 1.0f / U;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const float d = widen<T>(raw[u][j]) - m;
-          q = fmaf(d, d, q);
-        }
-        const float d = m - mean[j];
-        mean[j] = fmaf(d, f, mean[j]);
-        sq[j] += fmaf(d * d, nf, q);
+        for (int u = 0; u < U; ++u)
+          if (at + u * step < full) q.raw[u] = load<T, V>(base + (at + u * step) * pitch, V);
       }
-      n += (float)U;
-    }
-    // what is left: the loads together all the same
+    };
+    Batch head;
+    fetch(head, 0);
+    walk(
+        head, whole, fetch,
+        [&](const Batch& q) __attribute__((always_inline)) {
+          const float f = (float)U * __builtin_amdgcn_rcpf(n + (float)U), nf = n * f;
 #pragma unroll
-    for (int u = 0; u < U - 1; ++u)
-      if (sr + u * step < full) raw[u] = load<T, V>(base + (sr + u * step) * pitch, V);
+          for (int j = 0; j < V; ++j) {
+            float m = 0.0f, sum = 0.0f;
 #pragma unroll
-    for (int u = 0; u < U - 1; ++u)
-      if (sr + u * step < full) one(raw[u], V);
+            for (int u = 0; u < U; ++u) m += widen<T>(q.raw[u][j]);
+            m *= 1.0f / U;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+              const float d = widen<T>(q.raw[u][j]) - m;
+              sum = fmaf(d, d, sum);
+            }
+            const float d = m - mean[j];
+            mean[j] = fmaf(d, f, mean[j]);
+            sq[j] += fmaf(d * d, nf, sum);
+          }
+          n += (float)U;
+        },
+        [&](const Batch& q) __attribute__((always_inline)) {
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+            if (sr + (whole * U + u) * step < full) one(q.raw[u], V);
+        });
     const int end = a.g.SR - 1, valid = valid_of(a.g, a.c, end, k.p);
     if (full < k.sr1 && (unsigned)(end - k.sr0) % (unsigned)step == (unsigned)k.r && valid > 0) {
       one(load<T, V>(base + end * pitch, valid), valid);
@@ -351,7 +449,7 @@ __global__ __launch_bounds__(norm::kThreads) void norm_stats_kernel(const NormAr
       for (int j = 0; j < V; ++j) {
         const float nb = s_n[j][o], sum = cnt[j] + nb;
         if (nb > 0.0f) {
-          const float d = s_mean[j][o] - mean[j], f = nb / sum;
+          const float d = s_mean[j][o] - mean[j], f = nb * __builtin_amdgcn_rcpf(sum);
           mean[j] = fmaf(d, f, mean[j]);
           sq[j] += s_sq[j][o] + d * d * cnt[j] * f;
           cnt[j] = sum;
@@ -360,88 +458,179 @@ __global__ __launch_bounds__(norm::kThreads) void norm_stats_kernel(const NormAr
       }
     }
   }
-  if (k.active && k.r == 0) {
-    float2* out = a.part + ((long)k.image * a.g.chunks + k.part) * a.g.P * V + (long)k.p * V;
+  if (!a.gpart) {
+    if (k.active && k.r == 0) {
+      float2* out = a.part + ((long)k.image * a.g.chunks + k.part) * a.g.P * V + (long)k.p * V;
 #pragma unroll
-    for (int j = 0; j < V; ++j) out[j] = make_float2(mean[j], sq[j]);
+      for (int j = 0; j < V; ++j) out[j] = make_float2(mean[j], sq[j]);
+    }
+    return;
+  }
+  __syncthreads();
+  // the superrow's elements as groups
+  const int lanes = a.g.lanes, lane = t & (lanes - 1), per = kThreads / lanes;
+  const double inv = 1.0 / ((double)chunk_pixels(a, k.part) * a.cg);
+  for (int g = t / lanes; g < a.groups; g += per) {
+    const double2 s = lanes_sum(
+        lane, lanes, a.g.R, a.cg,
+        [&](int rr, int ch) __attribute__((always_inline)) {
+          const int q = rr * a.c + g * a.cg + ch;
+          return make_float2(s_mean[q % V][q / V], s_sq[q % V][q / V]);
+        },
+        [&](int rr, int ch, float2 e) __attribute__((always_inline)) {
+          const int q = rr * a.c + g * a.cg + ch;
+          return raw_sums(s_n[q % V][q / V], e);
+        });
+    if (lane == 0) {
+      const double mean_g = s.x * inv, sq_g = s.y - mean_g * s.x;
+      a.gpart[((long)k.image * a.g.chunks + k.part) * a.groups + g] = make_float2((float)mean_g, sq_g < 0.0 ? 0.0f : (float)sq_g);
+    }
   }
 }
 
-template <typename T, int V, bool SILU>
-__global__ __launch_bounds__(norm::kThreads) void norm_apply_kernel(const NormArgs a) {
+template <typename T, int V, bool SILU, bool STREAM>
+__global__ __launch_bounds__(norm::kThreads, 4) void norm_apply_kernel(const NormArgs a) {
   using namespace norm;
-  constexpr int U = kBatch<V>;
+  constexpr int U = kBatch;
+  extern __shared__ char lds[];
+  float2* const stat = reinterpret_cast<float2*>(lds);      // [group]: (mean, rstd), where sums are a group's
   const Place k = place(a.g, blockIdx.x);
-  if (!k.active) return;
-  Terms<V> c;
-  all_terms<V>(a, k.image, where<V>(a, k.p * V), c);
-#pragma unroll
-  for (int j = 0; j < V; ++j) c.w[j] *= c.rstd[j];
   const char* base = static_cast<const char*>(a.x) + (k.image * a.x_image + (long)k.p * V) * (long)sizeof(T);
   char* out = static_cast<char*>(a.y) + ((long)k.image * a.pixels * a.c + (long)k.p * V) * (long)sizeof(T);
   const long pitch = a.x_pitch * (long)sizeof(T), out_pitch = (long)a.g.P * V * (long)sizeof(T);
   const int step = a.g.rpi, full = min(k.sr1, full_rows(a.g));
-  int sr = k.sr0 + k.r;
-  typename RawOf<typename Bits<T>::type, V>::type raw[U];
-  for (; sr + (U - 1) * step < full; sr += U * step) {
+  struct Batch {
+    typename RawOf<typename Bits<T>::type, V>::type raw[U];
+  };
+  const int sr = k.sr0 + k.r, whole = max(full - k.sr0, 0) / (U * step);
+  auto fetch = [&](Batch& q, int i) __attribute__((always_inline)) {
+    const int at = sr + i * U * step;
+    if (i < whole) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) raw[u] = load<T, V>(base + (sr + u * step) * pitch, V);
+      for (int u = 0; u < U; ++u) q.raw[u] = load<T, V>(base + (at + u * step) * pitch, V);
+    } else {
 #pragma unroll
-    for (int u = 0; u < U; ++u) normalise<T, V, SILU>(a, raw[u], c, out + (sr + u * step) * out_pitch, V);
+      for (int u = 0; u < U; ++u) {
+        const int valid = at + u * step < k.sr1 ? valid_of(a.g, a.c, at + u * step, k.p) : 0;
+        if (valid > 0) q.raw[u] = load<T, V>(base + (at + u * step) * pitch, valid);
+      }
+    }
+  };
+  // (what does not wait for the image's statistics is under way before they are joined)
+  Batch head;
+  Terms<V> c;
+  Where<V> here;
+  if (k.active) {
+    fetch(head, 0);
+    here = where<V>(a, k.p * V);
+    channel_terms<V>(a, here, c);
   }
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int at = sr + u * step, valid = at < k.sr1 ? valid_of(a.g, a.c, at, k.p) : 0;
-    if (valid > 0) raw[u] = load<T, V>(base + at * pitch, valid);
+  if (a.gpart) {
+    const int lanes = a.g.lanes, lane = (int)threadIdx.x & (lanes - 1), per = kThreads / lanes;
+    const float2* const part = a.gpart + (long)k.image * a.g.chunks * a.groups;
+    for (int g = (int)threadIdx.x / lanes; g < a.groups; g += per) {
+      const double2 s = lanes_sum(
+          lane, lanes, a.g.chunks, 1, [&](int chunk, int) __attribute__((always_inline)) { return part[chunk * a.groups + g]; },
+          [&](int chunk, int, float2 e) __attribute__((always_inline)) { return raw_sums((double)(chunk_pixels(a, chunk) * a.cg), e); });
+      if (lane == 0) {
+        const float2 m = statistics(s, a);
+        stat[g] = m;
+        if (k.part == 0 && a.mean_out) a.mean_out[k.image * a.groups + g] = m.x;
+        if (k.part == 0 && a.rstd_out) a.rstd_out[k.image * a.groups + g] = m.y;
+      }
+    }
+    __syncthreads();
   }
+  if (!k.active) return;
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int at = sr + u * step, valid = at < k.sr1 ? valid_of(a.g, a.c, at, k.p) : 0;
-    if (valid > 0) normalise<T, V, SILU>(a, raw[u], c, out + at * out_pitch, valid);
+  for (int j = 0; j < V; ++j) {
+    const int at = k.image * a.groups + here.group[j];
+    const float2 m = a.gpart ? stat[here.group[j]] : make_float2(a.mean[at], a.rstd[at]);
+    c.mean[j] = m.x;
+    c.w[j] *= m.y;
   }
+  int at = sr;
+  walk(
+      head, whole, fetch,
+      [&](const Batch& q) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u, at += step) normalise<T, V, SILU, STREAM>(a, q.raw[u], c, out + at * out_pitch, V);
+      },
+      [&](const Batch& q) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u, at += step) {
+          const int valid = at < k.sr1 ? valid_of(a.g, a.c, at, k.p) : 0;
+          if (valid > 0) normalise<T, V, SILU, STREAM>(a, q.raw[u], c, out + at * out_pitch, valid);
+        }
+      });
 }
 
 // Sums of dz and dz xhat over a chunk.
 template <typename T, int V, bool SILU>
-__global__ __launch_bounds__(norm::kThreads) void norm_grad_sums_kernel(const NormArgs a) {
+__global__ __launch_bounds__(norm::kThreads, 4) void norm_grad_sums_kernel(const NormArgs a) {
   using namespace norm;
-  constexpr int U = kBatch<V> / 2;
-  __shared__ float2 buffer[V * kThreads / 2];
+  constexpr int U = kGradBatch;
+  __shared__ float2 buffer[V * kThreads];
   const Place k = place(a.g, blockIdx.x);
   float sb[V], sw[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) sb[j] = sw[j] = 0.0f;
   if (k.active) {
     Terms<V> c;
-    all_terms<V>(a, k.image, where<V>(a, k.p * V), c);
     const char* xb = static_cast<const char*>(a.x) + (k.image * a.x_image + (long)k.p * V) * (long)sizeof(T);
     const char* db = static_cast<const char*>(a.dy) + (k.image * a.dy_image + (long)k.p * V) * (long)sizeof(T);
     const long pitch = a.x_pitch * (long)sizeof(T), dy_pitch = a.dy_pitch * (long)sizeof(T);
     const int step = a.g.rpi, full = min(k.sr1, full_rows(a.g));
-    int sr = k.sr0 + k.r;
-    typename RawOf<typename Bits<T>::type, V>::type x[U], dy[U];
-    for (; sr + (U - 1) * step < full; sr += U * step) {
+    struct Batch {
+      typename RawOf<typename Bits<T>::type, V>::type x[U], dy[U];
+    };
+    const int sr = k.sr0 + k.r, whole = max(full - k.sr0, 0) / (U * step);
+    auto fetch = [&](Batch& q, int i) __attribute__((always_inline)) {
+      const int at = sr + i * U * step;
+      if (i < whole) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) x[u] = load<T, V>(xb + (sr + u * step) * pitch, V), dy[u] = load<T, V>(db + (sr + u * step) * dy_pitch, V);
+        for (int u = 0; u < U; ++u) q.x[u] = load<T, V>(xb + (at + u * step) * pitch, V), q.dy[u] = load<T, V>(db + (at + u * step) * dy_pitch, V);
+      } else {
 #pragma unroll
-      for (int u = 0; u < U; ++u) gradient_sums<T, V, SILU>(a, x[u], dy[u], c, sb, sw, V);
-    }
+        for (int u = 0; u < U; ++u) {
+          const int valid = at + u * step < k.sr1 ? valid_of(a.g, a.c, at + u * step, k.p) : 0;
+          if (valid > 0) q.x[u] = load<T, V>(xb + (at + u * step) * pitch, valid), q.dy[u] = load<T, V>(db + (at + u * step) * dy_pitch, valid);
+        }
+      }
+    };
+    Batch head;
+    fetch(head, 0);
+    all_terms<V>(a, k.image, where<V>(a, k.p * V), c);
+    walk(
+        head, whole, fetch,
+        [&](const Batch& q) __attribute__((always_inline)) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int at = sr + u * step, valid = at < k.sr1 ? valid_of(a.g, a.c, at, k.p) : 0;
-      if (valid > 0) x[u] = load<T, V>(xb + at * pitch, valid), dy[u] = load<T, V>(db + at * dy_pitch, valid);
-    }
+          for (int u = 0; u < U; ++u) gradient_sums<T, V, SILU>(a, q.x[u], q.dy[u], c, sb, sw, V);
+        },
+        [&](const Batch& q) __attribute__((always_inline)) {
+          int at = sr + whole * U * step;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int at = sr + u * step, valid = at < k.sr1 ? valid_of(a.g, a.c, at, k.p) : 0;
-      if (valid > 0) gradient_sums<T, V, SILU>(a, x[u], dy[u], c, sb, sw, valid);
-    }
+          for (int u = 0; u < U; ++u, at += step) {
+            const int valid = at < k.sr1 ? valid_of(a.g, a.c, at, k.p) : 0;
+            if (valid > 0) gradient_sums<T, V, SILU>(a, q.x[u], q.dy[u], c, sb, sw, valid);
+          }
+        });
   }
   add_rows<V>(sb, sw, k.r, a.g.tp, a.g.rpi, k.active, buffer);
   if (k.active && k.r == 0) {
     float2* out = a.part + ((long)k.image * a.g.chunks + k.part) * a.g.P * V + (long)k.p * V;
 #pragma unroll
-    for (int j = 0; j < V; ++j) out[j] = make_float2(sb[j], sw[j]);
+    for (int j = 0; j < V; ++j) {
+      out[j] = make_float2(sb[j], sw[j]);
+      if (a.gpart) buffer[(int)threadIdx.x * V + j] = out[j];
+    }
+  }
+  if (!a.gpart) return;
+  __syncthreads();
+  const int lanes = a.g.lanes, lane = (int)threadIdx.x & (lanes - 1), per = kThreads / lanes;
+  for (int g = (int)threadIdx.x / lanes; g < a.groups; g += per) {
+    const double2 s = group_terms(a, buffer, lane, lanes, g, g * a.cg);
+    if (lane == 0) a.gpart[((long)k.image * a.g.chunks + k.part) * a.groups + g] = make_float2((float)s.x, (float)s.y);
   }
 }
 
@@ -476,106 +665,108 @@ __device__ inline void norm_vector_sums(const NormArgs& a, unsigned block, long 
 __global__ __launch_bounds__(norm::kThreads) inline void norm_vectors_kernel(const NormArgs a) { norm_vector_sums(a, blockIdx.x, a.n); }
 
 // The first `vector_groups` work-groups sum dweight and dbias (few numbers, long chains: beside the others they cost nothing), the others dx.
-template <typename T, int V, bool SILU>
-__global__ __launch_bounds__(norm::kThreads) void norm_grad_apply_kernel(const NormArgs a, unsigned vector_groups) {
+template <typename T, int V, bool SILU, bool STREAM>
+__global__ __launch_bounds__(norm::kThreads, 4) void norm_grad_apply_kernel(const NormArgs a, unsigned vector_groups) {
   using namespace norm;
-  constexpr int U = kBatch<V> / 2;
+  constexpr int U = kGradBatch;
   if (blockIdx.x < vector_groups) {
     norm_vector_sums(a, blockIdx.x, (long)a.n * a.g.chunks * a.g.R);
     return;
   }
+  extern __shared__ char lds[];
+  float2* const term = reinterpret_cast<float2*>(lds);      // [group], where sums are a group's
   const Place k = place(a.g, blockIdx.x - vector_groups);
-  if (!k.active) return;
-  Terms<V> c;
-  const Where<V> here = where<V>(a, k.p * V);
-  all_terms<V>(a, k.image, here, c);
-  float2 t[V];
-#pragma unroll
-  for (int j = 0; j < V; ++j) t[j] = a.terms[k.image * a.groups + here.group[j]];
   const char* xb = static_cast<const char*>(a.x) + (k.image * a.x_image + (long)k.p * V) * (long)sizeof(T);
   const char* db = static_cast<const char*>(a.dy) + (k.image * a.dy_image + (long)k.p * V) * (long)sizeof(T);
   char* out = static_cast<char*>(a.y) + ((long)k.image * a.pixels * a.c + (long)k.p * V) * (long)sizeof(T);
   const long pitch = a.x_pitch * (long)sizeof(T), dy_pitch = a.dy_pitch * (long)sizeof(T), out_pitch = (long)a.g.P * V * (long)sizeof(T);
   const int step = a.g.rpi, full = min(k.sr1, full_rows(a.g));
-  int sr = k.sr0 + k.r;
-  typename RawOf<typename Bits<T>::type, V>::type x[U], dy[U];
-  for (; sr + (U - 1) * step < full; sr += U * step) {
+  struct Batch {
+    typename RawOf<typename Bits<T>::type, V>::type x[U], dy[U];
+  };
+  const int sr = k.sr0 + k.r, whole = max(full - k.sr0, 0) / (U * step);
+  auto fetch = [&](Batch& q, int i) __attribute__((always_inline)) {
+    const int at = sr + i * U * step;
+    if (i < whole) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) x[u] = load<T, V>(xb + (sr + u * step) * pitch, V), dy[u] = load<T, V>(db + (sr + u * step) * dy_pitch, V);
+      for (int u = 0; u < U; ++u) q.x[u] = load<T, V>(xb + (at + u * step) * pitch, V), q.dy[u] = load<T, V>(db + (at + u * step) * dy_pitch, V);
+    } else {
 #pragma unroll
-    for (int u = 0; u < U; ++u) gradient<T, V, SILU>(a, x[u], dy[u], c, t, out + (sr + u * step) * out_pitch, V);
+      for (int u = 0; u < U; ++u) {
+        const int valid = at + u * step < k.sr1 ? valid_of(a.g, a.c, at + u * step, k.p) : 0;
+        if (valid > 0) q.x[u] = load<T, V>(xb + (at + u * step) * pitch, valid), q.dy[u] = load<T, V>(db + (at + u * step) * dy_pitch, valid);
+      }
+    }
+  };
+  Batch head;
+  Terms<V> c;
+  Where<V> here;
+  if (k.active) {
+    fetch(head, 0);
+    here = where<V>(a, k.p * V);
+    all_terms<V>(a, k.image, here, c);
   }
-#pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int at = sr + u * step, valid = at < k.sr1 ? valid_of(a.g, a.c, at, k.p) : 0;
-    if (valid > 0) x[u] = load<T, V>(xb + at * pitch, valid), dy[u] = load<T, V>(db + at * dy_pitch, valid);
+  if (a.gpart) {
+    const int lanes = a.g.lanes, lane = (int)threadIdx.x & (lanes - 1), per = kThreads / lanes;
+    const float2* const part = a.gpart + (long)k.image * a.g.chunks * a.groups;
+    for (int g = (int)threadIdx.x / lanes; g < a.groups; g += per) {
+      const double2 s = lanes_sum(
+          lane, lanes, a.g.chunks, 1, [&](int chunk, int) __attribute__((always_inline)) { return part[chunk * a.groups + g]; },
+          [&](int, int, float2 e) __attribute__((always_inline)) { return make_double2(e.x, e.y); });
+      if (lane == 0) term[g] = make_float2((float)(s.x * a.inv_count), (float)(s.y * a.inv_count));
+    }
+    __syncthreads();
   }
+  if (!k.active) return;
+  float2 t[V];
 #pragma unroll
-  for (int u = 0; u < U; ++u) {
-    const int at = sr + u * step, valid = at < k.sr1 ? valid_of(a.g, a.c, at, k.p) : 0;
-    if (valid > 0) gradient<T, V, SILU>(a, x[u], dy[u], c, t, out + at * out_pitch, valid);
-  }
+  for (int j = 0; j < V; ++j) t[j] = a.gpart ? term[here.group[j]] : a.terms[k.image * a.groups + here.group[j]];
+  int at = sr;
+  walk(
+      head, whole, fetch,
+      [&](const Batch& q) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u, at += step) gradient<T, V, SILU, STREAM>(a, q.x[u], q.dy[u], c, t, out + at * out_pitch, V);
+      },
+      [&](const Batch& q) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < U; ++u, at += step) {
+          const int valid = at < k.sr1 ? valid_of(a.g, a.c, at, k.p) : 0;
+          if (valid > 0) gradient<T, V, SILU, STREAM>(a, q.x[u], q.dy[u], c, t, out + at * out_pitch, valid);
+        }
+      });
 }
 
 // ---- whole form ----------------------------------------------------------------------------------
 // V numbers are 16 bytes; a thread holds NV vectors.
 
-namespace norm {
+// What holds of the slab's layout, known when the kernel is built: kMerge, V divides a group's channels, so a thread's numbers are of one group; kTail, the last superrow lacks pixels.
+enum NormSlab { kPlain, kMerge, kTail };
 
-// Sum over a group of pairs f(i) of its `outer` x `inner` entries, in 64 bits, by `lanes` neighbouring lanes (a power of two up to 64); all of them get it.
-template <typename F> __device__ __forceinline__ double2 lanes_sum(int lane, int lanes, int outer, int inner, F&& f) {
-  double2 s = {0.0, 0.0};
-  const int skip = lanes / inner, step = lanes - skip * inner;
-  int o = lane / inner, in = lane - o * inner;
-  while (o < outer) {
-    const double2 v = f(o, in);
-    s.x += v.x, s.y += v.y;
-    o += skip, in += step;
-    if (in >= inner) in -= inner, ++o;
-  }
-  for (int m = lanes >> 1; m > 0; m >>= 1) {
-    s.x += __shfl_xor(s.x, m, 64);
-    s.y += __shfl_xor(s.y, m, 64);
-  }
-  return s;
-}
-
-// lanes of a group so that `groups` of them fill the work-group
-__device__ __forceinline__ int lanes_of(int groups) {
-  int lanes = 64;
-  while (lanes > 1 && lanes * groups > (int)blockDim.x) lanes >>= 1;
-  return lanes;
-}
-
-}  // namespace norm
-
-// MERGE: V divides a group's channels, so a thread's numbers are of one group.
-template <typename T, int NV, bool MERGE>
+template <typename T, int NV, int SLAB, bool SILU>
 __global__ __launch_bounds__(1024) void norm_whole_kernel(const NormArgs a) {
   using namespace norm;
   constexpr int V = 16 / (int)sizeof(T);
+  constexpr bool MERGE = SLAB == kMerge, STREAM = false;
   extern __shared__ char lds[];
   const Place k = place_whole(a.g);
-  const int cols = a.g.tp * V, groups = a.groups / a.g.slabs;      // of the slab
+  const int cols = a.g.tp * V, groups = a.g.groups;                 // of the slab
   float2* const part = reinterpret_cast<float2*>(lds);              // [r][vector or element]: (mean, squares)
   float2* const stat = part + (MERGE ? a.g.tp : cols) * a.g.rpi;    // [group]: (mean, rstd)
-  const char* base = static_cast<const char*>(a.x) + (k.image * a.x_image + (long)k.p * V) * (long)sizeof(T);
-  const long pitch = a.x_pitch * (long)sizeof(T);
+  const char* base = static_cast<const char*>(a.x) + (k.image * a.x_image + (long)k.p * V + k.r * a.x_pitch) * (long)sizeof(T);
+  const long step = a.g.rpi * a.x_pitch * (long)sizeof(T);
+  // superrows of this thread, and the elements of the last one
+  const int rows = k.active ? a.g.few + (k.r < a.g.more ? 1 : 0) : 0;
+  const int last = SLAB == kTail && k.r == a.g.last_r ? min(a.g.tail * a.c - k.p * V, V) : V;
   typename RawOf<typename Bits<T>::type, V>::type raw[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+    if (i < rows) raw[i] = load<T, V>(base + i * step, i == rows - 1 ? last : V);
   Terms<V> c;
   Where<V> here;
   if (k.active) {
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int sr = k.r + i * a.g.rpi;
-      const int valid = sr < a.g.SR ? valid_of(a.g, a.c, sr, k.p) : 0;
-      if (valid > 0) raw[i] = load<T, V>(base + sr * pitch, valid);
-    }
     here = where<V>(a, k.p * V);
     channel_terms<V>(a, here, c);
-    // superrows of this thread; the last one of the image may lack elements
-    const int rows = a.g.few + (k.r < a.g.more ? 1 : 0);
-    const int last = k.r == a.g.last_r ? valid_of(a.g, a.c, a.g.SR - 1, k.p) : V;      // elements of its last vector
     if constexpr (MERGE) {
       float m = 0.0f, q = 0.0f;
 #pragma unroll
@@ -583,7 +774,7 @@ __global__ __launch_bounds__(1024) void norm_whole_kernel(const NormArgs a) {
         if (i < rows)
 #pragma unroll
           for (int j = 0; j < V; ++j) m += widen<T>(raw[i][j]);
-      m *= __builtin_amdgcn_rcpf((float)max(rows * V, 1));
+      m *= __builtin_amdgcn_rcpf((float)(rows * V));
 #pragma unroll
       for (int i = 0; i < NV; ++i)
         if (i < rows)
@@ -594,56 +785,63 @@ __global__ __launch_bounds__(1024) void norm_whole_kernel(const NormArgs a) {
           }
       part[threadIdx.x] = make_float2(m, q);
     } else {
-      const float all = __builtin_amdgcn_rcpf((float)max(rows, 1)), less = __builtin_amdgcn_rcpf((float)max(rows - 1, 1));
+      float m[V], q[V];
 #pragma unroll
-      for (int j = 0; j < V; ++j) {
-        const int have = j < last ? rows : rows - 1;
-        float m = 0.0f, q = 0.0f;
+      for (int j = 0; j < V; ++j) m[j] = q[j] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-          if (i < have) m += widen<T>(raw[i][j]);
-        m *= j < last ? all : less;
+      for (int i = 0; i < NV; ++i)
+        if (i < rows)
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-          if (i < have) {
-            const float d = widen<T>(raw[i][j]) - m;
-            q = fmaf(d, d, q);
-          }
-        part[k.r * cols + ((int)threadIdx.x - k.r * a.g.tp) * V + j] = make_float2(m, q);
-      }
+          for (int j = 0; j < V; ++j)
+            if (SLAB != kTail || i < rows - 1 || j < last) m[j] += widen<T>(raw[i][j]);
+      const float all = __builtin_amdgcn_rcpf((float)rows), less = __builtin_amdgcn_rcpf((float)max(rows - 1, 1));
+#pragma unroll
+      for (int j = 0; j < V; ++j) m[j] *= j < last ? all : less;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+        if (i < rows)
+#pragma unroll
+          for (int j = 0; j < V; ++j)
+            if (SLAB != kTail || i < rows - 1 || j < last) {
+              const float d = widen<T>(raw[i][j]) - m[j];
+              q[j] = fmaf(d, d, q[j]);
+            }
+      float4* const out = reinterpret_cast<float4*>(part + threadIdx.x * V);
+#pragma unroll
+      for (int j = 0; j < V; j += 2) out[j / 2] = make_float4(m[j], q[j], m[j + 1], q[j + 1]);
     }
   }
   __syncthreads();
   {
-    const int lanes = lanes_of(groups), lane = (int)threadIdx.x & (lanes - 1), per = (int)blockDim.x / lanes;
+    const int lanes = a.g.lanes, lane = (int)threadIdx.x & (lanes - 1), per = (int)blockDim.x / lanes;
     const int more = a.g.more, few = a.g.few, last_r = a.g.last_r;
     for (int g = (int)threadIdx.x / lanes; g < groups; g += per) {
       double2 s;
-      double first;
       if constexpr (MERGE) {
         const int vg = a.cg / V;
-        first = part[g * vg].x;
-        s = lanes_sum(lane, lanes, a.g.rpi, vg, [&](int r, int v) __attribute__((always_inline)) {
-          const float2 e = part[r * a.g.tp + g * vg + v];
-          const double n = (few + (r < more ? 1 : 0)) * V, d = (double)e.x - first;
-          return n > 0.0 ? make_double2(n * d, (double)e.y + n * d * d) : make_double2(0.0, 0.0);
-        });
+        s = lanes_sum(
+            lane, lanes, a.g.rpi, vg, [&](int r, int v) __attribute__((always_inline)) { return part[r * a.g.tp + g * vg + v]; },
+            [&](int r, int, float2 e) __attribute__((always_inline)) {
+              return raw_sums((double)((few + (r < more ? 1 : 0)) * V), e);
+            });
       } else {
-        first = part[g * a.cg].x;
-        s = lanes_sum(lane, lanes, a.g.rpi * a.g.R, a.cg, [&](int o, int ch) __attribute__((always_inline)) {
-          const int r = a.g.R == 1 ? o : o / a.g.R, rr = o - r * a.g.R;
-          const float2 e = part[r * cols + rr * a.c + g * a.cg + ch];
-          const double n = few + (r < more ? 1 : 0) - (r == last_r && rr >= a.g.tail ? 1 : 0), d = (double)e.x - first;
-          return n > 0.0 ? make_double2(n * d, (double)e.y + n * d * d) : make_double2(0.0, 0.0);
-        });
+        s = lanes_sum(
+            lane, lanes, a.g.rpi * a.g.R, a.cg,
+            [&](int o, int ch) __attribute__((always_inline)) {
+              const int r = a.g.R == 1 ? o : o / a.g.R, rr = o - r * a.g.R;
+              return part[r * cols + rr * a.c + g * a.cg + ch];
+            },
+            [&](int o, int, float2 e) __attribute__((always_inline)) {
+              const int r = a.g.R == 1 ? o : o / a.g.R, rr = o - r * a.g.R;
+              return raw_sums((double)(few + (r < more ? 1 : 0) - (SLAB == kTail && r == last_r && rr >= a.g.tail ? 1 : 0)), e);
+            });
       }
       if (lane == 0) {
-        const float2 m = statistics(s, first, a);
-        const float mean = m.x, rstd = m.y;
-        stat[g] = make_float2(mean, rstd);
+        const float2 m = statistics(s, a);
+        stat[g] = m;
         const int at = k.image * a.groups + k.part * groups + g;
-        if (a.mean_out) a.mean_out[at] = mean;
-        if (a.rstd_out) a.rstd_out[at] = rstd;
+        if (a.mean_out) a.mean_out[at] = m.x;
+        if (a.rstd_out) a.rstd_out[at] = m.y;
       }
     }
   }
@@ -655,63 +853,53 @@ __global__ __launch_bounds__(1024) void norm_whole_kernel(const NormArgs a) {
     c.mean[j] = s.x;
     c.w[j] *= s.y;
   }
-  char* out = static_cast<char*>(a.y) + ((long)k.image * a.pixels * a.c + (long)k.p * V) * (long)sizeof(T);
-  const long out_pitch = (long)a.g.P * V * (long)sizeof(T);
+  char* out = static_cast<char*>(a.y) + ((long)k.image * a.pixels * a.c + (long)(k.r * a.g.P + k.p) * V) * (long)sizeof(T);
+  const long out_step = (long)a.g.rpi * a.g.P * V * (long)sizeof(T);
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int sr = k.r + i * a.g.rpi;
-    const int valid = sr < a.g.SR ? valid_of(a.g, a.c, sr, k.p) : 0;
-    if (valid > 0) {
-      if (a.silu) normalise<T, V, true>(a, raw[i], c, out + sr * out_pitch, valid);
-      else normalise<T, V, false>(a, raw[i], c, out + sr * out_pitch, valid);
-    }
-  }
+  for (int i = 0; i < NV; ++i)
+    if (i < rows) normalise<T, V, SILU, STREAM>(a, raw[i], c, out + i * out_step, i == rows - 1 ? last : V);
 }
 
 // The gradient; dweight and dbias go to `part` [n][c] as an image's sums (or straight to their place where there is one image).
-template <typename T, int NV, bool SILU>
+template <typename T, int NV, int SLAB, bool SILU>
 __global__ __launch_bounds__(1024) void norm_whole_grad_kernel(const NormArgs a) {
   using namespace norm;
   constexpr int V = 16 / (int)sizeof(T);
+  constexpr bool STREAM = false;
   extern __shared__ char lds[];
   const Place k = place_whole(a.g);
-  const int cols = a.g.tp * V, groups = a.groups / a.g.slabs, channels = groups * a.cg;      // of the slab
+  const int cols = a.g.tp * V, groups = a.g.groups, channels = groups * a.cg;      // of the slab
   float2* const buffer = reinterpret_cast<float2*>(lds);
   float2* const col = buffer;                                // [element of the superrow]: sums (the buffer is free by then)
   float2* const term = buffer + cols;                        // [group]
-  const char* xb = static_cast<const char*>(a.x) + (k.image * a.x_image + (long)k.p * V) * (long)sizeof(T);
-  const char* db = static_cast<const char*>(a.dy) + (k.image * a.dy_image + (long)k.p * V) * (long)sizeof(T);
-  const long pitch = a.x_pitch * (long)sizeof(T), dy_pitch = a.dy_pitch * (long)sizeof(T);
+  const char* xb = static_cast<const char*>(a.x) + (k.image * a.x_image + (long)k.p * V + k.r * a.x_pitch) * (long)sizeof(T);
+  const char* db = static_cast<const char*>(a.dy) + (k.image * a.dy_image + (long)k.p * V + k.r * a.dy_pitch) * (long)sizeof(T);
+  const long step = a.g.rpi * a.x_pitch * (long)sizeof(T), dy_step = a.g.rpi * a.dy_pitch * (long)sizeof(T);
+  const int rows = k.active ? a.g.few + (k.r < a.g.more ? 1 : 0) : 0;
+  const int last = SLAB == kTail && k.r == a.g.last_r ? min(a.g.tail * a.c - k.p * V, V) : V;
   typename RawOf<typename Bits<T>::type, V>::type x[NV], dy[NV];
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+    if (i < rows) {
+      x[i] = load<T, V>(xb + i * step, i == rows - 1 ? last : V);
+      dy[i] = load<T, V>(db + i * dy_step, i == rows - 1 ? last : V);
+    }
   Terms<V> c;
   Where<V> here;
   float sb[V], sw[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) sb[j] = sw[j] = 0.0f;
   if (k.active) {
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int sr = k.r + i * a.g.rpi;
-      const int valid = sr < a.g.SR ? valid_of(a.g, a.c, sr, k.p) : 0;
-      if (valid > 0) {
-        x[i] = load<T, V>(xb + sr * pitch, valid);
-        dy[i] = load<T, V>(db + sr * dy_pitch, valid);
-      }
-    }
     here = where<V>(a, k.p * V);
     all_terms<V>(a, k.image, here, c);
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int sr = k.r + i * a.g.rpi;
-      const int valid = sr < a.g.SR ? valid_of(a.g, a.c, sr, k.p) : 0;
-      if (valid > 0) gradient_sums<T, V, SILU>(a, x[i], dy[i], c, sb, sw, valid);
-    }
+    for (int i = 0; i < NV; ++i)
+      if (i < rows) gradient_sums<T, V, SILU>(a, x[i], dy[i], c, sb, sw, i == rows - 1 ? last : V);
   }
   add_rows<V>(sb, sw, k.r, a.g.tp, a.g.rpi, k.active, buffer);
-  const int q0 = ((int)threadIdx.x) * V;
   if (k.active && k.r == 0) {
 #pragma unroll
-    for (int j = 0; j < V; ++j) col[q0 + j] = make_float2(sb[j], sw[j]);
+    for (int j = 0; j < V; ++j) col[(int)threadIdx.x * V + j] = make_float2(sb[j], sw[j]);
   }
   __syncthreads();
   const int ch0 = k.part * channels;
@@ -728,13 +916,9 @@ __global__ __launch_bounds__(1024) void norm_whole_grad_kernel(const NormArgs a)
     }
   }
   {
-    const int lanes = lanes_of(groups), lane = (int)threadIdx.x & (lanes - 1), per = (int)blockDim.x / lanes;
+    const int lanes = a.g.lanes, lane = (int)threadIdx.x & (lanes - 1), per = (int)blockDim.x / lanes;
     for (int g = (int)threadIdx.x / lanes; g < groups; g += per) {
-      const double2 s = lanes_sum(lane, lanes, a.g.R, a.cg, [&](int rr, int ch) __attribute__((always_inline)) {
-        const float2 e = col[rr * a.c + g * a.cg + ch];
-        const double w = a.weight ? a.weight[ch0 + g * a.cg + ch] : 1.0f;
-        return make_double2(w * e.x, w * e.y);
-      });
+      const double2 s = group_terms(a, col, lane, lanes, g, ch0 + g * a.cg);
       if (lane == 0) term[g] = make_float2((float)(s.x * a.inv_count), (float)(s.y * a.inv_count));
     }
   }
@@ -743,14 +927,79 @@ __global__ __launch_bounds__(1024) void norm_whole_grad_kernel(const NormArgs a)
   float2 t[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) t[j] = term[here.group[j] - k.part * groups];
-  char* out = static_cast<char*>(a.y) + ((long)k.image * a.pixels * a.c + (long)k.p * V) * (long)sizeof(T);
-  const long out_pitch = (long)a.g.P * V * (long)sizeof(T);
+  char* out = static_cast<char*>(a.y) + ((long)k.image * a.pixels * a.c + (long)(k.r * a.g.P + k.p) * V) * (long)sizeof(T);
+  const long out_step = (long)a.g.rpi * a.g.P * V * (long)sizeof(T);
 #pragma unroll
-  for (int i = 0; i < NV; ++i) {
-    const int sr = k.r + i * a.g.rpi;
-    const int valid = sr < a.g.SR ? valid_of(a.g, a.c, sr, k.p) : 0;
-    if (valid > 0) gradient<T, V, SILU>(a, x[i], dy[i], c, t, out + sr * out_pitch, valid);
-  }
+  for (int i = 0; i < NV; ++i)
+    if (i < rows) gradient<T, V, SILU, STREAM>(a, x[i], dy[i], c, t, out + i * out_step, i == rows - 1 ? last : V);
 }
+
+// ---- launches of a type ---------------------------------------------------------------------------
+
+enum NormPass { kNormWhole, kNormWholeGrad, kNormStats, kNormApply, kNormGradSums, kNormGradApply };
+
+struct NormLaunch {
+  unsigned grid, lds, vector_groups;      // bytes of LDS; work-groups for dweight and dbias
+  bool silu, stream;
+};
+
+namespace norm {
+
+template <typename F> void with_flag(bool b, F&& f) { b ? f(std::true_type()) : f(std::false_type()); }
+template <typename F> void with_vectors(int nv, F&& f) {      // rounded up to a built form
+  if (nv <= 1) f(std::integral_constant<int, 1>());
+  else if (nv <= 2) f(std::integral_constant<int, 2>());
+  else if (nv <= 4) f(std::integral_constant<int, 4>());
+  else if (nv <= 8) f(std::integral_constant<int, 8>());
+  else f(std::integral_constant<int, 16>());
+}
+template <typename F> void with_slab(int slab, F&& f) {
+  if (slab == kMerge) f(std::integral_constant<int, kMerge>());
+  else if (slab == kTail) f(std::integral_constant<int, kTail>());
+  else f(std::integral_constant<int, kPlain>());
+}
+template <typename T, typename F> void with_length(int v, F&& f) {
+  if (v == 1) f(std::integral_constant<int, 1>());
+  else if (v == 2) f(std::integral_constant<int, 2>());
+  else if (v == 4 || sizeof(T) == 4) f(std::integral_constant<int, 4>());
+  else f(std::integral_constant<int, sizeof(T) == 4 ? 4 : 8>());
+}
+
+}  // namespace norm
+
+template <typename T> void launch_norm(NormPass pass, const NormArgs& a, const NormLaunch& l, hipStream_t s) {
+  using namespace norm;
+  const NormGeom& g = a.g;
+  with_flag(l.silu, [&](auto silu) {
+    constexpr bool SILU = decltype(silu)::value;
+    if (pass == kNormWhole || pass == kNormWholeGrad) {
+      const int slab = g.tail != g.R ? kTail : pass == kNormWhole && a.cg % g.V == 0 ? kMerge : kPlain;
+      with_vectors(g.nv, [&](auto nv) {
+        with_slab(slab, [&](auto form) {
+          constexpr int NV = decltype(nv)::value, SLAB = decltype(form)::value;
+          if (pass == kNormWhole) {
+            norm_whole_kernel<T, NV, SLAB, SILU><<<l.grid, g.threads, l.lds, s>>>(a);
+          } else if constexpr (NV <= kNormWholeGradVectors && SLAB != kMerge) {
+            norm_whole_grad_kernel<T, NV, SLAB, SILU><<<l.grid, g.threads, l.lds, s>>>(a);
+          }
+        });
+      });
+      return;
+    }
+    with_length<T>(g.V, [&](auto v) {
+      constexpr int V = decltype(v)::value;
+      with_flag(l.stream, [&](auto stream) {
+        constexpr bool STREAM = decltype(stream)::value;
+        if (pass == kNormStats) norm_stats_kernel<T, V><<<l.grid, kThreads, 0, s>>>(a);
+        else if (pass == kNormApply) norm_apply_kernel<T, V, SILU, STREAM><<<l.grid, kThreads, l.lds, s>>>(a);
+        else if (pass == kNormGradSums) norm_grad_sums_kernel<T, V, SILU><<<l.grid, kThreads, 0, s>>>(a);
+        else norm_grad_apply_kernel<T, V, SILU, STREAM><<<l.grid + l.vector_groups, kThreads, l.lds, s>>>(a, l.vector_groups);
+      });
+    });
+  });
+}
+void launch_norm_f32(NormPass pass, const NormArgs& a, const NormLaunch& l, hipStream_t s);
+void launch_norm_f16(NormPass pass, const NormArgs& a, const NormLaunch& l, hipStream_t s);
+void launch_norm_bf16(NormPass pass, const NormArgs& a, const NormLaunch& l, hipStream_t s);
 
 }  // namespace cprune

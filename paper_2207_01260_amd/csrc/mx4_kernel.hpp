@@ -39,7 +39,7 @@ template <int BYTE> __device__ __forceinline__ float16v mma32(uint4 a, int as, u
 }
 
 template <bool SILU> __device__ __forceinline__ float finish(float z, float lo, float hi) {
-  if constexpr (SILU) return z * __builtin_amdgcn_rcpf(1.0f + __expf(-z));
+  if constexpr (SILU) return z * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(z * -1.44269504f));      // (2^x flushes below 2^-126: 1 + e^-z does not see it)
   z = z < lo ? lo : z;      // (comparisons and not minimum / maximum: a NaN stays one)
   return z > hi ? hi : z;
 }
