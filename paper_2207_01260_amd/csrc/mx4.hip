@@ -1,7 +1,6 @@
 // Entry points of the microscaled 4-bit numbers; quantisation and the way back (mx4_kernel.hpp has the products).
 #include <limits>
 
-#include "group_norm_kernel.hpp"
 #include "mx4_kernel.hpp"
 
 namespace cprune {
@@ -15,41 +14,12 @@ __device__ __forceinline__ unsigned quad_max(unsigned v) {
   return max(v, (unsigned)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, true));
 }
 
-// The scale's byte from the largest magnitude's bits (as integers, magnitudes order like numbers, NaN above infinity).
-__device__ __forceinline__ int scale_byte(unsigned top) {
-  const int e = (int)(top >> 23);
-  return e == 255 ? 255 : max(e - 2, 0);
-}
-__device__ __forceinline__ float scale_value(int s) {      // 2^(s - 127), NaN for 255
-  return __uint_as_float(s == 255 ? 0x7fc00000u : s == 0 ? 0x00400000u : (unsigned)s << 23);
-}
-
 // Codes and scale of eight numbers at p, of which `valid` are there; the four lanes of a quad hold a block.
 template <typename T> __device__ __forceinline__ unsigned quantize8(const T* p, int valid, int& s) {
-  constexpr int V = 16 / (int)sizeof(T);
-  float v[8];
-#pragma unroll
-  for (int h = 0; h < 8; h += V) {
-    if (valid - h > 0) {
-      const auto raw = norm::load<T, V>(p + h, valid - h);
-#pragma unroll
-      for (int j = 0; j < V; ++j) v[h + j] = norm::widen<T>(raw[j]);
-    } else {
-#pragma unroll
-      for (int j = 0; j < V; ++j) v[h + j] = 0.0f;
-    }
-  }
-  unsigned top = 0;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
-  s = scale_byte(quad_max(top));
-  const float f = scale_value(s);
-  unsigned c = 0;
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[0], v[1], f, 0);
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2], v[3], f, 1);
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4], v[5], f, 2);
-  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6], v[7], f, 3);
-  return s == 255 ? 0u : c;
+  mx4::Eight<T> e;
+  e.load(p, valid);
+  s = mx4::scale_byte(mx4::Eight<T>::widen(quad_max(e.top())));
+  return mx4::codes_of(e, s);
 }
 
 template <typename T>
@@ -117,32 +87,32 @@ template <typename T> __global__ __launch_bounds__(256) void mx4_arrange_kernel(
 template <typename T>
 __global__ __launch_bounds__(kQuad) void mx4_dequantize_kernel(const unsigned* __restrict__ codes, const unsigned char* __restrict__ scales,
                                                                int rows, int k, int blocks, T* __restrict__ y) {
-  constexpr int V = 16 / (int)sizeof(T);
   const unsigned i = blockIdx.x * (unsigned)kQuad + threadIdx.x, per = 4u * blocks;
   if (i >= (unsigned)rows * per) return;
   const unsigned row = i / per, at = (i - row * per) * 8;
   const int valid = k - (int)at;
   if (valid <= 0) return;
   const unsigned c = codes[i];
-  const float f = scale_value(scales[i >> 2]);
+  const float f = mx4::scale_value(scales[i >> 2]);
   typedef float float2v __attribute__((ext_vector_type(2)));
-  float v[8];
   // (exact: a code's value times a power of two; the product and not the instruction's own scale, whose NaN and 2^-127 it need not know)
-#define CPRUNE_MX4_PAIR(n)                                                       \
-  {                                                                              \
-    const float2v q = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, n);      \
-    v[2 * n] = q.x * f, v[2 * n + 1] = q.y * f;                                  \
-  }
-  CPRUNE_MX4_PAIR(0) CPRUNE_MX4_PAIR(1) CPRUNE_MX4_PAIR(2) CPRUNE_MX4_PAIR(3)
-#undef CPRUNE_MX4_PAIR
+  const float2v q[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 1),
+                        __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, 1.0f, 3)};
+  constexpr int V = 16 / (int)sizeof(T);
+  typedef T outs __attribute__((ext_vector_type(V), aligned(sizeof(T))));
   T* p = y + (long)row * k + at;
 #pragma unroll
   for (int h = 0; h < 8; h += V) {
-    if (valid - h <= 0) break;
-    float part[V];
+    outs v;
 #pragma unroll
-    for (int j = 0; j < V; ++j) part[j] = v[h + j];
-    norm::store<T, V>(p + h, part, valid - h);
+    for (int j = 0; j < V; ++j) v[j] = Elem<T>::from_f32(q[(h + j) / 2][j & 1] * f);
+    if (valid - h >= V) {
+      *reinterpret_cast<outs*>(p + h) = v;
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j)
+        if (h + j < valid) p[h + j] = v[j];
+    }
   }
 }
 
@@ -174,41 +144,87 @@ void launch_quantize(const void* x, int rows, int k, int x_stride, int dtype, vo
   });
 }
 
-// Scratch of a product: the tile kernel's operands, or the rows' codes.
+// How a product runs, and its scratch.
+enum ProductForm { kFew, kShort, kTiles };
 struct ProductPlan {
-  int mi;                            // blocks a wavefront of the tile kernel has on a side, 0: the wave kernel
+  ProductForm form;
+  int mi;                            // kTiles: 16-row blocks a wavefront has on a side
+  bool codes_first;                  // the rows' codes are made by a launch of their own, row by row
   size_t codes, x_scales, w_scales;  // bytes
   size_t total() const { return codes + x_scales + w_scales; }
 };
 
 ProductPlan plan_product(int rows, int k, int c_out, bool numbers) {
-  const long blocks = blocks_of(k), fours = (blocks + 15) / 16;
+  const long blocks = blocks_of(k), steps = (blocks + 3) / 4, fours = (steps + 3) / 4;
   ProductPlan q = {};
-  if (rows >= 512 && (double)(rows + 63) * fours * 512 < 2147483648.0) q.mi = (double)rows * c_out >= 256.0 * 256 * 128 ? 8 : 4;
-  if (q.mi) {
+  if (rows > 32 && steps <= 8 && (double)c_out * k <= 262144.0) {
+    q.form = kShort;
+  } else if (rows >= 512 && (double)(rows + 63) * fours * 512 < 2147483648.0) {
+    q.form = kTiles;
+    q.mi = (double)rows * c_out >= 256.0 * 256 * 128 ? 8 : 4;
     q.codes = (size_t)((rows + 15L) / 16 * fours * 4096);
     q.x_scales = (size_t)((rows + 63L) / 64 * fours * 1024);
     q.w_scales = (size_t)((c_out + 32L * q.mi - 1) / (32L * q.mi) * (q.mi / 2) * fours * 1024);
-  } else if (numbers) {
+  } else {
+    q.form = kFew;
+    q.codes_first = numbers && rows > 16;
+  }
+  if (q.codes_first) {
     q.codes = (size_t)((long)rows * blocks * 16);
-    q.x_scales = (size_t)((long)rows * blocks + 15) & ~(size_t)15;
+    q.x_scales = ((size_t)((long)rows * blocks) + 15) & ~(size_t)15;
   }
   return q;
 }
 
-// x: numbers of x_dtype, or (x_scales given) codes
+template <typename F> void with_flag(bool b, F&& f) { b ? f(std::true_type()) : f(std::false_type()); }
+template <typename X, typename T, bool SILU> void launch_few(Mx4Args p, hipStream_t s) {
+  const int steps = (p.blocks + 3) / 4;
+  auto go = [&](auto mb, auto nb, auto waves) {
+    constexpr int MB = decltype(mb)::value, NB = decltype(nb)::value, WAVES = decltype(waves)::value;
+    p.tiles = (p.c_out + 16 * MB - 1) / (16 * MB);
+    const unsigned grid = (unsigned)((long)p.tiles * ((p.rows + 16 * NB - 1) / (16 * NB)));
+    mx4_few_kernel<X, T, SILU, MB, NB, WAVES><<<grid, 64 * WAVES, 0, s>>>(p);
+  };
+  typedef std::integral_constant<int, 1> one;
+  typedef std::integral_constant<int, 2> two;
+  typedef std::integral_constant<int, 4> four;
+  typedef std::integral_constant<int, 16> sixteen;
+  if (p.rows <= 16) {
+    if (steps > 8) go(one(), one(), sixteen());
+    else go(one(), one(), four());
+  } else if constexpr (std::is_same<X, void>::value) {
+    if (p.rows <= 32) go(one(), two(), std::integral_constant<int, 8>());
+    else go(two(), four(), std::integral_constant<int, 8>());
+  }
+}
+template <typename X, typename T, bool SILU> void launch_short(const Mx4Args& p, hipStream_t s) {
+  const int steps = (p.blocks + 3) / 4;
+  const dim3 grid((unsigned)((p.rows + 63) / 64), 1);
+  auto go = [&](auto n) {
+    if (p.c_out > 32) mx4_rows_kernel<X, T, SILU, 4, 1, decltype(n)::value><<<grid, 256, 0, s>>>(p);
+    else mx4_rows_kernel<X, T, SILU, 2, 1, decltype(n)::value><<<grid, 256, 0, s>>>(p);
+  };
+  if (steps <= 1) go(std::integral_constant<int, 1>());
+  else if (steps <= 2) go(std::integral_constant<int, 2>());
+  else if (steps <= 4) go(std::integral_constant<int, 4>());
+  else go(std::integral_constant<int, 8>());
+}
+template <typename T, bool SILU> void launch_tiles(Mx4Args p, int mi, hipStream_t s) {
+  p.tiles = (p.c_out + 32 * mi - 1) / (32 * mi);
+  p.row_tiles = (p.rows + 32 * mi - 1) / (32 * mi);
+  const unsigned grid = (unsigned)((long)p.tiles * p.row_tiles);
+  if (mi == 8) mx4_tile_kernel<T, SILU, 8, 8><<<grid, 256, 0, s>>>(p);
+  else mx4_tile_kernel<T, SILU, 4, 4><<<grid, 256, 0, s>>>(p);
+}
+
+// x: numbers of `dtype`, or (x_scales given) codes
 void launch_product(Mx4Args p, const void* x, const void* x_scales, int k, long x_stride, int act, int dtype, void* ws, const ProductPlan& q, hipStream_t s) {
   const float inf = std::numeric_limits<float>::infinity();
   p.lo = act == CPRUNE_ACT_NONE ? -inf : 0.0f;
   p.hi = act == CPRUNE_ACT_RELU6 ? 6.0f : inf;
-  const bool silu = act == CPRUNE_ACT_SILU;
-  auto tiles = [&](int outs, int rows) {
-    p.tiles = (p.c_out + outs - 1) / outs;
-    p.row_tiles = (p.rows + rows - 1) / rows;
-    return dim3((unsigned)((long)p.tiles * p.row_tiles));
-  };
   char* const scratch = static_cast<char*>(ws);
-  if (q.mi) {
+  bool codes = x_scales != nullptr;
+  if (q.form == kTiles) {
     const int fours = (p.blocks + 15) / 16;
     Mx4Arrange r = {};
     r.x = x, r.xs = static_cast<const unsigned char*>(x_scales), r.ws = p.as, r.x_stride = x_stride;
@@ -218,30 +234,28 @@ void launch_product(Mx4Args p, const void* x, const void* x_scales, int k, long 
     r.x_scales = reinterpret_cast<unsigned*>(scratch + q.codes);
     r.w_scales = reinterpret_cast<unsigned*>(scratch + q.codes + q.x_scales);
     const unsigned groups = (unsigned)(r.row_groups + q.w_scales / 1024);
-    if (x_scales) mx4_arrange_kernel<void><<<groups, 256, 0, s>>>(r);
+    if (codes) mx4_arrange_kernel<void><<<groups, 256, 0, s>>>(r);
     else with_type(dtype, [&](auto t) { mx4_arrange_kernel<decltype(t)><<<groups, 256, 0, s>>>(r); });
     p.bo = reinterpret_cast<const unsigned char*>(r.codes), p.bso = r.x_scales, p.aso = r.w_scales;
-  } else if (!x_scales) {
+  } else if (q.codes_first) {
     launch_quantize(x, p.rows, k, (int)x_stride, dtype, scratch, scratch + q.codes, s);
     p.b = reinterpret_cast<const unsigned char*>(scratch), p.bs = p.b + q.codes;
-  } else {
+    codes = true;
+  } else if (codes) {
     p.b = static_cast<const unsigned char*>(x), p.bs = static_cast<const unsigned char*>(x_scales);
+  } else {
+    p.x = x, p.x_stride = x_stride, p.k = k;
   }
   with_type(dtype, [&](auto t) {
     using T = decltype(t);
-    if (q.mi == 8) {
-      const dim3 grid = tiles(256, 256);
-      if (silu) mx4_tile_kernel<T, true, 8, 8><<<grid, 256, 0, s>>>(p);
-      else mx4_tile_kernel<T, false, 8, 8><<<grid, 256, 0, s>>>(p);
-    } else if (q.mi == 4) {
-      const dim3 grid = tiles(128, 128);
-      if (silu) mx4_tile_kernel<T, true, 4, 4><<<grid, 256, 0, s>>>(p);
-      else mx4_tile_kernel<T, false, 4, 4><<<grid, 256, 0, s>>>(p);
-    } else {
-      const dim3 grid = tiles(32, 32);
-      if (silu) mx4_wave_kernel<T, true, 2, 2, 4><<<grid, 256, 0, s>>>(p);
-      else mx4_wave_kernel<T, false, 2, 2, 4><<<grid, 256, 0, s>>>(p);
-    }
+    with_flag(act == CPRUNE_ACT_SILU, [&](auto silu) {
+      constexpr bool SILU = decltype(silu)::value;
+      if (q.form == kTiles) launch_tiles<T, SILU>(p, q.mi, s);
+      else if (q.form == kShort && codes) launch_short<void, T, SILU>(p, s);
+      else if (q.form == kShort) launch_short<T, T, SILU>(p, s);
+      else if (codes) launch_few<void, T, SILU>(p, s);
+      else launch_few<T, T, SILU>(p, s);
+    });
   });
 }
 

@@ -8,7 +8,10 @@ namespace cprune {
 
 struct Mx4Args {
   const unsigned char *a, *as;   // weights' codes and scales, [c_out][blocks * 16], [c_out][blocks]
-  const unsigned char *b, *bs;   // the rows', [rows][blocks * 16], [rows][blocks]
+  const unsigned char *b, *bs;   // the rows', [rows][blocks * 16], [rows][blocks]; or
+  const void* x;                 // the rows as numbers, [rows][x_stride]
+  long x_stride;
+  int k;
   const float* bias;
   void* y;                       // [rows][c_out]
   int rows, c_out, blocks;
@@ -22,7 +25,6 @@ struct Mx4Args {
 namespace mx4 {
 
 typedef int int8v __attribute__((ext_vector_type(8)));
-constexpr unsigned kOne = 127;   // the scale's byte that stands for 1
 
 // The matrix instruction's operand: lane l holds row l % 16 and the 32 elements of block l / 16, in four registers; byte BYTE of `as` and `bs` is the
 // block's scale.
@@ -52,76 +54,290 @@ __device__ __forceinline__ uint4 load16(__amdgpu_buffer_rsrc_t r, unsigned off) 
 
 }  // namespace mx4
 
-// One wavefront-wide operand straight from memory, MB x NB blocks of 16 x 16 results a work-group, its WAVES wavefronts taking every WAVES-th
-// 128 terms; their sums are joined through LDS in a fixed order.  Blocks past the last row or term read zeros with scale 1.
-template <typename T, bool SILU, int MB, int NB, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void mx4_wave_kernel(const Mx4Args p) {
-  using namespace mx4;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lrow = lane & 15, lblk = lane >> 4;
-  const int tr = blockIdx.x / (unsigned)p.tiles, o0 = ((int)blockIdx.x - tr * p.tiles) * 16 * MB, r0 = tr * 16 * NB;
-  const unsigned a_bytes = (unsigned)p.c_out * p.blocks, b_bytes = (unsigned)p.rows * p.blocks;
-  const __amdgpu_buffer_rsrc_t ar = make_rsrc(p.a, a_bytes * 16), asr = make_rsrc(p.as, a_bytes), br = make_rsrc(p.b, b_bytes * 16),
-                               bsr = make_rsrc(p.bs, b_bytes);
-  float4_t acc[MB][NB];
+// ---- numbers to codes ------------------------------------------------------------------------------
+namespace mx4 {
+
+// Eight neighbouring numbers as they are in memory, zeros past the last.
+template <typename X> struct Eight {
+  typedef unsigned short ushort2v __attribute__((ext_vector_type(2)));
+  unsigned w[4];
+  __device__ __forceinline__ void load(const X* p, int valid) {
+    typedef unsigned uint4u __attribute__((ext_vector_type(4), aligned(2)));
+    if (valid >= 8) {
+      const uint4u v = *reinterpret_cast<const uint4u*>(p);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = v[i];
+    } else {
+      const unsigned short* h = reinterpret_cast<const unsigned short*>(p);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = (2 * i < valid ? (unsigned)h[2 * i] : 0u) | (2 * i + 1 < valid ? (unsigned)h[2 * i + 1] << 16 : 0u);
+    }
+  }
+  // largest magnitude, in a form that orders like it (as integers, magnitudes order like numbers, NaN above infinity)
+  __device__ __forceinline__ unsigned top() const {
+    ushort2v m = __builtin_bit_cast(ushort2v, w[0] & 0x7fff7fffu);
+#pragma unroll
+    for (int i = 1; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(ushort2v, w[i] & 0x7fff7fffu));
+    return max((unsigned)m[0], (unsigned)m[1]);
+  }
+  // the same as the bits of an fp32 number
+  static __device__ __forceinline__ unsigned widen(unsigned top) {
+    if constexpr (std::is_same<X, __bf16>::value) return top << 16;
+    else return __float_as_uint((float)__builtin_bit_cast(_Float16, (unsigned short)top));
+  }
+  template <int I> __device__ __forceinline__ unsigned pair(unsigned c, float scale) const {
+    if constexpr (std::is_same<X, __bf16>::value) {
+      typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+      return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, w[I]), scale, I);
+    } else {
+      typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+      return __builtin_amdgcn_cvt_scalef32_pk_fp4_f16(c, __builtin_bit_cast(half2v, w[I]), scale, I);
+    }
+  }
+};
+template <> struct Eight<float> {
+  float v[8];
+  __device__ __forceinline__ void load(const float* p, int valid) {
+    typedef float float4u __attribute__((ext_vector_type(4), aligned(4)));
+    if (valid >= 8) {
+      const float4u lo = *reinterpret_cast<const float4u*>(p), hi = *reinterpret_cast<const float4u*>(p + 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = lo[i], v[4 + i] = hi[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = i < valid ? p[i] : 0.0f;
+    }
+  }
+  __device__ __forceinline__ unsigned top() const {
+    unsigned m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+    return m;
+  }
+  static __device__ __forceinline__ unsigned widen(unsigned top) { return top; }
+  template <int I> __device__ __forceinline__ unsigned pair(unsigned c, float scale) const {
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2 * I], v[2 * I + 1], scale, I);
+  }
+};
+
+// the scale's byte from the largest magnitude's bits
+__device__ __forceinline__ int scale_byte(unsigned top) {
+  const int e = (int)(top >> 23);
+  return e == 255 ? 255 : max(e - 2, 0);
+}
+__device__ __forceinline__ float scale_value(int s) {      // 2^(s - 127), NaN for 255
+  return __uint_as_float(s == 255 ? 0x7fc00000u : s == 0 ? 0x00400000u : (unsigned)s << 23);
+}
+// eight codes; the instruction divides by the scale, rounds half to even and stops at 6
+template <typename X> __device__ __forceinline__ unsigned codes_of(const Eight<X>& e, int s) {
+  const float f = scale_value(s);
+  unsigned c = 0;
+  c = e.template pair<0>(c, f);
+  c = e.template pair<1>(c, f);
+  c = e.template pair<2>(c, f);
+  c = e.template pair<3>(c, f);
+  return s == 255 ? 0u : c;
+}
+
+// A block of 32 by one lane: the matrix instruction's operand and its scale.
+template <typename X> struct Block {
+  Eight<X> e[4];
+  __device__ __forceinline__ void load(const X* p, int valid) {
+    if (valid >= 32) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) e[i].load(p + 8 * i, 8);
+    } else if (valid > 0) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) e[i].load(p + 8 * i, valid - 8 * i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) e[i] = Eight<X>();
+    }
+  }
+  __device__ __forceinline__ void quantize(uint4& codes, int& scale) const {
+    scale = scale_byte(Eight<X>::widen(max(max(e[0].top(), e[1].top()), max(e[2].top(), e[3].top()))));
+    codes = make_uint4(codes_of(e[0], scale), codes_of(e[1], scale), codes_of(e[2], scale), codes_of(e[3], scale));
+  }
+};
+
+// The rows' side of a product: numbers of X, or codes (X = void).  Held: a lane's block on its way.
+template <typename X> struct Rows {
+  struct Held {
+    Block<X> b;
+    __device__ __forceinline__ void operand(uint4& codes, int& scale) const { b.quantize(codes, scale); }
+  };
+  const X* x;
+  long stride;
+  int rows, k;
+  __device__ __forceinline__ explicit Rows(const Mx4Args& p) : x(static_cast<const X*>(p.x)), stride(p.x_stride), rows(p.rows), k(p.k) {}
+  __device__ __forceinline__ void load(Held& h, int r, int blk) const { h.b.load(x + min(r, rows - 1) * stride + blk * 32l, r < rows ? k - blk * 32 : 0); }
+};
+template <> struct Rows<void> {
+  struct Held {
+    uint4 c;
+    int s;
+    __device__ __forceinline__ void operand(uint4& codes, int& scale) const { codes = c, scale = s; }
+  };
+  __amdgpu_buffer_rsrc_t codes_at, scales_at;
+  int rows, blocks;
+  __device__ __forceinline__ explicit Rows(const Mx4Args& p)
+      : codes_at(make_rsrc(p.b, (unsigned)p.rows * p.blocks * 16u)), scales_at(make_rsrc(p.bs, (unsigned)p.rows * p.blocks)), rows(p.rows), blocks(p.blocks) {}
+  __device__ __forceinline__ void load(Held& h, int r, int blk) const {
+    const bool in = r < rows && blk < blocks;
+    const unsigned at = (unsigned)r * blocks + blk;
+    h.c = load16(codes_at, in ? at * 16 : kOutOfRange);
+    h.s = (int)__builtin_amdgcn_raw_buffer_load_b8(scales_at, in ? (int)at : (int)kOutOfRange, 0, 0);      // (0 out of range: as good a scale as any for zeros)
+  }
+};
+
+// The weights' operands: rows o of 16, straight from memory.
+struct Weights {
+  __amdgpu_buffer_rsrc_t codes_at, scales_at;
+  int c_out, blocks;
+  __device__ __forceinline__ explicit Weights(const Mx4Args& p)
+      : codes_at(make_rsrc(p.a, (unsigned)p.c_out * p.blocks * 16u)), scales_at(make_rsrc(p.as, (unsigned)p.c_out * p.blocks)), c_out(p.c_out), blocks(p.blocks) {}
+  __device__ __forceinline__ void load(int o, int blk, uint4& c, int& s) const {
+    const bool in = o < c_out && blk < blocks;
+    const unsigned at = (unsigned)o * blocks + blk;
+    c = load16(codes_at, in ? at * 16 : kOutOfRange);
+    s = (int)__builtin_amdgcn_raw_buffer_load_b8(scales_at, in ? (int)at : (int)kOutOfRange, 0, 0);
+  }
+};
+
+// 4 MB neighbouring outputs of a row from the sums of MB blocks; block i's row 4 g + e is output 4 MB g + 4 i + e of the tile
+template <typename T, bool SILU, int MB> __device__ __forceinline__ void store_outputs(const Mx4Args& p, const float4_t (&v)[MB], const float4_t (&bias)[MB], int r, int o) {
+  if (r >= p.rows) return;
+  T* y = static_cast<T*>(p.y) + (long)r * p.c_out + o;
+  T z[4 * MB];
 #pragma unroll
   for (int i = 0; i < MB; ++i)
 #pragma unroll
-    for (int j = 0; j < NB; ++j) acc[i][j] = (float4_t){0.f, 0.f, 0.f, 0.f};
+    for (int e = 0; e < 4; ++e) z[4 * i + e] = Elem<T>::from_f32(finish<SILU>(v[i][e] + bias[i][e], p.lo, p.hi));
+  if (o + 4 * MB <= p.c_out) {
+    constexpr int W = 4 * MB < 16 / (int)sizeof(T) ? 4 * MB : 16 / (int)sizeof(T);      // numbers a store
+    typedef T outs __attribute__((ext_vector_type(W), aligned(sizeof(T))));
+#pragma unroll
+    for (int h = 0; h < 4 * MB; h += W) {
+      outs q;
+#pragma unroll
+      for (int e = 0; e < W; ++e) q[e] = z[h + e];
+      *reinterpret_cast<outs*>(y + h) = q;
+    }
+  } else {
+#pragma unroll
+    for (int h = 0; h < 4 * MB; ++h)
+      if (o + h < p.c_out) y[h] = z[h];
+  }
+}
+
+}  // namespace mx4
+
+// ---- few rows: the wavefronts of a work-group share the sum ------------------------------------------
+// 16 MB outputs by 16 NB rows a work-group; wavefront w takes steps w, w + WAVES, ... of 128 terms, both operands straight from memory (each weight is read
+// once, by one wavefront), the rows' numbers made codes by the lane that multiplies them.  The sums are joined through LDS in a fixed order.
+template <typename X, typename T, bool SILU, int MB, int NB, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void mx4_few_kernel(const Mx4Args p) {
+  using namespace mx4;
+  constexpr int U = 2;      // steps under way
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lrow = lane & 15, lblk = lane >> 4;
+  const int tr = blockIdx.x / (unsigned)p.tiles, o0 = ((int)blockIdx.x - tr * p.tiles) * 16 * MB, r0 = tr * 16 * NB;
+  const Weights w(p);
+  const Rows<X> x(p);
+  float4_t acc[NB][MB];
+#pragma unroll
+  for (int j = 0; j < NB; ++j)
+#pragma unroll
+    for (int i = 0; i < MB; ++i) acc[j][i] = (float4_t){0.f, 0.f, 0.f, 0.f};
   const int steps = (p.blocks + 3) / 4;
-  for (int st = wave; st < steps; st += WAVES) {
-    const int blk = st * 4 + lblk;
-    uint4 av[MB], bv[NB];
-    int as[MB], bs[NB];
+  for (int st = wave; st < steps; st += U * WAVES) {
+    uint4 a[U][MB];
+    int as[U][MB];
+    typename Rows<X>::Held rows[U][NB];
 #pragma unroll
-    for (int i = 0; i < MB; ++i) {
-      const int o = o0 + 16 * i + lrow;
-      const bool in = blk < p.blocks && o < p.c_out;
-      const unsigned at = (unsigned)o * p.blocks + blk;
-      av[i] = load16(ar, in ? at * 16 : kOutOfRange);
-      as[i] = in ? (int)__builtin_amdgcn_raw_buffer_load_b8(asr, (int)at, 0, 0) : (int)kOne;
+    for (int u = 0; u < U; ++u) {
+      const int blk = (st + u * WAVES) * 4 + lblk;      // (past the last one: zeros)
+#pragma unroll
+      for (int i = 0; i < MB; ++i) w.load(o0 + 4 * MB * (lrow >> 2) + 4 * i + (lrow & 3), blk, a[u][i], as[u][i]);
+#pragma unroll
+      for (int j = 0; j < NB; ++j) x.load(rows[u][j], r0 + 16 * j + lrow, blk);
     }
 #pragma unroll
-    for (int j = 0; j < NB; ++j) {
-      const int r = r0 + 16 * j + lrow;
-      const bool in = blk < p.blocks && r < p.rows;
-      const unsigned at = (unsigned)r * p.blocks + blk;
-      bv[j] = load16(br, in ? at * 16 : kOutOfRange);
-      bs[j] = in ? (int)__builtin_amdgcn_raw_buffer_load_b8(bsr, (int)at, 0, 0) : (int)kOne;
-    }
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-    for (int i = 0; i < MB; ++i)
+      for (int j = 0; j < NB; ++j) {
+        uint4 b;
+        int bs;
+        rows[u][j].operand(b, bs);
 #pragma unroll
-      for (int j = 0; j < NB; ++j) acc[i][j] = mma(av[i], as[i], bv[j], bs[j], acc[i][j]);
+        for (int i = 0; i < MB; ++i) acc[j][i] = mma(a[u][i], as[u][i], b, bs, acc[j][i]);
+      }
   }
   __shared__ float4_t sums[WAVES - 1][MB * NB][64];
   if (wave > 0) {
 #pragma unroll
-    for (int i = 0; i < MB; ++i)
+    for (int j = 0; j < NB; ++j)
 #pragma unroll
-      for (int j = 0; j < NB; ++j) sums[wave - 1][i * NB + j][lane] = acc[i][j];
+      for (int i = 0; i < MB; ++i) sums[wave - 1][j * MB + i][lane] = acc[j][i];
   }
   __syncthreads();
   if (wave > 0) return;
+  const int o = o0 + 4 * MB * lblk;
+  float4_t bias[MB];
 #pragma unroll
-  for (int i = 0; i < MB; ++i) {
-    const int o = o0 + 16 * i + 4 * lblk;
-    const float4_t bias = load_bias4(p.bias, p.c_out, o);
+  for (int i = 0; i < MB; ++i) bias[i] = load_bias4(p.bias, p.c_out, o + 4 * i);
 #pragma unroll
-    for (int j = 0; j < NB; ++j) {
-      float4_t v = acc[i][j];
-      for (int w = 0; w < WAVES - 1; ++w) v += sums[w][i * NB + j][lane];
-      const int r = r0 + 16 * j + lrow;
-      if (r >= p.rows) continue;
-      T* y = static_cast<T*>(p.y) + (long)r * p.c_out + o;
-      float z[4];
+  for (int j = 0; j < NB; ++j) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        z[e] = finish<SILU>(v[e] + bias[e], p.lo, p.hi);
-      }
+    for (int i = 0; i < MB; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (o + e < p.c_out) y[e] = Elem<T>::from_f32(z[e]);
+      for (int q = 0; q < WAVES - 1; ++q) acc[j][i] += sums[q][j * MB + i][lane];
+    store_outputs<T, SILU, MB>(p, acc[j], bias, r0 + 16 * j + lrow, o);
+  }
+}
+
+// ---- many rows of short sums: the rows stay in registers ----------------------------------------------
+// A wavefront holds the codes of 16 NB rows, all of their at most 128 STEPS terms, and goes over all outputs; the weights come from the caches, where the
+// four wavefronts of a work-group read the same ones at about the same time.  x is read once and y written once.
+template <typename X, typename T, bool SILU, int MB, int NB, int STEPS>
+__global__ __launch_bounds__(256) void mx4_rows_kernel(const Mx4Args p) {
+  using namespace mx4;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, lrow = lane & 15, lblk = lane >> 4;
+  const int r0 = ((int)blockIdx.x * 4 + wave) * 16 * NB;
+  if (r0 >= p.rows) return;
+  const Weights w(p);
+  const Rows<X> x(p);
+  uint4 b[NB][STEPS];
+  int bs[NB][STEPS];
+#pragma unroll
+  for (int j = 0; j < NB; ++j) {
+    typename Rows<X>::Held rows[STEPS];
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) x.load(rows[st], r0 + 16 * j + lrow, st * 4 + lblk);
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) rows[st].operand(b[j][st], bs[j][st]);
+  }
+  for (int o0 = (int)blockIdx.y * 16 * MB; o0 < p.c_out; o0 += (int)gridDim.y * 16 * MB) {
+    const int o = o0 + 4 * MB * lblk;
+    float4_t bias[MB], acc[NB][MB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i) bias[i] = load_bias4(p.bias, p.c_out, o + 4 * i);
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+      for (int i = 0; i < MB; ++i) acc[j][i] = (float4_t){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int st = 0; st < STEPS; ++st) {
+      uint4 a[MB];
+      int as[MB];
+#pragma unroll
+      for (int i = 0; i < MB; ++i) w.load(o0 + 4 * MB * (lrow >> 2) + 4 * i + (lrow & 3), st * 4 + lblk, a[i], as[i]);
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int i = 0; i < MB; ++i) acc[j][i] = mma(a[i], as[i], b[j][st], bs[j][st], acc[j][i]);
     }
+#pragma unroll
+    for (int j = 0; j < NB; ++j) store_outputs<T, SILU, MB>(p, acc[j], bias, r0 + 16 * j + lrow, o);
   }
 }
 

@@ -73,17 +73,18 @@ def test_products_refuse():
     for kw in (dict(xc=None), dict(xs=None), dict(wc=None), dict(ws=None), dict(y=None), dict(xc=FAKE + 4), dict(wc=FAKE + 4), dict(rows=0), dict(k=0),
                dict(c_out=0), dict(act=4), dict(act=-1), dict(dtype=3), dict(rows=1 << 26, k=1), dict(c_out=1 << 26, k=1), dict(rows=1 << 20, c_out=1 << 12)):
         assert m(**kw) == B.ERR_INVALID_ARG, kw
-    need = L.cprune_mx4_matmul_workspace_bytes(4096, 64, 4096)
+    big = dict(rows=4096, k=4096, c_out=4096)       # (a product that needs scratch)
+    need = L.cprune_mx4_matmul_workspace_bytes(4096, 4096, 4096)
     assert need > 0 and L.cprune_mx4_matmul_workspace_bytes(4096, 0, 4096) == 0
-    assert m(rows=4096, c_out=4096, scratch=None) == m(rows=4096, c_out=4096, size=need - 1) == B.ERR_WORKSPACE
-    assert m(rows=4096, c_out=4096, scratch=FAKE + 8) == B.ERR_INVALID_ARG
+    assert m(scratch=None, **big) == m(size=need - 1, **big) == B.ERR_WORKSPACE
+    assert m(scratch=FAKE + 8, **big) == B.ERR_INVALID_ARG
     f = lambda x=FAKE, rows=4, k=64, stride=64, wc=FAKE, wsc=FAKE, c_out=8, act=0, dtype=0, y=FAKE, ws=FAKE, size=1 << 30: L.cprune_mx4_linear(
         x, rows, k, stride, wc, wsc, c_out, None, act, dtype, y, ws, size, None)
     for kw in (dict(x=None), dict(wc=None), dict(wsc=None), dict(y=None), dict(wc=FAKE + 4), dict(rows=0), dict(k=0), dict(c_out=0), dict(stride=63),
                dict(act=4), dict(dtype=3), dict(rows=1 << 26, k=1, stride=1), dict(rows=1 << 20, k=64, stride=1 << 12)):
         assert f(**kw) == B.ERR_INVALID_ARG, kw
-    big = dict(rows=4096, k=64, c_out=4096)
-    need = L.cprune_mx4_linear_workspace_bytes(4096, 64, 4096, 0)
+    big = dict(rows=4096, k=4096, c_out=4096, stride=4096)
+    need = L.cprune_mx4_linear_workspace_bytes(4096, 4096, 4096, 0)
     assert need > 0
     assert f(ws=None, **big) == f(size=need - 1, **big) == B.ERR_WORKSPACE
     assert f(ws=FAKE + 8, **big) == B.ERR_INVALID_ARG
