@@ -33,55 +33,51 @@ __global__ __launch_bounds__(kQuad) void mx4_quantize_kernel(const T* __restrict
   if ((threadIdx.x & 3) == 0) scales[i >> 2] = (unsigned char)s;
 }
 
-// What the tile kernel reads.  Work-groups up to `row_groups`: 16 rows x 512 terms of the rows in operand order, from numbers or (T = void) from codes; a wavefront takes
-// every fourth block of a row, a quad of lanes one block.  The others: 256 words of the weights' scales.
+// What the tile kernel reads: a work-group lays out 16 rows x 512 terms of a side, the rows' first, then the weights'.  A wavefront takes every fourth block of
+// a row, a quad of lanes one block.
 struct Mx4Arrange {
   const void* x;                     // numbers, or codes
-  const unsigned char *xs, *ws;      // scales of codes, of the weights
+  const unsigned char *xs, *w, *ws;  // scales of codes; the weights' codes and scales
   long x_stride;
-  int rows, k, c_out, blocks, mi;    // mi: blocks of c_out of a wavefront of the tile kernel
+  int rows, k, c_out, blocks, mi;    // mi: blocks of a wavefront of the tile kernel on a side
   int row_groups;
-  unsigned *codes, *x_scales, *w_scales;
+  unsigned *x_codes, *x_scales, *w_codes, *w_scales;
 };
 
 template <typename T> __global__ __launch_bounds__(256) void mx4_arrange_kernel(const Mx4Arrange p) {
-  const int fours = (p.blocks + 15) / 16;
-  if ((int)blockIdx.x < p.row_groups) {
-    const int b = blockIdx.x / (unsigned)fours, four = (int)blockIdx.x - b * fours;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, lrow = lane >> 2, quarter = lane & 3;
-    const int row = b * 16 + lrow;
-    unsigned scales = 0;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const int step = four * 4 + t, blk = step * 4 + wave;
-      unsigned c = 0;
-      int s = 0;
-      if constexpr (std::is_same<T, void>::value) {
-        if (row < p.rows && blk < p.blocks) {
-          const long at = (long)row * p.blocks + blk;
-          c = static_cast<const unsigned*>(p.x)[at * 4 + quarter];
-          s = p.xs[at];
-        }
-      } else {
-        const int at = blk * 32 + quarter * 8;
-        c = quantize8(static_cast<const T*>(p.x) + min(row, p.rows - 1) * p.x_stride + at, row < p.rows ? p.k - at : 0, s);
-      }
-      p.codes[((long)b * 4 * fours + step) * 256 + (wave * 16 + lrow) * 4 + quarter] = c;
-      scales |= (unsigned)s << (8 * t);
-    }
-    if (quarter == 0) p.x_scales[((long)(b >> 2) * fours + four) * 256 + (b & 3) * 64 + wave * 16 + lrow] = scales;
-    return;
-  }
-  const int chunk = (int)blockIdx.x - p.row_groups, g = chunk / fours, four = chunk - g * fours;
-  const int b = g * 4 + ((int)threadIdx.x >> 6), lane = threadIdx.x & 63, lrow = lane & 15, lblk = lane >> 4;
-  const int o = b / p.mi * 16 * p.mi + (p.mi == 8 ? mx4::spread_row<8>(b % 8, lrow) : mx4::spread_row<4>(b % 4, lrow));
-  unsigned w = 0;
+  const int fours = (p.blocks + 15) / 16, ab = 2 * p.mi;
+  const bool weights = (int)blockIdx.x >= p.row_groups;
+  const unsigned group = blockIdx.x - (weights ? p.row_groups : 0);
+  const int b = group / (unsigned)fours, four = (int)group - b * fours;      // 16-row block, four steps
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, lrow = lane >> 2, quarter = lane & 3;
+  int row = b * 16 + lrow;
+  if (weights) row = b / p.mi * 16 * p.mi + (p.mi == 8 ? mx4::spread_row<8>(b % 8, lrow) : mx4::spread_row<4>(b % 4, lrow));
+  const bool from_codes = weights || std::is_same<T, void>::value;
+  const unsigned* const codes_in = static_cast<const unsigned*>(weights ? static_cast<const void*>(p.w) : p.x);
+  const unsigned char* const scales_in = weights ? p.ws : p.xs;
+  const int rows = weights ? p.c_out : p.rows;
+  const int tile = b / ab, in_tile = b - tile * ab;
+  unsigned* const codes = (weights ? p.w_codes : p.x_codes) + ((long)(tile * fours + four) * 4 * ab + in_tile) * 256 + (wave * 16 + lrow) * 4 + quarter;
+  unsigned scales = 0;
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
-    const int blk = (four * 4 + t) * 4 + lblk;
-    if (o < p.c_out && blk < p.blocks) w |= (unsigned)p.ws[(long)o * p.blocks + blk] << (8 * t);
+    const int blk = (four * 4 + t) * 4 + wave;
+    unsigned c = 0;
+    int s = 0;
+    if (from_codes) {
+      if (row < rows && blk < p.blocks) {
+        const long at = (long)row * p.blocks + blk;
+        c = codes_in[at * 4 + quarter];
+        s = scales_in[at];
+      }
+    } else if constexpr (!std::is_same<T, void>::value) {
+      const int at = blk * 32 + quarter * 8;
+      c = quantize8(static_cast<const T*>(p.x) + min(row, p.rows - 1) * p.x_stride + at, row < p.rows ? p.k - at : 0, s);
+    }
+    codes[(long)t * ab * 256] = c;
+    scales |= (unsigned)s << (8 * t);
   }
-  p.w_scales[(long)chunk * 256 + threadIdx.x] = w;
+  if (quarter == 0) (weights ? p.w_scales : p.x_scales)[((long)(tile * fours + four) * ab + in_tile) * 64 + wave * 16 + lrow] = scales;
 }
 
 template <typename T>
@@ -150,8 +146,8 @@ struct ProductPlan {
   ProductForm form;
   int mi;                            // kTiles: 16-row blocks a wavefront has on a side
   bool codes_first;                  // the rows' codes are made by a launch of their own, row by row
-  size_t codes, x_scales, w_scales;  // bytes
-  size_t total() const { return codes + x_scales + w_scales; }
+  size_t codes, x_scales, w_codes, w_scales;  // bytes
+  size_t total() const { return codes + x_scales + w_codes + w_scales; }
 };
 
 ProductPlan plan_product(int rows, int k, int c_out, bool numbers) {
@@ -159,12 +155,12 @@ ProductPlan plan_product(int rows, int k, int c_out, bool numbers) {
   ProductPlan q = {};
   if (rows > 32 && steps <= 8 && (double)c_out * k <= 262144.0) {
     q.form = kShort;
-  } else if (rows >= 512 && (double)(rows + 63) * fours * 512 < 2147483648.0) {
+  } else if (rows >= 512 && (double)(rows + 255) * fours * 512 < 2147483648.0 && (double)(c_out + 255) * fours * 512 < 2147483648.0) {
     q.form = kTiles;
     q.mi = (double)rows * c_out >= 256.0 * 256 * 128 ? 8 : 4;
-    q.codes = (size_t)((rows + 15L) / 16 * fours * 4096);
-    q.x_scales = (size_t)((rows + 63L) / 64 * fours * 1024);
-    q.w_scales = (size_t)((c_out + 32L * q.mi - 1) / (32L * q.mi) * (q.mi / 2) * fours * 1024);
+    const long side = 32L * q.mi, row_tiles = (rows + side - 1) / side, tiles = (c_out + side - 1) / side, run = 2L * q.mi * fours;
+    q.codes = (size_t)(row_tiles * run * 4096), q.x_scales = (size_t)(row_tiles * run * 256);
+    q.w_codes = (size_t)(tiles * run * 4096), q.w_scales = (size_t)(tiles * run * 256);
   } else {
     q.form = kFew;
     q.codes_first = numbers && rows > 16;
@@ -213,8 +209,8 @@ template <typename T, bool SILU> void launch_tiles(Mx4Args p, int mi, hipStream_
   p.tiles = (p.c_out + 32 * mi - 1) / (32 * mi);
   p.row_tiles = (p.rows + 32 * mi - 1) / (32 * mi);
   const unsigned grid = (unsigned)((long)p.tiles * p.row_tiles);
-  if (mi == 8) mx4_tile_kernel<T, SILU, 8, 8><<<grid, 256, 0, s>>>(p);
-  else mx4_tile_kernel<T, SILU, 4, 4><<<grid, 256, 0, s>>>(p);
+  if (mi == 8) mx4_tile_kernel<T, SILU, 8><<<grid, 256, 0, s>>>(p);
+  else mx4_tile_kernel<T, SILU, 4><<<grid, 256, 0, s>>>(p);
 }
 
 // x: numbers of `dtype`, or (x_scales given) codes
@@ -227,16 +223,18 @@ void launch_product(Mx4Args p, const void* x, const void* x_scales, int k, long 
   if (q.form == kTiles) {
     const int fours = (p.blocks + 15) / 16;
     Mx4Arrange r = {};
-    r.x = x, r.xs = static_cast<const unsigned char*>(x_scales), r.ws = p.as, r.x_stride = x_stride;
+    r.x = x, r.xs = static_cast<const unsigned char*>(x_scales), r.w = p.a, r.ws = p.as, r.x_stride = x_stride;
     r.rows = p.rows, r.k = k, r.c_out = p.c_out, r.blocks = p.blocks, r.mi = q.mi;
-    r.row_groups = (p.rows + 15) / 16 * fours;
-    r.codes = reinterpret_cast<unsigned*>(scratch);
+    r.x_codes = reinterpret_cast<unsigned*>(scratch);
     r.x_scales = reinterpret_cast<unsigned*>(scratch + q.codes);
-    r.w_scales = reinterpret_cast<unsigned*>(scratch + q.codes + q.x_scales);
-    const unsigned groups = (unsigned)(r.row_groups + q.w_scales / 1024);
+    r.w_codes = reinterpret_cast<unsigned*>(scratch + q.codes + q.x_scales);
+    r.w_scales = reinterpret_cast<unsigned*>(scratch + q.codes + q.x_scales + q.w_codes);
+    r.row_groups = (int)(q.codes / 4096);
+    const unsigned groups = (unsigned)(r.row_groups + q.w_codes / 4096);
     if (codes) mx4_arrange_kernel<void><<<groups, 256, 0, s>>>(r);
     else with_type(dtype, [&](auto t) { mx4_arrange_kernel<decltype(t)><<<groups, 256, 0, s>>>(r); });
-    p.bo = reinterpret_cast<const unsigned char*>(r.codes), p.bso = r.x_scales, p.aso = r.w_scales;
+    p.bo = reinterpret_cast<const uint4*>(r.x_codes), p.bso = r.x_scales;
+    p.ao = reinterpret_cast<const uint4*>(r.w_codes), p.aso = r.w_scales;
   } else if (q.codes_first) {
     launch_quantize(x, p.rows, k, (int)x_stride, dtype, scratch, scratch + q.codes, s);
     p.b = reinterpret_cast<const unsigned char*>(scratch), p.bs = p.b + q.codes;

@@ -17,9 +17,9 @@ struct Mx4Args {
   int rows, c_out, blocks;
   float lo, hi;
   int tiles, row_tiles;          // tiles of c_out, of rows
-  // tile kernel: the rows' codes in operand order and both sides' scales, from mx4_arrange_kernel
-  const unsigned char* bo;       // [16-row block][step of four blocks, a multiple of four][lane][16 bytes], zeros past the last row and block
-  const unsigned *aso, *bso;     // [four 16-row blocks][four steps][16-row block][lane], byte t the scale of step t
+  // tile kernel: both sides in operand order, zeros past the last row and block, from mx4_arrange_kernel
+  const uint4 *ao, *bo;          // [tile][step, a multiple of four][16-row block of the tile][lane]
+  const unsigned *aso, *bso;     // [tile][four steps][16-row block of the tile][lane], byte t the scale of step t
 };
 
 namespace mx4 {
@@ -342,8 +342,9 @@ __global__ __launch_bounds__(256) void mx4_rows_kernel(const Mx4Args p) {
 }
 
 // ---- many rows: tiles through LDS -----------------------------------------------------------------
-// Four wavefronts (2 x 2) of MI x NI blocks each: 32 MI outputs of c_out by 32 NI rows a work-group, K in steps of 128 terms.  A stage is the tile's codes
-// of one step in operand order, [16-row block][lane][16 bytes], written to LDS by the loads themselves (a lane's address picks what its place gets).
+// Four wavefronts (2 x 2) of MI x MI blocks each: 32 MI outputs of c_out by 32 MI rows a work-group, K in steps of 128 terms.  A stage is the tile's codes
+// of one step in operand order, [16-row block][lane][16 bytes], as a launch before has laid them out in memory: a step of a tile is one run of memory, so its
+// loads spread over all channels of the L2 (rows of 2^n bytes read side by side would meet in one), and they write to LDS themselves.
 // While step s is multiplied, the operands of s + 1 go to registers and the codes of s + 4 into the stage that s has left.
 // The matrix instruction takes 32 rows of each side; those of a wavefront's c_out are dealt so that a lane's results are 8 MI neighbours of one row of y.
 namespace mx4 {
@@ -380,57 +381,37 @@ __device__ __forceinline__ void tile_of(const Mx4Args& p, int& tr, int& tc) {
 
 }  // namespace mx4
 
-template <typename T, bool SILU, int MI, int NI>
+template <typename T, bool SILU, int MI>
 __global__ __launch_bounds__(256) void mx4_tile_kernel(const Mx4Args p) {
   using namespace mx4;
-  static_assert(MI == NI && MI % 4 == 0, "a wavefront loads blocks of one side, scales come for four blocks");
-  constexpr int AB = 2 * MI, BB = 2 * NI;           // 16-row blocks of the tile
-  constexpr int LOADS = (AB + BB) / 4;              // of which a wavefront loads these a step
+  static_assert(MI % 4 == 0, "scales come for four blocks");
+  constexpr int NI = MI, AB = 2 * MI;               // 16-row blocks of a side of the tile
+  constexpr int LOADS = AB / 2;                     // of which a wavefront loads these a step
   constexpr int CHUNKS = LOADS / 4;                 // and for four of them at a time the scales of four steps
-  __shared__ uint4 st0[(AB + BB) * 64], st1[(AB + BB) * 64], st2[(AB + BB) * 64], st3[(AB + BB) * 64];
-  __shared__ unsigned sc[(AB + BB) * 64];      // [16-row block][lane]: the scales of four steps
-  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), lrow = lane & 15, lblk = lane >> 4;
+  __shared__ uint4 st0[2 * AB * 64], st1[2 * AB * 64], st2[2 * AB * 64], st3[2 * AB * 64];
+  __shared__ unsigned sc[2 * AB * 64];              // [16-row block][lane]: the scales of four steps
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), lrow = lane & 15;
   const int wm = wave & 1, wn = wave >> 1;
   int tr, tc;
   tile_of(p, tr, tc);
-  const int o0 = tc * 16 * AB, r0 = tr * 16 * BB;
+  const int o0 = tc * 16 * AB, r0 = tr * 16 * AB;
   const int steps = (p.blocks + 3) / 4, fours = (steps + 3) / 4;
 
-  // Wavefronts 0 and 1 load the weights, 2 and 3 the rows.  What lies past the last output, row or step reads the last one again: results of such rows
-  // are not stored, and terms past the last block are zeros on the rows' side.
-  const unsigned char* const from = wave < 2 ? p.a : p.bo;
-  const unsigned pitch = wave < 2 ? 64u : 1024u;      // from step to step
-  unsigned off[LOADS], less = 0;
-  if (wave < 2) {
-#pragma unroll
-    for (int q = 0; q < LOADS; ++q) {
-      const int b = wave * LOADS + q;
-      off[q] = ((unsigned)min(o0 + b / MI * 16 * MI + spread_row<MI>(b % MI, lrow), p.c_out - 1) * p.blocks + lblk) * 16u;
-    }
-    less = 16u * max(0, (steps - 1) * 4 + lblk - (p.blocks - 1));
-  } else {
-#pragma unroll
-    for (int q = 0; q < LOADS; ++q)
-      off[q] = (unsigned)min((r0 >> 4) + (wave - 2) * LOADS + q, (p.rows - 1) >> 4) * fours * 4096u + lane * 16u;
-  }
-  const int last = wave < 2 ? steps - 1 : 4 * fours - 1;
+  // Wavefronts 0 and 1 load the weights, 2 and 3 the rows.  Steps past the last one read that one again.
+  const int half = wave & 1;
+  const uint4* const from = (wave < 2 ? p.ao + (size_t)tc * fours * 4 * AB * 64 : p.bo + (size_t)tr * fours * 4 * AB * 64) + half * LOADS * 64;
+  const unsigned* const scales_from = (wave < 2 ? p.aso + (size_t)tc * fours * AB * 64 : p.bso + (size_t)tr * fours * AB * 64) + half * LOADS * 64;
   auto fetch = [&](uint4* stage, int s) __attribute__((always_inline)) {
-    const unsigned char* const at = from + (size_t)min(s, last) * pitch;
-    const unsigned back = s >= last ? less : 0u;
+    const uint4* const at = from + (size_t)min(s, 4 * fours - 1) * (AB * 64);
 #pragma unroll
     for (int q = 0; q < LOADS; ++q)
-      __builtin_amdgcn_global_load_lds((global_void*)(at + (off[q] - back)), (lds_void*)(stage + (wave * LOADS + q) * 64), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((global_void*)(at + q * 64 + lane), (lds_void*)(stage + (wave * LOADS + q) * 64), 16, 0, 0);
   };
-  const unsigned* const scales_from = wave < 2 ? p.aso : p.bso;
-  unsigned scales_off[CHUNKS];
-#pragma unroll
-  for (int q = 0; q < CHUNKS; ++q)
-    scales_off[q] = (unsigned)(wave < 2 ? (o0 >> 6) + wave * CHUNKS + q : min((r0 >> 6) + (wave - 2) * CHUNKS + q, (p.rows - 1) >> 6)) * fours * 256u + lane * 4u;
   auto fetch_scales = [&](int four) __attribute__((always_inline)) {
-    const unsigned* const at = scales_from + (size_t)min(four, fours - 1) * 256;
+    const unsigned* const at = scales_from + (size_t)min(four, fours - 1) * (AB * 64);
 #pragma unroll
     for (int q = 0; q < CHUNKS; ++q)
-      __builtin_amdgcn_global_load_lds((global_void*)(at + scales_off[q]), (lds_void*)(sc + (wave * CHUNKS + q) * 256), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((global_void*)(at + q * 256 + lane * 4), (lds_void*)(sc + (wave * CHUNKS + q) * 256), 16, 0, 0);
   };
 
   constexpr int M = MI / 2, N = NI / 2;      // 32 x 32 results of a wavefront
