@@ -489,34 +489,61 @@ __global__ __launch_bounds__(256) void mx4_tile_kernel(const Mx4Args p) {
     if (s + 4 >= steps) break;
   }
 
-  // 8 MI neighbouring outputs of a row
-  const int o = o0 + wm * 16 * MI + 8 * MI * (lane >> 5);
+  // A lane has 8 MI neighbouring outputs of a row.  They go through LDS, each wavefront's own stage, so that a store covers whole runs of a row: straight
+  // from the registers every lane would write 8 bytes of another row.  16-byte pieces are moved by their row (exclusive or): neither side meets in a bank.
+  if constexpr (MI == 8) {
 #pragma unroll
-  for (int j = 0; j < N; ++j) {
-    const int r = r0 + (wn * N + j) * 32 + (lane & 31);
-    if (r >= p.rows) continue;
-    T* y = static_cast<T*>(p.y) + (long)r * p.c_out + o;
+    for (int i = 0; i < M; ++i)
+#pragma unroll
+      for (int j = 0; j < N; ++j) asm volatile("" : "+a"(acc[i][j]));      // (the sums leave the loop where they were in it)
+  }
+  wait_and_meet<0>();
+  constexpr int W = 16 / (int)sizeof(T);                    // numbers of a piece
+  constexpr int PIECES = 16 * MI / W;                       // of a row of the wavefront's outputs
+  constexpr int J = N * 32 * PIECES > 2 * AB * 64 ? N / 2 : N;      // 32-row blocks that fit a stage
+  uint4* const mine = wave == 0 ? st0 : wave == 1 ? st1 : wave == 2 ? st2 : st3;
+  int l = threadIdx.x & 63;
+  asm volatile("" : "+v"(l));      // (what follows from it is worked out here and not held through the loop, where there is no register for it)
+  const int o = o0 + wm * 16 * MI, row = l & 31, first = (l >> 5) * (8 * MI / W);
+  typedef T outs __attribute__((ext_vector_type(W), aligned(sizeof(T))));
+#pragma unroll
+  for (int j0 = 0; j0 < N; j0 += J) {
 #pragma unroll
     for (int i = 0; i < M; ++i) {
+      float4_t bias[4];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int at = 16 * i + 4 * q;
-        const float4_t bias = load_bias4(p.bias, p.c_out, o + at);
-        typedef T out4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
-        out4 z;
+      for (int q = 0; q < 4; ++q) bias[q] = load_bias4(p.bias, p.c_out, o + 8 * MI * (l >> 5) + 16 * i + 4 * q);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) z[e] = Elem<T>::from_f32(finish<SILU>(acc[i][j][4 * q + e] + bias[e], p.lo, p.hi));
-        if (o + at + 4 <= p.c_out) {
-          *reinterpret_cast<out4*>(y + at) = z;
-        } else {
+      for (int j = j0; j < j0 + J; ++j)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (o + at + e < p.c_out) y[at + e] = z[e];
+        for (int h = 0; h < 16; h += W) {
+          outs z;
+#pragma unroll
+          for (int e = 0; e < W; ++e) z[e] = Elem<T>::from_f32(finish<SILU>(acc[i][j][h + e] + bias[(h + e) / 4][(h + e) & 3], p.lo, p.hi));
+          const int piece = first + (16 * i + h) / W;
+          mine[((j - j0) * 32 + row) * PIECES + (piece ^ (row & (PIECES - 1)))] = __builtin_bit_cast(uint4, z);
+          __builtin_amdgcn_sched_barrier(0);      // (one piece after another: all sums at once are more than the registers)
         }
+    }
+    __builtin_amdgcn_wave_barrier();
+    constexpr int AT_ONCE = 64 / PIECES;                    // rows of a store
+#pragma unroll 4
+    for (int it = 0; it < J * 32 / AT_ONCE; ++it) {
+      const int at = it * AT_ONCE + l / PIECES, piece = l % PIECES;
+      const outs z = __builtin_bit_cast(outs, mine[at * PIECES + (piece ^ (at & 31 & (PIECES - 1)))]);
+      const int r = r0 + (wn * N + j0) * 32 + at, col = o + piece * W;
+      if (r >= p.rows) continue;
+      T* y = static_cast<T*>(p.y) + (long)r * p.c_out + col;
+      if (col + W <= p.c_out) {
+        *reinterpret_cast<outs*>(y) = z;
+      } else {
+#pragma unroll
+        for (int e = 0; e < W; ++e)
+          if (col + e < p.c_out) y[e] = z[e];
       }
     }
+    __builtin_amdgcn_wave_barrier();
   }
-  __builtin_amdgcn_s_waitcnt(7 << 4);      // (no load into LDS outlives its work-group)
 }
 
 }  // namespace cprune
