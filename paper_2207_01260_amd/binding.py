@@ -476,10 +476,11 @@ def cprune_fc(x, w, bias=None, act=ACT_NONE, stream=None):
 
 
 # ---- group norm, channels last ---------------------------------------------------
+# (These calls take a few microseconds on the device; what the caller's thread does before the launch, 10 us when written plainly, is their time.
+# So checks are made without building their messages, and tensors without torch's Python-side conveniences where it has quicker ones.)
 
-def _expect(ok: bool, what: str) -> None:
-    if not ok:
-        raise ValueError(what)
+def _refuse(what: str) -> None:
+    raise ValueError(what)
 
 
 def _rows_of(x: torch.Tensor, image_dims: int):
@@ -491,45 +492,53 @@ def _rows_of(x: torch.Tensor, image_dims: int):
     pixels = math.prod(shape[image_dims:-1])
     if x.is_contiguous():
         return lead, pixels, c, c
-    _expect(c == 1 or x.stride(-1) == 1, "channels must lie next to each other")
+    if c != 1 and x.stride(-1) != 1:
+        _refuse("channels must lie next to each other")
     pitch, span = None, 1
     for size, stride in zip(reversed(shape[:-1]), reversed(x.stride()[:-1])):
         if size != 1:
             if pitch is None:
                 pitch, rest = divmod(stride, span)
-                _expect(rest == 0, "pixels must lie evenly")
-            _expect(stride == pitch * span, "pixels must lie evenly")
+                if rest:
+                    _refuse("pixels must lie evenly")
+            if stride != pitch * span:
+                _refuse("pixels must lie evenly")
         span *= size
-    pitch = c if pitch is None else pitch
-    _expect(pitch >= c, "pixels must not overlap")
+    if pitch is None:
+        pitch = c
+    if pitch < c:
+        _refuse("pixels must not overlap")
     return lead, pixels, c, pitch
 
 
-def _on_gpu(x: torch.Tensor, dtype=None, shape=None) -> int:
+def _on_gpu(x: torch.Tensor, dtype, shape) -> int:
     """Address of a dense device tensor of a type and shape."""
-    _expect(x.is_cuda and x.is_contiguous(), "device-resident contiguous tensors only")
-    _expect(dtype is None or x.dtype == dtype, f"expected {dtype}, got {x.dtype}")
-    _expect(shape is None or tuple(x.shape) == shape, f"expected shape {shape}, got {tuple(x.shape)}")
+    if not x.is_cuda or not x.is_contiguous():
+        _refuse("device-resident contiguous tensors only")
+    if x.dtype != dtype or x.shape != shape:
+        _refuse(f"expected {dtype} {tuple(shape)}, got {x.dtype} {tuple(x.shape)}")
     return x.data_ptr()
-
-
-def _vector(x: Optional[torch.Tensor], c: int):
-    return None if x is None else _on_gpu(x, torch.float32, (c,))
 
 
 def _used_on(stream, *tensors) -> None:
     """Memory taken from torch's current stream is not handed out again before work on `stream` is done with it."""
-    if stream is not None:
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
 
 
 def _norm_desc(x: torch.Tensor, groups: int, act: int, eps: float):
-    _expect(x.is_cuda and x.dim() >= 2, "a channels-last device tensor [n, ..., c]")
-    _expect(x.dtype in DTYPE_OF_TORCH, f"no {x.dtype}")
+    if not x.is_cuda or x.dim() < 2:
+        _refuse("a channels-last device tensor [n, ..., c]")
+    dtype = DTYPE_OF_TORCH.get(x.dtype)
+    if dtype is None:
+        _refuse(f"no {x.dtype}")
     n, pixels, c, pitch = _rows_of(x, 1)
-    return NormDesc(n, pixels, c, groups, DTYPE_OF_TORCH[x.dtype], act, pitch, c, eps)
+    return NormDesc(n, pixels, c, groups, dtype, act, pitch, c, eps)
+
+
+def _dense_like(x: torch.Tensor) -> torch.Tensor:
+    return torch.empty_like(x) if x.is_contiguous() else x.new_empty(x.shape)
 
 
 def cprune_group_norm_act(x: torch.Tensor, groups: int, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None,
@@ -538,15 +547,24 @@ def cprune_group_norm_act(x: torch.Tensor, groups: int, weight: Optional[torch.T
     -> y dense, or (y, mean [n, groups], rstd [n, groups]) for the backward call."""
     L = _lib or lib()
     d = _norm_desc(x, groups, act, eps)
-    y = x.new_empty(x.shape)
-    mean = rstd = None
+    vec = (d.c,)
+    y = _dense_like(x)
+    mean = rstd = ws = None
+    mean_at = rstd_at = ws_at = None
     if want_stats:
         mean, rstd = x.new_empty((2, d.n, max(groups, 0)), dtype=torch.float32).unbind()
-    ws = _ws(L.cprune_group_norm_workspace_bytes(d, 0), x.device)
-    st = L.cprune_group_norm_act(d, x.data_ptr(), _vector(weight, d.c), _vector(bias, d.c), y.data_ptr(), _addr(mean), _addr(rstd),
-                                 _addr(ws), _size(ws), _raw_stream(stream))
-    _check(st, "cprune_group_norm_act")
-    _used_on(stream, y, mean, rstd, ws)
+        mean_at, rstd_at = mean.data_ptr(), rstd.data_ptr()
+    need = L.cprune_group_norm_workspace_bytes(d, 0)
+    if need:
+        ws = torch.empty(need, dtype=torch.uint8, device=x.device)
+        ws_at = ws.data_ptr()
+    st = L.cprune_group_norm_act(d, x.data_ptr(), None if weight is None else _on_gpu(weight, torch.float32, vec),
+                                 None if bias is None else _on_gpu(bias, torch.float32, vec), y.data_ptr(), mean_at, rstd_at, ws_at, need,
+                                 _raw_stream(stream))
+    if st:
+        _check(st, "cprune_group_norm_act")
+    if stream is not None:
+        _used_on(stream, y, mean, rstd, ws)
     return (y, mean, rstd) if want_stats else y
 
 
@@ -556,59 +574,78 @@ def cprune_group_norm_act_backward(dy: torch.Tensor, x: torch.Tensor, mean: torc
     """The gradient of cprune_group_norm_act at x: -> (dx dense, dweight fp32 [c], dbias fp32 [c]); the latter None without want_vectors."""
     L = _lib or lib()
     d = _norm_desc(x, groups, act, 0.0)
-    _expect(dy.is_cuda and dy.shape == x.shape and dy.dtype == x.dtype, "dy must be like x")
-    d.dy_stride = _rows_of(dy, 1)[3]
-    stats = (d.n, groups)
-    dx = x.new_empty(x.shape)
-    dweight = dbias = None
+    if not dy.is_cuda or dy.shape != x.shape or dy.dtype != x.dtype:
+        _refuse("dy must be like x")
+    if not dy.is_contiguous():
+        d.dy_stride = _rows_of(dy, 1)[3]
+    stats, vec = (d.n, groups), (d.c,)
+    dx = _dense_like(x)
+    dweight = dbias = ws = None
+    dweight_at = dbias_at = ws_at = None
     if want_vectors:
         dweight, dbias = x.new_empty((2, d.c), dtype=torch.float32).unbind()
-    ws = _ws(L.cprune_group_norm_workspace_bytes(d, 1), x.device)
-    st = L.cprune_group_norm_act_backward(d, dy.data_ptr(), x.data_ptr(), _on_gpu(mean, torch.float32, stats),
-                                          _on_gpu(rstd, torch.float32, stats), _vector(weight, d.c), _vector(bias, d.c), dx.data_ptr(),
-                                          _addr(dweight), _addr(dbias), _addr(ws), _size(ws), _raw_stream(stream))
-    _check(st, "cprune_group_norm_act_backward")
-    _used_on(stream, dx, dweight, dbias, ws)
+        dweight_at, dbias_at = dweight.data_ptr(), dbias.data_ptr()
+    need = L.cprune_group_norm_workspace_bytes(d, 1)
+    if need:
+        ws = torch.empty(need, dtype=torch.uint8, device=x.device)
+        ws_at = ws.data_ptr()
+    st = L.cprune_group_norm_act_backward(d, dy.data_ptr(), x.data_ptr(), _on_gpu(mean, torch.float32, stats), _on_gpu(rstd, torch.float32, stats),
+                                          None if weight is None else _on_gpu(weight, torch.float32, vec),
+                                          None if bias is None else _on_gpu(bias, torch.float32, vec), dx.data_ptr(), dweight_at, dbias_at, ws_at,
+                                          need, _raw_stream(stream))
+    if st:
+        _check(st, "cprune_group_norm_act_backward")
+    if stream is not None:
+        _used_on(stream, dx, dweight, dbias, ws)
     return dx, dweight, dbias
 
 
 # ---- microscaled 4-bit numbers ---------------------------------------------------
 
 def _mx4_rows(x: torch.Tensor):
-    _expect(x.is_cuda and x.dim() >= 1, "a device tensor [..., k]")
-    _expect(x.dtype in DTYPE_OF_TORCH, f"no {x.dtype}")
+    if not x.is_cuda or x.dim() < 1:
+        _refuse("a device tensor [..., k]")
+    dtype = DTYPE_OF_TORCH.get(x.dtype)
+    if dtype is None:
+        _refuse(f"no {x.dtype}")
     _, rows, k, pitch = _rows_of(x, 0)
-    return rows, k, pitch, DTYPE_OF_TORCH[x.dtype]
+    return rows, k, pitch, dtype
 
 
 def _mx4_pair(codes: torch.Tensor, scales: torch.Tensor, k: Optional[int]):
     """Addresses of codes and scales, and their rows and blocks."""
-    _expect(codes.dim() == 2 and scales.dim() == 2, "codes [rows, blocks * 16], scales [rows, blocks]")
-    rows, blocks = scales.shape
-    if k is not None:
-        _expect(blocks == (k + 31) // 32, f"{blocks} blocks do not hold {k} numbers a row")
-    return _on_gpu(codes, torch.uint8, (rows, 16 * blocks)), _on_gpu(scales, torch.uint8), rows, blocks
+    if scales.dim() != 2:
+        _refuse("codes [rows, blocks * 16], scales [rows, blocks]")
+    rows, blocks = shape = scales.shape
+    if k is not None and blocks != (k + 31) // 32:
+        _refuse(f"{blocks} blocks do not hold {k} numbers a row")
+    return _on_gpu(codes, torch.uint8, (rows, 16 * blocks)), _on_gpu(scales, torch.uint8, shape), rows, blocks
 
 
 def cprune_mx4_quantize(x: torch.Tensor, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """x [..., k] -> (codes uint8 [rows, ceil(k / 32) * 16], scales uint8 [rows, ceil(k / 32)])."""
     rows, k, pitch, dtype = _mx4_rows(x)
     blocks = (k + 31) // 32
-    codes = x.new_empty((rows, 16 * blocks), dtype=torch.uint8)
-    scales = x.new_empty((rows, blocks), dtype=torch.uint8)
+    dev = x.device
+    codes = torch.empty(rows, 16 * blocks, dtype=torch.uint8, device=dev)
+    scales = torch.empty(rows, blocks, dtype=torch.uint8, device=dev)
     st = (_lib or lib()).cprune_mx4_quantize(x.data_ptr(), rows, k, pitch, dtype, codes.data_ptr(), scales.data_ptr(), _raw_stream(stream))
-    _check(st, "cprune_mx4_quantize")
-    _used_on(stream, codes, scales)
+    if st:
+        _check(st, "cprune_mx4_quantize")
+    if stream is not None:
+        _used_on(stream, codes, scales)
     return codes, scales
 
 
 def cprune_mx4_dequantize(codes: torch.Tensor, scales: torch.Tensor, k: int, dtype: int = F32, stream=None) -> torch.Tensor:
     """-> [rows, k], the numbers that the codes stand for."""
     ca, sa, rows, _ = _mx4_pair(codes, scales, k)
-    y = codes.new_empty((rows, k), dtype=TORCH_DTYPE[dtype])
+    y = torch.empty(rows, k, dtype=TORCH_DTYPE[dtype], device=codes.device)
     st = (_lib or lib()).cprune_mx4_dequantize(ca, sa, rows, k, dtype, y.data_ptr(), _raw_stream(stream))
-    _check(st, "cprune_mx4_dequantize")
-    _used_on(stream, y)
+    if st:
+        _check(st, "cprune_mx4_dequantize")
+    if stream is not None:
+        _used_on(stream, y)
     return y
 
 
@@ -618,12 +655,18 @@ def cprune_mx4_matmul(x_codes: torch.Tensor, x_scales: torch.Tensor, w_codes: to
     L = _lib or lib()
     xa, xs, rows, blocks = _mx4_pair(x_codes, x_scales, None)
     wa, wsc, c_out, _ = _mx4_pair(w_codes, w_scales, 32 * blocks)
-    y = x_codes.new_empty((rows, c_out), dtype=TORCH_DTYPE[dtype])
-    ws = _ws(L.cprune_mx4_matmul_workspace_bytes(rows, 32 * blocks, c_out), y.device)
-    st = L.cprune_mx4_matmul(xa, xs, rows, 32 * blocks, wa, wsc, c_out, _vector(bias, c_out), act, dtype, y.data_ptr(), _addr(ws), _size(ws),
-                             _raw_stream(stream))
-    _check(st, "cprune_mx4_matmul")
-    _used_on(stream, y, ws)
+    y = torch.empty(rows, c_out, dtype=TORCH_DTYPE[dtype], device=x_codes.device)
+    ws = ws_at = None
+    need = L.cprune_mx4_matmul_workspace_bytes(rows, 32 * blocks, c_out)
+    if need:
+        ws = x_codes.new_empty(need)
+        ws_at = ws.data_ptr()
+    st = L.cprune_mx4_matmul(xa, xs, rows, 32 * blocks, wa, wsc, c_out, None if bias is None else _on_gpu(bias, torch.float32, (c_out,)), act,
+                             dtype, y.data_ptr(), ws_at, need, _raw_stream(stream))
+    if st:
+        _check(st, "cprune_mx4_matmul")
+    if stream is not None:
+        _used_on(stream, y, ws)
     return y
 
 
@@ -633,12 +676,18 @@ def cprune_mx4_linear(x: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Te
     L = _lib or lib()
     rows, k, pitch, dtype = _mx4_rows(x)
     wa, wsc, c_out, _ = _mx4_pair(w_codes, w_scales, k)
-    y = x.new_empty(x.shape[:-1] + (c_out,))
-    ws = _ws(L.cprune_mx4_linear_workspace_bytes(rows, k, c_out, dtype), x.device)
-    st = L.cprune_mx4_linear(x.data_ptr(), rows, k, pitch, wa, wsc, c_out, _vector(bias, c_out), act, dtype, y.data_ptr(), _addr(ws),
-                             _size(ws), _raw_stream(stream))
-    _check(st, "cprune_mx4_linear")
-    _used_on(stream, y, ws)
+    y = torch.empty(x.shape[:-1] + (c_out,), dtype=x.dtype, device=x.device)
+    ws = ws_at = None
+    need = L.cprune_mx4_linear_workspace_bytes(rows, k, c_out, dtype)
+    if need:
+        ws = torch.empty(need, dtype=torch.uint8, device=x.device)
+        ws_at = ws.data_ptr()
+    st = L.cprune_mx4_linear(x.data_ptr(), rows, k, pitch, wa, wsc, c_out, None if bias is None else _on_gpu(bias, torch.float32, (c_out,)), act,
+                             dtype, y.data_ptr(), ws_at, need, _raw_stream(stream))
+    if st:
+        _check(st, "cprune_mx4_linear")
+    if stream is not None:
+        _used_on(stream, y, ws)
     return y
 
 

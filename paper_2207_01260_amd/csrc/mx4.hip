@@ -1,4 +1,5 @@
 // Entry points of the microscaled 4-bit numbers; quantisation and the way back (mx4_kernel.hpp has the products).
+#include <algorithm>
 #include <limits>
 
 #include "mx4_kernel.hpp"
@@ -153,7 +154,9 @@ struct ProductPlan {
 ProductPlan plan_product(int rows, int k, int c_out, bool numbers) {
   const long blocks = blocks_of(k), steps = (blocks + 3) / 4, fours = (steps + 3) / 4;
   ProductPlan q = {};
-  if (rows > 32 && steps <= 8 && (double)c_out * k <= 262144.0) {
+  // Short sums: every 16 rows read all weights from the caches, so few weights or little work in all (12544 x 96 x 576 9.2 us, by tiles 14.0; 784 x 160 x 960
+  // 4.0 and 9.0; but 3136 x 1024 x 256 14.4 and 11.2, 50176 x 256 x 1024 135 and 64).
+  if (rows > 32 && steps <= 8 && ((double)c_out * k <= 65536.0 || (double)rows * c_out * k <= 268435456.0)) {
     q.form = kShort;
   } else if (rows >= 512 && (double)(rows + 255) * fours * 512 < 2147483648.0 && (double)(c_out + 255) * fours * 512 < 2147483648.0) {
     q.form = kTiles;
@@ -195,14 +198,17 @@ template <typename X, typename T, bool SILU> void launch_few(Mx4Args p, hipStrea
 }
 template <typename X, typename T, bool SILU> void launch_short(const Mx4Args& p, hipStream_t s) {
   const int steps = (p.blocks + 3) / 4;
-  const dim3 grid((unsigned)((p.rows + 63) / 64), 1);
+  const unsigned row_groups = (unsigned)((p.rows + 63) / 64), tiles = (unsigned)((p.c_out + (p.c_out > 32 ? 63 : 31)) / (p.c_out > 32 ? 64 : 32));
+  // (outputs are shared out where there are few rows: 12544 x 96 x 576 12.1 -> 9.2 us, 784 x 160 x 960 18.5 -> 4.0)
+  const dim3 grid(row_groups, std::min(tiles, std::max(1u, 1024u / row_groups)));
   auto go = [&](auto n) {
     if (p.c_out > 32) mx4_rows_kernel<X, T, SILU, 4, 1, decltype(n)::value><<<grid, 256, 0, s>>>(p);
     else mx4_rows_kernel<X, T, SILU, 2, 1, decltype(n)::value><<<grid, 256, 0, s>>>(p);
   };
   if (steps <= 1) go(std::integral_constant<int, 1>());
   else if (steps <= 2) go(std::integral_constant<int, 2>());
-  else if (steps <= 4) go(std::integral_constant<int, 4>());
+  else if (steps <= 3) go(std::integral_constant<int, 3>());
+  else if (steps <= 5) go(std::integral_constant<int, 5>());
   else go(std::integral_constant<int, 8>());
 }
 template <typename T, bool SILU> void launch_tiles(Mx4Args p, int mi, hipStream_t s) {
