@@ -8,4 +8,4 @@ workload generators (``synth``).  Importing the package loads nothing native:
 not been built.
 """
 
-__all__ = ["binding", "pipeline", "synth"]
+__all__ = ["binding", "pipeline", "pointwise", "synth"]
