@@ -52,7 +52,7 @@ template <typename T> __global__ __launch_bounds__(256) void mx4_arrange_kernel(
   const int b = group / (unsigned)fours, four = (int)group - b * fours;      // 16-row block, four steps
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, lrow = lane >> 2, quarter = lane & 3;
   int row = b * 16 + lrow;
-  if (weights) row = b / p.mi * 16 * p.mi + (p.mi == 8 ? mx4::spread_row<8>(b % 8, lrow) : mx4::spread_row<4>(b % 4, lrow));
+  if (weights) row = b / p.mi * 16 * p.mi + (p.mi == 8 ? mx4::spread_row<8>(b % 8, lrow) : p.mi == 4 ? mx4::spread_row<4>(b % 4, lrow) : mx4::spread_row<2>(b % 2, lrow));
   const bool from_codes = weights || std::is_same<T, void>::value;
   const unsigned* const codes_in = static_cast<const unsigned*>(weights ? static_cast<const void*>(p.w) : p.x);
   const unsigned char* const scales_in = weights ? p.ws : p.xs;
@@ -141,6 +141,8 @@ void launch_quantize(const void* x, int rows, int k, int x_stride, int dtype, vo
   });
 }
 
+constexpr int kShortSteps = 5;      // steps of 128 terms that the rows kernel is built for
+
 // How a product runs, and its scratch.
 enum ProductForm { kFew, kShort, kTiles };
 struct ProductPlan {
@@ -154,13 +156,19 @@ struct ProductPlan {
 ProductPlan plan_product(int rows, int k, int c_out, bool numbers) {
   const long blocks = blocks_of(k), steps = (blocks + 3) / 4, fours = (steps + 3) / 4;
   ProductPlan q = {};
-  // Short sums: every 16 rows read all weights from the caches, so few weights or little work in all (12544 x 96 x 576 9.2 us, by tiles 14.0; 784 x 160 x 960
-  // 4.0 and 9.0; but 3136 x 1024 x 256 14.4 and 11.2, 50176 x 256 x 1024 135 and 64).
-  if (rows > 32 && steps <= 8 && ((double)c_out * k <= 65536.0 || (double)rows * c_out * k <= 268435456.0)) {
+  // Measured on bf16 numbers, us (short / few / tiles): 12544 x 200 x 64 4.7 / 8.0 / 8.8; 784 x 160 x 960 4.0 / - / 9.0; 3136 x 576 x 96 6.9 / 7.4 / 8.0; but six to
+  // eight steps 500 x 1000 x 100 12.6 / 9.0 / 7.8, and many weights read by every 16 rows 50176 x 256 x 1024 135 / - / 64.
+  const bool is_short = steps <= kShortSteps && ((double)c_out * k <= 65536.0 || (double)rows * c_out * k <= 268435456.0);
+  // The tiles' launch that lays both sides out reads and writes all weights: 40 x 2048 x 8192 9.6 (few) / 13.7 (tiles), 64 x 4096 x 4096 16.6 / 16.8,
+  // 256 x 4096 x 4096 27.5 / 17.4, 64 x 1024 x 256 8.7 / 6.9.
+  const bool enough = rows > 64 || (rows > 32 && (double)c_out * k <= 1048576.0);
+  if (rows > 32 && is_short) {
     q.form = kShort;
-  } else if (rows >= 512 && (double)(rows + 255) * fours * 512 < 2147483648.0 && (double)(c_out + 255) * fours * 512 < 2147483648.0) {
+  } else if (enough && (double)(rows + 255) * fours * 512 < 2147483648.0 && (double)(c_out + 255) * fours * 512 < 2147483648.0) {
     q.form = kTiles;
-    q.mi = (double)rows * c_out >= 256.0 * 256 * 128 ? 8 : 4;
+    // the widest tiles that still give half of the compute units one: 1024 x 8192 x 1024 20.9 by 64, 26.9 by 128; 2048 x 2048 x 2048 18.3 by 128, 26.6 by 256
+    auto tiles_of = [&](long side) { return ((rows + side - 1) / side) * ((c_out + side - 1) / side); };
+    q.mi = tiles_of(256) >= 128 ? 8 : tiles_of(128) >= 128 ? 4 : 2;
     const long side = 32L * q.mi, row_tiles = (rows + side - 1) / side, tiles = (c_out + side - 1) / side, run = 2L * q.mi * fours;
     q.codes = (size_t)(row_tiles * run * 4096), q.x_scales = (size_t)(row_tiles * run * 256);
     q.w_codes = (size_t)(tiles * run * 4096), q.w_scales = (size_t)(tiles * run * 256);
@@ -208,15 +216,15 @@ template <typename X, typename T, bool SILU> void launch_short(const Mx4Args& p,
   if (steps <= 1) go(std::integral_constant<int, 1>());
   else if (steps <= 2) go(std::integral_constant<int, 2>());
   else if (steps <= 3) go(std::integral_constant<int, 3>());
-  else if (steps <= 5) go(std::integral_constant<int, 5>());
-  else go(std::integral_constant<int, 8>());
+  else go(std::integral_constant<int, kShortSteps>());
 }
 template <typename T, bool SILU> void launch_tiles(Mx4Args p, int mi, hipStream_t s) {
   p.tiles = (p.c_out + 32 * mi - 1) / (32 * mi);
   p.row_tiles = (p.rows + 32 * mi - 1) / (32 * mi);
   const unsigned grid = (unsigned)((long)p.tiles * p.row_tiles);
   if (mi == 8) mx4_tile_kernel<T, SILU, 8><<<grid, 256, 0, s>>>(p);
-  else mx4_tile_kernel<T, SILU, 4><<<grid, 256, 0, s>>>(p);
+  else if (mi == 4) mx4_tile_kernel<T, SILU, 4><<<grid, 256, 0, s>>>(p);
+  else mx4_tile_kernel<T, SILU, 2><<<grid, 256, 0, s>>>(p);
 }
 
 // x: numbers of `dtype`, or (x_scales given) codes

@@ -345,7 +345,8 @@ __global__ __launch_bounds__(256) void mx4_rows_kernel(const Mx4Args p) {
 // Four wavefronts (2 x 2) of MI x MI blocks each: 32 MI outputs of c_out by 32 MI rows a work-group, K in steps of 128 terms.  A stage is the tile's codes
 // of one step in operand order, [16-row block][lane][16 bytes], as a launch before has laid them out in memory: a step of a tile is one run of memory, so its
 // loads spread over all channels of the L2 (rows of 2^n bytes read side by side would meet in one), and they write to LDS themselves.
-// While step s is multiplied, the operands of s + 1 go to registers and the codes of s + 4 into the stage that s has left.
+// While step s is multiplied, the operands of s + 1 go to registers and the codes of s + STAGES into the stage that s has left: 4 stages where they fill
+// LDS (MI = 8), otherwise 8.
 // The matrix instruction takes 32 rows of each side; those of a wavefront's c_out are dealt so that a lane's results are 8 MI neighbours of one row of y.
 namespace mx4 {
 
@@ -384,12 +385,14 @@ __device__ __forceinline__ void tile_of(const Mx4Args& p, int& tr, int& tc) {
 template <typename T, bool SILU, int MI>
 __global__ __launch_bounds__(256) void mx4_tile_kernel(const Mx4Args p) {
   using namespace mx4;
-  static_assert(MI % 4 == 0, "scales come for four blocks");
   constexpr int NI = MI, AB = 2 * MI;               // 16-row blocks of a side of the tile
   constexpr int LOADS = AB / 2;                     // of which a wavefront loads these a step
-  constexpr int CHUNKS = LOADS / 4;                 // and for four of them at a time the scales of four steps
+  constexpr int CHUNKS = AB / 4;                    // of four blocks each, whose scales of four steps are one load
+  constexpr int STAGES = MI == 8 ? 4 : 8;
+  // (arrays of their own: an index into one would have every read wait for every load on its way)
   __shared__ uint4 st0[2 * AB * 64], st1[2 * AB * 64], st2[2 * AB * 64], st3[2 * AB * 64];
-  __shared__ unsigned sc[2 * AB * 64];              // [16-row block][lane]: the scales of four steps
+  __shared__ uint4 st4[STAGES > 4 ? 2 * AB * 64 : 1], st5[STAGES > 4 ? 2 * AB * 64 : 1], st6[STAGES > 4 ? 2 * AB * 64 : 1], st7[STAGES > 4 ? 2 * AB * 64 : 1];
+  __shared__ unsigned sc0[2 * AB * 64], sc1[STAGES > 4 ? 2 * AB * 64 : 1];      // [16-row block][lane]: the scales of four steps
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), lrow = lane & 15;
   const int wm = wave & 1, wn = wave >> 1;
   int tr, tc;
@@ -400,18 +403,22 @@ __global__ __launch_bounds__(256) void mx4_tile_kernel(const Mx4Args p) {
   // Wavefronts 0 and 1 load the weights, 2 and 3 the rows.  Steps past the last one read that one again.
   const int half = wave & 1;
   const uint4* const from = (wave < 2 ? p.ao + (size_t)tc * fours * 4 * AB * 64 : p.bo + (size_t)tr * fours * 4 * AB * 64) + half * LOADS * 64;
-  const unsigned* const scales_from = (wave < 2 ? p.aso + (size_t)tc * fours * AB * 64 : p.bso + (size_t)tr * fours * AB * 64) + half * LOADS * 64;
+  const unsigned* const scales_from = wave < 2 ? p.aso + (size_t)tc * fours * AB * 64 : p.bso + (size_t)tr * fours * AB * 64;
   auto fetch = [&](uint4* stage, int s) __attribute__((always_inline)) {
     const uint4* const at = from + (size_t)min(s, 4 * fours - 1) * (AB * 64);
 #pragma unroll
     for (int q = 0; q < LOADS; ++q)
       __builtin_amdgcn_global_load_lds((global_void*)(at + q * 64 + lane), (lds_void*)(stage + (wave * LOADS + q) * 64), 16, 0, 0);
   };
-  auto fetch_scales = [&](int four) __attribute__((always_inline)) {
+  auto fetch_scales = [&](unsigned* sc, int four) __attribute__((always_inline)) {
     const unsigned* const at = scales_from + (size_t)min(four, fours - 1) * (AB * 64);
+    constexpr int EACH = (CHUNKS + 1) / 2;
 #pragma unroll
-    for (int q = 0; q < CHUNKS; ++q)
-      __builtin_amdgcn_global_load_lds((global_void*)(at + q * 256 + lane * 4), (lds_void*)(sc + (wave * CHUNKS + q) * 256), 16, 0, 0);
+    for (int q = 0; q < EACH; ++q) {
+      const int c = half * EACH + q;
+      if (c < CHUNKS)
+        __builtin_amdgcn_global_load_lds((global_void*)(at + c * 256 + lane * 4), (lds_void*)(sc + ((wave >> 1) * CHUNKS + c) * 256), 16, 0, 0);
+    }
   };
 
   constexpr int M = MI / 2, N = NI / 2;      // 32 x 32 results of a wavefront
@@ -435,7 +442,7 @@ __global__ __launch_bounds__(256) void mx4_tile_kernel(const Mx4Args p) {
       for (int j = 0; j < N; ++j) b[h][j] = stage[(AB + wn * NI + 2 * j) * 64 + h * 32 + at0];
     }
   };
-  auto scales = [&]() __attribute__((always_inline)) {
+  auto scales = [&](const unsigned* sc) __attribute__((always_inline)) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
 #pragma unroll
@@ -445,20 +452,28 @@ __global__ __launch_bounds__(256) void mx4_tile_kernel(const Mx4Args p) {
     }
   };
 
-  fetch_scales(0);
+  fetch_scales(sc0, 0);
+  if (STAGES > 4) fetch_scales(sc1, 1);
   fetch(st0, 0);
   fetch(st1, 1);
   fetch(st2, 2);
   fetch(st3, 3);
-  wait_and_meet<3 * LOADS>();
+  if constexpr (STAGES > 4) {
+    fetch(st4, 4);
+    fetch(st5, 5);
+    fetch(st6, 6);
+    fetch(st7, 7);
+  }
+  wait_and_meet<(STAGES - 1) * LOADS>();
   operands(st0, fa[0], fb[0]);
-  scales();
-  // Step s = 4 n + B: its operands are in fa[B & 1], fb[B & 1].
-  auto step = [&](auto byte, int s, uint4* own, uint4* next) __attribute__((always_inline)) {
+  scales(sc0);
+  // Step s: its operands are in fa[B & 1], fb[B & 1], its scales byte B of sa and sb.  sc_own: the scales of this step's four, whose place is free while they
+  // are multiplied; sc_next: those of the next.
+  auto step = [&](auto byte, int s, uint4* own, uint4* next, unsigned* sc_own, unsigned* sc_next) __attribute__((always_inline)) {
     constexpr int B = decltype(byte)::value;
-    wait_and_meet<2 * LOADS>();      // the codes of s + 1 are there (s + 2 and s + 3 may be under way), and nobody reads `own` any more
-    if (B == 0) fetch_scales(s / 4 + 1);      // (ahead of the codes of s + 4: there when those are)
-    fetch(own, s + 4);
+    wait_and_meet<(STAGES - 2) * LOADS>();      // the codes of s + 1 are there (later ones may be under way), and nobody reads `own` any more
+    if (B == 0) fetch_scales(sc_own, s / 4 + STAGES / 4);      // (ahead of the codes of s + STAGES: there when those are, a step before they are read)
+    fetch(own, s + STAGES);
     operands(next, fa[(B + 1) & 1], fb[(B + 1) & 1]);
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -466,27 +481,49 @@ __global__ __launch_bounds__(256) void mx4_tile_kernel(const Mx4Args p) {
       for (int j = 0; j < N; ++j)
 #pragma unroll
         for (int i = 0; i < M; ++i) acc[i][j] = mma32<B>(fa[B & 1][h][i], sa[h][i], fb[B & 1][h][j], sb[h][j], acc[i][j]);
-    // an LDS read, a load and two products in turn
+    // an LDS read, a load and some products in turn
 #pragma unroll
     for (int q = 0; q < 2 * (M + N); ++q) {
       __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       if (q < LOADS) __builtin_amdgcn_sched_group_barrier(0x20, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x8, 2 * M * N / (2 * (M + N)), 0);
+      __builtin_amdgcn_sched_group_barrier(0x8, M * N > M + N ? M * N / (M + N) : 1, 0);
     }
-    if (B == 3) scales();
+    if (B == 3) scales(sc_next);
     asm volatile("" ::: "memory");      // (the reads above belong to this turn of the loop)
   };
-  // (One way out of the loop where the sums fill half the registers: with an exit behind each step they are copied at every turn.  The steps that
-  // fill up the last four multiply the zeros of the rows' side.)
-  for (int s = 0;; s += 4) {
-    step(std::integral_constant<int, 0>(), s, st0, st1);
-    if (MI < 8 && s + 1 >= steps) break;
-    step(std::integral_constant<int, 1>(), s + 1, st1, st2);
-    if (MI < 8 && s + 2 >= steps) break;
-    step(std::integral_constant<int, 2>(), s + 2, st2, st3);
-    if (MI < 8 && s + 3 >= steps) break;
-    step(std::integral_constant<int, 3>(), s + 3, st3, st0);
-    if (s + 4 >= steps) break;
+  typedef std::integral_constant<int, 0> byte0;
+  typedef std::integral_constant<int, 1> byte1;
+  typedef std::integral_constant<int, 2> byte2;
+  typedef std::integral_constant<int, 3> byte3;
+  if constexpr (STAGES == 4) {
+    // (One way out of the loop where the sums fill half the registers: with an exit behind each step they are copied at every turn.  The steps that fill up
+    // the last four multiply zeros.)
+    for (int s = 0;; s += 4) {
+      step(byte0(), s, st0, st1, sc0, sc0);
+      step(byte1(), s + 1, st1, st2, sc0, sc0);
+      step(byte2(), s + 2, st2, st3, sc0, sc0);
+      step(byte3(), s + 3, st3, st0, sc0, sc0);
+      if (s + 4 >= steps) break;
+    }
+  } else {
+    for (int s = 0;; s += 8) {
+      step(byte0(), s, st0, st1, sc0, sc1);
+      if (s + 1 >= steps) break;
+      step(byte1(), s + 1, st1, st2, sc0, sc1);
+      if (s + 2 >= steps) break;
+      step(byte2(), s + 2, st2, st3, sc0, sc1);
+      if (s + 3 >= steps) break;
+      step(byte3(), s + 3, st3, st4, sc0, sc1);
+      if (s + 4 >= steps) break;
+      step(byte0(), s + 4, st4, st5, sc1, sc0);
+      if (s + 5 >= steps) break;
+      step(byte1(), s + 5, st5, st6, sc1, sc0);
+      if (s + 6 >= steps) break;
+      step(byte2(), s + 6, st6, st7, sc1, sc0);
+      if (s + 7 >= steps) break;
+      step(byte3(), s + 7, st7, st0, sc1, sc0);
+      if (s + 8 >= steps) break;
+    }
   }
 
   // A lane has 8 MI neighbouring outputs of a row.  They go through LDS, each wavefront's own stage, so that a store covers whole runs of a row: straight

@@ -127,7 +127,8 @@ def test_blocks_with_infinity_or_nan_and_the_ends_of_the_scales():
 
 def act64(z, act):
     if act == B.ACT_SILU:
-        return z / (1 + np.exp(-z))
+        with np.errstate(over="ignore"):
+            return z / (1 + np.exp(-z))
     return np.clip(z, -np.inf if act == B.ACT_NONE else 0, 6 if act == B.ACT_RELU6 else np.inf)
 
 
@@ -153,7 +154,8 @@ E24 = 2.0 ** -24
 # rows, k, c_out: one of each, tails of every tile, few rows of long sums, many rows of short ones, both large
 PRODUCTS = [(1, 1, 1), (1, 32, 16), (1, 4096, 1000), (3, 70, 5), (16, 128, 64), (17, 129, 65), (33, 31, 33), (32, 1280, 1000), (5, 8192, 48), (64, 640, 129),
             (100, 333, 77), (129, 1000, 257), (255, 96, 31), (512, 512, 512), (513, 544, 300), (1000, 36, 24), (2049, 160, 100), (4000, 100, 3), (300, 4100, 520),
-            (1024, 2048, 768), (8, 2000, 4100), (2, 20000, 40)]
+            (1024, 2048, 768), (8, 2000, 4100), (2, 20000, 40), (64, 700, 70), (70, 1300, 130), (90, 5000, 33),
+            (1100, 1100, 1300), (2100, 130, 2200), (3000, 4100, 3100), (40, 600, 1000), (1500, 640, 90), (33, 8, 4097)]
 
 
 @pytest.mark.parametrize("dtype", TYPES)
