@@ -60,23 +60,36 @@ template <typename T> __global__ __launch_bounds__(256) void mx4_arrange_kernel(
   const int tile = b / ab, in_tile = b - tile * ab;
   unsigned* const codes = (weights ? p.w_codes : p.x_codes) + ((long)(tile * fours + four) * 4 * ab + in_tile) * 256 + (wave * 16 + lrow) * 4 + quarter;
   unsigned scales = 0;
-#pragma unroll
-  for (int t = 0; t < 4; ++t) {
-    const int blk = (four * 4 + t) * 4 + wave;
-    unsigned c = 0;
-    int s = 0;
-    if (from_codes) {
-      if (row < rows && blk < p.blocks) {
-        const long at = (long)row * p.blocks + blk;
-        c = codes_in[at * 4 + quarter];
-        s = scales_in[at];
-      }
-    } else if constexpr (!std::is_same<T, void>::value) {
-      const int at = blk * 32 + quarter * 8;
-      c = quantize8(static_cast<const T*>(p.x) + min(row, p.rows - 1) * p.x_stride + at, row < p.rows ? p.k - at : 0, s);
-    }
+  auto keep = [&](int t, unsigned c, int s) __attribute__((always_inline)) {
     codes[(long)t * ab * 256] = c;
     scales |= (unsigned)s << (8 * t);
+  };
+  if (from_codes) {
+    unsigned c[4];
+    int s[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int blk = (four * 4 + t) * 4 + wave;
+      const bool in = row < rows && blk < p.blocks;
+      const long at = (long)row * p.blocks + blk;
+      c[t] = in ? codes_in[at * 4 + quarter] : 0u;
+      s[t] = in ? scales_in[at] : 0;
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) keep(t, c[t], s[t]);
+  } else if constexpr (!std::is_same<T, void>::value) {
+    mx4::Eight<T> e[4];
+    const T* const from = static_cast<const T*>(p.x) + min(row, p.rows - 1) * p.x_stride;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int at = ((four * 4 + t) * 4 + wave) * 32 + quarter * 8;
+      e[t].load(from + at, row < p.rows ? p.k - at : 0);
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      const int s = mx4::scale_byte(mx4::Eight<T>::widen(quad_max(e[t].top())));
+      keep(t, mx4::codes_of(e[t], s), s);
+    }
   }
   if (quarter == 0) (weights ? p.w_scales : p.x_scales)[((long)(tile * fours + four) * ab + in_tile) * 64 + wave * 16 + lrow] = scales;
 }
