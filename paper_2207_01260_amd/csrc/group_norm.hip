@@ -102,13 +102,14 @@ int lanes_of(int groups, int threads) {
   return lanes;
 }
 
-// Work-groups of the whole form for a slab of `tp` vectors a superrow: as few threads as hold four vectors each, or up to the most.  false: too much.
+// Work-groups of the whole form for a slab of `tp` vectors a superrow: as few threads as hold half of what a thread can, or up to all of it.  (Bringing fewer
+// threads to a map: 64 x 14 x 14 x 576 bf16 with eight vectors each 12.6 us, four 15.3; its gradient at 32 images with four 15.2, eight 18.1.)  false: too much.
 bool fit_whole(NormGeom& g, int tp, int cg, int most_threads, int most_vectors) {
   if (tp > most_threads || (long)tp * g.V > kWholeColumns) return false;
   for (int t = 256; t <= most_threads; t *= 2) {
     if (t < tp) continue;
     const int rpi = std::min(t / tp, g.SR), nv = (g.SR + rpi - 1) / rpi;
-    if (nv <= 4 || (t == most_threads && nv <= most_vectors)) {
+    if (nv <= most_vectors / 2 || (t == most_threads && nv <= most_vectors)) {
       g.tp = tp, g.rpi = rpi, g.nv = nv, g.slabs = g.P / tp;
       g.threads = (tp * rpi + 63) / 64 * 64;
       g.few = g.SR / rpi, g.more = g.SR % rpi, g.last_r = (g.SR - 1) % rpi;
