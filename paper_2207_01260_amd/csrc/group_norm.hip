@@ -159,8 +159,8 @@ NormGeom geometry(const cprune_norm_desc& d, bool backward) {
   // four vectors a thread.
   const long want = std::max(1L, 512 / ((long)d.n * g.tiles));
   const long most = (g.SR + 4L * g.rpi - 1) / (4L * g.rpi);
-  // (and few enough that a work-group joins an image's sums with eight entries a thread)
-  const long few = std::max(4L, 8L * norm::kThreads / d.groups);
+  // (and few enough that a work-group joins an image's sums with sixteen entries a thread)
+  const long few = std::max(4L, 16L * norm::kThreads / d.groups);
   const long chunks = std::max(1L, std::min({want, most, few}));
   g.spc = (int)((g.SR + chunks - 1) / chunks);
   g.spc = (g.spc + g.rpi - 1) / g.rpi * g.rpi;

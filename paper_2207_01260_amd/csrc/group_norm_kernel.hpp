@@ -311,23 +311,23 @@ __device__ __forceinline__ double2 sum_lanes(double2 s, int lanes) {
 }
 
 // Sum over a group's `outer` x `inner` entries of pairs add(outer, inner, get(outer, inner)), in 64 bits and a fixed order, by `lanes` neighbouring lanes; all
-// of them get it.  Four entries are under way at a time; a lane counts its place on instead of dividing.
-template <typename Get, typename Add> __device__ __forceinline__ double2 lanes_sum(int lane, int lanes, int outer, int inner, Get&& get, Add&& add) {
+// of them get it.  U entries are under way at a time; a lane counts its place on instead of dividing.
+template <int U, typename Get, typename Add> __device__ __forceinline__ double2 lanes_sum(int lane, int lanes, int outer, int inner, Get&& get, Add&& add) {
   double2 s = {0.0, 0.0};
   const int skip = lanes / inner, step = lanes - skip * inner;
   int o = lane / inner, in = lane - o * inner;
   while (o < outer) {
-    float2 e[4];
-    int at[4][2];
+    float2 e[U];
+    int at[U][2];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
+    for (int u = 0; u < U; ++u) {
       at[u][0] = o, at[u][1] = in;
       if (o < outer) e[u] = get(o, in);
       o += skip, in += step;
       if (in >= inner) in -= inner, ++o;
     }
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
+    for (int u = 0; u < U; ++u)
       if (at[u][0] < outer) {
         const double2 v = add(at[u][0], at[u][1], e[u]);
         s.x += v.x, s.y += v.y;
@@ -344,7 +344,7 @@ __device__ __forceinline__ double2 raw_sums(double n, float2 e) {
 
 // Weighted sums of dz and dz xhat over the columns of group g, whose first channel is ch0.
 __device__ __forceinline__ double2 group_terms(const NormArgs& a, const float2* col, int lane, int lanes, int g, int ch0) {
-  return lanes_sum(
+  return lanes_sum<4>(
       lane, lanes, a.g.R, a.cg, [&](int rr, int ch) __attribute__((always_inline)) { return col[rr * a.c + g * a.cg + ch]; },
       [&](int, int ch, float2 e) __attribute__((always_inline)) {
         const double w = a.weight ? a.weight[ch0 + ch] : 1.0f;
@@ -471,7 +471,7 @@ __global__ __launch_bounds__(norm::kThreads, 4) void norm_stats_kernel(const Nor
   const int lanes = a.g.lanes, lane = t & (lanes - 1), per = kThreads / lanes;
   const double inv = 1.0 / ((double)chunk_pixels(a, k.part) * a.cg);
   for (int g = t / lanes; g < a.groups; g += per) {
-    const double2 s = lanes_sum(
+    const double2 s = lanes_sum<4>(
         lane, lanes, a.g.R, a.cg,
         [&](int rr, int ch) __attribute__((always_inline)) {
           const int q = rr * a.c + g * a.cg + ch;
@@ -529,7 +529,7 @@ __global__ __launch_bounds__(norm::kThreads, 4) void norm_apply_kernel(const Nor
     const int lanes = a.g.lanes, lane = (int)threadIdx.x & (lanes - 1), per = kThreads / lanes;
     const float2* const part = a.gpart + (long)k.image * a.g.chunks * a.groups;
     for (int g = (int)threadIdx.x / lanes; g < a.groups; g += per) {
-      const double2 s = lanes_sum(
+      const double2 s = lanes_sum<8>(
           lane, lanes, a.g.chunks, 1, [&](int chunk, int) __attribute__((always_inline)) { return part[chunk * a.groups + g]; },
           [&](int chunk, int, float2 e) __attribute__((always_inline)) { return raw_sums((double)(chunk_pixels(a, chunk) * a.cg), e); });
       if (lane == 0) {
@@ -710,7 +710,7 @@ __global__ __launch_bounds__(norm::kThreads, 4) void norm_grad_apply_kernel(cons
     const int lanes = a.g.lanes, lane = (int)threadIdx.x & (lanes - 1), per = kThreads / lanes;
     const float2* const part = a.gpart + (long)k.image * a.g.chunks * a.groups;
     for (int g = (int)threadIdx.x / lanes; g < a.groups; g += per) {
-      const double2 s = lanes_sum(
+      const double2 s = lanes_sum<8>(
           lane, lanes, a.g.chunks, 1, [&](int chunk, int) __attribute__((always_inline)) { return part[chunk * a.groups + g]; },
           [&](int, int, float2 e) __attribute__((always_inline)) { return make_double2(e.x, e.y); });
       if (lane == 0) term[g] = make_float2((float)(s.x * a.inv_count), (float)(s.y * a.inv_count));
@@ -819,13 +819,13 @@ __global__ __launch_bounds__(1024) void norm_whole_kernel(const NormArgs a) {
       double2 s;
       if constexpr (MERGE) {
         const int vg = a.cg / V;
-        s = lanes_sum(
+        s = lanes_sum<4>(
             lane, lanes, a.g.rpi, vg, [&](int r, int v) __attribute__((always_inline)) { return part[r * a.g.tp + g * vg + v]; },
             [&](int r, int, float2 e) __attribute__((always_inline)) {
               return raw_sums((double)((few + (r < more ? 1 : 0)) * V), e);
             });
       } else {
-        s = lanes_sum(
+        s = lanes_sum<4>(
             lane, lanes, a.g.rpi * a.g.R, a.cg,
             [&](int o, int ch) __attribute__((always_inline)) {
               const int r = a.g.R == 1 ? o : o / a.g.R, rr = o - r * a.g.R;
