@@ -67,10 +67,16 @@ template <typename X> struct Eight {
       const uint4u v = *reinterpret_cast<const uint4u*>(p);
 #pragma unroll
       for (int i = 0; i < 4; ++i) w[i] = v[i];
-    } else {
+    } else if (valid > 0) {      // (the last one again where there is none: loads that wait for nothing, a branch each would have them one by one)
       const unsigned short* h = reinterpret_cast<const unsigned short*>(p);
+      unsigned short v[8];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = (2 * i < valid ? (unsigned)h[2 * i] : 0u) | (2 * i + 1 < valid ? (unsigned)h[2 * i + 1] << 16 : 0u);
+      for (int i = 0; i < 8; ++i) v[i] = h[min(i, valid - 1)];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = (2 * i < valid ? (unsigned)v[2 * i] : 0u) | (2 * i + 1 < valid ? (unsigned)v[2 * i + 1] << 16 : 0u);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = 0;
     }
   }
   // largest magnitude, in a form that orders like it (as integers, magnitudes order like numbers, NaN above infinity)
@@ -103,9 +109,14 @@ template <> struct Eight<float> {
       const float4u lo = *reinterpret_cast<const float4u*>(p), hi = *reinterpret_cast<const float4u*>(p + 4);
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[i] = lo[i], v[4 + i] = hi[i];
+    } else if (valid > 0) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = p[min(i, valid - 1)];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = i < valid ? v[i] : 0.0f;
     } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = i < valid ? p[i] : 0.0f;
+      for (int i = 0; i < 8; ++i) v[i] = 0.0f;
     }
   }
   __device__ __forceinline__ unsigned top() const {
