@@ -497,7 +497,7 @@ int cprune_search_destroy(cprune_search* s);
  * Group norm with an activation, channels last, and its gradient: the normalisation of a
  * network that is tuned between pruning steps on batches too small for batch statistics.
  *
- * x [n][pixels][c], pixel i of an image x_stride elements behind pixel i - 1 (x_stride >= c, images n * pixels apart:
+ * x [n][pixels][c], pixel i of an image x_stride elements behind pixel i - 1 (x_stride >= c, images pixels * x_stride apart:
  * a dense tensor has x_stride = c, the first channels of a wider map have that map's c).  Over the pixels and the
  * c / groups channels of each (image, group):
  *   mean = sum x / m, var = sum (x - mean)^2 / m, rstd = 1 / sqrt(var + eps), m = pixels * c / groups
@@ -514,6 +514,7 @@ int cprune_search_destroy(cprune_search* s);
  * mean, rstd     fp32 [n][groups]; mean_out / rstd_out may be NULL
  * dy             as x, with dy_stride
  * dweight, dbias fp32 [c], each may be NULL.  Summed in a fixed order: repeated calls give identical bits.
+ * ws             cprune_group_norm_workspace_bytes(...) of scratch, 16-byte aligned; NULL where that is 0
  * n, pixels >= 1; groups divides c; eps > 0 and finite.  More (image, group) pairs than a launch has work-groups (2^22): CPRUNE_ERR_UNSUPPORTED. */
 typedef struct {
   int32_t n, pixels, c, groups;

@@ -16,28 +16,31 @@ __device__ __forceinline__ int chunk_count(const NormGeom& g, int chunk, int rr)
 }
 
 // Sum over the entries (chunk, pixel of the superrow, channel of the group) of an (image, group), one work-group, in 64 bits and a fixed order: f(chunk,
-// pixel, channel, entry).  Four entries are under way at a time; a thread counts its place on instead of dividing.
-template <typename F> __device__ __forceinline__ double2 entries_sum(const NormArgs& a, const float2* part, F&& f) {
+// pixel, entry, weight).  Eight entries are under way at a time; a thread counts its place on instead of dividing.
+template <typename F> __device__ __forceinline__ double2 entries_sum(const NormArgs& a, const float2* part, const float* weight, F&& f) {
   __shared__ double2 sums[1024 / 64];
   const int t = (int)threadIdx.x, n = (int)blockDim.x, row = a.g.R * a.c, per = a.g.R * a.cg;
   int chunk = t / per, rr = (t - chunk * per) / a.cg, ch = t - chunk * per - rr * a.cg;
   const int d_chunk = n / per, d_rr = (n - d_chunk * per) / a.cg, d_ch = n - d_chunk * per - d_rr * a.cg;
   double2 s = {0.0, 0.0};
   while (chunk < a.g.chunks) {
-    float2 e[4];
-    int at[4][3];
+    float2 e[8];
+    float w[8];
+    int at[8][2];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      at[u][0] = chunk, at[u][1] = rr, at[u][2] = ch;
-      e[u] = chunk < a.g.chunks ? part[(long)chunk * row + rr * a.c + ch] : make_float2(0.0f, 0.0f);
+    for (int u = 0; u < 8; ++u) {
+      at[u][0] = chunk, at[u][1] = rr;
+      const int from = min(chunk, a.g.chunks - 1);      // (past the last chunk: counted out below)
+      e[u] = part[(long)from * row + rr * a.c + ch];
+      w[u] = weight ? weight[ch] : 1.0f;
       ch += d_ch, rr += d_rr, chunk += d_chunk;
       if (ch >= a.cg) ch -= a.cg, ++rr;
       if (rr >= a.g.R) rr -= a.g.R, ++chunk;
     }
 #pragma unroll
-    for (int u = 0; u < 4; ++u)
+    for (int u = 0; u < 8; ++u)
       if (at[u][0] < a.g.chunks) {
-        const double2 v = f(at[u][0], at[u][1], at[u][2], e[u]);
+        const double2 v = f(at[u][0], at[u][1], e[u], w[u]);
         s.x += v.x, s.y += v.y;
       }
   }
@@ -57,7 +60,7 @@ template <typename F> __device__ __forceinline__ double2 entries_sum(const NormA
 __global__ __launch_bounds__(1024) void norm_join_stats_kernel(const NormArgs a, float* __restrict__ mean_out, float* __restrict__ rstd_out) {
   const int image = blockIdx.x / (unsigned)a.groups, group = blockIdx.x - image * a.groups;
   const float2* part = a.part + (long)image * a.g.chunks * a.g.R * a.c + group * a.cg;
-  const double2 s = entries_sum(a, part, [&](int chunk, int rr, int, float2 e) __attribute__((always_inline)) {
+  const double2 s = entries_sum(a, part, nullptr, [&](int chunk, int rr, float2 e, float) __attribute__((always_inline)) {
     return norm::raw_sums((double)chunk_count(a.g, chunk, rr), e);
   });
   if (threadIdx.x == 0) {
@@ -71,14 +74,13 @@ __global__ __launch_bounds__(1024) void norm_join_stats_kernel(const NormArgs a,
 __global__ __launch_bounds__(1024) void norm_join_grads_kernel(const NormArgs a, float2* __restrict__ terms) {
   const int image = blockIdx.x / (unsigned)a.groups, group = blockIdx.x - image * a.groups;
   const float2* part = a.part + (long)image * a.g.chunks * a.g.R * a.c + group * a.cg;
-  const double2 s = entries_sum(a, part, [&](int, int, int ch, float2 e) __attribute__((always_inline)) {
-    const double w = a.weight ? a.weight[group * a.cg + ch] : 1.0f;
-    return make_double2(w * e.x, w * e.y);
+  const double2 s = entries_sum(a, part, a.weight ? a.weight + group * a.cg : nullptr, [&](int, int, float2 e, float w) __attribute__((always_inline)) {
+    return make_double2((double)w * e.x, (double)w * e.y);
   });
   if (threadIdx.x == 0) terms[blockIdx.x] = make_float2((float)(s.x * a.inv_count), (float)(s.y * a.inv_count));
 }
 
-// threads of those: four entries each, 64 to 1024
+// threads of those: four entries each or more, 64 to 1024
 int join_threads(const NormArgs& a) {
   const long entries = (long)a.g.chunks * a.g.R * a.cg;
   int t = 64;
@@ -95,16 +97,16 @@ int vector_of(int c, int dtype, bool dense) {
 
 constexpr int kWholeColumns = 4096;      // elements of a slab's superrow (LDS)
 
-// Lanes that sum one of `groups` groups so that they fill the threads: a power of two up to a wavefront.
-int lanes_of(int groups, int threads) {
-  int lanes = 64;
-  while (lanes > 1 && lanes * groups > threads) lanes /= 2;
+// Threads that sum one of `groups` groups of `entries` each so that they fill the work-group: a power of two, past a wavefront where that leaves each four entries.
+int lanes_of(int groups, int threads, long entries) {
+  int lanes = 1024;
+  while (lanes > 1 && ((long)lanes * groups > threads || (lanes > 64 && lanes * 4L > entries))) lanes /= 2;
   return lanes;
 }
 
 // Work-groups of the whole form for a slab of `tp` vectors a superrow: as few threads as hold half of what a thread can, or up to all of it.  (Bringing fewer
 // threads to a map: 64 x 14 x 14 x 576 bf16 with eight vectors each 12.6 us, four 15.3; its gradient at 32 images with four 15.2, eight 18.1.)  false: too much.
-bool fit_whole(NormGeom& g, int tp, int cg, int most_threads, int most_vectors) {
+bool fit_whole(NormGeom& g, int tp, int cg, bool backward, int most_threads, int most_vectors) {
   if (tp > most_threads || (long)tp * g.V > kWholeColumns) return false;
   for (int t = 256; t <= most_threads; t *= 2) {
     if (t < tp) continue;
@@ -115,7 +117,7 @@ bool fit_whole(NormGeom& g, int tp, int cg, int most_threads, int most_vectors) 
       g.few = g.SR / rpi, g.more = g.SR % rpi, g.last_r = (g.SR - 1) % rpi;
       g.by_tp = norm_div(tp, 1024);
       g.groups = tp * g.V / (g.R * cg);
-      g.lanes = lanes_of(g.groups, g.threads);
+      g.lanes = lanes_of(g.groups, g.threads, (backward ? 1L : (long)rpi * g.R) * (cg % g.V || backward ? cg : cg / g.V));
       return true;
     }
   }
@@ -133,9 +135,16 @@ bool choose_whole(const cprune_norm_desc& d, bool backward, NormGeom& g) {
   const int least = g.R > 1 ? g.P : std::lcm(v, cg) / v;                  // vectors
   const int times = g.P / least;
   for (int k = times; k > 1; --k)
-    if (times % k == 0 && (long)least * k * 16 <= 128 && (long)d.n * (times / k) >= 256 && fit_whole(g, least * k, cg, most_threads, most_vectors)) return true;
-  return fit_whole(g, least, cg, most_threads, most_vectors);
+    if (times % k == 0 && (long)least * k * 16 <= 128 && (long)d.n * (times / k) >= 256 && fit_whole(g, least * k, cg, backward, most_threads, most_vectors)) return true;
+  // A compute unit alone brings some 10 to 20 GB/s from memory: the gradient of few and large slabs is split (27 x 7 x 22 x 111 fp16, 34 KB and 27 of them, 18.8 us
+  // whole, 13.1 split; but 6 x 20 x 15 x 608 fp32, 114 of them, 10.3 and 13.5, and one of 11 KB, 7 x 99 x 16, 6.6 and 10.0).
+  if (backward && (double)least * g.SR * 16 > 20000.0 && (long)d.n * times < 64) return false;
+  return fit_whole(g, least, cg, backward, most_threads, most_vectors);
 }
+
+// Split form: the work-groups that read x leave sums of groups, and those that read it again join them.  Not where each of many work-groups beside each other
+// would leave sums of many groups: a launch between has a work-group for each (image, group) then.
+bool sums_groups(const cprune_norm_desc& d, const NormGeom& g) { return g.tiles == 1 || d.groups <= 64; }
 
 NormGeom geometry(const cprune_norm_desc& d, bool backward) {
   NormGeom g = {};
@@ -152,19 +161,20 @@ NormGeom geometry(const cprune_norm_desc& d, bool backward) {
   g.tp = (g.P + g.tiles - 1) / g.tiles;
   g.rpi = norm::kThreads / g.tp;
   g.threads = norm::kThreads;
-  g.groups = d.groups, g.lanes = lanes_of(d.groups, norm::kThreads);
+  g.groups = d.groups;
   g.by_tp = norm_div(g.tp, 1024);
   // two work-groups a compute unit, which run at once (registers): what a work-group does but once, its sums' way through LDS before all, is much of a
   // launch on maps of some MB (32 x 56 x 56 x 64 bf16 with 512 work-groups 18.7 us, 1024 21.7, 256 18.5; 64 x 112 x 112 x 96 fp16 105, 108, 110).  At least
   // four vectors a thread.
   const long want = std::max(1L, 512 / ((long)d.n * g.tiles));
   const long most = (g.SR + 4L * g.rpi - 1) / (4L * g.rpi);
-  // (and few enough that a work-group joins an image's sums with sixteen entries a thread)
-  const long few = std::max(4L, 16L * norm::kThreads / d.groups);
+  // (and few enough that a work-group joins an image's sums with sixteen entries a thread, or where a launch of its own does it with 64)
+  const long few = std::max(4L, sums_groups(d, g) ? 16L * norm::kThreads / ((long)d.groups * g.tiles) : 65536L / ((long)g.R * (d.c / d.groups)));
   const long chunks = std::max(1L, std::min({want, most, few}));
   g.spc = (int)((g.SR + chunks - 1) / chunks);
   g.spc = (g.spc + g.rpi - 1) / g.rpi * g.rpi;
   g.chunks = (g.SR + g.spc - 1) / g.spc;
+  g.lanes = lanes_of(d.groups, norm::kThreads, (backward ? 1L : g.R) * (d.c / d.groups));
   return g;
 }
 
@@ -200,8 +210,9 @@ NormScratch scratch_of(const cprune_norm_desc& d, const NormGeom& g, bool backwa
     if (backward && d.n > 1) q.part = round16((size_t)d.n * d.c * pair);
     return q;
   }
-  if (backward || g.tiles > 1) q.part = round16((size_t)d.n * g.chunks * g.R * d.c * pair);
-  if (g.tiles == 1) q.gpart = round16((size_t)d.n * g.chunks * d.groups * pair);
+  const bool groups = sums_groups(d, g);
+  if (backward || !groups) q.part = round16((size_t)d.n * g.chunks * (g.tiles > 1 ? g.R : 1) * d.c * pair);
+  if (groups) q.gpart = (size_t)d.n * g.chunks * g.tiles * d.groups * sizeof(double2);
   else q.stats = round16((size_t)d.n * d.groups * pair);
   return q;
 }
@@ -241,7 +252,7 @@ NormLaunch launch_of(const cprune_norm_desc& d, const NormArgs& a, bool backward
     const size_t pairs = backward ? std::max(g.V * g.threads / 2, cols + g.groups) : (a.cg % g.V == 0 ? g.tp : cols) * g.rpi + g.groups;
     l.lds = (unsigned)(pairs * sizeof(float2));
   } else {
-    if (g.tiles == 1) l.lds = (unsigned)(d.groups * sizeof(float2));
+    if (sums_groups(d, g)) l.lds = (unsigned)(d.groups * sizeof(float2));
     l.grid = (unsigned)(d.n * g.chunks * g.tiles);
   }
   return l;
@@ -266,6 +277,7 @@ extern "C" int cprune_group_norm_act(const cprune_norm_desc* d, const void* x, c
   if (too_many_groups(*d, g)) return CPRUNE_ERR_UNSUPPORTED;
   const NormScratch q = scratch_of(*d, g, false);
   if (q.total() && (!ws || ws_bytes < q.total())) return CPRUNE_ERR_WORKSPACE;
+  if (reinterpret_cast<uintptr_t>(ws) & 15) return CPRUNE_ERR_INVALID_ARG;
   hipStream_t s = static_cast<hipStream_t>(stream);
   NormArgs a = args_of(*d, g);
   a.x = x, a.y = y, a.weight = weight, a.bias = bias;
@@ -275,7 +287,7 @@ extern "C" int cprune_group_norm_act(const cprune_norm_desc* d, const void* x, c
   if (g.nv) {
     launch(d->dtype, kNormWhole, a, l, s);
   } else if (q.gpart) {
-    a.gpart = reinterpret_cast<float2*>(scratch);
+    a.gpart = reinterpret_cast<double2*>(scratch);
     launch(d->dtype, kNormStats, a, l, s);
     launch(d->dtype, kNormApply, a, l, s);
   } else {
@@ -302,6 +314,7 @@ extern "C" int cprune_group_norm_act_backward(const cprune_norm_desc* d, const v
   if (too_many_groups(*d, g)) return CPRUNE_ERR_UNSUPPORTED;
   const NormScratch q = scratch_of(*d, g, true);
   if (q.total() && (!ws || ws_bytes < q.total())) return CPRUNE_ERR_WORKSPACE;
+  if (reinterpret_cast<uintptr_t>(ws) & 15) return CPRUNE_ERR_INVALID_ARG;
   hipStream_t s = static_cast<hipStream_t>(stream);
   NormArgs a = args_of(*d, g);
   a.x = x, a.dy = dy, a.y = dx, a.weight = weight, a.bias = bias, a.mean = mean, a.rstd = rstd;
@@ -314,7 +327,7 @@ extern "C" int cprune_group_norm_act_backward(const cprune_norm_desc* d, const v
   } else {
     char* const behind = static_cast<char*>(ws) + q.part;
     float2* const terms = reinterpret_cast<float2*>(behind + q.gpart);
-    if (q.gpart) a.gpart = reinterpret_cast<float2*>(behind);
+    if (q.gpart) a.gpart = reinterpret_cast<double2*>(behind);
     a.terms = terms;
     launch(d->dtype, kNormGradSums, a, l, s);
     if (!q.gpart) norm_join_grads_kernel<<<d->n * d->groups, join_threads(a), 0, s>>>(a, terms);

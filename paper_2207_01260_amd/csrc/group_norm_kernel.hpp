@@ -33,7 +33,7 @@ struct NormGeom {
   NormDiv by_tp;        // of a thread's number
   int few, more, last_r;   // whole form: superrows of a thread, one more for r < more; the r that has the last one
   int slabs, nv;        // whole form: work-groups an image (of tp vectors a superrow each), vectors a thread holds
-  int groups, lanes;    // groups of a slab; lanes that sum one, a power of two
+  int groups, lanes;    // groups of a slab; threads that sum one, a power of two
 };
 
 constexpr int kNormWholeVectors = 16, kNormWholeGradVectors = 8;      // a thread of the whole form holds at most, of x or of x and dy each
@@ -48,8 +48,8 @@ struct NormArgs {
   float *dweight, *dbias;     // backward, or null
   int n;
   void* y;                    // forward: y, backward: dx
-  float2* part;               // split form [n][chunk][R * c]: forward (mean, squares about it), backward (sum dz, sum dz xhat)
-  float2* gpart;              // the same of each group [n][chunk][group], backward weighted; null: superrows wider than a work-group
+  float2* part;               // sums of channels or of a superrow's elements: forward (mean, squares about it), backward (sum dz, sum dz xhat)
+  double2* gpart;             // split form, sums of groups [n][chunk][tile][group]: forward (numbers, their squares), backward weighted; or null
   int pixels, c, cg, groups;
   NormDiv by_cg;              // of a channel
   double inv_count;           // 1 / (numbers of an (image, group))
@@ -79,9 +79,13 @@ template <typename T, int V> __device__ __forceinline__ typename RawOf<typename 
   typedef typename Bits<T>::type B;
   typedef typename RawOf<B, V>::type Raw;
   if (V == 1 || valid >= V) return *static_cast<const Raw*>(p);
-  Raw r;
+  Raw r = B(0);
+  if (valid <= 0) return r;
+  // (the last one again where there is none: loads that wait for nothing, a branch each would have them one by one)
 #pragma unroll
-  for (int j = 0; j < V; ++j) r[j] = j < valid ? static_cast<const B*>(p)[j] : B(0);
+  for (int j = 0; j < V; ++j) r[j] = static_cast<const B*>(p)[min(j, valid - 1)];
+#pragma unroll
+  for (int j = 0; j < V; ++j) r[j] = j < valid ? r[j] : B(0);
   return r;
 }
 // STREAM: past the caches, for a map that would only push itself out of them
@@ -163,10 +167,6 @@ __device__ __forceinline__ Place place_whole(const NormGeom& g) {
   k.sr0 = 0;
   k.sr1 = g.SR;
   return k;
-}
-// pixels of a chunk
-__device__ __forceinline__ int chunk_pixels(const NormArgs& a, int chunk) {
-  return min(a.pixels, (chunk + 1) * a.g.spc * a.g.R) - chunk * a.g.spc * a.g.R;
 }
 // elements of the vector at position p that superrow sr has
 __device__ __forceinline__ int valid_of(const NormGeom& g, int c, int sr, int p) {
@@ -317,7 +317,7 @@ template <int U, typename Get, typename Add> __device__ __forceinline__ double2 
   const int skip = lanes / inner, step = lanes - skip * inner;
   int o = lane / inner, in = lane - o * inner;
   while (o < outer) {
-    float2 e[U];
+    decltype(get(0, 0)) e[U];
     int at[U][2];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -336,20 +336,68 @@ template <int U, typename Get, typename Add> __device__ __forceinline__ double2 
   return sum_lanes(s, lanes);
 }
 
+// done(group, sum) for each of a work-group's groups, by one thread; sum(group, lane) is what a lane's wavefront (or less, where lanes are fewer) has of it.  More
+// than a wavefront's lanes, where there are few groups: their sums are joined through LDS, in a fixed order.  All threads call it; it ends without a barrier.
+template <typename Sum, typename Done> __device__ __forceinline__ void each_group(int lanes, int groups, Sum&& sum, Done&& done) {
+  const int t = (int)threadIdx.x, lane = t & (lanes - 1);
+  if (lanes <= 64) {
+    const int per = (int)blockDim.x / lanes;
+    for (int g = t / lanes; g < groups; g += per) {
+      const double2 s = sum(g, lane);
+      if (lane == 0) done(g, s);
+    }
+    return;
+  }
+  __shared__ double2 waves[1024 / 64];
+  const int mine = t / lanes, each = lanes / 64;
+  if (mine < groups) {
+    const double2 s = sum(mine, lane);
+    if ((t & 63) == 0) waves[t >> 6] = s;
+  }
+  __syncthreads();
+  if (t < groups) {
+    double2 s = waves[t * each];
+    for (int i = 1; i < each; ++i) s.x += waves[t * each + i].x, s.y += waves[t * each + i].y;
+    done(t, s);
+  }
+}
+
 // sums of n numbers and of their squares from their (mean, squares about it)
 __device__ __forceinline__ double2 raw_sums(double n, float2 e) {
   const double nm = n * e.x;
   return n > 0.0 ? make_double2(nm, (double)e.y + nm * e.x) : make_double2(0.0, 0.0);
 }
 
-// Weighted sums of dz and dz xhat over the columns of group g, whose first channel is ch0.
-__device__ __forceinline__ double2 group_terms(const NormArgs& a, const float2* col, int lane, int lanes, int g, int ch0) {
+// The sums of dz and dz xhat of a superrow's elements (LDS) as those of its channels, which go to out(channel, sums), and with weights in their place in LDS:
+// a thread a channel, so that a weight is loaded once.  All threads call it; ch0 is the first of the `channels`.
+template <typename Out> __device__ __forceinline__ void fold_columns(const NormArgs& a, float2* col, int channels, int ch0, Out&& out) {
+  __syncthreads();
+  for (int ch = threadIdx.x; ch < channels; ch += (int)blockDim.x) {
+    const float w = a.weight ? a.weight[ch0 + ch] : 1.0f;
+    float2 s = col[ch];
+    for (int rr = 1; rr < a.g.R; ++rr) s.x += col[rr * a.c + ch].x, s.y += col[rr * a.c + ch].y;
+    out(ch, s);
+    col[ch] = make_float2(w * s.x, w * s.y);
+  }
+  __syncthreads();
+}
+// The sum of add(place in the tile, ...) over the elements of group g that a work-group's tile of the superrow has, `count` of them from element q0 on.
+template <typename At> __device__ __forceinline__ double2 tile_sum(const NormArgs& a, int lane, int lanes, int g, int q0, int count, At&& at) {
+  double2 s = {0.0, 0.0};
+  for (int rr = 0; rr < a.g.R; ++rr) {
+    const int base = rr * a.c + g * a.cg - q0, end = min(base + a.cg, count);
+    for (int e = max(base, 0) + lane; e < end; e += lanes) {
+      const double2 v = at(e);
+      s.x += v.x, s.y += v.y;
+    }
+  }
+  return sum_lanes(s, lanes);
+}
+// Their sum over group g.
+__device__ __forceinline__ double2 group_terms(const NormArgs& a, const float2* col, int lane, int lanes, int g) {
   return lanes_sum<4>(
-      lane, lanes, a.g.R, a.cg, [&](int rr, int ch) __attribute__((always_inline)) { return col[rr * a.c + g * a.cg + ch]; },
-      [&](int, int ch, float2 e) __attribute__((always_inline)) {
-        const double w = a.weight ? a.weight[ch0 + ch] : 1.0f;
-        return make_double2(w * e.x, w * e.y);
-      });
+      lane, lanes, a.cg, 1, [&](int ch, int) __attribute__((always_inline)) { return col[g * a.cg + ch]; },
+      [&](int, int, float2 e) __attribute__((always_inline)) { return make_double2(e.x, e.y); });
 }
 
 }  // namespace norm
@@ -467,25 +515,18 @@ __global__ __launch_bounds__(norm::kThreads, 4) void norm_stats_kernel(const Nor
     return;
   }
   __syncthreads();
-  // the superrow's elements as groups
-  const int lanes = a.g.lanes, lane = t & (lanes - 1), per = kThreads / lanes;
-  const double inv = 1.0 / ((double)chunk_pixels(a, k.part) * a.cg);
-  for (int g = t / lanes; g < a.groups; g += per) {
-    const double2 s = lanes_sum<4>(
-        lane, lanes, a.g.R, a.cg,
-        [&](int rr, int ch) __attribute__((always_inline)) {
-          const int q = rr * a.c + g * a.cg + ch;
-          return make_float2(s_mean[q % V][q / V], s_sq[q % V][q / V]);
-        },
-        [&](int rr, int ch, float2 e) __attribute__((always_inline)) {
-          const int q = rr * a.c + g * a.cg + ch;
-          return raw_sums(s_n[q % V][q / V], e);
+  // the tile's elements as groups
+  const int lanes = a.g.lanes;
+  const int p0 = k.p - (t - k.r * a.g.tp), count = min(a.g.tp, a.g.P - p0) * V;
+  double2* const out = a.gpart + (((long)k.image * a.g.chunks + k.part) * a.g.tiles + p0 / a.g.tp) * a.groups;
+  each_group(
+      lanes, a.groups,
+      [&](int g, int lane) __attribute__((always_inline)) {
+        return tile_sum(a, lane, lanes, g, p0 * V, count, [&](int e) __attribute__((always_inline)) {
+          return raw_sums(s_n[e % V][e / V], make_float2(s_mean[e % V][e / V], s_sq[e % V][e / V]));
         });
-    if (lane == 0) {
-      const double mean_g = s.x * inv, sq_g = s.y - mean_g * s.x;
-      a.gpart[((long)k.image * a.g.chunks + k.part) * a.groups + g] = make_float2((float)mean_g, sq_g < 0.0 ? 0.0f : (float)sq_g);
-    }
-  }
+      },
+      [&](int g, double2 s) __attribute__((always_inline)) { out[g] = s; });
 }
 
 template <typename T, int V, bool SILU, bool STREAM>
@@ -526,19 +567,21 @@ __global__ __launch_bounds__(norm::kThreads, 4) void norm_apply_kernel(const Nor
     channel_terms<V>(a, here, c);
   }
   if (a.gpart) {
-    const int lanes = a.g.lanes, lane = (int)threadIdx.x & (lanes - 1), per = kThreads / lanes;
-    const float2* const part = a.gpart + (long)k.image * a.g.chunks * a.groups;
-    for (int g = (int)threadIdx.x / lanes; g < a.groups; g += per) {
-      const double2 s = lanes_sum<8>(
-          lane, lanes, a.g.chunks, 1, [&](int chunk, int) __attribute__((always_inline)) { return part[chunk * a.groups + g]; },
-          [&](int chunk, int, float2 e) __attribute__((always_inline)) { return raw_sums((double)(chunk_pixels(a, chunk) * a.cg), e); });
-      if (lane == 0) {
-        const float2 m = statistics(s, a);
-        stat[g] = m;
-        if (k.part == 0 && a.mean_out) a.mean_out[k.image * a.groups + g] = m.x;
-        if (k.part == 0 && a.rstd_out) a.rstd_out[k.image * a.groups + g] = m.y;
-      }
-    }
+    const int lanes = a.g.lanes;
+    const double2* const part = a.gpart + (long)k.image * a.g.chunks * a.g.tiles * a.groups;
+    each_group(
+        lanes, a.groups,
+        [&](int g, int lane) __attribute__((always_inline)) {
+          return lanes_sum<8>(
+              lane, lanes, a.g.chunks * a.g.tiles, 1, [&](int i, int) __attribute__((always_inline)) { return part[i * a.groups + g]; },
+              [&](int, int, double2 e) __attribute__((always_inline)) { return e; });
+        },
+        [&](int g, double2 s) __attribute__((always_inline)) {
+          const float2 m = statistics(s, a);
+          stat[g] = m;
+          if (k.part == 0 && a.mean_out) a.mean_out[k.image * a.groups + g] = m.x;      // (each tile the same)
+          if (k.part == 0 && a.rstd_out) a.rstd_out[k.image * a.groups + g] = m.y;
+        });
     __syncthreads();
   }
   if (!k.active) return;
@@ -572,9 +615,9 @@ __global__ __launch_bounds__(norm::kThreads, 4) void norm_grad_sums_kernel(const
   constexpr int U = kGradBatch;
   __shared__ float2 buffer[V * kThreads];
   const Place k = place(a.g, blockIdx.x);
-  float sb[V], sw[V];
+  float sb[V], sw[V], weight[V];
 #pragma unroll
-  for (int j = 0; j < V; ++j) sb[j] = sw[j] = 0.0f;
+  for (int j = 0; j < V; ++j) sb[j] = sw[j] = 0.0f, weight[j] = 1.0f;
   if (k.active) {
     Terms<V> c;
     const char* xb = static_cast<const char*>(a.x) + (k.image * a.x_image + (long)k.p * V) * (long)sizeof(T);
@@ -601,6 +644,8 @@ __global__ __launch_bounds__(norm::kThreads, 4) void norm_grad_sums_kernel(const
     Batch head;
     fetch(head, 0);
     all_terms<V>(a, k.image, where<V>(a, k.p * V), c);
+#pragma unroll
+    for (int j = 0; j < V; ++j) weight[j] = c.w[j];
     walk(
         head, whole, fetch,
         [&](const Batch& q) __attribute__((always_inline)) {
@@ -617,21 +662,31 @@ __global__ __launch_bounds__(norm::kThreads, 4) void norm_grad_sums_kernel(const
         });
   }
   add_rows<V>(sb, sw, k.r, a.g.tp, a.g.rpi, k.active, buffer);
+  // Sums of channels where a work-group has whole superrows, otherwise of their elements.
+  const bool whole_rows = a.g.tiles == 1;
+  const int p0 = k.p - ((int)threadIdx.x - k.r * a.g.tp), count = min(a.g.tp, a.g.P - p0) * V;
+  float2* const part = a.part + ((long)k.image * a.g.chunks + k.part) * (whole_rows ? a.c : a.g.P * V);
   if (k.active && k.r == 0) {
-    float2* out = a.part + ((long)k.image * a.g.chunks + k.part) * a.g.P * V + (long)k.p * V;
+    float2* const out = buffer + (k.p - p0) * V;
 #pragma unroll
     for (int j = 0; j < V; ++j) {
-      out[j] = make_float2(sb[j], sw[j]);
-      if (a.gpart) buffer[(int)threadIdx.x * V + j] = out[j];
+      if (!whole_rows) part[k.p * V + j] = make_float2(sb[j], sw[j]);
+      const float w = whole_rows ? 1.0f : weight[j];
+      out[j] = make_float2(w * sb[j], w * sw[j]);
     }
   }
   if (!a.gpart) return;
-  __syncthreads();
-  const int lanes = a.g.lanes, lane = (int)threadIdx.x & (lanes - 1), per = kThreads / lanes;
-  for (int g = (int)threadIdx.x / lanes; g < a.groups; g += per) {
-    const double2 s = group_terms(a, buffer, lane, lanes, g, g * a.cg);
-    if (lane == 0) a.gpart[((long)k.image * a.g.chunks + k.part) * a.groups + g] = make_float2((float)s.x, (float)s.y);
-  }
+  const int lanes = a.g.lanes;
+  double2* const out = a.gpart + (((long)k.image * a.g.chunks + k.part) * a.g.tiles + p0 / a.g.tp) * a.groups;
+  if (whole_rows) fold_columns(a, buffer, a.c, 0, [&](int ch, float2 s) __attribute__((always_inline)) { part[ch] = s; });
+  else __syncthreads();
+  each_group(
+      lanes, a.groups,
+      [&](int g, int lane) __attribute__((always_inline)) {
+        return whole_rows ? group_terms(a, buffer, lane, lanes, g)
+                          : tile_sum(a, lane, lanes, g, p0 * V, count, [&](int e) __attribute__((always_inline)) { return make_double2(buffer[e].x, buffer[e].y); });
+      },
+      [&](int g, double2 s) __attribute__((always_inline)) { out[g] = s; });
 }
 
 // dweight and dbias of eight channels from all images' partial sums, `per` rows of c of them an image; 32 threads a channel, 64 bits, a fixed order.
@@ -670,7 +725,7 @@ __global__ __launch_bounds__(norm::kThreads, 4) void norm_grad_apply_kernel(cons
   using namespace norm;
   constexpr int U = kGradBatch;
   if (blockIdx.x < vector_groups) {
-    norm_vector_sums(a, blockIdx.x, (long)a.n * a.g.chunks * a.g.R);
+    norm_vector_sums(a, blockIdx.x, (long)a.n * a.g.chunks * (a.g.tiles == 1 ? 1 : a.g.R));
     return;
   }
   extern __shared__ char lds[];
@@ -707,14 +762,18 @@ __global__ __launch_bounds__(norm::kThreads, 4) void norm_grad_apply_kernel(cons
     all_terms<V>(a, k.image, here, c);
   }
   if (a.gpart) {
-    const int lanes = a.g.lanes, lane = (int)threadIdx.x & (lanes - 1), per = kThreads / lanes;
-    const float2* const part = a.gpart + (long)k.image * a.g.chunks * a.groups;
-    for (int g = (int)threadIdx.x / lanes; g < a.groups; g += per) {
-      const double2 s = lanes_sum<8>(
-          lane, lanes, a.g.chunks, 1, [&](int chunk, int) __attribute__((always_inline)) { return part[chunk * a.groups + g]; },
-          [&](int, int, float2 e) __attribute__((always_inline)) { return make_double2(e.x, e.y); });
-      if (lane == 0) term[g] = make_float2((float)(s.x * a.inv_count), (float)(s.y * a.inv_count));
-    }
+    const int lanes = a.g.lanes;
+    const double2* const part = a.gpart + (long)k.image * a.g.chunks * a.g.tiles * a.groups;
+    each_group(
+        lanes, a.groups,
+        [&](int g, int lane) __attribute__((always_inline)) {
+          return lanes_sum<8>(
+              lane, lanes, a.g.chunks * a.g.tiles, 1, [&](int i, int) __attribute__((always_inline)) { return part[i * a.groups + g]; },
+              [&](int, int, double2 e) __attribute__((always_inline)) { return e; });
+        },
+        [&](int g, double2 s) __attribute__((always_inline)) {
+          term[g] = make_float2((float)(s.x * a.inv_count), (float)(s.y * a.inv_count));
+        });
     __syncthreads();
   }
   if (!k.active) return;
@@ -812,39 +871,35 @@ __global__ __launch_bounds__(1024) void norm_whole_kernel(const NormArgs a) {
     }
   }
   __syncthreads();
-  {
-    const int lanes = a.g.lanes, lane = (int)threadIdx.x & (lanes - 1), per = (int)blockDim.x / lanes;
-    const int more = a.g.more, few = a.g.few, last_r = a.g.last_r;
-    for (int g = (int)threadIdx.x / lanes; g < groups; g += per) {
-      double2 s;
-      if constexpr (MERGE) {
-        const int vg = a.cg / V;
-        s = lanes_sum<4>(
-            lane, lanes, a.g.rpi, vg, [&](int r, int v) __attribute__((always_inline)) { return part[r * a.g.tp + g * vg + v]; },
-            [&](int r, int, float2 e) __attribute__((always_inline)) {
-              return raw_sums((double)((few + (r < more ? 1 : 0)) * V), e);
-            });
-      } else {
-        s = lanes_sum<4>(
-            lane, lanes, a.g.rpi * a.g.R, a.cg,
-            [&](int o, int ch) __attribute__((always_inline)) {
-              const int r = a.g.R == 1 ? o : o / a.g.R, rr = o - r * a.g.R;
-              return part[r * cols + rr * a.c + g * a.cg + ch];
-            },
-            [&](int o, int, float2 e) __attribute__((always_inline)) {
-              const int r = a.g.R == 1 ? o : o / a.g.R, rr = o - r * a.g.R;
-              return raw_sums((double)(few + (r < more ? 1 : 0) - (SLAB == kTail && r == last_r && rr >= a.g.tail ? 1 : 0)), e);
-            });
-      }
-      if (lane == 0) {
+  const int lanes = a.g.lanes, more = a.g.more, few = a.g.few, last_r = a.g.last_r;
+  each_group(
+      lanes, groups,
+      [&](int g, int lane) __attribute__((always_inline)) {
+        if constexpr (MERGE) {
+          const int vg = a.cg / V;
+          return lanes_sum<4>(
+              lane, lanes, a.g.rpi, vg, [&](int r, int v) __attribute__((always_inline)) { return part[r * a.g.tp + g * vg + v]; },
+              [&](int r, int, float2 e) __attribute__((always_inline)) { return raw_sums((double)((few + (r < more ? 1 : 0)) * V), e); });
+        } else {
+          return lanes_sum<4>(
+              lane, lanes, a.g.rpi * a.g.R, a.cg,
+              [&](int o, int ch) __attribute__((always_inline)) {
+                const int r = a.g.R == 1 ? o : o / a.g.R, rr = o - r * a.g.R;
+                return part[r * cols + rr * a.c + g * a.cg + ch];
+              },
+              [&](int o, int, float2 e) __attribute__((always_inline)) {
+                const int r = a.g.R == 1 ? o : o / a.g.R, rr = o - r * a.g.R;
+                return raw_sums((double)(few + (r < more ? 1 : 0) - (SLAB == kTail && r == last_r && rr >= a.g.tail ? 1 : 0)), e);
+              });
+        }
+      },
+      [&](int g, double2 s) __attribute__((always_inline)) {
         const float2 m = statistics(s, a);
         stat[g] = m;
         const int at = k.image * a.groups + k.part * groups + g;
         if (a.mean_out) a.mean_out[at] = m.x;
         if (a.rstd_out) a.rstd_out[at] = m.y;
-      }
-    }
-  }
+      });
   __syncthreads();
   if (!k.active) return;
 #pragma unroll
@@ -901,27 +956,19 @@ __global__ __launch_bounds__(1024) void norm_whole_grad_kernel(const NormArgs a)
 #pragma unroll
     for (int j = 0; j < V; ++j) col[(int)threadIdx.x * V + j] = make_float2(sb[j], sw[j]);
   }
-  __syncthreads();
   const int ch0 = k.part * channels;
-  if (a.dweight || a.dbias) {
-    for (int ch = threadIdx.x; ch < channels; ch += blockDim.x) {
-      float2 s = col[ch];
-      for (int rr = 1; rr < a.g.R; ++rr) s.x += col[rr * a.c + ch].x, s.y += col[rr * a.c + ch].y;
-      if (a.n > 1) {
-        a.part[(long)k.image * a.c + ch0 + ch] = s;
-      } else {
-        if (a.dbias) a.dbias[ch0 + ch] = s.x;
-        if (a.dweight) a.dweight[ch0 + ch] = s.y;
-      }
+  fold_columns(a, col, channels, ch0, [&](int ch, float2 s) __attribute__((always_inline)) {
+    if (a.n > 1) {
+      if (a.dweight || a.dbias) a.part[(long)k.image * a.c + ch0 + ch] = s;
+    } else {
+      if (a.dbias) a.dbias[ch0 + ch] = s.x;
+      if (a.dweight) a.dweight[ch0 + ch] = s.y;
     }
-  }
-  {
-    const int lanes = a.g.lanes, lane = (int)threadIdx.x & (lanes - 1), per = (int)blockDim.x / lanes;
-    for (int g = (int)threadIdx.x / lanes; g < groups; g += per) {
-      const double2 s = group_terms(a, col, lane, lanes, g, ch0 + g * a.cg);
-      if (lane == 0) term[g] = make_float2((float)(s.x * a.inv_count), (float)(s.y * a.inv_count));
-    }
-  }
+  });
+  const int lanes = a.g.lanes;
+  each_group(
+      lanes, groups, [&](int g, int lane) __attribute__((always_inline)) { return group_terms(a, col, lane, lanes, g); },
+      [&](int g, double2 s) __attribute__((always_inline)) { term[g] = make_float2((float)(s.x * a.inv_count), (float)(s.y * a.inv_count)); });
   __syncthreads();
   if (!k.active) return;
   float2 t[V];

@@ -274,3 +274,17 @@ def test_on_another_stream_and_in_a_graph():
         y, mean, rstd = B.cprune_group_norm_act(xs, 4, weight, bias, act=B.ACT_SILU, want_stats=True)
         grads = B.cprune_group_norm_act_backward(dy, xs, mean, rstd, 4, weight, bias, act=B.ACT_SILU)
         assert torch.equal(ys, y) and all(torch.equal(p, q) for p, q in zip(gs, grads)), i
+
+
+# superrows wider than a work-group, of few groups (some across two work-groups) and of many; few and large slabs; groups summed by more than a wavefront
+FORMS = [(2, 20, 21, 1051, 1), (3, 9, 10, 1052, 4), (2, 30, 31, 1290, 6), (1, 33, 40, 1300, 100), (1, 5, 300, 1300, 65), (4, 4, 55, 239, 1), (2, 77, 16, 33, 11),
+         (2, 15, 16, 99, 3), (2, 40, 41, 160, 2)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", FORMS)
+def test_forms(shape, dtype):
+    forward_check(shape, dtype, 0, B.ACT_SILU, True)
+    forward_check(shape, dtype, 5, B.ACT_RELU, False)
+    backward_check(shape, dtype, 0, B.ACT_SILU, True)
+    backward_check(shape, dtype, 5, B.ACT_NONE, False)

@@ -116,3 +116,10 @@ def test_the_binding_looks_at_its_tensors():
         rows(x[:, :1].expand(2, 3, 3, 8), 1)              # pixels on top of each other
     with pytest.raises(ValueError):
         rows(x.permute(0, 2, 1, 3)[..., :5], 1)           # pixels in another order
+
+
+def test_norm_refuses_unaligned_scratch():
+    L, d = B.lib(), _norm(n=2, pixels=1 << 16, c=12)
+    odd = FAKE + 8
+    assert L.cprune_group_norm_act(d, FAKE, None, None, FAKE, None, None, odd, 1 << 40, None) == B.ERR_INVALID_ARG
+    assert L.cprune_group_norm_act_backward(d, FAKE, FAKE, FAKE, FAKE, None, None, FAKE, None, None, odd, 1 << 40, None) == B.ERR_INVALID_ARG
