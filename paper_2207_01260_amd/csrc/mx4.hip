@@ -166,7 +166,8 @@ struct ProductPlan {
   size_t total() const { return codes + x_scales + w_codes + w_scales; }
 };
 
-ProductPlan plan_product(int rows, int k, int c_out, bool numbers) {
+// dtype: of the rows' numbers, -1 for codes
+ProductPlan plan_product(int rows, int k, int c_out, int dtype) {
   const long blocks = blocks_of(k), steps = (blocks + 3) / 4, fours = (steps + 3) / 4;
   ProductPlan q = {};
   // Measured on bf16 numbers, us (short / few / tiles): 12544 x 200 x 64 4.7 / 8.0 / 8.8; 784 x 160 x 960 4.0 / - / 9.0; 3136 x 576 x 96 6.9 / 7.4 / 8.0; but six to
@@ -187,7 +188,10 @@ ProductPlan plan_product(int rows, int k, int c_out, bool numbers) {
     q.w_codes = (size_t)(tiles * run * 4096), q.w_scales = (size_t)(tiles * run * 256);
   } else {
     q.form = kFew;
-    q.codes_first = numbers && rows > 16;
+    // Up to 16 rows the work-groups make the codes themselves, each all of them, a lane reading 64 or 128 bytes of a row of its own.  Where that is much and slow,
+    // by twice the bytes or as 16-bit rows of odd length begin between two dwords, a launch before is quicker: 16 x 4097 x 1000 bf16 15.6 -> 6.1 us and 10.4 -> 6.3 in
+    // fp32, 4 x 8191 x 1000 13.7 -> 9.1 and 12.5 -> 9.1; but 8 x 1025 x 1000 no difference, 8 x 4096 x 1000 bf16 6.6 and 7.3.
+    q.codes_first = dtype >= 0 && (rows > 16 || ((dtype == CPRUNE_F32 || k % 2) && (long)rows * k >= 32768));
   }
   if (q.codes_first) {
     q.codes = (size_t)((long)rows * blocks * 16);
@@ -320,7 +324,7 @@ extern "C" int cprune_mx4_dequantize(const void* codes, const void* scales, int 
 
 extern "C" size_t cprune_mx4_matmul_workspace_bytes(int rows, int k, int c_out) {
   if (check_product(rows, k, c_out, CPRUNE_ACT_NONE, CPRUNE_F32) != CPRUNE_OK) return 0;
-  return plan_product(rows, k, c_out, false).total();
+  return plan_product(rows, k, c_out, -1).total();
 }
 
 extern "C" int cprune_mx4_matmul(const void* x_codes, const void* x_scales, int rows, int k, const void* w_codes, const void* w_scales,
@@ -329,7 +333,7 @@ extern "C" int cprune_mx4_matmul(const void* x_codes, const void* x_scales, int 
   const int rc = check_product(rows, k, c_out, act, dtype);
   if (rc != CPRUNE_OK) return rc;
   if (!x_codes || !x_scales || !w_codes || !w_scales || !y || !aligned16(x_codes) || !aligned16(w_codes)) return CPRUNE_ERR_INVALID_ARG;
-  const ProductPlan q = plan_product(rows, k, c_out, false);
+  const ProductPlan q = plan_product(rows, k, c_out, -1);
   if (q.total() && (!ws || ws_bytes < q.total())) return CPRUNE_ERR_WORKSPACE;
   if (!aligned16(ws)) return CPRUNE_ERR_INVALID_ARG;
   Mx4Args p = {};
@@ -342,7 +346,7 @@ extern "C" int cprune_mx4_matmul(const void* x_codes, const void* x_scales, int 
 
 extern "C" size_t cprune_mx4_linear_workspace_bytes(int rows, int k, int c_out, cprune_dtype dtype) {
   if (check_product(rows, k, c_out, CPRUNE_ACT_NONE, dtype) != CPRUNE_OK) return 0;
-  return plan_product(rows, k, c_out, true).total();
+  return plan_product(rows, k, c_out, dtype).total();
 }
 
 extern "C" int cprune_mx4_linear(const void* x, int rows, int k, int x_stride, const void* w_codes, const void* w_scales, int c_out,
@@ -351,7 +355,7 @@ extern "C" int cprune_mx4_linear(const void* x, int rows, int k, int x_stride, c
   if (rc == CPRUNE_OK) rc = check_numbers(rows, k, x_stride, dtype);
   if (rc != CPRUNE_OK) return rc;
   if (!x || !w_codes || !w_scales || !y || !aligned16(w_codes)) return CPRUNE_ERR_INVALID_ARG;
-  const ProductPlan q = plan_product(rows, k, c_out, true);
+  const ProductPlan q = plan_product(rows, k, c_out, dtype);
   if (q.total() && (!ws || ws_bytes < q.total())) return CPRUNE_ERR_WORKSPACE;
   if (!aligned16(ws)) return CPRUNE_ERR_INVALID_ARG;
   Mx4Args p = {};

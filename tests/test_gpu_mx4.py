@@ -238,3 +238,12 @@ def test_on_another_stream_and_in_a_graph():
         torch.cuda.synchronize()
         assert torch.equal(ys, B.cprune_mx4_linear(xs, wc, ws, act=B.ACT_SILU))
         assert torch.equal(back, B.cprune_mx4_dequantize(*B.cprune_mx4_quantize(xs), 320, B.BF16))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,k,c_out", [(14, 6145, 33), (4, 8193, 70), (16, 2049, 9), (1, 40001, 20)])
+def test_few_rows_of_long_and_odd_sums(rows, k, c_out, dtype):
+    x, w = numbers(rows, k, dtype), numbers(c_out, k, torch.float32, seed=1) / math.sqrt(k)
+    wc, ws = B.cprune_mx4_quantize(w)
+    y = B.cprune_mx4_linear(x, wc, ws)
+    product_check(y, decode(*encode(np64(x)), k), decode(*encode(np64(w)), k), None, B.ACT_NONE, dtype)
