@@ -180,9 +180,12 @@ ProductPlan plan_product(int rows, int k, int c_out, int dtype) {
     q.form = kShort;
   } else if (enough && (double)(rows + 255) * fours * 512 < 2147483648.0 && (double)(c_out + 255) * fours * 512 < 2147483648.0) {
     q.form = kTiles;
-    // the widest tiles that still give half of the compute units one: 1024 x 8192 x 1024 20.9 by 64, 26.9 by 128; 2048 x 2048 x 2048 18.3 by 128, 26.6 by 256
+    // Tiles of 128, of which two or three work-groups share a compute unit, one's first loads and last stores beside another's products; of 64 where that leaves
+    // less than half of the compute units one (1024 x 8192 x 1024 22.2 by 64, 24.7 by 128; 2048 x 2048 x 2048 17.3 and 16.0); of 256, alone on a compute unit
+    // but with half the bytes through the caches, for many tiles of long sums (us by 256 / by 128: 16384 x 8192 x 8192 549 / 609, 8192 x 4096 x 8192 167 / 174,
+    // but 16384 x 2048 x 8192 209 / 194, 16384 x 8192 x 2100 212 / 198).
     auto tiles_of = [&](long side) { return ((rows + side - 1) / side) * ((c_out + side - 1) / side); };
-    q.mi = tiles_of(256) >= 128 ? 8 : tiles_of(128) >= 128 ? 4 : 2;
+    q.mi = steps >= 32 && tiles_of(256) >= 1024 ? 8 : tiles_of(128) >= 128 ? 4 : 2;
     const long side = 32L * q.mi, row_tiles = (rows + side - 1) / side, tiles = (c_out + side - 1) / side, run = 2L * q.mi * fours;
     q.codes = (size_t)(row_tiles * run * 4096), q.x_scales = (size_t)(row_tiles * run * 256);
     q.w_codes = (size_t)(tiles * run * 4096), q.w_scales = (size_t)(tiles * run * 256);
@@ -239,9 +242,11 @@ template <typename T, bool SILU> void launch_tiles(Mx4Args p, int mi, hipStream_
   p.tiles = (p.c_out + 32 * mi - 1) / (32 * mi);
   p.row_tiles = (p.rows + 32 * mi - 1) / (32 * mi);
   const unsigned grid = (unsigned)((long)p.tiles * p.row_tiles);
-  if (mi == 8) mx4_tile_kernel<T, SILU, 8><<<grid, 256, 0, s>>>(p);
-  else if (mi == 4) mx4_tile_kernel<T, SILU, 4><<<grid, 256, 0, s>>>(p);
-  else mx4_tile_kernel<T, SILU, 2><<<grid, 256, 0, s>>>(p);
+  // three stages where a compute unit has work for a third work-group (11008 x 256 x 2880 30.8 -> 27.7 us; 1024 x 8192 x 1024, one each, 28.6 and with four 24.7)
+  if (mi == 8) mx4_tile_kernel<T, SILU, 8, 4><<<grid, 256, 0, s>>>(p);
+  else if (mi == 4 && grid > 256) mx4_tile_kernel<T, SILU, 4, 3><<<grid, 256, 0, s>>>(p);
+  else if (mi == 4) mx4_tile_kernel<T, SILU, 4, 4><<<grid, 256, 0, s>>>(p);
+  else mx4_tile_kernel<T, SILU, 2, 4><<<grid, 256, 0, s>>>(p);
 }
 
 // x: numbers of `dtype`, or (x_scales given) codes

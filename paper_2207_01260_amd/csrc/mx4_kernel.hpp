@@ -356,8 +356,7 @@ __global__ __launch_bounds__(256) void mx4_rows_kernel(const Mx4Args p) {
 // Four wavefronts (2 x 2) of MI x MI blocks each: 32 MI outputs of c_out by 32 MI rows a work-group, K in steps of 128 terms.  A stage is the tile's codes
 // of one step in operand order, [16-row block][lane][16 bytes], as a launch before has laid them out in memory: a step of a tile is one run of memory, so its
 // loads spread over all channels of the L2 (rows of 2^n bytes read side by side would meet in one), and they write to LDS themselves.
-// While step s is multiplied, the operands of s + 1 go to registers and the codes of s + STAGES into the stage that s has left: 4 stages where they fill
-// LDS (MI = 8), otherwise 8.
+// While step s is multiplied, the operands of s + 1 go to registers and the codes of s + STAGES into the stage that s has left.
 // The matrix instruction takes 32 rows of each side; those of a wavefront's c_out are dealt so that a lane's results are 8 MI neighbours of one row of y.
 namespace mx4 {
 
@@ -393,17 +392,15 @@ __device__ __forceinline__ void tile_of(const Mx4Args& p, int& tr, int& tc) {
 
 }  // namespace mx4
 
-template <typename T, bool SILU, int MI>
+template <typename T, bool SILU, int MI, int STAGES>
 __global__ __launch_bounds__(256) void mx4_tile_kernel(const Mx4Args p) {
   using namespace mx4;
   constexpr int NI = MI, AB = 2 * MI;               // 16-row blocks of a side of the tile
   constexpr int LOADS = AB / 2;                     // of which a wavefront loads these a step
   constexpr int CHUNKS = AB / 4;                    // of four blocks each, whose scales of four steps are one load
-  constexpr int STAGES = MI == 8 ? 4 : 8;
   // (arrays of their own: an index into one would have every read wait for every load on its way)
-  __shared__ uint4 st0[2 * AB * 64], st1[2 * AB * 64], st2[2 * AB * 64], st3[2 * AB * 64];
-  __shared__ uint4 st4[STAGES > 4 ? 2 * AB * 64 : 1], st5[STAGES > 4 ? 2 * AB * 64 : 1], st6[STAGES > 4 ? 2 * AB * 64 : 1], st7[STAGES > 4 ? 2 * AB * 64 : 1];
-  __shared__ unsigned sc0[2 * AB * 64], sc1[STAGES > 4 ? 2 * AB * 64 : 1];      // [16-row block][lane]: the scales of four steps
+  __shared__ uint4 st0[2 * AB * 64], st1[2 * AB * 64], st2[2 * AB * 64], st3[STAGES > 3 ? 2 * AB * 64 : 1];
+  __shared__ unsigned sc0[2 * AB * 64];      // [16-row block][lane]: the scales of four steps
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), lrow = lane & 15;
   const int wm = wave & 1, wn = wave >> 1;
   int tr, tc;
@@ -464,26 +461,19 @@ __global__ __launch_bounds__(256) void mx4_tile_kernel(const Mx4Args p) {
   };
 
   fetch_scales(sc0, 0);
-  if (STAGES > 4) fetch_scales(sc1, 1);
   fetch(st0, 0);
   fetch(st1, 1);
   fetch(st2, 2);
-  fetch(st3, 3);
-  if constexpr (STAGES > 4) {
-    fetch(st4, 4);
-    fetch(st5, 5);
-    fetch(st6, 6);
-    fetch(st7, 7);
-  }
+  if constexpr (STAGES > 3) fetch(st3, 3);
   wait_and_meet<(STAGES - 1) * LOADS>();
   operands(st0, fa[0], fb[0]);
   scales(sc0);
   // Step s: its operands are in fa[B & 1], fb[B & 1], its scales byte B of sa and sb.  sc_own: the scales of this step's four, whose place is free while they
   // are multiplied; sc_next: those of the next.
-  auto step = [&](auto byte, int s, uint4* own, uint4* next, unsigned* sc_own, unsigned* sc_next) __attribute__((always_inline)) {
+  auto step = [&](auto byte, int s, uint4* own, uint4* next) __attribute__((always_inline)) {
     constexpr int B = decltype(byte)::value;
     wait_and_meet<(STAGES - 2) * LOADS>();      // the codes of s + 1 are there (later ones may be under way), and nobody reads `own` any more
-    if (B == 0) fetch_scales(sc_own, s / 4 + STAGES / 4);      // (ahead of the codes of s + STAGES: there when those are, a step before they are read)
+    if (B == 0) fetch_scales(sc0, s / 4 + 1);      // (ahead of the codes of s + STAGES: there when those are, a step before they are read)
     fetch(own, s + STAGES);
     operands(next, fa[(B + 1) & 1], fb[(B + 1) & 1]);
 #pragma unroll
@@ -499,7 +489,7 @@ __global__ __launch_bounds__(256) void mx4_tile_kernel(const Mx4Args p) {
       if (q < LOADS) __builtin_amdgcn_sched_group_barrier(0x20, 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x8, M * N > M + N ? M * N / (M + N) : 1, 0);
     }
-    if (B == 3) scales(sc_next);
+    if (B == 3) scales(sc0);
     asm volatile("" ::: "memory");      // (the reads above belong to this turn of the loop)
   };
   typedef std::integral_constant<int, 0> byte0;
@@ -510,30 +500,29 @@ __global__ __launch_bounds__(256) void mx4_tile_kernel(const Mx4Args p) {
     // (One way out of the loop where the sums fill half the registers: with an exit behind each step they are copied at every turn.  The steps that fill up
     // the last four multiply zeros.)
     for (int s = 0;; s += 4) {
-      step(byte0(), s, st0, st1, sc0, sc0);
-      step(byte1(), s + 1, st1, st2, sc0, sc0);
-      step(byte2(), s + 2, st2, st3, sc0, sc0);
-      step(byte3(), s + 3, st3, st0, sc0, sc0);
+      step(byte0(), s, st0, st1);
+      step(byte1(), s + 1, st1, st2);
+      step(byte2(), s + 2, st2, st3);
+      step(byte3(), s + 3, st3, st0);
       if (s + 4 >= steps) break;
     }
   } else {
-    for (int s = 0;; s += 8) {
-      step(byte0(), s, st0, st1, sc0, sc1);
-      if (s + 1 >= steps) break;
-      step(byte1(), s + 1, st1, st2, sc0, sc1);
-      if (s + 2 >= steps) break;
-      step(byte2(), s + 2, st2, st3, sc0, sc1);
-      if (s + 3 >= steps) break;
-      step(byte3(), s + 3, st3, st4, sc0, sc1);
+    for (int s = 0;; s += 12) {
+      step(byte0(), s, st0, st1);
+      step(byte1(), s + 1, st1, st2);
+      step(byte2(), s + 2, st2, st0);
+      step(byte3(), s + 3, st0, st1);
       if (s + 4 >= steps) break;
-      step(byte0(), s + 4, st4, st5, sc1, sc0);
-      if (s + 5 >= steps) break;
-      step(byte1(), s + 5, st5, st6, sc1, sc0);
-      if (s + 6 >= steps) break;
-      step(byte2(), s + 6, st6, st7, sc1, sc0);
-      if (s + 7 >= steps) break;
-      step(byte3(), s + 7, st7, st0, sc1, sc0);
+      step(byte0(), s + 4, st1, st2);
+      step(byte1(), s + 5, st2, st0);
+      step(byte2(), s + 6, st0, st1);
+      step(byte3(), s + 7, st1, st2);
       if (s + 8 >= steps) break;
+      step(byte0(), s + 8, st2, st0);
+      step(byte1(), s + 9, st0, st1);
+      step(byte2(), s + 10, st1, st2);
+      step(byte3(), s + 11, st2, st0);
+      if (s + 12 >= steps) break;
     }
   }
 
@@ -548,8 +537,9 @@ __global__ __launch_bounds__(256) void mx4_tile_kernel(const Mx4Args p) {
   wait_and_meet<0>();
   constexpr int W = 16 / (int)sizeof(T);                    // numbers of a piece
   constexpr int PIECES = 16 * MI / W;                       // of a row of the wavefront's outputs
-  constexpr int J = N * 32 * PIECES > 2 * AB * 64 ? N / 2 : N;      // 32-row blocks that fit a stage
-  uint4* const mine = wave == 0 ? st0 : wave == 1 ? st1 : wave == 2 ? st2 : st3;
+  constexpr int ROOM = STAGES == 4 ? 2 * AB * 64 : AB * 64;
+  constexpr int J = N * 32 * PIECES > ROOM ? N / 2 : N;      // 32-row blocks that fit
+  uint4* const mine = STAGES == 4 ? (wave == 0 ? st0 : wave == 1 ? st1 : wave == 2 ? st2 : st3) : (wave < 2 ? st0 : st1) + (wave & 1) * ROOM;
   int l = threadIdx.x & 63;
   asm volatile("" : "+v"(l));      // (what follows from it is worked out here and not held through the loop, where there is no register for it)
   const int o = o0 + wm * 16 * MI, row = l & 31, first = (l >> 5) * (8 * MI / W);

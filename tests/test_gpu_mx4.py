@@ -247,3 +247,28 @@ def test_few_rows_of_long_and_odd_sums(rows, k, c_out, dtype):
     wc, ws = B.cprune_mx4_quantize(w)
     y = B.cprune_mx4_linear(x, wc, ws)
     product_check(y, decode(*encode(np64(x)), k), decode(*encode(np64(w)), k), None, B.ACT_NONE, dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,k,c_out", [(8200, 4100, 8000), (1300, 700, 2000), (2050, 70, 2500), (700, 5000, 600)])
+def test_products_of_many_tiles(rows, k, c_out, dtype):
+    """Tiles of every width, all outputs against a product in 64 bits."""
+    def codes_of(n, seed):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        blocks = -(-k // 32)
+        codes = torch.randint(0, 256, (n, blocks * 16), generator=g, device="cuda", dtype=torch.uint8)
+        scales = torch.randint(120, 126, (n, blocks), generator=g, device="cuda", dtype=torch.uint8)
+        four = torch.stack([codes & 15, codes >> 4], dim=2).reshape(n, -1)
+        four[:, k:] = 0
+        packed = (four[:, 0::2] | four[:, 1::2] << 4).contiguous()
+        table = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6], dtype=torch.float64, device="cuda")
+        v = torch.where(four > 7, -1.0, 1.0).double() * table[(four & 7).int()] * torch.exp2(scales.double() - 127).repeat_interleave(32, dim=1)
+        return packed, scales, v[:, :k].contiguous()
+    xc, xs, xv = codes_of(rows, 1)
+    wc, ws, wv = codes_of(c_out, 2)
+    bias = torch.randn(c_out, generator=torch.Generator().manual_seed(3)).cuda()
+    y = B.cprune_mx4_matmul(xc, xs, wc, ws, B.DTYPE_OF_TORCH[dtype], bias).double()
+    wt = wv.t().contiguous()
+    want, size = xv @ wt + bias.double(), xv.abs() @ wt.abs() + bias.double().abs()
+    over = (y - want).abs() - (U[dtype] * want.abs() + (k / 128 + 16) * E24 * size + TINY[dtype])
+    assert over.max().item() <= 0, f"{int((over > 0).sum())} of {over.numel()} past the bound"
