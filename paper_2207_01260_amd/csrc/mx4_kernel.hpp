@@ -215,29 +215,31 @@ struct Weights {
   }
 };
 
-// 4 MB neighbouring outputs of a row from the sums of MB blocks; block i's row 4 g + e is output 4 MB g + 4 i + e of the tile
-template <typename T, bool SILU, int MB> __device__ __forceinline__ void store_outputs(const Mx4Args& p, const float4_t (&v)[MB], const float4_t (&bias)[MB], int r, int o) {
+// The first of the four outputs, counted from the tile's, that block i of MB and lane group g (of four) work out: the groups' 16-byte pieces of a row lie side by
+// side, so that a store covers 64 bytes of it (200704 x 24 x 144 bf16 24.0 -> 22.4 us, 11910 x 23 x 1630 18.6 -> 16.5, against a lane with its outputs in one run).
+template <typename T, int MB> __device__ __forceinline__ int output_of(int i, int g) {
+  constexpr int P = MB > 1 && sizeof(T) == 2 ? 2 : 1;      // blocks of a piece
+  return 16 * P * (i / P) + 4 * P * g + 4 * (i % P);
+}
+// The outputs of lane group g from the sums of MB blocks; o is the tile's first.
+template <typename T, bool SILU, int MB> __device__ __forceinline__ void store_outputs(const Mx4Args& p, const float4_t (&v)[MB], const float4_t (&bias)[MB], int r, int o, int g) {
   if (r >= p.rows) return;
+  constexpr int P = MB > 1 && sizeof(T) == 2 ? 2 : 1, W = 4 * P;      // numbers of a piece
   T* y = static_cast<T*>(p.y) + (long)r * p.c_out + o;
-  T z[4 * MB];
+  typedef T outs __attribute__((ext_vector_type(W), aligned(sizeof(T))));
 #pragma unroll
-  for (int i = 0; i < MB; ++i)
+  for (int h = 0; h < MB; h += P) {
+    outs q;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) z[4 * i + e] = Elem<T>::from_f32(finish<SILU>(v[i][e] + bias[i][e], p.lo, p.hi));
-  if (o + 4 * MB <= p.c_out) {
-    constexpr int W = 4 * MB < 16 / (int)sizeof(T) ? 4 * MB : 16 / (int)sizeof(T);      // numbers a store
-    typedef T outs __attribute__((ext_vector_type(W), aligned(sizeof(T))));
+    for (int e = 0; e < W; ++e) q[e] = Elem<T>::from_f32(finish<SILU>(v[h + e / 4][e & 3] + bias[h + e / 4][e & 3], p.lo, p.hi));
+    const int at = output_of<T, MB>(h, g);
+    if (o + at + W <= p.c_out) {
+      *reinterpret_cast<outs*>(y + at) = q;
+    } else {
 #pragma unroll
-    for (int h = 0; h < 4 * MB; h += W) {
-      outs q;
-#pragma unroll
-      for (int e = 0; e < W; ++e) q[e] = z[h + e];
-      *reinterpret_cast<outs*>(y + h) = q;
+      for (int e = 0; e < W; ++e)
+        if (o + at + e < p.c_out) y[at + e] = q[e];
     }
-  } else {
-#pragma unroll
-    for (int h = 0; h < 4 * MB; ++h)
-      if (o + h < p.c_out) y[h] = z[h];
   }
 }
 
@@ -268,7 +270,7 @@ __global__ __launch_bounds__(64 * WAVES) void mx4_few_kernel(const Mx4Args p) {
     for (int u = 0; u < U; ++u) {
       const int blk = (st + u * WAVES) * 4 + lblk;      // (past the last one: zeros)
 #pragma unroll
-      for (int i = 0; i < MB; ++i) w.load(o0 + 4 * MB * (lrow >> 2) + 4 * i + (lrow & 3), blk, a[u][i], as[u][i]);
+      for (int i = 0; i < MB; ++i) w.load(o0 + output_of<T, MB>(i, lrow >> 2) + (lrow & 3), blk, a[u][i], as[u][i]);
 #pragma unroll
       for (int j = 0; j < NB; ++j) x.load(rows[u][j], r0 + 16 * j + lrow, blk);
     }
@@ -292,17 +294,16 @@ __global__ __launch_bounds__(64 * WAVES) void mx4_few_kernel(const Mx4Args p) {
   }
   __syncthreads();
   if (wave > 0) return;
-  const int o = o0 + 4 * MB * lblk;
   float4_t bias[MB];
 #pragma unroll
-  for (int i = 0; i < MB; ++i) bias[i] = load_bias4(p.bias, p.c_out, o + 4 * i);
+  for (int i = 0; i < MB; ++i) bias[i] = load_bias4(p.bias, p.c_out, o0 + output_of<T, MB>(i, lblk));
 #pragma unroll
   for (int j = 0; j < NB; ++j) {
 #pragma unroll
     for (int i = 0; i < MB; ++i)
 #pragma unroll
       for (int q = 0; q < WAVES - 1; ++q) acc[j][i] += sums[q][j * MB + i][lane];
-    store_outputs<T, SILU, MB>(p, acc[j], bias, r0 + 16 * j + lrow, o);
+    store_outputs<T, SILU, MB>(p, acc[j], bias, r0 + 16 * j + lrow, o0, lblk);
   }
 }
 
@@ -328,10 +329,9 @@ __global__ __launch_bounds__(256) void mx4_rows_kernel(const Mx4Args p) {
     for (int st = 0; st < STEPS; ++st) rows[st].operand(b[j][st], bs[j][st]);
   }
   for (int o0 = (int)blockIdx.y * 16 * MB; o0 < p.c_out; o0 += (int)gridDim.y * 16 * MB) {
-    const int o = o0 + 4 * MB * lblk;
-    float4_t bias[MB], acc[NB][MB];
+      float4_t bias[MB], acc[NB][MB];
 #pragma unroll
-    for (int i = 0; i < MB; ++i) bias[i] = load_bias4(p.bias, p.c_out, o + 4 * i);
+    for (int i = 0; i < MB; ++i) bias[i] = load_bias4(p.bias, p.c_out, o0 + output_of<T, MB>(i, lblk));
 #pragma unroll
     for (int j = 0; j < NB; ++j)
 #pragma unroll
@@ -341,14 +341,14 @@ __global__ __launch_bounds__(256) void mx4_rows_kernel(const Mx4Args p) {
       uint4 a[MB];
       int as[MB];
 #pragma unroll
-      for (int i = 0; i < MB; ++i) w.load(o0 + 4 * MB * (lrow >> 2) + 4 * i + (lrow & 3), st * 4 + lblk, a[i], as[i]);
+      for (int i = 0; i < MB; ++i) w.load(o0 + output_of<T, MB>(i, lrow >> 2) + (lrow & 3), st * 4 + lblk, a[i], as[i]);
 #pragma unroll
       for (int j = 0; j < NB; ++j)
 #pragma unroll
         for (int i = 0; i < MB; ++i) acc[j][i] = mma(a[i], as[i], b[j][st], bs[j][st], acc[j][i]);
     }
 #pragma unroll
-    for (int j = 0; j < NB; ++j) store_outputs<T, SILU, MB>(p, acc[j], bias, r0 + 16 * j + lrow, o);
+    for (int j = 0; j < NB; ++j) store_outputs<T, SILU, MB>(p, acc[j], bias, r0 + 16 * j + lrow, o0, lblk);
   }
 }
 
