@@ -56,7 +56,7 @@ template <typename F> __device__ __forceinline__ double2 entries_sum(const NormA
   return s;
 }
 
-// The chunks' statistics as those of an (image, group).
+// The chunks' statistics as those of an (image, group), where a superrow is wider than a work-group and groups are many.
 __global__ __launch_bounds__(1024) void norm_join_stats_kernel(const NormArgs a, float* __restrict__ mean_out, float* __restrict__ rstd_out) {
   const int image = blockIdx.x / (unsigned)a.groups, group = blockIdx.x - image * a.groups;
   const float2* part = a.part + (long)image * a.g.chunks * a.g.R * a.c + group * a.cg;
@@ -70,7 +70,7 @@ __global__ __launch_bounds__(1024) void norm_join_stats_kernel(const NormArgs a,
   }
 }
 
-// The two means of an (image, group).
+// The two means of an (image, group), likewise.
 __global__ __launch_bounds__(1024) void norm_join_grads_kernel(const NormArgs a, float2* __restrict__ terms) {
   const int image = blockIdx.x / (unsigned)a.groups, group = blockIdx.x - image * a.groups;
   const float2* part = a.part + (long)image * a.g.chunks * a.g.R * a.c + group * a.cg;
