@@ -3,7 +3,8 @@
  * pruning: L1-norm filter ranking, weight / activation channel gather with
  * batch-norm folding, MFMA implicit-GEMM convolution with fused bias,
  * residual and activation, the memory-bound layers around it, per-shape kernel
- * variant selection by timing on the device, and whole-network inference.
+ * variant selection by timing on the device, and whole-network inference; beside them
+ * a channels-last group norm with its gradient and products of 4-bit numbers.
  *
  * Conventions for every call
  *   - Returns an int status: CPRUNE_OK (0) or a negative CPRUNE_ERR_* code.  On an
