@@ -695,27 +695,25 @@ __global__ __launch_bounds__(norm::kThreads, 4) void norm_grad_sums_kernel(const
 
 // dweight and dbias of eight channels from all images' partial sums, `per` rows of c of them an image; 32 threads a channel, 64 bits, a fixed order.
 __device__ inline void norm_vector_sums(const NormArgs& a, unsigned block, long count) {
-  __shared__ double2 sums[32][8];
-  const int ch = (int)block * 8 + ((int)threadIdx.x & 7), lane = (int)threadIdx.x >> 3;
+  __shared__ double2 waves[norm::kThreads / 64][8];
+  const int t = (int)threadIdx.x, ch = (int)block * 8 + (t & 7), lane = t >> 3;
   double2 s = {0.0, 0.0};
   if (ch < a.c) {
-    long i = lane;
-    for (; i + 7 * 32 < count; i += 8 * 32) {
+    for (long i = lane; i < count; i += 8 * 32) {
       float2 p[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) p[u] = a.part[(i + u * 32) * a.c + ch];
+      for (int u = 0; u < 8; ++u) p[u] = a.part[min(i + u * 32, count - 1) * a.c + ch];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) s.x += p[u].x, s.y += p[u].y;
-    }
-    for (; i < count; i += 32) {
-      const float2 p = a.part[i * a.c + ch];
-      s.x += p.x, s.y += p.y;
+      for (int u = 0; u < 8; ++u)
+        if (i + u * 32 < count) s.x += p[u].x, s.y += p[u].y;
     }
   }
-  sums[lane][threadIdx.x & 7] = s;
+#pragma unroll
+  for (int o = 8; o < 64; o *= 2) s.x += __shfl_xor(s.x, o, 64), s.y += __shfl_xor(s.y, o, 64);
+  if ((t & 63) < 8) waves[t >> 6][t & 7] = s;
   __syncthreads();
-  if (lane == 0 && ch < a.c) {
-    for (int i = 1; i < 32; ++i) s.x += sums[i][threadIdx.x].x, s.y += sums[i][threadIdx.x].y;
+  if (t < 8 && ch < a.c) {
+    for (int i = 1; i < norm::kThreads / 64; ++i) s.x += waves[i][t].x, s.y += waves[i][t].y;
     if (a.dbias) a.dbias[ch] = (float)s.x;
     if (a.dweight) a.dweight[ch] = (float)s.y;
   }
