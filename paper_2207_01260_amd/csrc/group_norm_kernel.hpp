@@ -240,19 +240,40 @@ template <int V> __device__ __forceinline__ Where<V> where(const NormArgs& a, in
 template <int V> struct Terms {
   float mean[V], rstd[V], w[V], b[V];
 };
-template <int V> __device__ __forceinline__ void channel_terms(const NormArgs& a, const Where<V>& at, Terms<V>& k) {
+// A vector's channels follow each other, unless a superrow's next pixel begins in it: their terms are 16-byte loads, one each for what a group shares.  (A load of
+// each by itself, 32 of them for eight elements, is a microsecond or two of a work-group.)
+template <int V> __device__ __forceinline__ void channel_values(const float* from, float without, const Where<V>& at, float (&v)[V]) {
+  if (!from) {
 #pragma unroll
-  for (int j = 0; j < V; ++j) {
-    k.w[j] = a.weight ? a.weight[at.ch[j]] : 1.0f;
-    k.b[j] = a.bias ? a.bias[at.ch[j]] : 0.0f;
+    for (int j = 0; j < V; ++j) v[j] = without;
+  } else if (at.ch[V - 1] - at.ch[0] == V - 1) {
+    constexpr int W = V < 4 ? V : 4;
+    typedef typename RawOf<float, W>::type Some;
+#pragma unroll
+    for (int h = 0; h < V; h += W) {
+      const Some q = *reinterpret_cast<const Some*>(from + at.ch[0] + h);
+#pragma unroll
+      for (int j = 0; j < W; ++j) v[h + j] = q[j];
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[j] = from[at.ch[j]];
   }
+}
+template <int V> __device__ __forceinline__ void channel_terms(const NormArgs& a, const Where<V>& at, Terms<V>& k) {
+  channel_values<V>(a.weight, 1.0f, at, k.w);
+  channel_values<V>(a.bias, 0.0f, at, k.b);
 }
 template <int V> __device__ __forceinline__ void all_terms(const NormArgs& a, int image, const Where<V>& at, Terms<V>& k) {
   channel_terms<V>(a, at, k);
+  const float *const mean = a.mean + image * a.groups, *const rstd = a.rstd + image * a.groups;
+  if (at.group[V - 1] == at.group[0] && at.ch[V - 1] >= at.ch[0]) {
+    const float m = mean[at.group[0]], r = rstd[at.group[0]];
 #pragma unroll
-  for (int j = 0; j < V; ++j) {
-    k.mean[j] = a.mean[image * a.groups + at.group[j]];
-    k.rstd[j] = a.rstd[image * a.groups + at.group[j]];
+    for (int j = 0; j < V; ++j) k.mean[j] = m, k.rstd[j] = r;
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j) k.mean[j] = mean[at.group[j]], k.rstd[j] = rstd[at.group[j]];
   }
 }
 
