@@ -138,8 +138,15 @@ bool choose_whole(const cprune_norm_desc& d, bool backward, NormGeom& g) {
     if (times % k == 0 && (long)least * k * 16 <= 128 && (long)d.n * (times / k) >= 256 && fit_whole(g, least * k, cg, backward, most_threads, most_vectors)) return true;
   // A compute unit alone brings some 10 to 20 GB/s from memory: the gradient of few and large slabs is split (27 x 7 x 22 x 111 fp16, 34 KB and 27 of them, 18.8 us
   // whole, 13.1 split; but 6 x 20 x 15 x 608 fp32, 114 of them, 10.3 and 13.5, and one of 11 KB, 7 x 99 x 16, 6.6 and 10.0).
-  if (backward && (double)least * g.SR * 16 > 20000.0 && (long)d.n * times < 64) return false;
-  return fit_whole(g, least, cg, backward, most_threads, most_vectors);
+  const double slab = (double)least * g.SR * 16;
+  const long slabs = (long)d.n * times;
+  if (backward && slab > 20000.0 && slabs < 64) return false;
+  // (forward only where a thread's numbers are of several groups, whose sums take longer here: 20 x 67 x 9 x 98 fp16, 20 of 118 KB, 17.7 whole, 11.8 split; 13 x 38 x 30 x 160,
+  // 52 of 91 KB, 10.8 and 13.1)
+  if (!backward && !merge && slab > 65536.0 && slabs < 32) return false;
+  if (!fit_whole(g, least, cg, backward, most_threads, most_vectors)) return false;
+  // (the gradient's fullest form spills registers: not for more than one round of it, 31 x 108 x 10 x 800 bf16 62 whole, 50 split)
+  return !(backward && g.nv > 4 && slabs > 256);
 }
 
 // Split form: the work-groups that read x leave sums of groups, and those that read it again join them.  Not where each of many work-groups beside each other

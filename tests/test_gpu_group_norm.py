@@ -288,3 +288,10 @@ def test_forms(shape, dtype):
     forward_check(shape, dtype, 5, B.ACT_RELU, False)
     backward_check(shape, dtype, 0, B.ACT_SILU, True)
     backward_check(shape, dtype, 5, B.ACT_NONE, False)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", [(20, 67, 9, 98, 49), (31, 108, 10, 80, 4), (13, 38, 30, 160, 16)])
+def test_forms_of_large_slabs(shape, dtype):
+    forward_check(shape, dtype, 0, B.ACT_SILU, True)
+    backward_check(shape, dtype, 0, B.ACT_SILU, True)
