@@ -427,7 +427,7 @@ __device__ __forceinline__ double2 group_terms(const NormArgs& a, const float2* 
 
 // Statistics of a chunk: each thread's running mean and squares about it, four numbers at a time about their own mean (no difference of large sums, whatever
 // the numbers' mean), then joined over the work-group's superrows pair by pair, and as sums of groups in 64 bits.  Bound by memory on large maps: 64 x 112 x 112
-// x 96 fp16, 154 MB read, 30.2 us, 5.1 TB/s; on small ones by the chain load, sum, LDS, store (1 x 112 x 112 x 96 some 6 us).
+// x 96 fp16, 154 MB read, 29.7 us, 5.2 TB/s; on small ones by the chain load, sum, LDS, store (1 x 112 x 112 x 96 some 6 us).
 template <typename T, int V>
 __global__ __launch_bounds__(norm::kThreads, 4) void norm_stats_kernel(const NormArgs a) {
   using namespace norm;
@@ -552,7 +552,7 @@ __global__ __launch_bounds__(norm::kThreads, 4) void norm_stats_kernel(const Nor
 }
 
 // The second pass: an image's statistics from its work-groups' sums (each work-group for itself: a launch between costs more than reading some KB again), then y.
-// Its first loads are under way meanwhile.  64 x 112 x 112 x 96 fp16, 308 MB read and written, 58.5 us, 5.3 TB/s.
+// Its first loads are under way meanwhile.  64 x 112 x 112 x 96 fp16, 308 MB read and written, 56.6 us, 5.4 TB/s.
 template <typename T, int V, bool SILU, bool STREAM>
 __global__ __launch_bounds__(norm::kThreads, 4) void norm_apply_kernel(const NormArgs a) {
   using namespace norm;
@@ -633,7 +633,7 @@ __global__ __launch_bounds__(norm::kThreads, 4) void norm_apply_kernel(const Nor
 }
 
 // Sums of dz and dz xhat over a chunk; the activation's argument is worked out again from x, which costs less than a map of it.  64 x 56 x 56 x 144 fp16, 116 MB
-// read, 24.2 us, 4.8 TB/s.
+// read, 22.1 us, 5.2 TB/s.
 template <typename T, int V, bool SILU>
 __global__ __launch_bounds__(norm::kThreads, 4) void norm_grad_sums_kernel(const NormArgs a) {
   using namespace norm;
@@ -743,7 +743,7 @@ __device__ inline void norm_vector_sums(const NormArgs& a, unsigned block, long 
 __global__ __launch_bounds__(norm::kThreads) inline void norm_vectors_kernel(const NormArgs a) { norm_vector_sums(a, blockIdx.x, a.n); }
 
 // The first `vector_groups` work-groups sum dweight and dbias (few numbers, long chains: beside the others they cost nothing), the others dx from x and dy again.
-// 64 x 56 x 56 x 144 fp16, 173 MB, 31.1 us, 5.6 TB/s.
+// 64 x 56 x 56 x 144 fp16, 173 MB, 29.2 us, 5.9 TB/s.
 template <typename T, int V, bool SILU, bool STREAM>
 __global__ __launch_bounds__(norm::kThreads, 4) void norm_grad_apply_kernel(const NormArgs a, unsigned vector_groups) {
   using namespace norm;
@@ -822,7 +822,7 @@ __global__ __launch_bounds__(norm::kThreads, 4) void norm_grad_apply_kernel(cons
 
 // ---- whole form ----------------------------------------------------------------------------------
 // V numbers are 16 bytes; a thread holds NV vectors.  x is read once and y follows from registers; statistics are of the numbers about each thread's own mean, joined
-// through LDS.  Bound by that chain, one work-group or two a compute unit: 32 x 56 x 56 x 64 bf16, 26 MB, 15.0 us (in two passes 18.7), 1 x 14 x 14 x 96 fp32 5.0 us.
+// through LDS.  Bound by that chain, one work-group or two a compute unit: 32 x 56 x 56 x 64 bf16, 26 MB, 15.1 us (in two passes 18.7), 1 x 14 x 14 x 96 fp32 4.9 us.
 
 // What holds of the slab's layout, known when the kernel is built: kMerge, V divides a group's channels, so a thread's numbers are of one group; kTail, the last superrow lacks pixels.
 enum NormSlab { kPlain, kMerge, kTail };
@@ -940,8 +940,8 @@ __global__ __launch_bounds__(1024) void norm_whole_kernel(const NormArgs a) {
     if (i < rows) normalise<T, V, SILU, STREAM>(a, raw[i], c, out + i * out_step, i == rows - 1 ? last : V);
 }
 
-// The gradient; dweight and dbias go to `part` [n][c] as an image's sums (or straight to their place where there is one image).  32 x 14 x 14 x 576 bf16, 22 MB, 13.4 us
-// and the launch that sums the images' vectors 3.9.
+// The gradient; dweight and dbias go to `part` [n][c] as an image's sums (or straight to their place where there is one image).  32 x 14 x 14 x 576 bf16, 22 MB, 12.8 us
+// and the launch that sums the images' vectors 3.8.
 template <typename T, int NV, int SLAB, bool SILU>
 __global__ __launch_bounds__(1024) void norm_whole_grad_kernel(const NormArgs a) {
   using namespace norm;

@@ -359,7 +359,7 @@ __global__ __launch_bounds__(256) void mx4_rows_kernel(const Mx4Args p) {
 // of one step in operand order, [16-row block][lane][16 bytes], as a launch before has laid them out in memory: a step of a tile is one run of memory, so its
 // loads spread over all channels of the L2 (rows of 2^n bytes read side by side would meet in one), and they write to LDS themselves.
 // While step s is multiplied, the operands of s + 1 go to registers and the codes of s + STAGES into the stage that s has left.
-// 16384 x 8192 x 8192 from operands in place: 525 us, 4.2 PFLOP/s, tiles of 256.  The matrix pipes are busy 58 % of the clocks, and the clock itself is down: the same
+// 16384 x 8192 x 8192 from operands in place: 504 to 525 us, 4.2 to 4.4 PFLOP/s, tiles of 256.  The matrix pipes are busy 58 % of the clocks, and the clock itself is down: the same
 // instructions on codes that are all zero take a fifth less.  The rest is a tile's first loads and last stores, some 14 us of 65 a round.
 // The matrix instruction takes 32 rows of each side; those of a wavefront's c_out are dealt so that a lane's results are 8 MI neighbours of one row of y.
 namespace mx4 {
