@@ -267,7 +267,7 @@ template <int V> __device__ __forceinline__ void channel_terms(const NormArgs& a
 template <int V> __device__ __forceinline__ void all_terms(const NormArgs& a, int image, const Where<V>& at, Terms<V>& k) {
   channel_terms<V>(a, at, k);
   const float *const mean = a.mean + image * a.groups, *const rstd = a.rstd + image * a.groups;
-  if (at.group[V - 1] == at.group[0] && at.ch[V - 1] >= at.ch[0]) {
+  if (at.group[V - 1] == at.group[0] && at.ch[V - 1] - at.ch[0] == V - 1) {      // (past a pixel's end the last may be of the first one's group again, others between)
     const float m = mean[at.group[0]], r = rstd[at.group[0]];
 #pragma unroll
     for (int j = 0; j < V; ++j) k.mean[j] = m, k.rstd[j] = r;

@@ -295,3 +295,11 @@ def test_forms(shape, dtype):
 def test_forms_of_large_slabs(shape, dtype):
     forward_check(shape, dtype, 0, B.ACT_SILU, True)
     backward_check(shape, dtype, 0, B.ACT_SILU, True)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", [(2, 10, 109, 3, 3), (2, 9, 13, 7, 7), (3, 11, 5, 6, 3), (2, 40, 41, 9, 3), (1, 300, 301, 3, 3), (1, 200, 301, 7, 7)])
+def test_vectors_that_end_in_their_first_group_again(shape, dtype):
+    """Fewer channels than a vector has, or one less than it takes to come back: first and last element of one group, others between."""
+    forward_check(shape, dtype, 0, B.ACT_SILU, True)
+    backward_check(shape, dtype, 0, B.ACT_SILU, True)
