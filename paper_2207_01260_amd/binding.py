@@ -483,6 +483,9 @@ def _refuse(what: str) -> None:
     raise ValueError(what)
 
 
+_MOST = 0x7fffffff      # elements of a tensor, with the gaps between its rows; ctypes cuts a larger number down to 32 bits without a word
+
+
 def _rows_of(x: torch.Tensor, image_dims: int):
     """(product of the first `image_dims` sizes, product of those between, channels, elements between pixels) of a channels-last tensor whose
     pixels lie evenly: dense, or the first channels of a wider dense tensor."""
@@ -491,6 +494,8 @@ def _rows_of(x: torch.Tensor, image_dims: int):
     lead = math.prod(shape[:image_dims])
     pixels = math.prod(shape[image_dims:-1])
     if x.is_contiguous():
+        if lead * pixels * c > _MOST:
+            _refuse("fewer than 2^31 elements only")
         return lead, pixels, c, c
     if c != 1 and x.stride(-1) != 1:
         _refuse("channels must lie next to each other")
@@ -508,6 +513,8 @@ def _rows_of(x: torch.Tensor, image_dims: int):
         pitch = c
     if pitch < c:
         _refuse("pixels must not overlap")
+    if lead * pixels * pitch > _MOST:
+        _refuse("fewer than 2^31 elements only, gaps between rows counted")
     return lead, pixels, c, pitch
 
 
@@ -533,6 +540,8 @@ def _norm_desc(x: torch.Tensor, groups: int, act: int, eps: float):
     dtype = DTYPE_OF_TORCH.get(x.dtype)
     if dtype is None:
         _refuse(f"no {x.dtype}")
+    if groups > _MOST:
+        _refuse(f"no {groups} groups")
     n, pixels, c, pitch = _rows_of(x, 1)
     return NormDesc(n, pixels, c, groups, dtype, act, pitch, c, eps)
 
@@ -617,6 +626,8 @@ def _mx4_pair(codes: torch.Tensor, scales: torch.Tensor, k: Optional[int]):
     if scales.dim() != 2:
         _refuse("codes [rows, blocks * 16], scales [rows, blocks]")
     rows, blocks = shape = scales.shape
+    if 32 * rows * blocks > _MOST:
+        _refuse("fewer than 2^31 numbers only")
     if k is not None and blocks != (k + 31) // 32:
         _refuse(f"{blocks} blocks do not hold {k} numbers a row")
     return _on_gpu(codes, torch.uint8, (rows, 16 * blocks)), _on_gpu(scales, torch.uint8, shape), rows, blocks
