@@ -160,7 +160,7 @@ NormGeom geometry(const cprune_norm_desc& d, bool backward) {
   g.V = vector_of(d.c, d.dtype, dense);
   g.R = g.V / std::gcd(g.V, d.c);
   g.P = (int)((long)g.R * d.c / g.V);
-  g.SR = (d.pixels + g.R - 1) / g.R;
+  g.SR = (int)(((long)d.pixels + g.R - 1) / g.R);
   g.tail = d.pixels - (g.SR - 1) * g.R;
   g.tiles = g.chunks = 1;
   if (choose_whole(d, backward, g)) return g;
@@ -198,11 +198,17 @@ int check(const cprune_norm_desc* d, bool backward) {
   return CPRUNE_OK;
 }
 
-// (a launch holds fewer than 2^32 threads)
-bool too_many_groups(const cprune_norm_desc& d, const NormGeom& g) {
-  const double launch = g.nv ? (double)d.n * g.slabs * g.threads
-                             : std::max((double)d.n * g.chunks * g.tiles + (d.c + 7) / 8, (double)d.n * d.groups * 4) * norm::kThreads;
-  return launch >= 4294967296.0;
+// A launch holds fewer than 2^32 threads, and places in a superrow are counted in 32 bits.
+bool fits(const cprune_norm_desc& d, const NormGeom& g, bool backward) {
+  const double vectors = ((long)d.c + 7) / 8;      // work-groups for dweight and dbias
+  if (g.nv) return std::max((double)d.n * g.slabs * g.threads, backward && d.n > 1 ? vectors * norm::kThreads : 0.0) < 4294967296.0;
+  return std::max((double)d.n * g.chunks * g.tiles + vectors, (double)d.n * d.groups * 4) * norm::kThreads < 4294967296.0;
+}
+// The geometry of a call that has passed check(); false where it is more than the launches hold.
+bool plan(const cprune_norm_desc& d, bool backward, NormGeom& g) {
+  if (d.c >= 1 << 27 && d.c % (d.dtype == CPRUNE_F32 ? 4 : 8)) return false;      // (split, so its vectors are too many; a superrow might pass 2^31)
+  g = geometry(d, backward);
+  return fits(d, g, backward);
 }
 
 size_t round16(size_t b) { return (b + 15) & ~(size_t)15; }
@@ -272,8 +278,9 @@ NormLaunch launch_of(const cprune_norm_desc& d, const NormArgs& a, bool backward
 using namespace cprune;
 
 extern "C" size_t cprune_group_norm_workspace_bytes(const cprune_norm_desc* d, int backward) {
-  if (check(d, backward != 0) != CPRUNE_OK) return 0;
-  return scratch_of(*d, geometry(*d, backward != 0), backward != 0).total();
+  NormGeom g;
+  if (check(d, backward != 0) != CPRUNE_OK || !plan(*d, backward != 0, g)) return 0;
+  return scratch_of(*d, g, backward != 0).total();
 }
 
 extern "C" int cprune_group_norm_act(const cprune_norm_desc* d, const void* x, const float* weight, const float* bias, void* y,
@@ -281,8 +288,8 @@ extern "C" int cprune_group_norm_act(const cprune_norm_desc* d, const void* x, c
   const int rc = check(d, false);
   if (rc != CPRUNE_OK) return rc;
   if (!x || !y) return CPRUNE_ERR_INVALID_ARG;
-  const NormGeom g = geometry(*d, false);
-  if (too_many_groups(*d, g)) return CPRUNE_ERR_UNSUPPORTED;
+  NormGeom g;
+  if (!plan(*d, false, g)) return CPRUNE_ERR_UNSUPPORTED;
   const NormScratch q = scratch_of(*d, g, false);
   if (q.total() && (!ws || ws_bytes < q.total())) return CPRUNE_ERR_WORKSPACE;
   if (reinterpret_cast<uintptr_t>(ws) & 15) return CPRUNE_ERR_INVALID_ARG;
@@ -318,8 +325,8 @@ extern "C" int cprune_group_norm_act_backward(const cprune_norm_desc* d, const v
   const int rc = check(d, true);
   if (rc != CPRUNE_OK) return rc;
   if (!dy || !x || !mean || !rstd || !dx) return CPRUNE_ERR_INVALID_ARG;
-  const NormGeom g = geometry(*d, true);
-  if (too_many_groups(*d, g)) return CPRUNE_ERR_UNSUPPORTED;
+  NormGeom g;
+  if (!plan(*d, true, g)) return CPRUNE_ERR_UNSUPPORTED;
   const NormScratch q = scratch_of(*d, g, true);
   if (q.total() && (!ws || ws_bytes < q.total())) return CPRUNE_ERR_WORKSPACE;
   if (reinterpret_cast<uintptr_t>(ws) & 15) return CPRUNE_ERR_INVALID_ARG;

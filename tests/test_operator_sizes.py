@@ -36,3 +36,42 @@ def test_codes_and_groups():
     with pytest.raises(ValueError, match="groups"):
         B._norm_desc(torch.empty(2, 3, 8).as_subclass(OnDevice), 2 ** 32 + 2, 0, 1e-5)
     assert B._norm_desc(torch.empty(2, 3, 8).as_subclass(OnDevice), 2, 0, 1e-5).groups == 2
+
+
+FAKE = 0x1000   # never dereferenced: refused first
+
+
+def _norm(n, pixels, c, groups, dtype=B.F16, stride=None):
+    return B.NormDesc(n, pixels, c, groups, dtype, 0, stride or c, stride or c, 1e-5)
+
+
+def _calls(d):
+    L = B.lib()
+    return (L.cprune_group_norm_act(d, FAKE, None, None, FAKE, None, None, FAKE, 1 << 60, None),
+            L.cprune_group_norm_act_backward(d, FAKE, FAKE, FAKE, FAKE, None, None, FAKE, FAKE, FAKE, FAKE, 1 << 60, None))
+
+
+@pytest.mark.parametrize("dtype", [B.F32, B.F16, B.BF16])
+def test_the_most_pixels_are_counted(dtype):
+    """A superrow of one channel is four or eight pixels: the last ones begin a superrow more."""
+    L = B.lib()
+    for back in (0, 1):
+        whole = L.cprune_group_norm_workspace_bytes(_norm(1, 2 ** 31 - 8, 1, 1, dtype), back)
+        assert whole > 0
+        for pixels in (2 ** 31 - 7, 2 ** 31 - 3, 2 ** 31 - 1):
+            assert L.cprune_group_norm_workspace_bytes(_norm(1, pixels, 1, 1, dtype), back) >= whole
+
+
+@pytest.mark.parametrize("d", [(1, 1, 2 ** 31 - 1, 1), (1, 1, 2 ** 31 - 255, 1), (1, 1, 2 ** 29 + 1, 1), (1, 1, 2 ** 28 + 1, 1), (1, 2, 2 ** 27 + 4, 2)])
+def test_channels_past_what_a_launch_holds(d):
+    """(scratch asked for a call that is refused: 1.8e19 bytes at the first)"""
+    for dtype in (B.F16, B.BF16) + ((B.F32,) if d[2] % 4 else ()):
+        desc = _norm(*d, dtype)
+        assert _calls(desc) == (B.ERR_UNSUPPORTED, B.ERR_UNSUPPORTED)
+        assert B.lib().cprune_group_norm_workspace_bytes(desc, 0) == B.lib().cprune_group_norm_workspace_bytes(desc, 1) == 0
+
+
+def test_gradients_of_too_many_channels_of_several_images():
+    """One launch holds the maps; the one that sums 2^29 channels' vectors over the images would take 2^34 threads."""
+    d = _norm(2, 1, 2 ** 29, 2 ** 26)
+    assert _calls(d)[1] == B.ERR_UNSUPPORTED and B.lib().cprune_group_norm_workspace_bytes(d, 1) == 0
