@@ -516,8 +516,8 @@ int cprune_search_destroy(cprune_search* s);
  * dy             as x, with dy_stride
  * dweight, dbias fp32 [c], each may be NULL.  Summed in a fixed order: repeated calls give identical bits.
  * ws             cprune_group_norm_workspace_bytes(...) of scratch, 16-byte aligned; NULL where that is 0
- * n, pixels >= 1; groups divides c; eps > 0 and finite.  More than a launch holds, from some 2^22 (image, group) pairs
- *                or 2^27 channels on: CPRUNE_ERR_UNSUPPORTED, and a workspace of 0. */
+ * n, pixels >= 1; groups divides c; eps > 0 and finite.  More than a launch holds, from some 2^24 images, 2^27
+ *                channels or, past 2048 channels, 2^22 (image, group) pairs on: CPRUNE_ERR_UNSUPPORTED, and a workspace of 0. */
 typedef struct {
   int32_t n, pixels, c, groups;
   int32_t dtype; /* cprune_dtype of x, y, dy, dx */

@@ -82,8 +82,8 @@ __global__ __launch_bounds__(1024) void norm_join_grads_kernel(const NormArgs a,
 }
 
 // threads of those: four entries each or more, 64 to 1024
-int join_threads(const NormArgs& a) {
-  const long entries = (long)a.g.chunks * a.g.R * a.cg;
+int join_threads(const NormGeom& g, int cg) {
+  const long entries = (long)g.chunks * g.R * cg;
   int t = 64;
   while (t < 1024 && 4L * t < entries) t *= 2;
   return t;
@@ -202,7 +202,8 @@ int check(const cprune_norm_desc* d, bool backward) {
 bool fits(const cprune_norm_desc& d, const NormGeom& g, bool backward) {
   const double vectors = ((long)d.c + 7) / 8;      // work-groups for dweight and dbias
   if (g.nv) return std::max((double)d.n * g.slabs * g.threads, backward && d.n > 1 ? vectors * norm::kThreads : 0.0) < 4294967296.0;
-  return std::max((double)d.n * g.chunks * g.tiles + vectors, (double)d.n * d.groups * 4) * norm::kThreads < 4294967296.0;
+  const double join = sums_groups(d, g) ? 0.0 : (double)d.n * d.groups * join_threads(g, d.c / d.groups);
+  return std::max(((double)d.n * g.chunks * g.tiles + vectors) * norm::kThreads, join) < 4294967296.0;
 }
 // The geometry of a call that has passed check(); false where it is more than the launches hold.
 bool plan(const cprune_norm_desc& d, bool backward, NormGeom& g) {
@@ -312,7 +313,7 @@ extern "C" int cprune_group_norm_act(const cprune_norm_desc* d, const void* x, c
     float* rstd = rstd_out ? rstd_out : stats + (size_t)d->n * d->groups;
     a.mean = mean, a.rstd = rstd;
     launch(d->dtype, kNormStats, a, l, s);
-    norm_join_stats_kernel<<<d->n * d->groups, join_threads(a), 0, s>>>(a, mean, rstd);
+    norm_join_stats_kernel<<<d->n * d->groups, join_threads(g, a.cg), 0, s>>>(a, mean, rstd);
     launch(d->dtype, kNormApply, a, l, s);
   }
   CPRUNE_LAUNCH_CHECK();
@@ -345,7 +346,7 @@ extern "C" int cprune_group_norm_act_backward(const cprune_norm_desc* d, const v
     if (q.gpart) a.gpart = reinterpret_cast<double2*>(behind);
     a.terms = terms;
     launch(d->dtype, kNormGradSums, a, l, s);
-    if (!q.gpart) norm_join_grads_kernel<<<d->n * d->groups, join_threads(a), 0, s>>>(a, terms);
+    if (!q.gpart) norm_join_grads_kernel<<<d->n * d->groups, join_threads(g, a.cg), 0, s>>>(a, terms);
     launch(d->dtype, kNormGradApply, a, l, s);
   }
   CPRUNE_LAUNCH_CHECK();

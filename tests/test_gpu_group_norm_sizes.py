@@ -38,3 +38,25 @@ def test_the_most_pixels():
         assert bool(((y[0, s].double() - want).abs() <= 2.0 ** -11 * want.abs() + 1e-5).all())
         want = r * (1.5 * dy[0, s].double() - t1 - xhat * t2)
         assert bool(((dx[0, s].double() - want).abs() <= 2.0 ** -11 * want.abs() + 1e-5).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,p,c,groups,stride", [(2 ** 22, 1, 3, 1, 4), (2 ** 21, 2, 3, 3, 4)])
+def test_many_images_of_the_first_channels(n, p, c, groups, stride, dtype):
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x, dy = (torch.randn(n, p, stride, generator=g, device="cuda").to(dtype)[..., :c] for _ in range(2))
+    y, mean, rstd = B.cprune_group_norm_act(x, groups, eps=1.0, want_stats=True)
+    dx, dweight, dbias = B.cprune_group_norm_act_backward(dy, x, mean, rstd, groups)
+    x64, d = x.double().reshape(n, p, groups, -1), dy.double().reshape(n, p, groups, -1)
+    m64 = x64.mean(dim=(1, 3), keepdim=True)
+    r64 = ((x64 - m64).square().mean(dim=(1, 3), keepdim=True) + 1.0) ** -0.5
+    xhat = (x64 - m64) * r64
+    u = 2.0 ** -24 if dtype == torch.float32 else 2.0 ** -8
+    # (groups of two or three numbers, eps 1: every term is of order one, and some 32 roundings of them)
+    for got, want in ((mean, m64), (rstd, r64), (y, xhat), (dx, r64 * (d - d.mean(dim=(1, 3), keepdim=True) - xhat * (d * xhat).mean(dim=(1, 3), keepdim=True)))):
+        want = want.reshape(got.shape)
+        slack = 32 * E * (1 + x64.abs().amax()) * (1 + d.abs().amax())
+        assert bool(((got.double() - want).abs() <= (u if got.dtype == dtype else E) * want.abs() + slack).all())
+    for got, v in ((dbias, d), (dweight, d * xhat)):
+        v = v.reshape(n * p, c)
+        assert bool(((got.double() - v.sum(dim=0)).abs() <= 64 * E * (1 + v.abs()).sum(dim=0)).all())

@@ -75,3 +75,10 @@ def test_gradients_of_too_many_channels_of_several_images():
     """One launch holds the maps; the one that sums 2^29 channels' vectors over the images would take 2^34 threads."""
     d = _norm(2, 1, 2 ** 29, 2 ** 26)
     assert _calls(d)[1] == B.ERR_UNSUPPORTED and B.lib().cprune_group_norm_workspace_bytes(d, 1) == 0
+
+
+@pytest.mark.parametrize("d", [(2 ** 22, 1, 3, 1, B.F16, 4), (2 ** 21, 2, 3, 3, B.F32, 4), (2 ** 17, 1, 63, 63, B.BF16, 64)])
+def test_many_images_of_few_channels_are_taken(d):
+    """(image, group) pairs count where a launch has a work-group for each, and these have none"""
+    for back in (0, 1):
+        assert B.lib().cprune_group_norm_workspace_bytes(_norm(*d), back) > 0
