@@ -1,0 +1,205 @@
+"""Group norm and its gradient over their range: numbers far from zero, infinities and NaN, long and wide maps, maps that are stored past the caches.
+
+References are the formulas in 64 bits on the same inputs.  u is the type's half unit in the last place, e = 2^-24.  Bounds of y, dx, dweight and dbias as
+the sums behind them have them: a chain of at most a few hundred fp32 additions, joined in 64 bits, errs by less than 64 e of the magnitudes' sum."""
+import math
+
+import pytest
+import torch
+
+from paper_2207_01260_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+TYPES = [torch.float32, torch.float16, torch.bfloat16]
+U = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
+TINY = {torch.float32: 2.0 ** -149, torch.float16: 2.0 ** -24, torch.bfloat16: 2.0 ** -133}
+SIZE = {torch.float32: 4, torch.float16: 2, torch.bfloat16: 2}
+E = 2.0 ** -24
+EPS = 1e-5
+
+
+def over(s, c):
+    """[n, groups] -> [n, 1, c]"""
+    return s.double().repeat_interleave(c // s.shape[1], dim=1)[:, None]
+
+
+def per_group(v, groups):
+    """[n, pixels, c] -> sums over (image, group), [n, groups]"""
+    n, p, c = v.shape
+    return v.sum(dim=1).reshape(n, groups, c // groups).sum(dim=2)
+
+
+def statistics(x, groups):
+    m = x.shape[1] * x.shape[2] // groups
+    mean = per_group(x, groups) / m
+    var = per_group((x - over(mean, x.shape[2])).square(), groups) / m
+    return mean, (var + float(torch.tensor(EPS))) ** -0.5
+
+
+def top_of(x, groups):
+    n, p, c = x.shape
+    return x.abs().amax(dim=1).reshape(n, groups, c // groups).amax(dim=2)
+
+
+def within(got, want, bound, what):
+    got = got.double()
+    assert got.shape == want.shape and not torch.isnan(got).any(), what
+    excess = (got - want).abs() - bound
+    assert float(excess.max()) <= 0, f"{what}: {int((excess > 0).sum())} of {excess.numel()} past the bound, by {float(excess.max()):.3g}"
+
+
+def numbers(n, p, c, dtype, seed, wide=0, offset=0.0, spread=1.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = (torch.randn(n, p, c + wide, generator=g, device="cuda") * spread + offset).to(dtype)
+    dy = torch.randn(n, p, c + wide, generator=g, device="cuda").to(dtype)
+    weight = 0.5 + torch.rand(c, generator=g, device="cuda")
+    bias = 0.3 * torch.randn(c, generator=g, device="cuda")
+    return x[..., :c], dy[..., :c], weight, bias
+
+
+def launches(x, groups, backward):
+    """0 where one launch holds an image's channels in registers: it needs no scratch (the gradient of one image)"""
+    n, p, c = x.shape
+    d = B.NormDesc(n, p, c, groups, B.DTYPE_OF_TORCH[x.dtype], 0, x.stride(1), x.stride(1), EPS)
+    return B.lib().cprune_group_norm_workspace_bytes(d, int(backward))
+
+
+def slope(z, act):
+    if act == B.ACT_SILU:
+        s = torch.sigmoid(z)
+        return s * (1 + z * (1 - s))
+    inside = torch.ones_like(z, dtype=torch.bool)
+    if act in (B.ACT_RELU, B.ACT_RELU6):
+        inside &= z > 0
+    if act == B.ACT_RELU6:
+        inside &= z < 6
+    return inside.double()
+
+
+def value(z, act):
+    if act == B.ACT_SILU:
+        return z * torch.sigmoid(z)
+    return z if act == B.ACT_NONE else z.clamp(0, 6 if act == B.ACT_RELU6 else None)
+
+
+def forward_check(x, groups, weight, bias, act):
+    y, mean, rstd = B.cprune_group_norm_act(x, groups, weight, bias, eps=EPS, act=act, want_stats=True)
+    x64, c, dtype = x.double(), x.shape[2], x.dtype
+    m64, r64 = statistics(x64, groups)
+    top = top_of(x64, groups)
+    within(mean, m64, 32 * E * top, "mean")
+    within(rstd, r64, 32 * E * r64 * (1 + r64 * m64.abs()), "rstd")
+    # the mean's error over the spread, the spread's own, some roundings of the argument's terms
+    xw = (x64 - over(m64, c)) * over(r64, c) * weight.double()
+    z = xw + bias.double()
+    slack = 32 * E * (over(top * r64, c) * weight.double().abs() + xw.abs() * (1 + over(r64 * m64.abs(), c))) + 8 * E * (xw.abs() + bias.double().abs())
+    if act == B.ACT_SILU:      # (its slope is below 1.1, its own roundings a few of the result, its exponential's e |z|)
+        slack = 1.1 * slack + 8 * E * (1 + z.abs()) * z.abs()
+    want = value(z, act)
+    within(y, want, U[dtype] * want.abs() + (1 + U[dtype]) * slack + TINY[dtype], "y")
+    return mean, rstd
+
+
+def backward_check(x, dy, groups, weight, bias, act, mean=None, rstd=None, skip_dx=None):
+    n, p, c = x.shape
+    dtype, m = x.dtype, p * c // groups
+    x64 = x.double()
+    if mean is None:
+        mean, rstd = (t.float() for t in statistics(x64, groups))
+    mm, rr, w, b = over(mean, c), over(rstd, c), weight.double(), bias.double()
+    xhat = (x64 - mm) * rr
+    z = xhat * w + b
+    if act in (B.ACT_RELU, B.ACT_RELU6):      # (both sides take the same branch)
+        near = z.abs() < 1e-4
+        if act == B.ACT_RELU6:
+            near |= (z - 6).abs() < 1e-4
+        dy[near] = 0
+    dz = dy.double() * slope(z, act)
+    t1, t2 = (over(per_group(v, groups) / m, c) for v in (dz * w, dz * w * xhat))
+    want = rr * (dz * w - t1 - xhat * t2)
+    off = (x64.abs() + mm.abs()) * rr
+    soft = 1 + (z.abs() + off) if act == B.ACT_SILU else torch.ones_like(z)
+    d = dy.double().abs() * soft
+    a = d * w.abs()
+    size = a + over(per_group(a, groups) / m, c) + xhat.abs() * over(per_group(a * (xhat.abs() + off), groups) / m, c) + off * t2.abs()
+    dx, dweight, dbias = B.cprune_group_norm_act_backward(dy, x, mean, rstd, groups, weight, bias, act=act)
+    within(dbias, dz.sum(dim=(0, 1)), 64 * E * d.sum(dim=(0, 1)) + 1e-30, "dbias")
+    within(dweight, (dz * xhat).sum(dim=(0, 1)), 64 * E * (d * (xhat.abs() + off)).sum(dim=(0, 1)) + 1e-30, "dweight")
+    keep = torch.ones(c, dtype=torch.bool, device="cuda")
+    if skip_dx is not None:
+        keep[skip_dx] = False
+    within(dx[..., keep], want[..., keep], (U[dtype] * want.abs() + 64 * E * rr * size + TINY[dtype])[..., keep], "dx")
+
+
+# (n, pixels, c, groups, wide): one launch (groups of whole vectors, of parts of vectors, pixels that do not fill a superrow) and the split form in its kinds
+WHOLE = [(2, 196, 64, 4, 0), (2, 196, 40, 8, 0), (2, 169, 83, 1, 0)]
+SPLIT = [(2, 25600, 24, 3, 0), (1, 41567, 83, 1, 0), (1, 8100, 2051, 7, 0), (1, 1320, 1300, 100, 0), (1, 16500, 1280, 1280, 0), (2, 900, 45, 5, 1)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", WHOLE + SPLIT)
+def test_all_channels_far_from_zero(shape, dtype):
+    """One offset for all numbers, about a thousand spreads away (bf16: two hundred, its numbers there are four apart): in fp32 a variance from the difference of
+    sums is off by ten times the bound and more (medians over such numbers)."""
+    n, p, c, groups, wide = shape
+    x, dy, weight, bias = numbers(n, p, c, dtype, 1, wide, 1000.0, 4.0 if dtype == torch.bfloat16 else 1.0)
+    assert (launches(x, groups, False) == 0) == (shape in WHOLE)
+    mean, rstd = forward_check(x, groups, weight, bias, B.ACT_NONE)
+    assert float((mean * rstd).median()) > (200 if dtype == torch.bfloat16 else 800)
+    backward_check(x, dy, groups, weight, bias, B.ACT_NONE)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", [(2, 196, 64, 4, 0), (2, 169, 83, 1, 0), (2, 25600, 24, 3, 0), (2, 900, 45, 5, 1), (2, 700, 2052, 4, 0), (2, 1320, 1300, 100, 0)])
+def test_infinity_and_nan_stay_in_their_image_and_group(shape, dtype):
+    n, p, c, groups, wide = shape
+    cg = c // groups
+    spoilt = torch.zeros(n, p, c, dtype=torch.bool, device="cuda")
+    spoilt[1, :, :cg] = True
+    own = torch.zeros(c, dtype=torch.bool, device="cuda")
+    own[:cg] = True
+    for act in (B.ACT_RELU, B.ACT_SILU):
+        x, dy, weight, bias = numbers(n, p, c, dtype, 4, wide)
+        clean, mean, rstd = B.cprune_group_norm_act(x, groups, weight, bias, act=act, want_stats=True)
+        grads = B.cprune_group_norm_act_backward(dy, x, mean, rstd, groups, weight, bias, act=act)
+        for bad in (math.inf, -math.inf, math.nan):
+            x2 = torch.nn.functional.pad(x, (0, wide))[..., :c] if wide else x.clone()
+            x2[1, p // 2, 0] = bad
+            y, mean2, rstd2 = B.cprune_group_norm_act(x2, groups, weight, bias, act=act, want_stats=True)
+            assert torch.isnan(y[spoilt]).all() and torch.equal(y[~spoilt], clean[~spoilt])
+            got = B.cprune_group_norm_act_backward(dy, x2, mean2, rstd2, groups, weight, bias, act=act)
+            assert torch.isnan(got[0][spoilt]).all() and torch.equal(got[0][~spoilt], grads[0][~spoilt])
+            assert torch.equal(got[1][~own], grads[1][~own]) and torch.equal(got[2][~own], grads[2][~own])
+            # the same number in dy
+            dy2 = torch.nn.functional.pad(dy, (0, wide))[..., :c] if wide else dy.clone()
+            at = int((clean[1, :, 0] > 0).nonzero()[0])      # (where the activation passes it on)
+            dy2[1, at, 0] = bad
+            got = B.cprune_group_norm_act_backward(dy2, x, mean, rstd, groups, weight, bias, act=act)
+            assert not torch.isfinite(got[0][spoilt]).any() and torch.equal(got[0][~spoilt], grads[0][~spoilt])
+            assert not torch.isfinite(got[1][0]) and not torch.isfinite(got[2][0])
+            assert torch.equal(got[1][1:], grads[1][1:]) and torch.equal(got[2][1:], grads[2][1:])
+
+
+# one image of many groups, whose sums many work-groups leave; superrows of many tiles
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", [(1, 16500, 1280, 1280, 0), (1, 16501, 1280, 640, 0), (2, 9000, 515, 515, 0), (1, 64, 65906, 62, 0), (1, 5001, 601, 601, 1), (3, 70000, 8, 2, 0)])
+def test_long_maps_of_many_groups(shape, dtype):
+    n, p, c, groups, wide = shape
+    for act in (B.ACT_NONE, B.ACT_SILU, B.ACT_RELU6):
+        x, dy, weight, bias = numbers(n, p, c, dtype, 5, wide)
+        forward_check(x, groups, weight, bias, act)
+        backward_check(x, dy, groups, weight, bias, act)
+
+
+# more than 128 MB read and written, so stored past the caches: odd channels (stores begin anywhere, the last superrow is not full), whole vectors, single elements
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", [(8, 90300, 99, 9, 0), (4, 100000, 128, 32, 0), (4, 63003, 135, 5, 1)])
+def test_maps_past_the_caches(shape, dtype):
+    n, p, c, groups, wide = shape
+    assert 2 * n * p * c * SIZE[dtype] > 1 << 27
+    for act in (B.ACT_SILU, B.ACT_RELU):
+        x, dy, weight, bias = numbers(n, p, c, dtype, 6, wide)
+        forward_check(x, groups, weight, bias, act)
+        backward_check(x, dy, groups, weight, bias, act)
+        del x, dy
