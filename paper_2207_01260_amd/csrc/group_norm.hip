@@ -237,9 +237,9 @@ NormArgs args_of(const cprune_norm_desc& d, const NormGeom& g) {
   a.pixels = d.pixels, a.c = d.c, a.groups = d.groups, a.cg = d.c / d.groups;
   a.x_image = (long)d.pixels * d.x_stride, a.x_pitch = (long)g.R * d.x_stride;
   a.dy_image = (long)d.pixels * d.dy_stride, a.dy_pitch = (long)g.R * d.dy_stride;
-  const float inf = std::numeric_limits<float>::infinity();
-  a.lo = d.act == CPRUNE_ACT_NONE ? -inf : 0.0f;
-  a.hi = d.act == CPRUNE_ACT_RELU6 ? 6.0f : inf;
+  const float open = std::numeric_limits<float>::quiet_NaN();
+  a.lo = d.act == CPRUNE_ACT_NONE ? open : 0.0f;
+  a.hi = d.act == CPRUNE_ACT_RELU6 ? 6.0f : open;
   a.n = d.n, a.eps = d.eps;
   a.by_cg = norm_div(a.cg, a.c);
   a.inv_count = 1.0 / ((double)d.pixels * a.cg);

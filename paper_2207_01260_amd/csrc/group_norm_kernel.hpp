@@ -54,7 +54,7 @@ struct NormArgs {
   NormDiv by_cg;              // of a channel
   double inv_count;           // 1 / (numbers of an (image, group))
   long x_image, x_pitch, dy_image, dy_pitch;   // elements from image to image, from superrow to superrow
-  float lo, hi;               // clamp of the activation
+  float lo, hi;               // clamp of the activation; NaN where there is none: no number is past it, no infinity at it
   NormGeom g;
 };
 

@@ -46,7 +46,7 @@ def within(got, want, bound, what):
     got = got.double()
     assert got.shape == want.shape and not torch.isnan(got).any(), what
     excess = (got - want).abs() - bound
-    assert float(excess.max()) <= 0, f"{what}: {int((excess > 0).sum())} of {excess.numel()} past the bound, by {float(excess.max()):.3g}"
+    assert bool((excess <= 0).all()), f"{what}: {int((excess > 0).sum())} of {excess.numel()} past the bound, by {float(excess.max()):.3g}"
 
 
 def numbers(n, p, c, dtype, seed, wide=0, offset=0.0, spread=1.0):
@@ -148,6 +148,21 @@ def test_all_channels_far_from_zero(shape, dtype):
     mean, rstd = forward_check(x, groups, weight, bias, B.ACT_NONE)
     assert float((mean * rstd).median()) > (200 if dtype == torch.bfloat16 else 800)
     backward_check(x, dy, groups, weight, bias, B.ACT_NONE)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("shape", WHOLE + SPLIT)
+def test_gradient_at_infinite_arguments(shape, dtype):
+    """Without an upper clamp the slope is 1 up to infinity, without a lower one down to it."""
+    n, p, c, groups, wide = shape
+    for act in (B.ACT_NONE, B.ACT_RELU, B.ACT_RELU6):
+        x, dy, weight, bias = numbers(n, p, c, dtype, 2, wide)
+        bias[0], bias[1] = math.inf, -math.inf
+        backward_check(x, dy, groups, weight, bias, act)
+        # an argument past the largest number: 3e38 xhat (dx of its group overflows too)
+        x, dy, weight, bias = numbers(n, p, c, dtype, 3, wide)
+        weight[c - 1] = 3e38
+        backward_check(x, dy, groups, weight, bias, act, skip_dx=slice(c - c // groups, c))
 
 
 @pytest.mark.parametrize("dtype", TYPES)
