@@ -16,10 +16,25 @@ __device__ __forceinline__ int chunk_count(const NormGeom& g, int chunk, int rr)
   return sr1 - sr0 - (sr1 == g.SR && rr >= g.tail ? 1 : 0);
 }
 
+// A work-group's sum of its threads' pairs, in a fixed order, in every thread.
+__device__ __forceinline__ double2 block_sum(double2 s) {
+  __shared__ double2 sums[1024 / 64];
+  const int t = (int)threadIdx.x;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    s.x += __shfl_down(s.x, o, 64);
+    s.y += __shfl_down(s.y, o, 64);
+  }
+  if ((t & 63) == 0) sums[t >> 6] = s;
+  __syncthreads();
+  s = sums[0];
+  for (int i = 1; i < (int)blockDim.x / 64; ++i) s.x += sums[i].x, s.y += sums[i].y;
+  return s;
+}
+
 // Sum over the entries (chunk, pixel of the superrow, channel of the group) of an (image, group), one work-group, in 64 bits and a fixed order: f(chunk,
 // pixel, entry, weight).  Eight entries are under way at a time; a thread counts its place on instead of dividing.
 template <typename F> __device__ __forceinline__ double2 entries_sum(const NormArgs& a, const float2* part, const float* weight, F&& f) {
-  __shared__ double2 sums[1024 / 64];
   const int t = (int)threadIdx.x, n = (int)blockDim.x, row = a.g.R * a.c, per = a.g.R * a.cg;
   int chunk = t / per, rr = (t - chunk * per) / a.cg, ch = t - chunk * per - rr * a.cg;
   const int d_chunk = n / per, d_rr = (n - d_chunk * per) / a.cg, d_ch = n - d_chunk * per - d_rr * a.cg;
@@ -45,16 +60,7 @@ template <typename F> __device__ __forceinline__ double2 entries_sum(const NormA
         s.x += v.x, s.y += v.y;
       }
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    s.x += __shfl_down(s.x, o, 64);
-    s.y += __shfl_down(s.y, o, 64);
-  }
-  if ((t & 63) == 0) sums[t >> 6] = s;
-  __syncthreads();
-  s = sums[0];
-  for (int i = 1; i < n / 64; ++i) s.x += sums[i].x, s.y += sums[i].y;
-  return s;
+  return block_sum(s);
 }
 
 // The chunks' statistics as those of an (image, group), where a superrow is wider than a work-group and groups are many.
@@ -81,9 +87,33 @@ __global__ __launch_bounds__(1024) void norm_join_grads_kernel(const NormArgs a,
   if (threadIdx.x == 0) terms[blockIdx.x] = make_float2((float)(s.x * a.inv_count), (float)(s.y * a.inv_count));
 }
 
+// The chunks' and tiles' sums of an (image, group) as its statistics, or as the two means (GRAD).
+template <bool GRAD> __global__ __launch_bounds__(1024) void norm_join_groups_kernel(const NormArgs a, float* __restrict__ mean_out, float* __restrict__ rstd_out, float2* __restrict__ terms) {
+  const int image = blockIdx.x / (unsigned)a.groups, group = blockIdx.x - image * a.groups, count = a.g.chunks * a.g.tiles, n = (int)blockDim.x;
+  const double2* const part = a.gpart + (long)image * count * a.groups + group;
+  double2 s = {0.0, 0.0};
+  for (int i = (int)threadIdx.x; i < count; i += 8 * n) {
+    double2 e[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) e[u] = part[(long)min(i + u * n, count - 1) * a.groups];
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (i + u * n < count) s.x += e[u].x, s.y += e[u].y;
+  }
+  s = block_sum(s);
+  if (threadIdx.x != 0) return;
+  if constexpr (GRAD) {
+    terms[blockIdx.x] = make_float2((float)(s.x * a.inv_count), (float)(s.y * a.inv_count));
+  } else {
+    const float2 m = norm::statistics(s, a);
+    mean_out[blockIdx.x] = m.x;
+    rstd_out[blockIdx.x] = m.y;
+  }
+}
+
 // threads of those: four entries each or more, 64 to 1024
 int join_threads(const NormGeom& g, int cg) {
-  const long entries = (long)g.chunks * g.R * cg;
+  const long entries = g.joined ? (long)g.chunks * g.tiles : (long)g.chunks * g.R * cg;
   int t = 64;
   while (t < 1024 && 4L * t < entries) t *= 2;
   return t;
@@ -154,6 +184,8 @@ bool choose_whole(const cprune_norm_desc& d, bool backward, NormGeom& g) {
 // would leave sums of many groups: a launch between has a work-group for each (image, group) then.
 bool sums_groups(const cprune_norm_desc& d, const NormGeom& g) { return g.tiles == 1 || d.groups <= 64; }
 
+constexpr int kChain = 512;
+
 NormGeom geometry(const cprune_norm_desc& d, bool backward) {
   NormGeom g = {};
   const bool dense = d.x_stride == d.c && (!backward || d.dy_stride == d.c);
@@ -178,7 +210,12 @@ NormGeom geometry(const cprune_norm_desc& d, bool backward) {
   const long most = (g.SR + 4L * g.rpi - 1) / (4L * g.rpi);
   // (and few enough that a work-group joins an image's sums with sixteen entries a thread, or where a launch of its own does it with 64)
   const long few = std::max(4L, sums_groups(d, g) ? 16L * norm::kThreads / ((long)d.groups * g.tiles) : 65536L / ((long)g.R * (d.c / d.groups)));
-  const long chunks = std::max(1L, std::min({want, most, few}));
+  // A thread adds no more than kChain numbers one after another in 32 bits, which lose up to a part in 2^24 each of what is there already: longer runs have more
+  // chunks, whose sums are joined in 64 bits.  Where those are more than the work-groups may join themselves, a launch between does it, and nothing limits them
+  // (1 x 16500 x 1280 fp16 of 1280 groups in 4 chunks 1430 us, with the launch 46; its gradient 3170 and 67).
+  const long least = (g.SR + (long)kChain * g.rpi - 1) / ((long)kChain * g.rpi);
+  g.joined = sums_groups(d, g) && least > few;
+  const long chunks = std::max({1L, least, std::min({want, most, g.joined ? want : few})});
   g.spc = (int)((g.SR + chunks - 1) / chunks);
   g.spc = (g.spc + g.rpi - 1) / g.rpi * g.rpi;
   g.chunks = (g.SR + g.spc - 1) / g.spc;
@@ -202,7 +239,7 @@ int check(const cprune_norm_desc* d, bool backward) {
 bool fits(const cprune_norm_desc& d, const NormGeom& g, bool backward) {
   const double vectors = ((long)d.c + 7) / 8;      // work-groups for dweight and dbias
   if (g.nv) return std::max((double)d.n * g.slabs * g.threads, backward && d.n > 1 ? vectors * norm::kThreads : 0.0) < 4294967296.0;
-  const double join = sums_groups(d, g) ? 0.0 : (double)d.n * d.groups * join_threads(g, d.c / d.groups);
+  const double join = sums_groups(d, g) && !g.joined ? 0.0 : (double)d.n * d.groups * join_threads(g, d.c / d.groups);
   return std::max(((double)d.n * g.chunks * g.tiles + vectors) * norm::kThreads, join) < 4294967296.0;
 }
 // The geometry of a call that has passed check(); false where it is more than the launches hold.
@@ -228,7 +265,7 @@ NormScratch scratch_of(const cprune_norm_desc& d, const NormGeom& g, bool backwa
   const bool groups = sums_groups(d, g);
   if (backward || !groups) q.part = round16((size_t)d.n * g.chunks * (g.tiles > 1 ? g.R : 1) * d.c * pair);
   if (groups) q.gpart = (size_t)d.n * g.chunks * g.tiles * d.groups * sizeof(double2);
-  else q.stats = round16((size_t)d.n * d.groups * pair);
+  if (!groups || g.joined) q.stats = round16((size_t)d.n * d.groups * pair);
   return q;
 }
 
@@ -302,18 +339,18 @@ extern "C" int cprune_group_norm_act(const cprune_norm_desc* d, const void* x, c
   char* const scratch = static_cast<char*>(ws);
   if (g.nv) {
     launch(d->dtype, kNormWhole, a, l, s);
-  } else if (q.gpart) {
-    a.gpart = reinterpret_cast<double2*>(scratch);
-    launch(d->dtype, kNormStats, a, l, s);
-    launch(d->dtype, kNormApply, a, l, s);
   } else {
-    a.part = reinterpret_cast<float2*>(scratch);
-    float* stats = reinterpret_cast<float*>(scratch + q.part);
-    float* mean = mean_out ? mean_out : stats;
-    float* rstd = rstd_out ? rstd_out : stats + (size_t)d->n * d->groups;
-    a.mean = mean, a.rstd = rstd;
+    if (q.gpart) a.gpart = reinterpret_cast<double2*>(scratch);
+    else a.part = reinterpret_cast<float2*>(scratch);
     launch(d->dtype, kNormStats, a, l, s);
-    norm_join_stats_kernel<<<d->n * d->groups, join_threads(g, a.cg), 0, s>>>(a, mean, rstd);
+    if (q.stats) {
+      float* stats = reinterpret_cast<float*>(scratch + q.part + q.gpart);
+      float* mean = mean_out ? mean_out : stats;
+      float* rstd = rstd_out ? rstd_out : stats + (size_t)d->n * d->groups;
+      if (g.joined) norm_join_groups_kernel<false><<<d->n * d->groups, join_threads(g, a.cg), 0, s>>>(a, mean, rstd, nullptr);
+      else norm_join_stats_kernel<<<d->n * d->groups, join_threads(g, a.cg), 0, s>>>(a, mean, rstd);
+      a.mean = mean, a.rstd = rstd, a.gpart = nullptr;
+    }
     launch(d->dtype, kNormApply, a, l, s);
   }
   CPRUNE_LAUNCH_CHECK();
@@ -346,7 +383,9 @@ extern "C" int cprune_group_norm_act_backward(const cprune_norm_desc* d, const v
     if (q.gpart) a.gpart = reinterpret_cast<double2*>(behind);
     a.terms = terms;
     launch(d->dtype, kNormGradSums, a, l, s);
-    if (!q.gpart) norm_join_grads_kernel<<<d->n * d->groups, join_threads(g, a.cg), 0, s>>>(a, terms);
+    if (g.joined) norm_join_groups_kernel<true><<<d->n * d->groups, join_threads(g, a.cg), 0, s>>>(a, nullptr, nullptr, terms);
+    else if (!q.gpart) norm_join_grads_kernel<<<d->n * d->groups, join_threads(g, a.cg), 0, s>>>(a, terms);
+    if (g.joined) a.gpart = nullptr;
     launch(d->dtype, kNormGradApply, a, l, s);
   }
   CPRUNE_LAUNCH_CHECK();

@@ -10,7 +10,8 @@
 // Two forms, chosen by what an image's channels take:
 //  - whole: a work-group holds all pixels of some whole groups' channels in registers, so x is read once, in one launch (two for the gradient);
 //  - split: work-groups walk over runs ("chunks") of superrows of an image, leaving sums for each group; a second launch joins an image's sums where
-//    it needs them and reads x again.  Where a superrow is wider than a work-group, sums are left for each of its elements and a launch between joins them.
+//    it needs them and reads x again.  Where a superrow is wider than a work-group and groups are many, sums are left for each of its elements and a launch
+//    between joins them; one joins the sums of groups where many groups have many chunks.
 #pragma once
 #include <type_traits>
 
@@ -34,6 +35,7 @@ struct NormGeom {
   int few, more, last_r;   // whole form: superrows of a thread, one more for r < more; the r that has the last one
   int slabs, nv;        // whole form: work-groups an image (of tp vectors a superrow each), vectors a thread holds
   int groups, lanes;    // groups of a slab; threads that sum one, a power of two
+  bool joined;          // split form: a launch between joins the work-groups' sums of groups
 };
 
 constexpr int kNormWholeVectors = 16, kNormWholeGradVectors = 8;      // a thread of the whole form holds at most, of x or of x and dy each

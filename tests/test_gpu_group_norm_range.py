@@ -196,6 +196,29 @@ def test_infinity_and_nan_stay_in_their_image_and_group(shape, dtype):
             assert torch.equal(got[1][1:], grads[1][1:]) and torch.equal(got[2][1:], grads[2][1:])
 
 
+def test_sums_over_many_pixels_lose_nothing():
+    """Terms that a long fp32 chain would round the same way every time: 1 + 2^-13 on a sum past 2^11 is 1."""
+    p, c = 65536, 1024
+    term = 1 + 2.0 ** -13
+    one, zero = torch.ones(1, c, device="cuda"), torch.zeros(1, c, device="cuda")
+    x = torch.ones(1, p, c, device="cuda")
+    dy = torch.full((1, p, c), term, device="cuda")
+    dx, dweight, dbias = B.cprune_group_norm_act_backward(dy, x, zero, one, c)      # xhat = 1
+    want = torch.full((c,), p * term, dtype=torch.float64, device="cuda")
+    within(dbias, want, 64 * E * want, "dbias")
+    within(dweight, want, 64 * E * want, "dweight")
+    # dz - mean(dz) - xhat mean(dz xhat)
+    within(dx, torch.full_like(dx, -term, dtype=torch.float64), torch.full_like(dx, 3 * 64 * E * term, dtype=torch.float64), "dx")
+    del dx, dy
+    # squares of +-s, mean 0
+    s = math.sqrt(1 + 2.0 ** -13)
+    x[:, 0::2], x[:, 1::2] = s, -s
+    _, mean, rstd = B.cprune_group_norm_act(x, c, want_stats=True)
+    want = torch.full_like(rstd, (float(x[0, 0, 0]) ** 2 + float(torch.tensor(EPS))) ** -0.5, dtype=torch.float64)
+    within(mean, torch.zeros_like(want), torch.full_like(want, 32 * E * s), "mean")
+    within(rstd, want, 32 * E * want, "rstd")
+
+
 # one image of many groups, whose sums many work-groups leave; superrows of many tiles
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("shape", [(1, 16500, 1280, 1280, 0), (1, 16501, 1280, 640, 0), (2, 9000, 515, 515, 0), (1, 64, 65906, 62, 0), (1, 5001, 601, 601, 1), (3, 70000, 8, 2, 0)])
