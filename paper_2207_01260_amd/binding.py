@@ -527,11 +527,20 @@ def _on_gpu(x: torch.Tensor, dtype, shape) -> int:
     return x.data_ptr()
 
 
-def _used_on(stream, *tensors) -> None:
-    """Memory taken from torch's current stream is not handed out again before work on `stream` is done with it."""
-    for t in tensors:
-        if t is not None:
+def _on(stream, call, *args):
+    """call(*args) with `stream` as torch's current one.  Outputs and scratch are then of that stream's memory: nothing that the caller's stream has work
+    pending on is written.  Neither they nor the inputs are handed out again before both streams are done with them.  That the inputs are there, and that the
+    outputs are waited for, the caller sees to."""
+    here = torch.cuda.current_stream()
+    with torch.cuda.stream(stream):
+        out = call(*args)
+    for t in args:
+        if isinstance(t, torch.Tensor):
             t.record_stream(stream)
+    for t in out if isinstance(out, tuple) else (out,):
+        if t is not None:
+            t.record_stream(here)
+    return out
 
 
 def _norm_desc(x: torch.Tensor, groups: int, act: int, eps: float):
@@ -554,6 +563,8 @@ def cprune_group_norm_act(x: torch.Tensor, groups: int, weight: Optional[torch.T
                           eps: float = 1e-5, act: int = ACT_NONE, want_stats: bool = False, stream=None):
     """x [n, ..., c], channels last (dense, or the first channels of a wider map); weight, bias fp32 [c].
     -> y dense, or (y, mean [n, groups], rstd [n, groups]) for the backward call."""
+    if stream is not None:
+        return _on(stream, cprune_group_norm_act, x, groups, weight, bias, eps, act, want_stats)
     L = _lib or lib()
     d = _norm_desc(x, groups, act, eps)
     vec = (d.c,)
@@ -569,11 +580,9 @@ def cprune_group_norm_act(x: torch.Tensor, groups: int, weight: Optional[torch.T
         ws_at = ws.data_ptr()
     st = L.cprune_group_norm_act(d, x.data_ptr(), None if weight is None else _on_gpu(weight, torch.float32, vec),
                                  None if bias is None else _on_gpu(bias, torch.float32, vec), y.data_ptr(), mean_at, rstd_at, ws_at, need,
-                                 _raw_stream(stream))
+                                 _raw_stream())
     if st:
         _check(st, "cprune_group_norm_act")
-    if stream is not None:
-        _used_on(stream, y, mean, rstd, ws)
     return (y, mean, rstd) if want_stats else y
 
 
@@ -581,6 +590,8 @@ def cprune_group_norm_act_backward(dy: torch.Tensor, x: torch.Tensor, mean: torc
                                    weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, act: int = ACT_NONE,
                                    want_vectors: bool = True, stream=None):
     """The gradient of cprune_group_norm_act at x: -> (dx dense, dweight fp32 [c], dbias fp32 [c]); the latter None without want_vectors."""
+    if stream is not None:
+        return _on(stream, cprune_group_norm_act_backward, dy, x, mean, rstd, groups, weight, bias, act, want_vectors)
     L = _lib or lib()
     d = _norm_desc(x, groups, act, 0.0)
     if not dy.is_cuda or dy.shape != x.shape or dy.dtype != x.dtype:
@@ -601,11 +612,9 @@ def cprune_group_norm_act_backward(dy: torch.Tensor, x: torch.Tensor, mean: torc
     st = L.cprune_group_norm_act_backward(d, dy.data_ptr(), x.data_ptr(), _on_gpu(mean, torch.float32, stats), _on_gpu(rstd, torch.float32, stats),
                                           None if weight is None else _on_gpu(weight, torch.float32, vec),
                                           None if bias is None else _on_gpu(bias, torch.float32, vec), dx.data_ptr(), dweight_at, dbias_at, ws_at,
-                                          need, _raw_stream(stream))
+                                          need, _raw_stream())
     if st:
         _check(st, "cprune_group_norm_act_backward")
-    if stream is not None:
-        _used_on(stream, dx, dweight, dbias, ws)
     return dx, dweight, dbias
 
 
@@ -635,34 +644,36 @@ def _mx4_pair(codes: torch.Tensor, scales: torch.Tensor, k: Optional[int]):
 
 def cprune_mx4_quantize(x: torch.Tensor, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
     """x [..., k] -> (codes uint8 [rows, ceil(k / 32) * 16], scales uint8 [rows, ceil(k / 32)])."""
+    if stream is not None:
+        return _on(stream, cprune_mx4_quantize, x)
     rows, k, pitch, dtype = _mx4_rows(x)
     blocks = (k + 31) // 32
     dev = x.device
     codes = torch.empty(rows, 16 * blocks, dtype=torch.uint8, device=dev)
     scales = torch.empty(rows, blocks, dtype=torch.uint8, device=dev)
-    st = (_lib or lib()).cprune_mx4_quantize(x.data_ptr(), rows, k, pitch, dtype, codes.data_ptr(), scales.data_ptr(), _raw_stream(stream))
+    st = (_lib or lib()).cprune_mx4_quantize(x.data_ptr(), rows, k, pitch, dtype, codes.data_ptr(), scales.data_ptr(), _raw_stream())
     if st:
         _check(st, "cprune_mx4_quantize")
-    if stream is not None:
-        _used_on(stream, codes, scales)
     return codes, scales
 
 
 def cprune_mx4_dequantize(codes: torch.Tensor, scales: torch.Tensor, k: int, dtype: int = F32, stream=None) -> torch.Tensor:
     """-> [rows, k], the numbers that the codes stand for."""
+    if stream is not None:
+        return _on(stream, cprune_mx4_dequantize, codes, scales, k, dtype)
     ca, sa, rows, _ = _mx4_pair(codes, scales, k)
     y = torch.empty(rows, k, dtype=TORCH_DTYPE[dtype], device=codes.device)
-    st = (_lib or lib()).cprune_mx4_dequantize(ca, sa, rows, k, dtype, y.data_ptr(), _raw_stream(stream))
+    st = (_lib or lib()).cprune_mx4_dequantize(ca, sa, rows, k, dtype, y.data_ptr(), _raw_stream())
     if st:
         _check(st, "cprune_mx4_dequantize")
-    if stream is not None:
-        _used_on(stream, y)
     return y
 
 
 def cprune_mx4_matmul(x_codes: torch.Tensor, x_scales: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tensor, dtype: int,
                       bias: Optional[torch.Tensor] = None, act: int = ACT_NONE, stream=None) -> torch.Tensor:
     """Both operands as codes (rows filled up with zeros past k): -> y [rows, c_out] of dtype."""
+    if stream is not None:
+        return _on(stream, cprune_mx4_matmul, x_codes, x_scales, w_codes, w_scales, dtype, bias, act)
     L = _lib or lib()
     xa, xs, rows, blocks = _mx4_pair(x_codes, x_scales, None)
     wa, wsc, c_out, _ = _mx4_pair(w_codes, w_scales, 32 * blocks)
@@ -673,17 +684,17 @@ def cprune_mx4_matmul(x_codes: torch.Tensor, x_scales: torch.Tensor, w_codes: to
         ws = x_codes.new_empty(need)
         ws_at = ws.data_ptr()
     st = L.cprune_mx4_matmul(xa, xs, rows, 32 * blocks, wa, wsc, c_out, None if bias is None else _on_gpu(bias, torch.float32, (c_out,)), act,
-                             dtype, y.data_ptr(), ws_at, need, _raw_stream(stream))
+                             dtype, y.data_ptr(), ws_at, need, _raw_stream())
     if st:
         _check(st, "cprune_mx4_matmul")
-    if stream is not None:
-        _used_on(stream, y, ws)
     return y
 
 
 def cprune_mx4_linear(x: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Tensor, bias: Optional[torch.Tensor] = None,
                       act: int = ACT_NONE, stream=None) -> torch.Tensor:
     """x [..., k] in numbers, w as codes: -> y [..., c_out], the type of x."""
+    if stream is not None:
+        return _on(stream, cprune_mx4_linear, x, w_codes, w_scales, bias, act)
     L = _lib or lib()
     rows, k, pitch, dtype = _mx4_rows(x)
     wa, wsc, c_out, _ = _mx4_pair(w_codes, w_scales, k)
@@ -694,11 +705,9 @@ def cprune_mx4_linear(x: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Te
         ws = torch.empty(need, dtype=torch.uint8, device=x.device)
         ws_at = ws.data_ptr()
     st = L.cprune_mx4_linear(x.data_ptr(), rows, k, pitch, wa, wsc, c_out, None if bias is None else _on_gpu(bias, torch.float32, (c_out,)), act,
-                             dtype, y.data_ptr(), ws_at, need, _raw_stream(stream))
+                             dtype, y.data_ptr(), ws_at, need, _raw_stream())
     if st:
         _check(st, "cprune_mx4_linear")
-    if stream is not None:
-        _used_on(stream, y, ws)
     return y
 
 
