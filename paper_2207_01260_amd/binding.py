@@ -185,11 +185,35 @@ def _size(ws: Optional[torch.Tensor]) -> int:
     return ws.numel() if ws is not None else 0
 
 
+def _tensors(values):
+    for v in values:
+        if isinstance(v, torch.Tensor):
+            yield v
+        elif isinstance(v, (tuple, list)):
+            yield from _tensors(v)
+
+
+def _on(stream, call, *args):
+    """call(*args) with `stream` as torch's current one.  Outputs and scratch are then of that stream's memory: nothing that the caller's stream has work
+    pending on is written.  Neither they nor the inputs are handed out again before both streams are done with them.  That the inputs are there, and that the
+    outputs are waited for, the caller sees to."""
+    here = torch.cuda.current_stream()
+    with torch.cuda.stream(stream):
+        out = call(*args)
+    for t in _tensors(args):
+        t.record_stream(stream)
+    for t in _tensors((out,)):
+        t.record_stream(here)
+    return out
+
+
 # ---- ranking / gather ------------------------------------------------------
 
 def cprune_rank_filters(w: torch.Tensor, keep: int, want_scores=True, want_order=True,
                         stream=None):
     """-> (scores fp64 or None, order int32 or None, kept int32 ascending)."""
+    if stream is not None:
+        return _on(stream, cprune_rank_filters, w, keep, want_scores, want_order)
     assert w.dtype == torch.float32 and w.dim() == 4
     c_out, cpg, kh, kw = w.shape
     dev = w.device
@@ -200,7 +224,7 @@ def cprune_rank_filters(w: torch.Tensor, keep: int, want_scores=True, want_order
     ws = _ws(nws, dev)
     st = lib().cprune_rank_filters(_ptr(w), C.c_int(c_out), C.c_int(cpg), C.c_int(kh), C.c_int(kw),
                                    C.c_int(keep), _ptr(scores), _ptr(order), _ptr(kept), _ptr(ws),
-                                   C.c_size_t(_size(ws)), _stream(stream))
+                                   C.c_size_t(_size(ws)), _stream())
     _check(st, "cprune_rank_filters")
     return scores, order, kept
 
@@ -300,6 +324,8 @@ def cprune_rank_filter_group(ws_list, keep: int, want_scores=True, want_order=Tr
     """Layers that must lose the same channels, ranked on the sum of their filter norms.
     ws_list: fp32 device weight tensors with the same number of filters.
     -> (scores fp64 or None, order int32 or None, kept int32 ascending)."""
+    if stream is not None:
+        return _on(stream, cprune_rank_filter_group, ws_list, keep, want_scores, want_order)
     c_out = ws_list[0].shape[0]
     assert all(w.dtype == torch.float32 and w.shape[0] == c_out for w in ws_list)
     dev = ws_list[0].device
@@ -314,7 +340,7 @@ def cprune_rank_filter_group(ws_list, keep: int, want_scores=True, want_order=Tr
     ws = _ws(lib().cprune_rank_filters_workspace_bytes(C.c_int(c_out)), dev)
     st = lib().cprune_rank_filter_group(ptrs, lens, C.c_int(n), C.c_int(c_out), C.c_int(keep), _ptr(scores),
                                         _ptr(order), _ptr(kept), _ptr(ws), C.c_size_t(_size(ws)),
-                                        _stream(stream))
+                                        _stream())
     _check(st, "cprune_rank_filter_group")
     return scores, order, kept
 
@@ -324,6 +350,8 @@ def cprune_gather_pruned_weights(w: torch.Tensor, keep_out=None, keep_in=None, b
                                  stream=None) -> Tuple[torch.Tensor, Optional[torch.Tensor]]:
     """bn = (gamma, beta, mean, var) device fp32 vectors over the unpruned filters, or None.
     -> (w_out [n_out][n_in][kh][kw] in out_dtype, bias_out fp32 [n_out] or None)."""
+    if stream is not None:
+        return _on(stream, cprune_gather_pruned_weights, w, keep_out, keep_in, bn, eps, conv_bias, out_dtype)
     assert w.dtype == torch.float32 and w.dim() == 4
     c_out, c_in, kh, kw = w.shape
     n_out = c_out if keep_out is None else keep_out.numel()
@@ -336,17 +364,19 @@ def cprune_gather_pruned_weights(w: torch.Tensor, keep_out=None, keep_in=None, b
         _ptr(w), C.c_int(c_out), C.c_int(c_in), C.c_int(kh), C.c_int(kw),
         _ptr(keep_out), C.c_int(n_out), _ptr(keep_in), C.c_int(n_in),
         _ptr(g), _ptr(b), _ptr(m), _ptr(v), C.c_float(eps), _ptr(conv_bias),
-        C.c_int(out_dtype), _ptr(w_out), _ptr(bias_out), _stream(stream))
+        C.c_int(out_dtype), _ptr(w_out), _ptr(bias_out), _stream())
     _check(st, "cprune_gather_pruned_weights")
     return w_out, bias_out
 
 
 def cprune_gather_channels(x: torch.Tensor, idx: torch.Tensor, stream=None) -> torch.Tensor:
+    if stream is not None:
+        return _on(stream, cprune_gather_channels, x, idx)
     n, c, h, w = x.shape
     y = torch.empty((n, idx.numel(), h, w), dtype=x.dtype, device=x.device)
     st = lib().cprune_gather_channels(_ptr(x), C.c_int(n), C.c_int(c), C.c_int(h), C.c_int(w),
                                       C.c_int(DTYPE_OF_TORCH[x.dtype]), _ptr(idx),
-                                      C.c_int(idx.numel()), _ptr(y), _stream(stream))
+                                      C.c_int(idx.numel()), _ptr(y), _stream())
     _check(st, "cprune_gather_channels")
     return y
 
@@ -393,6 +423,8 @@ def cprune_conv2d_bn_relu(d: ConvDesc, x, w, bias=None, residual=None, tile_vari
                           ws: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None,
                           stream=None) -> torch.Tensor:
     # (what the caller's thread does per call is the time of a small layer: 64 -> 45 at 32x32, one image, 11.7 us before, the kernel 6.5)
+    if stream is not None:
+        return _on(stream, cprune_conv2d_bn_relu, d, x, w, bias, residual, tile_variant, ws, y)
     L = _lib or lib()
     if y is None:
         y = x.new_empty(out_shape(d), dtype=TORCH_DTYPE[d.dtype])
@@ -408,7 +440,7 @@ def cprune_conv2d_bn_relu(d: ConvDesc, x, w, bias=None, residual=None, tile_vari
                 tile_variant = v.value
         ws = _ws(L.cprune_conv_workspace_bytes(d, tile_variant), x.device)
     st = L.cprune_conv2d_bn_relu(d, _addr(x), _addr(w), _addr(bias), _addr(residual), y_addr, tile_variant, _addr(ws),
-                                 _size(ws), _raw_stream(stream))
+                                 _size(ws), _raw_stream())
     _check(st, "cprune_conv2d_bn_relu")
     return y
 
@@ -416,6 +448,8 @@ def cprune_conv2d_bn_relu(d: ConvDesc, x, w, bias=None, residual=None, tile_vari
 def cprune_select_tile(d: ConvDesc, x, w, bias=None, residual=None, warmup: int = 2,
                        iters: int = 8, stream=None):
     """-> (variant, best_ms, all_ms list)."""
+    if stream is not None:
+        return _on(stream, cprune_select_tile, d, x, w, bias, residual, warmup, iters)
     y = torch.empty(out_shape(d), dtype=TORCH_DTYPE[d.dtype], device=x.device)
     ws = _ws(cprune_conv_workspace_bytes(d, -1), x.device)
     nv = cprune_num_tile_variants()
@@ -423,7 +457,7 @@ def cprune_select_tile(d: ConvDesc, x, w, bias=None, residual=None, warmup: int 
     v, best = C.c_int(-1), C.c_float(0)
     st = lib().cprune_select_tile(C.byref(d), _ptr(x), _ptr(w), _ptr(bias), _ptr(residual), _ptr(y),
                                   _ptr(ws), C.c_size_t(_size(ws)), C.c_int(warmup), C.c_int(iters),
-                                  C.byref(v), C.byref(best), all_ms, _stream(stream))
+                                  C.byref(v), C.byref(best), all_ms, _stream())
     _check(st, "cprune_select_tile")
     return v.value, best.value, list(all_ms)
 
@@ -441,26 +475,32 @@ def cprune_cached_tile(d: ConvDesc) -> Tuple[int, bool]:
 # ---- other layers --------------------------------------------------------------
 
 def cprune_maxpool2d(x, k, stride, pad=0, stream=None):
+    if stream is not None:
+        return _on(stream, cprune_maxpool2d, x, k, stride, pad)
     n, c, h, w = x.shape
     ho, wo = (h + 2 * pad - k) // stride + 1, (w + 2 * pad - k) // stride + 1
     y = torch.empty((n, c, ho, wo), dtype=x.dtype, device=x.device)
     st = lib().cprune_maxpool2d(_ptr(x), C.c_int(n), C.c_int(c), C.c_int(h), C.c_int(w), C.c_int(k),
                                 C.c_int(stride), C.c_int(pad), C.c_int(DTYPE_OF_TORCH[x.dtype]),
-                                _ptr(y), _stream(stream))
+                                _ptr(y), _stream())
     _check(st, "cprune_maxpool2d")
     return y
 
 
 def cprune_global_avgpool(x, stream=None):
+    if stream is not None:
+        return _on(stream, cprune_global_avgpool, x)
     n, c, h, w = x.shape
     y = torch.empty((n, c), dtype=x.dtype, device=x.device)
     st = lib().cprune_global_avgpool(_ptr(x), C.c_int(n), C.c_int(c), C.c_int(h), C.c_int(w),
-                                     C.c_int(DTYPE_OF_TORCH[x.dtype]), _ptr(y), _stream(stream))
+                                     C.c_int(DTYPE_OF_TORCH[x.dtype]), _ptr(y), _stream())
     _check(st, "cprune_global_avgpool")
     return y
 
 
 def cprune_fc(x, w, bias=None, act=ACT_NONE, stream=None):
+    if stream is not None:
+        return _on(stream, cprune_fc, x, w, bias, act)
     n = x.shape[0]
     f = x.numel() // n
     c_out = w.shape[0]
@@ -470,7 +510,7 @@ def cprune_fc(x, w, bias=None, act=ACT_NONE, stream=None):
              x.device)
     st = lib().cprune_fc(_ptr(x), _ptr(w), _ptr(bias), C.c_int(n), C.c_int(f), C.c_int(c_out),
                          C.c_int(act), C.c_int(dt), _ptr(y), _ptr(ws), C.c_size_t(_size(ws)),
-                         _stream(stream))
+                         _stream())
     _check(st, "cprune_fc")
     return y
 
@@ -525,22 +565,6 @@ def _on_gpu(x: torch.Tensor, dtype, shape) -> int:
     if x.dtype != dtype or x.shape != shape:
         _refuse(f"expected {dtype} {tuple(shape)}, got {x.dtype} {tuple(x.shape)}")
     return x.data_ptr()
-
-
-def _on(stream, call, *args):
-    """call(*args) with `stream` as torch's current one.  Outputs and scratch are then of that stream's memory: nothing that the caller's stream has work
-    pending on is written.  Neither they nor the inputs are handed out again before both streams are done with them.  That the inputs are there, and that the
-    outputs are waited for, the caller sees to."""
-    here = torch.cuda.current_stream()
-    with torch.cuda.stream(stream):
-        out = call(*args)
-    for t in args:
-        if isinstance(t, torch.Tensor):
-            t.record_stream(stream)
-    for t in out if isinstance(out, tuple) else (out,):
-        if t is not None:
-            t.record_stream(here)
-    return out
 
 
 def _norm_desc(x: torch.Tensor, groups: int, act: int, eps: float):
@@ -895,6 +919,8 @@ class Net:
         self.out_features = c.value * h.value * w.value
 
     def forward(self, x, logits=None, use_graph=False, stream=None):
+        if stream is not None and logits is None and not use_graph:
+            return _on(stream, self.forward, x)
         n = x.shape[0]
         if logits is None and use_graph:
             # a recorded graph is keyed by (n, x, logits): without a buffer of the caller's, the same one is
