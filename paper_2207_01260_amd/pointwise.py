@@ -17,23 +17,48 @@ from . import binding as B
 from . import synth
 
 
+def _between(stream, call, *args):
+    """call(*args) on `stream`, between what torch's current stream has had and what it gets."""
+    here = torch.cuda.current_stream()
+    stream.wait_stream(here)
+    with torch.cuda.stream(stream):
+        out = call(*args)
+    here.wait_stream(stream)
+    return out
+
+
 class PointwiseBlock:
     """x [n, h, w, c] channels last -> [n, h, w, filters kept].  w: the 1x1 layer's raw weights, fp32 [c_out][c][1][1] on the device; its `keep` strongest
-    filters survive."""
+    filters survive.
+
+    What is given a `stream` runs there, behind what the current stream has been given so far and ahead of what it is given next: the block's weights are one
+    set, which `tune` changes on the current stream.  The other calls run on the current stream."""
 
     def __init__(self, w: torch.Tensor, keep: int, groups: int, act: int = B.ACT_SILU, stream=None):
-        c = w.shape[1]
-        _, _, self.kept = B.cprune_rank_filters(w, keep, want_scores=False, want_order=False, stream=stream)
-        kept_w, _ = B.cprune_gather_pruned_weights(w, self.kept, stream=stream)
-        self.w = kept_w.reshape(keep, c)
-        self.codes, self.scales = B.cprune_mx4_quantize(self.w, stream=stream)
         self.groups, self.act = groups, act
+        if stream is None:
+            self._build(w, keep)
+        else:
+            for t in _between(stream, self._build, w, keep):
+                t.record_stream(torch.cuda.current_stream())
+
+    def _build(self, w: torch.Tensor, keep: int):
+        c = w.shape[1]
+        _, _, self.kept = B.cprune_rank_filters(w, keep, want_scores=False, want_order=False)
+        kept_w, _ = B.cprune_gather_pruned_weights(w, self.kept)
+        self.w = kept_w.reshape(keep, c)
+        self.codes, self.scales = B.cprune_mx4_quantize(self.w)
         self.weight = torch.ones(c, device=w.device)
         self.bias = torch.zeros(c, device=w.device)
+        return self.kept, self.w, self.codes, self.scales, self.weight, self.bias
 
     def forward(self, x: torch.Tensor, stream=None) -> torch.Tensor:
-        z = B.cprune_group_norm_act(x, self.groups, self.weight, self.bias, act=self.act, stream=stream)
-        return B.cprune_mx4_linear(z, self.codes, self.scales, stream=stream)
+        if stream is not None:
+            y = _between(stream, self.forward, x)
+            y.record_stream(torch.cuda.current_stream())
+            return y
+        z = B.cprune_group_norm_act(x, self.groups, self.weight, self.bias, act=self.act)
+        return B.cprune_mx4_linear(z, self.codes, self.scales)
 
     def full(self, x: torch.Tensor) -> torch.Tensor:
         """The block's answer with its weights as they were."""
