@@ -10,6 +10,7 @@ through the numbers that the weights' codes stand for (the rounding of the activ
 prints the mean squared error before and after, relative to the answers' own, and the time of a forward pass.
 """
 import argparse
+import math
 
 import torch
 
@@ -67,17 +68,20 @@ class PointwiseBlock:
         return y.reshape(z.shape[:-1] + (y.shape[-1],))
 
     def gradients(self, x: torch.Tensor, target: torch.Tensor):
-        """-> (mean squared error against target, its gradients by the norm's weight and bias and by x)."""
+        """-> (mean squared error against target, its gradients by the norm's weight and bias and by x, in fp32)."""
         z, mean, rstd = B.cprune_group_norm_act(x, self.groups, self.weight, self.bias, act=self.act, want_stats=True)
         y = B.cprune_mx4_linear(z, self.codes, self.scales)
         miss = y.float() - target.float()
-        dy = (miss * (2.0 / miss.numel())).to(x.dtype)
+        # An answer's share, 2 / count, is below fp16's normal numbers from 33000 answers on: the power of two that brings it to between a half and one is taken
+        # out again behind the norm.  (The other types' bits are the same either way.)
+        up = 2.0 ** math.floor(math.log2(miss.numel() / 2.0))
+        dy = (miss * (2.0 / miss.numel() * up)).to(x.dtype)
         c = x.shape[-1]
         # dz = dy w: a fully connected layer with the decoded weights' transpose as its weights
         back = B.cprune_mx4_dequantize(self.codes, self.scales, c, B.DTYPE_OF_TORCH[x.dtype]).t().contiguous()
         dz = B.cprune_fc(dy.reshape(-1, dy.shape[-1]), back).reshape(x.shape)
         dx, dweight, dbias = B.cprune_group_norm_act_backward(dz, x, mean, rstd, self.groups, self.weight, self.bias, act=self.act)
-        return miss.square().mean(), dweight, dbias, dx
+        return miss.square().mean(), dweight / up, dbias / up, dx.float() / up
 
     def tune(self, x: torch.Tensor, target: torch.Tensor, steps: int, rate: float):
         """Gradient descent on the norm's vectors; -> the error of every step."""
