@@ -32,8 +32,8 @@ if ROOT not in sys.path:
 # workload: from the rocprofv3 counter runs summarised in profiles/vgg16_b64_f32_hbm_traffic.md (three
 # pinned selections, because the timed selection flips between near-equal variants).  The figures belong
 # to the kernel sources they were measured on: TRAFFIC_SOURCE_HASH is kernel_source_hash() of that tree,
-# and any change to a file under csrc/ since then reports null instead of a stale figure (as does a
-# selection that runs a kernel on a layer it was not profiled on).
+# and any change since then to a file that a network is built from reports null instead of a stale figure (as
+# does a selection that runs a kernel on a layer it was not profiled on).
 TRAFFIC_SOURCE_HASH = "23089d51be4c9abf"
 TRAFFIC = {
     ("conv_stem2_kernel<float, 2>", 64, "conv2"): 3351054,
@@ -71,13 +71,16 @@ def dominant_traffic(kernel, batch, layers):
     return int(sum(figures) / len(figures))
 
 
-def kernel_source_hash():
-    """sha256 over the HIP sources the library is built from (names and contents, in name order)."""
+# sources of calls that no network makes; nothing else includes them
+APART = ("group_norm", "mx4")
+
+
+def kernel_source_hash(d=os.path.join(ROOT, "paper_2207_01260_amd", "csrc")):
+    """sha256 over the HIP sources that networks run (names and contents, in name order): all but those of calls beside them."""
     import hashlib
-    d = os.path.join(ROOT, "paper_2207_01260_amd", "csrc")
     h = hashlib.sha256()
     for name in sorted(os.listdir(d)):
-        if name.endswith((".hip", ".hpp")):
+        if name.endswith((".hip", ".hpp")) and not name.startswith(APART):
             h.update(name.encode())
             h.update(open(os.path.join(d, name), "rb").read())
     return h.hexdigest()[:16]
