@@ -2,6 +2,10 @@
 marshalling only.  Tensors are torch CUDA tensors (device memory and streams are
 PyTorch's); every step of the path runs in the library's kernels.  There is no
 fallback: a missing library raises.
+
+`stream`: a call runs on torch's current stream, or on the one it is given.  Then the
+caller orders that one behind whatever writes its inputs, and what reads its outputs
+behind it; their memory the call looks after.
 """
 
 from __future__ import annotations

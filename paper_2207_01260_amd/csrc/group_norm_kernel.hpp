@@ -123,7 +123,8 @@ template <bool SILU> __device__ __forceinline__ float slope(float z, float lo, f
   return z <= lo || z >= hi ? 0.0f : 1.0f;
 }
 // xhat and the activation's argument with each operation rounded, as the formula has them: whether a clamp passes a gradient does not
-// depend on which products and sums the compiler joins
+// depend on which products and sums the compiler joins.  (The forward pass has weight * rstd as one factor and one rounding less, so that within a few roundings
+// of a kink a clamped output may have a gradient, or one that is not clamped none.)
 __device__ __forceinline__ float centred(float x, float mean, float rstd) {
 #pragma clang fp contract(off)
   return (x - mean) * rstd;

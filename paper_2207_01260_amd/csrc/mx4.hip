@@ -198,7 +198,8 @@ ProductPlan plan_product(int rows, int k, int c_out, int dtype) {
     q.form = kFew;
     // Up to 16 rows the work-groups make the codes themselves, each all of them, a lane reading 64 or 128 bytes of a row of its own.  Where that is much and slow,
     // by twice the bytes or as 16-bit rows of odd length begin between two dwords, a launch before is quicker: 16 x 4097 x 1000 bf16 15.6 -> 6.1 us and 10.4 -> 6.3 in
-    // fp32, 4 x 8191 x 1000 13.7 -> 9.1 and 12.5 -> 9.1; but 8 x 1025 x 1000 no difference, 8 x 4096 x 1000 bf16 6.6 and 7.3.
+    // fp32; but 8 x 1025 x 1000 no difference, 8 x 4096 x 1000 bf16 6.6 and 7.3.  (4 x 8191 x 1000, just under the limit, 13.5 and 9.1.  The length stands for the rows'
+    // distance, which the question for scratch does not say: 16 rows of 4096 bf16 at a distance of 4109 stay without the launch, 12.3 us; at 4096 7.9, at 4108 5.6.)
     q.codes_first = dtype >= 0 && (rows > 16 || ((dtype == CPRUNE_F32 || k % 2) && (long)rows * k >= 32768));
   }
   if (q.codes_first) {
