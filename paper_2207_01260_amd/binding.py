@@ -923,8 +923,8 @@ class Net:
         self.out_features = c.value * h.value * w.value
 
     def forward(self, x, logits=None, use_graph=False, stream=None):
-        if stream is not None and logits is None and not use_graph:
-            return _on(stream, self.forward, x)
+        if stream is not None and logits is None:
+            return _on(stream, self.forward, x, None, use_graph)
         n = x.shape[0]
         if logits is None and use_graph:
             # a recorded graph is keyed by (n, x, logits): without a buffer of the caller's, the same one is
@@ -950,6 +950,8 @@ class Net:
         return list(ms)
 
     def activation(self, layer: int, n: int, shape, stream=None):
+        if stream is not None:
+            return _on(stream, self.activation, layer, n, shape)
         out = torch.empty((n,) + tuple(shape), dtype=TORCH_DTYPE[self.dtype], device="cuda")
         st = lib().cprune_net_copy_activation(self._h, C.c_int(layer), C.c_int(n), _ptr(out),
                                               C.c_size_t(out.numel() * out.element_size()),

@@ -102,3 +102,19 @@ def test_without_a_stream_it_is_the_current_one(world, name):
     world.taken.clear()
     call()
     assert world.launched == [HERE] and {s for s, _ in world.taken} == {HERE} and not world.kept
+
+
+@pytest.mark.parametrize("what", ["forward", "graph", "activation"])
+def test_a_networks_outputs(world, monkeypatch, what):
+    net = B.Net.__new__(B.Net)
+    net._h, net._graph_logits, net.dtype, net.out_shape, net.out_features = None, {}, B.F32, (10,), 10
+    empty = torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *a, device=None, **kw: empty(*a, **kw))
+    x = on_device(2, 3, 8, 8)
+    world.taken.clear()
+    out = net.activation(0, 2, (4, 8, 8), stream=SIDE) if what == "activation" else net.forward(x, use_graph=what == "graph", stream=SIDE)
+    assert world.launched == [SIDE] and world.taken == [(SIDE, out.data_ptr())] and (out.data_ptr(), HERE) in world.kept
+    if what != "activation":
+        assert (x.data_ptr(), SIDE) in world.kept
+    if what == "graph":
+        assert net.forward(x, use_graph=True, stream=SIDE) is out
