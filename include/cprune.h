@@ -503,7 +503,8 @@ int cprune_search_destroy(cprune_search* s);
  * c / groups channels of each (image, group):
  *   mean = sum x / m, var = sum (x - mean)^2 / m, rstd = 1 / sqrt(var + eps), m = pixels * c / groups
  *   y = act((x - mean) * rstd * weight_c + bias_c)
- * Statistics and sums are held in 32 bits or more whatever the type; y is rounded once.  An infinity or NaN in x spreads
+ * Statistics and sums are held in 32 bits or more whatever the type (a spread past 1e19, whose square fp32 does not hold, counts as
+ * infinite: rstd 0); y is rounded once.  An infinity or NaN in x spreads
  * over its own (image, group); ReLU and ReLU6 pass a NaN on.
  *
  * Backward, with z the activation's argument and dz = dy * act'(z) (0 at both ends of a clamp):
