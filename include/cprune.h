@@ -566,6 +566,55 @@ int cprune_mx4_linear(const void* x, int rows, int k, int x_stride, const void* 
                       const float* bias, cprune_act act, cprune_dtype dtype, void* y, void* ws, size_t ws_bytes,
                       void* stream);
 
+/* ------------------------------------------------------------------------
+ * A teacher's top logits and the loss of a student against them: what a pruned network is tuned with, for a few steps, from the answers of the
+ * network it was pruned from.
+ *
+ * z          [rows][classes] of dtype, rows z_stride elements apart (z_stride >= classes); -infinity: a class that is masked
+ *
+ * cprune_top_logits: the k largest of each row, descending, equal ones (0 and -0 are) by their class, NaN before all.
+ * values     [rows][k] of dtype
+ * ids        int32 [rows][k]; a masked class is never listed: places that are left over hold -infinity and -1
+ * ws         cprune_top_logits_workspace_bytes(...) of scratch, 16-byte aligned; NULL where that is 0
+ * 1 <= k <= classes; k <= 256 and rows < 2^22, more: CPRUNE_ERR_UNSUPPORTED, and a workspace of 0. */
+size_t cprune_top_logits_workspace_bytes(int rows, int classes, int k, cprune_dtype dtype);
+int cprune_top_logits(const void* z, int rows, int classes, int z_stride, int k, cprune_dtype dtype, void* values, int32_t* ids,
+                      void* ws, size_t ws_bytes, void* stream);
+
+/* Distillation.  With T the temperature, h the share of the hard label, p the softmax of teacher / T over a row's list, q_T the softmax of z / T and q_1
+ * that of z, both over all classes:
+ *   loss = (1 - h) T^2 sum over the list of p (log p - log q_T) - h log q_1[label]
+ *   dz   = dloss ((1 - h) T (q_T - p) + h (q_1 - [label]))        (a class listed more than once has the sum of its p)
+ * Sums in 32 bits, in a fixed order; dz is rounded once.
+ * ids        int32 [rows][k]: a class outside [0, classes), or a teacher logit of -infinity, is no entry
+ * teacher    [rows][k] of teacher_dtype
+ * labels     int32 [rows] or NULL; outside [0, classes): the row has none
+ * dloss      fp32 [rows], what the rows' losses count
+ * loss       fp32 [rows]
+ * stats      fp32 [3][rows], for the backward call, or NULL: a row's largest logit m and the logarithms of sum exp((z - m) / T) and sum exp(z - m)
+ * dz         dense [rows][classes], the type of z; it overlaps no input
+ * A row without an entry, or without a label, goes without that term, and so does a term whose factor (1 - h or h) is 0; without both, with a dloss of 0, or
+ * with every class masked its gradient is 0 whatever else it holds (and in the first and the last case its loss).  A listed class that the row masks makes the
+ * loss infinite, not the gradient.  +infinity or NaN in z makes the row's loss and gradient NaN, in teacher the loss and the gradient of the listed classes.
+ * cprune_distill_step: loss and gradient at once, z read once (rows of up to 131072 numbers of 16 bits or 65536 of 32).
+ * ws         cprune_distill_workspace_bytes(d) of scratch for cprune_distill_loss and _step, 16-byte aligned; NULL where that is 0
+ * temperature > 0, it, its square and its inverse finite; 0 <= hard <= 1; k >= 1; k <= 256 and rows < 2^22, more: CPRUNE_ERR_UNSUPPORTED, and a
+ * workspace of 0. */
+typedef struct {
+  int32_t rows, classes, k;
+  int32_t dtype, teacher_dtype; /* cprune_dtype */
+  int32_t z_stride;
+  float temperature, hard;
+} cprune_distill_desc;
+size_t cprune_distill_workspace_bytes(const cprune_distill_desc* d);
+int cprune_distill_loss(const cprune_distill_desc* d, const void* z, const int32_t* ids, const void* teacher,
+                        const int32_t* labels, float* loss, float* stats, void* ws, size_t ws_bytes, void* stream);
+int cprune_distill_loss_backward(const cprune_distill_desc* d, const float* dloss, const void* z, const int32_t* ids,
+                                 const void* teacher, const int32_t* labels, const float* stats, void* dz, void* stream);
+int cprune_distill_step(const cprune_distill_desc* d, const float* dloss, const void* z, const int32_t* ids,
+                        const void* teacher, const int32_t* labels, float* loss, void* dz, void* ws, size_t ws_bytes,
+                        void* stream);
+
 /* ---- measured ceilings (for reporting kernel throughput against what the device
  * delivers, next to its datasheet peaks; the paper reports end-to-end rates only) ----
  * cprune_probe_mfma: rate of back-to-back dense MFMA instructions of `dtype` on register

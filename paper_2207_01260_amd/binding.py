@@ -42,6 +42,11 @@ class LayerDesc(C.Structure):
                  "act")] + [("weight", C.c_void_p), ("bias", C.c_void_p)]
 
 
+class DistillDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("rows", "classes", "k", "dtype", "teacher_dtype", "z_stride")] + \
+               [("temperature", C.c_float), ("hard", C.c_float)]
+
+
 class PruneLayer(C.Structure):
     _fields_ = [("w", C.c_void_p)] + [(n, C.c_int32) for n in
                                       ("c_out", "c_in", "kh", "kw", "keep", "rows_from", "cols_from")] + \
@@ -83,6 +88,8 @@ EXPORTS = [
     "cprune_group_norm_workspace_bytes", "cprune_group_norm_act", "cprune_group_norm_act_backward",
     "cprune_mx4_quantize", "cprune_mx4_dequantize", "cprune_mx4_matmul_workspace_bytes", "cprune_mx4_matmul",
     "cprune_mx4_linear_workspace_bytes", "cprune_mx4_linear",
+    "cprune_top_logits_workspace_bytes", "cprune_top_logits", "cprune_distill_workspace_bytes", "cprune_distill_loss",
+    "cprune_distill_loss_backward", "cprune_distill_step",
 ]
 
 _lib = None
@@ -128,6 +135,14 @@ def lib():
         L.cprune_mx4_linear_workspace_bytes.argtypes = [C.c_int] * 4
         L.cprune_mx4_linear.argtypes = [C.c_void_p] + [C.c_int] * 3 + [C.c_void_p] * 2 + [C.c_int, C.c_void_p, C.c_int, C.c_int] + \
             [C.c_void_p] * 2 + [C.c_size_t, C.c_void_p]
+        for name in ("cprune_top_logits_workspace_bytes", "cprune_distill_workspace_bytes"):
+            getattr(L, name).restype = C.c_size_t
+        L.cprune_top_logits_workspace_bytes.argtypes = [C.c_int] * 4
+        L.cprune_top_logits.argtypes = [C.c_void_p] + [C.c_int] * 5 + [C.c_void_p] * 3 + [C.c_size_t, C.c_void_p]
+        L.cprune_distill_workspace_bytes.argtypes = [C.POINTER(DistillDesc)]
+        L.cprune_distill_loss.argtypes = [C.POINTER(DistillDesc)] + [C.c_void_p] * 7 + [C.c_size_t, C.c_void_p]
+        L.cprune_distill_loss_backward.argtypes = [C.POINTER(DistillDesc)] + [C.c_void_p] * 8
+        L.cprune_distill_step.argtypes = [C.POINTER(DistillDesc)] + [C.c_void_p] * 8 + [C.c_size_t, C.c_void_p]
         _lib = L
     return _lib
 
@@ -737,6 +752,115 @@ def cprune_mx4_linear(x: torch.Tensor, w_codes: torch.Tensor, w_scales: torch.Te
     if st:
         _check(st, "cprune_mx4_linear")
     return y
+
+
+# ---- a teacher's top logits, distillation ----------------------------------------
+
+def _one_device(x: torch.Tensor, *others: Optional[torch.Tensor]) -> None:
+    """All on the current device, whose stream the call runs on."""
+    device = x.get_device()
+    for t in others:
+        if t is not None and t.get_device() != device:
+            _refuse("tensors of one device only")
+    if device >= 0 and device != torch._C._cuda_getDevice():
+        _refuse(f"tensors of device {device}, device {torch._C._cuda_getDevice()} is current")
+
+
+def _scratch(need: int, x: torch.Tensor):
+    """(tensor, its address), or (None, None)."""
+    if not need:
+        return None, None
+    ws = torch.empty(need, dtype=torch.uint8, device=x.device)
+    return ws, ws.data_ptr()
+
+
+def cprune_top_logits(z: torch.Tensor, k: int, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """z [..., classes] (dense, or the first classes of wider rows) -> (values [..., k], the type of z, classes int32 [..., k]): the k largest of each row,
+    descending, equal ones by their class; -infinity is a masked class: a place left over has that value and class -1."""
+    if stream is not None:
+        return _on(stream, cprune_top_logits, z, k)
+    L = _lib or lib()
+    rows, classes, pitch, dtype = _mx4_rows(z)
+    _one_device(z)
+    if not 1 <= k <= classes:
+        _refuse(f"no {k} of {classes} classes")
+    shape = z.shape[:-1] + (k,)
+    values = torch.empty(shape, dtype=z.dtype, device=z.device)
+    ids = torch.empty(shape, dtype=torch.int32, device=z.device)
+    need = L.cprune_top_logits_workspace_bytes(rows, classes, k, dtype)
+    ws, ws_at = _scratch(need, z)
+    st = L.cprune_top_logits(z.data_ptr(), rows, classes, pitch, k, dtype, values.data_ptr(), ids.data_ptr(), ws_at, need, _raw_stream())
+    if st:
+        _check(st, "cprune_top_logits")
+    return values, ids
+
+
+def _distill(z, ids, teacher, labels, temperature, hard, dloss=None):
+    """-> (descriptor, addresses of ids, teacher, labels)"""
+    rows, classes, pitch, dtype = _mx4_rows(z)
+    lead = z.shape[:-1]
+    k = ids.shape[-1] if ids.dim() else 0
+    teacher_dtype = DTYPE_OF_TORCH.get(teacher.dtype)
+    if teacher_dtype is None:
+        _refuse(f"no teacher in {teacher.dtype}")
+    _one_device(z, ids, teacher, labels, dloss)
+    d = DistillDesc(rows, classes, k, dtype, teacher_dtype, pitch, temperature, hard)
+    return d, _on_gpu(ids, torch.int32, lead + (k,)), _on_gpu(teacher, teacher.dtype, lead + (k,)), \
+        None if labels is None else _on_gpu(labels, torch.int32, lead)
+
+
+def cprune_distill_loss(z: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, labels: Optional[torch.Tensor] = None, temperature: float = 1.0,
+                        hard: float = 0.0, want_stats: bool = False, stream=None):
+    """z [..., classes], the student's logits; ids int32 [..., k] (-1: no entry) and teacher [..., k], a teacher's largest ones; labels int32 [...]
+    (-1: none), counted by `hard`.  -> loss fp32 [...], or (loss, stats fp32 [3, rows]) for the backward call."""
+    if stream is not None:
+        return _on(stream, cprune_distill_loss, z, ids, teacher, labels, temperature, hard, want_stats)
+    L = _lib or lib()
+    d, ids_at, teacher_at, labels_at = _distill(z, ids, teacher, labels, temperature, hard)
+    loss = torch.empty(z.shape[:-1], dtype=torch.float32, device=z.device)
+    stats = torch.empty(3, d.rows, dtype=torch.float32, device=z.device) if want_stats else None
+    need = L.cprune_distill_workspace_bytes(d)
+    ws, ws_at = _scratch(need, z)
+    st = L.cprune_distill_loss(d, z.data_ptr(), ids_at, teacher_at, labels_at, loss.data_ptr(), None if stats is None else stats.data_ptr(), ws_at, need,
+                               _raw_stream())
+    if st:
+        _check(st, "cprune_distill_loss")
+    return (loss, stats) if want_stats else loss
+
+
+def cprune_distill_loss_backward(dloss: torch.Tensor, z: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, stats: torch.Tensor,
+                                 labels: Optional[torch.Tensor] = None, temperature: float = 1.0, hard: float = 0.0, stream=None) -> torch.Tensor:
+    """The gradient of cprune_distill_loss at z, with dloss fp32 [...] what the rows' losses count: -> dz dense, the type of z."""
+    if stream is not None:
+        return _on(stream, cprune_distill_loss_backward, dloss, z, ids, teacher, stats, labels, temperature, hard)
+    L = _lib or lib()
+    d, ids_at, teacher_at, labels_at = _distill(z, ids, teacher, labels, temperature, hard, dloss)
+    _one_device(z, stats)
+    dz = _dense_like(z)
+    st = L.cprune_distill_loss_backward(d, _on_gpu(dloss, torch.float32, z.shape[:-1]), z.data_ptr(), ids_at, teacher_at, labels_at,
+                                        _on_gpu(stats, torch.float32, (3, d.rows)), dz.data_ptr(), _raw_stream())
+    if st:
+        _check(st, "cprune_distill_loss_backward")
+    return dz
+
+
+def cprune_distill_step(dloss: torch.Tensor, z: torch.Tensor, ids: torch.Tensor, teacher: torch.Tensor, labels: Optional[torch.Tensor] = None,
+                        temperature: float = 1.0, hard: float = 0.0, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Loss and gradient in one pass, where dloss, what the rows' losses count, is known before them: -> (loss fp32 [...], dz dense)."""
+    if stream is not None:
+        return _on(stream, cprune_distill_step, dloss, z, ids, teacher, labels, temperature, hard)
+    L = _lib or lib()
+    d, ids_at, teacher_at, labels_at = _distill(z, ids, teacher, labels, temperature, hard, dloss)
+    lead = z.shape[:-1]
+    loss = torch.empty(lead, dtype=torch.float32, device=z.device)
+    dz = _dense_like(z)
+    need = L.cprune_distill_workspace_bytes(d)
+    ws, ws_at = _scratch(need, z)
+    st = L.cprune_distill_step(d, _on_gpu(dloss, torch.float32, lead), z.data_ptr(), ids_at, teacher_at, labels_at, loss.data_ptr(), dz.data_ptr(),
+                               ws_at, need, _raw_stream())
+    if st:
+        _check(st, "cprune_distill_step")
+    return loss, dz
 
 
 # ---- search-side rules (host only) ----------------------------------------------

@@ -1,0 +1,121 @@
+// Rows of logits: what the top-logits and the distillation kernels share.
+//
+// A work-group has a row, or a run of one; a thread reads 16 bytes at a time, V numbers, vector t + i NT of the row its i-th.  Rows may begin at any element
+// (an odd number of classes, the first classes of wider rows): loads and stores of 16 bytes need the element's alignment only, and what is left past the last
+// whole vector goes by the element.  Places past a row's end hold -infinity, a class that is not there.
+#pragma once
+#include <cfloat>
+#include <type_traits>
+
+#include "common.hpp"
+
+namespace cprune {
+namespace logits {
+
+constexpr float kLog2e = 1.44269504f;
+
+template <typename T> struct Raw;
+template <> struct Raw<float> {
+  static constexpr int V = 4;
+  static constexpr unsigned kNone = 0xff800000u;
+};
+template <> struct Raw<_Float16> {
+  static constexpr int V = 8;
+  static constexpr unsigned kNone = 0xfc00fc00u;
+};
+template <> struct Raw<__bf16> {
+  static constexpr int V = 8;
+  static constexpr unsigned kNone = 0xff80ff80u;
+};
+
+template <typename T> __device__ __forceinline__ float widen(T v) { return (float)v; }
+template <> __device__ __forceinline__ float widen<__bf16>(__bf16 v) { return __uint_as_float((unsigned)__builtin_bit_cast(unsigned short, v) << 16); }
+
+template <typename T> __device__ __forceinline__ void unpack(const uint4& r, float (&x)[Raw<T>::V]) {
+  const unsigned w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (sizeof(T) == 4) {
+      x[i] = __uint_as_float(w[i]);
+    } else if constexpr (std::is_same<T, __bf16>::value) {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    } else {
+      x[2 * i] = (float)__builtin_bit_cast(_Float16, (unsigned short)w[i]);
+      x[2 * i + 1] = (float)__builtin_bit_cast(_Float16, (unsigned short)(w[i] >> 16));
+    }
+  }
+}
+
+// (What is held is unpacked again each time: without this the compiler keeps the unpacked numbers, twice the registers and more.)
+__device__ __forceinline__ void pin(uint4& r) { asm volatile("" : "+v"(r.x), "+v"(r.y), "+v"(r.z), "+v"(r.w)); }
+
+// `classes` numbers at p.
+template <typename T> struct Row {
+  static constexpr int V = Raw<T>::V;
+  const T* p;
+  int full, tail;      // whole vectors, numbers behind them
+  __device__ __forceinline__ Row(const T* p, int classes) : p(p), full(classes / V), tail(classes % V) {}
+  __device__ __forceinline__ int vectors() const { return full + (tail != 0); }
+  __device__ __forceinline__ uint4 load(int i) const {
+    typedef unsigned uint4u __attribute__((ext_vector_type(4), aligned(2)));
+    uint4 r = make_uint4(Raw<T>::kNone, Raw<T>::kNone, Raw<T>::kNone, Raw<T>::kNone);
+    if (i < full) {
+      const uint4u v = *reinterpret_cast<const uint4u*>(p + (long)i * V);
+      r = make_uint4(v.x, v.y, v.z, v.w);
+    } else if (i == full && tail) {
+      const T* const q = p + (long)i * V;
+      if constexpr (sizeof(T) == 4) {
+        unsigned v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = __float_as_uint(q[min(j, tail - 1)]);
+        r = make_uint4(v[0], tail > 1 ? v[1] : r.y, tail > 2 ? v[2] : r.z, r.w);
+      } else {
+        const unsigned short* const h = reinterpret_cast<const unsigned short*>(q);
+        unsigned v[8], w[4];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = h[min(j, tail - 1)];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = j < tail ? v[j] : Raw<T>::kNone & 0xffffu;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = v[2 * j] | v[2 * j + 1] << 16;
+        r = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+    return r;
+  }
+};
+
+template <typename T> __device__ __forceinline__ void store(T* p, int i, int full, int tail, const float (&x)[Raw<T>::V]) {
+  constexpr int V = Raw<T>::V;
+  typedef T outs __attribute__((ext_vector_type(V), aligned(2)));
+  if (i < full) {
+    outs v;
+#pragma unroll
+    for (int j = 0; j < V; ++j) v[j] = (T)x[j];
+    *reinterpret_cast<outs*>(p + (long)i * V) = v;
+  } else if (i == full) {
+#pragma unroll
+    for (int j = 0; j < V; ++j)
+      if (j < tail) p[(long)i * V + j] = (T)x[j];
+  }
+}
+
+// Largest of two, NaN where one is.
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+template <int V> __device__ __forceinline__ float largest(const float (&x)[V]) {
+  float m = x[0];
+#pragma unroll
+  for (int i = 1; i < V; ++i) m = larger(m, x[i]);
+  return m;
+}
+
+template <typename F> void with_type(int dtype, F&& f) {
+  if (dtype == CPRUNE_F32) f(float());
+  else if (dtype == CPRUNE_F16) f(_Float16());
+  else f(__bf16());
+}
+
+}  // namespace logits
+}  // namespace cprune
