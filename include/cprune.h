@@ -615,6 +615,46 @@ int cprune_distill_step(const cprune_distill_desc* d, const float* dloss, const 
                         const void* teacher, const int32_t* labels, float* loss, void* dz, void* ws, size_t ws_bytes,
                         void* stream);
 
+/* ------------------------------------------------------------------------
+ * Low-rank adapters beside a shared projection: what may still change of a layer whose own weights are 4-bit codes (cprune_mx4_linear gives its base), or
+ * several tuned variants of one network served at once, each row of a batch with its own.
+ *
+ *   hidden_r = scale_i A_i x_r,   y_r = act(base_r + B_i hidden_r),   i = which_r;   i outside [0, adapters): y_r = act(base_r), hidden_r = 0
+ *
+ * x          [rows][k] of dtype, rows x_stride elements apart
+ * a, b       dense [adapters][rank][k] and [adapters][c_out][rank] of dtype (an adapter of a smaller rank is filled up with zeros)
+ * which      int32 [rows], or NULL: every row has adapter 0
+ * scale      fp32 [adapters], or NULL: 1
+ * base       [rows][c_out] of dtype, rows base_stride apart, or NULL: 0
+ * y          dense [rows][c_out] of dtype, summed in 32 bits, rounded once; it may be base itself (dense), otherwise it overlaps no input
+ * hidden     fp32 [rows][rank], for the backward call, or NULL
+ * ws         cprune_adapter_workspace_bytes(d, backward) of scratch, 16-byte aligned; NULL where that is 0
+ *
+ * Backward, dy being the gradient of the sum before the activation and g_r = scale_i B_i^T dy_r:
+ *   dx_r = dx_base_r + A_i^T g_r,   dA_i = sum of g_r x_r^T,   dB_i = sum of dy_r hidden_r^T   over the rows of adapter i
+ * (rows without an adapter: dx_r = dx_base_r; adapters without rows: gradients of 0)
+ * dy         [rows][c_out] of dtype, rows dy_stride apart
+ * dx_base    [rows][k] of dtype, rows base_stride apart, or NULL: what reaches x through the projection
+ * dx         dense [rows][k] of dtype; it may be dx_base itself (dense)
+ * da, db     fp32, as a and b; dx, or da and db together, may be NULL
+ * Sums are in 32 bits, in a fixed order: repeated calls give identical bits.
+ * rank <= 128, adapters <= 1024, more: CPRUNE_ERR_UNSUPPORTED, and a workspace of 0. */
+typedef struct {
+  int32_t rows, k, c_out, rank, adapters;
+  int32_t dtype;       /* cprune_dtype of x, a, b, base, y, dy, dx */
+  int32_t act;         /* cprune_act; forward only */
+  int32_t mixed;       /* 1: which is given */
+  int32_t x_stride, base_stride, dy_stride; /* dy_stride: backward only; base_stride: where a base is given */
+} cprune_adapter_desc;
+size_t cprune_adapter_workspace_bytes(const cprune_adapter_desc* d, int backward);
+int cprune_adapter_linear(const cprune_adapter_desc* d, const void* x, const void* a, const void* b, const int32_t* which,
+                          const float* scale, const void* base, void* y, float* hidden, void* ws, size_t ws_bytes,
+                          void* stream);
+int cprune_adapter_linear_backward(const cprune_adapter_desc* d, const void* dy, const void* x, const float* hidden,
+                                   const void* a, const void* b, const int32_t* which, const float* scale,
+                                   const void* dx_base, void* dx, float* da, float* db, void* ws, size_t ws_bytes,
+                                   void* stream);
+
 /* ---- measured ceilings (for reporting kernel throughput against what the device
  * delivers, next to its datasheet peaks; the paper reports end-to-end rates only) ----
  * cprune_probe_mfma: rate of back-to-back dense MFMA instructions of `dtype` on register

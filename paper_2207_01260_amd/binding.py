@@ -47,6 +47,10 @@ class DistillDesc(C.Structure):
                [("temperature", C.c_float), ("hard", C.c_float)]
 
 
+class AdapterDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("rows", "k", "c_out", "rank", "adapters", "dtype", "act", "mixed", "x_stride", "base_stride", "dy_stride")]
+
+
 class PruneLayer(C.Structure):
     _fields_ = [("w", C.c_void_p)] + [(n, C.c_int32) for n in
                                       ("c_out", "c_in", "kh", "kw", "keep", "rows_from", "cols_from")] + \
@@ -90,6 +94,7 @@ EXPORTS = [
     "cprune_mx4_linear_workspace_bytes", "cprune_mx4_linear",
     "cprune_top_logits_workspace_bytes", "cprune_top_logits", "cprune_distill_workspace_bytes", "cprune_distill_loss",
     "cprune_distill_loss_backward", "cprune_distill_step",
+    "cprune_adapter_workspace_bytes", "cprune_adapter_linear", "cprune_adapter_linear_backward",
 ]
 
 _lib = None
@@ -135,7 +140,7 @@ def lib():
         L.cprune_mx4_linear_workspace_bytes.argtypes = [C.c_int] * 4
         L.cprune_mx4_linear.argtypes = [C.c_void_p] + [C.c_int] * 3 + [C.c_void_p] * 2 + [C.c_int, C.c_void_p, C.c_int, C.c_int] + \
             [C.c_void_p] * 2 + [C.c_size_t, C.c_void_p]
-        for name in ("cprune_top_logits_workspace_bytes", "cprune_distill_workspace_bytes"):
+        for name in ("cprune_top_logits_workspace_bytes", "cprune_distill_workspace_bytes", "cprune_adapter_workspace_bytes"):
             getattr(L, name).restype = C.c_size_t
         L.cprune_top_logits_workspace_bytes.argtypes = [C.c_int] * 4
         L.cprune_top_logits.argtypes = [C.c_void_p] + [C.c_int] * 5 + [C.c_void_p] * 3 + [C.c_size_t, C.c_void_p]
@@ -143,6 +148,9 @@ def lib():
         L.cprune_distill_loss.argtypes = [C.POINTER(DistillDesc)] + [C.c_void_p] * 7 + [C.c_size_t, C.c_void_p]
         L.cprune_distill_loss_backward.argtypes = [C.POINTER(DistillDesc)] + [C.c_void_p] * 8
         L.cprune_distill_step.argtypes = [C.POINTER(DistillDesc)] + [C.c_void_p] * 8 + [C.c_size_t, C.c_void_p]
+        L.cprune_adapter_workspace_bytes.argtypes = [C.POINTER(AdapterDesc), C.c_int]
+        L.cprune_adapter_linear.argtypes = [C.POINTER(AdapterDesc)] + [C.c_void_p] * 9 + [C.c_size_t, C.c_void_p]
+        L.cprune_adapter_linear_backward.argtypes = [C.POINTER(AdapterDesc)] + [C.c_void_p] * 12 + [C.c_size_t, C.c_void_p]
         _lib = L
     return _lib
 
@@ -861,6 +869,90 @@ def cprune_distill_step(dloss: torch.Tensor, z: torch.Tensor, ids: torch.Tensor,
     if st:
         _check(st, "cprune_distill_step")
     return loss, dz
+
+
+# ---- low-rank adapters -----------------------------------------------------------
+
+def _adapters(x, a, b, which, scale):
+    """-> (descriptor without act and further strides, addresses of a, b, which, scale)"""
+    rows, k, pitch, dtype = _mx4_rows(x)
+    if a.dim() != 3 or b.dim() != 3:
+        _refuse("a [adapters, rank, k], b [adapters, c_out, rank]")
+    n, rank = a.shape[:2]
+    c_out = b.shape[1]
+    if rows * c_out > _MOST or n * rank * max(k, c_out) > _MOST:
+        _refuse("fewer than 2^31 elements only")
+    d = AdapterDesc(rows, k, c_out, rank, n, dtype, 0, which is not None, pitch, 0, 0)
+    return d, _on_gpu(a, x.dtype, (n, rank, k)), _on_gpu(b, x.dtype, (n, c_out, rank)), \
+        None if which is None else _on_gpu(which, torch.int32, x.shape[:-1]), None if scale is None else _on_gpu(scale, torch.float32, (n,))
+
+
+def _beside(t: torch.Tensor, x: torch.Tensor, columns: int) -> int:
+    """Elements between the rows of t, which are as many as those of x."""
+    if not t.is_cuda or t.dtype != x.dtype or t.shape != x.shape[:-1] + (columns,):
+        _refuse(f"expected {x.dtype} {tuple(x.shape[:-1]) + (columns,)}, got {t.dtype} {tuple(t.shape)}")
+    return _rows_of(t, 0)[3]
+
+
+def cprune_adapter_linear(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, which: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
+                          base: Optional[torch.Tensor] = None, act: int = ACT_NONE, want_hidden: bool = False, out: Optional[torch.Tensor] = None, stream=None):
+    """x [..., k] (dense, or the first channels of wider rows), a [adapters, rank, k], b [adapters, c_out, rank], the type of x; which int32 [...], each row's
+    adapter (-1: none; not given: 0); scale fp32 [adapters]; base [..., c_out], what the shared projection made of x.
+    -> y [..., c_out], act(base + scale B A x), in `out` where that is given (base itself, for one); or (y, hidden fp32 [..., rank]) for the backward call."""
+    if stream is not None:
+        return _on(stream, cprune_adapter_linear, x, a, b, which, scale, base, act, want_hidden, out)
+    L = _lib or lib()
+    d, a_at, b_at, which_at, scale_at = _adapters(x, a, b, which, scale)
+    _one_device(x, a, b, which, scale, base, out)
+    d.act = act
+    shape = x.shape[:-1] + (d.c_out,)
+    base_at = None
+    if base is not None:
+        d.base_stride = _beside(base, x, d.c_out)
+        base_at = base.data_ptr()
+    y = torch.empty(shape, dtype=x.dtype, device=x.device) if out is None else out
+    y_at = y.data_ptr() if out is None else _on_gpu(out, x.dtype, shape)
+    hidden = hidden_at = None
+    if want_hidden:
+        hidden = torch.empty(x.shape[:-1] + (d.rank,), dtype=torch.float32, device=x.device)
+        hidden_at = hidden.data_ptr()
+    need = L.cprune_adapter_workspace_bytes(d, 0)
+    ws, ws_at = _scratch(need, x)
+    st = L.cprune_adapter_linear(d, x.data_ptr(), a_at, b_at, which_at, scale_at, base_at, y_at, hidden_at, ws_at, need, _raw_stream())
+    if st:
+        _check(st, "cprune_adapter_linear")
+    return (y, hidden) if want_hidden else y
+
+
+def cprune_adapter_linear_backward(dy: torch.Tensor, x: torch.Tensor, hidden: torch.Tensor, a: torch.Tensor, b: torch.Tensor,
+                                   which: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None, dx_base: Optional[torch.Tensor] = None,
+                                   want_dx: bool = True, want_weights: bool = True, stream=None):
+    """The gradients of cprune_adapter_linear, dy [..., c_out] being that of the sum before the activation; dx_base [..., k]: what reaches x through the projection.
+    -> (dx dense, da fp32, db fp32); None for what is not wanted."""
+    if stream is not None:
+        return _on(stream, cprune_adapter_linear_backward, dy, x, hidden, a, b, which, scale, dx_base, want_dx, want_weights)
+    L = _lib or lib()
+    d, a_at, b_at, which_at, scale_at = _adapters(x, a, b, which, scale)
+    _one_device(x, dy, hidden, a, b, which, scale, dx_base)
+    d.dy_stride = _beside(dy, x, d.c_out)
+    dx = da = db = dx_at = da_at = db_at = base_at = None
+    if want_dx:
+        dx = _dense_like(x)
+        dx_at = dx.data_ptr()
+        if dx_base is not None:
+            d.base_stride = _beside(dx_base, x, d.k)
+            base_at = dx_base.data_ptr()
+    if want_weights:
+        da = torch.empty(a.shape, dtype=torch.float32, device=x.device)
+        db = torch.empty(b.shape, dtype=torch.float32, device=x.device)
+        da_at, db_at = da.data_ptr(), db.data_ptr()
+    need = L.cprune_adapter_workspace_bytes(d, 1)
+    ws, ws_at = _scratch(need, x)
+    st = L.cprune_adapter_linear_backward(d, dy.data_ptr(), x.data_ptr(), _on_gpu(hidden, torch.float32, x.shape[:-1] + (d.rank,)), a_at, b_at, which_at, scale_at,
+                                          base_at, dx_at, da_at, db_at, ws_at, need, _raw_stream())
+    if st:
+        _check(st, "cprune_adapter_linear_backward")
+    return dx, da, db
 
 
 # ---- search-side rules (host only) ----------------------------------------------

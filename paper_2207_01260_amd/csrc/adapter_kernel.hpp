@@ -1,0 +1,563 @@
+// Low-rank adapters: hidden_r = scale_i A_i x_r, y_r = act(base_r + B_i hidden_r), and their gradients, i the row's adapter.
+//
+// Rows in tiles of 64 with one adapter: all rows in their order where there is one adapter, the rows of each adapter behind each other where a launch before has
+// sorted them (adapter_plan_kernel), or, up to 64 rows, those that a work-group finds with a ballot.  A tile's rows are gathered: a row is long, its place is not.
+//
+// Products on the matrix cores, operands straight from memory: 16 bytes of a row for each lane, lane l row l % 16 and the terms from 4 V times the step and V (l / 16)
+// on, V numbers of 16 bytes.  fp32 takes four instructions a step, one for each of a lane's four terms (the terms' order does not matter, both operands
+// have the same).
+//  - narrow: 64 rows of x against A (or of dy against B's transpose), 4 wavefronts sharing the terms, work-groups sharing long sums; bound by reading x.
+//  - widen: hidden against B (or g against A's transpose), 8 neighbouring results in each lane; bound by reading base and writing y.
+//  - outer: dy against hidden (x against g), summed over rows.  The terms are rows: a lane reads 16 bytes of V rows and turns the V x V numbers over in registers.
+//    Runs of rows leave sums, joined in a fixed order.  Bound by reading dy (x).
+// hidden and g are fp32; against 16-bit operands they go as bf16 parts, of 8 bits each: two for y and dx, whose own rounding is 2^-8 or 2^-11 (what is
+// left is under 2^-15 of a term), three for dA and dB in fp32, which are all of it.  An fp16 operand beside them is two bf16 parts itself, exactly.
+#pragma once
+#include <type_traits>
+
+#include "conv_kernel.hpp"
+
+namespace cprune {
+
+constexpr int kTileRows = 64;
+
+// Places: tile t has rows order[64 t .. 64 t + 63], -1 where it has fewer.
+struct AdapterTiles {
+  const int* which;        // few: the rows' adapters, a ballot finds the tile of row t if that is its first
+  const int* order;        // sorted, or null: row 64 t + i
+  const int* tile_of;      // sorted: adapter of a tile, -1 for rows without; past the last tile -2
+  int rows, adapters;
+  bool few;
+};
+
+struct NarrowArgs {
+  AdapterTiles tiles;
+  const void* x;           // [rows][stride]
+  long stride;
+  int k, rank;
+  const void* a;           // [adapters][rank][k]
+  float* part;             // [splits][rows][RP]
+  int splits, per;         // work-groups that share a sum, steps of each
+};
+
+struct WidenArgs {
+  AdapterTiles tiles;
+  const float* part;       // [splits][rows][RP]
+  int splits, rank;
+  const float* scale;      // or null
+  const void* b;           // [adapters][c][b_stride], rank numbers of each row
+  int c, b_stride;
+  const void* base;
+  long base_stride;
+  void* y;                 // [rows][c]
+  float* hidden;           // [rows][rank] or null
+  float lo, hi;
+  int columns;             // of a work-group, a multiple of 128
+};
+
+// hidden and g as the outer product's operands: 16-bit, three bf16 parts [3][RP][places], fp32 [RP][places]
+struct PartsArgs {
+  AdapterTiles tiles;
+  const float* part;       // g: [splits][rows][RP]
+  int splits;
+  const float* hidden;     // [rows][rank]
+  const float* scale;
+  int rank, places;
+  void *g_out, *hidden_out;
+  float* g;                // [rows][RP], summed and scaled; or null
+};
+
+struct OuterSide {
+  const void* x;           // [rows][stride]
+  long stride;
+  int c;                   // columns
+  const void* parts;       // the other operand
+  float* sums;             // [spans][c][RP], or [spans][RP][c] (across)
+  int groups;              // work-groups for a span
+};
+struct OuterArgs {
+  AdapterTiles tiles;
+  OuterSide side[2];       // dy and hidden; x and g
+  int rank, places;
+  const int* span_first;   // [spans + 1] first tile of a span; sorted only
+  int span_tiles, tile_count;   // otherwise: tiles of a span, all tiles
+};
+
+struct AdapterLaunch {
+  unsigned grid;
+  int ranks;               // RP / 16, RP the rank filled up to 16, 32, 64 or 128
+  bool silu;
+};
+enum AdapterPass { kAdapterNarrow, kAdapterWiden, kAdapterParts, kAdapterOuter };
+void launch_adapter_f32(AdapterPass pass, const void* args, const AdapterLaunch& l, hipStream_t s);
+void launch_adapter_f16(AdapterPass pass, const void* args, const AdapterLaunch& l, hipStream_t s);
+void launch_adapter_bf16(AdapterPass pass, const void* args, const AdapterLaunch& l, hipStream_t s);
+
+namespace adapter {
+
+template <typename T> constexpr int kV = 16 / (int)sizeof(T);       // numbers of 16 bytes
+template <typename T> constexpr int kStep = 4 * kV<T>;              // terms of a step
+
+// V numbers at p, of which `valid` are there, zeros past them
+template <typename T> __device__ __forceinline__ uint4 load(const T* p, int valid) {
+  typedef unsigned uint4u __attribute__((ext_vector_type(4), aligned(2)));
+  if (valid >= kV<T>) {
+    const uint4u v = *reinterpret_cast<const uint4u*>(p);
+    return make_uint4(v.x, v.y, v.z, v.w);
+  }
+  if (valid <= 0) return make_uint4(0, 0, 0, 0);
+  unsigned w[4];
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(p[min(i, valid - 1)]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = i < valid ? w[i] : 0u;
+  } else {
+    const unsigned short* const h = reinterpret_cast<const unsigned short*>(p);
+    unsigned v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = h[min(i, valid - 1)];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = (2 * i < valid ? v[2 * i] : 0u) | (2 * i + 1 < valid ? v[2 * i + 1] << 16 : 0u);
+  }
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// result v of lane l: row 4 (l / 16) + v of the first operand, l % 16 of the second
+template <typename T> __device__ __forceinline__ float4_t mma(const uint4& a, const uint4& b, float4_t acc) {
+  if constexpr (sizeof(T) == 4) {
+    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.x), __uint_as_float(b.x), acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.y), __uint_as_float(b.y), acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.z), __uint_as_float(b.z), acc, 0, 0, 0);
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.w), __uint_as_float(b.w), acc, 0, 0, 0);
+  } else if constexpr (std::is_same<T, _Float16>::value) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, a), __builtin_bit_cast(half8_t, b), acc, 0, 0, 0);
+  } else {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), acc, 0, 0, 0);
+  }
+}
+
+// Numbers in fp32 as bf16 parts: the first 8 bits, cut off, then of what is left; three parts are all 24 (an infinity is the first part alone)
+__device__ __forceinline__ float part_of(float& left) {
+  const float p = __uint_as_float(__float_as_uint(left) & 0xffff0000u);
+  left = __builtin_isinf(left) ? 0.0f : left - p;
+  return p;
+}
+__device__ __forceinline__ unsigned pair(float a, float b) { return __float_as_uint(a) >> 16 | (__float_as_uint(b) & 0xffff0000u); }
+template <int N> __device__ __forceinline__ void parts_of(float (&v)[8], uint4 (&p)[N]) {
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = part_of(v[i]);
+    p[n] = make_uint4(pair(f[0], f[1]), pair(f[2], f[3]), pair(f[4], f[5]), pair(f[6], f[7]));
+  }
+}
+// eight fp16 numbers as two bf16 parts
+__device__ __forceinline__ void halves_of(const uint4& r, uint4 (&p)[2]) {
+  const half8_t h = __builtin_bit_cast(half8_t, r);
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = (float)h[i];
+  parts_of<2>(v, p);
+}
+
+// What an operand of memory and N parts of an fp32 one make; a and p either way round (SWAP: p's are the first operand)
+template <typename T, int N, bool SWAP> __device__ __forceinline__ float4_t mma_parts(const uint4& a, const uint4 (&p)[N], float4_t acc) {
+  auto go = [&](const uint4& u, const uint4& v) __attribute__((always_inline)) { acc = SWAP ? mma<__bf16>(v, u, acc) : mma<__bf16>(u, v, acc); };
+  if constexpr (std::is_same<T, _Float16>::value) {
+    uint4 h[2];
+    halves_of(a, h);
+#pragma unroll
+    for (int n = N == 2 ? 1 : N - 2; n >= 0; --n) go(h[1], p[n]);      // (past three parts of one: 2^-22 of a term)
+#pragma unroll
+    for (int n = N - 1; n >= 0; --n) go(h[0], p[n]);
+  } else {
+#pragma unroll
+    for (int n = N - 1; n >= 0; --n) go(a, p[n]);
+  }
+  return acc;
+}
+
+// A tile's adapter (-1: none, -2: no such tile) and rows, -1 where there are fewer; in LDS
+struct Tile {
+  int row[kTileRows];
+};
+__device__ __forceinline__ int open_tile(const AdapterTiles& t, int tile, Tile& out, int& count) {
+  const int i = (int)threadIdx.x;
+  int adapter = 0;
+  if (t.few) {
+    const int lane = i & 63;
+    int mine = lane < t.rows ? t.which[lane] : -2;
+    if (lane < t.rows && (unsigned)mine >= (unsigned)t.adapters) mine = -1;
+    adapter = __shfl(mine, tile, 64);
+    const unsigned long long same = __ballot(mine == adapter);
+    if (__ffsll(same) - 1 != tile) return -2;
+    count = __popcll(same);
+    if (i < kTileRows) {
+      out.row[i] = -1;
+    }
+    __syncthreads();
+    if (i < kTileRows && mine == adapter) out.row[__popcll(same & ((1ull << lane) - 1))] = lane;
+  } else if (t.order) {
+    adapter = t.tile_of[tile];
+    if (adapter == -2) return -2;
+    if (i < kTileRows) out.row[i] = t.order[tile * kTileRows + i];
+    count = kTileRows;
+  } else {
+    if (i < kTileRows) {
+      const int r = tile * kTileRows + i;
+      out.row[i] = r < t.rows ? r : -1;
+    }
+    count = min(kTileRows, t.rows - tile * kTileRows);
+    if (t.adapters < 1) adapter = -1;
+  }
+  __syncthreads();
+  return adapter;
+}
+
+// ---- narrow ----------------------------------------------------------------------
+
+template <typename T, int NR>
+__global__ __launch_bounds__(256) void adapter_narrow_kernel(const NarrowArgs p) {
+  constexpr int V = kV<T>, STEP = kStep<T>, RP = 16 * NR, U = NR <= 2 ? 4 : 2;
+  __shared__ Tile tile;
+  __shared__ float sums[4][16][RP + 4];
+  const int t = (int)threadIdx.x, lane = t & 63, wave = t >> 6, quarter = lane >> 4, lrow = lane & 15;
+  const int tile_no = blockIdx.x / (unsigned)p.splits, split = blockIdx.x - tile_no * p.splits;
+  int count;
+  const int adapter = open_tile(p.tiles, tile_no, tile, count);
+  if (adapter < 0) return;      // (rows without an adapter: what would be read here is known to be 0)
+  const T* const a = static_cast<const T*>(p.a) + (long)adapter * p.rank * p.k;
+  const T* rows[4];
+  bool there[4];
+#pragma unroll
+  for (int f = 0; f < 4; ++f) {
+    const int r = tile.row[16 * f + lrow];
+    there[f] = r >= 0;
+    rows[f] = static_cast<const T*>(p.x) + (long)max(r, 0) * p.stride + quarter * V;
+  }
+  float4_t acc[4][NR];
+#pragma unroll
+  for (int f = 0; f < 4; ++f)
+#pragma unroll
+    for (int n = 0; n < NR; ++n) acc[f][n] = (float4_t){0.f, 0.f, 0.f, 0.f};
+  const int frags = (count + 15) / 16;
+  const int first = split * p.per, steps = min(p.per, (p.k - 1) / STEP + 1 - first);
+  // a wavefront has every fourth U steps
+  for (int s = first + wave * U; s < first + steps; s += 4 * U) {
+    uint4 xs[U][4], as[U][NR];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int at = (s + u) * STEP, valid = s + u < first + steps ? p.k - at - quarter * V : 0;
+#pragma unroll
+      for (int f = 0; f < 4; ++f)
+        if (f < frags) xs[u][f] = load(rows[f] + at, there[f] ? valid : 0);
+#pragma unroll
+      for (int n = 0; n < NR; ++n) {
+        const int j = 16 * n + lrow;
+        as[u][n] = load(a + (long)j * p.k + at + quarter * V, j < p.rank ? valid : 0);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int f = 0; f < 4; ++f)
+        if (f < frags) {
+#pragma unroll
+          for (int n = 0; n < NR; ++n) acc[f][n] = mma<T>(as[u][n], xs[u][f], acc[f][n]);
+        }
+  }
+#pragma unroll
+  for (int f = 0; f < 4; ++f) {
+    if (f >= frags) break;
+    if (f) __syncthreads();
+#pragma unroll
+    for (int n = 0; n < NR; ++n) *reinterpret_cast<float4_t*>(&sums[wave][lrow][16 * n + 4 * quarter]) = acc[f][n];
+    __syncthreads();
+    for (int i = t; i < 16 * RP / 4; i += 256) {
+      const int r = i / (RP / 4), j = 4 * (i - r * (RP / 4)), row = tile.row[16 * f + r];
+      if (row < 0) continue;
+      float4_t v = *reinterpret_cast<const float4_t*>(&sums[0][r][j]);
+#pragma unroll
+      for (int w = 1; w < 4; ++w) v += *reinterpret_cast<const float4_t*>(&sums[w][r][j]);
+      *reinterpret_cast<float4_t*>(p.part + ((long)split * p.tiles.rows + row) * RP + j) = v;
+    }
+  }
+}
+
+// ---- widen -----------------------------------------------------------------------
+
+template <typename T, int NR, bool SILU>
+__global__ __launch_bounds__(256) void adapter_widen_kernel(const WidenArgs p) {
+  constexpr int V = kV<T>, STEP = kStep<T>, RP = 16 * NR, NS = (RP + STEP - 1) / STEP, N = sizeof(T) == 4 ? 1 : 2;
+  __shared__ Tile tile;
+  __shared__ float hidden[kTileRows][NS * STEP + 4];
+  const int t = (int)threadIdx.x, lane = t & 63, wave = t >> 6, quarter = lane >> 4, lrow = lane & 15;
+  const int chunks = (p.c - 1) / p.columns + 1;
+  const int tile_no = blockIdx.x / (unsigned)chunks, chunk = blockIdx.x - tile_no * chunks;
+  int count;
+  const int adapter = open_tile(p.tiles, tile_no, tile, count);
+  if (adapter == -2) return;
+  const int frags = (count + 15) / 16;
+  // the rows' hidden numbers, zeros past the rank
+  const float scale = adapter >= 0 && p.scale ? p.scale[adapter] : 1.0f;
+  for (int i = t; i < 16 * frags * NS * STEP / 4; i += 256) {
+    const int r = i / (NS * STEP / 4), j = 4 * (i - r * (NS * STEP / 4)), row = tile.row[r];
+    float4_t v = {0.f, 0.f, 0.f, 0.f};
+    if (row >= 0 && adapter >= 0 && j < RP) {
+      const float* const from = p.part + (long)row * RP + j;
+      for (int s = 0; s < p.splits; ++s) v += *reinterpret_cast<const float4_t*>(from + (long)s * p.tiles.rows * RP);
+      v *= scale;
+    }
+    *reinterpret_cast<float4_t*>(&hidden[r][j]) = v;
+    if (p.hidden && chunk == 0 && row >= 0) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (j + e < p.rank) p.hidden[(long)row * p.rank + j + e] = v[e];
+    }
+  }
+  __syncthreads();
+  uint4 h[4][NS][N];
+  int rows[4];
+#pragma unroll
+  for (int f = 0; f < 4; ++f) {
+    rows[f] = tile.row[16 * f + lrow];
+    if (f >= frags) continue;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      const float* const from = &hidden[16 * f + lrow][s * STEP + quarter * V];
+      if constexpr (sizeof(T) == 4) {
+        h[f][s][0] = *reinterpret_cast<const uint4*>(from);
+      } else {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = from[e];
+        parts_of<N>(v, h[f][s]);
+      }
+    }
+  }
+  const T* const b = static_cast<const T*>(p.b) + (long)max(adapter, 0) * p.c * p.b_stride;
+  const int end = min(p.c, (chunk + 1) * p.columns);
+  // 32 columns at a time: a lane has eight neighbouring ones of them, from the two operands whose rows are taken so
+  for (int c0 = chunk * p.columns + 32 * wave; c0 < end; c0 += 128) {
+    uint4 w[2][NS];
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const int c = c0 + (lrow >> 2) * 8 + g * 4 + (lrow & 3);
+#pragma unroll
+      for (int s = 0; s < NS; ++s) w[g][s] = load(b + (long)c * p.b_stride + s * STEP + quarter * V, c < p.c && adapter >= 0 ? p.rank - s * STEP - quarter * V : 0);
+    }
+    const int c = c0 + 8 * quarter, valid = p.c - c;
+#pragma unroll
+    for (int f = 0; f < 4; ++f) {
+      if (f >= frags) break;
+      float4_t acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+      for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+          if constexpr (sizeof(T) == 4) acc[g] = mma<float>(w[g][s], h[f][s][0], acc[g]);
+          else acc[g] = mma_parts<T, N, false>(w[g][s], h[f][s], acc[g]);
+        }
+      if (rows[f] < 0 || valid <= 0) continue;
+      float v[8] = {acc[0][0], acc[0][1], acc[0][2], acc[0][3], acc[1][0], acc[1][1], acc[1][2], acc[1][3]};
+      typedef T numbers __attribute__((ext_vector_type(V)));
+      if (p.base) {
+        const T* const from = static_cast<const T*>(p.base) + (long)rows[f] * p.base_stride + c;
+#pragma unroll
+        for (int q = 0; q < 8; q += V) {
+          const numbers z = __builtin_bit_cast(numbers, load(from + q, valid - q));
+#pragma unroll
+          for (int e = 0; e < V; ++e) v[q + e] += Elem<T>::to_f32(z[e]);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if constexpr (SILU) {
+          v[e] = v[e] * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v[e] * -1.44269504f));      // (2^x flushes below 2^-126: 1 + e^-z does not see it)
+        } else {
+          v[e] = v[e] < p.lo ? p.lo : v[e];      // (comparisons and not minimum / maximum: a NaN stays one)
+          v[e] = v[e] > p.hi ? p.hi : v[e];
+        }
+      }
+      T* const to = static_cast<T*>(p.y) + (long)rows[f] * p.c + c;
+      typedef T outs __attribute__((ext_vector_type(V), aligned(2)));
+#pragma unroll
+      for (int q = 0; q < 8; q += V) {
+        outs o;
+#pragma unroll
+        for (int e = 0; e < V; ++e) o[e] = Elem<T>::from_f32(v[q + e]);
+        if (valid - q >= V) {
+          *reinterpret_cast<outs*>(to + q) = o;
+        } else {
+#pragma unroll
+          for (int e = 0; e < V; ++e)
+            if (q + e < valid) to[q + e] = o[e];
+        }
+      }
+    }
+  }
+}
+
+// ---- operands of the outer products ----------------------------------------------
+
+// A work-group has a tile: 64 places of every rank; 8 (4) neighbouring places a thread.
+template <typename T, int NR>
+__global__ __launch_bounds__(256) void adapter_parts_kernel(const PartsArgs p) {
+  constexpr int V = kV<T>, RP = 16 * NR, N = sizeof(T) == 4 ? 1 : 3;
+  __shared__ Tile tile;
+  const int t = (int)threadIdx.x;
+  int count;
+  const int adapter = open_tile(p.tiles, blockIdx.x, tile, count);
+  if (adapter == -2) return;
+  const float scale = adapter >= 0 && p.scale ? p.scale[adapter] : 1.0f;
+  // ranks of a place lie side by side in memory, places of a rank in what is written: through the caches
+  for (int i = t; i < RP * kTileRows / V; i += 256) {
+    const int j = i % RP, at = i / RP * V;
+    float g[V], h[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const int row = tile.row[at + e];
+      g[e] = h[e] = 0.0f;
+      if (row >= 0 && adapter >= 0) {
+        for (int s = 0; s < p.splits; ++s) g[e] += p.part[((long)s * p.tiles.rows + row) * RP + j];
+        g[e] *= scale;
+        if (p.g_out && j < p.rank) h[e] = p.hidden[(long)row * p.rank + j];
+      }
+      if (p.g && row >= 0) p.g[(long)row * RP + j] = g[e];
+    }
+    if (!p.g_out) continue;
+    const long to = (long)j * p.places + blockIdx.x * kTileRows + at, part = (long)RP * p.places;
+    if constexpr (sizeof(T) == 4) {
+      *reinterpret_cast<float4_t*>(static_cast<float*>(p.g_out) + to) = (float4_t){g[0], g[1], g[2], g[3]};
+      *reinterpret_cast<float4_t*>(static_cast<float*>(p.hidden_out) + to) = (float4_t){h[0], h[1], h[2], h[3]};
+    } else {
+      uint4 q[N];
+      parts_of<N>(g, q);
+#pragma unroll
+      for (int n = 0; n < N; ++n) *reinterpret_cast<uint4*>(static_cast<__bf16*>(p.g_out) + n * part + to) = q[n];
+      parts_of<N>(h, q);
+#pragma unroll
+      for (int n = 0; n < N; ++n) *reinterpret_cast<uint4*>(static_cast<__bf16*>(p.hidden_out) + n * part + to) = q[n];
+    }
+  }
+}
+
+// ---- outer -----------------------------------------------------------------------
+
+// V rows of V numbers, turned over: out[i] has number i of every row
+template <typename T> __device__ __forceinline__ void turn(const uint4 (&r)[kV<T>], uint4 (&out)[kV<T>]) {
+  if constexpr (sizeof(T) == 4) {
+    out[0] = make_uint4(r[0].x, r[1].x, r[2].x, r[3].x);
+    out[1] = make_uint4(r[0].y, r[1].y, r[2].y, r[3].y);
+    out[2] = make_uint4(r[0].z, r[1].z, r[2].z, r[3].z);
+    out[3] = make_uint4(r[0].w, r[1].w, r[2].w, r[3].w);
+  } else {
+    auto word = [](const uint4& v, int i) __attribute__((always_inline)) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; };
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      unsigned w[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) w[q] = __builtin_amdgcn_perm(word(r[2 * q + 1], i / 2), word(r[2 * q], i / 2), i & 1 ? 0x07060302u : 0x05040100u);
+      out[i] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+  }
+}
+
+// A wavefront has 16 V columns of a span of tiles with one adapter, all ranks; ACROSS: results lie [rank][column] instead of [column][rank].
+template <typename T, int NR, bool ACROSS>
+__device__ __forceinline__ void outer_side(const OuterArgs& p, const OuterSide& side, int span, int group, int first, int last) {
+  constexpr int V = kV<T>, STEP = kStep<T>, RP = 16 * NR, N = sizeof(T) == 4 ? 1 : 3;
+  const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, quarter = lane >> 4, lrow = lane & 15;
+  const int c = (group * 4 + wave) * 16 * V + lrow * V, valid = side.c - c;
+  float4_t acc[V][NR];
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+#pragma unroll
+    for (int n = 0; n < NR; ++n) acc[i][n] = (float4_t){0.f, 0.f, 0.f, 0.f};
+  const T* const x = static_cast<const T*>(side.x) + c;
+  const long part = (long)RP * p.places;
+  for (int at = first * kTileRows; at < last * kTileRows; at += STEP) {
+    uint4 r[V], turned[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const int place = at + quarter * V + e;
+      const int row = p.tiles.order ? p.tiles.order[place] : place < p.tiles.rows ? place : -1;
+      r[e] = load(x + (long)max(row, 0) * side.stride, row >= 0 ? valid : 0);
+    }
+    turn<T>(r, turned);
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      const long from = (long)(16 * n + lrow) * p.places + at + quarter * V;
+      uint4 q[N];
+#pragma unroll
+      for (int m = 0; m < N; ++m) {
+        if constexpr (sizeof(T) == 4) q[m] = *reinterpret_cast<const uint4*>(static_cast<const float*>(side.parts) + from);
+        else q[m] = *reinterpret_cast<const uint4*>(static_cast<const __bf16*>(side.parts) + m * part + from);
+      }
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        if constexpr (sizeof(T) == 4) acc[i][n] = ACROSS ? mma<float>(q[0], turned[i], acc[i][n]) : mma<float>(turned[i], q[0], acc[i][n]);
+        else acc[i][n] = mma_parts<T, N, ACROSS>(turned[i], q, acc[i][n]);
+      }
+    }
+  }
+  float* const sums = side.sums + (long)span * side.c * RP;
+  if constexpr (ACROSS) {      // a lane's results: ranks 16 n + 4 quarter + v, columns c + i
+#pragma unroll
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+      for (int v = 0; v < 4; ++v)
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+          if (i < valid) sums[(long)(16 * n + 4 * quarter + v) * side.c + c + i] = acc[i][n][v];
+  } else {                     // columns V (4 quarter + v) + i of the wavefront's, ranks 16 n + lrow
+    const int c0 = (group * 4 + wave) * 16 * V;
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        const int col = c0 + V * (4 * quarter + v) + i;
+        if (col < side.c) {
+#pragma unroll
+          for (int n = 0; n < NR; ++n) sums[(long)col * RP + 16 * n + lrow] = acc[i][n][v];
+        }
+      }
+  }
+}
+
+template <typename T, int NR>
+__global__ __launch_bounds__(256) void adapter_outer_kernel(const OuterArgs p) {
+  const int groups = p.side[0].groups + p.side[1].groups;
+  const int span = blockIdx.x / (unsigned)groups;
+  int group = blockIdx.x - span * groups;
+  int first, last;
+  if (p.span_first) {
+    first = p.span_first[span], last = p.span_first[span + 1];
+    if (last <= first) return;      // (as many spans as there may be)
+  } else {
+    first = span * p.span_tiles, last = min(first + p.span_tiles, p.tile_count);
+  }
+  if (group < p.side[0].groups) outer_side<T, NR, false>(p, p.side[0], span, group, first, last);
+  else outer_side<T, NR, true>(p, p.side[1], span, group - p.side[0].groups, first, last);
+}
+
+template <typename T, int NR> void launch_ranks(AdapterPass pass, const void* args, const AdapterLaunch& l, hipStream_t s) {
+  if (pass == kAdapterNarrow) adapter_narrow_kernel<T, NR><<<l.grid, 256, 0, s>>>(*static_cast<const NarrowArgs*>(args));
+  else if (pass == kAdapterParts) adapter_parts_kernel<T, NR><<<l.grid, 256, 0, s>>>(*static_cast<const PartsArgs*>(args));
+  else if (pass == kAdapterOuter) adapter_outer_kernel<T, NR><<<l.grid, 256, 0, s>>>(*static_cast<const OuterArgs*>(args));
+  else if (l.silu) adapter_widen_kernel<T, NR, true><<<l.grid, 256, 0, s>>>(*static_cast<const WidenArgs*>(args));
+  else adapter_widen_kernel<T, NR, false><<<l.grid, 256, 0, s>>>(*static_cast<const WidenArgs*>(args));
+}
+
+}  // namespace adapter
+
+template <typename T> void launch_adapter(AdapterPass pass, const void* args, const AdapterLaunch& l, hipStream_t s) {
+  if (l.ranks == 1) adapter::launch_ranks<T, 1>(pass, args, l, s);
+  else if (l.ranks == 2) adapter::launch_ranks<T, 2>(pass, args, l, s);
+  else if (l.ranks == 4) adapter::launch_ranks<T, 4>(pass, args, l, s);
+  else adapter::launch_ranks<T, 8>(pass, args, l, s);
+}
+
+}  // namespace cprune
