@@ -13,12 +13,13 @@ constexpr int kFewRows = 64;      // rows that a wavefront's ballot sorts
 struct SortArgs {
   const int* which;
   int rows, adapters, places, span_tiles, spans;
+  int waves;                 // that walk
   int *order, *tile_of;      // [places], [places / 64]
   int *span_first;           // [spans + 1]
   int *span_of;              // [adapters + 1], an adapter's first span
 };
 
-constexpr int kSortWaves = 8;
+constexpr int kSortWaves = 16;
 
 // last of n + 1 ascending numbers in `from` that is not past x
 __device__ __forceinline__ int last_of(const int* from, int n, int x) {
@@ -31,37 +32,46 @@ __device__ __forceinline__ int last_of(const int* from, int n, int x) {
   return lo;
 }
 
-// One work-group: the rows of each adapter behind each other in their order, in tiles of their own, rows without an adapter last.  Wavefronts count runs of rows,
-// a group of equal ones at a time, and place them on a second walk.
-__global__ __launch_bounds__(64 * kSortWaves) void adapter_sort_kernel(const SortArgs p) {
-  extern __shared__ int shared[];
-  __shared__ int2 waves[kSortWaves];
+// One work-group: the rows of each adapter behind each other in their order, in tiles of their own, rows without an adapter last.  Wavefronts count runs of rows and
+// place them on a second walk; in 64 rows the equal ones find each other by the bits of their adapter, and their first counts for all.
+__device__ void sort_rows(const SortArgs& p, int* shared, int2* waves) {
   const int t = (int)threadIdx.x, lane = t & 63, wave = t >> 6, n = p.adapters, buckets = n + 1, threads = 64 * kSortWaves;
   int* const count = shared;                              // [wavefront][bucket]
-  int* const tile_at = count + kSortWaves * buckets;      // [buckets + 1]
+  int* const tile_at = count + p.waves * buckets;      // [buckets + 1]
   int* const span_at = tile_at + buckets + 1;             // [adapters + 1]
-  for (int i = t; i < kSortWaves * buckets; i += threads) count[i] = 0;
+  for (int i = t; i < p.waves * buckets; i += threads) count[i] = 0;
   __syncthreads();
-  const int run = ((p.rows - 1) / threads + 1) * 64, from = (int)min((long)wave * run, (long)p.rows), end = (int)min((long)from + run, (long)p.rows);
+  const int run = ((p.rows - 1) / (64 * p.waves) + 1) * 64, from = (int)min((long)wave * run, (long)p.rows), end = (int)min((long)from + run, (long)p.rows);
+  const int bits = 32 - __clz(n);
   int* const mine = count + wave * buckets;
   auto walk = [&](auto&& place) __attribute__((always_inline)) {
-    for (int r0 = from; r0 < end; r0 += 64) {
-      const int r = r0 + lane;
-      int b = r < end ? p.which[r] : 0;
-      if ((unsigned)b >= (unsigned)n) b = n;
-      unsigned long long left = __ballot(r < end);
-      while (left) {
-        const int lead = __ffsll(left) - 1, value = __shfl(b, lead, 64);
-        const unsigned long long same = __ballot(r < end && b == value);
-        int at = 0;
-        if (lane == lead) {
-          at = mine[value];
-          mine[value] = at + __popcll(same);
+    for (int r0 = from; r0 < end; r0 += 64 * 16) {
+      int b[16];
+#pragma unroll
+      for (int u = 0; u < 16; ++u) {      // (all under way at once)
+        const int r = r0 + 64 * u + lane;
+        b[u] = r < end ? p.which[r] : -1;
+      }
+#pragma unroll
+      for (int u = 0; u < 16; ++u) {
+        const int r = r0 + 64 * u + lane;
+        if (r - lane >= end) break;
+        const bool in = r < end;
+        const int v = (unsigned)b[u] < (unsigned)n ? b[u] : n;
+        unsigned long long same = __ballot(in);
+        if (__all(!in || v == __builtin_amdgcn_readfirstlane(v))) {
+          // (as in a long request's rows)
+        } else {
+          for (int i = 0; i < bits; ++i) {
+            const unsigned long long set = __ballot(v >> i & 1);
+            same &= v >> i & 1 ? set : ~set;
+          }
         }
-        at = __shfl(at, lead, 64);
-        if (same >> lane & 1) place(at + __popcll(same & ((1ull << lane) - 1)), r);
-        left &= ~same;
-        __builtin_amdgcn_wave_barrier();      // (the next of the same adapter may be another lane's)
+        const int lead = __ffsll(same) - 1;
+        int at = 0;
+        if (in && lane == lead) at = atomicAdd(&mine[v], __popcll(same));      // (the wavefront's own: in its order)
+        at = __shfl(at, lead & 63, 64);
+        if (in) place(at + __popcll(same & ((1ull << lane) - 1)), r);
       }
     }
   };
@@ -72,12 +82,12 @@ __global__ __launch_bounds__(64 * kSortWaves) void adapter_sort_kernel(const Sor
   int2 sum = {0, 0};
   auto tiles_of = [&](int b) {
     int rows = 0;
-    for (int w = 0; w < kSortWaves; ++w) rows += count[w * buckets + b];
-    return make_int2(rows, (rows + kTileRows - 1) / kTileRows);
+    for (int w = 0; w < p.waves; ++w) rows += count[w * buckets + b];
+    return (rows + kTileRows - 1) / kTileRows;
   };
   auto spans_of = [&](int b, int tiles) { return b < n ? (tiles + p.span_tiles - 1) / p.span_tiles : 0; };
   for (int b = b0; b < b1; ++b) {
-    const int tiles = tiles_of(b).y;
+    const int tiles = tiles_of(b);
     sum.x += tiles, sum.y += spans_of(b, tiles);
   }
   int2 before = sum;
@@ -90,16 +100,16 @@ __global__ __launch_bounds__(64 * kSortWaves) void adapter_sort_kernel(const Sor
   before.x -= sum.x, before.y -= sum.y;
   for (int w = 0; w < wave; ++w) before.x += waves[w].x, before.y += waves[w].y;
   for (int b = b0; b < b1; ++b) {
-    const int2 of = tiles_of(b);
+    const int tiles = tiles_of(b);
     tile_at[b] = before.x;
-    if (b <= n) span_at[b] = before.y;
+    span_at[b] = before.y;
     int at = before.x * kTileRows;
-    for (int w = 0; w < kSortWaves; ++w) {
+    for (int w = 0; w < p.waves; ++w) {
       const int c = count[w * buckets + b];
       count[w * buckets + b] = at;
       at += c;
     }
-    before.x += of.y, before.y += spans_of(b, of.y);
+    before.x += tiles, before.y += spans_of(b, tiles);
     for (; at < before.x * kTileRows; ++at) p.order[at] = -1;
     if (b == n) tile_at[buckets] = before.x;
   }
@@ -119,37 +129,88 @@ __global__ __launch_bounds__(64 * kSortWaves) void adapter_sort_kernel(const Sor
   walk([&](int at, int r) { p.order[at] = r; });
 }
 
-// A [adapter][rank][k] -> [adapter][k][padded], zeros past the rank; B [adapter][c][rank] -> [adapter][rank][c].  A thread has a column of one.
-template <typename T>
-__global__ __launch_bounds__(256) void adapter_turn_kernel(const T* __restrict__ a, const T* __restrict__ b, int adapters, int rank, int padded, int k, int c, T* __restrict__ at,
-                                                           T* __restrict__ bt) {
-  const unsigned i = blockIdx.x * 256u + threadIdx.x;
-  if (i < (unsigned)adapters * k) {
-    if (!at) return;
-    const unsigned n = i / k, col = i - n * k;
-    for (int j = 0; j < padded; ++j) at[(long)i * padded + j] = j < rank ? a[((long)n * rank + j) * k + col] : (T)0.0f;
-  } else if (i - (unsigned)adapters * k < (unsigned)adapters * c) {
-    const unsigned m = i - (unsigned)adapters * k, n = m / c, col = m - n * c;
-    for (int j = 0; j < rank; ++j) bt[((long)n * rank + j) * c + col] = b[(long)m * rank + j];
+// Matrices [rows][cols] one behind the other -> [cols][pitch], zeros from `rows` to the pitch; 64 x 64 of one through LDS.
+struct TurnArgs {
+  const void* from;
+  void* to;
+  int rows, cols, pitch;
+  int row_tiles, col_tiles;
+};
+template <typename T> __device__ __forceinline__ void turn_tile(const TurnArgs& p, int tile, T* shared) {
+  constexpr int PITCH = 65;
+  const int t = (int)threadIdx.x, lane = t & 63, line = t >> 6;
+  const int per = p.row_tiles * p.col_tiles, matrix = tile / per, in = tile - matrix * per, r0 = in / p.col_tiles * 64, c0 = in % p.col_tiles * 64;
+  const T* const from = static_cast<const T*>(p.from) + (long)matrix * p.rows * p.cols;
+  T* const to = static_cast<T*>(p.to) + (long)matrix * p.cols * p.pitch;
+  constexpr int LINES = kSortWaves, EACH = 64 / LINES;
+  T v[EACH];
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
+    const int r = r0 + line + LINES * i, c = c0 + lane;
+    v[i] = r < p.rows && c < p.cols ? from[(long)r * p.cols + c] : T(0);
+  }
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) shared[(line + LINES * i) * PITCH + lane] = v[i];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
+    const int c = c0 + line + LINES * i, r = r0 + lane;
+    if (c < p.cols && r < p.pitch) to[(long)c * p.pitch + r] = shared[lane * PITCH + line + LINES * i];
   }
 }
 
-// Sums of an adapter's spans, one behind the other: db [adapter][c][rank] from [span][c][RP], da [adapter][rank][k] from [span][RP][k].
+// What the products need first: the rows' order, by the first work-group where it is asked for, beside it the transposes of A, [k][rank filled up to eight],
+// and B, [rank][c].
+template <typename T>
+__global__ __launch_bounds__(64 * kSortWaves) void adapter_prepare_kernel(const SortArgs sort, const TurnArgs a, const TurnArgs b, int tiles_a) {
+  extern __shared__ int shared[];
+  __shared__ int2 waves[kSortWaves];
+  int i = blockIdx.x;
+  if (sort.which) {
+    if (i == 0) {
+      sort_rows(sort, shared, waves);
+      return;
+    }
+    --i;
+  }
+  if (i < tiles_a) turn_tile<T>(a, i, reinterpret_cast<T*>(shared));
+  else turn_tile<T>(b, i - tiles_a, reinterpret_cast<T*>(shared));
+}
+
+// Sums of an adapter's spans in their order: db [adapter][c][rank] from [span][c][RP], da [adapter][rank][k] from [span][RP][k].  Lanes share a result where there are
+// few: one of LANES threads has every LANES-th span.
+template <int LANES>
 __global__ __launch_bounds__(256) void adapter_join_kernel(const float* __restrict__ sums_b, const float* __restrict__ sums_a, const int* __restrict__ span_of, int spans, int adapters,
                                                            int rank, int rp, int k, int c, float* __restrict__ da, float* __restrict__ db) {
-  const long all_b = (long)adapters * c * rank, i = (long)blockIdx.x * 256 + threadIdx.x;
+  constexpr int RESULTS = 256 / LANES;
+  __shared__ float parts[256];
+  const int t = (int)threadIdx.x, in_group = t % RESULTS, turn = t / RESULTS;
+  const long all_b = (long)adapters * c * rank, all = all_b + (long)adapters * rank * k, i = (long)blockIdx.x * RESULTS + in_group;
   const bool of_b = i < all_b;
   const long m = of_b ? i : i - all_b;
-  if (!of_b && m >= (long)adapters * rank * k) return;
-  const long per = of_b ? (long)c * rank : (long)rank * k;
-  const int n = (int)(m / per);
-  const long in = m - n * per, pitch = of_b ? (long)c * rp : (long)rp * k;
-  const long at = of_b ? in / rank * rp + in % rank : in;
-  const int first = span_of ? span_of[n] : 0, last = span_of ? span_of[n + 1] : n == 0 ? spans : 0;
-  const float* const from = (of_b ? sums_b : sums_a) + at;
   float s = 0.0f;
-  for (int q = first; q < last; ++q) s += from[q * pitch];
-  (of_b ? db : da)[m] = s;
+  if (i < all) {
+    const long per = of_b ? (long)c * rank : (long)rank * k;
+    const int n = (int)(m / per);
+    const long in = m - n * per, pitch = of_b ? (long)c * rp : (long)rp * k;
+    const long at = of_b ? in / rank * rp + in % rank : in;
+    const int first = span_of ? span_of[n] : 0, last = span_of ? span_of[n + 1] : n == 0 ? spans : 0;
+    const float* const from = (of_b ? sums_b : sums_a) + at;
+    int q = first + turn;
+    for (; q + 3 * LANES < last; q += 4 * LANES) {
+      const float v[4] = {from[q * pitch], from[(q + LANES) * pitch], from[(q + 2 * LANES) * pitch], from[(q + 3 * LANES) * pitch]};
+      s += v[0], s += v[1], s += v[2], s += v[3];
+    }
+    for (; q < last; q += LANES) s += from[q * pitch];
+  }
+  if constexpr (LANES > 1) {
+    parts[t] = s;
+    __syncthreads();
+    if (turn) return;
+#pragma unroll
+    for (int l = 1; l < LANES; ++l) s += parts[l * RESULTS + in_group];
+  }
+  if (i < all) (of_b ? db : da)[m] = s;
 }
 
 // ---- host ------------------------------------------------------------------------
@@ -210,11 +271,11 @@ AdapterPlan plan_of(const cprune_adapter_desc& d, bool backward) {
   q.at = round256((size_t)d.adapters * d.k * q.padded * es);
   q.g = round256((size_t)d.rows * q.rp * sizeof(float));
   q.parts = round256((size_t)q.rp * q.places * (es == 4 ? 4 : 6));
-  const int wide = 4 * 16 * (16 / (int)es);      // columns of a work-group
+  const int wide = 16 * (16 / (int)es);      // columns of a work-group
   q.groups_b = (d.c_out - 1) / wide + 1, q.groups_a = (d.k - 1) / wide + 1;
   // spans: enough work-groups, and long enough that their sums are few beside what is read
-  const int groups = q.groups_a + q.groups_b, want = std::max(1, 1024 / groups);
-  q.span_tiles = std::max({1, (d.rows / kTileRows) / want, d.rank / 16});
+  const int groups = q.groups_a + q.groups_b, want = std::max(1, 768 / groups);
+  q.span_tiles = std::max(2, ((d.rows - 1) / kTileRows + want) / want);
   q.spans = q.sorted ? std::min(q.tiles, q.tiles / q.span_tiles + d.adapters) : (q.tiles - 1) / q.span_tiles + 1;
   if (q.sorted) {
     q.span_first = round256((size_t)(q.spans + 1) * sizeof(int));
@@ -229,9 +290,10 @@ AdapterPlan plan_of(const cprune_adapter_desc& d, bool backward) {
 bool fits(const cprune_adapter_desc& d, const AdapterPlan& q, bool backward) {
   const double most = 4294967296.0 / 256;
   const int c = backward ? d.k : d.c_out;
-  if ((double)q.tiles * q.splits >= most || (double)q.tiles * ((c - 1) / 128 + 1) >= most || (double)q.tiles * kTileRows >= 2147483648.0) return false;
+  if ((double)q.tiles * q.splits >= most || (double)q.tiles * ((c - 1) / 128 + 1) >= most || (double)q.tiles * kTileRows >= 2147483648.0 || (double)q.tiles * q.ranks >= most) return false;
   if (!backward) return true;
-  return (double)q.spans * (q.groups_a + q.groups_b) < most && (double)d.adapters * d.rank * ((double)d.k + d.c_out) < 4294967040.0;
+  const double turned = (double)d.adapters * ((d.k + 63.0) / 64 + (d.c_out + 63.0) / 64) * 2;      // (ranks of up to 128 are two tiles)
+  return turned < most / 4 - 1 && (double)q.spans * (q.groups_a + q.groups_b) < most && (double)d.adapters * d.rank * ((double)d.k + d.c_out) < 4294967040.0;
 }
 
 void launch(int dtype, AdapterPass pass, const void* args, const AdapterLaunch& l, hipStream_t s) {
@@ -255,17 +317,31 @@ AdapterTiles tiles_of(const cprune_adapter_desc& d, const AdapterPlan& q, const 
   return t;
 }
 
-void sort_rows(const cprune_adapter_desc& d, const AdapterPlan& q, AdapterTiles& t, int* span_first, int* span_of, Scratch& ws, hipStream_t s) {
-  int* const order = ws.take<int>(q.order);
-  int* const tile_of = ws.take<int>(q.tile_of);
-  const SortArgs a = {t.which, d.rows, d.adapters, q.places, std::max(1, q.span_tiles), q.spans, order, tile_of, span_first, span_of};
-  const size_t lds = ((size_t)kSortWaves * (d.adapters + 1) + 2 * d.adapters + 4) * sizeof(int);
-  adapter_sort_kernel<<<1, 64 * kSortWaves, lds, s>>>(a);
-  t.order = order, t.tile_of = tile_of;
+// The launch before the products; a, b: what is turned over, or empty
+void prepare(const cprune_adapter_desc& d, const AdapterPlan& q, AdapterTiles& t, int* span_first, int* span_of, const TurnArgs& a, const TurnArgs& b, Scratch& ws,
+             hipStream_t s) {
+  SortArgs sort = {};
+  if (q.sorted) {
+    int* const order = ws.take<int>(q.order);
+    int* const tile_of = ws.take<int>(q.tile_of);
+    sort = {t.which, d.rows, d.adapters, q.places, std::max(1, q.span_tiles), q.spans, d.adapters > 512 ? kSortWaves / 2 : kSortWaves, order, tile_of, span_first, span_of};
+    t.order = order, t.tile_of = tile_of;
+  }
+  const int tiles_a = a.row_tiles * a.col_tiles * d.adapters, tiles_b = b.row_tiles * b.col_tiles * d.adapters;
+  const unsigned grid = (unsigned)(q.sorted + tiles_a + tiles_b);
+  if (!grid) return;
+  const size_t es = dtype_size(d.dtype);
+  size_t lds = q.sorted ? ((size_t)sort.waves * (d.adapters + 1) + 2 * d.adapters + 4) * sizeof(int) : 0;
+  if (tiles_a + tiles_b) lds = std::max(lds, 64 * 65 * es);
+  if (es == 4) adapter_prepare_kernel<unsigned><<<grid, 64 * kSortWaves, lds, s>>>(sort, a, b, tiles_a);
+  else adapter_prepare_kernel<unsigned short><<<grid, 64 * kSortWaves, lds, s>>>(sort, a, b, tiles_a);
 }
 
+// What does not stay in the last-level cache (256 MB, shared with what else is in use) is stored past it.
+bool past_caches(const cprune_adapter_desc& d, int c, const void* base) { return (base ? 2.0 : 1.0) * d.rows * c * dtype_size(d.dtype) > 134217728.0; }
+
 int columns_of(const AdapterPlan& q, int c) {      // of a work-group: fewer where tiles are few
-  int columns = 512;
+  int columns = 1024;
   while (columns > 128 && (long)q.tiles * ((c - 1) / columns + 1) < 1024) columns /= 2;
   return columns;
 }
@@ -293,7 +369,7 @@ extern "C" int cprune_adapter_linear(const cprune_adapter_desc* d, const void* x
   hipStream_t s = static_cast<hipStream_t>(stream);
   Scratch scratch = {static_cast<char*>(ws)};
   AdapterTiles tiles = tiles_of(*d, q, which);
-  if (q.sorted) sort_rows(*d, q, tiles, nullptr, nullptr, scratch, s);
+  prepare(*d, q, tiles, nullptr, nullptr, {}, {}, scratch, s);
   float* const part = scratch.take<float>(q.part);
   AdapterLaunch l = {(unsigned)(q.tiles * q.splits), q.ranks, d->act == CPRUNE_ACT_SILU};
   const NarrowArgs n = {tiles, x, d->x_stride, d->k, d->rank, a, part, q.splits, q.per};
@@ -304,6 +380,7 @@ extern "C" int cprune_adapter_linear(const cprune_adapter_desc* d, const void* x
   w.base = base, w.base_stride = d->base_stride, w.y = y, w.hidden = hidden;
   w.lo = d->act == CPRUNE_ACT_NONE || d->act == CPRUNE_ACT_SILU ? -open : 0.0f, w.hi = d->act == CPRUNE_ACT_RELU6 ? 6.0f : open;
   w.columns = columns_of(q, d->c_out);
+  w.stream = past_caches(*d, d->c_out, base);
   l.grid = (unsigned)(q.tiles * ((d->c_out - 1) / w.columns + 1));
   launch(d->dtype, kAdapterWiden, &w, l, s);
   CPRUNE_LAUNCH_CHECK();
@@ -327,22 +404,17 @@ extern "C" int cprune_adapter_linear_backward(const cprune_adapter_desc* d, cons
   AdapterTiles tiles = tiles_of(*d, q, which);
   int* const span_first = scratch.take<int>(q.span_first);
   int* const span_of = scratch.take<int>(q.span_of);
-  if (q.sorted) sort_rows(*d, q, tiles, span_first, span_of, scratch, s);
-  float* const part = scratch.take<float>(q.part);
   char* const bt = scratch.take<char>(q.bt);
   char* const at = scratch.take<char>(q.at);
+  auto tiles64 = [](int n) { return (n + 63) / 64; };
+  const TurnArgs turn_a = {a, at, d->rank, d->k, q.padded, tiles64(q.padded), tiles64(d->k)}, turn_b = {b, bt, d->c_out, d->rank, d->c_out, tiles64(d->c_out), tiles64(d->rank)};
+  prepare(*d, q, tiles, span_first, span_of, dx ? turn_a : TurnArgs(), turn_b, scratch, s);
+  float* const part = scratch.take<float>(q.part);
   float* const g = scratch.take<float>(q.g);
   char* const g_parts = scratch.take<char>(q.parts);
   char* const hidden_parts = scratch.take<char>(q.parts);
   float* const sums_b = scratch.take<float>(q.sums_b);
   float* const sums_a = scratch.take<float>(q.sums_a);
-  const unsigned turns = (unsigned)(((long)d->adapters * ((long)d->k + d->c_out) + 255) / 256);
-  if (d->dtype == CPRUNE_F32)
-    adapter_turn_kernel<unsigned><<<turns, 256, 0, s>>>(static_cast<const unsigned*>(a), static_cast<const unsigned*>(b), d->adapters, d->rank, q.padded, d->k, d->c_out,
-                                                        dx ? reinterpret_cast<unsigned*>(at) : nullptr, reinterpret_cast<unsigned*>(bt));
-  else
-    adapter_turn_kernel<unsigned short><<<turns, 256, 0, s>>>(static_cast<const unsigned short*>(a), static_cast<const unsigned short*>(b), d->adapters, d->rank, q.padded, d->k,
-                                                              d->c_out, dx ? reinterpret_cast<unsigned short*>(at) : nullptr, reinterpret_cast<unsigned short*>(bt));
   AdapterLaunch l = {(unsigned)(q.tiles * q.splits), q.ranks, false};
   const NarrowArgs n = {tiles, dy, d->dy_stride, d->c_out, d->rank, bt, part, q.splits, q.per};
   launch(d->dtype, kAdapterNarrow, &n, l, s);
@@ -350,7 +422,7 @@ extern "C" int cprune_adapter_linear_backward(const cprune_adapter_desc* d, cons
   r.tiles = tiles, r.part = part, r.splits = q.splits, r.hidden = hidden, r.scale = scale, r.rank = d->rank, r.places = q.places;
   r.g = dx ? g : nullptr;
   if (da) r.g_out = g_parts, r.hidden_out = hidden_parts;
-  l.grid = (unsigned)q.tiles;
+  l.grid = (unsigned)(q.tiles * q.ranks);
   launch(d->dtype, kAdapterParts, &r, l, s);
   if (dx) {
     const float open = std::numeric_limits<float>::infinity();
@@ -358,6 +430,7 @@ extern "C" int cprune_adapter_linear_backward(const cprune_adapter_desc* d, cons
     w.tiles = tiles, w.part = g, w.splits = 1, w.rank = q.padded, w.b = at, w.c = d->k, w.b_stride = q.padded;
     w.base = dx_base, w.base_stride = d->base_stride, w.y = dx, w.lo = -open, w.hi = open;
     w.columns = columns_of(q, d->k);
+    w.stream = past_caches(*d, d->k, dx_base);
     l.grid = (unsigned)(q.tiles * ((d->k - 1) / w.columns + 1));
     launch(d->dtype, kAdapterWiden, &w, l, s);
   }
@@ -370,7 +443,12 @@ extern "C" int cprune_adapter_linear_backward(const cprune_adapter_desc* d, cons
     l.grid = (unsigned)(q.spans * (q.groups_a + q.groups_b));
     launch(d->dtype, kAdapterOuter, &o, l, s);
     const long all = (long)d->adapters * d->rank * ((long)d->k + d->c_out);
-    adapter_join_kernel<<<(unsigned)((all + 255) / 256), 256, 0, s>>>(sums_b, sums_a, span_of, q.spans, d->adapters, d->rank, q.rp, d->k, d->c_out, da, db);
+    auto join = [&](auto lanes) {
+      constexpr int LANES = decltype(lanes)::value;
+      adapter_join_kernel<LANES><<<(unsigned)((all * LANES + 255) / 256), 256, 0, s>>>(sums_b, sums_a, span_of, q.spans, d->adapters, d->rank, q.rp, d->k, d->c_out, da, db);
+    };
+    if (all <= 65536 && q.spans >= 8) join(std::integral_constant<int, 8>());
+    else join(std::integral_constant<int, 1>());
   }
   CPRUNE_LAUNCH_CHECK();
   return CPRUNE_OK;

@@ -53,6 +53,7 @@ struct WidenArgs {
   float* hidden;           // [rows][rank] or null
   float lo, hi;
   int columns;             // of a work-group, a multiple of 128
+  bool stream;             // y is stored past the caches
 };
 
 // hidden and g as the outer product's operands: 16-bit, three bf16 parts [3][RP][places], fp32 [RP][places]
@@ -216,6 +217,21 @@ __device__ __forceinline__ int open_tile(const AdapterTiles& t, int tile, Tile& 
   return adapter;
 }
 
+// four numbers of each of the splits' parts, added up; four loads under way
+__device__ __forceinline__ float4_t sum_parts(const float* from, int splits, long pitch) {
+  float4_t v = {0.f, 0.f, 0.f, 0.f};
+  int s = 0;
+  for (; s + 4 <= splits; s += 4) {
+    float4_t q[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) q[u] = *reinterpret_cast<const float4_t*>(from + (s + u) * pitch);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) v += q[u];
+  }
+  for (; s < splits; ++s) v += *reinterpret_cast<const float4_t*>(from + s * pitch);
+  return v;
+}
+
 // ---- narrow ----------------------------------------------------------------------
 
 template <typename T, int NR>
@@ -243,13 +259,14 @@ __global__ __launch_bounds__(256) void adapter_narrow_kernel(const NarrowArgs p)
 #pragma unroll
     for (int n = 0; n < NR; ++n) acc[f][n] = (float4_t){0.f, 0.f, 0.f, 0.f};
   const int frags = (count + 15) / 16;
-  const int first = split * p.per, steps = min(p.per, (p.k - 1) / STEP + 1 - first);
-  // a wavefront has every fourth U steps
-  for (int s = first + wave * U; s < first + steps; s += 4 * U) {
+  // a wavefront has a quarter of the work-group's steps
+  const int steps = min(p.per, (p.k - 1) / STEP + 1 - split * p.per), run = (steps + 3) / 4;
+  const int first = split * p.per + wave * run, last = min(first + run, split * p.per + steps);
+  for (int s = first; s < last; s += U) {
     uint4 xs[U][4], as[U][NR];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int at = (s + u) * STEP, valid = s + u < first + steps ? p.k - at - quarter * V : 0;
+      const int at = (s + u) * STEP, valid = s + u < last ? p.k - at - quarter * V : 0;
 #pragma unroll
       for (int f = 0; f < 4; ++f)
         if (f < frags) xs[u][f] = load(rows[f] + at, there[f] ? valid : 0);
@@ -290,7 +307,7 @@ __global__ __launch_bounds__(256) void adapter_narrow_kernel(const NarrowArgs p)
 
 template <typename T, int NR, bool SILU>
 __global__ __launch_bounds__(256) void adapter_widen_kernel(const WidenArgs p) {
-  constexpr int V = kV<T>, STEP = kStep<T>, RP = 16 * NR, NS = (RP + STEP - 1) / STEP, N = sizeof(T) == 4 ? 1 : 2;
+  constexpr int V = kV<T>, STEP = kStep<T>, RP = 16 * NR, NS = (RP + STEP - 1) / STEP, N = sizeof(T) == 4 ? 1 : 2, Q = 8 / V;
   __shared__ Tile tile;
   __shared__ float hidden[kTileRows][NS * STEP + 4];
   const int t = (int)threadIdx.x, lane = t & 63, wave = t >> 6, quarter = lane >> 4, lrow = lane & 15;
@@ -300,16 +317,41 @@ __global__ __launch_bounds__(256) void adapter_widen_kernel(const WidenArgs p) {
   const int adapter = open_tile(p.tiles, tile_no, tile, count);
   if (adapter == -2) return;
   const int frags = (count + 15) / 16;
+  int rows[4];
+#pragma unroll
+  for (int f = 0; f < 4; ++f) rows[f] = tile.row[16 * f + lrow];
+  // 32 columns at a time: a lane has eight neighbouring ones of them, from the two operands whose rows are taken so.  What a step needs from memory is asked for a
+  // step ahead.
+  const T* const b = static_cast<const T*>(p.b) + (long)max(adapter, 0) * p.c * p.b_stride;
+  const int run = p.columns / 4, begin = chunk * p.columns + wave * run, end = min(p.c, begin + run);
+  struct Step {
+    uint4 w[2][NS], z[4][Q];
+  };
+  auto fetch = [&](int c0, Step& q) __attribute__((always_inline)) {
+    if (p.base) {
+      const int c = c0 + 8 * quarter;
+#pragma unroll
+      for (int f = 0; f < 4; ++f)
+        if (f < frags) {
+#pragma unroll
+          for (int i = 0; i < Q; ++i) q.z[f][i] = load(static_cast<const T*>(p.base) + (long)max(rows[f], 0) * p.base_stride + c + i * V, rows[f] >= 0 ? p.c - c - i * V : 0);
+        }
+    }
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const int c = c0 + (lrow >> 2) * 8 + g * 4 + (lrow & 3);
+#pragma unroll
+      for (int s = 0; s < NS; ++s) q.w[g][s] = load(b + (long)c * p.b_stride + s * STEP + quarter * V, c < p.c && adapter >= 0 ? p.rank - s * STEP - quarter * V : 0);
+    }
+  };
+  Step now;
+  if (begin < end) fetch(begin, now);
   // the rows' hidden numbers, zeros past the rank
   const float scale = adapter >= 0 && p.scale ? p.scale[adapter] : 1.0f;
   for (int i = t; i < 16 * frags * NS * STEP / 4; i += 256) {
     const int r = i / (NS * STEP / 4), j = 4 * (i - r * (NS * STEP / 4)), row = tile.row[r];
     float4_t v = {0.f, 0.f, 0.f, 0.f};
-    if (row >= 0 && adapter >= 0 && j < RP) {
-      const float* const from = p.part + (long)row * RP + j;
-      for (int s = 0; s < p.splits; ++s) v += *reinterpret_cast<const float4_t*>(from + (long)s * p.tiles.rows * RP);
-      v *= scale;
-    }
+    if (row >= 0 && adapter >= 0 && j < RP) v = scale * sum_parts(p.part + (long)row * RP + j, p.splits, (long)p.tiles.rows * RP);
     *reinterpret_cast<float4_t*>(&hidden[r][j]) = v;
     if (p.hidden && chunk == 0 && row >= 0) {
 #pragma unroll
@@ -319,10 +361,8 @@ __global__ __launch_bounds__(256) void adapter_widen_kernel(const WidenArgs p) {
   }
   __syncthreads();
   uint4 h[4][NS][N];
-  int rows[4];
 #pragma unroll
   for (int f = 0; f < 4; ++f) {
-    rows[f] = tile.row[16 * f + lrow];
     if (f >= frags) continue;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
@@ -337,17 +377,9 @@ __global__ __launch_bounds__(256) void adapter_widen_kernel(const WidenArgs p) {
       }
     }
   }
-  const T* const b = static_cast<const T*>(p.b) + (long)max(adapter, 0) * p.c * p.b_stride;
-  const int end = min(p.c, (chunk + 1) * p.columns);
-  // 32 columns at a time: a lane has eight neighbouring ones of them, from the two operands whose rows are taken so
-  for (int c0 = chunk * p.columns + 32 * wave; c0 < end; c0 += 128) {
-    uint4 w[2][NS];
-#pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      const int c = c0 + (lrow >> 2) * 8 + g * 4 + (lrow & 3);
-#pragma unroll
-      for (int s = 0; s < NS; ++s) w[g][s] = load(b + (long)c * p.b_stride + s * STEP + quarter * V, c < p.c && adapter >= 0 ? p.rank - s * STEP - quarter * V : 0);
-    }
+  for (int c0 = begin; c0 < end; c0 += 32) {
+    Step next;
+    if (c0 + 32 < end) fetch(c0 + 32, next);
     const int c = c0 + 8 * quarter, valid = p.c - c;
 #pragma unroll
     for (int f = 0; f < 4; ++f) {
@@ -357,19 +389,18 @@ __global__ __launch_bounds__(256) void adapter_widen_kernel(const WidenArgs p) {
       for (int g = 0; g < 2; ++g)
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
-          if constexpr (sizeof(T) == 4) acc[g] = mma<float>(w[g][s], h[f][s][0], acc[g]);
-          else acc[g] = mma_parts<T, N, false>(w[g][s], h[f][s], acc[g]);
+          if constexpr (sizeof(T) == 4) acc[g] = mma<float>(now.w[g][s], h[f][s][0], acc[g]);
+          else acc[g] = mma_parts<T, N, false>(now.w[g][s], h[f][s], acc[g]);
         }
       if (rows[f] < 0 || valid <= 0) continue;
       float v[8] = {acc[0][0], acc[0][1], acc[0][2], acc[0][3], acc[1][0], acc[1][1], acc[1][2], acc[1][3]};
       typedef T numbers __attribute__((ext_vector_type(V)));
       if (p.base) {
-        const T* const from = static_cast<const T*>(p.base) + (long)rows[f] * p.base_stride + c;
 #pragma unroll
-        for (int q = 0; q < 8; q += V) {
-          const numbers z = __builtin_bit_cast(numbers, load(from + q, valid - q));
+        for (int i = 0; i < Q; ++i) {
+          const numbers z = __builtin_bit_cast(numbers, now.z[f][i]);
 #pragma unroll
-          for (int e = 0; e < V; ++e) v[q + e] += Elem<T>::to_f32(z[e]);
+          for (int e = 0; e < V; ++e) v[i * V + e] += Elem<T>::to_f32(z[e]);
         }
       }
 #pragma unroll
@@ -384,62 +415,70 @@ __global__ __launch_bounds__(256) void adapter_widen_kernel(const WidenArgs p) {
       T* const to = static_cast<T*>(p.y) + (long)rows[f] * p.c + c;
       typedef T outs __attribute__((ext_vector_type(V), aligned(2)));
 #pragma unroll
-      for (int q = 0; q < 8; q += V) {
+      for (int i = 0; i < 8; i += V) {
         outs o;
 #pragma unroll
-        for (int e = 0; e < V; ++e) o[e] = Elem<T>::from_f32(v[q + e]);
-        if (valid - q >= V) {
-          *reinterpret_cast<outs*>(to + q) = o;
+        for (int e = 0; e < V; ++e) o[e] = Elem<T>::from_f32(v[i + e]);
+        if (valid - i >= V) {
+          if (p.stream) __builtin_nontemporal_store(o, reinterpret_cast<outs*>(to + i));
+          else *reinterpret_cast<outs*>(to + i) = o;
         } else {
 #pragma unroll
           for (int e = 0; e < V; ++e)
-            if (q + e < valid) to[q + e] = o[e];
+            if (i + e < valid) to[i + e] = o[e];
         }
       }
     }
+    now = next;
   }
 }
 
 // ---- operands of the outer products ----------------------------------------------
 
-// A work-group has a tile: 64 places of every rank; 8 (4) neighbouring places a thread.
+// A work-group has 64 places of 16 ranks: read four ranks of a place at a time, turned over in LDS, written 8 (4) places of a rank at a time.
 template <typename T, int NR>
 __global__ __launch_bounds__(256) void adapter_parts_kernel(const PartsArgs p) {
   constexpr int V = kV<T>, RP = 16 * NR, N = sizeof(T) == 4 ? 1 : 3;
   __shared__ Tile tile;
-  const int t = (int)threadIdx.x;
+  __shared__ float turned[2][16][kTileRows + 4];
+  const int t = (int)threadIdx.x, tile_no = blockIdx.x / NR, j0 = 16 * (blockIdx.x - tile_no * NR);
   int count;
-  const int adapter = open_tile(p.tiles, blockIdx.x, tile, count);
+  const int adapter = open_tile(p.tiles, tile_no, tile, count);
   if (adapter == -2) return;
   const float scale = adapter >= 0 && p.scale ? p.scale[adapter] : 1.0f;
-  // ranks of a place lie side by side in memory, places of a rank in what is written: through the caches
-  for (int i = t; i < RP * kTileRows / V; i += 256) {
-    const int j = i % RP, at = i / RP * V;
-    float g[V], h[V];
+  {
+    const int place = t >> 2, j = 4 * (t & 3), row = tile.row[place];
+    float4_t g = {0.f, 0.f, 0.f, 0.f};
+    float h[4] = {0.f, 0.f, 0.f, 0.f};
+    if (row >= 0 && adapter >= 0) {
+      if (p.g_out) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      const int row = tile.row[at + e];
-      g[e] = h[e] = 0.0f;
-      if (row >= 0 && adapter >= 0) {
-        for (int s = 0; s < p.splits; ++s) g[e] += p.part[((long)s * p.tiles.rows + row) * RP + j];
-        g[e] *= scale;
-        if (p.g_out && j < p.rank) h[e] = p.hidden[(long)row * p.rank + j];
+        for (int e = 0; e < 4; ++e) h[e] = j0 + j + e < p.rank ? p.hidden[(long)row * p.rank + j0 + j + e] : 0.0f;
       }
-      if (p.g && row >= 0) p.g[(long)row * RP + j] = g[e];
+      g = scale * sum_parts(p.part + (long)row * RP + j0 + j, p.splits, (long)p.tiles.rows * RP);
     }
-    if (!p.g_out) continue;
-    const long to = (long)j * p.places + blockIdx.x * kTileRows + at, part = (long)RP * p.places;
+    if (p.g && row >= 0) *reinterpret_cast<float4_t*>(p.g + (long)row * RP + j0 + j) = g;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) turned[0][j + e][place] = g[e], turned[1][j + e][place] = h[e];
+  }
+  if (!p.g_out) return;
+  __syncthreads();
+  constexpr int PER = kTileRows / V;      // threads a rank
+  for (int i = t; i < 2 * 16 * PER; i += 256) {
+    const int which = i / (16 * PER), j = i / PER % 16, at = i % PER * V;
+    const float* const from = &turned[which][j][at];
+    void* const out = which ? p.hidden_out : p.g_out;
+    const long to = (long)(j0 + j) * p.places + tile_no * kTileRows + at;
     if constexpr (sizeof(T) == 4) {
-      *reinterpret_cast<float4_t*>(static_cast<float*>(p.g_out) + to) = (float4_t){g[0], g[1], g[2], g[3]};
-      *reinterpret_cast<float4_t*>(static_cast<float*>(p.hidden_out) + to) = (float4_t){h[0], h[1], h[2], h[3]};
+      *reinterpret_cast<float4_t*>(static_cast<float*>(out) + to) = *reinterpret_cast<const float4_t*>(from);
     } else {
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = from[e];
       uint4 q[N];
-      parts_of<N>(g, q);
+      parts_of<N>(v, q);
 #pragma unroll
-      for (int n = 0; n < N; ++n) *reinterpret_cast<uint4*>(static_cast<__bf16*>(p.g_out) + n * part + to) = q[n];
-      parts_of<N>(h, q);
-#pragma unroll
-      for (int n = 0; n < N; ++n) *reinterpret_cast<uint4*>(static_cast<__bf16*>(p.hidden_out) + n * part + to) = q[n];
+      for (int n = 0; n < N; ++n) *reinterpret_cast<uint4*>(static_cast<__bf16*>(out) + (long)n * RP * p.places + to) = q[n];
     }
   }
 }
@@ -465,12 +504,13 @@ template <typename T> __device__ __forceinline__ void turn(const uint4 (&r)[kV<T
   }
 }
 
-// A wavefront has 16 V columns of a span of tiles with one adapter, all ranks; ACROSS: results lie [rank][column] instead of [column][rank].
+// A work-group has 16 V columns of a span of tiles with one adapter, all ranks, its wavefronts every fourth step of the rows; ACROSS: results lie [rank][column]
+// instead of [column][rank].  A step's numbers are asked for a step ahead, its rows' places two.
 template <typename T, int NR, bool ACROSS>
-__device__ __forceinline__ void outer_side(const OuterArgs& p, const OuterSide& side, int span, int group, int first, int last) {
+__device__ __forceinline__ void outer_side(const OuterArgs& p, const OuterSide& side, int span, int group, int first, int last, float4_t* joined) {
   constexpr int V = kV<T>, STEP = kStep<T>, RP = 16 * NR, N = sizeof(T) == 4 ? 1 : 3;
   const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, quarter = lane >> 4, lrow = lane & 15;
-  const int c = (group * 4 + wave) * 16 * V + lrow * V, valid = side.c - c;
+  const int c0 = group * 16 * V, c = c0 + lrow * V, valid = side.c - c;
   float4_t acc[V][NR];
 #pragma unroll
   for (int i = 0; i < V; ++i)
@@ -478,57 +518,97 @@ __device__ __forceinline__ void outer_side(const OuterArgs& p, const OuterSide& 
     for (int n = 0; n < NR; ++n) acc[i][n] = (float4_t){0.f, 0.f, 0.f, 0.f};
   const T* const x = static_cast<const T*>(side.x) + c;
   const long part = (long)RP * p.places;
-  for (int at = first * kTileRows; at < last * kTileRows; at += STEP) {
-    uint4 r[V], turned[V];
+  const int end = last * kTileRows;
+  struct Rows {
+    int at[V];
+  };
+  auto find = [&](int at, Rows& rows) __attribute__((always_inline)) {      // (past the span: none)
+    const int place = at + quarter * V;
+    if (at >= end) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      const int place = at + quarter * V + e;
-      const int row = p.tiles.order ? p.tiles.order[place] : place < p.tiles.rows ? place : -1;
-      r[e] = load(x + (long)max(row, 0) * side.stride, row >= 0 ? valid : 0);
+      for (int e = 0; e < V; ++e) rows.at[e] = -1;
+    } else if (p.tiles.order) {
+#pragma unroll
+      for (int e = 0; e < V; e += 4) {
+        const int4 o = *reinterpret_cast<const int4*>(p.tiles.order + place + e);
+        rows.at[e] = o.x, rows.at[e + 1] = o.y, rows.at[e + 2] = o.z, rows.at[e + 3] = o.w;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e) rows.at[e] = place + e < p.tiles.rows ? place + e : -1;
     }
-    turn<T>(r, turned);
+  };
+  auto fetch = [&](const Rows& rows, uint4 (&r)[V]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) r[e] = load(x + (long)max(rows.at[e], 0) * side.stride, rows.at[e] >= 0 ? valid : 0);
+  };
+  int at = first * kTileRows + wave * STEP;
+  Rows ahead;
+  uint4 now[V];
+  find(at, ahead);
+  fetch(ahead, now);
+  find(at + 4 * STEP, ahead);
+  for (; at < end; at += 4 * STEP) {
+    uint4 q[NR][N];
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
       const long from = (long)(16 * n + lrow) * p.places + at + quarter * V;
-      uint4 q[N];
 #pragma unroll
       for (int m = 0; m < N; ++m) {
-        if constexpr (sizeof(T) == 4) q[m] = *reinterpret_cast<const uint4*>(static_cast<const float*>(side.parts) + from);
-        else q[m] = *reinterpret_cast<const uint4*>(static_cast<const __bf16*>(side.parts) + m * part + from);
-      }
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        if constexpr (sizeof(T) == 4) acc[i][n] = ACROSS ? mma<float>(q[0], turned[i], acc[i][n]) : mma<float>(turned[i], q[0], acc[i][n]);
-        else acc[i][n] = mma_parts<T, N, ACROSS>(turned[i], q, acc[i][n]);
+        if constexpr (sizeof(T) == 4) q[n][m] = *reinterpret_cast<const uint4*>(static_cast<const float*>(side.parts) + from);
+        else q[n][m] = *reinterpret_cast<const uint4*>(static_cast<const __bf16*>(side.parts) + m * part + from);
       }
     }
-  }
-  float* const sums = side.sums + (long)span * side.c * RP;
-  if constexpr (ACROSS) {      // a lane's results: ranks 16 n + 4 quarter + v, columns c + i
-#pragma unroll
-    for (int n = 0; n < NR; ++n)
-#pragma unroll
-      for (int v = 0; v < 4; ++v)
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-          if (i < valid) sums[(long)(16 * n + 4 * quarter + v) * side.c + c + i] = acc[i][n][v];
-  } else {                     // columns V (4 quarter + v) + i of the wavefront's, ranks 16 n + lrow
-    const int c0 = (group * 4 + wave) * 16 * V;
+    uint4 next[V], turned[V];
+    fetch(ahead, next);
+    find(at + 8 * STEP, ahead);
+    turn<T>(now, turned);
 #pragma unroll
     for (int i = 0; i < V; ++i)
 #pragma unroll
-      for (int v = 0; v < 4; ++v) {
-        const int col = c0 + V * (4 * quarter + v) + i;
-        if (col < side.c) {
+      for (int n = 0; n < NR; ++n) {
+        if constexpr (sizeof(T) == 4) acc[i][n] = ACROSS ? mma<float>(q[n][0], turned[i], acc[i][n]) : mma<float>(turned[i], q[n][0], acc[i][n]);
+        else acc[i][n] = mma_parts<T, N, ACROSS>(turned[i], q[n], acc[i][n]);
+      }
 #pragma unroll
-          for (int n = 0; n < NR; ++n) sums[(long)col * RP + 16 * n + lrow] = acc[i][n][v];
+    for (int e = 0; e < V; ++e) now[e] = next[e];
+  }
+  // the wavefronts' sums joined through LDS, 8 results of each at a time
+  float* const sums = side.sums + (long)span * side.c * RP;
+  constexpr int G = 8 / NR < V ? 8 / NR : V;
+#pragma unroll
+  for (int i0 = 0; i0 < V; i0 += G) {
+    if (i0) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < G; ++i)
+#pragma unroll
+      for (int n = 0; n < NR; ++n) joined[((i * NR + n) * 4 + wave) * 64 + lane] = acc[i0 + i][n];
+    __syncthreads();
+#pragma unroll
+    for (int m = 0; m < (G * NR + 3) / 4; ++m) {
+      const int item = m * 4 + wave, i = i0 + item / NR, n = item % NR;
+      if (item >= G * NR) break;
+      float4_t v = joined[item * 4 * 64 + lane];
+#pragma unroll
+      for (int w = 1; w < 4; ++w) v += joined[(item * 4 + w) * 64 + lane];
+      if constexpr (ACROSS) {      // ranks 16 n + 4 quarter + e, column c + i
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (i < valid) sums[(long)(16 * n + 4 * quarter + e) * side.c + c + i] = v[e];
+      } else {                     // columns V (4 quarter + e) + i, rank 16 n + lrow
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int col = c0 + V * (4 * quarter + e) + i;
+          if (col < side.c) sums[(long)col * RP + 16 * n + lrow] = v[e];
         }
       }
+    }
   }
 }
 
 template <typename T, int NR>
 __global__ __launch_bounds__(256) void adapter_outer_kernel(const OuterArgs p) {
+  __shared__ float4_t joined[8 * 4 * 64];
   const int groups = p.side[0].groups + p.side[1].groups;
   const int span = blockIdx.x / (unsigned)groups;
   int group = blockIdx.x - span * groups;
@@ -539,8 +619,8 @@ __global__ __launch_bounds__(256) void adapter_outer_kernel(const OuterArgs p) {
   } else {
     first = span * p.span_tiles, last = min(first + p.span_tiles, p.tile_count);
   }
-  if (group < p.side[0].groups) outer_side<T, NR, false>(p, p.side[0], span, group, first, last);
-  else outer_side<T, NR, true>(p, p.side[1], span, group - p.side[0].groups, first, last);
+  if (group < p.side[0].groups) outer_side<T, NR, false>(p, p.side[0], span, group, first, last, joined);
+  else outer_side<T, NR, true>(p, p.side[1], span, group - p.side[0].groups, first, last, joined);
 }
 
 template <typename T, int NR> void launch_ranks(AdapterPass pass, const void* args, const AdapterLaunch& l, hipStream_t s) {
