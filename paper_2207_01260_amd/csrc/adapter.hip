@@ -32,8 +32,8 @@ __device__ __forceinline__ int last_of(const int* from, int n, int x) {
   return lo;
 }
 
-// One work-group: the rows of each adapter behind each other in their order, in tiles of their own, rows without an adapter last.  Wavefronts count runs of rows and
-// place them on a second walk; in 64 rows the equal ones find each other by the bits of their adapter, and their first counts for all.
+// One work-group: the rows of each adapter behind each other in their order, in tiles of their own, rows without an adapter last.  Wavefronts count runs of rows, up to 1024
+// each at once, and place them behind what the others have counted; in 64 rows the equal ones find each other by the bits of their adapter, and their first counts for all.
 __device__ void sort_rows(const SortArgs& p, int* shared, int2* waves) {
   const int t = (int)threadIdx.x, lane = t & 63, wave = t >> 6, n = p.adapters, buckets = n + 1, threads = 64 * kSortWaves;
   int* const count = shared;                              // [wavefront][bucket]
@@ -44,38 +44,54 @@ __device__ void sort_rows(const SortArgs& p, int* shared, int2* waves) {
   const int run = ((p.rows - 1) / (64 * p.waves) + 1) * 64, from = (int)min((long)wave * run, (long)p.rows), end = (int)min((long)from + run, (long)p.rows);
   const int bits = 32 - __clz(n);
   int* const mine = count + wave * buckets;
-  auto walk = [&](auto&& place) __attribute__((always_inline)) {
-    for (int r0 = from; r0 < end; r0 += 64 * 16) {
-      int b[16];
+  // 16 times 64 rows: their adapters, all under way at once; then, of each, how many the wavefront has had of the same one before
+  auto load = [&](int r0, int (&b)[16]) __attribute__((always_inline)) {
 #pragma unroll
-      for (int u = 0; u < 16; ++u) {      // (all under way at once)
-        const int r = r0 + 64 * u + lane;
-        b[u] = r < end ? p.which[r] : -1;
-      }
+    for (int u = 0; u < 16; ++u) {
+      const int r = r0 + 64 * u + lane;
+      b[u] = r < end ? p.which[r] : -1;
+    }
 #pragma unroll
-      for (int u = 0; u < 16; ++u) {
-        const int r = r0 + 64 * u + lane;
-        if (r - lane >= end) break;
-        const bool in = r < end;
-        const int v = (unsigned)b[u] < (unsigned)n ? b[u] : n;
-        unsigned long long same = __ballot(in);
-        if (__all(!in || v == __builtin_amdgcn_readfirstlane(v))) {
-          // (as in a long request's rows)
-        } else {
-          for (int i = 0; i < bits; ++i) {
-            const unsigned long long set = __ballot(v >> i & 1);
-            same &= v >> i & 1 ? set : ~set;
-          }
-        }
-        const int lead = __ffsll(same) - 1;
-        int at = 0;
-        if (in && lane == lead) at = atomicAdd(&mine[v], __popcll(same));      // (the wavefront's own: in its order)
-        at = __shfl(at, lead & 63, 64);
-        if (in) place(at + __popcll(same & ((1ull << lane) - 1)), r);
+    for (int u = 0; u < 16; ++u) b[u] = (unsigned)b[u] < (unsigned)n ? b[u] : n;
+  };
+  auto match = [&](int r0, const int (&b)[16], int (&at)[16]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < 16; ++u) {
+      const int first = r0 + 64 * u;
+      if (first >= end) break;
+      const int v = b[u], one = __builtin_amdgcn_readfirstlane(v);
+      if (first + 64 <= end && __all(v == one)) {      // (as in a long request's rows)
+        int before = 0;
+        if (lane == 0) before = atomicAdd(&mine[one], 64);
+        at[u] = __builtin_amdgcn_readfirstlane(before) + lane;
+        continue;
       }
+      const bool in = first + lane < end;
+      unsigned long long same = __ballot(in);
+#pragma unroll 1
+      for (int i = 0; i < bits; ++i) {
+        const unsigned long long set = __ballot(v >> i & 1);
+        same &= v >> i & 1 ? set : ~set;
+      }
+      const int lead = __ffsll(same) - 1;
+      int before = 0;
+      if (in && lane == lead) before = atomicAdd(&mine[v], __popcll(same));      // (the wavefront's own: in its order)
+      at[u] = __shfl(before, lead & 63, 64) + __popcll(same & ((1ull << lane) - 1));
     }
   };
-  walk([](int, int) {});
+  auto place = [&](int r0, const int (&b)[16], const int (&at)[16], bool from_zero) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < 16; ++u) {
+      const int r = r0 + 64 * u + lane;
+      if (r < end) p.order[at[u] + (from_zero ? mine[b[u]] : 0)] = r;
+    }
+  };
+  int b[16], at[16];
+  const bool once = run <= 64 * 16;
+  for (int r0 = from; r0 < end; r0 += 64 * 16) {
+    load(r0, b);
+    match(r0, b, at);
+  }
   __syncthreads();
   // tiles and spans of each bucket, and where they begin
   const int each = (buckets - 1) / threads + 1, b0 = min(t * each, buckets), b1 = min(b0 + each, buckets);
@@ -126,7 +142,15 @@ __device__ void sort_rows(const SortArgs& p, int* shared, int2* waves) {
     }
     for (int i = t; i <= n; i += threads) p.span_of[i] = span_at[i];
   }
-  walk([&](int at, int r) { p.order[at] = r; });
+  if (once) {
+    if (from < end) place(from, b, at, true);
+    return;
+  }
+  for (int r0 = from; r0 < end; r0 += 64 * 16) {
+    load(r0, b);
+    match(r0, b, at);
+    place(r0, b, at, false);
+  }
 }
 
 // Matrices [rows][cols] one behind the other -> [cols][pitch], zeros from `rows` to the pitch; 64 x 64 of one through LDS.
@@ -257,7 +281,7 @@ AdapterPlan plan_of(const cprune_adapter_desc& d, bool backward) {
   q.places = (int)std::min(2147483647L, (long)q.tiles * kTileRows);      // (more is refused)
   // enough work-groups to bring x, each wavefront four steps at least
   const int terms = backward ? d.c_out : d.k, steps = (terms - 1) / q.step + 1;
-  const int splits = std::max(1, std::min({1024 / q.tiles, steps / 16, 16}));
+  const int splits = std::max(1, std::min({768 / q.tiles, steps / 16, 16}));
   q.per = (steps - 1) / splits + 1;
   q.splits = (steps - 1) / q.per + 1;
   q.part = round256((size_t)q.splits * d.rows * q.rp * sizeof(float));
@@ -290,7 +314,7 @@ AdapterPlan plan_of(const cprune_adapter_desc& d, bool backward) {
 bool fits(const cprune_adapter_desc& d, const AdapterPlan& q, bool backward) {
   const double most = 4294967296.0 / 256;
   const int c = backward ? d.k : d.c_out;
-  if ((double)q.tiles * q.splits >= most || (double)q.tiles * ((c - 1) / 128 + 1) >= most || (double)q.tiles * kTileRows >= 2147483648.0 || (double)q.tiles * q.ranks >= most) return false;
+  if ((double)q.tiles * q.splits >= most || (double)q.tiles * ((c - 1) / 256 + 1) >= most || (double)q.tiles * kTileRows >= 2147483648.0 || (double)q.tiles * q.ranks >= most) return false;
   if (!backward) return true;
   const double turned = (double)d.adapters * ((d.k + 63.0) / 64 + (d.c_out + 63.0) / 64) * 2;      // (ranks of up to 128 are two tiles)
   return turned < most / 4 - 1 && (double)q.spans * (q.groups_a + q.groups_b) < most && (double)d.adapters * d.rank * ((double)d.k + d.c_out) < 4294967040.0;
@@ -342,7 +366,7 @@ bool past_caches(const cprune_adapter_desc& d, int c, const void* base) { return
 
 int columns_of(const AdapterPlan& q, int c) {      // of a work-group: fewer where tiles are few
   int columns = 1024;
-  while (columns > 128 && (long)q.tiles * ((c - 1) / columns + 1) < 1024) columns /= 2;
+  while (columns > 256 && (long)q.tiles * ((c - 1) / columns + 1) < 512) columns /= 2;
   return columns;
 }
 

@@ -217,6 +217,12 @@ __device__ __forceinline__ int open_tile(const AdapterTiles& t, int tile, Tile& 
   return adapter;
 }
 
+// what a wavefront has written to LDS is there for its other lanes
+__device__ __forceinline__ void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
 // four numbers of each of the splits' parts, added up; four loads under way
 __device__ __forceinline__ float4_t sum_parts(const float* from, int splits, long pitch) {
   float4_t v = {0.f, 0.f, 0.f, 0.f};
@@ -236,7 +242,7 @@ __device__ __forceinline__ float4_t sum_parts(const float* from, int splits, lon
 
 template <typename T, int NR>
 __global__ __launch_bounds__(256) void adapter_narrow_kernel(const NarrowArgs p) {
-  constexpr int V = kV<T>, STEP = kStep<T>, RP = 16 * NR, U = NR <= 2 ? 4 : 2;
+  constexpr int V = kV<T>, STEP = kStep<T>, RP = 16 * NR, U = NR <= 2 ? 4 : NR <= 4 ? 2 : 1;
   __shared__ Tile tile;
   __shared__ float sums[4][16][RP + 4];
   const int t = (int)threadIdx.x, lane = t & 63, wave = t >> 6, quarter = lane >> 4, lrow = lane & 15;
@@ -307,8 +313,9 @@ __global__ __launch_bounds__(256) void adapter_narrow_kernel(const NarrowArgs p)
 
 template <typename T, int NR, bool SILU>
 __global__ __launch_bounds__(256) void adapter_widen_kernel(const WidenArgs p) {
-  constexpr int V = kV<T>, STEP = kStep<T>, RP = 16 * NR, NS = (RP + STEP - 1) / STEP, N = sizeof(T) == 4 ? 1 : 2, Q = 8 / V;
+  constexpr int V = kV<T>, STEP = kStep<T>, RP = 16 * NR, NS = (RP + STEP - 1) / STEP, N = sizeof(T) == 4 ? 1 : 2;
   __shared__ Tile tile;
+  __shared__ float results[4][16][64 + 4];
   __shared__ float hidden[kTileRows][NS * STEP + 4];
   const int t = (int)threadIdx.x, lane = t & 63, wave = t >> 6, quarter = lane >> 4, lrow = lane & 15;
   const int chunks = (p.c - 1) / p.columns + 1;
@@ -317,35 +324,19 @@ __global__ __launch_bounds__(256) void adapter_widen_kernel(const WidenArgs p) {
   const int adapter = open_tile(p.tiles, tile_no, tile, count);
   if (adapter == -2) return;
   const int frags = (count + 15) / 16;
-  int rows[4];
-#pragma unroll
-  for (int f = 0; f < 4; ++f) rows[f] = tile.row[16 * f + lrow];
-  // 32 columns at a time: a lane has eight neighbouring ones of them, from the two operands whose rows are taken so.  What a step needs from memory is asked for a
-  // step ahead.
+  // 64 columns at a time: the weights of the next ones are asked for before these are multiplied
   const T* const b = static_cast<const T*>(p.b) + (long)max(adapter, 0) * p.c * p.b_stride;
   const int run = p.columns / 4, begin = chunk * p.columns + wave * run, end = min(p.c, begin + run);
-  struct Step {
-    uint4 w[2][NS], z[4][Q];
-  };
-  auto fetch = [&](int c0, Step& q) __attribute__((always_inline)) {
-    if (p.base) {
-      const int c = c0 + 8 * quarter;
+  auto weights = [&](int c0, uint4 (&w)[4][NS]) __attribute__((always_inline)) {
 #pragma unroll
-      for (int f = 0; f < 4; ++f)
-        if (f < frags) {
+    for (int g = 0; g < 4; ++g) {
+      const int c = c0 + 16 * g + lrow;
 #pragma unroll
-          for (int i = 0; i < Q; ++i) q.z[f][i] = load(static_cast<const T*>(p.base) + (long)max(rows[f], 0) * p.base_stride + c + i * V, rows[f] >= 0 ? p.c - c - i * V : 0);
-        }
-    }
-#pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      const int c = c0 + (lrow >> 2) * 8 + g * 4 + (lrow & 3);
-#pragma unroll
-      for (int s = 0; s < NS; ++s) q.w[g][s] = load(b + (long)c * p.b_stride + s * STEP + quarter * V, c < p.c && adapter >= 0 ? p.rank - s * STEP - quarter * V : 0);
+      for (int s = 0; s < NS; ++s) w[g][s] = load(b + (long)c * p.b_stride + s * STEP + quarter * V, c < p.c && adapter >= 0 ? p.rank - s * STEP - quarter * V : 0);
     }
   };
-  Step now;
-  if (begin < end) fetch(begin, now);
+  uint4 w[4][NS];
+  if (begin < end) weights(begin, w);
   // the rows' hidden numbers, zeros past the rank
   const float scale = adapter >= 0 && p.scale ? p.scale[adapter] : 1.0f;
   for (int i = t; i < 16 * frags * NS * STEP / 4; i += 256) {
@@ -377,59 +368,85 @@ __global__ __launch_bounds__(256) void adapter_widen_kernel(const WidenArgs p) {
       }
     }
   }
-  for (int c0 = begin; c0 < end; c0 += 32) {
-    Step next;
-    if (c0 + 32 < end) fetch(c0 + 32, next);
-    const int c = c0 + 8 * quarter, valid = p.c - c;
+  // Results go through LDS, 16 rows of a wavefront at a time, so that base and y are met in whole lines: LINE lanes of 16 bytes a row
+  constexpr int LINE = 64 / V, EACH = 16 * LINE / 64;
+  float (*const out)[64 + 4] = results[wave];
+  const int line = lane / LINE, col = lane % LINE * V;
+  for (int c0 = begin; c0 < end; c0 += 64) {
+    const int c = c0 + col, valid = p.c - c;
+    uint4 z[4][EACH], next[4][NS];
+    if (p.base) {
+#pragma unroll
+      for (int f = 0; f < 4; ++f)
+        if (f < frags) {
+#pragma unroll
+          for (int i = 0; i < EACH; ++i) {
+            const int row = tile.row[16 * f + i * (64 / LINE) + line];
+            z[f][i] = load(static_cast<const T*>(p.base) + (long)max(row, 0) * p.base_stride + c, row >= 0 ? valid : 0);
+          }
+        }
+    }
+    if (c0 + 64 < end) weights(c0 + 64, next);
 #pragma unroll
     for (int f = 0; f < 4; ++f) {
       if (f >= frags) break;
-      float4_t acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-      for (int g = 0; g < 2; ++g)
+      for (int g = 0; g < 4; ++g) {
+        float4_t acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
-          if constexpr (sizeof(T) == 4) acc[g] = mma<float>(now.w[g][s], h[f][s][0], acc[g]);
-          else acc[g] = mma_parts<T, N, false>(now.w[g][s], h[f][s], acc[g]);
+          if constexpr (sizeof(T) == 4) acc = mma<float>(w[g][s], h[f][s][0], acc);
+          else acc = mma_parts<T, N, false>(w[g][s], h[f][s], acc);
         }
-      if (rows[f] < 0 || valid <= 0) continue;
-      float v[8] = {acc[0][0], acc[0][1], acc[0][2], acc[0][3], acc[1][0], acc[1][1], acc[1][2], acc[1][3]};
-      typedef T numbers __attribute__((ext_vector_type(V)));
-      if (p.base) {
-#pragma unroll
-        for (int i = 0; i < Q; ++i) {
-          const numbers z = __builtin_bit_cast(numbers, now.z[f][i]);
-#pragma unroll
-          for (int e = 0; e < V; ++e) v[i * V + e] += Elem<T>::to_f32(z[e]);
-        }
+        *reinterpret_cast<float4_t*>(&out[lrow][16 * g + 4 * quarter]) = acc;
       }
+      wave_sync();
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        if constexpr (SILU) {
-          v[e] = v[e] * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v[e] * -1.44269504f));      // (2^x flushes below 2^-126: 1 + e^-z does not see it)
-        } else {
-          v[e] = v[e] < p.lo ? p.lo : v[e];      // (comparisons and not minimum / maximum: a NaN stays one)
-          v[e] = v[e] > p.hi ? p.hi : v[e];
+      for (int i = 0; i < EACH; ++i) {
+        const int in = i * (64 / LINE) + line, row = tile.row[16 * f + in];
+        float v[V];
+#pragma unroll
+        for (int e = 0; e < V; e += 4) {
+          const float4_t q = *reinterpret_cast<const float4_t*>(&out[in][col + e]);
+#pragma unroll
+          for (int u = 0; u < 4; ++u) v[e + u] = q[u];
         }
-      }
-      T* const to = static_cast<T*>(p.y) + (long)rows[f] * p.c + c;
-      typedef T outs __attribute__((ext_vector_type(V), aligned(2)));
+        if (p.base) {
+          typedef T numbers __attribute__((ext_vector_type(V)));
+          const numbers n = __builtin_bit_cast(numbers, z[f][i]);
 #pragma unroll
-      for (int i = 0; i < 8; i += V) {
+          for (int e = 0; e < V; ++e) v[e] += Elem<T>::to_f32(n[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          if constexpr (SILU) {
+            v[e] = v[e] * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v[e] * -1.44269504f));      // (2^x flushes below 2^-126: 1 + e^-z does not see it)
+          } else {
+            v[e] = v[e] < p.lo ? p.lo : v[e];      // (comparisons and not minimum / maximum: a NaN stays one)
+            v[e] = v[e] > p.hi ? p.hi : v[e];
+          }
+        }
+        if (row < 0) continue;
+        T* const to = static_cast<T*>(p.y) + (long)row * p.c + c;
+        typedef T outs __attribute__((ext_vector_type(V), aligned(2)));
         outs o;
 #pragma unroll
-        for (int e = 0; e < V; ++e) o[e] = Elem<T>::from_f32(v[i + e]);
-        if (valid - i >= V) {
-          if (p.stream) __builtin_nontemporal_store(o, reinterpret_cast<outs*>(to + i));
-          else *reinterpret_cast<outs*>(to + i) = o;
+        for (int e = 0; e < V; ++e) o[e] = Elem<T>::from_f32(v[e]);
+        if (valid >= V) {
+          if (p.stream) __builtin_nontemporal_store(o, reinterpret_cast<outs*>(to));
+          else *reinterpret_cast<outs*>(to) = o;
         } else {
 #pragma unroll
           for (int e = 0; e < V; ++e)
-            if (i + e < valid) to[i + e] = o[e];
+            if (e < valid) to[e] = o[e];
         }
       }
+      wave_sync();
     }
-    now = next;
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+      for (int s = 0; s < NS; ++s) w[g][s] = next[g][s];
   }
 }
 

@@ -211,6 +211,10 @@ struct Slope {
     if constexpr (TWO) v += exp2_of(d * kLog2e) * by_1;
     return v;
   }
+  template <bool TWO, int V> __device__ __forceinline__ void over(float (&x)[V], float scale) const {
+#pragma unroll
+    for (int j = 0; j < V; ++j) x[j] = none ? 0.0f : at<TWO>(x[j], scale);
+  }
 };
 
 // LDS of a work-group with a row or a run of one
@@ -243,11 +247,12 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(const DistillArgs a) {
   List l;
   if (wave == 0) l.load(a, row_no);
   uint4 held[NV ? NV : 1];
-  const int rounds = NV ? NV : (row.vectors() + NT - 1) / NT;
   if constexpr (NV != 0) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) held[i] = row.load(t + i * NT);
+    for (int i = 0; i < NV; ++i) held[i] = row.load(t + i * NT, row.full);
   }
+  float edge[V];
+  row.edge(t == NT - 1, edge);
   if (wave == 0) {
     l.read<T>(a, row.p);
     if (a.dz) sh.shares.put(l, a.k);
@@ -263,10 +268,11 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(const DistillArgs a) {
       s.add(x, a.scale);
     }
   } else {
-    for (int i = 0; i < rounds; i += 8) {
+#pragma unroll 1
+    for (int i = t; i - lane < row.full; i += 8 * NT) {      // (whole wavefronts)
       uint4 r[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) r[u] = row.load(t + (i + u) * NT);
+      for (int u = 0; u < 8; ++u) r[u] = row.load(i + u * NT, row.full);
 #pragma unroll
       for (int u = 0; u < 8; ++u) {
         float x[V];
@@ -275,6 +281,7 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(const DistillArgs a) {
       }
     }
   }
+  if (row.tail) s.add(edge, a.scale);
   s.over_wave(a.scale);
   if (lane == 0) sh.sums[wave] = make_float4(s.m, s.at_t, s.at_1, 0.0f);
   __syncthreads();
@@ -307,9 +314,8 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(const DistillArgs a) {
   auto out = [&](int i, const uint4& r) __attribute__((always_inline)) {
     float x[V];
     logits::unpack<T>(r, x);
-#pragma unroll
-    for (int j = 0; j < V; ++j) x[j] = g.none ? 0.0f : g.at<TWO>(x[j], a.scale);
-    logits::store<T>(dz, i, row.full, row.tail, x);
+    g.over<TWO>(x, a.scale);
+    if (i < row.full) logits::store<T>(dz, i, x);
   };
   if constexpr (NV != 0) {
 #pragma unroll
@@ -318,13 +324,18 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(const DistillArgs a) {
       out(t + i * NT, held[i]);
     }
   } else {
-    for (int i = 0; i < rounds; i += 8) {
+#pragma unroll 1
+    for (int i = t; i < row.full; i += 8 * NT) {
       uint4 r[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) r[u] = row.load(t + (i + u) * NT);
+      for (int u = 0; u < 8; ++u) r[u] = row.load(i + u * NT, row.full);
 #pragma unroll
-      for (int u = 0; u < 8; ++u) out(t + (i + u) * NT, r[u]);
+      for (int u = 0; u < 8; ++u) out(i + u * NT, r[u]);
     }
+  }
+  if (t == NT - 1) {
+    g.over<TWO>(edge, a.scale);
+    logits::store_edge<T>(dz, row, edge);
   }
   __syncthreads();
   if (wave == 0 && !g.none) patch<T, TWO>(a, l, sh.shares, g, dz, 0, a.classes);
@@ -337,18 +348,24 @@ __global__ __launch_bounds__(256) void distill_parts_kernel(const DistillArgs a)
   __shared__ float4 sums[4];
   const int t = (int)threadIdx.x, lane = t & 63, wave = t >> 6, row_no = blockIdx.x / (unsigned)a.chunks, chunk = blockIdx.x - row_no * a.chunks;
   const logits::Row<T> row(static_cast<const T*>(a.z) + row_no * a.z_stride, a.classes);
-  const int end = min((chunk + 1) * a.per, row.vectors());
+  const int end = min((chunk + 1) * a.per, row.full);
   Sums<TWO> s;
-  for (int i = chunk * a.per + t; i < end; i += 1024) {
+#pragma unroll 1
+  for (int i = chunk * a.per + t; i - lane < end; i += 1024) {      // (whole wavefronts)
     uint4 r[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) r[u] = row.load(i + u * 256 < end ? i + u * 256 : row.full + 1);
+    for (int u = 0; u < 4; ++u) r[u] = row.load(i + u * 256, end);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       float x[V];
       logits::unpack<T>(r[u], x);
       s.add(x, a.scale);
     }
+  }
+  if (row.tail && chunk == a.chunks - 1) {
+    float x[V];
+    row.edge(t == 0, x);
+    s.add(x, a.scale);
   }
   s.over_wave(a.scale);
   if (lane == 0) sums[wave] = make_float4(s.m, s.at_t, s.at_1, 0.0f);
@@ -370,11 +387,14 @@ __global__ __launch_bounds__(NT) void distill_finish_kernel(const DistillArgs a)
   const logits::Row<T> row(static_cast<const T*>(a.z) + row_no * a.z_stride, a.classes);
   List l;
   if (wave == 0) l.load(a, row_no);
-  const int from = chunk * a.per, end = min(from + a.per, row.vectors());
+  const int from = chunk * a.per, end = min(from + a.per, row.full);
+  const bool last = chunk == a.chunks - 1;
   uint4 r[4];
+  float edge[V];
   if (a.dz) {
 #pragma unroll
-    for (int u = 0; u < 4; ++u) r[u] = row.load(from + t + u * NT < end ? from + t + u * NT : row.full + 1);
+    for (int u = 0; u < 4; ++u) r[u] = row.load(from + t + u * NT, end);
+    row.edge(last && t == NT - 1, edge);
   }
   if (wave == 0) {
     l.read<T>(a, row.p);
@@ -419,23 +439,26 @@ __global__ __launch_bounds__(NT) void distill_finish_kernel(const DistillArgs a)
   g.none |= empty;
   if constexpr (!TWO) g.by_t += g.by_1;
   T* const dz = static_cast<T*>(a.dz) + (long)row_no * a.classes;
+#pragma unroll 1
   for (int i = from + t; i < end; i += 4 * NT) {
-    if (i != from + t) {
+    uint4 next[4];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) r[u] = row.load(i + u * NT < end ? i + u * NT : row.full + 1);
-    }
+    for (int u = 0; u < 4; ++u) next[u] = row.load(i + (4 + u) * NT, end);
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      if (i + u * NT >= end) break;
       float x[V];
       logits::unpack<T>(r[u], x);
-#pragma unroll
-      for (int j = 0; j < V; ++j) x[j] = g.none ? 0.0f : g.at<TWO>(x[j], a.scale);
-      logits::store<T>(dz, i + u * NT, row.full, row.tail, x);
+      g.over<TWO>(x, a.scale);
+      if (i + u * NT < end) logits::store<T>(dz, i + u * NT, x);
+      r[u] = next[u];
     }
   }
+  if (last && t == NT - 1) {
+    g.over<TWO>(edge, a.scale);
+    logits::store_edge<T>(dz, row, edge);
+  }
   __syncthreads();
-  if (wave == 0 && !g.none) patch<T, TWO>(a, l, sh.shares, g, dz, from * V, min((long)end * V, (long)a.classes));
+  if (wave == 0 && !g.none) patch<T, TWO>(a, l, sh.shares, g, dz, from * V, last ? a.classes : end * V);
 }
 
 template <typename T, bool TWO> void launch_rows(const DistillArgs& a, const DistillLaunch& l, hipStream_t s) {

@@ -1,8 +1,8 @@
 // Rows of logits: what the top-logits and the distillation kernels share.
 //
 // A work-group has a row, or a run of one; a thread reads 16 bytes at a time, V numbers, vector t + i NT of the row its i-th.  Rows may begin at any element
-// (an odd number of classes, the first classes of wider rows): loads and stores of 16 bytes need the element's alignment only, and what is left past the last
-// whole vector goes by the element.  Places past a row's end hold -infinity, a class that is not there.
+// (an odd number of classes, the first classes of wider rows): loads and stores of 16 bytes need the element's alignment only.  Places past a row's
+// end hold -infinity, a class that is not there.
 #pragma once
 #include <cfloat>
 #include <type_traits>
@@ -50,55 +50,48 @@ template <typename T> __device__ __forceinline__ void unpack(const uint4& r, flo
 // (What is held is unpacked again each time: without this the compiler keeps the unpacked numbers, twice the registers and more.)
 __device__ __forceinline__ void pin(uint4& r) { asm volatile("" : "+v"(r.x), "+v"(r.y), "+v"(r.z), "+v"(r.w)); }
 
-// `classes` numbers at p.
+// `classes` numbers at p: whole vectors and, past them, an edge of fewer than V numbers, which is one thread's and apart from the loops (its code in each of
+// their steps would be most of a kernel).
 template <typename T> struct Row {
   static constexpr int V = Raw<T>::V;
   const T* p;
   int full, tail;      // whole vectors, numbers behind them
   __device__ __forceinline__ Row(const T* p, int classes) : p(p), full(classes / V), tail(classes % V) {}
-  __device__ __forceinline__ int vectors() const { return full + (tail != 0); }
-  __device__ __forceinline__ uint4 load(int i) const {
+  static __device__ __forceinline__ uint4 none() { return make_uint4(Raw<T>::kNone, Raw<T>::kNone, Raw<T>::kNone, Raw<T>::kNone); }
+  // vector i of those before `end`
+  __device__ __forceinline__ uint4 load(int i, int end) const {
     typedef unsigned uint4u __attribute__((ext_vector_type(4), aligned(2)));
-    uint4 r = make_uint4(Raw<T>::kNone, Raw<T>::kNone, Raw<T>::kNone, Raw<T>::kNone);
-    if (i < full) {
+    uint4 r = none();
+    if (i < end) {
       const uint4u v = *reinterpret_cast<const uint4u*>(p + (long)i * V);
       r = make_uint4(v.x, v.y, v.z, v.w);
-    } else if (i == full && tail) {
-      const T* const q = p + (long)i * V;
-      if constexpr (sizeof(T) == 4) {
-        unsigned v[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[j] = __float_as_uint(q[min(j, tail - 1)]);
-        r = make_uint4(v[0], tail > 1 ? v[1] : r.y, tail > 2 ? v[2] : r.z, r.w);
-      } else {
-        const unsigned short* const h = reinterpret_cast<const unsigned short*>(q);
-        unsigned v[8], w[4];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = h[min(j, tail - 1)];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = j < tail ? v[j] : Raw<T>::kNone & 0xffffu;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) w[j] = v[2 * j] | v[2 * j + 1] << 16;
-        r = make_uint4(w[0], w[1], w[2], w[3]);
-      }
     }
     return r;
   }
+  // the edge, for the thread that asks for it
+  __device__ __forceinline__ void edge(bool mine, float (&x)[V]) const {
+#pragma unroll
+    for (int j = 0; j < V; ++j) x[j] = -__builtin_inff();
+    if (mine) {
+#pragma unroll
+      for (int j = 0; j < V - 1; ++j)
+        if (j < tail) x[j] = widen<T>(p[(long)full * V + j]);
+    }
+  }
 };
 
-template <typename T> __device__ __forceinline__ void store(T* p, int i, int full, int tail, const float (&x)[Raw<T>::V]) {
+template <typename T> __device__ __forceinline__ void store(T* p, int i, const float (&x)[Raw<T>::V]) {
   constexpr int V = Raw<T>::V;
   typedef T outs __attribute__((ext_vector_type(V), aligned(2)));
-  if (i < full) {
-    outs v;
+  outs v;
 #pragma unroll
-    for (int j = 0; j < V; ++j) v[j] = (T)x[j];
-    *reinterpret_cast<outs*>(p + (long)i * V) = v;
-  } else if (i == full) {
+  for (int j = 0; j < V; ++j) v[j] = (T)x[j];
+  *reinterpret_cast<outs*>(p + (long)i * V) = v;
+}
+template <typename T> __device__ __forceinline__ void store_edge(T* p, const Row<T>& row, const float (&x)[Raw<T>::V]) {
 #pragma unroll
-    for (int j = 0; j < V; ++j)
-      if (j < tail) p[(long)i * V + j] = (T)x[j];
-  }
+  for (int j = 0; j < Raw<T>::V - 1; ++j)
+    if (j < row.tail) p[(long)row.full * Raw<T>::V + j] = (T)x[j];
 }
 
 // Largest of two, NaN where one is.

@@ -1,9 +1,9 @@
 // The largest logits of each row with their classes: descending, equal ones by their class, NaN before all; -infinity is a class that is not there and is never
 // listed.
 //
-// A bound first: each thread's largest number is one of the row's, so at least k numbers reach the k-th largest of those.  With many more threads than k the
-// numbers that reach it are hardly more than k; they go to a list in LDS, in any order, and each one's place is the count of those before it.  A row is read
-// from memory once, held in registers (up to 131072 numbers of 16 bits, 65536 of 32).  What bounds it is that read.
+// A bound first: each thread's largest number is one of the row's, so at least k numbers reach the k-th largest of those.  With more threads than k the numbers
+// that reach it are hardly more than k, in few threads, and those read theirs again; they go to a list in LDS, in any order, and each one's place is
+// the count of those before it.  What bounds it is reading z once.
 #include <algorithm>
 
 #include "logits.hpp"
@@ -35,8 +35,8 @@ struct TopArgs {
   int* ids;
 };
 
-// NV vectors a thread; 0: as many as the row has, read each time they are needed.  One row, or one run of it, a work-group.
-template <typename T, typename OUT, int NT, int NV>
+// One row, or one run of it, a work-group.
+template <typename T, typename OUT, int NT>
 __global__ __launch_bounds__(NT) void top_kernel(const TopArgs a) {
   constexpr int V = Raw<T>::V, NW = NT / 64;
   __shared__ unsigned keys[NT], list_key[kList + kMostK];
@@ -47,37 +47,41 @@ __global__ __launch_bounds__(NT) void top_kernel(const TopArgs a) {
   const int row_no = blockIdx.x / (unsigned)a.chunks, chunk = blockIdx.x - row_no * a.chunks;
   const long first = (long)chunk * a.per;
   const logits::Row<T> row(static_cast<const T*>(a.z) + row_no * a.stride + first, (int)min((long)a.per, a.classes - first));
-  const int rounds = NV ? NV : (row.vectors() + NT - 1) / NT;
-  uint4 held[NV ? NV : 1];
-  if constexpr (NV != 0) {
+  const int rounds = (row.full + NT - 1) / NT;
+  // f(number of the vector, its numbers); the edge is the last thread's
+  auto each = [&](auto&& f) __attribute__((always_inline)) {
+    constexpr int U = 8;
+#pragma unroll 1
+    for (int i = t; i < row.full; i += U * NT) {
+      uint4 r[U];
 #pragma unroll
-    for (int i = 0; i < NV; ++i) held[i] = row.load(t + i * NT);
-  }
-  // f(number of the vector, its numbers), from memory or from registers
-  auto each_again = [&](auto&& f) __attribute__((always_inline)) {
-    float x[V];
-    for (int i = 0; i < rounds; i += 4) {
-      uint4 r[4];
+      for (int u = 0; u < U; ++u) r[u] = row.load(i + u * NT, row.full);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) r[u] = row.load(t + (i + u) * NT);
-#pragma unroll
-      for (int u = 0; u < 4; ++u) {
+      for (int u = 0; u < U; ++u) {
+        float x[V];
         logits::unpack<T>(r[u], x);
-        f(t + (i + u) * NT, x);
+        f(i + u * NT, x);
       }
     }
+    if (row.tail && t == NT - 1) {
+      float x[V];
+      row.edge(true, x);
+      f(row.full, x);
+    }
   };
-  auto each = [&](auto&& f) __attribute__((always_inline)) {
-    if constexpr (NV != 0) {
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        float x[V];
-        logits::pin(held[i]);
-        logits::unpack<T>(held[i], x);
-        f(t + i * NT, x);
+  // the same a vector at a time, where few have anything to do
+  auto each_slowly = [&](auto&& f) __attribute__((always_inline)) {
+#pragma unroll 1
+    for (int i = t; i < row.full + (row.tail && t == NT - 1 ? NT : 0); i += NT) {
+      float x[V];
+      int at = i;
+      if (i < row.full) {
+        logits::unpack<T>(row.load(i, row.full), x);
+      } else {
+        row.edge(true, x);
+        at = row.full;
       }
-    } else {
-      each_again(f);
+      f(at, x);
     }
   };
   float top = -__builtin_inff();
@@ -109,8 +113,7 @@ __global__ __launch_bounds__(NT) void top_kernel(const TopArgs a) {
     if (i < kList) list_key[i] = key_of(x), list_at[i] = at;
   };
   if (!(top < from))
-    each([&](int i, const float (&x)[V]) __attribute__((always_inline)) {
-      if (logits::largest(x) < from) return;
+    each_slowly([&](int i, const float (&x)[V]) __attribute__((always_inline)) {
 #pragma unroll
       for (int j = 0; j < V; ++j)
         if (!(x[j] < from)) append(x[j], i * V + j);
@@ -131,7 +134,7 @@ __global__ __launch_bounds__(NT) void top_kernel(const TopArgs a) {
     };
     auto reach = [&](unsigned b) __attribute__((always_inline)) {
       int mine = 0;
-      each_again([&](int, const float (&x)[V]) __attribute__((always_inline)) {
+      each_slowly([&](int, const float (&x)[V]) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < V; ++j) mine += key_of(x[j]) >= b;
       });
@@ -145,18 +148,20 @@ __global__ __launch_bounds__(NT) void top_kernel(const TopArgs a) {
     }
     if (t == 0) count = 0;
     __syncthreads();
-    each_again([&](int i, const float (&x)[V]) __attribute__((always_inline)) {
+    each_slowly([&](int i, const float (&x)[V]) __attribute__((always_inline)) {
 #pragma unroll
       for (int j = 0; j < V; ++j)
         if (key_of(x[j]) > low) append(x[j], i * V + j);
     });
     __syncthreads();
     const int above = count;
-    // the first of the equal ones, round by round of NT vectors, in their order
+    // the first of the equal ones, round by round of NT vectors and the edge, in their order
     int have = 0;
-    for (int i = 0; i < rounds && have < a.k; ++i) {
+    for (int i = 0; i <= rounds && have < a.k; ++i) {
       float x[V];
-      logits::unpack<T>(row.load(t + i * NT), x);
+      const int at = i < rounds ? t + i * NT : row.full;
+      if (i < rounds) logits::unpack<T>(row.load(at, row.full), x);
+      else row.edge(t == 0, x);
       int mine = 0;
 #pragma unroll
       for (int j = 0; j < V; ++j) mine += key_of(x[j]) == low;
@@ -178,7 +183,7 @@ __global__ __launch_bounds__(NT) void top_kernel(const TopArgs a) {
 #pragma unroll
       for (int j = 0; j < V; ++j)
         if (key_of(x[j]) == low) {
-          if (before < a.k) list_key[above + before] = low, list_at[above + before] = (t + i * NT) * V + j;
+          if (before < a.k) list_key[above + before] = low, list_at[above + before] = at * V + j;
           ++before;
         }
     }
@@ -229,11 +234,9 @@ template <typename T, typename OUT> void launch_top(const TopArgs& a, int rows, 
   const unsigned grid = (unsigned)rows * a.chunks;
   const int vectors = (a.per + Raw<T>::V - 1) / Raw<T>::V;
   // four threads or more for each of the k, if the row has them
-  if (vectors <= 256 && (a.k <= 16 || vectors <= 64)) top_kernel<T, OUT, 64, 4><<<grid, 64, 0, s>>>(a);
-  else if (vectors <= 2048 && (a.k <= 64 || vectors <= 256)) top_kernel<T, OUT, 256, 8><<<grid, 256, 0, s>>>(a);
-  else if (vectors <= 8192) top_kernel<T, OUT, 1024, 8><<<grid, 1024, 0, s>>>(a);
-  else if (vectors <= 16384) top_kernel<T, OUT, 1024, 16><<<grid, 1024, 0, s>>>(a);
-  else top_kernel<T, OUT, 1024, 0><<<grid, 1024, 0, s>>>(a);
+  if (vectors <= 512 && (a.k <= 16 || vectors <= 64)) top_kernel<T, OUT, 64><<<grid, 64, 0, s>>>(a);
+  else if (a.k <= 64 || vectors <= 256) top_kernel<T, OUT, 256><<<grid, 256, 0, s>>>(a);
+  else top_kernel<T, OUT, 1024><<<grid, 1024, 0, s>>>(a);
 }
 
 int check_top(int rows, int classes, long stride, int k, int dtype) {
