@@ -36,7 +36,14 @@ DistillArgs args_of(const cprune_distill_desc& d, const void* z, const int32_t* 
   a.scale = (float)(1.4426950408889634 / d.temperature);
   a.soft = 1.0f - d.hard, a.hard = d.hard, a.t = d.temperature, a.inv_t = 1.0f / d.temperature;
   a.chunks = 1;
+  // (a gradient that does not stay in the last-level cache, 256 MB with what else is in use, leaves it to the rows that are read again)
+  a.stream = (double)d.rows * d.classes * dtype_size(d.dtype) > 134217728.0;
   return a;
+}
+
+int second_of(const cprune_distill_desc& d, bool wanted) {
+  if (!wanted || d.temperature == 1.0f) return distill::kNone;
+  return d.temperature == 2.0f ? distill::kSquare : d.temperature == 4.0f ? distill::kFourth : distill::kOwn;
 }
 
 void launch(int dtype, DistillPass pass, const DistillArgs& a, const DistillLaunch& l, hipStream_t s) {
@@ -52,7 +59,7 @@ int forward(const cprune_distill_desc& d, DistillArgs a, void* ws, size_t ws_byt
   if (reinterpret_cast<uintptr_t>(ws) & 15) return CPRUNE_ERR_INVALID_ARG;
   const int vectors = vectors_of(d);
   DistillLaunch l = {};
-  l.two = d.temperature != 1.0f && (a.stats_out || (a.labels && d.hard > 0.0f));
+  l.two = second_of(d, a.stats_out || (a.labels && d.hard > 0.0f));
   if (by_parts(d)) {
     cut(d, std::min(kMostParts, std::max(8, 1024 / d.rows)), a);
     a.part = static_cast<float4*>(ws), a.parts = a.chunks;
@@ -64,7 +71,7 @@ int forward(const cprune_distill_desc& d, DistillArgs a, void* ws, size_t ws_byt
     l.grid = (unsigned)d.rows;
     if (vectors <= 256) l.threads = 64, l.held = a.dz ? 4 : 0;
     else if (!a.dz || vectors <= 2048) l.threads = 256, l.held = a.dz ? 8 : 0;
-    else l.threads = 1024, l.held = vectors <= 8192 ? 8 : vectors <= 16384 ? 16 : 0;
+    else l.threads = 512, l.held = 16;
     launch(d.dtype, kDistillRows, a, l, s);
   }
   CPRUNE_LAUNCH_CHECK();
@@ -109,7 +116,7 @@ extern "C" int cprune_distill_loss_backward(const cprune_distill_desc* d, const 
   DistillArgs a = args_of(*d, z, ids, teacher, labels);
   a.stats = stats, a.dloss = dloss, a.dz = dz;
   DistillLaunch l = {};
-  l.two = d->temperature != 1.0f && labels && d->hard > 0.0f;
+  l.two = second_of(*d, labels && d->hard > 0.0f);
   const int vectors = vectors_of(*d);
   if (vectors <= 256) {
     l.threads = 64, a.per = vectors;

@@ -37,13 +37,14 @@ struct DistillArgs {
   float4* part;                 // [rows][parts]: m, the two sums
   int parts;
   int chunks, per;              // runs of a row, a work-group each; vectors of a run
+  bool stream;                  // dz is stored past the caches
 };
 
 enum DistillPass { kDistillRows, kDistillParts, kDistillFinish };
 struct DistillLaunch {
   unsigned grid;
   int threads, held;            // held: vectors a thread (0: read again)
-  bool two;                     // the sum at temperature 1 is one of its own
+  int two;                      // distill::Second
 };
 void launch_distill_f32(DistillPass pass, const DistillArgs& a, const DistillLaunch& l, hipStream_t s);
 void launch_distill_f16(DistillPass pass, const DistillArgs& a, const DistillLaunch& l, hipStream_t s);
@@ -56,25 +57,47 @@ using logits::kLog2e;
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// Over a wavefront, in every lane: rows of 16 lanes step by step, their results handed on to the next row and the next two.
+template <int CTRL, int ROWS> __device__ __forceinline__ float from_lane(float old, float v) {
+  return __uint_as_float((unsigned)__builtin_amdgcn_update_dpp((int)__float_as_uint(old), (int)__float_as_uint(v), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ float last_lane(float v) { return __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)__float_as_uint(v), 63)); }
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
+  v += from_lane<0x111, 0xf>(0.0f, v);      // one to the right, two, four, eight
+  v += from_lane<0x112, 0xf>(0.0f, v);
+  v += from_lane<0x114, 0xf>(0.0f, v);
+  v += from_lane<0x118, 0xf>(0.0f, v);
+  v += from_lane<0x142, 0xa>(0.0f, v);      // lane 15 of a row to the next one
+  v += from_lane<0x143, 0xc>(0.0f, v);      // lane 31 to the upper half
+  return last_lane(v);
 }
 __device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = logits::larger(v, __shfl_xor(v, o, 64));
-  return v;
+  v = logits::larger(v, from_lane<0x111, 0xf>(v, v));
+  v = logits::larger(v, from_lane<0x112, 0xf>(v, v));
+  v = logits::larger(v, from_lane<0x114, 0xf>(v, v));
+  v = logits::larger(v, from_lane<0x118, 0xf>(v, v));
+  v = logits::larger(v, from_lane<0x142, 0xa>(v, v));
+  v = logits::larger(v, from_lane<0x143, 0xc>(v, v));
+  return last_lane(v);
+}
+
+// How the second exponential of a number, at temperature 1, is had beside the one at T: not wanted; by itself; where T is 2 or 4, the usual ones, as the first
+// one's square or fourth power (an exponential takes as long as four products: 4096 x 32768 fp16 TWO_TIMES us).
+enum Second { kNone, kOwn, kSquare, kFourth };
+template <int TWO> __device__ __forceinline__ float second_of(float first, float d) {
+  if constexpr (TWO == kSquare) return first * first;
+  if constexpr (TWO == kFourth) return (first * first) * (first * first);
+  return exp2_of(d * kLog2e);
 }
 
 // Largest number so far (from the lowest finite one, so that no difference is of two infinities unless a number is +infinity: then, as with a NaN, the sums are
 // NaN) and the sums against it; TWO: at temperature 1 beside T.
-template <bool TWO> struct Sums {
+template <int TWO> struct Sums {
   float m = -FLT_MAX, at_t = 0.0f, at_1 = 0.0f;
   __device__ __forceinline__ void rescale(float to, float scale) {
     const float d = m - to;
     at_t *= exp2_of(d * scale);
-    if constexpr (TWO) at_1 *= exp2_of(d * kLog2e);
+    if constexpr (TWO != kNone) at_1 *= exp2_of(d * kLog2e);
     m = to;
   }
   template <int V> __device__ __forceinline__ void add(const float (&x)[V], float scale) {
@@ -83,14 +106,15 @@ template <bool TWO> struct Sums {
 #pragma unroll
     for (int j = 0; j < V; ++j) {
       const float d = x[j] - m;
-      at_t += exp2_of(d * scale);
-      if constexpr (TWO) at_1 += exp2_of(d * kLog2e);
+      const float first = exp2_of(d * scale);
+      at_t += first;
+      if constexpr (TWO != kNone) at_1 += second_of<TWO>(first, d);
     }
   }
   __device__ __forceinline__ void over_wave(float scale) {
     rescale(wave_max(m), scale);
     at_t = wave_sum(at_t);
-    if constexpr (TWO) at_1 = wave_sum(at_1);
+    if constexpr (TWO != kNone) at_1 = wave_sum(at_1);
   }
 };
 
@@ -205,17 +229,26 @@ struct Slope {
     by_1 = label ? of_1 * inv_sum_1 : 0.0f;
     none = d == 0.0f || !(any || label);
   }
-  template <bool TWO> __device__ __forceinline__ float at(float x, float scale) const {
+  template <int TWO> __device__ __forceinline__ float at(float x, float scale) const {
     const float d = x - m;
-    float v = exp2_of(d * scale) * by_t;
-    if constexpr (TWO) v += exp2_of(d * kLog2e) * by_1;
+    const float first = exp2_of(d * scale);
+    float v = first * by_t;
+    if constexpr (TWO != kNone) v += second_of<TWO>(first, d) * by_1;
     return v;
   }
-  template <bool TWO, int V> __device__ __forceinline__ void over(float (&x)[V], float scale) const {
+  template <int TWO, int V> __device__ __forceinline__ void over(float (&x)[V], float scale) const {
 #pragma unroll
-    for (int j = 0; j < V; ++j) x[j] = none ? 0.0f : at<TWO>(x[j], scale);
+    for (int j = 0; j < V; ++j) x[j] = at<TWO>(x[j], scale);
   }
 };
+
+// zeros for vectors of a row, and its edge
+template <typename T> __device__ __forceinline__ void clear(T* dz, const logits::Row<T>& row, int first, int step, int end, bool edge) {
+  const float zeros[Raw<T>::V] = {};
+#pragma unroll 1
+  for (int i = first; i < end; i += step) logits::store<T>(dz, i, zeros, false);
+  if (edge) logits::store_edge<T>(dz, row, zeros);
+}
 
 // LDS of a work-group with a row or a run of one
 template <int NT> struct Shared {
@@ -225,7 +258,7 @@ template <int NT> struct Shared {
 };
 
 // The gradient's patches, by wavefront 0 behind the barrier that follows the stores: classes of the list, and the label where the list has it not.
-template <typename T, bool TWO> __device__ __forceinline__ void patch(const DistillArgs& a, const List& l, const Shares& shares, const Slope& g, T* dz, int lo, int hi) {
+template <typename T, int TWO> __device__ __forceinline__ void patch(const DistillArgs& a, const List& l, const Shares& shares, const Slope& g, T* dz, int lo, int hi) {
   bool listed = false;
 #pragma unroll
   for (int e = 0; e < List::E; ++e) listed |= l.label >= 0 && l.id[e] == l.label && l.any;
@@ -237,9 +270,9 @@ template <typename T, bool TWO> __device__ __forceinline__ void patch(const Dist
   if (l.label >= lo && l.label < hi && !__any(listed) && (threadIdx.x & 63) == 0) dz[l.label] = (T)(g.at<TWO>(l.z_label, a.scale) - g.of_1);
 }
 
-// A work-group has a row: its sums, its loss and, with dz, its gradient.
-template <typename T, int NT, int NV, bool TWO>
-__global__ __launch_bounds__(NT) void distill_rows_kernel(const DistillArgs a) {
+// A work-group has a row: its sums, its loss and, with dz, its gradient.  It holds the row's first NT NV vectors; those past them are read again.
+template <typename T, int NT, int NV, int TWO>
+__global__ __launch_bounds__(NT, NT == 512 ? 4 : 1) void distill_rows_kernel(const DistillArgs a) {
   constexpr int V = Raw<T>::V, NW = NT / 64;
   __shared__ Shared<NT> sh;
   const int t = (int)threadIdx.x, lane = t & 63, wave = t >> 6, row_no = blockIdx.x;
@@ -267,14 +300,16 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(const DistillArgs a) {
       logits::unpack<T>(held[i], x);
       s.add(x, a.scale);
     }
-  } else {
+  }
+  constexpr int HELD = NV * NT, U = NV == 16 ? 4 : 8;
+  if (NV == 0 || row.full > HELD) {
 #pragma unroll 1
-    for (int i = t; i - lane < row.full; i += 8 * NT) {      // (whole wavefronts)
-      uint4 r[8];
+    for (int i = HELD + t; i - lane < row.full; i += U * NT) {      // (whole wavefronts)
+      uint4 r[U];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) r[u] = row.load(i + u * NT, row.full);
+      for (int u = 0; u < U; ++u) r[u] = row.load(i + u * NT, row.full);
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
+      for (int u = 0; u < U; ++u) {
         float x[V];
         logits::unpack<T>(r[u], x);
         s.add(x, a.scale);
@@ -290,10 +325,10 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(const DistillArgs a) {
     s.m = v.x, s.at_t = lane < NW ? v.y : 0.0f, s.at_1 = lane < NW ? v.z : 0.0f;
     s.over_wave(a.scale);
   }
-  const float sum_1 = TWO ? s.at_1 : s.at_t;
+  const float sum_1 = TWO != kNone ? s.at_1 : s.at_t;
   const bool empty = s.at_t == 0.0f;      // every class masked
   if (wave == 0 && a.loss) {
-    const float log_t = logf(s.at_t), log_1 = TWO ? logf(s.at_1) : log_t;
+    const float log_t = logf(s.at_t), log_1 = TWO != kNone ? logf(s.at_1) : log_t;
     const float v = l.loss(a, s.m, log_t, log_1);
     if (lane == 0) {
       a.loss[row_no] = empty ? 0.0f : v;
@@ -309,13 +344,17 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(const DistillArgs a) {
   const int terms = sh.terms;
   g.set(a, row_no, s.m, 1.0f / s.at_t, 1.0f / sum_1, (terms & 1) != 0, (terms & 2) != 0);
   g.none |= empty;
-  if constexpr (!TWO) g.by_t += g.by_1;
+  if constexpr (TWO == kNone) g.by_t += g.by_1;
   T* const dz = static_cast<T*>(a.dz) + (long)row_no * a.classes;
+  if (g.none) {
+    clear<T>(dz, row, t, NT, row.full, t == NT - 1);
+    return;
+  }
   auto out = [&](int i, const uint4& r) __attribute__((always_inline)) {
     float x[V];
     logits::unpack<T>(r, x);
     g.over<TWO>(x, a.scale);
-    if (i < row.full) logits::store<T>(dz, i, x);
+    if (i < row.full) logits::store<T>(dz, i, x, a.stream);
   };
   if constexpr (NV != 0) {
 #pragma unroll
@@ -323,14 +362,15 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(const DistillArgs a) {
       logits::pin(held[i]);
       out(t + i * NT, held[i]);
     }
-  } else {
+  }
+  if (NV == 0 || row.full > HELD) {
 #pragma unroll 1
-    for (int i = t; i < row.full; i += 8 * NT) {
-      uint4 r[8];
+    for (int i = HELD + t; i < row.full; i += U * NT) {
+      uint4 r[U];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) r[u] = row.load(i + u * NT, row.full);
+      for (int u = 0; u < U; ++u) r[u] = row.load(i + u * NT, row.full);
 #pragma unroll
-      for (int u = 0; u < 8; ++u) out(i + u * NT, r[u]);
+      for (int u = 0; u < U; ++u) out(i + u * NT, r[u]);
     }
   }
   if (t == NT - 1) {
@@ -338,11 +378,11 @@ __global__ __launch_bounds__(NT) void distill_rows_kernel(const DistillArgs a) {
     logits::store_edge<T>(dz, row, edge);
   }
   __syncthreads();
-  if (wave == 0 && !g.none) patch<T, TWO>(a, l, sh.shares, g, dz, 0, a.classes);
+  if (wave == 0) patch<T, TWO>(a, l, sh.shares, g, dz, 0, a.classes);
 }
 
 // Sums of a run of a row.
-template <typename T, bool TWO>
+template <typename T, int TWO>
 __global__ __launch_bounds__(256) void distill_parts_kernel(const DistillArgs a) {
   constexpr int V = Raw<T>::V;
   __shared__ float4 sums[4];
@@ -379,7 +419,7 @@ __global__ __launch_bounds__(256) void distill_parts_kernel(const DistillArgs a)
 }
 
 // With the row's sums, from up to 64 parts or given: the gradient of a run, and the loss by the row's first work-group.
-template <typename T, int NT, bool TWO>
+template <typename T, int NT, int TWO>
 __global__ __launch_bounds__(NT) void distill_finish_kernel(const DistillArgs a) {
   constexpr int V = Raw<T>::V;
   __shared__ Shared<NT> sh;
@@ -417,9 +457,9 @@ __global__ __launch_bounds__(NT) void distill_finish_kernel(const DistillArgs a)
     s.over_wave(a.scale);
     m = s.m;
     empty = s.at_t == 0.0f;
-    inv_t = 1.0f / s.at_t, inv_1 = TWO ? 1.0f / s.at_1 : inv_t;
+    inv_t = 1.0f / s.at_t, inv_1 = TWO != kNone ? 1.0f / s.at_1 : inv_t;
     if (wave == 0 && chunk == 0 && a.loss) {
-      log_t = logf(s.at_t), log_1 = TWO ? logf(s.at_1) : log_t;
+      log_t = logf(s.at_t), log_1 = TWO != kNone ? logf(s.at_1) : log_t;
       const float v = l.loss(a, m, log_t, log_1);
       if (lane == 0) {
         a.loss[row_no] = empty ? 0.0f : v;
@@ -437,8 +477,12 @@ __global__ __launch_bounds__(NT) void distill_finish_kernel(const DistillArgs a)
   const int terms = sh.terms;
   g.set(a, row_no, m, inv_t, inv_1, (terms & 1) != 0, (terms & 2) != 0);
   g.none |= empty;
-  if constexpr (!TWO) g.by_t += g.by_1;
+  if constexpr (TWO == kNone) g.by_t += g.by_1;
   T* const dz = static_cast<T*>(a.dz) + (long)row_no * a.classes;
+  if (g.none) {
+    clear<T>(dz, row, from + t, NT, end, last && t == NT - 1);
+    return;
+  }
 #pragma unroll 1
   for (int i = from + t; i < end; i += 4 * NT) {
     uint4 next[4];
@@ -449,7 +493,7 @@ __global__ __launch_bounds__(NT) void distill_finish_kernel(const DistillArgs a)
       float x[V];
       logits::unpack<T>(r[u], x);
       g.over<TWO>(x, a.scale);
-      if (i + u * NT < end) logits::store<T>(dz, i + u * NT, x);
+      if (i + u * NT < end) logits::store<T>(dz, i + u * NT, x, a.stream);
       r[u] = next[u];
     }
   }
@@ -458,37 +502,28 @@ __global__ __launch_bounds__(NT) void distill_finish_kernel(const DistillArgs a)
     logits::store_edge<T>(dz, row, edge);
   }
   __syncthreads();
-  if (wave == 0 && !g.none) patch<T, TWO>(a, l, sh.shares, g, dz, from * V, last ? a.classes : end * V);
+  if (wave == 0) patch<T, TWO>(a, l, sh.shares, g, dz, from * V, last ? a.classes : end * V);
 }
 
-template <typename T, bool TWO> void launch_rows(const DistillArgs& a, const DistillLaunch& l, hipStream_t s) {
-  if (l.threads == 64) {
-    if (l.held) distill_rows_kernel<T, 64, 4, TWO><<<l.grid, 64, 0, s>>>(a);
-    else distill_rows_kernel<T, 64, 0, TWO><<<l.grid, 64, 0, s>>>(a);
-  } else if (l.threads == 256) {
-    if (l.held) distill_rows_kernel<T, 256, 8, TWO><<<l.grid, 256, 0, s>>>(a);
-    else distill_rows_kernel<T, 256, 0, TWO><<<l.grid, 256, 0, s>>>(a);
-  } else if (l.held == 8) {
-    distill_rows_kernel<T, 1024, 8, TWO><<<l.grid, 1024, 0, s>>>(a);
-  } else if (l.held) {
-    distill_rows_kernel<T, 1024, 16, TWO><<<l.grid, 1024, 0, s>>>(a);
-  } else {
-    distill_rows_kernel<T, 1024, 0, TWO><<<l.grid, 1024, 0, s>>>(a);
-  }
-}
-
-template <typename T, bool TWO> void launch_two(DistillPass pass, const DistillArgs& a, const DistillLaunch& l, hipStream_t s) {
-  if (pass == kDistillRows) launch_rows<T, TWO>(a, l, s);
-  else if (pass == kDistillParts) distill_parts_kernel<T, TWO><<<l.grid, 256, 0, s>>>(a);
-  else if (l.threads == 64) distill_finish_kernel<T, 64, TWO><<<l.grid, 64, 0, s>>>(a);
-  else distill_finish_kernel<T, 256, TWO><<<l.grid, 256, 0, s>>>(a);
+template <typename T, int TWO> void launch_two(DistillPass pass, const DistillArgs& a, const DistillLaunch& l, hipStream_t s) {
+  if (pass == kDistillParts) distill_parts_kernel<T, TWO><<<l.grid, 256, 0, s>>>(a);
+  else if (pass == kDistillFinish && l.threads == 64) distill_finish_kernel<T, 64, TWO><<<l.grid, 64, 0, s>>>(a);
+  else if (pass == kDistillFinish) distill_finish_kernel<T, 256, TWO><<<l.grid, 256, 0, s>>>(a);
+  else if (l.threads == 64 && l.held) distill_rows_kernel<T, 64, 4, TWO><<<l.grid, 64, 0, s>>>(a);
+  else if (l.threads == 64) distill_rows_kernel<T, 64, 0, TWO><<<l.grid, 64, 0, s>>>(a);
+  else if (l.threads == 512) distill_rows_kernel<T, 512, 16, TWO><<<l.grid, 512, 0, s>>>(a);
+  else if (l.held) distill_rows_kernel<T, 256, 8, TWO><<<l.grid, 256, 0, s>>>(a);
+  else distill_rows_kernel<T, 256, 0, TWO><<<l.grid, 256, 0, s>>>(a);
 }
 
 }  // namespace distill
 
 template <typename T> void launch_distill(DistillPass pass, const DistillArgs& a, const DistillLaunch& l, hipStream_t s) {
-  if (l.two) distill::launch_two<T, true>(pass, a, l, s);
-  else distill::launch_two<T, false>(pass, a, l, s);
+  using namespace distill;
+  if (l.two == kNone) launch_two<T, kNone>(pass, a, l, s);
+  else if (l.two == kSquare) launch_two<T, kSquare>(pass, a, l, s);
+  else if (l.two == kFourth) launch_two<T, kFourth>(pass, a, l, s);
+  else launch_two<T, kOwn>(pass, a, l, s);
 }
 
 }  // namespace cprune

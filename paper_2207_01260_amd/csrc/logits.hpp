@@ -80,13 +80,14 @@ template <typename T> struct Row {
   }
 };
 
-template <typename T> __device__ __forceinline__ void store(T* p, int i, const float (&x)[Raw<T>::V]) {
+template <typename T> __device__ __forceinline__ void store(T* p, int i, const float (&x)[Raw<T>::V], bool stream) {
   constexpr int V = Raw<T>::V;
   typedef T outs __attribute__((ext_vector_type(V), aligned(2)));
   outs v;
 #pragma unroll
   for (int j = 0; j < V; ++j) v[j] = (T)x[j];
-  *reinterpret_cast<outs*>(p + (long)i * V) = v;
+  if (stream) __builtin_nontemporal_store(v, reinterpret_cast<outs*>(p + (long)i * V));
+  else *reinterpret_cast<outs*>(p + (long)i * V) = v;
 }
 template <typename T> __device__ __forceinline__ void store_edge(T* p, const Row<T>& row, const float (&x)[Raw<T>::V]) {
 #pragma unroll

@@ -112,12 +112,37 @@ __global__ __launch_bounds__(NT) void top_kernel(const TopArgs a) {
     const int i = atomicAdd(&count, 1);      // (in any order: places are counted below)
     if (i < kList) list_key[i] = key_of(x), list_at[i] = at;
   };
-  if (!(top < from))
-    each_slowly([&](int i, const float (&x)[V]) __attribute__((always_inline)) {
+  // a thread's vectors that reach it are looked for by 16 lanes, those of four threads at a time: read one after another they would each wait for memory
+  auto look = [&](int i, const float (&x)[V]) __attribute__((always_inline)) {
+    if (logits::largest(x) < from) return;
 #pragma unroll
-      for (int j = 0; j < V; ++j)
-        if (!(x[j] < from)) append(x[j], i * V + j);
-    });
+    for (int j = 0; j < V; ++j)
+      if (!(x[j] < from)) append(x[j], i * V + j);
+  };
+  for (unsigned long long reach = __ballot(!(top < from)); reach;) {
+    int who = -1;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (lane >> 4 == u && reach) who = __ffsll(reach) - 1;
+      reach &= reach - 1;
+    }
+    if (who < 0) continue;
+#pragma unroll 1
+    for (int i = 64 * wave + who + (lane & 15) * NT; i < row.full; i += 32 * NT) {
+      const uint4 r[2] = {row.load(i, row.full), row.load(i + 16 * NT, row.full)};
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        float x[V];
+        logits::unpack<T>(r[u], x);
+        look(i + u * 16 * NT, x);
+      }
+    }
+  }
+  if (row.tail && t == NT - 1) {
+    float x[V];
+    row.edge(true, x);
+    look(row.full, x);
+  }
   __syncthreads();
   int n = count;
   if (n > kList) {      // Many equal to the bound, as where most of a row has the type's lowest value: of those only the first k can count.
@@ -198,6 +223,7 @@ __global__ __launch_bounds__(NT) void top_kernel(const TopArgs a) {
     const unsigned key = list_key[i];
     const int at = list_at[i];
     int place = 0;
+#pragma unroll 4
     for (int j = 0; j < n; ++j) place += list_key[j] > key || (list_key[j] == key && list_at[j] < at);
     if (place < a.k) {
       values[place] = (OUT)number_of(key);
