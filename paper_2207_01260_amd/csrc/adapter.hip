@@ -32,8 +32,8 @@ __device__ __forceinline__ int last_of(const int* from, int n, int x) {
   return lo;
 }
 
-// One work-group: the rows of each adapter behind each other in their order, in tiles of their own, rows without an adapter last.  Wavefronts count runs of rows, up to 1024
-// each at once, and place them behind what the others have counted; in 64 rows the equal ones find each other by the bits of their adapter, and their first counts for all.
+// One work-group: the rows of each adapter behind each other in their order, in tiles of their own, rows without an adapter last.  Wavefronts count runs of rows and
+// place them on a second walk, behind what the others have counted.
 __device__ void sort_rows(const SortArgs& p, int* shared, int2* waves) {
   const int t = (int)threadIdx.x, lane = t & 63, wave = t >> 6, n = p.adapters, buckets = n + 1, threads = 64 * kSortWaves;
   int* const count = shared;                              // [wavefront][bucket]
@@ -44,90 +44,67 @@ __device__ void sort_rows(const SortArgs& p, int* shared, int2* waves) {
   const int run = ((p.rows - 1) / (64 * p.waves) + 1) * 64, from = (int)min((long)wave * run, (long)p.rows), end = (int)min((long)from + run, (long)p.rows);
   const int bits = 32 - __clz(n);
   int* const mine = count + wave * buckets;
-  // 16 times 64 rows: their adapters, all under way at once; then, of each, how many the wavefront has had of the same one before
-  auto load = [&](int r0, int (&b)[16]) __attribute__((always_inline)) {
+  // The wavefront's rows 1024 at a time: their adapters are asked for at once and kept in LDS, so that the loops over them are short code.
+  unsigned short* const kept = reinterpret_cast<unsigned short*>(span_at + buckets + 1 + (buckets & 1)) + wave * 1024;
+  auto load = [&](int r0) __attribute__((always_inline)) {
+    int b[16];
 #pragma unroll
     for (int u = 0; u < 16; ++u) {
       const int r = r0 + 64 * u + lane;
       b[u] = r < end ? p.which[r] : -1;
     }
 #pragma unroll
-    for (int u = 0; u < 16; ++u) b[u] = (unsigned)b[u] < (unsigned)n ? b[u] : n;
+    for (int u = 0; u < 16; ++u) kept[64 * u + lane] = (unsigned short)((unsigned)b[u] < (unsigned)n ? b[u] : n);
   };
-  auto match = [&](int r0, const int (&b)[16], int (&at)[16]) __attribute__((always_inline)) {
-#pragma unroll
+  const bool once = run <= 1024;
+  for (int r0 = from; r0 < end; r0 += 1024) {
+    load(r0);
+#pragma unroll 4
     for (int u = 0; u < 16; ++u) {
-      const int first = r0 + 64 * u;
-      if (first >= end) break;
-      const int v = b[u], one = __builtin_amdgcn_readfirstlane(v);
-      if (first + 64 <= end && __all(v == one)) {      // (as in a long request's rows)
-        int before = 0;
-        if (lane == 0) before = atomicAdd(&mine[one], 64);
-        at[u] = __builtin_amdgcn_readfirstlane(before) + lane;
-        continue;
+      const int r = r0 + 64 * u, v = kept[64 * u + lane], one = __builtin_amdgcn_readfirstlane(v), here = min(64, end - r);
+      if (__all(v == one || lane >= here)) {      // (as in a long request's rows)
+        if (lane == 0 && here > 0) atomicAdd(&mine[one], here);
+      } else if (lane < here) {
+        atomicAdd(&mine[v], 1);
       }
-      const bool in = first + lane < end;
-      unsigned long long same = __ballot(in);
-#pragma unroll 1
-      for (int i = 0; i < bits; ++i) {
-        const unsigned long long set = __ballot(v >> i & 1);
-        same &= v >> i & 1 ? set : ~set;
-      }
-      const int lead = __ffsll(same) - 1;
-      int before = 0;
-      if (in && lane == lead) before = atomicAdd(&mine[v], __popcll(same));      // (the wavefront's own: in its order)
-      at[u] = __shfl(before, lead & 63, 64) + __popcll(same & ((1ull << lane) - 1));
     }
-  };
-  auto place = [&](int r0, const int (&b)[16], const int (&at)[16], bool from_zero) __attribute__((always_inline)) {
-#pragma unroll
-    for (int u = 0; u < 16; ++u) {
-      const int r = r0 + 64 * u + lane;
-      if (r < end) p.order[at[u] + (from_zero ? mine[b[u]] : 0)] = r;
-    }
-  };
-  int b[16], at[16];
-  const bool once = run <= 64 * 16;
-  for (int r0 = from; r0 < end; r0 += 64 * 16) {
-    load(r0, b);
-    match(r0, b, at);
   }
   __syncthreads();
-  // tiles and spans of each bucket, and where they begin
-  const int each = (buckets - 1) / threads + 1, b0 = min(t * each, buckets), b1 = min(b0 + each, buckets);
-  int2 sum = {0, 0};
-  auto tiles_of = [&](int b) {
-    int rows = 0;
-    for (int w = 0; w < p.waves; ++w) rows += count[w * buckets + b];
-    return (rows + kTileRows - 1) / kTileRows;
-  };
-  auto spans_of = [&](int b, int tiles) { return b < n ? (tiles + p.span_tiles - 1) / p.span_tiles : 0; };
-  for (int b = b0; b < b1; ++b) {
-    const int tiles = tiles_of(b);
-    sum.x += tiles, sum.y += spans_of(b, tiles);
-  }
-  int2 before = sum;
-  for (int o = 1; o < 64; o <<= 1) {
-    const int x = __shfl_up(before.x, o, 64), y = __shfl_up(before.y, o, 64);
-    if (lane >= o) before.x += x, before.y += y;
-  }
-  if (lane == 63) waves[wave] = before;
-  __syncthreads();
-  before.x -= sum.x, before.y -= sum.y;
-  for (int w = 0; w < wave; ++w) before.x += waves[w].x, before.y += waves[w].y;
-  for (int b = b0; b < b1; ++b) {
-    const int tiles = tiles_of(b);
-    tile_at[b] = before.x;
-    span_at[b] = before.y;
-    int at = before.x * kTileRows;
-    for (int w = 0; w < p.waves; ++w) {
-      const int c = count[w * buckets + b];
-      count[w * buckets + b] = at;
-      at += c;
+  // Where each bucket's tiles and spans begin, and in them each wavefront's rows: 16 lanes have a bucket, those of the wavefronts beside each other.
+  if (t == 0) tile_at[0] = span_at[0] = 0;
+  const int w = t & 15;
+  for (int b0 = 0; b0 < buckets; b0 += threads / 16) {
+    const int b = b0 + t / 16;
+    const int c = b < buckets && w < p.waves ? count[w * buckets + b] : 0;
+    int upto = c;
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) {
+      const int v = __shfl_up(upto, o, 16);
+      upto += w >= o ? v : 0;
     }
-    before.x += tiles, before.y += spans_of(b, tiles);
-    for (; at < before.x * kTileRows; ++at) p.order[at] = -1;
-    if (b == n) tile_at[buckets] = before.x;
+    const int rows = __shfl(upto, 15, 16), tiles = (rows + kTileRows - 1) / kTileRows, spans = b < n ? (tiles + p.span_tiles - 1) / p.span_tiles : 0;
+    // (over the wavefront's four buckets, the work-group's wavefronts and the buckets before)
+    int2 before = {w == 0 ? tiles : 0, w == 0 ? spans : 0};
+#pragma unroll
+    for (int o = 16; o < 64; o <<= 1) {
+      const int x = __shfl_up(before.x, o, 64), y = __shfl_up(before.y, o, 64);
+      before.x += lane >= o ? x : 0, before.y += lane >= o ? y : 0;
+    }
+    __syncthreads();      // (tile_at and `waves` of the buckets before)
+    if (lane == 48) waves[wave] = before;
+    __syncthreads();
+    int2 base = {tile_at[b0], span_at[b0]};
+    for (int v = 0; v < wave; ++v) base.x += waves[v].x, base.y += waves[v].y;
+    const int first_tile = __shfl(base.x + before.x - tiles, lane & 48, 64);
+    if (b < buckets) {
+      const int at = first_tile * kTileRows;
+      if (w < p.waves) count[w * buckets + b] = at + upto - c;
+      for (int i = at + rows + w; i < at + tiles * kTileRows; i += 16) p.order[i] = -1;
+      if (w == 0) {
+        tile_at[b + 1] = first_tile + tiles;
+        if (b < n) span_at[b + 1] = base.y + before.y;
+      }
+    }
   }
   __syncthreads();
   const int tiles = tile_at[buckets];
@@ -142,14 +119,41 @@ __device__ void sort_rows(const SortArgs& p, int* shared, int2* waves) {
     }
     for (int i = t; i <= n; i += threads) p.span_of[i] = span_at[i];
   }
-  if (once) {
-    if (from < end) place(from, b, at, true);
-    return;
-  }
-  for (int r0 = from; r0 < end; r0 += 64 * 16) {
-    load(r0, b);
-    match(r0, b, at);
-    place(r0, b, at, false);
+  // The rows' places.  In 64 rows the equal ones find each other by the bits of their adapter, and their first counts for all; four times 64 rows side by side.
+  for (int r0 = from; r0 < end; r0 += 1024) {
+    if (!once) load(r0);
+#pragma unroll 1
+    for (int u0 = 0; u0 < 16 && r0 + 64 * u0 < end; u0 += 4) {
+      int v[4], at[4];
+      unsigned long long same[4];
+      bool runs = true;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        v[u] = kept[64 * (u0 + u) + lane];
+        same[u] = __ballot(r0 + 64 * (u0 + u) + lane < end);
+        runs &= __all(v[u] == __builtin_amdgcn_readfirstlane(v[u])) != 0;
+      }
+      if (!runs) {
+#pragma unroll 1
+        for (int i = 0; i < bits; ++i) {
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const unsigned long long set = __ballot(v[u] >> i & 1);
+            same[u] &= v[u] >> i & 1 ? set : ~set;
+          }
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        at[u] = 0;
+        if (same[u] >> lane & 1 && lane == __ffsll(same[u]) - 1) at[u] = atomicAdd(&mine[v[u]], __popcll(same[u]));      // (the wavefront's own, in its order)
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int to = __shfl(at[u], (__ffsll(same[u]) - 1) & 63, 64) + __popcll(same[u] & ((1ull << lane) - 1));
+        if (same[u] >> lane & 1) p.order[to] = r0 + 64 * (u0 + u) + lane;
+      }
+    }
   }
 }
 
@@ -199,6 +203,18 @@ __global__ __launch_bounds__(64 * kSortWaves) void adapter_prepare_kernel(const 
   }
   if (i < tiles_a) turn_tile<T>(a, i, reinterpret_cast<T*>(shared));
   else turn_tile<T>(b, i - tiles_a, reinterpret_cast<T*>(shared));
+}
+
+// B [row][rank] -> [row][padded], zeros past the rank, 16 bytes a thread: where ranks do not fill vectors.
+template <typename T>
+__global__ __launch_bounds__(256) void adapter_pad_kernel(const T* __restrict__ b, long vectors, int rank, int padded, uint4* __restrict__ out) {
+  constexpr int V = adapter::kV<T>;
+  const long i = (long)blockIdx.x * 256 + threadIdx.x;
+  if (i >= vectors) return;
+  const int per = padded / V;
+  const long row = i / per;
+  const int at = (int)(i - row * per) * V;
+  out[i] = adapter::load_some(b + row * rank + at, rank - at);
 }
 
 // Sums of an adapter's spans in their order: db [adapter][c][rank] from [span][c][RP], da [adapter][rank][k] from [span][RP][k].  Lanes share a result where there are
@@ -268,6 +284,9 @@ struct AdapterPlan {
   size_t total() const { return order + tile_of + span_first + span_of + part + bt + at + g + 2 * parts + sums_b + sums_a; }
 };
 
+// Tiles as they are likely to be: half of the adapters' last ones are there, half are not.
+int rounded_tiles(const cprune_adapter_desc& d, const AdapterPlan& q) { return q.sorted ? std::min(q.tiles, d.rows / kTileRows + 1 + d.adapters / 2) : q.tiles; }
+
 AdapterPlan plan_of(const cprune_adapter_desc& d, bool backward) {
   AdapterPlan q = {};
   const size_t es = dtype_size(d.dtype);
@@ -280,8 +299,8 @@ AdapterPlan plan_of(const cprune_adapter_desc& d, bool backward) {
   if (q.sorted) q.tiles = std::min(d.rows, d.rows / kTileRows + d.adapters + 1);
   q.places = (int)std::min(2147483647L, (long)q.tiles * kTileRows);      // (more is refused)
   // enough work-groups to bring x, each wavefront four steps at least
-  const int terms = backward ? d.c_out : d.k, steps = (terms - 1) / q.step + 1;
-  const int splits = std::max(1, std::min({768 / q.tiles, steps / 16, 16}));
+  const int terms = backward ? d.c_out : d.k, steps = std::max(1, terms / q.step);      // (whole ones)
+  const int splits = std::max(1, std::min({256 * narrow_waves(q.ranks) / rounded_tiles(d, q), steps / 16, 16}));
   q.per = (steps - 1) / splits + 1;
   q.splits = (steps - 1) / q.per + 1;
   q.part = round256((size_t)q.splits * d.rows * q.rp * sizeof(float));
@@ -289,8 +308,11 @@ AdapterPlan plan_of(const cprune_adapter_desc& d, bool backward) {
     q.order = round256((size_t)q.places * sizeof(int));
     q.tile_of = round256((size_t)q.tiles * sizeof(int));
   }
-  if (!backward) return q;
   q.padded = (d.rank + 7) / 8 * 8;
+  if (!backward) {
+    if (d.rank % 8) q.bt = round256((size_t)d.adapters * d.c_out * q.padded * es);
+    return q;
+  }
   q.bt = round256((size_t)d.adapters * d.rank * d.c_out * es);
   q.at = round256((size_t)d.adapters * d.k * q.padded * es);
   q.g = round256((size_t)d.rows * q.rp * sizeof(float));
@@ -298,7 +320,7 @@ AdapterPlan plan_of(const cprune_adapter_desc& d, bool backward) {
   const int wide = 16 * (16 / (int)es);      // columns of a work-group
   q.groups_b = (d.c_out - 1) / wide + 1, q.groups_a = (d.k - 1) / wide + 1;
   // spans: enough work-groups, and long enough that their sums are few beside what is read
-  const int groups = q.groups_a + q.groups_b, want = std::max(1, 768 / groups);
+  const int groups = q.groups_a + q.groups_b, want = std::max(1, 256 * kOuterWaves / groups);
   q.span_tiles = std::max(2, ((d.rows - 1) / kTileRows + want) / want);
   q.spans = q.sorted ? std::min(q.tiles, q.tiles / q.span_tiles + d.adapters) : (q.tiles - 1) / q.span_tiles + 1;
   if (q.sorted) {
@@ -315,7 +337,7 @@ bool fits(const cprune_adapter_desc& d, const AdapterPlan& q, bool backward) {
   const double most = 4294967296.0 / 256;
   const int c = backward ? d.k : d.c_out;
   if ((double)q.tiles * q.splits >= most || (double)q.tiles * ((c - 1) / 256 + 1) >= most || (double)q.tiles * kTileRows >= 2147483648.0 || (double)q.tiles * q.ranks >= most) return false;
-  if (!backward) return true;
+  if (!backward) return (double)d.adapters * d.c_out * q.padded / 4 < 4294967040.0;
   const double turned = (double)d.adapters * ((d.k + 63.0) / 64 + (d.c_out + 63.0) / 64) * 2;      // (ranks of up to 128 are two tiles)
   return turned < most / 4 - 1 && (double)q.spans * (q.groups_a + q.groups_b) < most && (double)d.adapters * d.rank * ((double)d.k + d.c_out) < 4294967040.0;
 }
@@ -348,14 +370,14 @@ void prepare(const cprune_adapter_desc& d, const AdapterPlan& q, AdapterTiles& t
   if (q.sorted) {
     int* const order = ws.take<int>(q.order);
     int* const tile_of = ws.take<int>(q.tile_of);
-    sort = {t.which, d.rows, d.adapters, q.places, std::max(1, q.span_tiles), q.spans, d.adapters > 512 ? kSortWaves / 2 : kSortWaves, order, tile_of, span_first, span_of};
+    sort = {t.which, d.rows, d.adapters, q.places, std::max(1, q.span_tiles), q.spans, d.adapters > 384 ? kSortWaves / 2 : kSortWaves, order, tile_of, span_first, span_of};
     t.order = order, t.tile_of = tile_of;
   }
   const int tiles_a = a.row_tiles * a.col_tiles * d.adapters, tiles_b = b.row_tiles * b.col_tiles * d.adapters;
   const unsigned grid = (unsigned)(q.sorted + tiles_a + tiles_b);
   if (!grid) return;
   const size_t es = dtype_size(d.dtype);
-  size_t lds = q.sorted ? ((size_t)sort.waves * (d.adapters + 1) + 2 * d.adapters + 4) * sizeof(int) : 0;
+  size_t lds = q.sorted ? ((size_t)sort.waves * (d.adapters + 1) + 2 * d.adapters + 8) * sizeof(int) + 2048 * sort.waves : 0;
   if (tiles_a + tiles_b) lds = std::max(lds, 64 * 65 * es);
   if (es == 4) adapter_prepare_kernel<unsigned><<<grid, 64 * kSortWaves, lds, s>>>(sort, a, b, tiles_a);
   else adapter_prepare_kernel<unsigned short><<<grid, 64 * kSortWaves, lds, s>>>(sort, a, b, tiles_a);
@@ -364,10 +386,16 @@ void prepare(const cprune_adapter_desc& d, const AdapterPlan& q, AdapterTiles& t
 // What does not stay in the last-level cache (256 MB, shared with what else is in use) is stored past it.
 bool past_caches(const cprune_adapter_desc& d, int c, const void* base) { return (base ? 2.0 : 1.0) * d.rows * c * dtype_size(d.dtype) > 134217728.0; }
 
-int columns_of(const AdapterPlan& q, int c) {      // of a work-group: fewer where tiles are few
-  int columns = 1024;
-  while (columns > 256 && (long)q.tiles * ((c - 1) / columns + 1) < 512) columns /= 2;
-  return columns;
+// Columns of a work-group: those that take the fewest rounds of work-groups, by the columns of each and what it does but once, some 200 columns' time.
+int columns_of(const cprune_adapter_desc& d, const AdapterPlan& q, int c) {
+  const long resident = 256 * widen_waves(q.ranks, (int)dtype_size(d.dtype)), tiles = rounded_tiles(d, q);
+  int best = 256;
+  long least = std::numeric_limits<long>::max();
+  for (int columns = 256; columns <= 2048; columns *= 2) {
+    const long groups = tiles * ((c - 1) / columns + 1), cost = ((groups - 1) / resident + 1) * (std::min(columns, c) + 200);
+    if (cost < least) least = cost, best = columns;
+  }
+  return best;
 }
 
 }  // namespace
@@ -395,15 +423,24 @@ extern "C" int cprune_adapter_linear(const cprune_adapter_desc* d, const void* x
   AdapterTiles tiles = tiles_of(*d, q, which);
   prepare(*d, q, tiles, nullptr, nullptr, {}, {}, scratch, s);
   float* const part = scratch.take<float>(q.part);
-  AdapterLaunch l = {(unsigned)(q.tiles * q.splits), q.ranks, d->act == CPRUNE_ACT_SILU};
+  AdapterLaunch l = {(unsigned)(q.tiles * q.splits), q.ranks, d->rows <= 16, false};
   const NarrowArgs n = {tiles, x, d->x_stride, d->k, d->rank, a, part, q.splits, q.per};
   launch(d->dtype, kAdapterNarrow, &n, l, s);
   const float open = std::numeric_limits<float>::infinity();
   WidenArgs w = {};
-  w.tiles = tiles, w.part = part, w.splits = q.splits, w.rank = d->rank, w.scale = scale, w.b = b, w.c = d->c_out, w.b_stride = d->rank;
+  w.tiles = tiles, w.part = part, w.splits = q.splits, w.rank = d->rank, w.scale = scale, w.b = b, w.c = d->c_out, w.b_stride = q.padded;
+  w.silu = d->act == CPRUNE_ACT_SILU;
+  if (d->rank % 8) {
+    uint4* const padded = scratch.take<uint4>(q.bt);
+    const long vectors = (long)d->adapters * d->c_out * q.padded / (16 / (long)dtype_size(d->dtype));
+    const unsigned grid = (unsigned)((vectors + 255) / 256);
+    if (d->dtype == CPRUNE_F32) adapter_pad_kernel<float><<<grid, 256, 0, s>>>(static_cast<const float*>(b), vectors, d->rank, q.padded, padded);
+    else adapter_pad_kernel<__bf16><<<grid, 256, 0, s>>>(static_cast<const __bf16*>(b), vectors, d->rank, q.padded, padded);
+    w.b = padded;
+  }
   w.base = base, w.base_stride = d->base_stride, w.y = y, w.hidden = hidden;
   w.lo = d->act == CPRUNE_ACT_NONE || d->act == CPRUNE_ACT_SILU ? -open : 0.0f, w.hi = d->act == CPRUNE_ACT_RELU6 ? 6.0f : open;
-  w.columns = columns_of(q, d->c_out);
+  w.columns = columns_of(*d, q, d->c_out);
   w.stream = past_caches(*d, d->c_out, base);
   l.grid = (unsigned)(q.tiles * ((d->c_out - 1) / w.columns + 1));
   launch(d->dtype, kAdapterWiden, &w, l, s);
@@ -439,7 +476,8 @@ extern "C" int cprune_adapter_linear_backward(const cprune_adapter_desc* d, cons
   char* const hidden_parts = scratch.take<char>(q.parts);
   float* const sums_b = scratch.take<float>(q.sums_b);
   float* const sums_a = scratch.take<float>(q.sums_a);
-  AdapterLaunch l = {(unsigned)(q.tiles * q.splits), q.ranks, false};
+  const int v = 16 / (int)dtype_size(d->dtype);
+  AdapterLaunch l = {(unsigned)(q.tiles * q.splits), q.ranks, d->rows <= 16, d->k < v || d->c_out < v};
   const NarrowArgs n = {tiles, dy, d->dy_stride, d->c_out, d->rank, bt, part, q.splits, q.per};
   launch(d->dtype, kAdapterNarrow, &n, l, s);
   PartsArgs r = {};
@@ -451,9 +489,9 @@ extern "C" int cprune_adapter_linear_backward(const cprune_adapter_desc* d, cons
   if (dx) {
     const float open = std::numeric_limits<float>::infinity();
     WidenArgs w = {};
-    w.tiles = tiles, w.part = g, w.splits = 1, w.rank = q.padded, w.b = at, w.c = d->k, w.b_stride = q.padded;
+    w.tiles = tiles, w.part = g, w.splits = 1, w.rank = d->rank, w.b = at, w.c = d->k, w.b_stride = q.padded;
     w.base = dx_base, w.base_stride = d->base_stride, w.y = dx, w.lo = -open, w.hi = open;
-    w.columns = columns_of(q, d->k);
+    w.columns = columns_of(*d, q, d->k);
     w.stream = past_caches(*d, d->k, dx_base);
     l.grid = (unsigned)(q.tiles * ((d->k - 1) / w.columns + 1));
     launch(d->dtype, kAdapterWiden, &w, l, s);

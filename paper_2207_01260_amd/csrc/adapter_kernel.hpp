@@ -21,6 +21,11 @@ namespace cprune {
 
 constexpr int kTileRows = 64;
 
+// Work-groups of 256 that a compute unit holds at once, by registers; what is cut into work-groups is cut for whole rounds of them.
+constexpr int narrow_waves(int ranks) { return ranks <= 2 ? 3 : ranks <= 4 ? 2 : 1; }
+constexpr int widen_waves(int ranks, int size) { return ranks <= 2 ? (size == 2 ? 3 : 2) : ranks == 4 && size == 2 ? 2 : 1; }
+constexpr int kOuterWaves = 2;
+
 // Places: tile t has rows order[64 t .. 64 t + 63], -1 where it has fewer.
 struct AdapterTiles {
   const int* which;        // few: the rows' adapters, a ballot finds the tile of row t if that is its first
@@ -45,7 +50,7 @@ struct WidenArgs {
   const float* part;       // [splits][rows][RP]
   int splits, rank;
   const float* scale;      // or null
-  const void* b;           // [adapters][c][b_stride], rank numbers of each row
+  const void* b;           // [adapters][c][b_stride], rank numbers of each row, then zeros: a multiple of 8
   int c, b_stride;
   const void* base;
   long base_stride;
@@ -54,6 +59,7 @@ struct WidenArgs {
   float lo, hi;
   int columns;             // of a work-group, a multiple of 128
   bool stream;             // y is stored past the caches
+  bool silu;
 };
 
 // hidden and g as the outer product's operands: 16-bit, three bf16 parts [3][RP][places], fp32 [RP][places]
@@ -87,7 +93,8 @@ struct OuterArgs {
 struct AdapterLaunch {
   unsigned grid;
   int ranks;               // RP / 16, RP the rank filled up to 16, 32, 64 or 128
-  bool silu;
+  bool few;                // tiles of up to 16 rows (narrow, widen)
+  bool thin;               // a side has fewer than V columns (outer)
 };
 enum AdapterPass { kAdapterNarrow, kAdapterWiden, kAdapterParts, kAdapterOuter };
 void launch_adapter_f32(AdapterPass pass, const void* args, const AdapterLaunch& l, hipStream_t s);
@@ -99,13 +106,16 @@ namespace adapter {
 template <typename T> constexpr int kV = 16 / (int)sizeof(T);       // numbers of 16 bytes
 template <typename T> constexpr int kStep = 4 * kV<T>;              // terms of a step
 
-// V numbers at p, of which `valid` are there, zeros past them
-template <typename T> __device__ __forceinline__ uint4 load(const T* p, int valid) {
+// V numbers at p, at any element
+template <typename T> __device__ __forceinline__ uint4 load(const T* p) {
   typedef unsigned uint4u __attribute__((ext_vector_type(4), aligned(2)));
-  if (valid >= kV<T>) {
-    const uint4u v = *reinterpret_cast<const uint4u*>(p);
-    return make_uint4(v.x, v.y, v.z, v.w);
-  }
+  const uint4u v = *reinterpret_cast<const uint4u*>(p);
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
+__device__ __forceinline__ uint4 keep(const uint4& v, bool all) { return make_uint4(all ? v.x : 0u, all ? v.y : 0u, all ? v.z : 0u, all ? v.w : 0u); }
+// V numbers at p, of which `valid` are there, zeros past them.  Long code: for what is left at an end, not for a loop's every load.
+template <typename T> __device__ __forceinline__ uint4 load_some(const T* p, int valid) {
+  if (valid >= kV<T>) return load(p);
   if (valid <= 0) return make_uint4(0, 0, 0, 0);
   unsigned w[4];
   if constexpr (sizeof(T) == 4) {
@@ -240,9 +250,11 @@ __device__ __forceinline__ float4_t sum_parts(const float* from, int splits, lon
 
 // ---- narrow ----------------------------------------------------------------------
 
-template <typename T, int NR>
-__global__ __launch_bounds__(256) void adapter_narrow_kernel(const NarrowArgs p) {
-  constexpr int V = kV<T>, STEP = kStep<T>, RP = 16 * NR, U = NR <= 2 ? 4 : NR <= 4 ? 2 : 1;
+// F: a tile's rows in sixteens, 4, or 1 where there are no more.  Rows that a tile has not are its first one again: they make results of their own, which nobody
+// reads.  Ranks past the last are the last again, left out by who reads them.
+template <typename T, int NR, int F>
+__global__ __launch_bounds__(256, narrow_waves(NR)) void adapter_narrow_kernel(const NarrowArgs p) {
+  constexpr int V = kV<T>, STEP = kStep<T>, RP = 16 * NR, U = F == 1 ? (NR <= 4 ? 4 : 2) : (NR <= 2 ? 2 : 1);
   __shared__ Tile tile;
   __shared__ float sums[4][16][RP + 4];
   const int t = (int)threadIdx.x, lane = t & 63, wave = t >> 6, quarter = lane >> 4, lrow = lane & 15;
@@ -250,49 +262,75 @@ __global__ __launch_bounds__(256) void adapter_narrow_kernel(const NarrowArgs p)
   int count;
   const int adapter = open_tile(p.tiles, tile_no, tile, count);
   if (adapter < 0) return;      // (rows without an adapter: what would be read here is known to be 0)
-  const T* const a = static_cast<const T*>(p.a) + (long)adapter * p.rank * p.k;
-  const T* rows[4];
-  bool there[4];
+  const T* rows[F];
+  const T* ranks[NR];
 #pragma unroll
-  for (int f = 0; f < 4; ++f) {
+  for (int f = 0; f < F; ++f) {
     const int r = tile.row[16 * f + lrow];
-    there[f] = r >= 0;
-    rows[f] = static_cast<const T*>(p.x) + (long)max(r, 0) * p.stride + quarter * V;
+    rows[f] = static_cast<const T*>(p.x) + (long)(r >= 0 ? r : tile.row[0]) * p.stride + quarter * V;
   }
-  float4_t acc[4][NR];
 #pragma unroll
-  for (int f = 0; f < 4; ++f)
+  for (int n = 0; n < NR; ++n) ranks[n] = static_cast<const T*>(p.a) + ((long)adapter * p.rank + min(16 * n + lrow, p.rank - 1)) * p.k + quarter * V;
+  float4_t acc[F][NR];
+#pragma unroll
+  for (int f = 0; f < F; ++f)
 #pragma unroll
     for (int n = 0; n < NR; ++n) acc[f][n] = (float4_t){0.f, 0.f, 0.f, 0.f};
-  const int frags = (count + 15) / 16;
-  // a wavefront has a quarter of the work-group's steps
-  const int steps = min(p.per, (p.k - 1) / STEP + 1 - split * p.per), run = (steps + 3) / 4;
-  const int first = split * p.per + wave * run, last = min(first + run, split * p.per + steps);
-  for (int s = first; s < last; s += U) {
-    uint4 xs[U][4], as[U][NR];
+  struct Operands {
+    uint4 x[F], a[NR];
+  };
+  auto fetch = [&](int s, Operands& q) __attribute__((always_inline)) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int at = (s + u) * STEP, valid = s + u < last ? p.k - at - quarter * V : 0;
+    for (int f = 0; f < F; ++f) q.x[f] = load(rows[f] + (long)s * STEP);
 #pragma unroll
-      for (int f = 0; f < 4; ++f)
-        if (f < frags) xs[u][f] = load(rows[f] + at, there[f] ? valid : 0);
+    for (int n = 0; n < NR; ++n) q.a[n] = load(ranks[n] + (long)s * STEP);
+  };
+  auto multiply = [&](const Operands& q) __attribute__((always_inline)) {
 #pragma unroll
-      for (int n = 0; n < NR; ++n) {
-        const int j = 16 * n + lrow;
-        as[u][n] = load(a + (long)j * p.k + at + quarter * V, j < p.rank ? valid : 0);
-      }
+    for (int f = 0; f < F; ++f)
+#pragma unroll
+      for (int n = 0; n < NR; ++n) acc[f][n] = mma<T>(q.a[n], q.x[f], acc[f][n]);
+  };
+  // a wavefront has a quarter of the work-group's whole steps, U of them under way while U are multiplied
+  const int whole = p.k / STEP, begin = split * p.per, steps = min(p.per, whole - begin), run = (steps + 3) / 4;
+  const int last = min(begin + (wave + 1) * run, begin + steps);
+  int s = begin + wave * run;
+  if (s + U <= last) {
+    Operands now[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) fetch(s + u, now[u]);
+#pragma unroll 1
+    for (; s + 2 * U <= last; s += U) {
+      Operands next[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) fetch(s + U + u, next[u]);
+#pragma unroll
+      for (int u = 0; u < U; ++u) multiply(now[u]);
+#pragma unroll
+      for (int u = 0; u < U; ++u) now[u] = next[u];
     }
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-      for (int f = 0; f < 4; ++f)
-        if (f < frags) {
-#pragma unroll
-          for (int n = 0; n < NR; ++n) acc[f][n] = mma<T>(as[u][n], xs[u][f], acc[f][n]);
-        }
+    for (int u = 0; u < U; ++u) multiply(now[u]);
+    s += U;
   }
+#pragma unroll 1
+  for (; s < last; ++s) {
+    Operands q;
+    fetch(s, q);
+    multiply(q);
+  }
+  if (p.k % STEP && split == p.splits - 1 && wave == 3) {      // what is left of a row
+    const int at = whole * STEP, valid = p.k - at - quarter * V;
+    Operands q;
 #pragma unroll
-  for (int f = 0; f < 4; ++f) {
+    for (int f = 0; f < F; ++f) q.x[f] = load_some(rows[f] + at, valid);
+#pragma unroll
+    for (int n = 0; n < NR; ++n) q.a[n] = load_some(ranks[n] + at, valid);
+    multiply(q);
+  }
+  const int frags = min((count + 15) / 16, F);
+#pragma unroll
+  for (int f = 0; f < F; ++f) {
     if (f >= frags) break;
     if (f) __syncthreads();
 #pragma unroll
@@ -311,49 +349,53 @@ __global__ __launch_bounds__(256) void adapter_narrow_kernel(const NarrowArgs p)
 
 // ---- widen -----------------------------------------------------------------------
 
-template <typename T, int NR, bool SILU>
-__global__ __launch_bounds__(256) void adapter_widen_kernel(const WidenArgs p) {
+template <typename T, int NR, int F>
+__global__ __launch_bounds__(256, widen_waves(NR, sizeof(T))) void adapter_widen_kernel(const WidenArgs p) {
   constexpr int V = kV<T>, STEP = kStep<T>, RP = 16 * NR, NS = (RP + STEP - 1) / STEP, N = sizeof(T) == 4 ? 1 : 2;
   __shared__ Tile tile;
   __shared__ float results[4][16][64 + 4];
-  __shared__ float hidden[kTileRows][NS * STEP + 4];
+  __shared__ float hidden[16 * F][NS * STEP + 4];
   const int t = (int)threadIdx.x, lane = t & 63, wave = t >> 6, quarter = lane >> 4, lrow = lane & 15;
   const int chunks = (p.c - 1) / p.columns + 1;
   const int tile_no = blockIdx.x / (unsigned)chunks, chunk = blockIdx.x - tile_no * chunks;
   int count;
   const int adapter = open_tile(p.tiles, tile_no, tile, count);
   if (adapter == -2) return;
-  const int frags = (count + 15) / 16;
-  // 64 columns at a time: the weights of the next ones are asked for before these are multiplied
+  const int frags = min((count + 15) / 16, F);      // (a sorted tile is 64 places, whatever its rows)
+  // 64 columns at a time.  Columns past the last are the last again, whose results nobody stores.
   const T* const b = static_cast<const T*>(p.b) + (long)max(adapter, 0) * p.c * p.b_stride;
   const int run = p.columns / 4, begin = chunk * p.columns + wave * run, end = min(p.c, begin + run);
   auto weights = [&](int c0, uint4 (&w)[4][NS]) __attribute__((always_inline)) {
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      const int c = c0 + 16 * g + lrow;
+      const T* const from = b + (long)min(c0 + 16 * g + lrow, p.c - 1) * p.b_stride;
 #pragma unroll
-      for (int s = 0; s < NS; ++s) w[g][s] = load(b + (long)c * p.b_stride + s * STEP + quarter * V, c < p.c && adapter >= 0 ? p.rank - s * STEP - quarter * V : 0);
+      for (int s = 0; s < NS; ++s) {
+        const int j = s * STEP + quarter * V;
+        w[g][s] = keep(load(from + (j < p.b_stride ? j : 0)), j < p.b_stride && adapter >= 0);
+      }
     }
   };
+  constexpr bool AHEAD = NS <= 2;      // the next columns' weights are asked for before these are multiplied, where registers hold both
   uint4 w[4][NS];
-  if (begin < end) weights(begin, w);
+  if (AHEAD && begin < end) weights(begin, w);
   // the rows' hidden numbers, zeros past the rank
   const float scale = adapter >= 0 && p.scale ? p.scale[adapter] : 1.0f;
   for (int i = t; i < 16 * frags * NS * STEP / 4; i += 256) {
     const int r = i / (NS * STEP / 4), j = 4 * (i - r * (NS * STEP / 4)), row = tile.row[r];
     float4_t v = {0.f, 0.f, 0.f, 0.f};
-    if (row >= 0 && adapter >= 0 && j < RP) v = scale * sum_parts(p.part + (long)row * RP + j, p.splits, (long)p.tiles.rows * RP);
-    *reinterpret_cast<float4_t*>(&hidden[r][j]) = v;
-    if (p.hidden && chunk == 0 && row >= 0) {
+    if (row >= 0 && adapter >= 0 && j < p.rank) v = scale * sum_parts(p.part + (long)row * RP + j, p.splits, (long)p.tiles.rows * RP);
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (j + e < p.rank) p.hidden[(long)row * p.rank + j + e] = v[e];
+    for (int e = 0; e < 4; ++e) {
+      v[e] = j + e < p.rank ? v[e] : 0.0f;
+      if (p.hidden && chunk == 0 && row >= 0 && j + e < p.rank) p.hidden[(long)row * p.rank + j + e] = v[e];
     }
+    *reinterpret_cast<float4_t*>(&hidden[r][j]) = v;
   }
   __syncthreads();
-  uint4 h[4][NS][N];
+  uint4 h[F][NS][N];
 #pragma unroll
-  for (int f = 0; f < 4; ++f) {
+  for (int f = 0; f < F; ++f) {
     if (f >= frags) continue;
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
@@ -368,27 +410,42 @@ __global__ __launch_bounds__(256) void adapter_widen_kernel(const WidenArgs p) {
       }
     }
   }
+  auto finish = [&](float v) __attribute__((always_inline)) {
+    if (p.silu) return v * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * -1.44269504f));      // (2^x flushes below 2^-126: 1 + e^-z does not see it)
+    v = v < p.lo ? p.lo : v;      // (comparisons and not minimum / maximum: a NaN stays one)
+    return v > p.hi ? p.hi : v;
+  };
   // Results go through LDS, 16 rows of a wavefront at a time, so that base and y are met in whole lines: LINE lanes of 16 bytes a row
   constexpr int LINE = 64 / V, EACH = 16 * LINE / 64;
+  typedef T numbers __attribute__((ext_vector_type(V)));
+  typedef T outs __attribute__((ext_vector_type(V), aligned(2)));
   float (*const out)[64 + 4] = results[wave];
-  const int line = lane / LINE, col = lane % LINE * V;
+  const int line = lane / LINE, col = lane % LINE * V, tail = p.c % V;
+  const T* const base = static_cast<const T*>(p.base);
+  T* const y = static_cast<T*>(p.y);
+#pragma unroll 1
   for (int c0 = begin; c0 < end; c0 += 64) {
-    const int c = c0 + col, valid = p.c - c;
-    uint4 z[4][EACH], next[4][NS];
-    if (p.base) {
+    const int c = c0 + col;
+    const bool whole = c + V <= p.c;
+    uint4 z[F][EACH], next[4][NS];
+    if (p.base && p.c >= V) {
 #pragma unroll
-      for (int f = 0; f < 4; ++f)
+      for (int f = 0; f < F; ++f)
         if (f < frags) {
 #pragma unroll
           for (int i = 0; i < EACH; ++i) {
             const int row = tile.row[16 * f + i * (64 / LINE) + line];
-            z[f][i] = load(static_cast<const T*>(p.base) + (long)max(row, 0) * p.base_stride + c, row >= 0 ? valid : 0);
+            z[f][i] = load(base + (long)(row >= 0 ? row : tile.row[0]) * p.base_stride + min(c, p.c - V));
           }
         }
     }
-    if (c0 + 64 < end) weights(c0 + 64, next);
+    if constexpr (AHEAD) {
+      weights(min(c0 + 64, end - 1), next);
+    } else {
+      weights(c0, w);
+    }
 #pragma unroll
-    for (int f = 0; f < 4; ++f) {
+    for (int f = 0; f < F; ++f) {
       if (f >= frags) break;
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
@@ -412,41 +469,37 @@ __global__ __launch_bounds__(256) void adapter_widen_kernel(const WidenArgs p) {
           for (int u = 0; u < 4; ++u) v[e + u] = q[u];
         }
         if (p.base) {
-          typedef T numbers __attribute__((ext_vector_type(V)));
           const numbers n = __builtin_bit_cast(numbers, z[f][i]);
 #pragma unroll
           for (int e = 0; e < V; ++e) v[e] += Elem<T>::to_f32(n[e]);
         }
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          if constexpr (SILU) {
-            v[e] = v[e] * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v[e] * -1.44269504f));      // (2^x flushes below 2^-126: 1 + e^-z does not see it)
-          } else {
-            v[e] = v[e] < p.lo ? p.lo : v[e];      // (comparisons and not minimum / maximum: a NaN stays one)
-            v[e] = v[e] > p.hi ? p.hi : v[e];
-          }
-        }
-        if (row < 0) continue;
-        T* const to = static_cast<T*>(p.y) + (long)row * p.c + c;
-        typedef T outs __attribute__((ext_vector_type(V), aligned(2)));
         outs o;
 #pragma unroll
-        for (int e = 0; e < V; ++e) o[e] = Elem<T>::from_f32(v[e]);
-        if (valid >= V) {
-          if (p.stream) __builtin_nontemporal_store(o, reinterpret_cast<outs*>(to));
-          else *reinterpret_cast<outs*>(to) = o;
-        } else {
-#pragma unroll
-          for (int e = 0; e < V; ++e)
-            if (e < valid) to[e] = o[e];
+        for (int e = 0; e < V; ++e) o[e] = Elem<T>::from_f32(finish(v[e]));
+        if (row >= 0 && whole) {
+          outs* const to = reinterpret_cast<outs*>(y + (long)row * p.c + c);
+          if (p.stream) __builtin_nontemporal_store(o, to);
+          else *to = o;
+        }
+      }
+      if (tail && c0 + 64 >= p.c) {      // the last columns, fewer than a vector
+#pragma unroll 1
+        for (int i = lane; i < 16 * tail; i += 64) {
+          const int in = i / tail, at = p.c - tail + i - in * tail, row = tile.row[16 * f + in];
+          if (row < 0) continue;
+          float v = out[in][at - c0];
+          if (p.base) v += Elem<T>::to_f32(base[(long)row * p.base_stride + at]);
+          y[(long)row * p.c + at] = Elem<T>::from_f32(finish(v));
         }
       }
       wave_sync();
     }
+    if constexpr (AHEAD) {
 #pragma unroll
-    for (int g = 0; g < 4; ++g)
+      for (int g = 0; g < 4; ++g)
 #pragma unroll
-      for (int s = 0; s < NS; ++s) w[g][s] = next[g][s];
+        for (int s = 0; s < NS; ++s) w[g][s] = next[g][s];
+    }
   }
 }
 
@@ -473,6 +526,8 @@ __global__ __launch_bounds__(256) void adapter_parts_kernel(const PartsArgs p) {
         for (int e = 0; e < 4; ++e) h[e] = j0 + j + e < p.rank ? p.hidden[(long)row * p.rank + j0 + j + e] : 0.0f;
       }
       g = scale * sum_parts(p.part + (long)row * RP + j0 + j, p.splits, (long)p.tiles.rows * RP);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) g[e] = j0 + j + e < p.rank ? g[e] : 0.0f;
     }
     if (p.g && row >= 0) *reinterpret_cast<float4_t*>(p.g + (long)row * RP + j0 + j) = g;
 #pragma unroll
@@ -521,18 +576,23 @@ template <typename T> __device__ __forceinline__ void turn(const uint4 (&r)[kV<T
   }
 }
 
-// A work-group has 16 V columns of a span of tiles with one adapter, all ranks, its wavefronts every fourth step of the rows; ACROSS: results lie [rank][column]
-// instead of [column][rank].  A step's numbers are asked for a step ahead, its rows' places two.
-template <typename T, int NR, bool ACROSS>
+// THIN: a side has fewer than V columns, read one by one.  Otherwise a lane past the last column has the last V again, and stores what their lanes do.
+// A work-group has 16 V columns of a span of tiles with one adapter, all ranks.  Its wavefronts share them: 32 ranks each, so that two fit a SIMD, and steps of the rows where
+// ranks are fewer.  ACROSS: results lie [rank][column] instead of [column][rank].  A step's numbers are asked for a step ahead, its rows' places two.
+template <typename T, int NR, bool ACROSS, bool THIN>
 __device__ __forceinline__ void outer_side(const OuterArgs& p, const OuterSide& side, int span, int group, int first, int last, float4_t* joined) {
-  constexpr int V = kV<T>, STEP = kStep<T>, RP = 16 * NR, N = sizeof(T) == 4 ? 1 : 3;
-  const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, quarter = lane >> 4, lrow = lane & 15;
-  const int c0 = group * 16 * V, c = c0 + lrow * V, valid = side.c - c;
-  float4_t acc[V][NR];
+  constexpr int V = kV<T>, STEP = kStep<T>, RP = 16 * NR, N = sizeof(T) == 4 ? 1 : 3, NW = NR < 2 ? NR : 2, SHARES = NR / NW, STREAMS = 4 / SHARES;
+  const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, quarter = lane >> 4, lrow = lane & 15, share = wave % SHARES, stream = wave / SHARES;
+  auto column = [&](int lane_row) __attribute__((always_inline)) {      // first of the V that lanes of a row number have
+    const int c = group * 16 * V + lane_row * V;
+    return THIN ? c : min(c, side.c - V);
+  };
+  const int c = column(lrow), valid = side.c - c;
+  float4_t acc[V][NW];
 #pragma unroll
   for (int i = 0; i < V; ++i)
 #pragma unroll
-    for (int n = 0; n < NR; ++n) acc[i][n] = (float4_t){0.f, 0.f, 0.f, 0.f};
+    for (int n = 0; n < NW; ++n) acc[i][n] = (float4_t){0.f, 0.f, 0.f, 0.f};
   const T* const x = static_cast<const T*>(side.x) + c;
   const long part = (long)RP * p.places;
   const int end = last * kTileRows;
@@ -555,59 +615,72 @@ __device__ __forceinline__ void outer_side(const OuterArgs& p, const OuterSide& 
       for (int e = 0; e < V; ++e) rows.at[e] = place + e < p.tiles.rows ? place + e : -1;
     }
   };
+  const int any_row = p.tiles.order ? p.tiles.order[first * kTileRows] : first * kTileRows;      // (in the place of none, made zeros where it is multiplied)
   auto fetch = [&](const Rows& rows, uint4 (&r)[V]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) r[e] = load(x + (long)max(rows.at[e], 0) * side.stride, rows.at[e] >= 0 ? valid : 0);
+    for (int e = 0; e < V; ++e) {
+      const T* const from = x + (long)(rows.at[e] >= 0 ? rows.at[e] : any_row) * side.stride;
+      r[e] = THIN ? load_some(from, valid) : load(from);
+    }
   };
-  int at = first * kTileRows + wave * STEP;
-  Rows ahead;
+  int at = first * kTileRows + stream * STEP;
+  Rows ahead, there;
   uint4 now[V];
-  find(at, ahead);
-  fetch(ahead, now);
-  find(at + 4 * STEP, ahead);
-  for (; at < end; at += 4 * STEP) {
-    uint4 q[NR][N];
-#pragma unroll
-    for (int n = 0; n < NR; ++n) {
-      const long from = (long)(16 * n + lrow) * p.places + at + quarter * V;
+  find(at, there);
+  fetch(there, now);
+  find(at + STREAMS * STEP, ahead);
+  for (; at < end; at += STREAMS * STEP) {
+    auto operand = [&](int n, uint4 (&q)[N]) __attribute__((always_inline)) {
+      const long from = (long)(16 * (share * NW + n) + lrow) * p.places + at + quarter * V;
 #pragma unroll
       for (int m = 0; m < N; ++m) {
-        if constexpr (sizeof(T) == 4) q[n][m] = *reinterpret_cast<const uint4*>(static_cast<const float*>(side.parts) + from);
-        else q[n][m] = *reinterpret_cast<const uint4*>(static_cast<const __bf16*>(side.parts) + m * part + from);
+        if constexpr (sizeof(T) == 4) q[m] = *reinterpret_cast<const uint4*>(static_cast<const float*>(side.parts) + from);
+        else q[m] = *reinterpret_cast<const uint4*>(static_cast<const __bf16*>(side.parts) + m * part + from);
       }
-    }
+    };
+    uint4 q[2][N];      // (the next sixteen ranks' beside these)
+    operand(0, q[0]);
     uint4 next[V], turned[V];
     fetch(ahead, next);
-    find(at + 8 * STEP, ahead);
+    bool gap = false;
+#pragma unroll
+    for (int e = 0; e < V; ++e) gap |= there.at[e] < 0;
+    if (__any(gap)) {
+#pragma unroll
+      for (int e = 0; e < V; ++e) now[e] = keep(now[e], there.at[e] >= 0);
+    }
+    there = ahead;
+    find(at + 2 * STREAMS * STEP, ahead);
     turn<T>(now, turned);
 #pragma unroll
-    for (int i = 0; i < V; ++i)
+    for (int n = 0; n < NW; ++n) {
+      if (n + 1 < NW) operand(n + 1, q[(n + 1) % 2]);
 #pragma unroll
-      for (int n = 0; n < NR; ++n) {
-        if constexpr (sizeof(T) == 4) acc[i][n] = ACROSS ? mma<float>(q[n][0], turned[i], acc[i][n]) : mma<float>(turned[i], q[n][0], acc[i][n]);
-        else acc[i][n] = mma_parts<T, N, ACROSS>(turned[i], q[n], acc[i][n]);
+      for (int i = 0; i < V; ++i) {
+        if constexpr (sizeof(T) == 4) acc[i][n] = ACROSS ? mma<float>(q[n % 2][0], turned[i], acc[i][n]) : mma<float>(turned[i], q[n % 2][0], acc[i][n]);
+        else acc[i][n] = mma_parts<T, N, ACROSS>(turned[i], q[n % 2], acc[i][n]);
       }
+    }
 #pragma unroll
     for (int e = 0; e < V; ++e) now[e] = next[e];
   }
-  // the wavefronts' sums joined through LDS, 8 results of each at a time
+  // the wavefronts' sums joined through LDS, up to 8 results of each at a time
   float* const sums = side.sums + (long)span * side.c * RP;
-  constexpr int G = 8 / NR < V ? 8 / NR : V;
+  constexpr int G = 8 / NW < V ? 8 / NW : V, ITEMS = G * NR;
 #pragma unroll
   for (int i0 = 0; i0 < V; i0 += G) {
     if (i0) __syncthreads();
 #pragma unroll
     for (int i = 0; i < G; ++i)
 #pragma unroll
-      for (int n = 0; n < NR; ++n) joined[((i * NR + n) * 4 + wave) * 64 + lane] = acc[i0 + i][n];
+      for (int n = 0; n < NW; ++n) joined[((i * NW + n) * 4 + wave) * 64 + lane] = acc[i0 + i][n];
     __syncthreads();
+#pragma unroll 1
+    for (int item = wave; item < ITEMS; item += 4) {
+      const int of = item % SHARES, in = item / SHARES, i = i0 + in / NW, n = of * NW + in % NW;
+      float4_t v = joined[(in * 4 + of) * 64 + lane];
 #pragma unroll
-    for (int m = 0; m < (G * NR + 3) / 4; ++m) {
-      const int item = m * 4 + wave, i = i0 + item / NR, n = item % NR;
-      if (item >= G * NR) break;
-      float4_t v = joined[item * 4 * 64 + lane];
-#pragma unroll
-      for (int w = 1; w < 4; ++w) v += joined[(item * 4 + w) * 64 + lane];
+      for (int w = 1; w < STREAMS; ++w) v += joined[(in * 4 + w * SHARES + of) * 64 + lane];
       if constexpr (ACROSS) {      // ranks 16 n + 4 quarter + e, column c + i
 #pragma unroll
         for (int e = 0; e < 4; ++e)
@@ -615,7 +688,7 @@ __device__ __forceinline__ void outer_side(const OuterArgs& p, const OuterSide& 
       } else {                     // columns V (4 quarter + e) + i, rank 16 n + lrow
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int col = c0 + V * (4 * quarter + e) + i;
+          const int col = column(4 * quarter + e) + i;
           if (col < side.c) sums[(long)col * RP + 16 * n + lrow] = v[e];
         }
       }
@@ -623,8 +696,8 @@ __device__ __forceinline__ void outer_side(const OuterArgs& p, const OuterSide& 
   }
 }
 
-template <typename T, int NR>
-__global__ __launch_bounds__(256) void adapter_outer_kernel(const OuterArgs p) {
+template <typename T, int NR, bool THIN>
+__global__ __launch_bounds__(256, kOuterWaves) void adapter_outer_kernel(const OuterArgs p) {
   __shared__ float4_t joined[8 * 4 * 64];
   const int groups = p.side[0].groups + p.side[1].groups;
   const int span = blockIdx.x / (unsigned)groups;
@@ -636,16 +709,18 @@ __global__ __launch_bounds__(256) void adapter_outer_kernel(const OuterArgs p) {
   } else {
     first = span * p.span_tiles, last = min(first + p.span_tiles, p.tile_count);
   }
-  if (group < p.side[0].groups) outer_side<T, NR, false>(p, p.side[0], span, group, first, last, joined);
-  else outer_side<T, NR, true>(p, p.side[1], span, group - p.side[0].groups, first, last, joined);
+  if (group < p.side[0].groups) outer_side<T, NR, false, THIN>(p, p.side[0], span, group, first, last, joined);
+  else outer_side<T, NR, true, THIN>(p, p.side[1], span, group - p.side[0].groups, first, last, joined);
 }
 
 template <typename T, int NR> void launch_ranks(AdapterPass pass, const void* args, const AdapterLaunch& l, hipStream_t s) {
-  if (pass == kAdapterNarrow) adapter_narrow_kernel<T, NR><<<l.grid, 256, 0, s>>>(*static_cast<const NarrowArgs*>(args));
+  if (pass == kAdapterNarrow && l.few) adapter_narrow_kernel<T, NR, 1><<<l.grid, 256, 0, s>>>(*static_cast<const NarrowArgs*>(args));
+  else if (pass == kAdapterNarrow) adapter_narrow_kernel<T, NR, 4><<<l.grid, 256, 0, s>>>(*static_cast<const NarrowArgs*>(args));
+  else if (pass == kAdapterWiden && l.few) adapter_widen_kernel<T, NR, 1><<<l.grid, 256, 0, s>>>(*static_cast<const WidenArgs*>(args));
+  else if (pass == kAdapterWiden) adapter_widen_kernel<T, NR, 4><<<l.grid, 256, 0, s>>>(*static_cast<const WidenArgs*>(args));
   else if (pass == kAdapterParts) adapter_parts_kernel<T, NR><<<l.grid, 256, 0, s>>>(*static_cast<const PartsArgs*>(args));
-  else if (pass == kAdapterOuter) adapter_outer_kernel<T, NR><<<l.grid, 256, 0, s>>>(*static_cast<const OuterArgs*>(args));
-  else if (l.silu) adapter_widen_kernel<T, NR, true><<<l.grid, 256, 0, s>>>(*static_cast<const WidenArgs*>(args));
-  else adapter_widen_kernel<T, NR, false><<<l.grid, 256, 0, s>>>(*static_cast<const WidenArgs*>(args));
+  else if (l.thin) adapter_outer_kernel<T, NR, true><<<l.grid, 256, 0, s>>>(*static_cast<const OuterArgs*>(args));
+  else adapter_outer_kernel<T, NR, false><<<l.grid, 256, 0, s>>>(*static_cast<const OuterArgs*>(args));
 }
 
 }  // namespace adapter
