@@ -115,7 +115,8 @@ __device__ void sort_rows(const SortArgs& p, int* shared, int2* waves) {
   if (p.span_first) {
     for (int i = t; i <= p.spans; i += threads) {
       const int b = last_of(span_at, n, i);
-      p.span_first[i] = b < n ? tile_at[b] + (i - span_at[b]) * p.span_tiles : tile_at[n];
+      // (an adapter's spans are as even as they can be)
+      p.span_first[i] = b < n ? tile_at[b] + (int)((long)(i - span_at[b]) * (tile_at[b + 1] - tile_at[b]) / (span_at[b + 1] - span_at[b])) : tile_at[n];
     }
     for (int i = t; i <= n; i += threads) p.span_of[i] = span_at[i];
   }
@@ -298,11 +299,17 @@ AdapterPlan plan_of(const cprune_adapter_desc& d, bool backward) {
   q.tiles = q.few ? d.rows : (d.rows - 1) / kTileRows + 1;
   if (q.sorted) q.tiles = std::min(d.rows, d.rows / kTileRows + d.adapters + 1);
   q.places = (int)std::min(2147483647L, (long)q.tiles * kTileRows);      // (more is refused)
-  // enough work-groups to bring x, each wavefront four steps at least
-  const int terms = backward ? d.c_out : d.k, steps = std::max(1, terms / q.step);      // (whole ones)
-  const int splits = std::max(1, std::min({256 * narrow_waves(q.ranks) / rounded_tiles(d, q), steps / 16, 16}));
-  q.per = (steps - 1) / splits + 1;
-  q.splits = (steps - 1) / q.per + 1;
+  // Work-groups that share a sum: as many as leave the busiest compute unit least to do, by the chunks of its work-groups and what each does but once, some three
+  // chunks' time.
+  const int terms = backward ? d.c_out : d.k, chunks = std::max(1, terms / (4 * q.step));      // (whole ones)
+  const long tiles = rounded_tiles(d, q);
+  long least = std::numeric_limits<long>::max();
+  for (int splits = 1; splits <= std::min(chunks, 32); ++splits) {
+    const int per = (chunks - 1) / splits + 1;
+    const long cost = ((tiles * ((chunks - 1) / per + 1) - 1) / 256 + 1) * (per + 3);
+    if (cost < least) least = cost, q.per = per;
+  }
+  q.splits = (chunks - 1) / q.per + 1;
   q.part = round256((size_t)q.splits * d.rows * q.rp * sizeof(float));
   if (q.sorted) {
     q.order = round256((size_t)q.places * sizeof(int));
@@ -391,7 +398,7 @@ int columns_of(const cprune_adapter_desc& d, const AdapterPlan& q, int c) {
   const long resident = 256 * widen_waves(q.ranks, (int)dtype_size(d.dtype)), tiles = rounded_tiles(d, q);
   int best = 256;
   long least = std::numeric_limits<long>::max();
-  for (int columns = 256; columns <= 2048; columns *= 2) {
+  for (int columns = 256; columns <= 2048; columns += 256) {
     const long groups = tiles * ((c - 1) / columns + 1), cost = ((groups - 1) / resident + 1) * (std::min(columns, c) + 200);
     if (cost < least) least = cost, best = columns;
   }

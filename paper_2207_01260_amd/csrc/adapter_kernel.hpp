@@ -3,10 +3,10 @@
 // Rows in tiles of 64 with one adapter: all rows in their order where there is one adapter, the rows of each adapter behind each other where a launch before has
 // sorted them (adapter_plan_kernel), or, up to 64 rows, those that a work-group finds with a ballot.  A tile's rows are gathered: a row is long, its place is not.
 //
-// Products on the matrix cores, operands straight from memory: 16 bytes of a row for each lane, lane l row l % 16 and the terms from 4 V times the step and V (l / 16)
-// on, V numbers of 16 bytes.  fp32 takes four instructions a step, one for each of a lane's four terms (the terms' order does not matter, both operands
+// Products on the matrix cores, an operand 16 bytes of a row for each lane: lane l has row l % 16 and the terms from 4 V times the step and V (l / 16) on, V numbers of 16
+// bytes.  fp32 takes four instructions a step, one for each of a lane's four terms (the terms' order does not matter, both operands
 // have the same).
-//  - narrow: 64 rows of x against A (or of dy against B's transpose), 4 wavefronts sharing the terms, work-groups sharing long sums; bound by reading x.
+//  - narrow: 64 rows of x against A (or of dy against B's transpose) through LDS, 4 wavefronts sharing the terms, work-groups sharing long sums; bound by reading x.
 //  - widen: hidden against B (or g against A's transpose), 8 neighbouring results in each lane; bound by reading base and writing y.
 //  - outer: dy against hidden (x against g), summed over rows.  The terms are rows: a lane reads 16 bytes of V rows and turns the V x V numbers over in registers.
 //    Runs of rows leave sums, joined in a fixed order.  Bound by reading dy (x).
@@ -42,7 +42,7 @@ struct NarrowArgs {
   int k, rank;
   const void* a;           // [adapters][rank][k]
   float* part;             // [splits][rows][RP]
-  int splits, per;         // work-groups that share a sum, steps of each
+  int splits, per;         // work-groups that share a sum, chunks of 256 bytes of each
 };
 
 struct WidenArgs {
@@ -250,84 +250,91 @@ __device__ __forceinline__ float4_t sum_parts(const float* from, int splits, lon
 
 // ---- narrow ----------------------------------------------------------------------
 
-// F: a tile's rows in sixteens, 4, or 1 where there are no more.  Rows that a tile has not are its first one again: they make results of their own, which nobody
-// reads.  Ranks past the last are the last again, left out by who reads them.
+// 256 bytes of every row at a time through LDS, two ahead of what is multiplied: asked for in whole lines, 16 lanes a row (as operands, 16 rows x 64 bytes, a compute
+// unit brings half as much: rank 32, 16384 x 4096 bf16 NARROW_TIMES us).  F: a tile's rows in sixteens, 4, or 1 where there are no more.  Rows that a
+// tile has not are its first one again: they make results of their own, which nobody reads.  Ranks past the last are the last again, left out by who reads them.
 template <typename T, int NR, int F>
 __global__ __launch_bounds__(256, narrow_waves(NR)) void adapter_narrow_kernel(const NarrowArgs p) {
-  constexpr int V = kV<T>, STEP = kStep<T>, RP = 16 * NR, U = F == 1 ? (NR <= 4 ? 4 : 2) : (NR <= 2 ? 2 : 1);
+  constexpr int V = kV<T>, RP = 16 * NR, PIECES = 16, CHUNK = PIECES * V, PITCH = PIECES + 1, LINES = 16 * (F + NR);
   __shared__ Tile tile;
-  __shared__ float sums[4][16][RP + 4];
+  __shared__ uint4 staged[2][LINES][PITCH];
   const int t = (int)threadIdx.x, lane = t & 63, wave = t >> 6, quarter = lane >> 4, lrow = lane & 15;
   const int tile_no = blockIdx.x / (unsigned)p.splits, split = blockIdx.x - tile_no * p.splits;
   int count;
   const int adapter = open_tile(p.tiles, tile_no, tile, count);
   if (adapter < 0) return;      // (rows without an adapter: what would be read here is known to be 0)
-  const T* rows[F];
-  const T* ranks[NR];
+  // this thread's piece of every sixteenth line: rows, then ranks
+  const int line = t >> 4, piece = t & 15;
+  const T* from[F + NR];
 #pragma unroll
   for (int f = 0; f < F; ++f) {
-    const int r = tile.row[16 * f + lrow];
-    rows[f] = static_cast<const T*>(p.x) + (long)(r >= 0 ? r : tile.row[0]) * p.stride + quarter * V;
+    const int r = tile.row[16 * f + line];
+    from[f] = static_cast<const T*>(p.x) + (long)(r >= 0 ? r : tile.row[0]) * p.stride + piece * V;
   }
 #pragma unroll
-  for (int n = 0; n < NR; ++n) ranks[n] = static_cast<const T*>(p.a) + ((long)adapter * p.rank + min(16 * n + lrow, p.rank - 1)) * p.k + quarter * V;
+  for (int n = 0; n < NR; ++n) from[F + n] = static_cast<const T*>(p.a) + ((long)adapter * p.rank + min(16 * n + line, p.rank - 1)) * p.k + piece * V;
+  struct Chunk {
+    uint4 v[F + NR];
+  };
+  auto fetch = [&](int c, Chunk& q) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < F + NR; ++i) q.v[i] = load(from[i] + (long)c * CHUNK);
+  };
+  auto stage = [&](int buffer, const Chunk& q) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < F + NR; ++i) staged[buffer][16 * i + line][piece] = q.v[i];
+  };
   float4_t acc[F][NR];
 #pragma unroll
   for (int f = 0; f < F; ++f)
 #pragma unroll
     for (int n = 0; n < NR; ++n) acc[f][n] = (float4_t){0.f, 0.f, 0.f, 0.f};
-  struct Operands {
-    uint4 x[F], a[NR];
-  };
-  auto fetch = [&](int s, Operands& q) __attribute__((always_inline)) {
+  // a wavefront has a quarter of the chunk's terms: four pieces of every line
+  auto multiply = [&](int buffer) __attribute__((always_inline)) {
+    uint4 x[F];
 #pragma unroll
-    for (int f = 0; f < F; ++f) q.x[f] = load(rows[f] + (long)s * STEP);
+    for (int f = 0; f < F; ++f) x[f] = staged[buffer][16 * f + lrow][4 * wave + quarter];
 #pragma unroll
-    for (int n = 0; n < NR; ++n) q.a[n] = load(ranks[n] + (long)s * STEP);
-  };
-  auto multiply = [&](const Operands& q) __attribute__((always_inline)) {
+    for (int n = 0; n < NR; ++n) {
+      const uint4 a = staged[buffer][16 * (F + n) + lrow][4 * wave + quarter];
 #pragma unroll
-    for (int f = 0; f < F; ++f)
-#pragma unroll
-      for (int n = 0; n < NR; ++n) acc[f][n] = mma<T>(q.a[n], q.x[f], acc[f][n]);
-  };
-  // a wavefront has a quarter of the work-group's whole steps, U of them under way while U are multiplied
-  const int whole = p.k / STEP, begin = split * p.per, steps = min(p.per, whole - begin), run = (steps + 3) / 4;
-  const int last = min(begin + (wave + 1) * run, begin + steps);
-  int s = begin + wave * run;
-  if (s + U <= last) {
-    Operands now[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) fetch(s + u, now[u]);
-#pragma unroll 1
-    for (; s + 2 * U <= last; s += U) {
-      Operands next[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) fetch(s + U + u, next[u]);
-#pragma unroll
-      for (int u = 0; u < U; ++u) multiply(now[u]);
-#pragma unroll
-      for (int u = 0; u < U; ++u) now[u] = next[u];
+      for (int f = 0; f < F; ++f) acc[f][n] = mma<T>(a, x[f], acc[f][n]);
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u) multiply(now[u]);
-    s += U;
+  };
+  const int whole = p.k / CHUNK, first = split * p.per, last = min(first + p.per, whole);
+  Chunk now, next;
+  if (first < last) {
+    fetch(first, now);
+    fetch(min(first + 1, last - 1), next);
+    stage(0, now);
   }
 #pragma unroll 1
-  for (; s < last; ++s) {
-    Operands q;
-    fetch(s, q);
-    multiply(q);
+  for (int c = first; c < last; c += 2) {
+    __syncthreads();
+    fetch(min(c + 2, last - 1), now);
+    multiply(0);
+    stage(1, next);
+    if (c + 1 >= last) break;
+    __syncthreads();
+    fetch(min(c + 3, last - 1), next);
+    multiply(1);
+    stage(0, now);
   }
-  if (p.k % STEP && split == p.splits - 1 && wave == 3) {      // what is left of a row
-    const int at = whole * STEP, valid = p.k - at - quarter * V;
-    Operands q;
+  if (p.k % CHUNK && split == p.splits - 1) {      // what is left of the rows, zeros past it
+    __syncthreads();
+#pragma unroll 1
+    for (int i = 0; i < F + NR; ++i) {
+      const T* q = from[0];
 #pragma unroll
-    for (int f = 0; f < F; ++f) q.x[f] = load_some(rows[f] + at, valid);
-#pragma unroll
-    for (int n = 0; n < NR; ++n) q.a[n] = load_some(ranks[n] + at, valid);
-    multiply(q);
+      for (int u = 1; u < F + NR; ++u) q = i == u ? from[u] : q;
+      staged[0][16 * i + line][piece] = load_some(q + (long)whole * CHUNK, p.k - whole * CHUNK - piece * V);
+    }
+    __syncthreads();
+    multiply(0);
   }
+  __syncthreads();
+  float (*const sums)[16][RP + 4] = reinterpret_cast<float (*)[16][RP + 4]>(staged);      // [wavefront]
+  static_assert(sizeof(float) * 4 * 16 * (RP + 4) <= sizeof(staged), "the wavefronts' sums take the chunks' place");
   const int frags = min((count + 15) / 16, F);
 #pragma unroll
   for (int f = 0; f < F; ++f) {
