@@ -12,11 +12,10 @@ constexpr int kFewRows = 64;      // rows that a wavefront's ballot sorts
 
 struct SortArgs {
   const int* which;
-  int rows, adapters, places, span_tiles, spans;
+  int rows, adapters, places;
   int waves;                 // that walk
   int *order, *tile_of;      // [places], [places / 64]
-  int *span_first;           // [spans + 1]
-  int *span_of;              // [adapters + 1], an adapter's first span
+  int* tile_at;              // [adapters + 1], an adapter's first tile, or null
 };
 
 constexpr int kSortWaves = 16;
@@ -34,18 +33,17 @@ __device__ __forceinline__ int last_of(const int* from, int n, int x) {
 
 // One work-group: the rows of each adapter behind each other in their order, in tiles of their own, rows without an adapter last.  Wavefronts count runs of rows and
 // place them on a second walk, behind what the others have counted.
-__device__ void sort_rows(const SortArgs& p, int* shared, int2* waves) {
+__device__ void sort_rows(const SortArgs& p, int* shared, int* waves) {
   const int t = (int)threadIdx.x, lane = t & 63, wave = t >> 6, n = p.adapters, buckets = n + 1, threads = 64 * kSortWaves;
   int* const count = shared;                              // [wavefront][bucket]
   int* const tile_at = count + p.waves * buckets;      // [buckets + 1]
-  int* const span_at = tile_at + buckets + 1;             // [adapters + 1]
   for (int i = t; i < p.waves * buckets; i += threads) count[i] = 0;
   __syncthreads();
   const int run = ((p.rows - 1) / (64 * p.waves) + 1) * 64, from = (int)min((long)wave * run, (long)p.rows), end = (int)min((long)from + run, (long)p.rows);
   const int bits = 32 - __clz(n);
   int* const mine = count + wave * buckets;
   // The wavefront's rows 1024 at a time: their adapters are asked for at once and kept in LDS, so that the loops over them are short code.
-  unsigned short* const kept = reinterpret_cast<unsigned short*>(span_at + buckets + 1 + (buckets & 1)) + wave * 1024;
+  unsigned short* const kept = reinterpret_cast<unsigned short*>(tile_at + buckets + 1) + wave * 1024;
   auto load = [&](int r0) __attribute__((always_inline)) {
     int b[16];
 #pragma unroll
@@ -70,8 +68,8 @@ __device__ void sort_rows(const SortArgs& p, int* shared, int2* waves) {
     }
   }
   __syncthreads();
-  // Where each bucket's tiles and spans begin, and in them each wavefront's rows: 16 lanes have a bucket, those of the wavefronts beside each other.
-  if (t == 0) tile_at[0] = span_at[0] = 0;
+  // Where each bucket's tiles begin, and in them each wavefront's rows: 16 lanes have a bucket, those of the wavefronts beside each other.
+  if (t == 0) tile_at[0] = 0;
   const int w = t & 15;
   for (int b0 = 0; b0 < buckets; b0 += threads / 16) {
     const int b = b0 + t / 16;
@@ -82,28 +80,25 @@ __device__ void sort_rows(const SortArgs& p, int* shared, int2* waves) {
       const int v = __shfl_up(upto, o, 16);
       upto += w >= o ? v : 0;
     }
-    const int rows = __shfl(upto, 15, 16), tiles = (rows + kTileRows - 1) / kTileRows, spans = b < n ? (tiles + p.span_tiles - 1) / p.span_tiles : 0;
+    const int rows = __shfl(upto, 15, 16), tiles = (rows + kTileRows - 1) / kTileRows;
     // (over the wavefront's four buckets, the work-group's wavefronts and the buckets before)
-    int2 before = {w == 0 ? tiles : 0, w == 0 ? spans : 0};
+    int before = w == 0 ? tiles : 0;
 #pragma unroll
     for (int o = 16; o < 64; o <<= 1) {
-      const int x = __shfl_up(before.x, o, 64), y = __shfl_up(before.y, o, 64);
-      before.x += lane >= o ? x : 0, before.y += lane >= o ? y : 0;
+      const int v = __shfl_up(before, o, 64);
+      before += lane >= o ? v : 0;
     }
     __syncthreads();      // (tile_at and `waves` of the buckets before)
     if (lane == 48) waves[wave] = before;
     __syncthreads();
-    int2 base = {tile_at[b0], span_at[b0]};
-    for (int v = 0; v < wave; ++v) base.x += waves[v].x, base.y += waves[v].y;
-    const int first_tile = __shfl(base.x + before.x - tiles, lane & 48, 64);
+    int base = tile_at[b0];
+    for (int v = 0; v < wave; ++v) base += waves[v];
+    const int first_tile = __shfl(base + before - tiles, lane & 48, 64);
     if (b < buckets) {
       const int at = first_tile * kTileRows;
       if (w < p.waves) count[w * buckets + b] = at + upto - c;
       for (int i = at + rows + w; i < at + tiles * kTileRows; i += 16) p.order[i] = -1;
-      if (w == 0) {
-        tile_at[b + 1] = first_tile + tiles;
-        if (b < n) span_at[b + 1] = base.y + before.y;
-      }
+      if (w == 0) tile_at[b + 1] = first_tile + tiles;
     }
   }
   __syncthreads();
@@ -112,14 +107,8 @@ __device__ void sort_rows(const SortArgs& p, int* shared, int2* waves) {
     const int b = last_of(tile_at, buckets, i);
     p.tile_of[i] = i >= tiles ? -2 : b < n ? b : -1;
   }
-  if (p.span_first) {
-    for (int i = t; i <= p.spans; i += threads) {
-      const int b = last_of(span_at, n, i);
-      // (an adapter's spans are as even as they can be)
-      p.span_first[i] = b < n ? tile_at[b] + (int)((long)(i - span_at[b]) * (tile_at[b + 1] - tile_at[b]) / (span_at[b + 1] - span_at[b])) : tile_at[n];
-    }
-    for (int i = t; i <= n; i += threads) p.span_of[i] = span_at[i];
-  }
+  if (p.tile_at)
+    for (int i = t; i <= n; i += threads) p.tile_at[i] = tile_at[i];
   // The rows' places.  In 64 rows the equal ones find each other by the bits of their adapter, and their first counts for all; four times 64 rows side by side.
   for (int r0 = from; r0 < end; r0 += 1024) {
     if (!once) load(r0);
@@ -193,7 +182,7 @@ template <typename T> __device__ __forceinline__ void turn_tile(const TurnArgs& 
 template <typename T>
 __global__ __launch_bounds__(64 * kSortWaves) void adapter_prepare_kernel(const SortArgs sort, const TurnArgs a, const TurnArgs b, int tiles_a) {
   extern __shared__ int shared[];
-  __shared__ int2 waves[kSortWaves];
+  __shared__ int waves[kSortWaves];
   int i = blockIdx.x;
   if (sort.which) {
     if (i == 0) {
@@ -218,10 +207,10 @@ __global__ __launch_bounds__(256) void adapter_pad_kernel(const T* __restrict__ 
   out[i] = adapter::load_some(b + row * rank + at, rank - at);
 }
 
-// Sums of an adapter's spans in their order: db [adapter][c][rank] from [span][c][RP], da [adapter][rank][k] from [span][RP][k].  Lanes share a result where there are
-// few: one of LANES threads has every LANES-th span.
+// Sums of an adapter's slices in their order: db [adapter][c][rank] from [slice + adapter][c][RP], da [adapter][rank][k] from [slice + adapter][RP][k].  Threads share a result
+// where there are few: one of LANES has every LANES-th slice.
 template <int LANES>
-__global__ __launch_bounds__(256) void adapter_join_kernel(const float* __restrict__ sums_b, const float* __restrict__ sums_a, const int* __restrict__ span_of, int spans, int adapters,
+__global__ __launch_bounds__(256) void adapter_join_kernel(const float* __restrict__ sums_b, const float* __restrict__ sums_a, const int* __restrict__ tile_at, int tile_count, int slices, int adapters,
                                                            int rank, int rp, int k, int c, float* __restrict__ da, float* __restrict__ db) {
   constexpr int RESULTS = 256 / LANES;
   __shared__ float parts[256];
@@ -235,7 +224,9 @@ __global__ __launch_bounds__(256) void adapter_join_kernel(const float* __restri
     const int n = (int)(m / per);
     const long in = m - n * per, pitch = of_b ? (long)c * rp : (long)rp * k;
     const long at = of_b ? in / rank * rp + in % rank : in;
-    const int first = span_of ? span_of[n] : 0, last = span_of ? span_of[n + 1] : n == 0 ? spans : 0;
+    // slices that the adapter's tiles lie in: slice s begins at tile s tiles / slices
+    const int t0 = tile_at ? tile_at[n] : 0, t1 = tile_at ? tile_at[n + 1] : n == 0 ? tile_count : 0, tiles = tile_at ? tile_at[adapters] : tile_count;
+    const int first = t0 < t1 ? (int)(((long)(t0 + 1) * slices - 1) / tiles) + n : 0, last = t0 < t1 ? (int)(((long)t1 * slices - 1) / tiles) + n + 1 : 0;
     const float* const from = (of_b ? sums_b : sums_a) + at;
     int q = first + turn;
     for (; q + 3 * LANES < last; q += 4 * LANES) {
@@ -279,14 +270,17 @@ struct AdapterPlan {
   int tiles, places;                   // tiles there may be
   int splits, per;                     // of narrow
   int padded;                          // backward: rank of A's transpose
-  int span_tiles, spans;
-  int groups_b, groups_a;              // work-groups a span, for dB and dA
-  size_t order, tile_of, span_first, span_of, part, bt, at, g, parts, sums_b, sums_a;      // bytes
-  size_t total() const { return order + tile_of + span_first + span_of + part + bt + at + g + 2 * parts + sums_b + sums_a; }
+  int slices;
+  int groups_b, groups_a;              // work-groups a slice, for dB and dA
+  size_t order, tile_of, tile_at, part, bt, at, g, parts, sums_b, sums_a;      // bytes
+  size_t total() const { return order + tile_of + tile_at + part + bt + at + g + 2 * parts + sums_b + sums_a; }
 };
 
 // Tiles as they are likely to be: half of the adapters' last ones are there, half are not.
-int rounded_tiles(const cprune_adapter_desc& d, const AdapterPlan& q) { return q.sorted ? std::min(q.tiles, d.rows / kTileRows + 1 + d.adapters / 2) : q.tiles; }
+int rounded_tiles(const cprune_adapter_desc& d, const AdapterPlan& q) {
+  if (q.few) return std::min(q.tiles, d.adapters + 1);
+  return q.sorted ? std::min(q.tiles, d.rows / kTileRows + 1 + d.adapters / 2) : q.tiles;
+}
 
 AdapterPlan plan_of(const cprune_adapter_desc& d, bool backward) {
   AdapterPlan q = {};
@@ -326,16 +320,13 @@ AdapterPlan plan_of(const cprune_adapter_desc& d, bool backward) {
   q.parts = round256((size_t)q.rp * q.places * (es == 4 ? 4 : 6));
   const int wide = 16 * (16 / (int)es);      // columns of a work-group
   q.groups_b = (d.c_out - 1) / wide + 1, q.groups_a = (d.k - 1) / wide + 1;
-  // spans: enough work-groups, and long enough that their sums are few beside what is read
-  const int groups = q.groups_a + q.groups_b, want = std::max(1, 256 * kOuterWaves / groups);
-  q.span_tiles = std::max(2, ((d.rows - 1) / kTileRows + want) / want);
-  q.spans = q.sorted ? std::min(q.tiles, q.tiles / q.span_tiles + d.adapters) : (q.tiles - 1) / q.span_tiles + 1;
-  if (q.sorted) {
-    q.span_first = round256((size_t)(q.spans + 1) * sizeof(int));
-    q.span_of = round256((size_t)(d.adapters + 1) * sizeof(int));
-  }
-  q.sums_b = round256((size_t)q.spans * d.c_out * q.rp * sizeof(float));
-  q.sums_a = round256((size_t)q.spans * d.k * q.rp * sizeof(float));
+  // slices: a round of work-groups, of two tiles at least
+  const int groups = q.groups_a + q.groups_b;
+  q.slices = std::max(1, std::min(256 * kOuterWaves / groups, (d.rows - 1) / kTileRows / 2 + 1));
+  if (q.sorted) q.tile_at = round256((size_t)(d.adapters + 1) * sizeof(int));
+  const size_t sums = q.slices + (q.sorted ? d.adapters : 1) - 1;
+  q.sums_b = round256(sums * d.c_out * q.rp * sizeof(float));
+  q.sums_a = round256(sums * d.k * q.rp * sizeof(float));
   return q;
 }
 
@@ -346,7 +337,7 @@ bool fits(const cprune_adapter_desc& d, const AdapterPlan& q, bool backward) {
   if ((double)q.tiles * q.splits >= most || (double)q.tiles * ((c - 1) / 256 + 1) >= most || (double)q.tiles * kTileRows >= 2147483648.0 || (double)q.tiles * q.ranks >= most) return false;
   if (!backward) return (double)d.adapters * d.c_out * q.padded / 4 < 4294967040.0;
   const double turned = (double)d.adapters * ((d.k + 63.0) / 64 + (d.c_out + 63.0) / 64) * 2;      // (ranks of up to 128 are two tiles)
-  return turned < most / 4 - 1 && (double)q.spans * (q.groups_a + q.groups_b) < most && (double)d.adapters * d.rank * ((double)d.k + d.c_out) < 4294967040.0;
+  return turned < most / 4 - 1 && (double)q.slices * (q.groups_a + q.groups_b) < most && (double)d.adapters * d.rank * ((double)d.k + d.c_out) < 4294967040.0;
 }
 
 void launch(int dtype, AdapterPass pass, const void* args, const AdapterLaunch& l, hipStream_t s) {
@@ -371,20 +362,20 @@ AdapterTiles tiles_of(const cprune_adapter_desc& d, const AdapterPlan& q, const 
 }
 
 // The launch before the products; a, b: what is turned over, or empty
-void prepare(const cprune_adapter_desc& d, const AdapterPlan& q, AdapterTiles& t, int* span_first, int* span_of, const TurnArgs& a, const TurnArgs& b, Scratch& ws,
+void prepare(const cprune_adapter_desc& d, const AdapterPlan& q, AdapterTiles& t, int* tile_at, const TurnArgs& a, const TurnArgs& b, Scratch& ws,
              hipStream_t s) {
   SortArgs sort = {};
   if (q.sorted) {
     int* const order = ws.take<int>(q.order);
     int* const tile_of = ws.take<int>(q.tile_of);
-    sort = {t.which, d.rows, d.adapters, q.places, std::max(1, q.span_tiles), q.spans, d.adapters > 384 ? kSortWaves / 2 : kSortWaves, order, tile_of, span_first, span_of};
+    sort = {t.which, d.rows, d.adapters, q.places, d.adapters > 384 ? kSortWaves / 2 : kSortWaves, order, tile_of, tile_at};
     t.order = order, t.tile_of = tile_of;
   }
   const int tiles_a = a.row_tiles * a.col_tiles * d.adapters, tiles_b = b.row_tiles * b.col_tiles * d.adapters;
   const unsigned grid = (unsigned)(q.sorted + tiles_a + tiles_b);
   if (!grid) return;
   const size_t es = dtype_size(d.dtype);
-  size_t lds = q.sorted ? ((size_t)sort.waves * (d.adapters + 1) + 2 * d.adapters + 8) * sizeof(int) + 2048 * sort.waves : 0;
+  size_t lds = q.sorted ? ((size_t)sort.waves * (d.adapters + 1) + d.adapters + 2) * sizeof(int) + 2048 * sort.waves : 0;
   if (tiles_a + tiles_b) lds = std::max(lds, 64 * 65 * es);
   if (es == 4) adapter_prepare_kernel<unsigned><<<grid, 64 * kSortWaves, lds, s>>>(sort, a, b, tiles_a);
   else adapter_prepare_kernel<unsigned short><<<grid, 64 * kSortWaves, lds, s>>>(sort, a, b, tiles_a);
@@ -428,7 +419,7 @@ extern "C" int cprune_adapter_linear(const cprune_adapter_desc* d, const void* x
   hipStream_t s = static_cast<hipStream_t>(stream);
   Scratch scratch = {static_cast<char*>(ws)};
   AdapterTiles tiles = tiles_of(*d, q, which);
-  prepare(*d, q, tiles, nullptr, nullptr, {}, {}, scratch, s);
+  prepare(*d, q, tiles, nullptr, {}, {}, scratch, s);
   float* const part = scratch.take<float>(q.part);
   AdapterLaunch l = {(unsigned)(q.tiles * q.splits), q.ranks, d->rows <= 16, false};
   const NarrowArgs n = {tiles, x, d->x_stride, d->k, d->rank, a, part, q.splits, q.per};
@@ -470,13 +461,12 @@ extern "C" int cprune_adapter_linear_backward(const cprune_adapter_desc* d, cons
   hipStream_t s = static_cast<hipStream_t>(stream);
   Scratch scratch = {static_cast<char*>(ws)};
   AdapterTiles tiles = tiles_of(*d, q, which);
-  int* const span_first = scratch.take<int>(q.span_first);
-  int* const span_of = scratch.take<int>(q.span_of);
+  int* const tile_at = scratch.take<int>(q.tile_at);
   char* const bt = scratch.take<char>(q.bt);
   char* const at = scratch.take<char>(q.at);
   auto tiles64 = [](int n) { return (n + 63) / 64; };
   const TurnArgs turn_a = {a, at, d->rank, d->k, q.padded, tiles64(q.padded), tiles64(d->k)}, turn_b = {b, bt, d->c_out, d->rank, d->c_out, tiles64(d->c_out), tiles64(d->rank)};
-  prepare(*d, q, tiles, span_first, span_of, dx ? turn_a : TurnArgs(), turn_b, scratch, s);
+  prepare(*d, q, tiles, tile_at, dx ? turn_a : TurnArgs(), turn_b, scratch, s);
   float* const part = scratch.take<float>(q.part);
   float* const g = scratch.take<float>(q.g);
   char* const g_parts = scratch.take<char>(q.parts);
@@ -506,17 +496,17 @@ extern "C" int cprune_adapter_linear_backward(const cprune_adapter_desc* d, cons
   if (da) {
     OuterArgs o = {};
     o.tiles = tiles, o.rank = d->rank, o.places = q.places;
-    o.span_first = span_first, o.span_tiles = q.span_tiles, o.tile_count = q.tiles;
+    o.tile_at = tile_at, o.tile_count = q.tiles, o.slices = q.slices;
     o.side[0] = {dy, d->dy_stride, d->c_out, hidden_parts, sums_b, q.groups_b};
     o.side[1] = {x, d->x_stride, d->k, g_parts, sums_a, q.groups_a};
-    l.grid = (unsigned)(q.spans * (q.groups_a + q.groups_b));
+    l.grid = (unsigned)(q.slices * (q.groups_a + q.groups_b));
     launch(d->dtype, kAdapterOuter, &o, l, s);
     const long all = (long)d->adapters * d->rank * ((long)d->k + d->c_out);
     auto join = [&](auto lanes) {
       constexpr int LANES = decltype(lanes)::value;
-      adapter_join_kernel<LANES><<<(unsigned)((all * LANES + 255) / 256), 256, 0, s>>>(sums_b, sums_a, span_of, q.spans, d->adapters, d->rank, q.rp, d->k, d->c_out, da, db);
+      adapter_join_kernel<LANES><<<(unsigned)((all * LANES + 255) / 256), 256, 0, s>>>(sums_b, sums_a, tile_at, q.tiles, q.slices, d->adapters, d->rank, q.rp, d->k, d->c_out, da, db);
     };
-    if (all <= 65536 && q.spans >= 8) join(std::integral_constant<int, 8>());
+    if (all <= 65536 && q.slices >= 8) join(std::integral_constant<int, 8>());
     else join(std::integral_constant<int, 1>());
   }
   CPRUNE_LAUNCH_CHECK();

@@ -9,7 +9,7 @@
 //  - narrow: 64 rows of x against A (or of dy against B's transpose) through LDS, 4 wavefronts sharing the terms, work-groups sharing long sums; bound by reading x.
 //  - widen: hidden against B (or g against A's transpose), 8 neighbouring results in each lane; bound by reading base and writing y.
 //  - outer: dy against hidden (x against g), summed over rows.  The terms are rows: a lane reads 16 bytes of V rows and turns the V x V numbers over in registers.
-//    Runs of rows leave sums, joined in a fixed order.  Bound by reading dy (x).
+//    Equal slices of the rows leave sums for each adapter that they meet, joined in a fixed order.  Bound by reading dy (x).
 // hidden and g are fp32; against 16-bit operands they go as bf16 parts, of 8 bits each: two for y and dx, whose own rounding is 2^-8 or 2^-11 (what is
 // left is under 2^-15 of a term), three for dA and dB in fp32, which are all of it.  An fp16 operand beside them is two bf16 parts itself, exactly.
 #pragma once
@@ -62,7 +62,7 @@ struct WidenArgs {
   bool silu;
 };
 
-// hidden and g as the outer product's operands: 16-bit, three bf16 parts [3][RP][places], fp32 [RP][places]
+// hidden and g as the outer product's operands, by steps of its terms, places: 16-bit, three bf16 parts [3][places / 32][RP][32], fp32 [places / 16][RP][16]
 struct PartsArgs {
   AdapterTiles tiles;
   const float* part;       // g: [splits][rows][RP]
@@ -79,15 +79,16 @@ struct OuterSide {
   long stride;
   int c;                   // columns
   const void* parts;       // the other operand
-  float* sums;             // [spans][c][RP], or [spans][RP][c] (across)
-  int groups;              // work-groups for a span
+  float* sums;             // [slices + adapters - 1][c][RP], or [..][RP][c] (across)
+  int groups;              // work-groups for a slice
 };
 struct OuterArgs {
   AdapterTiles tiles;
   OuterSide side[2];       // dy and hidden; x and g
   int rank, places;
-  const int* span_first;   // [spans + 1] first tile of a span; sorted only
-  int span_tiles, tile_count;   // otherwise: tiles of a span, all tiles
+  const int* tile_at;      // sorted: [adapters + 1], an adapter's first tile
+  int tile_count;          // otherwise
+  int slices;              // that the tiles are cut into, whatever their adapters: what adapter i has of slice s is sum s + i
 };
 
 struct AdapterLaunch {
@@ -547,7 +548,7 @@ __global__ __launch_bounds__(256) void adapter_parts_kernel(const PartsArgs p) {
     const int which = i / (16 * PER), j = i / PER % 16, at = i % PER * V;
     const float* const from = &turned[which][j][at];
     void* const out = which ? p.hidden_out : p.g_out;
-    const long to = (long)(j0 + j) * p.places + tile_no * kTileRows + at;
+    const long place = (long)tile_no * kTileRows + at, to = (place / kStep<T> * RP + j0 + j) * kStep<T> + place % kStep<T>;
     if constexpr (sizeof(T) == 4) {
       *reinterpret_cast<float4_t*>(static_cast<float*>(out) + to) = *reinterpret_cast<const float4_t*>(from);
     } else {
@@ -583,96 +584,107 @@ template <typename T> __device__ __forceinline__ void turn(const uint4 (&r)[kV<T
   }
 }
 
+// A work-group has 16 V columns of a run of tiles with one adapter, all ranks; 128 rows of them at a time go through LDS, the next ones asked for meanwhile.  Its wavefronts
+// share the ranks, 32 each, so that two fit a SIMD, and the rows where ranks are fewer.  ACROSS: results lie [rank][column] instead of [column][rank].
 // THIN: a side has fewer than V columns, read one by one.  Otherwise a lane past the last column has the last V again, and stores what their lanes do.
-// A work-group has 16 V columns of a span of tiles with one adapter, all ranks.  Its wavefronts share them: 32 ranks each, so that two fit a SIMD, and steps of the rows where
-// ranks are fewer.  ACROSS: results lie [rank][column] instead of [column][rank].  A step's numbers are asked for a step ahead, its rows' places two.
+constexpr int kOuterRows = 128;
+struct OuterShared {
+  uint4 staged[2][kOuterRows][16 + 1];
+};
 template <typename T, int NR, bool ACROSS, bool THIN>
-__device__ __forceinline__ void outer_side(const OuterArgs& p, const OuterSide& side, int span, int group, int first, int last, float4_t* joined) {
-  constexpr int V = kV<T>, STEP = kStep<T>, RP = 16 * NR, N = sizeof(T) == 4 ? 1 : 3, NW = NR < 2 ? NR : 2, SHARES = NR / NW, STREAMS = 4 / SHARES;
-  const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, quarter = lane >> 4, lrow = lane & 15, share = wave % SHARES, stream = wave / SHARES;
+__device__ __forceinline__ void outer_side(const OuterArgs& p, const OuterSide& side, int group, int slice, OuterShared& shared) {
+  constexpr int V = kV<T>, STEP = kStep<T>, RP = 16 * NR, N = sizeof(T) == 4 ? 1 : 3, NW = NR < 2 ? NR : 2, SHARES = NR / NW, STREAMS = 4 / SHARES, EACH = kOuterRows / 16;
+  const int t = (int)threadIdx.x, lane = t & 63, wave = t >> 6, quarter = lane >> 4, lrow = lane & 15, share = wave % SHARES, stream = wave / SHARES;
   auto column = [&](int lane_row) __attribute__((always_inline)) {      // first of the V that lanes of a row number have
     const int c = group * 16 * V + lane_row * V;
     return THIN ? c : min(c, side.c - V);
   };
   const int c = column(lrow), valid = side.c - c;
+  const T* const x = static_cast<const T*>(side.x) + column(t & 15);
+  const long part = (long)RP * p.places;
+  const int line = t >> 4, tiles = p.tile_at ? p.tile_at[p.tiles.adapters] : p.tile_count;
+  const int slice_end = (int)((long)(slice + 1) * tiles / p.slices);
+#pragma unroll 1
+  for (int first = (int)((long)slice * tiles / p.slices), last; first < slice_end; first = last) {      // an adapter's tiles of the slice
+  const int adapter = p.tile_at ? p.tiles.tile_of[first] : 0;
+  last = p.tile_at ? min(slice_end, p.tile_at[adapter + 1]) : slice_end;
+  const int end = last * kTileRows;
+  const int any_row = p.tiles.order ? p.tiles.order[first * kTileRows] : first * kTileRows;      // (read in the place of none, kept out)
   float4_t acc[V][NW];
 #pragma unroll
   for (int i = 0; i < V; ++i)
 #pragma unroll
     for (int n = 0; n < NW; ++n) acc[i][n] = (float4_t){0.f, 0.f, 0.f, 0.f};
-  const T* const x = static_cast<const T*>(side.x) + c;
-  const long part = (long)RP * p.places;
-  const int end = last * kTileRows;
-  struct Rows {
-    int at[V];
-  };
-  auto find = [&](int at, Rows& rows) __attribute__((always_inline)) {      // (past the span: none)
-    const int place = at + quarter * V;
-    if (at >= end) {
+  auto find = [&](int at, int (&rows)[EACH]) __attribute__((always_inline)) {      // this thread's rows of those from place `at` on
 #pragma unroll
-      for (int e = 0; e < V; ++e) rows.at[e] = -1;
-    } else if (p.tiles.order) {
-#pragma unroll
-      for (int e = 0; e < V; e += 4) {
-        const int4 o = *reinterpret_cast<const int4*>(p.tiles.order + place + e);
-        rows.at[e] = o.x, rows.at[e + 1] = o.y, rows.at[e + 2] = o.z, rows.at[e + 3] = o.w;
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < V; ++e) rows.at[e] = place + e < p.tiles.rows ? place + e : -1;
+    for (int e = 0; e < EACH; ++e) {
+      const int place = at + 16 * e + line;
+      rows[e] = place >= end ? -1 : p.tiles.order ? p.tiles.order[place] : place < p.tiles.rows ? place : -1;
     }
   };
-  const int any_row = p.tiles.order ? p.tiles.order[first * kTileRows] : first * kTileRows;      // (in the place of none, made zeros where it is multiplied)
-  auto fetch = [&](const Rows& rows, uint4 (&r)[V]) __attribute__((always_inline)) {
+  auto fetch = [&](const int (&rows)[EACH], uint4 (&v)[EACH]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      const T* const from = x + (long)(rows.at[e] >= 0 ? rows.at[e] : any_row) * side.stride;
-      r[e] = THIN ? load_some(from, valid) : load(from);
+    for (int e = 0; e < EACH; ++e) {
+      const T* const from = x + (long)(rows[e] >= 0 ? rows[e] : any_row) * side.stride;
+      v[e] = THIN ? load_some(from, side.c - (t & 15) * V) : load(from);
     }
   };
-  int at = first * kTileRows + stream * STEP;
-  Rows ahead, there;
-  uint4 now[V];
-  find(at, there);
-  fetch(there, now);
-  find(at + STREAMS * STEP, ahead);
-  for (; at < end; at += STREAMS * STEP) {
-    auto operand = [&](int n, uint4 (&q)[N]) __attribute__((always_inline)) {
-      const long from = (long)(16 * (share * NW + n) + lrow) * p.places + at + quarter * V;
+  auto stage = [&](int buffer, const int (&rows)[EACH], const uint4 (&v)[EACH]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) shared.staged[buffer][16 * e + line][t & 15] = keep(v[e], rows[e] >= 0);
+  };
+  // the other operand of the step at a place, a step ahead; (past the last one: the first again)
+  auto operand = [&](int place, uint4 (&q)[NW][N]) __attribute__((always_inline)) {
+    const long from = ((long)(place < end ? place : first * kTileRows) / STEP * RP + 16 * share * NW + lrow) * STEP + quarter * V;
+#pragma unroll
+    for (int n = 0; n < NW; ++n)
 #pragma unroll
       for (int m = 0; m < N; ++m) {
-        if constexpr (sizeof(T) == 4) q[m] = *reinterpret_cast<const uint4*>(static_cast<const float*>(side.parts) + from);
-        else q[m] = *reinterpret_cast<const uint4*>(static_cast<const __bf16*>(side.parts) + m * part + from);
+        if constexpr (sizeof(T) == 4) q[n][m] = *reinterpret_cast<const uint4*>(static_cast<const float*>(side.parts) + from + 16 * STEP * n);
+        else q[n][m] = *reinterpret_cast<const uint4*>(static_cast<const __bf16*>(side.parts) + m * part + from + 16 * STEP * n);
       }
-    };
-    uint4 q[2][N];      // (the next sixteen ranks' beside these)
-    operand(0, q[0]);
-    uint4 next[V], turned[V];
-    fetch(ahead, next);
-    bool gap = false;
+  };
+  int at = first * kTileRows, buffer = 0;
+  int rows[EACH], ahead[EACH];
+  uint4 v[EACH], q[NW][N];
+  find(at, rows);
+  fetch(rows, v);
+  operand(at + stream * STEP, q);
+  find(at + kOuterRows, ahead);
+  stage(0, rows, v);
+#pragma unroll 1
+  for (; at < end; at += kOuterRows, buffer ^= 1) {
+    __syncthreads();
 #pragma unroll
-    for (int e = 0; e < V; ++e) gap |= there.at[e] < 0;
-    if (__any(gap)) {
+    for (int e = 0; e < EACH; ++e) rows[e] = ahead[e];
+    fetch(rows, v);
+    find(at + 2 * kOuterRows, ahead);
+#pragma unroll 1
+    for (int in = stream * STEP; in < kOuterRows && at + in < end; in += STREAMS * STEP) {
+      uint4 next[NW][N], r[V], turned[V];
+      operand(at + in + STREAMS * STEP, next);
 #pragma unroll
-      for (int e = 0; e < V; ++e) now[e] = keep(now[e], there.at[e] >= 0);
+      for (int e = 0; e < V; ++e) r[e] = shared.staged[buffer][in + quarter * V + e][lrow];
+      turn<T>(r, turned);
+#pragma unroll
+      for (int n = 0; n < NW; ++n)
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          if constexpr (sizeof(T) == 4) acc[i][n] = ACROSS ? mma<float>(q[n][0], turned[i], acc[i][n]) : mma<float>(turned[i], q[n][0], acc[i][n]);
+          else acc[i][n] = mma_parts<T, N, ACROSS>(turned[i], q[n], acc[i][n]);
+        }
+#pragma unroll
+      for (int n = 0; n < NW; ++n)
+#pragma unroll
+        for (int m = 0; m < N; ++m) q[n][m] = next[n][m];
     }
-    there = ahead;
-    find(at + 2 * STREAMS * STEP, ahead);
-    turn<T>(now, turned);
-#pragma unroll
-    for (int n = 0; n < NW; ++n) {
-      if (n + 1 < NW) operand(n + 1, q[(n + 1) % 2]);
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        if constexpr (sizeof(T) == 4) acc[i][n] = ACROSS ? mma<float>(q[n % 2][0], turned[i], acc[i][n]) : mma<float>(turned[i], q[n % 2][0], acc[i][n]);
-        else acc[i][n] = mma_parts<T, N, ACROSS>(turned[i], q[n % 2], acc[i][n]);
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < V; ++e) now[e] = next[e];
+    stage(buffer ^ 1, rows, v);      // (read two steps ago)
   }
+  __syncthreads();
+  float4_t* const joined = reinterpret_cast<float4_t*>(&shared);
+  static_assert(sizeof(OuterShared) >= 8 * 4 * 64 * sizeof(float4_t), "the wavefronts' sums take the rows' place");
   // the wavefronts' sums joined through LDS, up to 8 results of each at a time
-  float* const sums = side.sums + (long)span * side.c * RP;
+  float* const sums = side.sums + (long)(slice + adapter) * side.c * RP;
   constexpr int G = 8 / NW < V ? 8 / NW : V, ITEMS = G * NR;
 #pragma unroll
   for (int i0 = 0; i0 < V; i0 += G) {
@@ -701,23 +713,17 @@ __device__ __forceinline__ void outer_side(const OuterArgs& p, const OuterSide& 
       }
     }
   }
+  __syncthreads();
+  }
 }
 
 template <typename T, int NR, bool THIN>
 __global__ __launch_bounds__(256, kOuterWaves) void adapter_outer_kernel(const OuterArgs p) {
-  __shared__ float4_t joined[8 * 4 * 64];
+  __shared__ OuterShared shared;
   const int groups = p.side[0].groups + p.side[1].groups;
-  const int span = blockIdx.x / (unsigned)groups;
-  int group = blockIdx.x - span * groups;
-  int first, last;
-  if (p.span_first) {
-    first = p.span_first[span], last = p.span_first[span + 1];
-    if (last <= first) return;      // (as many spans as there may be)
-  } else {
-    first = span * p.span_tiles, last = min(first + p.span_tiles, p.tile_count);
-  }
-  if (group < p.side[0].groups) outer_side<T, NR, false, THIN>(p, p.side[0], span, group, first, last, joined);
-  else outer_side<T, NR, true, THIN>(p, p.side[1], span, group - p.side[0].groups, first, last, joined);
+  const int slice = blockIdx.x / (unsigned)groups, group = blockIdx.x - slice * groups;
+  if (group < p.side[0].groups) outer_side<T, NR, false, THIN>(p, p.side[0], group, slice, shared);
+  else outer_side<T, NR, true, THIN>(p, p.side[1], group - p.side[0].groups, slice, shared);
 }
 
 template <typename T, int NR> void launch_ranks(AdapterPass pass, const void* args, const AdapterLaunch& l, hipStream_t s) {
