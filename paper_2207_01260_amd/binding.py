@@ -778,7 +778,7 @@ def _scratch(need: int, x: torch.Tensor):
     """(tensor, its address), or (None, None)."""
     if not need:
         return None, None
-    ws = torch.empty(need, dtype=torch.uint8, device=x.device)
+    ws = x.new_empty(need, dtype=torch.uint8)
     return ws, ws.data_ptr()
 
 
@@ -793,8 +793,8 @@ def cprune_top_logits(z: torch.Tensor, k: int, stream=None) -> Tuple[torch.Tenso
     if not 1 <= k <= classes:
         _refuse(f"no {k} of {classes} classes")
     shape = z.shape[:-1] + (k,)
-    values = torch.empty(shape, dtype=z.dtype, device=z.device)
-    ids = torch.empty(shape, dtype=torch.int32, device=z.device)
+    values = z.new_empty(shape)
+    ids = z.new_empty(shape, dtype=torch.int32)
     need = L.cprune_top_logits_workspace_bytes(rows, classes, k, dtype)
     ws, ws_at = _scratch(need, z)
     st = L.cprune_top_logits(z.data_ptr(), rows, classes, pitch, k, dtype, values.data_ptr(), ids.data_ptr(), ws_at, need, _raw_stream())
@@ -825,8 +825,8 @@ def cprune_distill_loss(z: torch.Tensor, ids: torch.Tensor, teacher: torch.Tenso
         return _on(stream, cprune_distill_loss, z, ids, teacher, labels, temperature, hard, want_stats)
     L = _lib or lib()
     d, ids_at, teacher_at, labels_at = _distill(z, ids, teacher, labels, temperature, hard)
-    loss = torch.empty(z.shape[:-1], dtype=torch.float32, device=z.device)
-    stats = torch.empty(3, d.rows, dtype=torch.float32, device=z.device) if want_stats else None
+    loss = z.new_empty(z.shape[:-1], dtype=torch.float32)
+    stats = z.new_empty((3, d.rows), dtype=torch.float32) if want_stats else None
     need = L.cprune_distill_workspace_bytes(d)
     ws, ws_at = _scratch(need, z)
     st = L.cprune_distill_loss(d, z.data_ptr(), ids_at, teacher_at, labels_at, loss.data_ptr(), None if stats is None else stats.data_ptr(), ws_at, need,
@@ -860,7 +860,7 @@ def cprune_distill_step(dloss: torch.Tensor, z: torch.Tensor, ids: torch.Tensor,
     L = _lib or lib()
     d, ids_at, teacher_at, labels_at = _distill(z, ids, teacher, labels, temperature, hard, dloss)
     lead = z.shape[:-1]
-    loss = torch.empty(lead, dtype=torch.float32, device=z.device)
+    loss = z.new_empty(lead, dtype=torch.float32)
     dz = _dense_like(z)
     need = L.cprune_distill_workspace_bytes(d)
     ws, ws_at = _scratch(need, z)
@@ -887,11 +887,11 @@ def _adapters(x, a, b, which, scale):
         None if which is None else _on_gpu(which, torch.int32, x.shape[:-1]), None if scale is None else _on_gpu(scale, torch.float32, (n,))
 
 
-def _beside(t: torch.Tensor, x: torch.Tensor, columns: int) -> int:
-    """Elements between the rows of t, which are as many as those of x."""
-    if not t.is_cuda or t.dtype != x.dtype or t.shape != x.shape[:-1] + (columns,):
-        _refuse(f"expected {x.dtype} {tuple(x.shape[:-1]) + (columns,)}, got {t.dtype} {tuple(t.shape)}")
-    return _rows_of(t, 0)[3]
+def _beside(t: torch.Tensor, x: torch.Tensor, shape) -> int:
+    """Elements between the rows of t, of a shape and the type of x."""
+    if not t.is_cuda or t.dtype != x.dtype or t.shape != shape:
+        _refuse(f"expected {x.dtype} {tuple(shape)}, got {t.dtype} {tuple(t.shape)}")
+    return shape[-1] if t.is_contiguous() else _rows_of(t, 0)[3]
 
 
 def cprune_adapter_linear(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, which: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None,
@@ -905,16 +905,17 @@ def cprune_adapter_linear(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, whi
     d, a_at, b_at, which_at, scale_at = _adapters(x, a, b, which, scale)
     _one_device(x, a, b, which, scale, base, out)
     d.act = act
-    shape = x.shape[:-1] + (d.c_out,)
+    lead = x.shape[:-1]
+    shape = lead + (d.c_out,)
     base_at = None
     if base is not None:
-        d.base_stride = _beside(base, x, d.c_out)
+        d.base_stride = _beside(base, x, shape)
         base_at = base.data_ptr()
-    y = torch.empty(shape, dtype=x.dtype, device=x.device) if out is None else out
+    y = x.new_empty(shape) if out is None else out
     y_at = y.data_ptr() if out is None else _on_gpu(out, x.dtype, shape)
     hidden = hidden_at = None
     if want_hidden:
-        hidden = torch.empty(x.shape[:-1] + (d.rank,), dtype=torch.float32, device=x.device)
+        hidden = x.new_empty(lead + (d.rank,), dtype=torch.float32)
         hidden_at = hidden.data_ptr()
     need = L.cprune_adapter_workspace_bytes(d, 0)
     ws, ws_at = _scratch(need, x)
@@ -934,21 +935,22 @@ def cprune_adapter_linear_backward(dy: torch.Tensor, x: torch.Tensor, hidden: to
     L = _lib or lib()
     d, a_at, b_at, which_at, scale_at = _adapters(x, a, b, which, scale)
     _one_device(x, dy, hidden, a, b, which, scale, dx_base)
-    d.dy_stride = _beside(dy, x, d.c_out)
+    lead = x.shape[:-1]
+    d.dy_stride = _beside(dy, x, lead + (d.c_out,))
     dx = da = db = dx_at = da_at = db_at = base_at = None
     if want_dx:
         dx = _dense_like(x)
         dx_at = dx.data_ptr()
         if dx_base is not None:
-            d.base_stride = _beside(dx_base, x, d.k)
+            d.base_stride = _beside(dx_base, x, x.shape)
             base_at = dx_base.data_ptr()
     if want_weights:
-        da = torch.empty(a.shape, dtype=torch.float32, device=x.device)
-        db = torch.empty(b.shape, dtype=torch.float32, device=x.device)
+        da = a.new_empty(a.shape, dtype=torch.float32)
+        db = b.new_empty(b.shape, dtype=torch.float32)
         da_at, db_at = da.data_ptr(), db.data_ptr()
     need = L.cprune_adapter_workspace_bytes(d, 1)
     ws, ws_at = _scratch(need, x)
-    st = L.cprune_adapter_linear_backward(d, dy.data_ptr(), x.data_ptr(), _on_gpu(hidden, torch.float32, x.shape[:-1] + (d.rank,)), a_at, b_at, which_at, scale_at,
+    st = L.cprune_adapter_linear_backward(d, dy.data_ptr(), x.data_ptr(), _on_gpu(hidden, torch.float32, lead + (d.rank,)), a_at, b_at, which_at, scale_at,
                                           base_at, dx_at, da_at, db_at, ws_at, need, _raw_stream())
     if st:
         _check(st, "cprune_adapter_linear_backward")

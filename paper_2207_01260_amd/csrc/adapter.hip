@@ -195,18 +195,6 @@ __global__ __launch_bounds__(64 * kSortWaves) void adapter_prepare_kernel(const 
   else turn_tile<T>(b, i - tiles_a, reinterpret_cast<T*>(shared));
 }
 
-// B [row][rank] -> [row][padded], zeros past the rank, 16 bytes a thread: where ranks do not fill vectors.
-template <typename T>
-__global__ __launch_bounds__(256) void adapter_pad_kernel(const T* __restrict__ b, long vectors, int rank, int padded, uint4* __restrict__ out) {
-  constexpr int V = adapter::kV<T>;
-  const long i = (long)blockIdx.x * 256 + threadIdx.x;
-  if (i >= vectors) return;
-  const int per = padded / V;
-  const long row = i / per;
-  const int at = (int)(i - row * per) * V;
-  out[i] = adapter::load_some(b + row * rank + at, rank - at);
-}
-
 // Sums of an adapter's slices in their order: db [adapter][c][rank] from [slice + adapter][c][RP], da [adapter][rank][k] from [slice + adapter][RP][k].  Threads share a result
 // where there are few: one of LANES has every LANES-th slice.
 template <int LANES>
@@ -335,7 +323,7 @@ bool fits(const cprune_adapter_desc& d, const AdapterPlan& q, bool backward) {
   const double most = 4294967296.0 / 256;
   const int c = backward ? d.k : d.c_out;
   if ((double)q.tiles * q.splits >= most || (double)q.tiles * ((c - 1) / 256 + 1) >= most || (double)q.tiles * kTileRows >= 2147483648.0 || (double)q.tiles * q.ranks >= most) return false;
-  if (!backward) return (double)d.adapters * d.c_out * q.padded / 4 < 4294967040.0;
+  if (!backward) return (double)q.tiles * q.splits * 256 + (double)d.adapters * d.c_out * q.padded / 4 < 4294967040.0;
   const double turned = (double)d.adapters * ((d.k + 63.0) / 64 + (d.c_out + 63.0) / 64) * 2;      // (ranks of up to 128 are two tiles)
   return turned < most / 4 - 1 && (double)q.slices * (q.groups_a + q.groups_b) < most && (double)d.adapters * d.rank * ((double)d.k + d.c_out) < 4294967040.0;
 }
@@ -357,7 +345,7 @@ struct Scratch {
 
 AdapterTiles tiles_of(const cprune_adapter_desc& d, const AdapterPlan& q, const int32_t* which) {
   AdapterTiles t = {};
-  t.which = which, t.rows = d.rows, t.adapters = d.adapters, t.few = q.few;
+  t.which = which, t.rows = d.rows, t.adapters = d.adapters, t.count = q.tiles, t.few = q.few;
   return t;
 }
 
@@ -422,20 +410,18 @@ extern "C" int cprune_adapter_linear(const cprune_adapter_desc* d, const void* x
   prepare(*d, q, tiles, nullptr, {}, {}, scratch, s);
   float* const part = scratch.take<float>(q.part);
   AdapterLaunch l = {(unsigned)(q.tiles * q.splits), q.ranks, d->rows <= 16, false};
-  const NarrowArgs n = {tiles, x, d->x_stride, d->k, d->rank, a, part, q.splits, q.per};
+  NarrowArgs n = {tiles, x, d->x_stride, d->k, d->rank, a, part, q.splits, q.per};
+  if (d->rank % 8) {
+    n.b = b, n.b_out = scratch.take<char>(q.bt), n.b_rank = d->rank, n.b_padded = q.padded;
+    n.b_vectors = (long)d->adapters * d->c_out * q.padded / (16 / (long)dtype_size(d->dtype));
+    b = n.b_out;
+    l.grid += (unsigned)((n.b_vectors + 255) / 256);
+  }
   launch(d->dtype, kAdapterNarrow, &n, l, s);
   const float open = std::numeric_limits<float>::infinity();
   WidenArgs w = {};
   w.tiles = tiles, w.part = part, w.splits = q.splits, w.rank = d->rank, w.scale = scale, w.b = b, w.c = d->c_out, w.b_stride = q.padded;
   w.silu = d->act == CPRUNE_ACT_SILU;
-  if (d->rank % 8) {
-    uint4* const padded = scratch.take<uint4>(q.bt);
-    const long vectors = (long)d->adapters * d->c_out * q.padded / (16 / (long)dtype_size(d->dtype));
-    const unsigned grid = (unsigned)((vectors + 255) / 256);
-    if (d->dtype == CPRUNE_F32) adapter_pad_kernel<float><<<grid, 256, 0, s>>>(static_cast<const float*>(b), vectors, d->rank, q.padded, padded);
-    else adapter_pad_kernel<__bf16><<<grid, 256, 0, s>>>(static_cast<const __bf16*>(b), vectors, d->rank, q.padded, padded);
-    w.b = padded;
-  }
   w.base = base, w.base_stride = d->base_stride, w.y = y, w.hidden = hidden;
   w.lo = d->act == CPRUNE_ACT_NONE || d->act == CPRUNE_ACT_SILU ? -open : 0.0f, w.hi = d->act == CPRUNE_ACT_RELU6 ? 6.0f : open;
   w.columns = columns_of(*d, q, d->c_out);

@@ -31,7 +31,7 @@ struct AdapterTiles {
   const int* which;        // few: the rows' adapters, a ballot finds the tile of row t if that is its first
   const int* order;        // sorted, or null: row 64 t + i
   const int* tile_of;      // sorted: adapter of a tile, -1 for rows without; past the last tile -2
-  int rows, adapters;
+  int rows, adapters, count;      // (tiles there may be)
   bool few;
 };
 
@@ -43,6 +43,11 @@ struct NarrowArgs {
   const void* a;           // [adapters][rank][k]
   float* part;             // [splits][rows][RP]
   int splits, per;         // work-groups that share a sum, chunks of 256 bytes of each
+  // B filled up for widen by the work-groups past these, 16 bytes a thread: [row][b_rank] -> [row][b_padded], zeros past the rank; b_vectors 0: none
+  const void* b;
+  void* b_out;
+  long b_vectors;
+  int b_rank, b_padded;
 };
 
 struct WidenArgs {
@@ -261,6 +266,15 @@ __global__ __launch_bounds__(256, narrow_waves(NR)) void adapter_narrow_kernel(c
   __shared__ uint4 staged[2][LINES][PITCH];
   const int t = (int)threadIdx.x, lane = t & 63, wave = t >> 6, quarter = lane >> 4, lrow = lane & 15;
   const int tile_no = blockIdx.x / (unsigned)p.splits, split = blockIdx.x - tile_no * p.splits;
+  if (tile_no >= p.tiles.count) {
+    const long i = (long)(blockIdx.x - p.tiles.count * p.splits) * 256 + t;
+    if (i >= p.b_vectors) return;
+    const int per = p.b_padded / V;
+    const long row = i / per;
+    const int at = (int)(i - row * per) * V;
+    static_cast<uint4*>(p.b_out)[i] = load_some(static_cast<const T*>(p.b) + row * p.b_rank + at, p.b_rank - at);
+    return;
+  }
   int count;
   const int adapter = open_tile(p.tiles, tile_no, tile, count);
   if (adapter < 0) return;      // (rows without an adapter: what would be read here is known to be 0)
@@ -387,6 +401,25 @@ __global__ __launch_bounds__(256, widen_waves(NR, sizeof(T))) void adapter_widen
   constexpr bool AHEAD = NS <= 2;      // the next columns' weights are asked for before these are multiplied, where registers hold both
   uint4 w[4][NS];
   if (AHEAD && begin < end) weights(begin, w);
+  // base, of the next columns as soon as these rows' have been used; LINE lanes of 16 bytes a row, so that it and y are met in whole lines
+  constexpr int LINE = 64 / V, EACH = 16 * LINE / 64;
+  const int line = lane / LINE, col = lane % LINE * V, tail = p.c % V;
+  const T* const base = static_cast<const T*>(p.base);
+  T* const y = static_cast<T*>(p.y);
+  const bool with_base = base && p.c >= V;
+  uint4 z[F][EACH];
+  auto ask = [&](int f, int c0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const int row = tile.row[16 * f + i * (64 / LINE) + line];
+      z[f][i] = load(base + (long)(row >= 0 ? row : tile.row[0]) * p.base_stride + min(c0 + col, p.c - V));
+    }
+  };
+  if (with_base && begin < end) {
+#pragma unroll
+    for (int f = 0; f < F; ++f)
+      if (f < frags) ask(f, begin);
+  }
   // the rows' hidden numbers, zeros past the rank
   const float scale = adapter >= 0 && p.scale ? p.scale[adapter] : 1.0f;
   for (int i = t; i < 16 * frags * NS * STEP / 4; i += 256) {
@@ -423,30 +456,15 @@ __global__ __launch_bounds__(256, widen_waves(NR, sizeof(T))) void adapter_widen
     v = v < p.lo ? p.lo : v;      // (comparisons and not minimum / maximum: a NaN stays one)
     return v > p.hi ? p.hi : v;
   };
-  // Results go through LDS, 16 rows of a wavefront at a time, so that base and y are met in whole lines: LINE lanes of 16 bytes a row
-  constexpr int LINE = 64 / V, EACH = 16 * LINE / 64;
+  // Results go through LDS, 16 rows of a wavefront at a time
   typedef T numbers __attribute__((ext_vector_type(V)));
   typedef T outs __attribute__((ext_vector_type(V), aligned(2)));
   float (*const out)[64 + 4] = results[wave];
-  const int line = lane / LINE, col = lane % LINE * V, tail = p.c % V;
-  const T* const base = static_cast<const T*>(p.base);
-  T* const y = static_cast<T*>(p.y);
 #pragma unroll 1
   for (int c0 = begin; c0 < end; c0 += 64) {
     const int c = c0 + col;
     const bool whole = c + V <= p.c;
-    uint4 z[F][EACH], next[4][NS];
-    if (p.base && p.c >= V) {
-#pragma unroll
-      for (int f = 0; f < F; ++f)
-        if (f < frags) {
-#pragma unroll
-          for (int i = 0; i < EACH; ++i) {
-            const int row = tile.row[16 * f + i * (64 / LINE) + line];
-            z[f][i] = load(base + (long)(row >= 0 ? row : tile.row[0]) * p.base_stride + min(c, p.c - V));
-          }
-        }
-    }
+    uint4 next[4][NS];
     if constexpr (AHEAD) {
       weights(min(c0 + 64, end - 1), next);
     } else {
@@ -500,6 +518,7 @@ __global__ __launch_bounds__(256, widen_waves(NR, sizeof(T))) void adapter_widen
           y[(long)row * p.c + at] = Elem<T>::from_f32(finish(v));
         }
       }
+      if (with_base && c0 + 64 < end) ask(f, c0 + 64);
       wave_sync();
     }
     if constexpr (AHEAD) {
