@@ -418,12 +418,10 @@ extern "C" int cprune_adapter_linear(const cprune_adapter_desc* d, const void* x
     l.grid += (unsigned)((n.b_vectors + 255) / 256);
   }
   launch(d->dtype, kAdapterNarrow, &n, l, s);
-  const float open = std::numeric_limits<float>::infinity();
   WidenArgs w = {};
   w.tiles = tiles, w.part = part, w.splits = q.splits, w.rank = d->rank, w.scale = scale, w.b = b, w.c = d->c_out, w.b_stride = q.padded;
-  w.silu = d->act == CPRUNE_ACT_SILU;
   w.base = base, w.base_stride = d->base_stride, w.y = y, w.hidden = hidden;
-  w.lo = d->act == CPRUNE_ACT_NONE || d->act == CPRUNE_ACT_SILU ? -open : 0.0f, w.hi = d->act == CPRUNE_ACT_RELU6 ? 6.0f : open;
+  w.act = d->act;
   w.columns = columns_of(*d, q, d->c_out);
   w.stream = past_caches(*d, d->c_out, base);
   l.grid = (unsigned)(q.tiles * ((d->c_out - 1) / w.columns + 1));
@@ -470,10 +468,9 @@ extern "C" int cprune_adapter_linear_backward(const cprune_adapter_desc* d, cons
   l.grid = (unsigned)(q.tiles * q.ranks);
   launch(d->dtype, kAdapterParts, &r, l, s);
   if (dx) {
-    const float open = std::numeric_limits<float>::infinity();
-    WidenArgs w = {};
+      WidenArgs w = {};
     w.tiles = tiles, w.part = g, w.splits = 1, w.rank = d->rank, w.b = at, w.c = d->k, w.b_stride = q.padded;
-    w.base = dx_base, w.base_stride = d->base_stride, w.y = dx, w.lo = -open, w.hi = open;
+    w.base = dx_base, w.base_stride = d->base_stride, w.y = dx, w.act = CPRUNE_ACT_NONE;
     w.columns = columns_of(*d, q, d->k);
     w.stream = past_caches(*d, d->k, dx_base);
     l.grid = (unsigned)(q.tiles * ((d->k - 1) / w.columns + 1));

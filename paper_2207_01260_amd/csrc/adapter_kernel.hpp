@@ -61,10 +61,9 @@ struct WidenArgs {
   long base_stride;
   void* y;                 // [rows][c]
   float* hidden;           // [rows][rank] or null
-  float lo, hi;
+  int act;
   int columns;             // of a work-group, a multiple of 128
   bool stream;             // y is stored past the caches
-  bool silu;
 };
 
 // hidden and g as the outer product's operands, by steps of its terms, places: 16-bit, three bf16 parts [3][places / 32][RP][32], fp32 [places / 16][RP][16]
@@ -373,9 +372,9 @@ __global__ __launch_bounds__(256, narrow_waves(NR)) void adapter_narrow_kernel(c
 
 template <typename T, int NR, int F>
 __global__ __launch_bounds__(256, widen_waves(NR, sizeof(T))) void adapter_widen_kernel(const WidenArgs p) {
-  constexpr int V = kV<T>, STEP = kStep<T>, RP = 16 * NR, NS = (RP + STEP - 1) / STEP, N = sizeof(T) == 4 ? 1 : 2;
+  constexpr int V = kV<T>, STEP = kStep<T>, RP = 16 * NR, NS = (RP + STEP - 1) / STEP, N = sizeof(T) == 4 ? 1 : 2, M = std::is_same<T, _Float16>::value ? 2 : 1;
   __shared__ Tile tile;
-  __shared__ float results[4][16][64 + 4];
+  __shared__ float results[4][F == 1 ? 1 : 2][16][64 + 4];
   __shared__ float hidden[16 * F][NS * STEP + 4];
   const int t = (int)threadIdx.x, lane = t & 63, wave = t >> 6, quarter = lane >> 4, lrow = lane & 15;
   const int chunks = (p.c - 1) / p.columns + 1;
@@ -384,6 +383,16 @@ __global__ __launch_bounds__(256, widen_waves(NR, sizeof(T))) void adapter_widen
   const int adapter = open_tile(p.tiles, tile_no, tile, count);
   if (adapter == -2) return;
   const int frags = min((count + 15) / 16, F);      // (a sorted tile is 64 places, whatever its rows)
+  // The rows' hidden numbers, zeros past the rank: asked for before all else, so that what is asked for next need not be waited for with them.
+  constexpr int ITEMS = (16 * F * NS * STEP / 4 + 255) / 256;
+  float4_t held[ITEMS];
+  const float scale = adapter >= 0 && p.scale ? p.scale[adapter] : 1.0f;
+#pragma unroll
+  for (int u = 0; u < ITEMS; ++u) {
+    const int i = t + 256 * u, r = i / (NS * STEP / 4), j = 4 * (i - r * (NS * STEP / 4)), row = r < 16 * F ? tile.row[r] : -1;
+    held[u] = (float4_t){0.f, 0.f, 0.f, 0.f};
+    if (row >= 0 && adapter >= 0 && j < p.rank) held[u] = sum_parts(p.part + (long)row * RP + j, p.splits, (long)p.tiles.rows * RP);
+  }
   // 64 columns at a time.  Columns past the last are the last again, whose results nobody stores.
   const T* const b = static_cast<const T*>(p.b) + (long)max(adapter, 0) * p.c * p.b_stride;
   const int run = p.columns / 4, begin = chunk * p.columns + wave * run, end = min(p.c, begin + run);
@@ -399,8 +408,8 @@ __global__ __launch_bounds__(256, widen_waves(NR, sizeof(T))) void adapter_widen
     }
   };
   constexpr bool AHEAD = NS <= 2;      // the next columns' weights are asked for before these are multiplied, where registers hold both
-  uint4 w[4][NS];
-  if (AHEAD && begin < end) weights(begin, w);
+  uint4 next[4][NS];
+  if (AHEAD && begin < end) weights(begin, next);
   // base, of the next columns as soon as these rows' have been used; LINE lanes of 16 bytes a row, so that it and y are met in whole lines
   constexpr int LINE = 64 / V, EACH = 16 * LINE / 64;
   const int line = lane / LINE, col = lane % LINE * V, tail = p.c % V;
@@ -420,15 +429,15 @@ __global__ __launch_bounds__(256, widen_waves(NR, sizeof(T))) void adapter_widen
     for (int f = 0; f < F; ++f)
       if (f < frags) ask(f, begin);
   }
-  // the rows' hidden numbers, zeros past the rank
-  const float scale = adapter >= 0 && p.scale ? p.scale[adapter] : 1.0f;
-  for (int i = t; i < 16 * frags * NS * STEP / 4; i += 256) {
-    const int r = i / (NS * STEP / 4), j = 4 * (i - r * (NS * STEP / 4)), row = tile.row[r];
-    float4_t v = {0.f, 0.f, 0.f, 0.f};
-    if (row >= 0 && adapter >= 0 && j < p.rank) v = scale * sum_parts(p.part + (long)row * RP + j, p.splits, (long)p.tiles.rows * RP);
+#pragma unroll
+  for (int u = 0; u < ITEMS; ++u) {
+    const int i = t + 256 * u, r = i / (NS * STEP / 4), j = 4 * (i - r * (NS * STEP / 4));
+    if (r >= 16 * F) break;
+    const int row = tile.row[r];
+    float4_t v = scale * held[u];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      v[e] = j + e < p.rank ? v[e] : 0.0f;
+      v[e] = j + e < p.rank && row >= 0 && adapter >= 0 ? v[e] : 0.0f;
       if (p.hidden && chunk == 0 && row >= 0 && j + e < p.rank) p.hidden[(long)row * p.rank + j + e] = v[e];
     }
     *reinterpret_cast<float4_t*>(&hidden[r][j]) = v;
@@ -452,38 +461,53 @@ __global__ __launch_bounds__(256, widen_waves(NR, sizeof(T))) void adapter_widen
     }
   }
   auto finish = [&](float v) __attribute__((always_inline)) {
-    if (p.silu) return v * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * -1.44269504f));      // (2^x flushes below 2^-126: 1 + e^-z does not see it)
-    v = v < p.lo ? p.lo : v;      // (comparisons and not minimum / maximum: a NaN stays one)
-    return v > p.hi ? p.hi : v;
+    if (p.act == CPRUNE_ACT_SILU) return v * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * -1.44269504f));      // (2^x flushes below 2^-126: 1 + e^-z does not see it)
+    if (p.act != CPRUNE_ACT_NONE) v = v < 0.0f ? 0.0f : v;      // (comparisons and not minimum / maximum: a NaN stays one)
+    return p.act == CPRUNE_ACT_RELU6 && v > 6.0f ? 6.0f : v;
   };
-  // Results go through LDS, 16 rows of a wavefront at a time
   typedef T numbers __attribute__((ext_vector_type(V)));
   typedef T outs __attribute__((ext_vector_type(V), aligned(2)));
-  float (*const out)[64 + 4] = results[wave];
+  // Results go through LDS, 16 rows of a wavefront at a time, the next ones multiplied while these are finished
 #pragma unroll 1
   for (int c0 = begin; c0 < end; c0 += 64) {
     const int c = c0 + col;
     const bool whole = c + V <= p.c;
-    uint4 next[4][NS];
-    if constexpr (AHEAD) {
-      weights(min(c0 + 64, end - 1), next);
-    } else {
-      weights(c0, w);
-    }
+    uint4 w[4][NS][M];
+    if constexpr (!AHEAD) weights(c0, next);
 #pragma unroll
-    for (int f = 0; f < F; ++f) {
-      if (f >= frags) break;
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        if constexpr (M == 2) halves_of(next[g][s], w[g][s]);
+        else w[g][s][0] = next[g][s];
+      }
+    if constexpr (AHEAD) weights(min(c0 + 64, end - 1), next);
+    auto multiply = [&](int f) __attribute__((always_inline)) {
+      float (*const out)[64 + 4] = results[wave][F == 1 ? 0 : f & 1];
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         float4_t acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
-          if constexpr (sizeof(T) == 4) acc = mma<float>(w[g][s], h[f][s][0], acc);
-          else acc = mma_parts<T, N, false>(w[g][s], h[f][s], acc);
+          if constexpr (sizeof(T) == 4) {
+            acc = mma<float>(w[g][s][0], h[f][s][0], acc);
+          } else {
+#pragma unroll
+            for (int m = M - 1; m >= 0; --m)
+#pragma unroll
+              for (int n = N - 1; n >= 0; --n) acc = mma<__bf16>(w[g][s][m], h[f][s][n], acc);
+          }
         }
         *reinterpret_cast<float4_t*>(&out[lrow][16 * g + 4 * quarter]) = acc;
       }
-      wave_sync();
+    };
+    multiply(0);
+    wave_sync();
+#pragma unroll
+    for (int f = 0; f < F; ++f) {
+      if (f >= frags) break;
+      if (f + 1 < F && f + 1 < frags) multiply(f + 1);
+      const float (*const out)[64 + 4] = results[wave][F == 1 ? 0 : f & 1];
 #pragma unroll
       for (int i = 0; i < EACH; ++i) {
         const int in = i * (64 / LINE) + line, row = tile.row[16 * f + in];
@@ -494,14 +518,18 @@ __global__ __launch_bounds__(256, widen_waves(NR, sizeof(T))) void adapter_widen
 #pragma unroll
           for (int u = 0; u < 4; ++u) v[e + u] = q[u];
         }
-        if (p.base) {
+        if (with_base) {
           const numbers n = __builtin_bit_cast(numbers, z[f][i]);
 #pragma unroll
           for (int e = 0; e < V; ++e) v[e] += Elem<T>::to_f32(n[e]);
         }
+        if (p.act != CPRUNE_ACT_NONE) {
+#pragma unroll
+          for (int e = 0; e < V; ++e) v[e] = finish(v[e]);
+        }
         outs o;
 #pragma unroll
-        for (int e = 0; e < V; ++e) o[e] = Elem<T>::from_f32(finish(v[e]));
+        for (int e = 0; e < V; ++e) o[e] = Elem<T>::from_f32(v[e]);
         if (row >= 0 && whole) {
           outs* const to = reinterpret_cast<outs*>(y + (long)row * p.c + c);
           if (p.stream) __builtin_nontemporal_store(o, to);
@@ -514,18 +542,12 @@ __global__ __launch_bounds__(256, widen_waves(NR, sizeof(T))) void adapter_widen
           const int in = i / tail, at = p.c - tail + i - in * tail, row = tile.row[16 * f + in];
           if (row < 0) continue;
           float v = out[in][at - c0];
-          if (p.base) v += Elem<T>::to_f32(base[(long)row * p.base_stride + at]);
+          if (base) v += Elem<T>::to_f32(base[(long)row * p.base_stride + at]);
           y[(long)row * p.c + at] = Elem<T>::from_f32(finish(v));
         }
       }
       if (with_base && c0 + 64 < end) ask(f, c0 + 64);
       wave_sync();
-    }
-    if constexpr (AHEAD) {
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-#pragma unroll
-        for (int s = 0; s < NS; ++s) w[g][s] = next[g][s];
     }
   }
 }
