@@ -3,11 +3,13 @@
 and Algorithm 1's latency-gated iteration (Section 3.2), with every latency measured on the
 GPU through the library.
 
-Accuracy is not computed here (no dataset, no training): `accuracy` is a function the caller
+Accuracy on a dataset is not computed here (there is none): `accuracy` is a function the caller
 supplies; the default accepts every candidate, which leaves the latency gate, the task order
-and the step rule as the things that decide.
+and the step rule as the things that decide.  With --recover a candidate is first brought back,
+for some steps, to what the search's first model answered (adapters beside its classifier in 4
+bits, from that model's largest logits), and judged by how many images it then answers alike.
 
-    python -m paper_2207_01260_amd.search [--net vgg16] [--batch 64] [--iterations 4]
+    python -m paper_2207_01260_amd.search [--net vgg16] [--batch 64] [--iterations 4] [--recover 0]
 """
 import argparse
 import json
@@ -18,6 +20,7 @@ import torch
 
 from . import binding as B
 from . import pipeline, synth
+from .recover import AdaptedLinear
 
 
 # ---- Algorithm 1: the library decides, the caller measures ------------------------------
@@ -108,8 +111,9 @@ class DeviceSearch:
     table, per-layer times and the forward time."""
 
     def __init__(self, net: synth.NetSpec, params: List[dict], config_id: int, batch: int,
-                 dtype: int = B.F32, steps: int = 30):
+                 dtype: int = B.F32, steps: int = 30, recover: int = 0):
         self.net, self.batch, self.dtype, self.steps = net, batch, dtype, steps
+        self.recover, self.teacher = recover, None
         self.dparams = pipeline.upload_params(params)
         self.x = torch.from_numpy(synth.net_input(net, config_id, batch)).cuda().to(B.TORCH_DTYPE[dtype])
         self.prunable = [i for i, L in enumerate(net.layers) if L.prune_out == "own"]
@@ -161,8 +165,13 @@ class DeviceSearch:
             step = B.cprune_variant_prune_step(v, shp[m[0]][1]) if v >= 0 else 16
             table[keys[t]] = (m, {"variant": v, "c_out": shp[m[0]][1], "time_ms": times[t], "impact": impact[t],
                                   "step": step})
-        handle.close()
         st = {"table": table, "order": [keys[t] for t in order], "ms": ms}
+        if self.recover:
+            last = self.net.layers[-1]
+            w, bias = layers[-1]["w"], layers[-1]["b"]
+            st["features"] = handle.activation(last.input, self.batch, (w.shape[1], 1, 1)).reshape(self.batch, w.shape[1])
+            st["logits"], st["classifier"] = out, (w, bias)
+        handle.close()
         self._cache[key] = st
         self.trace.append((dict(model), table, st["order"], ms))
         return st
@@ -173,6 +182,18 @@ class DeviceSearch:
 
     def measure(self, model) -> float:
         return self._state(model)["ms"]
+
+    def accuracy(self, model) -> float:
+        """The share of the images that the model, its classifier in 4 bits and brought back for `recover` steps, answers as the first model asked about did."""
+        st = self._state(model)
+        if self.teacher is None:
+            self.teacher = B.cprune_top_logits(st["logits"], min(8, st["logits"].shape[1]))
+        values, ids = self.teacher
+        layer = AdaptedLinear(*st["classifier"])
+        x = st["features"]
+        layer.tune(x, ids, values, self.recover, rate=0.5 / max(1.0, float(x.float().square().mean())))
+        _, top = B.cprune_top_logits(layer.forward(x), 1)
+        return float((top == ids[:, :1]).float().mean())
 
     def prune(self, model, task, subgraphs, program) -> Optional[Dict[int, int]]:
         """Every prunable subgraph of the task loses the number of filters the program's
@@ -190,14 +211,14 @@ class DeviceSearch:
 
 
 def run(net_name="vgg16", batch=64, dtype=B.F32, alpha=0.95, beta=0.98, a_goal=0.0, iterations=4,
-        accuracy: Optional[Callable] = None):
+        accuracy: Optional[Callable] = None, recover: int = 0):
     net, cid = {"vgg16": (synth.vgg16(10, 32), 2), "resnet18": (synth.resnet18(1000, 224), 3),
                 "mobilenetv2": (synth.mobilenetv2(1000, 224), 4),
                 "mnasnet": (synth.mnasnet(1000, 224), 6)}[net_name]
     params = synth.layer_params(net, cid)
-    ds = DeviceSearch(net, params, cid, batch, dtype)
+    ds = DeviceSearch(net, params, cid, batch, dtype, recover=recover)
     model = ds.initial_model(params)
-    acc = accuracy or (lambda m: 1.0)
+    acc = accuracy or (ds.accuracy if recover else lambda m: 1.0)
     final, log = run_search(model, a_goal, alpha, beta, ds.tune, ds.prune, ds.measure, acc,
                             max_iterations=iterations)
     return ds, model, final, log
@@ -209,15 +230,16 @@ def main():
     ap.add_argument("--batch", type=int, default=64)
     ap.add_argument("--iterations", type=int, default=4)
     ap.add_argument("--beta", type=float, default=0.98)
+    ap.add_argument("--recover", type=int, default=0, help="steps of bringing a candidate back before it is judged (0: every candidate is accepted)")
     args = ap.parse_args()
-    ds, start, final, log = run(args.net, args.batch, iterations=args.iterations, beta=args.beta)
+    ds, start, final, log = run(args.net, args.batch, iterations=args.iterations, beta=args.beta, recover=args.recover)
     table, order = ds.tune(start)
     print(json.dumps({"start_ms": round(ds.measure(start), 4), "tasks_by_impact": [
         {"task": list(map(str, t)), "layers": table[t][0], **{k: (round(v, 5) if isinstance(v, float) else v)
                                                              for k, v in table[t][1].items()}} for t in order]}))
     for task, l_m, l_t, a_s, verdict in log:
         print(json.dumps({"task": list(map(str, task)), "l_m": None if l_m is None else round(l_m, 4),
-                          "l_t": round(l_t, 4), "verdict": verdict}))
+                          "l_t": round(l_t, 4), "verdict": verdict, **({"a_s": a_s} if args.recover else {})}))
     print(json.dumps({"final_ms": round(ds.measure(final), 4), "kept": [final[i] for i in sorted(final)]}))
 
 
