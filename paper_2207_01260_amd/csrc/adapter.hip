@@ -199,38 +199,45 @@ __global__ __launch_bounds__(64 * kSortWaves) void adapter_prepare_kernel(const 
 // where there are few: one of LANES has every LANES-th slice.
 template <int LANES>
 __global__ __launch_bounds__(256) void adapter_join_kernel(const float* __restrict__ sums_b, const float* __restrict__ sums_a, const int* __restrict__ tile_at, int tile_count, int slices, int adapters,
-                                                           int rank, int rp, int k, int c, float* __restrict__ da, float* __restrict__ db) {
-  constexpr int RESULTS = 256 / LANES;
+                                                           int rank, int rp, int k, int c, int groups_b, int groups_a, float* __restrict__ da, float* __restrict__ db) {
+  constexpr int RESULTS = 256 / LANES, EACH = LANES == 1 ? 4 : 1;      // of a pass; passes of a work-group
   __shared__ float parts[256];
   const int t = (int)threadIdx.x, in_group = t % RESULTS, turn = t / RESULTS;
-  const long all_b = (long)adapters * c * rank, all = all_b + (long)adapters * rank * k, i = (long)blockIdx.x * RESULTS + in_group;
-  const bool of_b = i < all_b;
-  const long m = of_b ? i : i - all_b;
-  float s = 0.0f;
-  if (i < all) {
-    const long per = of_b ? (long)c * rank : (long)rank * k;
-    const int n = (int)(m / per);
-    const long in = m - n * per, pitch = of_b ? (long)c * rp : (long)rp * k;
-    const long at = of_b ? in / rank * rp + in % rank : in;
-    // slices that the adapter's tiles lie in: slice s begins at tile s tiles / slices
-    const int t0 = tile_at ? tile_at[n] : 0, t1 = tile_at ? tile_at[n + 1] : n == 0 ? tile_count : 0, tiles = tile_at ? tile_at[adapters] : tile_count;
-    const int first = t0 < t1 ? (int)(((long)(t0 + 1) * slices - 1) / tiles) + n : 0, last = t0 < t1 ? (int)(((long)t1 * slices - 1) / tiles) + n + 1 : 0;
-    const float* const from = (of_b ? sums_b : sums_a) + at;
+  const int n = blockIdx.x / (unsigned)(groups_a + groups_b), group = blockIdx.x - n * (groups_a + groups_b);
+  const bool of_b = group < groups_b;
+  const unsigned per = of_b ? (unsigned)c * rank : (unsigned)rank * k, from = (unsigned)(of_b ? group : group - groups_b) * (RESULTS * EACH);
+  const long pitch = of_b ? (long)c * rp : (long)rp * k;
+  // slices that the adapter's tiles lie in: slice s begins at tile s tiles / slices
+  const int t0 = tile_at ? tile_at[n] : 0, t1 = tile_at ? tile_at[n + 1] : n == 0 ? tile_count : 0, tiles = tile_at ? tile_at[adapters] : tile_count;
+  const int first = t0 < t1 ? (int)(((long)(t0 + 1) * slices - 1) / tiles) + n : 0, last = t0 < t1 ? (int)(((long)t1 * slices - 1) / tiles) + n + 1 : 0;
+  const float* const sums = of_b ? sums_b : sums_a;
+  float* const out = (of_b ? db : da) + (long)n * per;
+  float s[EACH];
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) {
+    const unsigned in = from + e * RESULTS + in_group;
+    s[e] = 0.0f;
+    if (in >= per) continue;
+    const float* const at = sums + (of_b ? in / rank * rp + in % rank : in);
     int q = first + turn;
     for (; q + 3 * LANES < last; q += 4 * LANES) {
-      const float v[4] = {from[q * pitch], from[(q + LANES) * pitch], from[(q + 2 * LANES) * pitch], from[(q + 3 * LANES) * pitch]};
-      s += v[0], s += v[1], s += v[2], s += v[3];
+      const float v[4] = {at[q * pitch], at[(q + LANES) * pitch], at[(q + 2 * LANES) * pitch], at[(q + 3 * LANES) * pitch]};
+      s[e] += v[0], s[e] += v[1], s[e] += v[2], s[e] += v[3];
     }
-    for (; q < last; q += LANES) s += from[q * pitch];
+    for (; q < last; q += LANES) s[e] += at[q * pitch];
   }
   if constexpr (LANES > 1) {
-    parts[t] = s;
+    parts[t] = s[0];
     __syncthreads();
     if (turn) return;
 #pragma unroll
-    for (int l = 1; l < LANES; ++l) s += parts[l * RESULTS + in_group];
+    for (int l = 1; l < LANES; ++l) s[0] += parts[l * RESULTS + in_group];
   }
-  if (i < all) (of_b ? db : da)[m] = s;
+#pragma unroll
+  for (int e = 0; e < EACH; ++e) {
+    const unsigned in = from + e * RESULTS + in_group;
+    if (in < per) out[in] = s[e];
+  }
 }
 
 // ---- host ------------------------------------------------------------------------
@@ -325,7 +332,7 @@ bool fits(const cprune_adapter_desc& d, const AdapterPlan& q, bool backward) {
   if ((double)q.tiles * q.splits >= most || (double)q.tiles * ((c - 1) / 256 + 1) >= most || (double)q.tiles * kTileRows >= 2147483648.0 || (double)q.tiles * q.ranks >= most) return false;
   if (!backward) return (double)q.tiles * q.splits * 256 + (double)d.adapters * d.c_out * q.padded / 4 < 4294967040.0;
   const double turned = (double)d.adapters * ((d.k + 63.0) / 64 + (d.c_out + 63.0) / 64) * 2;      // (ranks of up to 128 are two tiles)
-  return turned < most / 4 - 1 && (double)q.slices * (q.groups_a + q.groups_b) < most && (double)d.adapters * d.rank * ((double)d.k + d.c_out) < 4294967040.0;
+  return turned < most / 4 - 1 && (double)q.slices * (q.groups_a + q.groups_b) < most && (double)d.adapters * (d.rank * ((double)d.k + d.c_out) / 1024 + 2) < most;
 }
 
 void launch(int dtype, AdapterPass pass, const void* args, const AdapterLaunch& l, hipStream_t s) {
@@ -372,13 +379,17 @@ void prepare(const cprune_adapter_desc& d, const AdapterPlan& q, AdapterTiles& t
 // What does not stay in the last-level cache (256 MB, shared with what else is in use) is stored past it.
 bool past_caches(const cprune_adapter_desc& d, int c, const void* base) { return (base ? 2.0 : 1.0) * d.rows * c * dtype_size(d.dtype) > 134217728.0; }
 
-// Columns of a work-group: those that take the fewest rounds of work-groups, by the columns of each and what it does but once, some 200 columns' time.
+// Columns of a work-group: those that leave the busiest compute unit least to do, by the columns of its work-groups and what each does but once, some 150 columns' time.
 int columns_of(const cprune_adapter_desc& d, const AdapterPlan& q, int c) {
-  const long resident = 256 * widen_waves(q.ranks, (int)dtype_size(d.dtype)), tiles = rounded_tiles(d, q);
+  const long tiles = rounded_tiles(d, q);
   int best = 256;
+  if (q.few) {      // (a few rows each, all waiting for memory: side by side; 48 x 8192 x 8192, 32 adapters, 10.5 us in 512 columns, 16.3 in 1280)
+    while (best < 2048 && tiles * ((c - 1) / best + 1) > 768) best *= 2;
+    return best;
+  }
   long least = std::numeric_limits<long>::max();
   for (int columns = 256; columns <= 2048; columns += 256) {
-    const long groups = tiles * ((c - 1) / columns + 1), cost = ((groups - 1) / resident + 1) * (std::min(columns, c) + 200);
+    const long cost = ((tiles * ((c - 1) / columns + 1) - 1) / 256 + 1) * (std::min(columns, c) + 150);
     if (cost < least) least = cost, best = columns;
   }
   return best;
@@ -487,7 +498,10 @@ extern "C" int cprune_adapter_linear_backward(const cprune_adapter_desc* d, cons
     const long all = (long)d->adapters * d->rank * ((long)d->k + d->c_out);
     auto join = [&](auto lanes) {
       constexpr int LANES = decltype(lanes)::value;
-      adapter_join_kernel<LANES><<<(unsigned)((all * LANES + 255) / 256), 256, 0, s>>>(sums_b, sums_a, tile_at, q.tiles, q.slices, d->adapters, d->rank, q.rp, d->k, d->c_out, da, db);
+      const long results = 256 / LANES * (LANES == 1 ? 4 : 1);      // of a work-group
+      const int of_b = (int)(((long)d->c_out * d->rank - 1) / results + 1), of_a = (int)(((long)d->k * d->rank - 1) / results + 1);
+      adapter_join_kernel<LANES><<<(unsigned)(d->adapters * (of_a + of_b)), 256, 0, s>>>(sums_b, sums_a, tile_at, q.tiles, q.slices, d->adapters, d->rank, q.rp, d->k, d->c_out, of_b, of_a,
+                                                                                         da, db);
     };
     if (all <= 65536 && q.slices >= 8) join(std::integral_constant<int, 8>());
     else join(std::integral_constant<int, 1>());

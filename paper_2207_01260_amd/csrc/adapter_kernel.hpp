@@ -23,7 +23,7 @@ constexpr int kTileRows = 64;
 
 // Work-groups of 256 that a compute unit holds at once, by registers; what is cut into work-groups is cut for whole rounds of them.
 constexpr int narrow_waves(int ranks) { return ranks <= 2 ? 3 : ranks <= 4 ? 2 : 1; }
-constexpr int widen_waves(int ranks, int size) { return ranks <= 2 ? (size == 2 ? 3 : 2) : ranks == 4 && size == 2 ? 2 : 1; }
+constexpr int widen_waves(int ranks, int size) { return ranks * size <= 8 ? 3 : ranks * size <= 16 ? 2 : 1; }
 constexpr int kOuterWaves = 2;
 
 // Places: tile t has rows order[64 t .. 64 t + 63], -1 where it has fewer.
@@ -375,7 +375,7 @@ __global__ __launch_bounds__(256, widen_waves(NR, sizeof(T))) void adapter_widen
   constexpr int V = kV<T>, STEP = kStep<T>, RP = 16 * NR, NS = (RP + STEP - 1) / STEP, N = sizeof(T) == 4 ? 1 : 2, M = std::is_same<T, _Float16>::value ? 2 : 1;
   __shared__ Tile tile;
   __shared__ float results[4][F == 1 ? 1 : 2][16][64 + 4];
-  __shared__ float hidden[16 * F][NS * STEP + 4];
+  __shared__ uint4 hidden[16 * F][NS * N * 4 + 1];      // as operands: step, part, quarter
   const int t = (int)threadIdx.x, lane = t & 63, wave = t >> 6, quarter = lane >> 4, lrow = lane & 15;
   const int chunks = (p.c - 1) / p.columns + 1;
   const int tile_no = blockIdx.x / (unsigned)chunks, chunk = blockIdx.x - tile_no * chunks;
@@ -440,26 +440,24 @@ __global__ __launch_bounds__(256, widen_waves(NR, sizeof(T))) void adapter_widen
       v[e] = j + e < p.rank && row >= 0 && adapter >= 0 ? v[e] : 0.0f;
       if (p.hidden && chunk == 0 && row >= 0 && j + e < p.rank) p.hidden[(long)row * p.rank + j + e] = v[e];
     }
-    *reinterpret_cast<float4_t*>(&hidden[r][j]) = v;
-  }
-  __syncthreads();
-  uint4 h[F][NS][N];
+    if constexpr (sizeof(T) == 4) {
+      *reinterpret_cast<float4_t*>(&hidden[r][j / 4]) = v;
+    } else {
 #pragma unroll
-  for (int f = 0; f < F; ++f) {
-    if (f >= frags) continue;
+      for (int n = 0; n < N; ++n) {
+        float f[4];
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      const float* const from = &hidden[16 * f + lrow][s * STEP + quarter * V];
-      if constexpr (sizeof(T) == 4) {
-        h[f][s][0] = *reinterpret_cast<const uint4*>(from);
-      } else {
-        float v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = from[e];
-        parts_of<N>(v, h[f][s]);
+        for (int e = 0; e < 4; ++e) {
+          float left = v[e];
+          f[e] = part_of(left);
+          v[e] = left;
+        }
+        uint2* const to = reinterpret_cast<uint2*>(&hidden[r][(j / STEP * N + n) * 4 + j % STEP / V]);
+        to[j / 4 & 1] = make_uint2(pair(f[0], f[1]), pair(f[2], f[3]));
       }
     }
   }
+  __syncthreads();
   auto finish = [&](float v) __attribute__((always_inline)) {
     if (p.act == CPRUNE_ACT_SILU) return v * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * -1.44269504f));      // (2^x flushes below 2^-126: 1 + e^-z does not see it)
     if (p.act != CPRUNE_ACT_NONE) v = v < 0.0f ? 0.0f : v;      // (comparisons and not minimum / maximum: a NaN stays one)
@@ -484,18 +482,23 @@ __global__ __launch_bounds__(256, widen_waves(NR, sizeof(T))) void adapter_widen
     if constexpr (AHEAD) weights(min(c0 + 64, end - 1), next);
     auto multiply = [&](int f) __attribute__((always_inline)) {
       float (*const out)[64 + 4] = results[wave][F == 1 ? 0 : f & 1];
+      uint4 h[NS][N];
+#pragma unroll
+      for (int s = 0; s < NS; ++s)
+#pragma unroll
+        for (int n = 0; n < N; ++n) h[s][n] = hidden[16 * f + lrow][(s * N + n) * 4 + quarter];
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         float4_t acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
           if constexpr (sizeof(T) == 4) {
-            acc = mma<float>(w[g][s][0], h[f][s][0], acc);
+            acc = mma<float>(w[g][s][0], h[s][0], acc);
           } else {
 #pragma unroll
             for (int m = M - 1; m >= 0; --m)
 #pragma unroll
-              for (int n = N - 1; n >= 0; --n) acc = mma<__bf16>(w[g][s][m], h[f][s][n], acc);
+              for (int n = N - 1; n >= 0; --n) acc = mma<__bf16>(w[g][s][m], h[s][n], acc);
           }
         }
         *reinterpret_cast<float4_t*>(&out[lrow][16 * g + 4 * quarter]) = acc;
