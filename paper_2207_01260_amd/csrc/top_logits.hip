@@ -2,8 +2,8 @@
 // listed.
 //
 // A bound first: each thread's largest number is one of the row's, so at least k numbers reach the k-th largest of those.  With more threads than k the numbers
-// that reach it are hardly more than k, in few threads, and those read theirs again; they go to a list in LDS, in any order, and each one's place is
-// the count of those before it.  What bounds it is reading z once.
+// that reach it are hardly more than k.  They are looked for where a thread's run of vectors reaches it, go to a list in LDS, in any order, and each one's place
+// is the count of those before it.  What bounds it is reading z once.
 #include <algorithm>
 
 #include "logits.hpp"
@@ -14,7 +14,8 @@ namespace {
 using logits::Raw;
 
 constexpr int kMostK = 256;
-constexpr int kList = 2048;      // numbers that reach the bound, in LDS; kMostK more of its equals
+constexpr int kSlots = 8, kRuns = 512;
+constexpr int kList = 1024;      // numbers that reach the bound, in LDS; kMostK more of its equals
 
 // 32 bits that order like numbers, -0 as 0, NaN above all; and the number again
 __device__ __forceinline__ unsigned key_of(float x) {
@@ -41,35 +42,16 @@ __global__ __launch_bounds__(NT) void top_kernel(const TopArgs a) {
   constexpr int V = Raw<T>::V, NW = NT / 64;
   __shared__ unsigned keys[NT], list_key[kList + kMostK];
   __shared__ int list_at[kList + kMostK];
-  __shared__ int count, sums[NW];
+  __shared__ int count, owners, sums[NW];
+  __shared__ unsigned short slots[kSlots][NT];
+  __shared__ int runs[kRuns];
   __shared__ unsigned bound;
   const int t = (int)threadIdx.x, lane = t & 63, wave = t >> 6;
   const int row_no = blockIdx.x / (unsigned)a.chunks, chunk = blockIdx.x - row_no * a.chunks;
   const long first = (long)chunk * a.per;
   const logits::Row<T> row(static_cast<const T*>(a.z) + row_no * a.stride + first, (int)min((long)a.per, a.classes - first));
   const int rounds = (row.full + NT - 1) / NT;
-  // f(number of the vector, its numbers); the edge is the last thread's
-  auto each = [&](auto&& f) __attribute__((always_inline)) {
-    constexpr int U = 8;
-#pragma unroll 1
-    for (int i = t; i < row.full; i += U * NT) {
-      uint4 r[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) r[u] = row.load(i + u * NT, row.full);
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        float x[V];
-        logits::unpack<T>(r[u], x);
-        f(i + u * NT, x);
-      }
-    }
-    if (row.tail && t == NT - 1) {
-      float x[V];
-      row.edge(true, x);
-      f(row.full, x);
-    }
-  };
-  // the same a vector at a time, where few have anything to do
+  // f(number of the vector, its numbers), a vector at a time; the edge is the last thread's
   auto each_slowly = [&](auto&& f) __attribute__((always_inline)) {
 #pragma unroll 1
     for (int i = t; i < row.full + (row.tail && t == NT - 1 ? NT : 0); i += NT) {
@@ -84,10 +66,37 @@ __global__ __launch_bounds__(NT) void top_kernel(const TopArgs a) {
       f(at, x);
     }
   };
+  // A thread's largest number, and of each of up to kSlots runs of four or more of its vectors the upper half of the largest one's key
+  const int fours = (rounds + 3) / 4, per = (fours + kSlots - 1) / kSlots;
+  for (int i = 0; i < min(fours, kSlots); ++i) slots[i][t] = 0;
   float top = -__builtin_inff();
-  each([&](int, const float (&x)[V]) __attribute__((always_inline)) { top = logits::larger(top, logits::largest(x)); });
+#pragma unroll 1
+  for (int q = 0; q < fours; q += 2) {
+    constexpr int U = 8;
+    uint4 r[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) r[u] = row.load(t + (4 * q + u) * NT, row.full);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      float m = -__builtin_inff();
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        float x[V];
+        logits::unpack<T>(r[4 * h + u], x);
+        m = logits::larger(m, logits::largest(x));
+      }
+      top = logits::larger(top, m);
+      unsigned short* const slot = &slots[min((q + h) / per, kSlots - 1)][t];      // (past the last four: nothing)
+      *slot = max(*slot, (unsigned short)(key_of(m) >> 16));
+    }
+  }
+  if (row.tail && t == NT - 1) {
+    float x[V];
+    row.edge(true, x);
+    top = logits::larger(top, logits::largest(x));
+  }
   keys[t] = key_of(top);
-  if (t == 0) count = 0;
+  if (t == 0) count = owners = 0;
   __syncthreads();
   if (wave == 0) {      // bit by bit the largest bound that k threads reach, or one that few more do
     unsigned mine[NW], b = 0;
@@ -112,30 +121,32 @@ __global__ __launch_bounds__(NT) void top_kernel(const TopArgs a) {
     const int i = atomicAdd(&count, 1);      // (in any order: places are counted below)
     if (i < kList) list_key[i] = key_of(x), list_at[i] = at;
   };
-  // a thread's vectors that reach it are looked for by 16 lanes, those of four threads at a time: read one after another they would each wait for memory
+  // the runs that reach it are read again, four lanes each
   auto look = [&](int i, const float (&x)[V]) __attribute__((always_inline)) {
     if (logits::largest(x) < from) return;
 #pragma unroll
     for (int j = 0; j < V; ++j)
       if (!(x[j] < from)) append(x[j], i * V + j);
   };
-  for (unsigned long long reach = __ballot(!(top < from)); reach;) {
-    int who = -1;
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      if (lane >> 4 == u && reach) who = __ffsll(reach) - 1;
-      reach &= reach - 1;
-    }
-    if (who < 0) continue;
+  if (!(top < from)) {
 #pragma unroll 1
-    for (int i = 64 * wave + who + (lane & 15) * NT; i < row.full; i += 32 * NT) {
-      const uint4 r[2] = {row.load(i, row.full), row.load(i + 16 * NT, row.full)};
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        float x[V];
-        logits::unpack<T>(r[u], x);
-        look(i + u * 16 * NT, x);
+    for (int i = 0; i < min(fours, kSlots); ++i)
+      if (slots[i][t] >= low >> 16) {
+        const int at = atomicAdd(&owners, 1);      // (in any order, as the list)
+        if (at < kRuns) runs[at] = i * NT + t;
       }
+  }
+  __syncthreads();
+  const int found = min(owners, kRuns);
+#pragma unroll 1
+  for (int o = t >> 2; o < found; o += NT / 4) {
+    const int run = runs[o] / NT, of = runs[o] % NT;
+#pragma unroll 1
+    for (int f = run * per; f < (run + 1) * per; ++f) {
+      const int i = of + (4 * f + (t & 3)) * NT;
+      float x[V];
+      logits::unpack<T>(row.load(i, row.full), x);
+      look(i, x);
     }
   }
   if (row.tail && t == NT - 1) {
@@ -145,7 +156,7 @@ __global__ __launch_bounds__(NT) void top_kernel(const TopArgs a) {
   }
   __syncthreads();
   int n = count;
-  if (n > kList) {      // Many equal to the bound, as where most of a row has the type's lowest value: of those only the first k can count.
+  if (n > kList || owners > kRuns) {      // Many equal to the bound, as where most of a row has the type's lowest value: of those only the first k can count.
     auto total = [&](int mine) __attribute__((always_inline)) {
 #pragma unroll
       for (int o = 32; o > 0; o >>= 1) mine += __shfl_xor(mine, o, 64);
