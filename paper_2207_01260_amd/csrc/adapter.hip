@@ -273,7 +273,7 @@ struct AdapterPlan {
 
 // Tiles as they are likely to be: half of the adapters' last ones are there, half are not.
 int rounded_tiles(const cprune_adapter_desc& d, const AdapterPlan& q) {
-  if (q.few) return std::min(q.tiles, d.adapters + 1);
+  if (q.few) return std::min(q.tiles, d.adapters + 1 + d.rows / kFewTile);
   return q.sorted ? std::min(q.tiles, d.rows / kTileRows + 1 + d.adapters / 2) : q.tiles;
 }
 
@@ -420,7 +420,7 @@ extern "C" int cprune_adapter_linear(const cprune_adapter_desc* d, const void* x
   AdapterTiles tiles = tiles_of(*d, q, which);
   prepare(*d, q, tiles, nullptr, {}, {}, scratch, s);
   float* const part = scratch.take<float>(q.part);
-  AdapterLaunch l = {(unsigned)(q.tiles * q.splits), q.ranks, d->rows <= 16, false};
+  AdapterLaunch l = {(unsigned)(q.tiles * q.splits), q.ranks, q.few || d->rows <= kFewTile, false};
   NarrowArgs n = {tiles, x, d->x_stride, d->k, d->rank, a, part, q.splits, q.per};
   if (d->rank % 8) {
     n.b = b, n.b_out = scratch.take<char>(q.bt), n.b_rank = d->rank, n.b_padded = q.padded;
@@ -469,7 +469,7 @@ extern "C" int cprune_adapter_linear_backward(const cprune_adapter_desc* d, cons
   float* const sums_b = scratch.take<float>(q.sums_b);
   float* const sums_a = scratch.take<float>(q.sums_a);
   const int v = 16 / (int)dtype_size(d->dtype);
-  AdapterLaunch l = {(unsigned)(q.tiles * q.splits), q.ranks, d->rows <= 16, d->k < v || d->c_out < v};
+  AdapterLaunch l = {(unsigned)(q.tiles * q.splits), q.ranks, d->rows <= kFewTile, d->k < v || d->c_out < v};
   const NarrowArgs n = {tiles, dy, d->dy_stride, d->c_out, d->rank, bt, part, q.splits, q.per};
   launch(d->dtype, kAdapterNarrow, &n, l, s);
   PartsArgs r = {};

@@ -1,7 +1,7 @@
 // Low-rank adapters: hidden_r = scale_i A_i x_r, y_r = act(base_r + B_i hidden_r), and their gradients, i the row's adapter.
 //
 // Rows in tiles of 64 with one adapter: all rows in their order where there is one adapter, the rows of each adapter behind each other where a launch before has
-// sorted them (adapter_plan_kernel), or, up to 64 rows, those that a work-group finds with a ballot.  A tile's rows are gathered: a row is long, its place is not.
+// sorted them, or, up to 64 rows, sixteen at most that a work-group finds with a ballot.  A tile's rows are gathered: a row is long, its place is not.
 //
 // Products on the matrix cores, an operand 16 bytes of a row for each lane: lane l has row l % 16 and the terms from 4 V times the step and V (l / 16) on, V numbers of 16
 // bytes.  fp32 takes four instructions a step, one for each of a lane's four terms (the terms' order does not matter, both operands
@@ -19,7 +19,7 @@
 
 namespace cprune {
 
-constexpr int kTileRows = 64;
+constexpr int kTileRows = 64, kFewTile = 16;
 
 // Work-groups of 256 that a compute unit holds at once, by registers; what is cut into work-groups is cut for whole rounds of them.
 constexpr int narrow_waves(int ranks) { return ranks <= 2 ? 3 : ranks <= 4 ? 2 : 1; }
@@ -28,7 +28,7 @@ constexpr int kOuterWaves = 2;
 
 // Places: tile t has rows order[64 t .. 64 t + 63], -1 where it has fewer.
 struct AdapterTiles {
-  const int* which;        // few: the rows' adapters, a ballot finds the tile of row t if that is its first
+  const int* which;        // few: the rows' adapters; tile t is that of row t and the next ones of its adapter, if as many as fill tiles are before it
   const int* order;        // sorted, or null: row 64 t + i
   const int* tile_of;      // sorted: adapter of a tile, -1 for rows without; past the last tile -2
   int rows, adapters, count;      // (tiles there may be)
@@ -207,14 +207,14 @@ __device__ __forceinline__ int open_tile(const AdapterTiles& t, int tile, Tile& 
     int mine = lane < t.rows ? t.which[lane] : -2;
     if (lane < t.rows && (unsigned)mine >= (unsigned)t.adapters) mine = -1;
     adapter = __shfl(mine, tile, 64);
-    const unsigned long long same = __ballot(mine == adapter);
-    if (__ffsll(same) - 1 != tile) return -2;
-    count = __popcll(same);
-    if (i < kTileRows) {
-      out.row[i] = -1;
-    }
+    unsigned long long same = __ballot(mine == adapter);
+    if (__popcll(same & ((1ull << tile) - 1)) % kFewTile) return -2;
+    same &= ~0ull << tile;
+    count = min(__popcll(same), kFewTile);
+    if (i < kTileRows) out.row[i] = -1;
     __syncthreads();
-    if (i < kTileRows && mine == adapter) out.row[__popcll(same & ((1ull << lane) - 1))] = lane;
+    const int at = __popcll(same & ((1ull << lane) - 1));
+    if (i < kTileRows && (same >> lane & 1) && at < kFewTile) out.row[at] = lane;
   } else if (t.order) {
     adapter = t.tile_of[tile];
     if (adapter == -2) return -2;
