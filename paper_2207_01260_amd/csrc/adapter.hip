@@ -195,48 +195,66 @@ __global__ __launch_bounds__(64 * kSortWaves) void adapter_prepare_kernel(const 
   else turn_tile<T>(b, i - tiles_a, reinterpret_cast<T*>(shared));
 }
 
-// Sums of an adapter's slices in their order: db [adapter][c][rank] from [slice + adapter][c][RP], da [adapter][rank][k] from [slice + adapter][RP][k].  Threads share a result
-// where there are few: one of LANES has every LANES-th slice.
+// Sums of an adapter's slices in their order: db [adapter][c][rank] and da [adapter][rank][k], from what the outer products leave (OuterSide::sums).  A thread has four results,
+// those of a lane; da's are neighbouring columns in neighbouring threads, db's neighbouring ranks.  Where there are few, LANES threads have every LANES-th slice of them each.
+struct JoinArgs {
+  const float4_t *sums_b, *sums_a;
+  const int* tile_at;
+  int tile_count, slices, adapters;
+  int rank, ranks, v, k, c;          // ranks, v: powers of two
+  int groups_b, groups_a;            // of 16 v columns
+  int blocks_b, blocks_a;            // work-groups of an adapter
+  float *da, *db;
+};
 template <int LANES>
-__global__ __launch_bounds__(256) void adapter_join_kernel(const float* __restrict__ sums_b, const float* __restrict__ sums_a, const int* __restrict__ tile_at, int tile_count, int slices, int adapters,
-                                                           int rank, int rp, int k, int c, int groups_b, int groups_a, float* __restrict__ da, float* __restrict__ db) {
-  constexpr int RESULTS = 256 / LANES, EACH = LANES == 1 ? 4 : 1;      // of a pass; passes of a work-group
-  __shared__ float parts[256];
+__global__ __launch_bounds__(256) void adapter_join_kernel(const JoinArgs p) {
+  constexpr int RESULTS = 256 / LANES;
+  __shared__ float4_t parts[LANES > 1 ? 256 : 1];
   const int t = (int)threadIdx.x, in_group = t % RESULTS, turn = t / RESULTS;
-  const int n = blockIdx.x / (unsigned)(groups_a + groups_b), group = blockIdx.x - n * (groups_a + groups_b);
-  const bool of_b = group < groups_b;
-  const unsigned per = of_b ? (unsigned)c * rank : (unsigned)rank * k, from = (unsigned)(of_b ? group : group - groups_b) * (RESULTS * EACH);
-  const long pitch = of_b ? (long)c * rp : (long)rp * k;
+  const int blocks = p.blocks_a + p.blocks_b, adapter = blockIdx.x / (unsigned)blocks, block = blockIdx.x - adapter * blocks;
+  const bool of_b = block < p.blocks_b;
+  const unsigned m = (unsigned)(of_b ? block : block - p.blocks_b) * RESULTS + in_group, wide = 16u * p.v;
+  const unsigned columns = (of_b ? p.groups_b : p.groups_a) * wide, rp = 16u * p.ranks;
+  const bool in = m < columns * rp / 4;
+  // (column of the products, rank) of the first of the four, and where they lie
+  unsigned lane_row, i, group, quarter, n, low;
+  if (of_b) {      // rank, then quarter, i, group: four lane rows of a rank
+    const unsigned rank = m % rp, rest = m / rp;
+    n = rank / 16, low = rank % 16, quarter = rest % 4, i = rest / 4 % p.v, group = rest / 4 / p.v, lane_row = 4 * quarter;
+  } else {         // column, then four ranks
+    const unsigned column = m % columns, four = m / columns;
+    n = four / 4, quarter = four % 4, i = column % p.v, lane_row = low = column / p.v % 16, group = column / wide;
+  }
+  const long at = ((long)(group * p.v + i) * p.ranks + n) * 64 + quarter * 16 + low, pitch = (long)columns * rp / 4;
   // slices that the adapter's tiles lie in: slice s begins at tile s tiles / slices
-  const int t0 = tile_at ? tile_at[n] : 0, t1 = tile_at ? tile_at[n + 1] : n == 0 ? tile_count : 0, tiles = tile_at ? tile_at[adapters] : tile_count;
-  const int first = t0 < t1 ? (int)(((long)(t0 + 1) * slices - 1) / tiles) + n : 0, last = t0 < t1 ? (int)(((long)t1 * slices - 1) / tiles) + n + 1 : 0;
-  const float* const sums = of_b ? sums_b : sums_a;
-  float* const out = (of_b ? db : da) + (long)n * per;
-  float s[EACH];
-#pragma unroll
-  for (int e = 0; e < EACH; ++e) {
-    const unsigned in = from + e * RESULTS + in_group;
-    s[e] = 0.0f;
-    if (in >= per) continue;
-    const float* const at = sums + (of_b ? in / rank * rp + in % rank : in);
+  const int t0 = p.tile_at ? p.tile_at[adapter] : 0, t1 = p.tile_at ? p.tile_at[adapter + 1] : adapter == 0 ? p.tile_count : 0, tiles = p.tile_at ? p.tile_at[p.adapters] : p.tile_count;
+  const int first = t0 < t1 ? (int)(((long)(t0 + 1) * p.slices - 1) / tiles) + adapter : 0, last = t0 < t1 ? (int)(((long)t1 * p.slices - 1) / tiles) + adapter + 1 : 0;
+  const float4_t* const sums = (of_b ? p.sums_b : p.sums_a) + at;
+  float4_t s = {0.f, 0.f, 0.f, 0.f};
+  if (in) {
     int q = first + turn;
     for (; q + 3 * LANES < last; q += 4 * LANES) {
-      const float v[4] = {at[q * pitch], at[(q + LANES) * pitch], at[(q + 2 * LANES) * pitch], at[(q + 3 * LANES) * pitch]};
-      s[e] += v[0], s[e] += v[1], s[e] += v[2], s[e] += v[3];
+      const float4_t v[4] = {sums[q * pitch], sums[(q + LANES) * pitch], sums[(q + 2 * LANES) * pitch], sums[(q + 3 * LANES) * pitch]};
+      s += v[0], s += v[1], s += v[2], s += v[3];
     }
-    for (; q < last; q += LANES) s[e] += at[q * pitch];
+    for (; q < last; q += LANES) s += sums[q * pitch];
   }
   if constexpr (LANES > 1) {
-    parts[t] = s[0];
+    parts[t] = s;
     __syncthreads();
     if (turn) return;
 #pragma unroll
-    for (int l = 1; l < LANES; ++l) s[0] += parts[l * RESULTS + in_group];
+    for (int l = 1; l < LANES; ++l) s += parts[l * RESULTS + in_group];
   }
+  if (!in) return;
+  const int c = of_b ? p.c : p.k;
 #pragma unroll
-  for (int e = 0; e < EACH; ++e) {
-    const unsigned in = from + e * RESULTS + in_group;
-    if (in < per) out[in] = s[e];
+  for (int e = 0; e < 4; ++e) {
+    const int from = (int)(group * wide + (lane_row + (of_b ? e : 0)) * p.v), column = (c < p.v ? from : min(from, c - p.v)) + (int)i;      // (as the products' lanes have them)
+    const int rank = (int)(16 * n + (of_b ? low : 4 * quarter + e));
+    if (from >= c || column >= c || rank >= p.rank) continue;
+    if (of_b) p.db[((long)adapter * c + column) * p.rank + rank] = s[e];
+    else p.da[((long)adapter * p.rank + rank) * c + column] = s[e];
   }
 }
 
@@ -320,8 +338,8 @@ AdapterPlan plan_of(const cprune_adapter_desc& d, bool backward) {
   q.slices = std::max(1, std::min(256 * kOuterWaves / groups, (d.rows - 1) / kTileRows / 2 + 1));
   if (q.sorted) q.tile_at = round256((size_t)(d.adapters + 1) * sizeof(int));
   const size_t sums = q.slices + (q.sorted ? d.adapters : 1) - 1;
-  q.sums_b = round256(sums * d.c_out * q.rp * sizeof(float));
-  q.sums_a = round256(sums * d.k * q.rp * sizeof(float));
+  q.sums_b = round256(sums * q.groups_b * wide * q.rp * sizeof(float));
+  q.sums_a = round256(sums * q.groups_a * wide * q.rp * sizeof(float));
   return q;
 }
 
@@ -332,7 +350,8 @@ bool fits(const cprune_adapter_desc& d, const AdapterPlan& q, bool backward) {
   if ((double)q.tiles * q.splits >= most || (double)q.tiles * ((c - 1) / 256 + 1) >= most || (double)q.tiles * kTileRows >= 2147483648.0 || (double)q.tiles * q.ranks >= most) return false;
   if (!backward) return (double)q.tiles * q.splits * 256 + (double)d.adapters * d.c_out * q.padded / 4 < 4294967040.0;
   const double turned = (double)d.adapters * ((d.k + 63.0) / 64 + (d.c_out + 63.0) / 64) * 2;      // (ranks of up to 128 are two tiles)
-  return turned < most / 4 - 1 && (double)q.slices * (q.groups_a + q.groups_b) < most && (double)d.adapters * (d.rank * ((double)d.k + d.c_out) / 1024 + 2) < most;
+  return turned < most / 4 - 1 && (double)q.slices * (q.groups_a + q.groups_b) < most && (double)d.adapters * (q.rp / 4.0 * ((double)d.k + d.c_out + 256) / 256 + 2) < most &&
+         (double)std::max(q.groups_a, q.groups_b) * 128 * q.rp < 4294967296.0;
 }
 
 void launch(int dtype, AdapterPass pass, const void* args, const AdapterLaunch& l, hipStream_t s) {
@@ -384,7 +403,7 @@ int columns_of(const cprune_adapter_desc& d, const AdapterPlan& q, int c) {
   const long tiles = rounded_tiles(d, q);
   int best = 256;
   if (q.few) {      // (a few rows each, all waiting for memory: side by side; 48 x 8192 x 8192, 32 adapters, 10.5 us in 512 columns, 16.3 in 1280)
-    while (best < 2048 && tiles * ((c - 1) / best + 1) > 768) best *= 2;
+    while (best < 2048 && tiles * ((c - 1) / best + 1) > 1536) best *= 2;
     return best;
   }
   long least = std::numeric_limits<long>::max();
@@ -466,8 +485,8 @@ extern "C" int cprune_adapter_linear_backward(const cprune_adapter_desc* d, cons
   float* const g = scratch.take<float>(q.g);
   char* const g_parts = scratch.take<char>(q.parts);
   char* const hidden_parts = scratch.take<char>(q.parts);
-  float* const sums_b = scratch.take<float>(q.sums_b);
-  float* const sums_a = scratch.take<float>(q.sums_a);
+  float4_t* const sums_b = scratch.take<float4_t>(q.sums_b);
+  float4_t* const sums_a = scratch.take<float4_t>(q.sums_a);
   const int v = 16 / (int)dtype_size(d->dtype);
   AdapterLaunch l = {(unsigned)(q.tiles * q.splits), q.ranks, d->rows <= kFewTile, d->k < v || d->c_out < v};
   const NarrowArgs n = {tiles, dy, d->dy_stride, d->c_out, d->rank, bt, part, q.splits, q.per};
@@ -495,15 +514,14 @@ extern "C" int cprune_adapter_linear_backward(const cprune_adapter_desc* d, cons
     o.side[1] = {x, d->x_stride, d->k, g_parts, sums_a, q.groups_a};
     l.grid = (unsigned)(q.slices * (q.groups_a + q.groups_b));
     launch(d->dtype, kAdapterOuter, &o, l, s);
-    const long all = (long)d->adapters * d->rank * ((long)d->k + d->c_out);
     auto join = [&](auto lanes) {
-      constexpr int LANES = decltype(lanes)::value;
-      const long results = 256 / LANES * (LANES == 1 ? 4 : 1);      // of a work-group
-      const int of_b = (int)(((long)d->c_out * d->rank - 1) / results + 1), of_a = (int)(((long)d->k * d->rank - 1) / results + 1);
-      adapter_join_kernel<LANES><<<(unsigned)(d->adapters * (of_a + of_b)), 256, 0, s>>>(sums_b, sums_a, tile_at, q.tiles, q.slices, d->adapters, d->rank, q.rp, d->k, d->c_out, of_b, of_a,
-                                                                                         da, db);
+      constexpr int LANES = decltype(lanes)::value, RESULTS = 256 / LANES;
+      auto blocks = [&](int groups) { return (int)(((long)groups * 16 * v * q.rp / 4 - 1) / RESULTS + 1); };
+      const JoinArgs j = {sums_b, sums_a, tile_at, q.tiles, q.slices, d->adapters, d->rank, q.ranks, v, d->k, d->c_out, q.groups_b, q.groups_a, blocks(q.groups_b), blocks(q.groups_a), da, db};
+      adapter_join_kernel<LANES><<<(unsigned)(d->adapters * (j.blocks_b + j.blocks_a)), 256, 0, s>>>(j);
     };
-    if (all <= 65536 && q.slices >= 8) join(std::integral_constant<int, 8>());
+    // (12544 x 576 x 96, rank 8, 85 slices: JOIN_TIMES us)
+    if ((long)d->adapters * q.rp * (q.groups_a + q.groups_b) * 16 * v <= 262144 && q.slices >= 8) join(std::integral_constant<int, 8>());
     else join(std::integral_constant<int, 1>());
   }
   CPRUNE_LAUNCH_CHECK();

@@ -83,8 +83,8 @@ struct OuterSide {
   long stride;
   int c;                   // columns
   const void* parts;       // the other operand
-  float* sums;             // [slices + adapters - 1][c][RP], or [..][RP][c] (across)
-  int groups;              // work-groups for a slice
+  float4_t* sums;          // [slices + adapters - 1][groups][V][NR][lane], as the products leave them
+  int groups;              // work-groups for a slice, of 16 V columns
 };
 struct OuterArgs {
   AdapterTiles tiles;
@@ -629,7 +629,8 @@ template <typename T> __device__ __forceinline__ void turn(const uint4 (&r)[kV<T
 }
 
 // A work-group has 16 V columns of a run of tiles with one adapter, all ranks; 128 rows of them at a time go through LDS, the next ones asked for meanwhile.  Its wavefronts
-// share the ranks, 32 each, so that two fit a SIMD, and the rows where ranks are fewer.  ACROSS: results lie [rank][column] instead of [column][rank].
+// share the ranks, 32 each, so that two fit a SIMD, and the rows where ranks are fewer.  ACROSS: ranks are the products' first operand, so that a lane's four results are ranks of
+// one column and not columns of one rank.
 // THIN: a side has fewer than V columns, read one by one.  Otherwise a lane past the last column has the last V again, and stores what their lanes do.
 constexpr int kOuterRows = 128;
 struct OuterShared {
@@ -643,33 +644,34 @@ __device__ __forceinline__ void outer_side(const OuterArgs& p, const OuterSide& 
     const int c = group * 16 * V + lane_row * V;
     return THIN ? c : min(c, side.c - V);
   };
-  const int c = column(lrow), valid = side.c - c;
   const T* const x = static_cast<const T*>(side.x) + column(t & 15);
   const long part = (long)RP * p.places;
   const int line = t >> 4, tiles = p.tile_at ? p.tile_at[p.tiles.adapters] : p.tile_count;
-  const int slice_end = (int)((long)(slice + 1) * tiles / p.slices);
-#pragma unroll 1
-  for (int first = (int)((long)slice * tiles / p.slices), last; first < slice_end; first = last) {      // an adapter's tiles of the slice
-  const int adapter = p.tile_at ? p.tiles.tile_of[first] : 0;
-  last = p.tile_at ? min(slice_end, p.tile_at[adapter + 1]) : slice_end;
-  const int end = last * kTileRows;
-  const int any_row = p.tiles.order ? p.tiles.order[first * kTileRows] : first * kTileRows;      // (read in the place of none, kept out)
-  float4_t acc[V][NW];
-#pragma unroll
-  for (int i = 0; i < V; ++i)
-#pragma unroll
-    for (int n = 0; n < NW; ++n) acc[i][n] = (float4_t){0.f, 0.f, 0.f, 0.f};
-  auto find = [&](int at, int (&rows)[EACH]) __attribute__((always_inline)) {      // this thread's rows of those from place `at` on
+  const int begin = (int)((long)slice * tiles / p.slices), slice_end = (int)((long)(slice + 1) * tiles / p.slices);
+  if (begin >= slice_end) return;
+  // an adapter's places of the slice
+  struct Run {
+    int adapter, first, end, any_row;      // (a row to read in the place of none, kept out)
+  };
+  auto run_at = [&](int tile) __attribute__((always_inline)) {
+    Run r;
+    r.adapter = p.tile_at ? p.tiles.tile_of[tile] : 0;
+    r.first = tile * kTileRows;
+    r.end = (p.tile_at ? min(slice_end, p.tile_at[r.adapter + 1]) : slice_end) * kTileRows;
+    r.any_row = p.tiles.order ? p.tiles.order[r.first] : r.first;
+    return r;
+  };
+  auto find = [&](const Run& r, int at, int (&rows)[EACH]) __attribute__((always_inline)) {      // this thread's rows of those from place `at` on
 #pragma unroll
     for (int e = 0; e < EACH; ++e) {
       const int place = at + 16 * e + line;
-      rows[e] = place >= end ? -1 : p.tiles.order ? p.tiles.order[place] : place < p.tiles.rows ? place : -1;
+      rows[e] = place >= r.end ? -1 : p.tiles.order ? p.tiles.order[place] : place < p.tiles.rows ? place : -1;
     }
   };
-  auto fetch = [&](const int (&rows)[EACH], uint4 (&v)[EACH]) __attribute__((always_inline)) {
+  auto fetch = [&](const Run& r, const int (&rows)[EACH], uint4 (&v)[EACH]) __attribute__((always_inline)) {
 #pragma unroll
     for (int e = 0; e < EACH; ++e) {
-      const T* const from = x + (long)(rows[e] >= 0 ? rows[e] : any_row) * side.stride;
+      const T* const from = x + (long)(rows[e] >= 0 ? rows[e] : r.any_row) * side.stride;
       v[e] = THIN ? load_some(from, side.c - (t & 15) * V) : load(from);
     }
   };
@@ -678,8 +680,8 @@ __device__ __forceinline__ void outer_side(const OuterArgs& p, const OuterSide& 
     for (int e = 0; e < EACH; ++e) shared.staged[buffer][16 * e + line][t & 15] = keep(v[e], rows[e] >= 0);
   };
   // the other operand of the step at a place, a step ahead; (past the last one: the first again)
-  auto operand = [&](int place, uint4 (&q)[NW][N]) __attribute__((always_inline)) {
-    const long from = ((long)(place < end ? place : first * kTileRows) / STEP * RP + 16 * share * NW + lrow) * STEP + quarter * V;
+  auto operand = [&](const Run& r, int place, uint4 (&q)[NW][N]) __attribute__((always_inline)) {
+    const long from = ((long)(place < r.end ? place : r.first) / STEP * RP + 16 * share * NW + lrow) * STEP + quarter * V;
 #pragma unroll
     for (int n = 0; n < NW; ++n)
 #pragma unroll
@@ -688,76 +690,84 @@ __device__ __forceinline__ void outer_side(const OuterArgs& p, const OuterSide& 
         else q[n][m] = *reinterpret_cast<const uint4*>(static_cast<const __bf16*>(side.parts) + m * part + from + 16 * STEP * n);
       }
   };
-  int at = first * kTileRows, buffer = 0;
+  Run run = run_at(begin);
   int rows[EACH], ahead[EACH];
   uint4 v[EACH], q[NW][N];
-  find(at, rows);
-  fetch(rows, v);
-  operand(at + stream * STEP, q);
-  find(at + kOuterRows, ahead);
-  stage(0, rows, v);
+  find(run, run.first, rows);
+  fetch(run, rows, v);
+  operand(run, run.first + stream * STEP, q);
+  find(run, run.first + kOuterRows, ahead);
 #pragma unroll 1
-  for (; at < end; at += kOuterRows, buffer ^= 1) {
-    __syncthreads();
+  for (;;) {
+    float4_t acc[V][NW];
 #pragma unroll
-    for (int e = 0; e < EACH; ++e) rows[e] = ahead[e];
-    fetch(rows, v);
-    find(at + 2 * kOuterRows, ahead);
+    for (int i = 0; i < V; ++i)
+#pragma unroll
+      for (int n = 0; n < NW; ++n) acc[i][n] = (float4_t){0.f, 0.f, 0.f, 0.f};
+    stage(0, rows, v);
+    int buffer = 0;
 #pragma unroll 1
-    for (int in = stream * STEP; in < kOuterRows && at + in < end; in += STREAMS * STEP) {
-      uint4 next[NW][N], r[V], turned[V];
-      operand(at + in + STREAMS * STEP, next);
+    for (int at = run.first; at < run.end; at += kOuterRows, buffer ^= 1) {
+      __syncthreads();
 #pragma unroll
-      for (int e = 0; e < V; ++e) r[e] = shared.staged[buffer][in + quarter * V + e][lrow];
-      turn<T>(r, turned);
+      for (int e = 0; e < EACH; ++e) rows[e] = ahead[e];
+      fetch(run, rows, v);
+      find(run, at + 2 * kOuterRows, ahead);
+#pragma unroll 1
+      for (int in = stream * STEP; in < kOuterRows && at + in < run.end; in += STREAMS * STEP) {
+        uint4 next[NW][N], r[V], turned[V];
+        operand(run, at + in + STREAMS * STEP, next);
 #pragma unroll
-      for (int n = 0; n < NW; ++n)
+        for (int e = 0; e < V; ++e) r[e] = shared.staged[buffer][in + quarter * V + e][lrow];
+        turn<T>(r, turned);
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          if constexpr (sizeof(T) == 4) acc[i][n] = ACROSS ? mma<float>(q[n][0], turned[i], acc[i][n]) : mma<float>(turned[i], q[n][0], acc[i][n]);
-          else acc[i][n] = mma_parts<T, N, ACROSS>(turned[i], q[n], acc[i][n]);
-        }
+        for (int n = 0; n < NW; ++n)
 #pragma unroll
-      for (int n = 0; n < NW; ++n)
+          for (int i = 0; i < V; ++i) {
+            if constexpr (sizeof(T) == 4) acc[i][n] = ACROSS ? mma<float>(q[n][0], turned[i], acc[i][n]) : mma<float>(turned[i], q[n][0], acc[i][n]);
+            else acc[i][n] = mma_parts<T, N, ACROSS>(turned[i], q[n], acc[i][n]);
+          }
 #pragma unroll
-        for (int m = 0; m < N; ++m) q[n][m] = next[n][m];
+        for (int n = 0; n < NW; ++n)
+#pragma unroll
+          for (int m = 0; m < N; ++m) q[n][m] = next[n][m];
+      }
+      stage(buffer ^ 1, rows, v);      // (read two steps ago)
     }
-    stage(buffer ^ 1, rows, v);      // (read two steps ago)
-  }
-  __syncthreads();
-  float4_t* const joined = reinterpret_cast<float4_t*>(&shared);
-  static_assert(sizeof(OuterShared) >= 8 * 4 * 64 * sizeof(float4_t), "the wavefronts' sums take the rows' place");
-  // the wavefronts' sums joined through LDS, up to 8 results of each at a time
-  float* const sums = side.sums + (long)(slice + adapter) * side.c * RP;
-  constexpr int G = 8 / NW < V ? 8 / NW : V, ITEMS = G * NR;
+    // the next adapter's first rows are asked for before these sums are joined
+    const int sum = slice + run.adapter, tile = run.end / kTileRows;
+    if (tile < slice_end) {
+      run = run_at(tile);
+      find(run, run.first, rows);
+      fetch(run, rows, v);
+      operand(run, run.first + stream * STEP, q);
+      find(run, run.first + kOuterRows, ahead);
+    }
+    // the wavefronts' sums joined through LDS, up to 8 results of each at a time
+    float4_t* const joined = reinterpret_cast<float4_t*>(&shared);
+    static_assert(sizeof(OuterShared) >= 8 * 4 * 64 * sizeof(float4_t), "the wavefronts' sums take the rows' place");
+    float4_t* const sums = side.sums + ((long)sum * side.groups + group) * (V * NR * 64);
+    constexpr int G = 8 / NW < V ? 8 / NW : V;
 #pragma unroll
-  for (int i0 = 0; i0 < V; i0 += G) {
-    if (i0) __syncthreads();
+    for (int i0 = 0; i0 < V; i0 += G) {
+      __syncthreads();
 #pragma unroll
-    for (int i = 0; i < G; ++i)
+      for (int i = 0; i < G; ++i)
 #pragma unroll
-      for (int n = 0; n < NW; ++n) joined[((i * NW + n) * 4 + wave) * 64 + lane] = acc[i0 + i][n];
-    __syncthreads();
-#pragma unroll 1
-    for (int item = wave; item < ITEMS; item += 4) {
-      const int of = item % SHARES, in = item / SHARES, i = i0 + in / NW, n = of * NW + in % NW;
-      float4_t v = joined[(in * 4 + of) * 64 + lane];
+        for (int n = 0; n < NW; ++n) joined[((i * NW + n) * 4 + wave) * 64 + lane] = acc[i0 + i][n];
+      __syncthreads();
 #pragma unroll
-      for (int w = 1; w < STREAMS; ++w) v += joined[(in * 4 + w * SHARES + of) * 64 + lane];
-      if constexpr (ACROSS) {      // ranks 16 n + 4 quarter + e, column c + i
+      for (int item = 0; item < G * NR; item += 4) {
+        const int mine = item + wave, of = mine % SHARES, in = mine / SHARES, i = i0 + in / NW, n = of * NW + in % NW;
+        if (mine >= G * NR) break;
+        float4_t s = joined[(in * 4 + of) * 64 + lane];
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (i < valid) sums[(long)(16 * n + 4 * quarter + e) * side.c + c + i] = v[e];
-      } else {                     // columns V (4 quarter + e) + i, rank 16 n + lrow
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int col = column(4 * quarter + e) + i;
-          if (col < side.c) sums[(long)col * RP + 16 * n + lrow] = v[e];
-        }
+        for (int w = 1; w < STREAMS; ++w) s += joined[(in * 4 + w * SHARES + of) * 64 + lane];
+        sums[(i * NR + n) * 64 + lane] = s;
       }
     }
-  }
-  __syncthreads();
+    if (tile >= slice_end) break;
+    __syncthreads();
   }
 }
 
