@@ -398,7 +398,8 @@ void prepare(const cprune_adapter_desc& d, const AdapterPlan& q, AdapterTiles& t
 // What does not stay in the last-level cache (256 MB, shared with what else is in use) is stored past it.
 bool past_caches(const cprune_adapter_desc& d, int c, const void* base) { return (base ? 2.0 : 1.0) * d.rows * c * dtype_size(d.dtype) > 134217728.0; }
 
-// Columns of a work-group: those that leave the busiest compute unit least to do, by the columns of its work-groups and what each does but once, some 150 columns' time.
+// Columns of a work-group: by what the busiest compute unit has to bring and by the rounds of work-groups, each with its columns' waits and what it does but once, some
+// 150 columns' time.
 int columns_of(const cprune_adapter_desc& d, const AdapterPlan& q, int c) {
   const long tiles = rounded_tiles(d, q);
   int best = 256;
@@ -408,7 +409,8 @@ int columns_of(const cprune_adapter_desc& d, const AdapterPlan& q, int c) {
   }
   long least = std::numeric_limits<long>::max();
   for (int columns = 256; columns <= 2048; columns += 256) {
-    const long cost = ((tiles * ((c - 1) / columns + 1) - 1) / 256 + 1) * (std::min(columns, c) + 150);
+    const long groups = tiles * ((c - 1) / columns + 1), each = std::min(columns, c);
+    const long cost = ((groups - 1) / 256 + 1) * each / 2 + ((groups - 1) / (256 * widen_waves(q.ranks, (int)dtype_size(d.dtype))) + 1) * (each + 150);
     if (cost < least) least = cost, best = columns;
   }
   return best;
