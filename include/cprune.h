@@ -4,7 +4,8 @@
  * batch-norm folding, MFMA implicit-GEMM convolution with fused bias,
  * residual and activation, the memory-bound layers around it, per-shape kernel
  * variant selection by timing on the device, and whole-network inference; beside them
- * a channels-last group norm with its gradient and products of 4-bit numbers.
+ * a channels-last group norm with its gradient, products of 4-bit numbers, the
+ * distillation loss of a network's answers and low-rank adapters, with gradients.
  *
  * Conventions for every call
  *   - Returns an int status: CPRUNE_OK (0) or a negative CPRUNE_ERR_* code.  On an
@@ -596,7 +597,7 @@ int cprune_top_logits(const void* z, int rows, int classes, int z_stride, int k,
  * A row without an entry, or without a label, goes without that term, and so does a term whose factor (1 - h or h) is 0; without both, with a dloss of 0, or
  * with every class masked its gradient is 0 whatever else it holds (and in the first and the last case its loss).  A listed class that the row masks makes the
  * loss infinite, not the gradient.  +infinity or NaN in z makes the row's loss and gradient NaN, in teacher the loss and the gradient of the listed classes.
- * cprune_distill_step: loss and gradient at once, z read once (rows of up to 131072 numbers of 16 bits or 65536 of 32).
+ * cprune_distill_step: loss and gradient at once, z read once (of each row 65536 numbers of 16 bits or 32768 of 32; what is past them twice).
  * ws         cprune_distill_workspace_bytes(d) of scratch for cprune_distill_loss and _step, 16-byte aligned; NULL where that is 0
  * temperature > 0, it, its square and its inverse finite; 0 <= hard <= 1; k >= 1; k <= 256 and rows < 2^22, more: CPRUNE_ERR_UNSUPPORTED, and a
  * workspace of 0. */
@@ -637,7 +638,8 @@ int cprune_distill_step(const cprune_distill_desc* d, const float* dloss, const 
  * dx_base    [rows][k] of dtype, rows base_stride apart, or NULL: what reaches x through the projection
  * dx         dense [rows][k] of dtype; it may be dx_base itself (dense)
  * da, db     fp32, as a and b; dx, or da and db together, may be NULL
- * Sums are in 32 bits, in a fixed order: repeated calls give identical bits.
+ * Sums are in 32 bits, in a fixed order: repeated calls give identical bits.  What a row holds that is not finite is its own y's and dx's, and its adapter's da's
+ * and db's, as infinities or NaN; a row without an adapter reaches neither.
  * rank <= 128, adapters <= 1024, more: CPRUNE_ERR_UNSUPPORTED, and a workspace of 0. */
 typedef struct {
   int32_t rows, k, c_out, rank, adapters;

@@ -255,9 +255,10 @@ __device__ __forceinline__ float4_t sum_parts(const float* from, int splits, lon
 
 // ---- narrow ----------------------------------------------------------------------
 
-// 256 bytes of every row at a time through LDS, two ahead of what is multiplied: asked for in whole lines, 16 lanes a row (as operands, 16 rows x 64 bytes, a compute
-// unit brings half as much: rank 32, 16384 x 4096 bf16 NARROW_TIMES us).  F: a tile's rows in sixteens, 4, or 1 where there are no more.  Rows that a
-// tile has not are its first one again: they make results of their own, which nobody reads.  Ranks past the last are the last again, left out by who reads them.
+// 256 bytes of every row at a time through LDS, two ahead of what is multiplied: asked for in whole lines, 16 lanes a row.  As operands, 16 rows x 64 bytes, a compute
+// unit brings half as much: 8192 x 4096 bf16 rank 64 took 31 us, now 23; 16384 x 4096 rank 32 took 42, now 39 (3.4 TB/s of x).  F: a tile's rows in sixteens, 4, or 1 where
+// there are no more.  Rows that a tile has not are its first one again: they make results of their own, which nobody reads.  Ranks past the last are the last
+// again, left out by who reads them.
 template <typename T, int NR, int F>
 __global__ __launch_bounds__(256, narrow_waves(NR)) void adapter_narrow_kernel(const NarrowArgs p) {
   constexpr int V = kV<T>, RP = 16 * NR, PIECES = 16, CHUNK = PIECES * V, PITCH = PIECES + 1, LINES = 16 * (F + NR);
@@ -720,10 +721,11 @@ __device__ __forceinline__ void outer_side(const OuterArgs& p, const OuterSide& 
 #pragma unroll
         for (int e = 0; e < V; ++e) r[e] = shared.staged[buffer][in + quarter * V + e][lrow];
         turn<T>(r, turned);
+        // (column by column, so that what an fp16 one is made into is used up before the next: rank by rank it spilled 74 registers; 8192 x 4096, rank 64: fp16 84 -> 71 us, bf16 49 -> 47 us)
 #pragma unroll
-        for (int n = 0; n < NW; ++n)
+        for (int i = 0; i < V; ++i)
 #pragma unroll
-          for (int i = 0; i < V; ++i) {
+          for (int n = 0; n < NW; ++n) {
             if constexpr (sizeof(T) == 4) acc[i][n] = ACROSS ? mma<float>(q[n][0], turned[i], acc[i][n]) : mma<float>(turned[i], q[n][0], acc[i][n]);
             else acc[i][n] = mma_parts<T, N, ACROSS>(turned[i], q[n], acc[i][n]);
           }

@@ -7,8 +7,8 @@
 // work-group.  All in 32 bits; the exponent's argument is (z - m) times log2(e) / T, a difference before the product, so that it is no less exact far from 0.
 //
 // Forms:
-//  - rows: a work-group has a row.  Where the gradient is wanted too the row stays in registers (131072 numbers of 16 bits, 65536 of 32) between its sums and
-//    its gradient: z is read once.  Longer ones are read again.
+//  - rows: a work-group has a row.  Where the gradient is wanted too the row stays in registers (65536 numbers of 16 bits, 32768 of 32) between its sums and
+//    its gradient: z is read once.  What is past them is read again.
 //  - parts: few long rows; work-groups leave the sums of a run of a row, and those of a second launch join them and take the gradient of their run.
 //  - the backward call has the sums already: the second launch alone.
 // Bound by memory.
@@ -82,7 +82,7 @@ __device__ __forceinline__ float wave_max(float v) {
 }
 
 // How the second exponential of a number, at temperature 1, is had beside the one at T: not wanted; by itself; where T is 2 or 4, the usual ones, as the first
-// one's square or fourth power (an exponential takes as long as four products: 4096 x 32768 fp16 TWO_TIMES us).
+// one's square or fourth power (an exponential takes as long as four products: 4096 x 32768 fp16 loss, temperature 2: 58.6 us with one of its own, 52.7 with the square).
 enum Second { kNone, kOwn, kSquare, kFourth };
 template <int TWO> __device__ __forceinline__ float second_of(float first, float d) {
   if constexpr (TWO == kSquare) return first * first;

@@ -1,0 +1,65 @@
+"""Top logits, the distillation loss and the adapters where rows are many, and two calls at once; bounds as in the tests of each."""
+import pytest
+import torch
+
+import test_gpu_adapter as adapter
+import test_gpu_distill as distill
+from paper_2207_01260_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+# (rows, k, c_out, rank, adapters): more rows than the sort's wavefronts keep, sixteen of them and (past 384 adapters) eight
+@pytest.mark.parametrize("order", ["one", "runs", "mixed"])
+@pytest.mark.parametrize("shape,dtype", [((40000, 24, 17, 5, 3), torch.float16), ((20000, 16, 16, 2, 700), torch.float32), ((17000, 72, 40, 9, 384), torch.bfloat16),
+                                         ((150001, 9, 8, 3, 2), torch.bfloat16)])
+def test_adapters(shape, dtype, order):
+    adapter.check(adapter.make(shape, dtype, order, seed=3))
+
+
+@pytest.mark.parametrize("dtype", adapter.TYPES)
+@pytest.mark.parametrize("rows", [5, 64, 65, 1000])
+def test_no_row_has_an_adapter(rows, dtype):
+    m = adapter.make((rows, 96, 50, 12, 4), dtype, "mixed", seed=4)
+    for nobody in (-1, 4, -2 ** 31, 2 ** 31 - 1):
+        m["which"].fill_(nobody)
+        w = (m["a"], m["b"], m["which"], m["scale"])
+        y, hidden = B.cprune_adapter_linear(m["x"], *w, m["base"], want_hidden=True)
+        assert torch.equal(y, m["base"]) and not hidden.any()
+        dx, da, db = B.cprune_adapter_linear_backward(m["dy"], m["x"], hidden, *w, m["dx_base"])
+        assert torch.equal(dx, m["dx_base"]) and not da.any() and not db.any()
+
+
+@pytest.mark.parametrize("rows,classes,k", [(70000, 3, 2), (66000, 40, 7)])
+@pytest.mark.parametrize("dtype", distill.TYPES)
+def test_top_and_loss(rows, classes, k, dtype):
+    m = distill.make(rows, classes, k, dtype, seed=5)
+    distill.check_top(m[0], k)
+    distill.check_all(*m, 2.0, 0.3)
+
+
+def test_two_calls_at_once():
+    """Streams beside each other, each with calls of its own: the answers are those of the calls alone."""
+    sets = [adapter.make((700, 800, 600, 20, 9), torch.bfloat16, "mixed", seed=s) for s in (6, 7)]
+    logits = [distill.make(2, 60000, 20, torch.float16, seed=s) for s in (8, 9)]
+
+    def work(m, l):
+        w = (m["a"], m["b"], m["which"], m["scale"])
+        y, hidden = B.cprune_adapter_linear(m["x"], *w, m["base"], want_hidden=True)
+        grads = B.cprune_adapter_linear_backward(m["dy"], m["x"], hidden, *w, m["dx_base"])
+        z, ids, teacher, labels, dloss = l
+        return (y, hidden) + grads + B.cprune_top_logits(z, 30) + B.cprune_distill_step(dloss, z, ids, teacher, labels, 2.0, 0.3)
+
+    alone = [work(m, l) for m, l in zip(sets, logits)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    got = [[], []]
+    for _ in range(10):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append(work(sets[i], logits[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for outs in got[i]:
+            for p, q in zip(outs, alone[i]):
+                assert torch.equal(p, q)
