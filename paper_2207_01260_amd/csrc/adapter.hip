@@ -395,9 +395,6 @@ void prepare(const cprune_adapter_desc& d, const AdapterPlan& q, AdapterTiles& t
   else adapter_prepare_kernel<unsigned short><<<grid, 64 * kSortWaves, lds, s>>>(sort, a, b, tiles_a);
 }
 
-// What does not stay in the last-level cache (256 MB, shared with what else is in use) is stored past it.
-bool past_caches(const cprune_adapter_desc& d, int c, const void* base) { return (base ? 2.0 : 1.0) * d.rows * c * dtype_size(d.dtype) > 134217728.0; }
-
 // Columns of a work-group: by what the busiest compute unit has to bring and by the rounds of work-groups, each with its columns' waits and what it does but once, some
 // 150 columns' time.
 int columns_of(const cprune_adapter_desc& d, const AdapterPlan& q, int c) {
@@ -455,7 +452,7 @@ extern "C" int cprune_adapter_linear(const cprune_adapter_desc* d, const void* x
   w.base = base, w.base_stride = d->base_stride, w.y = y, w.hidden = hidden;
   w.act = d->act;
   w.columns = columns_of(*d, q, d->c_out);
-  w.stream = past_caches(*d, d->c_out, base);
+  w.past = past_caches((double)d->rows * d->c_out * dtype_size(d->dtype));
   l.grid = (unsigned)(q.tiles * ((d->c_out - 1) / w.columns + 1));
   launch(d->dtype, kAdapterWiden, &w, l, s);
   CPRUNE_LAUNCH_CHECK();
@@ -500,11 +497,11 @@ extern "C" int cprune_adapter_linear_backward(const cprune_adapter_desc* d, cons
   l.grid = (unsigned)(q.tiles * q.ranks);
   launch(d->dtype, kAdapterParts, &r, l, s);
   if (dx) {
-      WidenArgs w = {};
+    WidenArgs w = {};
     w.tiles = tiles, w.part = g, w.splits = 1, w.rank = d->rank, w.b = at, w.c = d->k, w.b_stride = q.padded;
     w.base = dx_base, w.base_stride = d->base_stride, w.y = dx, w.act = CPRUNE_ACT_NONE;
     w.columns = columns_of(*d, q, d->k);
-    w.stream = past_caches(*d, d->k, dx_base);
+    w.past = past_caches((double)d->rows * d->k * dtype_size(d->dtype));
     l.grid = (unsigned)(q.tiles * ((d->k - 1) / w.columns + 1));
     launch(d->dtype, kAdapterWiden, &w, l, s);
   }

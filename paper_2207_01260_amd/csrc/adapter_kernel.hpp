@@ -16,6 +16,7 @@
 #include <type_traits>
 
 #include "conv_kernel.hpp"
+#include "past_caches.hpp"
 
 namespace cprune {
 
@@ -63,7 +64,7 @@ struct WidenArgs {
   float* hidden;           // [rows][rank] or null
   int act;
   int columns;             // of a work-group, a multiple of 128
-  bool stream;             // y is stored past the caches
+  bool past;               // y is stored past the caches
 };
 
 // hidden and g as the outer product's operands, by steps of its terms, places: 16-bit, three bf16 parts [3][places / 32][RP][32], fp32 [places / 16][RP][16]
@@ -536,8 +537,7 @@ __global__ __launch_bounds__(256, widen_waves(NR, sizeof(T))) void adapter_widen
         for (int e = 0; e < V; ++e) o[e] = Elem<T>::from_f32(v[e]);
         if (row >= 0 && whole) {
           outs* const to = reinterpret_cast<outs*>(y + (long)row * p.c + c);
-          if (p.stream) __builtin_nontemporal_store(o, to);
-          else *to = o;
+          CPRUNE_STORE(to, o, p.past);
         }
       }
       if (tail && c0 + 64 >= p.c) {      // the last columns, fewer than a vector

@@ -20,9 +20,11 @@ int vectors_of(const cprune_distill_desc& d) {
   return (d.classes - 1) / v + 1;
 }
 
-// Runs of a row for the launches that cut rows: a work-group of 256 has a vector or more for each thread.
+// Runs of a row for the launches that cut rows: a work-group of 256 has a vector or more for each thread.  Few rows, so that compute units would have none, and long ones,
+// so that a second launch costs less than it gains (bf16 steps, rows whole and cut: 8 x 16384 9.8 and 9.9 us, 8 x 32768 12.4 and 10.3, 64 x 131072 27.8 and 18.0, 127 x
+// 131072 29.4 and 23.3, 200 x 131072 32.4 and 33.6, 1 x 1000000 137 and 11.9).
 constexpr int kMostParts = 64;      // (joined by the lanes of a wavefront)
-bool by_parts(const cprune_distill_desc& d) { return d.rows < 128 && vectors_of(d) >= 1024; }
+bool by_parts(const cprune_distill_desc& d) { return d.rows < 128 && vectors_of(d) >= 4096; }
 void cut(const cprune_distill_desc& d, int runs, DistillArgs& a) {
   const int vectors = vectors_of(d);
   a.per = std::max(256, ((vectors - 1) / runs + 256) / 256 * 256);
@@ -36,8 +38,7 @@ DistillArgs args_of(const cprune_distill_desc& d, const void* z, const int32_t* 
   a.scale = (float)(1.4426950408889634 / d.temperature);
   a.soft = 1.0f - d.hard, a.hard = d.hard, a.t = d.temperature, a.inv_t = 1.0f / d.temperature;
   a.chunks = 1;
-  // (a gradient that does not stay in the last-level cache, 256 MB with what else is in use, leaves it to the rows that are read again)
-  a.stream = (double)d.rows * d.classes * dtype_size(d.dtype) > 134217728.0;
+  a.past = past_caches((double)d.rows * d.classes * dtype_size(d.dtype));
   return a;
 }
 
@@ -68,6 +69,7 @@ int forward(const cprune_distill_desc& d, DistillArgs a, void* ws, size_t ws_byt
     if (!a.dz) a.chunks = 1, l.grid = (unsigned)d.rows;
     launch(d.dtype, kDistillFinish, a, l, s);
   } else {
+    // the fewest threads that hold the row (16384 x 1000 fp32: 33 us with 64, 74 with 256; 2048 x 16384 bf16: 39 with 256, 60 with 512)
     l.grid = (unsigned)d.rows;
     if (vectors <= 256) l.threads = 64, l.held = a.dz ? 4 : 0;
     else if (!a.dz || vectors <= 2048) l.threads = 256, l.held = a.dz ? 8 : 0;

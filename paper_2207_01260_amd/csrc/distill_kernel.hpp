@@ -37,7 +37,7 @@ struct DistillArgs {
   float4* part;                 // [rows][parts]: m, the two sums
   int parts;
   int chunks, per;              // runs of a row, a work-group each; vectors of a run
-  bool stream;                  // dz is stored past the caches
+  bool past;                    // dz is stored past the caches
 };
 
 enum DistillPass { kDistillRows, kDistillParts, kDistillFinish };
@@ -354,7 +354,7 @@ __global__ __launch_bounds__(NT, NT == 512 ? 4 : 1) void distill_rows_kernel(con
     float x[V];
     logits::unpack<T>(r, x);
     g.over<TWO>(x, a.scale);
-    if (i < row.full) logits::store<T>(dz, i, x, a.stream);
+    if (i < row.full) logits::store<T>(dz, i, x, a.past);
   };
   if constexpr (NV != 0) {
 #pragma unroll
@@ -493,7 +493,7 @@ __global__ __launch_bounds__(NT) void distill_finish_kernel(const DistillArgs a)
       float x[V];
       logits::unpack<T>(r[u], x);
       g.over<TWO>(x, a.scale);
-      if (i + u * NT < end) logits::store<T>(dz, i + u * NT, x, a.stream);
+      if (i + u * NT < end) logits::store<T>(dz, i + u * NT, x, a.past);
       r[u] = next[u];
     }
   }

@@ -8,6 +8,7 @@
 #include <type_traits>
 
 #include "common.hpp"
+#include "past_caches.hpp"
 
 namespace cprune {
 namespace logits {
@@ -80,14 +81,14 @@ template <typename T> struct Row {
   }
 };
 
-template <typename T> __device__ __forceinline__ void store(T* p, int i, const float (&x)[Raw<T>::V], bool stream) {
+template <typename T> __device__ __forceinline__ void store(T* p, int i, const float (&x)[Raw<T>::V], bool past) {
   constexpr int V = Raw<T>::V;
   typedef T outs __attribute__((ext_vector_type(V), aligned(2)));
   outs v;
 #pragma unroll
   for (int j = 0; j < V; ++j) v[j] = (T)x[j];
-  if (stream) __builtin_nontemporal_store(v, reinterpret_cast<outs*>(p + (long)i * V));
-  else *reinterpret_cast<outs*>(p + (long)i * V) = v;
+  outs* const to = reinterpret_cast<outs*>(p + (long)i * V);
+  CPRUNE_STORE(to, v, past);
 }
 template <typename T> __device__ __forceinline__ void store_edge(T* p, const Row<T>& row, const float (&x)[Raw<T>::V]) {
 #pragma unroll

@@ -244,7 +244,9 @@ __global__ __launch_bounds__(NT) void top_kernel(const TopArgs a) {
   for (int i = n + t; i < a.k; i += NT) values[i] = (OUT)-__builtin_inff(), ids[i] = -1;
 }
 
-// Few long rows are cut into runs, each with its own list, and the lists are searched by a launch behind it.
+// Few very long rows are cut into runs, each with its own list, and the lists are searched by a launch behind it.  That pays where reading a row by one compute unit takes
+// longer than another launch, and for short lists: descending lists beside each other make the search's bound a loose one (one row in fp32, whole and cut: 131072
+// classes k 32 19 and 23 us, 300000 k 8 28 and 12, k 32 33 and 24, k 64 40 and 116; 64 rows of 300000 k 32 43 and 39, of 131072 25 and 30).
 struct TopPlan {
   int chunks, per;
   size_t values, ids;
@@ -253,7 +255,7 @@ struct TopPlan {
 TopPlan plan_top(int rows, int classes, int k, int dtype) {
   const int v = dtype == CPRUNE_F32 ? 4 : 8;
   TopPlan q = {1, classes, 0, 0};
-  if (rows <= 64 && classes >= 16384) {
+  if (rows <= 64 && k <= 32 && classes / v >= 65536) {
     q.per = 4096;
     while (q.per / v < 4 * k || (classes - 1) / q.per >= 64) q.per *= 2;
     q.chunks = (classes - 1) / q.per + 1;
@@ -270,7 +272,8 @@ TopPlan plan_top(int rows, int classes, int k, int dtype) {
 template <typename T, typename OUT> void launch_top(const TopArgs& a, int rows, hipStream_t s) {
   const unsigned grid = (unsigned)rows * a.chunks;
   const int vectors = (a.per + Raw<T>::V - 1) / Raw<T>::V;
-  // four threads or more for each of the k, if the row has them
+  // four threads or more for each of the k, if the row has them (16384 x 1000 fp32 k 8: 32 us with 64, 45 with 256; 2048 x 50257 bf16, 256 and 1024 threads: k 32 55 and 98
+  // us, k 64 66 and 104, k 128 106 and 120, 64 rows of k 112 35 and 27, k 256 1342 and 233)
   if (vectors <= 512 && (a.k <= 16 || vectors <= 64)) top_kernel<T, OUT, 64><<<grid, 64, 0, s>>>(a);
   else if (a.k <= 64 || vectors <= 256) top_kernel<T, OUT, 256><<<grid, 256, 0, s>>>(a);
   else top_kernel<T, OUT, 1024><<<grid, 1024, 0, s>>>(a);

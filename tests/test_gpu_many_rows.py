@@ -38,6 +38,30 @@ def test_top_and_loss(rows, classes, k, dtype):
     distill.check_all(*m, 2.0, 0.3)
 
 
+@pytest.mark.parametrize("rows,classes,k", [(2, 600001, 20), (64, 262145, 32), (1, 1200000, 33)])
+@pytest.mark.parametrize("dtype", distill.TYPES)
+def test_top_of_very_long_rows(rows, classes, k, dtype):
+    distill.check_top(distill.fill("ties" if rows == 2 else "", rows, classes, dtype, 7).cuda(), k)
+
+
+@pytest.mark.parametrize("dtype", distill.TYPES)
+def test_loss_of_a_very_long_row(dtype):
+    distill.check_all(*distill.make(1, 600001, 9, dtype, seed=6), 2.0, 0.3)
+
+
+@pytest.mark.parametrize("dtype,rows,classes", [(torch.float32, 900, 33333), (torch.bfloat16, 500, 131075)])
+def test_gradients_that_go_past_the_caches(dtype, rows, classes):
+    """More than 100 MB of them: as the formulas have them, and the first rows' bits are those of a call on these alone."""
+    z, ids, teacher, labels, dloss = distill.make(rows, classes, 8, dtype, seed=8)
+    _, dz = B.cprune_distill_step(dloss, z, ids, teacher, labels, 2.0, 0.3)
+    _, some = B.cprune_distill_step(dloss[:140], z[:140], ids[:140], teacher[:140], labels[:140], 2.0, 0.3)
+    assert torch.equal(dz[:140], some)
+    last = slice(rows - 5, rows)
+    _, _, want, bound = distill.loss64(z[last], ids[last], teacher[last], labels[last], 2.0, 0.3)
+    w, u = distill.wide64(dloss[last])[:, None], distill.U[dtype]
+    distill.near(dz[last], w * want, (abs(w) * bound + 2.0 ** -120) * (1 + u) + u * abs(w * want) + distill.TINY[dtype], "gradient")
+
+
 def test_two_calls_at_once():
     """Streams beside each other, each with calls of its own: the answers are those of the calls alone."""
     sets = [adapter.make((700, 800, 600, 20, 9), torch.bfloat16, "mixed", seed=s) for s in (6, 7)]
