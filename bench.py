@@ -72,7 +72,7 @@ def dominant_traffic(kernel, batch, layers):
 
 
 # sources of calls that no network makes; nothing else includes them
-APART = ("group_norm", "mx4")
+APART = ("group_norm", "mx4", "adapter", "distill", "logits", "past_caches", "top_logits")
 
 
 def kernel_source_hash(d=os.path.join(ROOT, "paper_2207_01260_amd", "csrc")):

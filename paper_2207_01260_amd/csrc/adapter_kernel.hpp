@@ -257,7 +257,8 @@ __device__ __forceinline__ float4_t sum_parts(const float* from, int splits, lon
 // ---- narrow ----------------------------------------------------------------------
 
 // 256 bytes of every row at a time through LDS, two ahead of what is multiplied: asked for in whole lines, 16 lanes a row.  As operands, 16 rows x 64 bytes, a compute
-// unit brings half as much: 8192 x 4096 bf16 rank 64 took 31 us, now 23; 16384 x 4096 rank 32 took 42, now 39 (3.4 TB/s of x).  F: a tile's rows in sixteens, 4, or 1 where
+// unit brings half as much: 8192 x 4096 bf16 rank 64 took 31 us, now 23; 16384 x 4096 rank 32 took 42, now 39 (3.4 TB/s of x; 28 where part of
+// x is still in the last-level cache).  F: a tile's rows in sixteens, 4, or 1 where
 // there are no more.  Rows that a tile has not are its first one again: they make results of their own, which nobody reads.  Ranks past the last are the last
 // again, left out by who reads them.
 template <typename T, int NR, int F>
@@ -372,6 +373,8 @@ __global__ __launch_bounds__(256, narrow_waves(NR)) void adapter_narrow_kernel(c
 
 // ---- widen -----------------------------------------------------------------------
 
+// A wavefront has 64 columns at a time of a tile's rows: B's numbers in registers, hidden in LDS as operands, results through LDS so that base and y are met in whole lines,
+// the next rows' base asked for as this one's is used.  Bound by base and y: 16384 x 11008, rank 32, bf16 147 us, 4.9 TB/s; 8192 x 4096, rank 64, 43 us.
 template <typename T, int NR, int F>
 __global__ __launch_bounds__(256, widen_waves(NR, sizeof(T))) void adapter_widen_kernel(const WidenArgs p) {
   constexpr int V = kV<T>, STEP = kStep<T>, RP = 16 * NR, NS = (RP + STEP - 1) / STEP, N = sizeof(T) == 4 ? 1 : 2, M = std::is_same<T, _Float16>::value ? 2 : 1;
