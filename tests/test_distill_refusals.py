@@ -25,9 +25,9 @@ def test_top_refuses_more_than_it_does():
     assert _top(k=257, classes=1000, stride=1000) == B.ERR_UNSUPPORTED
     assert _top(rows=1 << 22) == B.ERR_UNSUPPORTED
     assert L.cprune_top_logits_workspace_bytes(4, 1000, 257, 0) == L.cprune_top_logits_workspace_bytes(0, 1000, 5, 0) == 0
-    need = L.cprune_top_logits_workspace_bytes(2, 100000, 8, 1)
+    need = L.cprune_top_logits_workspace_bytes(2, 1000000, 8, 1)
     assert need > 0
-    long = dict(rows=2, classes=100000, stride=100000, k=8, dtype=1)
+    long = dict(rows=2, classes=1000000, stride=1000000, k=8, dtype=1)
     assert _top(ws=None, **long) == _top(size=need - 1, **long) == B.ERR_WORKSPACE
 
 
