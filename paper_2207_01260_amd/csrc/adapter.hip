@@ -226,9 +226,10 @@ __global__ __launch_bounds__(256) void adapter_join_kernel(const JoinArgs p) {
     n = four / 4, quarter = four % 4, i = column % p.v, lane_row = low = column / p.v % 16, group = column / wide;
   }
   const long at = ((long)(group * p.v + i) * p.ranks + n) * 64 + quarter * 16 + low, pitch = (long)columns * rp / 4;
-  // slices that the adapter's tiles lie in: slice s begins at tile s tiles / slices
+  // slices that the adapter's tiles lie in: slice s begins at tile s tiles / slices, and there are no more of them than tiles
   const int t0 = p.tile_at ? p.tile_at[adapter] : 0, t1 = p.tile_at ? p.tile_at[adapter + 1] : adapter == 0 ? p.tile_count : 0, tiles = p.tile_at ? p.tile_at[p.adapters] : p.tile_count;
-  const int first = t0 < t1 ? (int)(((long)(t0 + 1) * p.slices - 1) / tiles) + adapter : 0, last = t0 < t1 ? (int)(((long)t1 * p.slices - 1) / tiles) + adapter + 1 : 0;
+  const int slices = min(p.slices, tiles);
+  const int first = t0 < t1 ? (int)(((long)(t0 + 1) * slices - 1) / tiles) + adapter : 0, last = t0 < t1 ? (int)(((long)t1 * slices - 1) / tiles) + adapter + 1 : 0;
   const float4_t* const sums = (of_b ? p.sums_b : p.sums_a) + at;
   float4_t s = {0.f, 0.f, 0.f, 0.f};
   if (in) {

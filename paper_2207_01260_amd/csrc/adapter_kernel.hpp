@@ -93,7 +93,7 @@ struct OuterArgs {
   int rank, places;
   const int* tile_at;      // sorted: [adapters + 1], an adapter's first tile
   int tile_count;          // otherwise
-  int slices;              // that the tiles are cut into, whatever their adapters: what adapter i has of slice s is sum s + i
+  int slices;              // at most, that the tiles are cut into, whatever their adapters: what adapter i has of slice s is sum s + i
 };
 
 struct AdapterLaunch {
@@ -651,8 +651,10 @@ __device__ __forceinline__ void outer_side(const OuterArgs& p, const OuterSide& 
   const T* const x = static_cast<const T*>(side.x) + column(t & 15);
   const long part = (long)RP * p.places;
   const int line = t >> 4, tiles = p.tile_at ? p.tile_at[p.tiles.adapters] : p.tile_count;
-  const int begin = (int)((long)slice * tiles / p.slices), slice_end = (int)((long)(slice + 1) * tiles / p.slices);
-  if (begin >= slice_end) return;
+  // (no more slices than tiles, which rows without an adapter have none of: every slice has one, and leaves the sums that the join reads)
+  const int slices = min(p.slices, tiles);
+  if (slice >= slices) return;
+  const int begin = (int)((long)slice * tiles / slices), slice_end = (int)((long)(slice + 1) * tiles / slices);
   // an adapter's places of the slice
   struct Run {
     int adapter, first, end, any_row;      // (a row to read in the place of none, kept out)

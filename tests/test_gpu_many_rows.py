@@ -30,6 +30,43 @@ def test_no_row_has_an_adapter(rows, dtype):
         assert torch.equal(dx, m["dx_base"]) and not da.any() and not db.any()
 
 
+def poison():
+    """What the next calls take for their scratch and outputs holds NaN."""
+    torch.cuda.synchronize()
+    for size in (1 << 20, 1 << 23, 1 << 26, 1 << 28):
+        kept = [torch.full((size // 4,), float("nan"), device="cuda") for _ in range(4)]
+        small = [torch.full((n,), float("nan"), device="cuda") for n in (16, 128, 1000, 10000, 100000) for _ in range(8)]
+        del kept, small
+
+
+@pytest.mark.parametrize("dtype", adapter.TYPES)
+@pytest.mark.parametrize("rows,k,c_out,rank,with_one", [(8000, 40, 24, 8, 600), (8000, 40, 24, 40, 3), (5000, 200, 96, 5, 2000), (130, 30, 20, 4, 60), (4000, 64, 64, 16, 1)])
+def test_most_rows_have_no_adapter(rows, k, c_out, rank, with_one, dtype):
+    """Fewer tiles with an adapter than slices that the rows were cut into."""
+    m = adapter.make((rows, k, c_out, rank, 3), dtype, "mixed", seed=11)
+    g = torch.Generator().manual_seed(12)
+    some = torch.randperm(rows, generator=g)[:with_one].cuda()
+    which = torch.full_like(m["which"], -1)
+    which[some] = torch.randint(3, (with_one,), generator=g).int().cuda()
+    m["which"] = which
+    poison()
+    adapter.check(m)
+
+
+@pytest.mark.parametrize("dtype", adapter.TYPES)
+@pytest.mark.parametrize("shape,order", [((1, 96, 50, 12, 4), "mixed"), ((50, 700, 90, 7, 9), "mixed"), ((333, 129, 200, 33, 5), "mixed"), ((2000, 64, 48, 16, 6), "runs"),
+                                         ((700, 300, 40, 100, 1), "one")])
+def test_what_memory_held_before_is_not_read(shape, order, dtype):
+    m = adapter.make(shape, dtype, order, seed=13)
+    poison()
+    adapter.check(m)
+    for rows, classes, k in ((2, 300000, 20), (9, 1000, 8), (3, 40000, 70)):
+        args = distill.make(rows, classes, k, dtype, seed=14)
+        poison()
+        distill.check_top(args[0], min(k, 32))
+        distill.check_all(*args, 2.0, 0.3)
+
+
 @pytest.mark.parametrize("rows,classes,k", [(70000, 3, 2), (66000, 40, 7)])
 @pytest.mark.parametrize("dtype", distill.TYPES)
 def test_top_and_loss(rows, classes, k, dtype):
