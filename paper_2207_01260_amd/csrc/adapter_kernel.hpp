@@ -16,6 +16,7 @@
 #include <type_traits>
 
 #include "conv_kernel.hpp"
+#include "adapter_columns.hpp"
 #include "past_caches.hpp"
 
 namespace cprune {
@@ -644,11 +645,8 @@ template <typename T, int NR, bool ACROSS, bool THIN>
 __device__ __forceinline__ void outer_side(const OuterArgs& p, const OuterSide& side, int group, int slice, OuterShared& shared) {
   constexpr int V = kV<T>, STEP = kStep<T>, RP = 16 * NR, N = sizeof(T) == 4 ? 1 : 3, NW = NR < 2 ? NR : 2, SHARES = NR / NW, STREAMS = 4 / SHARES, EACH = kOuterRows / 16;
   const int t = (int)threadIdx.x, lane = t & 63, wave = t >> 6, quarter = lane >> 4, lrow = lane & 15, share = wave % SHARES, stream = wave / SHARES;
-  auto column = [&](int lane_row) __attribute__((always_inline)) {      // first of the V that lanes of a row number have
-    const int c = group * 16 * V + lane_row * V;
-    return THIN ? c : min(c, side.c - V);
-  };
-  const T* const x = static_cast<const T*>(side.x) + column(t & 15);
+  const OuterLane mine = outer_lane(side.c, V, group, t & 15, THIN);
+  const T* const x = static_cast<const T*>(side.x) + mine.column;
   const long part = (long)RP * p.places;
   const int line = t >> 4, tiles = p.tile_at ? p.tile_at[p.tiles.adapters] : p.tile_count;
   // (no more slices than tiles, which rows without an adapter have none of: every slice has one, and leaves the sums that the join reads)
@@ -678,7 +676,7 @@ __device__ __forceinline__ void outer_side(const OuterArgs& p, const OuterSide& 
 #pragma unroll
     for (int e = 0; e < EACH; ++e) {
       const T* const from = x + (long)(rows[e] >= 0 ? rows[e] : r.any_row) * side.stride;
-      v[e] = THIN ? load_some(from, side.c - (t & 15) * V) : load(from);
+      v[e] = THIN ? load_some(from, mine.there) : load(from);
     }
   };
   auto stage = [&](int buffer, const int (&rows)[EACH], const uint4 (&v)[EACH]) __attribute__((always_inline)) {
