@@ -251,9 +251,9 @@ __global__ __launch_bounds__(256) void adapter_join_kernel(const JoinArgs p) {
   const int c = of_b ? p.c : p.k;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const int from = (int)(group * wide + (lane_row + (of_b ? e : 0)) * p.v), column = (c < p.v ? from : min(from, c - p.v)) + (int)i;      // (as the products' lanes have them)
+    const int of = (int)(lane_row + (of_b ? e : 0)), column = outer_lane(c, p.v, (int)group, of).column + (int)i;
     const int rank = (int)(16 * n + (of_b ? low : 4 * quarter + e));
-    if (from >= c || column >= c || rank >= p.rank) continue;
+    if ((int)(group * wide) + of * p.v >= c || column >= c || rank >= p.rank) continue;
     if (of_b) p.db[((long)adapter * c + column) * p.rank + rank] = s[e];
     else p.da[((long)adapter * p.rank + rank) * c + column] = s[e];
   }

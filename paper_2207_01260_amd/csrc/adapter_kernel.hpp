@@ -636,7 +636,7 @@ template <typename T> __device__ __forceinline__ void turn(const uint4 (&r)[kV<T
 // A work-group has 16 V columns of a run of tiles with one adapter, all ranks; 128 rows of them at a time go through LDS, the next ones asked for meanwhile.  Its wavefronts
 // share the ranks, 32 each, so that two fit a SIMD, and the rows where ranks are fewer.  ACROSS: ranks are the products' first operand, so that a lane's four results are ranks of
 // one column and not columns of one rank.
-// THIN: a side has fewer than V columns, read one by one.  Otherwise a lane past the last column has the last V again, and stores what their lanes do.
+// THIN: a side has fewer than V columns, read one by one.  Which columns a lane has: adapter_columns.hpp.
 constexpr int kOuterRows = 128;
 struct OuterShared {
   uint4 staged[2][kOuterRows][16 + 1];
@@ -645,7 +645,7 @@ template <typename T, int NR, bool ACROSS, bool THIN>
 __device__ __forceinline__ void outer_side(const OuterArgs& p, const OuterSide& side, int group, int slice, OuterShared& shared) {
   constexpr int V = kV<T>, STEP = kStep<T>, RP = 16 * NR, N = sizeof(T) == 4 ? 1 : 3, NW = NR < 2 ? NR : 2, SHARES = NR / NW, STREAMS = 4 / SHARES, EACH = kOuterRows / 16;
   const int t = (int)threadIdx.x, lane = t & 63, wave = t >> 6, quarter = lane >> 4, lrow = lane & 15, share = wave % SHARES, stream = wave / SHARES;
-  const OuterLane mine = outer_lane(side.c, V, group, t & 15, THIN);
+  const OuterLane mine = outer_lane(side.c, V, group, t & 15);
   const T* const x = static_cast<const T*>(side.x) + mine.column;
   const long part = (long)RP * p.places;
   const int line = t >> 4, tiles = p.tile_at ? p.tile_at[p.tiles.adapters] : p.tile_count;
