@@ -380,7 +380,7 @@ template <typename T, int NR, int F>
 __global__ __launch_bounds__(256, widen_waves(NR, sizeof(T))) void adapter_widen_kernel(const WidenArgs p) {
   constexpr int V = kV<T>, STEP = kStep<T>, RP = 16 * NR, NS = (RP + STEP - 1) / STEP, N = sizeof(T) == 4 ? 1 : 2, M = std::is_same<T, _Float16>::value ? 2 : 1;
   __shared__ Tile tile;
-  __shared__ float results[4][F == 1 ? 1 : 2][16][64 + 4];
+  __shared__ alignas(16) float results[4][F == 1 ? 1 : 2][16][64 + 4];
   __shared__ uint4 hidden[16 * F][NS * N * 4 + 1];      // as operands: step, part, quarter
   const int t = (int)threadIdx.x, lane = t & 63, wave = t >> 6, quarter = lane >> 4, lrow = lane & 15;
   const int chunks = (p.c - 1) / p.columns + 1;
@@ -567,7 +567,7 @@ template <typename T, int NR>
 __global__ __launch_bounds__(256) void adapter_parts_kernel(const PartsArgs p) {
   constexpr int V = kV<T>, RP = 16 * NR, N = sizeof(T) == 4 ? 1 : 3;
   __shared__ Tile tile;
-  __shared__ float turned[2][16][kTileRows + 4];
+  __shared__ alignas(16) float turned[2][16][kTileRows + 4];
   const int t = (int)threadIdx.x, tile_no = blockIdx.x / NR, j0 = 16 * (blockIdx.x - tile_no * NR);
   int count;
   const int adapter = open_tile(p.tiles, tile_no, tile, count);

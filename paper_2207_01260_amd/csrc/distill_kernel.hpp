@@ -186,10 +186,10 @@ struct List {
   }
 };
 
-// What a class listed more than once has of p, and whether an entry is the first of its class; in LDS for as long as they are counted.
+// What a class listed more than once has of p, and whether an entry is the first of its class; in LDS for as long as they are counted, read four at a time.
 struct Shares {
-  int id[kMostList];
-  float p[kMostList];
+  alignas(16) int id[kMostList];
+  alignas(16) float p[kMostList];
   __device__ __forceinline__ void put(const List& l, int k) {
     const int lane = (int)threadIdx.x & 63;
 #pragma unroll
