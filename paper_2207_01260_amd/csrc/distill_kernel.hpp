@@ -4,7 +4,7 @@
 //   dz   = dloss ((1 - h) T (q_T - p) + h (q_1 - [label]))
 //
 // One pass over a row keeps its largest number m and the sums of exp((z - m) / T) and exp(z - m): a thread's, rescaled where its m grows, then joined over the
-// work-group.  All in 32 bits; the exponent's argument is (z - m) times log2(e) / T, a difference before the product, so that it is no less exact far from 0.
+// work-group.  All in 32 bits, a thread's in chains of 256 numbers at most, joined in another; the exponent's argument is (z - m) times log2(e) / T, a difference before the product, so that it is no less exact far from 0.
 //
 // Forms:
 //  - rows: a work-group has a row.  Where the gradient is wanted too the row stays in registers (65536 numbers of 16 bits, 32768 of 32) between its sums and
@@ -94,11 +94,20 @@ template <int TWO> __device__ __forceinline__ float second_of(float first, float
 // NaN) and the sums against it; TWO: at temperature 1 beside T.
 template <int TWO> struct Sums {
   float m = -FLT_MAX, at_t = 0.0f, at_1 = 0.0f;
+  float done_t = 0.0f, done_1 = 0.0f;      // of the numbers that are folded away
   __device__ __forceinline__ void rescale(float to, float scale) {
-    const float d = m - to;
-    at_t *= exp2_of(d * scale);
-    if constexpr (TWO != kNone) at_1 *= exp2_of(d * kLog2e);
+    const float d = m - to, by_t = exp2_of(d * scale);
+    at_t *= by_t, done_t *= by_t;
+    if constexpr (TWO != kNone) {
+      const float by_1 = exp2_of(d * kLog2e);
+      at_1 *= by_1, done_1 *= by_1;
+    }
     m = to;
+  }
+  // Behind every 256 numbers at most: a chain of n equal terms is off by up to n / 4 units of 2^-24 (131072 of one thread: 0.2%).
+  __device__ __forceinline__ void fold() {
+    done_t += at_t, at_t = 0.0f;
+    if constexpr (TWO != kNone) done_1 += at_1, at_1 = 0.0f;
   }
   template <int V> __device__ __forceinline__ void add(const float (&x)[V], float scale) {
     const float top = logits::largest(x);
@@ -113,8 +122,9 @@ template <int TWO> struct Sums {
   }
   __device__ __forceinline__ void over_wave(float scale) {
     rescale(wave_max(m), scale);
-    at_t = wave_sum(at_t);
-    if constexpr (TWO != kNone) at_1 = wave_sum(at_1);
+    fold();
+    at_t = wave_sum(done_t), done_t = 0.0f;
+    if constexpr (TWO != kNone) at_1 = wave_sum(done_1), done_1 = 0.0f;
   }
 };
 
@@ -303,6 +313,7 @@ __global__ __launch_bounds__(NT, NT == 512 ? 4 : 1) void distill_rows_kernel(con
   }
   constexpr int HELD = NV * NT, U = NV == 16 ? 4 : 8;
   if (NV == 0 || row.full > HELD) {
+    int since = 0;
 #pragma unroll 1
     for (int i = HELD + t; i - lane < row.full; i += U * NT) {      // (whole wavefronts)
       uint4 r[U];
@@ -314,6 +325,7 @@ __global__ __launch_bounds__(NT, NT == 512 ? 4 : 1) void distill_rows_kernel(con
         logits::unpack<T>(r[u], x);
         s.add(x, a.scale);
       }
+      if ((++since & (NV ? 3 : 256 / (U * V) - 1)) == 0) s.fold();      // (of 512 threads' rows 128 are held before the first)
     }
   }
   if (row.tail) s.add(edge, a.scale);
@@ -390,6 +402,7 @@ __global__ __launch_bounds__(256) void distill_parts_kernel(const DistillArgs a)
   const logits::Row<T> row(static_cast<const T*>(a.z) + row_no * a.z_stride, a.classes);
   const int end = min((chunk + 1) * a.per, row.full);
   Sums<TWO> s;
+  int since = 0;
 #pragma unroll 1
   for (int i = chunk * a.per + t; i - lane < end; i += 1024) {      // (whole wavefronts)
     uint4 r[4];
@@ -401,6 +414,7 @@ __global__ __launch_bounds__(256) void distill_parts_kernel(const DistillArgs a)
       logits::unpack<T>(r[u], x);
       s.add(x, a.scale);
     }
+    if ((++since & (64 / V - 1)) == 0) s.fold();
   }
   if (row.tail && chunk == a.chunks - 1) {
     float x[V];
