@@ -408,7 +408,7 @@ int columns_of(const cprune_adapter_desc& d, const AdapterPlan& q, int c) {
   long least = std::numeric_limits<long>::max();
   for (int columns = 256; columns <= 2048; columns += 256) {
     const long groups = tiles * ((c - 1) / columns + 1), each = std::min(columns, c);
-    const long cost = ((groups - 1) / 256 + 1) * each / 2 + ((groups - 1) / (256 * widen_waves(q.ranks, (int)dtype_size(d.dtype))) + 1) * (each + 150);
+    const long cost = ((groups - 1) / 256 + 1) * each / 2 + ((groups - 1) / (256 * widen_waves(q.ranks, (int)dtype_size(d.dtype), d.dtype == CPRUNE_F16)) + 1) * (each + 150);
     if (cost < least) least = cost, best = columns;
   }
   return best;

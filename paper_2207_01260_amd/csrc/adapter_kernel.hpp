@@ -10,8 +10,9 @@
 //  - widen: hidden against B (or g against A's transpose), 8 neighbouring results in each lane; bound by reading base and writing y.
 //  - outer: dy against hidden (x against g), summed over rows.  The terms are rows: a lane reads 16 bytes of V rows and turns the V x V numbers over in registers.
 //    Equal slices of the rows leave sums for each adapter that they meet, joined in a fixed order.  Bound by reading dy (x).
-// hidden and g are fp32; against 16-bit operands they go as bf16 parts, of 8 bits each: two for y and dx, whose own rounding is 2^-8 or 2^-11 (what is
-// left is under 2^-15 of a term), three for dA and dB in fp32, which are all of it.  An fp16 operand beside them is two bf16 parts itself, exactly.
+// hidden and g are fp32; against 16-bit operands they go as three bf16 parts, of 8 bits each, which are all of it.  An fp16 operand beside them is two bf16 parts itself,
+// exactly, so that every product is whole.  (Two parts for y and dx left out up to 2^-15 of a term, which is seen where terms cancel, and took as long up to rank 32, 1% less at
+// rank 64 in bf16, 8% in fp16.)
 #pragma once
 #include <type_traits>
 
@@ -24,8 +25,9 @@ namespace cprune {
 constexpr int kTileRows = 64, kFewTile = 16;
 
 // Work-groups of 256 that a compute unit holds at once, by registers; what is cut into work-groups is cut for whole rounds of them.
+// (widen in fp16 at rank 64 has B's parts besides: three spill 32 registers, and 16384 x 4096 x 11008 takes 290 us and not 242)
 constexpr int narrow_waves(int ranks) { return ranks <= 2 ? 3 : ranks <= 4 ? 2 : 1; }
-constexpr int widen_waves(int ranks, int size) { return ranks * size <= 8 ? 3 : ranks * size <= 16 ? 2 : 1; }
+constexpr int widen_waves(int ranks, int size, bool fp16) { return ranks * size <= (fp16 ? 4 : 8) ? 3 : ranks * size <= 16 ? 2 : 1; }
 constexpr int kOuterWaves = 2;
 
 // Places: tile t has rows order[64 t .. 64 t + 63], -1 where it has fewer.
@@ -187,7 +189,7 @@ template <typename T, int N, bool SWAP> __device__ __forceinline__ float4_t mma_
     uint4 h[2];
     halves_of(a, h);
 #pragma unroll
-    for (int n = N == 2 ? 1 : N - 2; n >= 0; --n) go(h[1], p[n]);      // (past three parts of one: 2^-22 of a term)
+    for (int n = N - 1; n >= 0; --n) go(h[1], p[n]);
 #pragma unroll
     for (int n = N - 1; n >= 0; --n) go(h[0], p[n]);
   } else {
@@ -377,10 +379,13 @@ __global__ __launch_bounds__(256, narrow_waves(NR)) void adapter_narrow_kernel(c
 // A wavefront has 64 columns at a time of a tile's rows: B's numbers in registers, hidden in LDS as operands, results through LDS so that base and y are met in whole lines,
 // the next rows' base asked for as this one's is used.  Bound by base and y: 16384 x 11008, rank 32, bf16 147 us, 4.9 TB/s; 8192 x 4096, rank 64, 43 us.
 template <typename T, int NR, int F>
-__global__ __launch_bounds__(256, widen_waves(NR, sizeof(T))) void adapter_widen_kernel(const WidenArgs p) {
-  constexpr int V = kV<T>, STEP = kStep<T>, RP = 16 * NR, NS = (RP + STEP - 1) / STEP, N = sizeof(T) == 4 ? 1 : 2, M = std::is_same<T, _Float16>::value ? 2 : 1;
+__global__ __launch_bounds__(256, (widen_waves(NR, sizeof(T), std::is_same<T, _Float16>::value))) void adapter_widen_kernel(const WidenArgs p) {
+  constexpr int V = kV<T>, STEP = kStep<T>, RP = 16 * NR, NS = (RP + STEP - 1) / STEP, N = sizeof(T) == 4 ? 1 : 3, M = std::is_same<T, _Float16>::value ? 2 : 1;
   __shared__ Tile tile;
-  __shared__ alignas(16) float results[4][F == 1 ? 1 : 2][16][64 + 4];
+  // Two buffers, the next rows multiplied while these are finished; one where hidden's parts and a second one leave room for fewer work-groups (8192 x 4096 x 4096 bf16, rank
+  // 64 87.6 us with two and 77.6 with one, rank 128 178 and 126).
+  constexpr int BUFS = F == 1 || (sizeof(T) == 2 && NR >= 4) ? 1 : 2;
+  __shared__ alignas(16) float results[4][BUFS][16][64 + 4];
   __shared__ uint4 hidden[16 * F][NS * N * 4 + 1];      // as operands: step, part, quarter
   const int t = (int)threadIdx.x, lane = t & 63, wave = t >> 6, quarter = lane >> 4, lrow = lane & 15;
   const int chunks = (p.c - 1) / p.columns + 1;
@@ -471,7 +476,7 @@ __global__ __launch_bounds__(256, widen_waves(NR, sizeof(T))) void adapter_widen
   };
   typedef T numbers __attribute__((ext_vector_type(V)));
   typedef T outs __attribute__((ext_vector_type(V), aligned(2)));
-  // Results go through LDS, 16 rows of a wavefront at a time, the next ones multiplied while these are finished
+  // Results go through LDS, 16 rows of a wavefront at a time
 #pragma unroll 1
   for (int c0 = begin; c0 < end; c0 += 64) {
     const int c = c0 + col;
@@ -487,7 +492,7 @@ __global__ __launch_bounds__(256, widen_waves(NR, sizeof(T))) void adapter_widen
       }
     if constexpr (AHEAD) weights(min(c0 + 64, end - 1), next);
     auto multiply = [&](int f) __attribute__((always_inline)) {
-      float (*const out)[64 + 4] = results[wave][F == 1 ? 0 : f & 1];
+      float (*const out)[64 + 4] = results[wave][f % BUFS];
       uint4 h[NS][N];
 #pragma unroll
       for (int s = 0; s < NS; ++s)
@@ -510,13 +515,20 @@ __global__ __launch_bounds__(256, widen_waves(NR, sizeof(T))) void adapter_widen
         *reinterpret_cast<float4_t*>(&out[lrow][16 * g + 4 * quarter]) = acc;
       }
     };
-    multiply(0);
-    wave_sync();
+    if constexpr (BUFS == 2) {
+      multiply(0);
+      wave_sync();
+    }
 #pragma unroll
     for (int f = 0; f < F; ++f) {
       if (f >= frags) break;
-      if (f + 1 < F && f + 1 < frags) multiply(f + 1);
-      const float (*const out)[64 + 4] = results[wave][F == 1 ? 0 : f & 1];
+      if constexpr (BUFS == 2) {
+        if (f + 1 < F && f + 1 < frags) multiply(f + 1);
+      } else {
+        multiply(f);
+        wave_sync();
+      }
+      const float (*const out)[64 + 4] = results[wave][f % BUFS];
 #pragma unroll
       for (int i = 0; i < EACH; ++i) {
         const int in = i * (64 / LINE) + line, row = tile.row[16 * f + in];
