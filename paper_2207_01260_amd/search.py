@@ -7,7 +7,8 @@ Accuracy on a dataset is not computed here (there is none): `accuracy` is a func
 supplies; the default accepts every candidate, which leaves the latency gate, the task order
 and the step rule as the things that decide.  With --recover a candidate is first brought back,
 for some steps, to what the search's first model answered (adapters beside its classifier in 4
-bits, from that model's largest logits), and judged by how many images it then answers alike.
+bits, from that model's largest logits), and judged by how many of the same images it then answers
+alike: there are no others, so this is what the tuning reaches, not what it would on new ones.
 
     python -m paper_2207_01260_amd.search [--net vgg16] [--batch 64] [--iterations 4] [--recover 0]
 """
@@ -184,7 +185,8 @@ class DeviceSearch:
         return self._state(model)["ms"]
 
     def accuracy(self, model) -> float:
-        """The share of the images that the model, its classifier in 4 bits and brought back for `recover` steps, answers as the first model asked about did."""
+        """The share of the images that the model, its classifier in 4 bits and brought back for `recover` steps, answers as the first model asked about did: the
+        images that the steps were on."""
         st = self._state(model)
         if self.teacher is None:
             self.teacher = B.cprune_top_logits(st["logits"], min(8, st["logits"].shape[1]))
@@ -230,7 +232,8 @@ def main():
     ap.add_argument("--batch", type=int, default=64)
     ap.add_argument("--iterations", type=int, default=4)
     ap.add_argument("--beta", type=float, default=0.98)
-    ap.add_argument("--recover", type=int, default=0, help="steps of bringing a candidate back before it is judged (0: every candidate is accepted)")
+    ap.add_argument("--recover", type=int, default=0, help="steps of bringing a candidate back before it is judged, by its answers to the images that the "
+                    "steps were on (0: every candidate is accepted)")
     args = ap.parse_args()
     ds, start, final, log = run(args.net, args.batch, iterations=args.iterations, beta=args.beta, recover=args.recover)
     table, order = ds.tune(start)
