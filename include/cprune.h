@@ -597,7 +597,8 @@ int cprune_top_logits(const void* z, int rows, int classes, int z_stride, int k,
  * A row without an entry, or without a label, goes without that term, and so does a term whose factor (1 - h or h) is 0; without both, with a dloss of 0, or
  * with every class masked its gradient is 0 whatever else it holds (and in the first and the last case its loss).  A listed class that the row masks makes the
  * loss infinite, not the gradient.  +infinity or NaN in z makes the row's loss and gradient NaN, in teacher the loss and the gradient of the listed classes.
- * cprune_distill_step: loss and gradient at once, z read once (of each row 65536 numbers of 16 bits or 32768 of 32; what is past them twice).
+ * cprune_distill_step: loss and gradient at once, z read once (of each row 65536 numbers of 16 bits or 32768 of 32; what is past them twice, and fewer than 128 rows of 32761
+ * classes of 16 bits, 16381 of 32, or more: all of them twice).
  * ws         cprune_distill_workspace_bytes(d) of scratch for cprune_distill_loss and _step, 16-byte aligned; NULL where that is 0
  * temperature > 0, it, its square and its inverse finite; 0 <= hard <= 1; k >= 1; k <= 256 and rows < 2^22, more: CPRUNE_ERR_UNSUPPORTED, and a
  * workspace of 0. */
