@@ -157,7 +157,10 @@ __global__ __launch_bounds__(NT) void top_kernel(const TopArgs a) {
   }
   __syncthreads();
   int n = count;
-  if (n > kList || owners > kRuns) {      // Many equal to the bound, as where most of a row has the type's lowest value: of those only the first k can count.
+  // Many equal to the bound, as where most of a row has the type's lowest value: of those only the first k can count.  The row is read again three times, or, where
+  // more than kList lie above the bound, some 35 times: 2048 x 50257 bf16, k 32 and 256, ordinary rows 46 and 219 us, one value throughout 142 and 259, mostly the lowest value 80 and
+  // 304, sorted rows 168 and 1310, 5000 NaN a row 1186 and 1220.
+  if (n > kList || owners > kRuns) {
     auto total = [&](int mine) __attribute__((always_inline)) {
 #pragma unroll
       for (int o = 32; o > 0; o >>= 1) mine += __shfl_xor(mine, o, 64);
@@ -273,10 +276,14 @@ TopPlan plan_top(int rows, int classes, int k, int dtype) {
 template <typename T, typename OUT> void launch_top(const TopArgs& a, int rows, hipStream_t s) {
   const unsigned grid = (unsigned)rows * a.chunks;
   const int vectors = (a.per + Raw<T>::V - 1) / Raw<T>::V;
-  // four threads or more for each of the k, if the row has them (16384 x 1000 fp32 k 8: 32 us with 64, 45 with 256; 2048 x 50257 bf16, 256 and 1024 threads: k 32 55 and 98
-  // us, k 64 66 and 104, k 128 106 and 120, 64 rows of k 112 35 and 27, k 256 1342 and 233)
+  // Four threads or more for each of the k, if the row has them, fewer where rows are many: a loose bound costs some rows' places, 1024 threads a row leave two rows to a
+  // compute unit.  16384 x 1000 fp32 k 8: 32 us with 64, 45 with 256.  bf16 with 256 and 1024:
+  //   2048 x 50257   k 32 55 and 98, k 64 66 and 104, k 72 65 and 104, k 100 78 and 109, k 128 113 and 118, k 160 167 and 129, k 256 1342 and 233
+  //   16384 x 4000   k 72 131 and 479, k 128 296 and 552      512 x 50257   k 72 28 and 32, k 128 65 and 40
+  //   512 x 10000    k 100 26 and 29                          256, 64 x 50257   k 100 31 and 26, 29 and 24
+  const int most = rows >= 2048 ? 128 : rows >= 512 ? 100 : 64;
   if (vectors <= 512 && (a.k <= 16 || vectors <= 64)) top_kernel<T, OUT, 64><<<grid, 64, 0, s>>>(a);
-  else if (a.k <= 64 || vectors <= 256) top_kernel<T, OUT, 256><<<grid, 256, 0, s>>>(a);
+  else if (a.k <= most || vectors <= 256) top_kernel<T, OUT, 256><<<grid, 256, 0, s>>>(a);
   else top_kernel<T, OUT, 1024><<<grid, 1024, 0, s>>>(a);
 }
 
