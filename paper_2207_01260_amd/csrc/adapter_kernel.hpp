@@ -377,7 +377,7 @@ __global__ __launch_bounds__(256, narrow_waves(NR)) void adapter_narrow_kernel(c
 // ---- widen -----------------------------------------------------------------------
 
 // A wavefront has 64 columns at a time of a tile's rows: B's numbers in registers, hidden in LDS as operands, results through LDS so that base and y are met in whole lines,
-// the next rows' base asked for as this one's is used.  Bound by base and y: 16384 x 11008, rank 32, bf16 147 us, 4.9 TB/s; 8192 x 4096, rank 64, 43 us.
+// the next rows' base asked for as this one's is used.  Bound by base and y: 16384 x 11008, rank 32, bf16 148 us, 4.9 TB/s; 8192 x 4096, rank 64, 44 us.
 template <typename T, int NR, int F>
 __global__ __launch_bounds__(256, (widen_waves(NR, sizeof(T), std::is_same<T, _Float16>::value))) void adapter_widen_kernel(const WidenArgs p) {
   constexpr int V = kV<T>, STEP = kStep<T>, RP = 16 * NR, NS = (RP + STEP - 1) / STEP, N = sizeof(T) == 4 ? 1 : 3, M = std::is_same<T, _Float16>::value ? 2 : 1;
@@ -736,7 +736,7 @@ __device__ __forceinline__ void outer_side(const OuterArgs& p, const OuterSide& 
 #pragma unroll
         for (int e = 0; e < V; ++e) r[e] = shared.staged[buffer][in + quarter * V + e][lrow];
         turn<T>(r, turned);
-        // (column by column, so that what an fp16 one is made into is used up before the next: rank by rank it spilled 74 registers; 8192 x 4096, rank 64: fp16 84 -> 71 us, bf16 49 -> 47 us)
+        // (column by column, so that what an fp16 one is made into is used up before the next: rank by rank it spilled 74 registers; 8192 x 4096, rank 64: fp16 84 -> 71 us with five products, 76 with all six, bf16 49 -> 47 us.  bf16 still spills 2 registers at rank 64 and 1 at 128)
 #pragma unroll
         for (int i = 0; i < V; ++i)
 #pragma unroll

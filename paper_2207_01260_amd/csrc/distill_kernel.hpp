@@ -82,7 +82,8 @@ __device__ __forceinline__ float wave_max(float v) {
 }
 
 // How the second exponential of a number, at temperature 1, is had beside the one at T: not wanted; by itself; where T is 2 or 4, the usual ones, as the first
-// one's square or fourth power (an exponential takes as long as four products: 4096 x 32768 fp16 loss, temperature 2: 58.6 us with one of its own, 52.7 with the square).
+// one's square or fourth power (an exponential takes as long as four products: 4096 x 32768 fp16 loss, temperature 2: 56.1 us with one of its own, 52.1 with the square).  The gradients' errors against 64
+// bits are the same within a tenth, fp32 at T = 4 4000 x 16000 2.71e-8 and 2.66e-8, 3000 x 1000 3.0e-8 and 2.8e-8: the rounding of the exponent's argument, which is most of it, is smaller by as much.
 enum Second { kNone, kOwn, kSquare, kFourth };
 template <int TWO> __device__ __forceinline__ float second_of(float first, float d) {
   if constexpr (TWO == kSquare) return first * first;
